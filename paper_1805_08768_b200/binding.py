@@ -7,6 +7,7 @@ is loaded on first use; if it is missing or cannot be loaded the call raises
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import List, Optional, Sequence, Tuple
@@ -29,6 +30,8 @@ EXPORTS = [
     "sbc_decode_workspace_bytes_batch", "sbc_decode_accumulate_batch", "sbc_decode_apply", "sbc_stream_bytes_values", "sbc_encode_values", "sbc_stream_bytes_sampled",
     "sbc_workspace_bytes_sampled", "sbc_encode_sampled", "sbc_decode_accumulate_sized", "sbc_decode_apply_sized",
     "sbc_debug_barrier_timeout",
+    "sbc_fp4_row_bytes", "sbc_fp4_scale_bytes", "sbc_fp4_workspace_bytes", "sbc_fp4_quantise", "sbc_fp4_dequantise",
+    "sbc_fp4_product",
 ]
 SIDE_VALUES = 2
 STATIC_WORKSPACE_BYTES = 8 << 20
@@ -63,6 +66,11 @@ class EncodeDiag(C.Structure):
 class TensorDesc(C.Structure):
     _fields_ = [("update", C.c_void_p), ("residual", C.c_void_p), ("numel", C.c_int64), ("p", C.c_double),
                 ("out_stream", C.c_void_p), ("out_capacity", C.c_size_t), ("out_mu", C.c_void_p)]
+
+
+class Fp4Desc(C.Structure):
+    _fields_ = [("values", C.c_void_p), ("scales", C.c_void_p), ("tensor_scale", C.c_void_p), ("rows", C.c_int64),
+                ("cols", C.c_int64), ("format", C.c_int32), ("reserved", C.c_int32)]
 
 
 class DecodeDesc(C.Structure):
@@ -149,6 +157,20 @@ def lib() -> C.CDLL:
         L.sbc_decode_apply_sized.restype = C.c_int
         L.sbc_decode_apply_sized.argtypes = [C.POINTER(C.c_void_p), C.POINTER(C.c_size_t), C.c_int, C.c_float,
                                              C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
+        L.sbc_fp4_row_bytes.restype = C.c_size_t
+        L.sbc_fp4_row_bytes.argtypes = [C.c_int64]
+        L.sbc_fp4_scale_bytes.restype = C.c_size_t
+        L.sbc_fp4_scale_bytes.argtypes = [C.c_int64, C.c_int64, C.c_int]
+        L.sbc_fp4_workspace_bytes.restype = C.c_size_t
+        L.sbc_fp4_workspace_bytes.argtypes = [C.c_int64, C.c_int64, C.c_int]
+        L.sbc_fp4_quantise.restype = C.c_int
+        L.sbc_fp4_quantise.argtypes = [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.POINTER(Fp4Desc),
+                                       C.POINTER(Fp4Desc), C.c_void_p, C.c_size_t, C.c_void_p]
+        L.sbc_fp4_dequantise.restype = C.c_int
+        L.sbc_fp4_dequantise.argtypes = [C.POINTER(Fp4Desc), C.c_void_p, C.c_int, C.c_int64, C.c_void_p]
+        L.sbc_fp4_product.restype = C.c_int
+        L.sbc_fp4_product.argtypes = [C.POINTER(Fp4Desc), C.POINTER(Fp4Desc), C.c_void_p, C.c_int, C.c_int64,
+                                      C.c_void_p, C.c_void_p]
         _lib = L
     return _lib
 
@@ -493,3 +515,141 @@ def sbc_encode_sampled(update: torch.Tensor, residual: torch.Tensor, p: float, s
                                     workspace.data_ptr(), workspace.numel(), _cuda_stream(stream))
     _check(code, "sbc_encode_sampled")
     return out_stream, out_mu
+
+
+# ---- language-model operators (include/sbc_lm.h) -----------------------------------
+
+DTYPE_CODES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+FP4_FORMATS = {"e8m0": 0, "e4m3": 1}   # block scales: powers of two for 32 elements, 8-bit floats for 16
+
+
+def _matrix(t: torch.Tensor, name: str) -> None:
+    if not (t.is_cuda and t.dim() == 2 and t.dtype in DTYPE_CODES):
+        raise TypeError(f"{name} must be a float32, bfloat16 or float16 CUDA matrix")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError(f"{name}: rows must not overlap")
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _fresh(stream):
+    """Context in which new buffers belong to the stream that the work is enqueued on."""
+    if stream is None:
+        return contextlib.nullcontext()
+    s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_cuda_stream(stream))
+    return torch.cuda.stream(s)
+
+
+class Fp4Tensor:
+    """A matrix (rows x cols) in 4-bit floating point with a scale per block; the layout is the C
+    header's.  ``values`` uint8 [rows, row bytes], ``scales`` uint8 (flat), ``tensor_scale`` float32 [1];
+    ``format`` is "e8m0" or "e4m3"."""
+
+    __slots__ = ("values", "scales", "tensor_scale", "rows", "cols", "format", "desc")
+
+    def __init__(self, values: torch.Tensor, scales: torch.Tensor, tensor_scale: torch.Tensor, rows: int, cols: int,
+                 format: str):
+        if format not in FP4_FORMATS:
+            raise ValueError(f"unknown 4-bit format {format!r}")
+        row_bytes = int(lib().sbc_fp4_row_bytes(cols))
+        scale_bytes = int(lib().sbc_fp4_scale_bytes(rows, cols, FP4_FORMATS[format]))
+        for t, name, n in ((values, "values", rows * row_bytes), (scales, "scales", scale_bytes)):
+            if not (t.is_cuda and t.dtype == torch.uint8 and t.is_contiguous()):
+                raise TypeError(f"{name} must be a contiguous uint8 CUDA tensor")
+            if n == 0 or t.numel() != n:
+                raise ValueError(f"{name}: {n} bytes needed for {rows} x {cols}, got {t.numel()}")
+        _dev_f32(tensor_scale, "tensor_scale")
+        if tensor_scale.numel() < 1:
+            raise ValueError("tensor_scale must hold one value")
+        self._set(values, scales, tensor_scale, rows, cols, format)
+
+    def _set(self, values, scales, tensor_scale, rows, cols, format):
+        self.values, self.scales, self.tensor_scale = values, scales, tensor_scale
+        self.rows, self.cols, self.format = rows, cols, format
+        self.desc = Fp4Desc(values.data_ptr(), scales.data_ptr(), tensor_scale.data_ptr(), rows, cols,
+                            FP4_FORMATS[format], 0)
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, format: str, device) -> "Fp4Tensor":
+        """Room for a rows x cols matrix, contents undefined."""
+        if format not in FP4_FORMATS:
+            raise ValueError(f"unknown 4-bit format {format!r}")
+        if rows < 1 or cols < 1:
+            raise ValueError("an Fp4Tensor has at least one row and one column")
+        row_bytes = (cols + 31) // 32 * 16
+        scale_bytes = int(lib().sbc_fp4_scale_bytes(rows, cols, FP4_FORMATS[format]))
+        room = torch.empty(rows * row_bytes + scale_bytes + 16, dtype=torch.uint8, device=device)
+        self = cls.__new__(cls)
+        self._set(room[:rows * row_bytes].view(rows, row_bytes), room[rows * row_bytes:-16],
+                  room[-16:-12].view(torch.float32), rows, cols, format)
+        return self
+
+    @property
+    def nbytes(self) -> int:
+        return self.values.numel() + self.scales.numel() + 4
+
+
+def _quantise(x, format, along_rows, along_cols, stream):
+    _matrix(x, "x")
+    if format not in FP4_FORMATS:
+        raise ValueError(f"unknown 4-bit format {format!r}")
+    rows, cols = x.shape
+    with _fresh(stream):
+        q = Fp4Tensor.empty(rows, cols, format, x.device) if along_rows else None
+        q_t = Fp4Tensor.empty(cols, rows, format, x.device) if along_cols else None
+        ws = torch.empty(int(lib().sbc_fp4_workspace_bytes(rows, cols, FP4_FORMATS[format])), dtype=torch.uint8,
+                         device=x.device)
+    code = lib().sbc_fp4_quantise(x.data_ptr(), DTYPE_CODES[x.dtype], rows, cols, _row_stride(x),
+                                  C.byref(q.desc) if q is not None else None,
+                                  C.byref(q_t.desc) if q_t is not None else None, ws.data_ptr(), ws.numel(),
+                                  _cuda_stream(stream))
+    _check(code, "sbc_fp4_quantise")
+    return q, q_t
+
+
+def sbc_fp4_quantise(x: torch.Tensor, format: str = "e8m0", transposed: bool = False, stream=None) -> Fp4Tensor:
+    """x (rows x cols) in 4 bits, blocks along its rows; with ``transposed`` its transpose (cols x rows),
+    blocks down the columns of x."""
+    return _quantise(x, format, not transposed, transposed, stream)[1 if transposed else 0]
+
+
+def sbc_fp4_quantise_both(x: torch.Tensor, format: str = "e8m0", stream=None) -> Tuple[Fp4Tensor, Fp4Tensor]:
+    """(x in 4 bits along its rows, its transpose in 4 bits), x read once: what a forward and a
+    backward product contract."""
+    return _quantise(x, format, True, True, stream)
+
+
+def sbc_fp4_dequantise(q: Fp4Tensor, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None,
+                       stream=None) -> torch.Tensor:
+    """The values that q stands for (rows x cols)."""
+    if out is None:
+        with _fresh(stream):
+            out = torch.empty(q.rows, q.cols, dtype=dtype, device=q.values.device)
+    _matrix(out, "out")
+    if tuple(out.shape) != (q.rows, q.cols):
+        raise ValueError(f"out must be {q.rows} x {q.cols}")
+    _check(lib().sbc_fp4_dequantise(C.byref(q.desc), out.data_ptr(), DTYPE_CODES[out.dtype], _row_stride(out),
+                                    _cuda_stream(stream)), "sbc_fp4_dequantise")
+    return out
+
+
+def sbc_fp4_product(a: Fp4Tensor, b: Fp4Tensor, dtype: torch.dtype = torch.bfloat16,
+                    out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """a b^T (a.rows x b.rows): tokens times weights, both in 4 bits, sums in 32 bits."""
+    if a.format != b.format or a.cols != b.cols:
+        raise ValueError(f"operands differ: {a.cols} columns of {a.format}, {b.cols} of {b.format}")
+    if out is None:
+        with _fresh(stream):
+            out = torch.empty(a.rows, b.rows, dtype=dtype, device=a.values.device)
+    _matrix(out, "out")
+    if tuple(out.shape) != (a.rows, b.rows):
+        raise ValueError(f"out must be {a.rows} x {b.rows}")
+    _check(lib().sbc_fp4_product(C.byref(a.desc), C.byref(b.desc), out.data_ptr(), DTYPE_CODES[out.dtype],
+                                 _row_stride(out), status.data_ptr() if status is not None else None,
+                                 _cuda_stream(stream)), "sbc_fp4_product")
+    return out

@@ -1,0 +1,243 @@
+// C entry points of the language-model operators (include/sbc_lm.h).
+#include <algorithm>
+
+#include "lm_common.cuh"
+#include "lm_product.cuh"
+#include "lm_quantise.cuh"
+
+using namespace sbclm;
+
+namespace {
+
+constexpr int64_t kMaxDim = 0x7fffffff;
+
+int width_of(int dtype) { return dtype == SBC_F32 ? 4 : (dtype == SBC_BF16 || dtype == SBC_F16) ? 2 : 0; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+int sm_count() {
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0)
+        return 148;
+    return n;
+}
+
+// What every row of a matrix starts at a multiple of, at most 16 bytes.
+int row_align(const void* p, int64_t stride, int width) {
+    const uintptr_t bits = (uintptr_t)p | (uintptr_t)(stride * width) | 16u;
+    return (int)(bits & (~bits + 1));
+}
+
+// A matrix argument: base, type and stride fit together.
+bool matrix_ok(const void* p, int dtype, int64_t rows, int64_t cols, int64_t stride) {
+    const int width = width_of(dtype);
+    return p && width && aligned(p, (uintptr_t)width) && rows >= 0 && rows <= kMaxDim && cols >= 1 && cols <= kMaxDim && stride >= cols &&
+           stride <= (int64_t)1 << 40;
+}
+
+int64_t ktiles_of(int64_t cols, int format) { return ceil_div(cols, format == SBC_FP4_E8M0 ? 128 : 64); }
+
+bool fp4_ok(const sbc_fp4* q) {
+    return q && q->values && q->scales && q->tensor_scale && aligned(q->values, 16) && aligned(q->scales, 16) &&
+           aligned(q->tensor_scale, 4) && q->rows >= 1 && q->rows <= kMaxDim && q->cols >= 1 && q->cols <= kMaxDim && q->reserved == 0 &&
+           (q->format == SBC_FP4_E8M0 || q->format == SBC_FP4_E4M3);
+}
+
+// dtype -> element type
+template <typename F> int by_dtype(int dtype, F f) {
+    switch (dtype) {
+        case SBC_F32: return f((float*)nullptr);
+        case SBC_BF16: return f((__nv_bfloat16*)nullptr);
+        case SBC_F16: return f((__half*)nullptr);
+    }
+    return SBC_EINVAL;
+}
+
+int launched() { return cudaGetLastError() == cudaSuccess ? SBC_OK : SBC_ECUDA; }
+
+template <typename T, int FMT> void launch_quantise(const QuantiseArgs& a, bool rows, bool cols, unsigned grid, cudaStream_t st) {
+    if (rows && cols)
+        k_fp4_quantise<T, FMT, true, true><<<grid, kQThreads, 0, st>>>(a);
+    else if (rows)
+        k_fp4_quantise<T, FMT, true, false><<<grid, kQThreads, 0, st>>>(a);
+    else
+        k_fp4_quantise<T, FMT, false, true><<<grid, kQThreads, 0, st>>>(a);
+}
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled() {
+    static const EncodeTiled fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return (EncodeTiled)p;
+    }();
+    return fn;
+}
+
+// Boxes of 128 bytes x `rows` of the elements' bytes, in the swizzle that the tensor cores read.
+bool values_map(CUtensorMap* map, const sbc_fp4* q, int rows) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)sbc_fp4_row_bytes(q->cols), (cuuint64_t)q->rows};
+    const cuuint64_t strides[1] = {dims[0]};
+    const cuuint32_t box[2] = {kPBytes, (cuuint32_t)rows}, ones[2] = {1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, q->values, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr int kSmemMost = 227 * 1024;
+
+template <typename T, int FMT>
+int launch_product(const CUtensorMap& mw, const CUtensorMap& mx, const ProductArgs& a, dim3 grid, int smem, cudaStream_t st) {
+    if (cudaFuncSetAttribute(k_fp4_product<T, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - 1024) != cudaSuccess)
+        return SBC_ECUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(kPThreads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 1;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = grid.z;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, k_fp4_product<T, FMT>, mw, mx, a) == cudaSuccess ? SBC_OK : SBC_ECUDA;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t sbc_fp4_row_bytes(int64_t cols) { return cols >= 1 && cols <= kMaxDim ? (size_t)(ceil_div(cols, 32) * 16) : 0; }
+
+size_t sbc_fp4_scale_bytes(int64_t rows, int64_t cols, int format) {
+    if (rows < 1 || rows > kMaxDim || cols < 1 || cols > kMaxDim || (format != SBC_FP4_E8M0 && format != SBC_FP4_E4M3)) return 0;
+    return (size_t)(ceil_div(rows, 128) * ktiles_of(cols, format) * 512);
+}
+
+size_t sbc_fp4_workspace_bytes(int64_t rows, int64_t cols, int format) {
+    return sbc_fp4_scale_bytes(rows, cols, format) ? 256 : 0;
+}
+
+int sbc_fp4_quantise(const void* x, int dtype, int64_t rows, int64_t cols, int64_t row_stride, const sbc_fp4* along_rows,
+                     const sbc_fp4* along_cols, void* workspace, size_t workspace_bytes, sbc_cuda_stream_t stream) {
+    if (!matrix_ok(x, dtype, rows, cols, row_stride) || rows < 1 || (!along_rows && !along_cols)) return SBC_EINVAL;
+    if (along_rows && (!fp4_ok(along_rows) || along_rows->rows != rows || along_rows->cols != cols)) return SBC_EINVAL;
+    if (along_cols && (!fp4_ok(along_cols) || along_cols->rows != cols || along_cols->cols != rows)) return SBC_EINVAL;
+    const int format = along_rows ? along_rows->format : along_cols->format;
+    if (along_rows && along_cols && along_cols->format != format) return SBC_EINVAL;
+    if (!workspace || !aligned(workspace, 16)) return SBC_EINVAL;
+    if (workspace_bytes < sbc_fp4_workspace_bytes(rows, cols, format)) return SBC_ECAPACITY;
+    const int64_t row_tiles = ceil_div(rows, kQTile), col_tiles = ceil_div(cols, kQTile);
+    if (row_tiles > kMaxDim / col_tiles) return SBC_EINVAL;
+
+    QuantiseArgs a = {};
+    a.x = x;
+    a.rows = rows;
+    a.cols = cols;
+    a.stride = row_stride;
+    a.align = row_align(x, row_stride, width_of(dtype));
+    a.col_tiles = (uint32_t)col_tiles;
+    a.amax = static_cast<const uint32_t*>(workspace);
+    if (along_rows) {
+        a.tensor_r = along_rows->tensor_scale;
+        a.values_r = static_cast<uint8_t*>(along_rows->values);
+        a.scales_r = static_cast<uint8_t*>(along_rows->scales);
+        a.pitch_r = (long long)sbc_fp4_row_bytes(cols);
+        a.ktiles_r = ktiles_of(cols, format);
+    }
+    if (along_cols) {
+        a.tensor_c = along_cols->tensor_scale;
+        a.values_c = static_cast<uint8_t*>(along_cols->values);
+        a.scales_c = static_cast<uint8_t*>(along_cols->scales);
+        a.pitch_c = (long long)sbc_fp4_row_bytes(rows);
+        a.ktiles_c = ktiles_of(rows, format);
+    }
+    return by_dtype(dtype, [&](auto* as) {
+        using T = std::remove_pointer_t<decltype(as)>;
+        cudaStream_t st = stream;
+        if (format == SBC_FP4_E4M3) {
+            if (cudaMemsetAsync(workspace, 0, 4, st) != cudaSuccess) return (int)SBC_ECUDA;
+            const int64_t blocks = std::min<int64_t>(ceil_div(rows * ceil_div(cols, 8), kQThreads), sm_count() * 8);
+            k_fp4_amax<T><<<(unsigned)blocks, kQThreads, 0, st>>>(a, static_cast<uint32_t*>(workspace));
+            launch_quantise<T, SBC_FP4_E4M3>(a, along_rows, along_cols, (unsigned)(row_tiles * col_tiles), st);
+        } else {
+            launch_quantise<T, SBC_FP4_E8M0>(a, along_rows, along_cols, (unsigned)(row_tiles * col_tiles), st);
+        }
+        return launched();
+    });
+}
+
+int sbc_fp4_dequantise(const sbc_fp4* q, void* out, int dtype, int64_t row_stride, sbc_cuda_stream_t stream) {
+    if (!fp4_ok(q) || !matrix_ok(out, dtype, q->rows, q->cols, row_stride)) return SBC_EINVAL;
+    DequantiseArgs a = {};
+    a.values = static_cast<const uint8_t*>(q->values);
+    a.scales = static_cast<const uint8_t*>(q->scales);
+    a.tensor = q->tensor_scale;
+    a.out = out;
+    a.rows = q->rows;
+    a.cols = q->cols;
+    a.stride = row_stride;
+    a.pitch = (long long)sbc_fp4_row_bytes(q->cols);
+    a.ktiles = ktiles_of(q->cols, q->format);
+    a.align = row_align(out, row_stride, width_of(dtype));
+    const int64_t blocks = std::min<int64_t>(ceil_div(q->rows * ceil_div(q->cols, 8), kQThreads), sm_count() * 16);
+    return by_dtype(dtype, [&](auto* as) {
+        using T = std::remove_pointer_t<decltype(as)>;
+        if (q->format == SBC_FP4_E4M3)
+            k_fp4_dequantise<T, SBC_FP4_E4M3><<<(unsigned)blocks, kQThreads, 0, stream>>>(a);
+        else
+            k_fp4_dequantise<T, SBC_FP4_E8M0><<<(unsigned)blocks, kQThreads, 0, stream>>>(a);
+        return launched();
+    });
+}
+
+int sbc_fp4_product(const sbc_fp4* a, const sbc_fp4* b, void* out, int dtype, int64_t row_stride, uint32_t* status,
+                    sbc_cuda_stream_t stream) {
+    if (!fp4_ok(a) || !fp4_ok(b) || a->format != b->format || a->cols != b->cols) return SBC_EINVAL;
+    if (!matrix_ok(out, dtype, a->rows, b->rows, row_stride) || !aligned(status, 4)) return SBC_EINVAL;
+    ProductArgs p = {};
+    p.scales_w = static_cast<const uint8_t*>(b->scales);
+    p.scales_x = static_cast<const uint8_t*>(a->scales);
+    p.tensor_w = b->tensor_scale;
+    p.tensor_x = a->tensor_scale;
+    p.out = out;
+    p.status = status;
+    p.rows_w = b->rows;
+    p.rows_x = a->rows;
+    p.stride = row_stride;
+    p.ktiles = ktiles_of(a->cols, a->format);
+    p.chunks = (int)ceil_div(a->cols, 256);
+    p.steps = (int)ceil_div(a->cols, 64);
+    p.nt = a->rows >= 256 ? 256 : (int)ceil_div(a->rows, 16) * 16;
+    const int row_tiles = (p.nt + 127) / 128, tiles_k = a->format == SBC_FP4_E8M0 ? 2 : 4;
+    const int stage = (kPRows * kPBytes + p.nt * kPBytes + tiles_k * 512 * (1 + row_tiles) + 1023) / 1024 * 1024;
+    p.stages = p.nt > 128 ? 4 : std::min(4, 110 * 1024 / stage);
+    const int cols = (p.nt + 31) / 32 * 32 + p.stages * 4 * tiles_k * (1 + row_tiles);
+    p.tmem_cols = 32;
+    while ((int)p.tmem_cols < cols) p.tmem_cols *= 2;
+    // as many blocks on an SM as its tensor memory serves, so that none waits for another's columns
+    const int smem = std::max(p.stages * stage + 1024, kSmemMost / (512 / (int)p.tmem_cols + 1) + 1024);
+    const int64_t tiles_w = ceil_div(b->rows, kPRows), tiles_x = ceil_div(a->rows, p.nt);
+    if (tiles_x > 65535) return SBC_EINVAL;
+    int parts = 1;
+    while (parts < 8 && tiles_w * tiles_x * parts * 2 <= 2 * sm_count() && p.chunks >= parts * 2) parts *= 2;
+    CUtensorMap mw, mx;
+    if (!values_map(&mw, b, kPRows) || !values_map(&mx, a, p.nt)) return SBC_ECUDA;
+    const dim3 grid((unsigned)tiles_w, (unsigned)tiles_x, (unsigned)parts);
+    return by_dtype(dtype, [&](auto* as) {
+        using T = std::remove_pointer_t<decltype(as)>;
+        return a->format == SBC_FP4_E4M3 ? launch_product<T, SBC_FP4_E4M3>(mw, mx, p, grid, smem, stream)
+                                         : launch_product<T, SBC_FP4_E8M0>(mw, mx, p, grid, smem, stream);
+    });
+}
+
+}  // extern "C"

@@ -1,0 +1,136 @@
+// Shared pieces of the language-model operators (sm_100a): element types, row access at any
+// alignment, barriers and bulk copies.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/sbc_lm.h"
+
+namespace sbclm {
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
+
+// Eight consecutive elements in registers.
+template <typename T> union Pack8 {
+    T e[8];
+    uint32_t w[2 * sizeof(T)];
+    uint2 d[sizeof(T)];
+    uint4 q[sizeof(T) / 2];
+};
+
+// Loads `have` (1..8) elements, zeros behind them; `align` is what every such address is a
+// multiple of (uniform over the launch), so one branch picks the widest load it allows.
+template <typename T> __device__ __forceinline__ void load8(Pack8<T>& v, const T* p, int have, int align) {
+    if (have >= 8 && align >= 16) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) v.q[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+    } else if (have >= 8 && align >= 8) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T); ++i) v.d[i] = __ldg(reinterpret_cast<const uint2*>(p) + i);
+    } else if (have >= 8 && align >= 4) {
+#pragma unroll
+        for (int i = 0; i < 2 * (int)sizeof(T); ++i) v.w[i] = __ldg(reinterpret_cast<const uint32_t*>(p) + i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v.e[i] = i < have ? p[i] : from_float<T>(0.f);
+    }
+}
+
+template <typename T> __device__ __forceinline__ void store8(T* p, const Pack8<T>& v, int have, int align) {
+    if (have >= 8 && align >= 16) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(p)[i] = v.q[i];
+    } else if (have >= 8 && align >= 8) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T); ++i) reinterpret_cast<uint2*>(p)[i] = v.d[i];
+    } else if (have >= 8 && align >= 4) {
+#pragma unroll
+        for (int i = 0; i < 2 * (int)sizeof(T); ++i) reinterpret_cast<uint32_t*>(p)[i] = v.w[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < have) p[i] = v.e[i];
+    }
+}
+
+// ---- shared-memory barriers and bulk copies ------------------------------------
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+// Waits for the phase of the given parity; gives up after a bounded number of tries (each of
+// which the hardware may suspend for a while), far beyond what any copy or product takes.
+constexpr uint32_t kWaitTries = 1u << 21;
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
+    for (uint32_t i = 0; i < kWaitTries; ++i)
+        if (mbar_try(bar, parity)) return true;
+    return false;
+}
+
+// Box of a 2-D byte matrix into shared memory; x is the byte within the row (a multiple of 16).
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+}
+// A run of bytes (both addresses and the size multiples of 16).
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+                 "r"(bytes), "r"(bar)
+                 : "memory");
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Address of `local` (a shared-memory address of this block) in block `rank` of the cluster.
+__device__ __forceinline__ uint32_t map_rank(uint32_t local, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float ld_cluster(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+}  // namespace sbclm

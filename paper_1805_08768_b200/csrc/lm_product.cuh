@@ -1,0 +1,232 @@
+// out = A B^T for two matrices in 4-bit floating point, on the tensor cores' block-scaled form.
+//
+// The weights' rows are the accumulator's 128 lanes and the tokens its columns, so one shape serves
+// one token and thousands: a tile is 128 weights x `nt` tokens, nt a multiple of 16 up to 256.  A
+// stage holds 256 elements (128 bytes, one swizzle line) of every row of both sides and their block
+// scales, which are copied to tensor memory as the tiles they are stored in.  With few tokens there
+// are few tiles, so a cluster of blocks shares a tile: each takes a run of stages, and the partial
+// accumulators are added in a fixed order through distributed shared memory.
+#pragma once
+
+#include "lm_common.cuh"
+
+namespace sbclm {
+
+constexpr int kPThreads = 192;      // four warps for the accumulator, one that loads, one that multiplies
+constexpr int kPRows = 128;         // weights per tile
+constexpr int kPBytes = 128;        // bytes of a row per stage: 256 elements
+constexpr int kPMaxStages = 8;
+
+struct ProductArgs {
+    const uint8_t *scales_w, *scales_x;
+    const float *tensor_w, *tensor_x;
+    void* out;
+    uint32_t* status;
+    long long rows_w, rows_x, stride;
+    long long ktiles;    // scale tiles per 128 rows
+    int chunks;          // stages' worth of columns
+    int steps;           // 64-element products over all columns
+    int nt;              // tokens per tile
+    int stages;
+    uint32_t tmem_cols;  // allocated columns (a power of two)
+};
+
+template <int FMT> struct ProductShape {
+    static constexpr int kTiles = FMT == SBC_FP4_E8M0 ? 2 : 4;  // scale tiles per stage and 128 rows
+    static constexpr uint32_t kIdesc =                            // 4-bit operands, both K-major, 128 lanes
+        (1u << 7) | (1u << 10) | (FMT == SBC_FP4_E8M0 ? 1u << 23 : 0u) | (1u << 27);
+};
+
+__device__ __forceinline__ uint64_t operand_desc(uint32_t smem) {  // 128-byte swizzle, 8 rows of 128 bytes per group
+    return (uint64_t)((smem & 0x3ffff) >> 4) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ uint64_t scale_desc(uint32_t smem) {    // no swizzle, 8 rows of 16 bytes per group
+    return (uint64_t)((smem & 0x3ffff) >> 4) | (1ull << 16) | ((uint64_t)(128 >> 4) << 32) | (1ull << 46);
+}
+
+__device__ __forceinline__ void scales_to_tmem(uint32_t tmem, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+template <int FMT>
+__device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t add) {
+    if (FMT == SBC_FP4_E8M0)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(add)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(add)
+            : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_load16(float* v, uint32_t addr) {
+    uint32_t* u = reinterpret_cast<uint32_t*>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]),
+          "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
+        : "r"(addr)
+        : "memory");
+}
+
+// grid (weight tiles, token tiles, blocks per tile), a cluster along z.
+template <typename T, int FMT>
+__global__ void __launch_bounds__(kPThreads) k_fp4_product(const __grid_constant__ CUtensorMap map_w,
+                                                           const __grid_constant__ CUtensorMap map_x, ProductArgs a) {
+    using S = ProductShape<FMT>;
+    extern __shared__ uint8_t raw[];
+    __shared__ uint64_t bars[2 * kPMaxStages + 1];
+    __shared__ uint32_t tmem_slot, gave_up;
+    const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+    const uint32_t smem = (smem_u32(raw) + 1023u) & ~1023u;
+    const int row_tiles = (a.nt + 127) / 128;                      // 128-row scale tiles on the token side
+    const uint32_t bytes_w = kPRows * kPBytes, bytes_x = (uint32_t)a.nt * kPBytes;
+    const uint32_t bytes_x_room = (bytes_x + 1023u) & ~1023u;
+    const uint32_t bytes_sc = S::kTiles * 512u;                    // one 128-row tile's scales
+    const uint32_t stage_bytes = bytes_w + bytes_x_room + bytes_sc * (1 + row_tiles);
+    const uint32_t stage_room = (stage_bytes + 1023u) & ~1023u;
+    const uint32_t bar0 = smem_u32(bars), done = bar0 + 16 * kPMaxStages;
+    const int rank = (int)blockIdx.z, parts = (int)gridDim.z;
+    const int first = (int)((long long)a.chunks * rank / parts), last = (int)((long long)a.chunks * (rank + 1) / parts);
+    const long long w0 = (long long)blockIdx.x * kPRows, x0 = (long long)blockIdx.y * a.nt;
+
+    if (t == 0) {
+        gave_up = 0;
+        for (int s = 0; s < a.stages; ++s) {
+            mbar_init(bar0 + 16 * s, 1);
+            mbar_init(bar0 + 16 * s + 8, 1);
+        }
+        mbar_init(done, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 5) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(a.tmem_cols)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = tmem_slot;
+    const uint32_t acc_cols = (uint32_t)(a.nt + 31) & ~31u;
+    const uint32_t sc_cols = 4u * S::kTiles * (1 + row_tiles);     // scale columns per stage
+
+    if (warp == 4 && lane == 0) {
+        int issued = first;
+        bool ok = true;
+        for (int c = first; c < last && ok; ++c) {
+            const int i = c - first, s = i % a.stages;
+            const uint32_t full = bar0 + 16 * s, empty = full + 8;
+            ok = mbar_wait(empty, ((i / a.stages) & 1) ^ 1);
+            if (!ok) break;
+            const long long k0 = (long long)c * S::kTiles;
+            const uint32_t sc = (uint32_t)min((long long)S::kTiles, a.ktiles - k0) * 512u;
+            const uint32_t at = smem + (uint32_t)s * stage_room, at_x = at + bytes_w, at_sc = at_x + bytes_x_room;
+            // a token tile's last 128 rows may lie beyond the scales' last tile
+            const int x_tiles = (int)min((long long)row_tiles, (a.rows_x + 127) / 128 - x0 / 128);
+            mbar_expect(full, bytes_w + bytes_x + sc * (1 + x_tiles));
+            tma_load_2d(at, &map_w, c * kPBytes, (int)w0, full);
+            tma_load_2d(at_x, &map_x, c * kPBytes, (int)x0, full);
+            bulk_load(at_sc, a.scales_w + (w0 / 128 * a.ktiles + k0) * 512, sc, full);
+            for (int j = 0; j < x_tiles; ++j)
+                bulk_load(at_sc + bytes_sc * (1 + j), a.scales_x + ((x0 / 128 + j) * a.ktiles + k0) * 512, sc, full);
+            issued = c + 1;
+        }
+        if (!ok) gave_up = 1;
+        // no copy may be in flight when the block ends
+        for (int c = max(first, issued - a.stages); c < issued; ++c)
+            mbar_wait(bar0 + 16 * ((c - first) % a.stages), ((c - first) / a.stages) & 1);
+    } else if (warp == 5 && lane == 0) {
+        bool ok = true;
+        const uint32_t idesc = S::kIdesc | ((uint32_t)(a.nt >> 3) << 17);
+        for (int c = first; c < last; ++c) {
+            const int i = c - first, s = i % a.stages;
+            const uint32_t full = bar0 + 16 * s, empty = full + 8;
+            ok = mbar_wait(full, (i / a.stages) & 1);
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t at = smem + (uint32_t)s * stage_room, at_x = at + bytes_w, at_sc = at_x + bytes_x_room;
+            const uint32_t sf_w = tmem + acc_cols + (uint32_t)s * sc_cols, sf_x = sf_w + 4 * S::kTiles;
+            const int steps = min(4, a.steps - c * 4);
+            // scales: a step's tiles of 128 rows stand in neighbouring columns
+#pragma unroll
+            for (int k = 0; k < S::kTiles; ++k) {
+                if (k * (4 / S::kTiles) >= steps) break;
+                scales_to_tmem(sf_w + 4 * k, scale_desc(at_sc + 512 * k));
+                for (int j = 0; j < row_tiles; ++j)
+                    scales_to_tmem(sf_x + 4 * (k * row_tiles + j), scale_desc(at_sc + bytes_sc * (1 + j) + 512 * k));
+            }
+            for (int k = 0; k < steps; ++k) {
+                // E8M0: two steps share a scale tile, each takes its half of every word
+                const int tile = FMT == SBC_FP4_E8M0 ? k / 2 : k;
+                const uint32_t half = FMT == SBC_FP4_E8M0 ? (uint32_t)(k & 1) * 2u : 0u;
+                multiply<FMT>(tmem, operand_desc(at + 32 * k), operand_desc(at_x + 32 * k), idesc | (half << 4) | (half << 29),
+                              sf_w + 4 * tile, sf_x + 4 * tile * row_tiles, (uint32_t)(i > 0 || k > 0));
+            }
+            commit(empty);
+        }
+        commit(done);
+        if (!ok) gave_up = 1;
+    }
+    __syncwarp();
+    // every block of a cluster has at least one chunk, so `done` always means a whole partial sum
+    const bool finished = mbar_wait(done, 0);
+    if (!finished) gave_up = 1;
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    __syncthreads();
+    const bool bad = gave_up != 0;
+    if (bad && t == 0 && a.status) atomicOr(a.status, SBC_STATUS_TIMEOUT);
+    const float nan = __uint_as_float(0x7fffffffu);
+    T* out = static_cast<T*>(a.out);
+    const float scale = FMT == SBC_FP4_E4M3 ? *a.tensor_w * *a.tensor_x : 1.f;
+    const int tokens = (int)min((long long)a.nt, a.rows_x - x0);
+    const long long j = w0 + warp * 32 + lane;
+    if (parts == 1) {
+        if (warp < 4) {
+            for (int n0 = 0; n0 < tokens; n0 += 16) {
+                float v[16];
+                tmem_load16(v, tmem + ((uint32_t)warp << 21) + n0);
+                if (j < a.rows_w) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (n0 + i < tokens) out[(x0 + n0 + i) * a.stride + j] = from_float<T>(bad ? nan : v[i] * scale);
+                }
+            }
+        }
+    } else {
+        // partial sums, one row of 128 lanes per token, over the stages that nothing uses any more
+        if (warp < 4) {
+            for (int n0 = 0; n0 < tokens; n0 += 16) {
+                float v[16];
+                tmem_load16(v, tmem + ((uint32_t)warp << 21) + n0);
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (n0 + i < tokens)
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(smem + (uint32_t)((n0 + i) * 128 + warp * 32 + lane) * 4u),
+                                     "f"(bad ? nan : v[i])
+                                     : "memory");
+            }
+        }
+        cluster_sync();
+        for (int i = rank * kPThreads + t; i < tokens * 128; i += parts * kPThreads) {
+            float sum = 0.f;
+            for (int p = 0; p < parts; ++p) sum += ld_cluster(map_rank(smem + (uint32_t)i * 4u, (uint32_t)p));
+            const long long w = w0 + i % 128;
+            if (w < a.rows_w) out[(x0 + i / 128) * a.stride + w] = from_float<T>(sum * scale);
+        }
+        cluster_sync();
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (warp == 5) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(a.tmem_cols));
+}
+
+}  // namespace sbclm

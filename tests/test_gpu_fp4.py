@@ -1,0 +1,245 @@
+"""4-bit floating point on the GPU against plain computations in 64 bits.
+
+Quantised values are compared for equality: every rounding decision of the format is that of exact
+arithmetic.  A product's tolerance follows from its sums: the products of two grid values and two
+block scales are exact in 32 bits, each of the ceil(cols / 64) accumulations into the 32-bit sum
+(and the adds inside the unit, counted as four more) may lose two bits more than a rounded addition
+of numbers no larger than sum |a b|, and the result is rounded once to the output's type.
+"""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():  # pragma: no cover
+    pytest.skip("needs a CUDA device", allow_module_level=True)
+
+from paper_1805_08768_b200 import binding as sbc
+
+DEV = torch.device("cuda:0")
+BLOCK = {"e8m0": 32, "e4m3": 16}
+GRID = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6], dtype=torch.float64, device=DEV)
+ROUND = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+
+
+def nearest(y, table):
+    """Entry of an ascending table nearest to y >= 0, the even index on a tie, the last one beyond it."""
+    hi = torch.searchsorted(table, y.contiguous()).clamp(max=len(table) - 1)
+    lo = (hi - 1).clamp(min=0)
+    up, down = table[hi] - y, y - table[lo]
+    take_hi = (up < down) | ((up == down) & (hi % 2 == 0)) | (y >= table[-1])
+    return torch.where(take_hi, table[hi], table[lo])
+
+
+def plain_round(x, fmt):
+    """x as its 4-bit form along the rows stands for it, float64; blocks with a non-finite value are NaN."""
+    x = x.double()
+    rows, cols = x.shape
+    size = BLOCK[fmt]
+    x = torch.cat((x, x.new_zeros(rows, -cols % size)), 1).reshape(rows, -1, size)
+    bad = ~torch.isfinite(x).all(2)
+    clean = torch.where(torch.isfinite(x), x, torch.zeros_like(x))
+    amax = clean.abs().amax(2)
+    log2 = torch.frexp(amax)[1] - 1
+    if fmt == "e8m0":
+        e = torch.where(amax > 0, log2 - 2, torch.full_like(log2, -127)).clamp(-127, 127)
+        scale = torch.ldexp(torch.ones_like(amax), e)
+    else:
+        top = clean.abs().max()
+        g = max(-126, math.frexp(float(top))[1] - 1 - 10) if float(top) > 0 else 0
+        table = torch.arange(0, 127, dtype=torch.uint8, device=DEV).view(torch.float8_e4m3fn).double()
+        scale = nearest(amax / 6 / 2.0 ** g, table) * 2.0 ** g
+    y = clean.abs() / torch.where(scale > 0, scale, torch.full_like(scale, math.inf))[:, :, None]
+    out = torch.sign(clean) * nearest(y, GRID) * scale[:, :, None]
+    out[bad] = math.nan
+    return out.reshape(rows, -1)[:, :cols]
+
+
+def same(got, want):
+    """Equal, the wanted value taken to the result's type (beyond its largest number: infinity)."""
+    want = want.to(got.dtype).double()
+    return bool(((got.double() == want) | (torch.isnan(got) & torch.isnan(want))).all())
+
+
+def values(rows, cols, dtype, seed):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    x = torch.randn(rows, cols, generator=g, device=DEV) * torch.exp(2 * torch.randn(1, cols, generator=g, device=DEV))
+    return x.to(dtype)
+
+
+SHAPES = [(1, 1), (1, 650), (3, 16), (5, 17), (2, 33), (127, 31), (128, 128), (129, 129), (35, 650), (300, 1300), (257, 4096),
+          (1000, 2), (8, 10000)]
+
+
+@pytest.mark.parametrize("fmt", ["e8m0", "e4m3"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_quantise_both_ways(shape, dtype, fmt):
+    x = values(*shape, dtype, 1 + shape[0])
+    q, q_t = sbc.sbc_fp4_quantise_both(x, fmt)
+    assert same(sbc.sbc_fp4_dequantise(q), plain_round(x, fmt))
+    assert same(sbc.sbc_fp4_dequantise(q_t), plain_round(x.t(), fmt))
+    # one orientation at a time writes the same bytes
+    one, other = sbc.sbc_fp4_quantise(x, fmt), sbc.sbc_fp4_quantise(x, fmt, transposed=True)
+    for a, b in ((one, q), (other, q_t)):
+        assert torch.equal(a.values, b.values) and torch.equal(a.scales, b.scales) and torch.equal(a.tensor_scale, b.tensor_scale)
+
+
+@pytest.mark.parametrize("fmt", ["e8m0", "e4m3"])
+@pytest.mark.parametrize("offset,extra", [(0, 8), (1, 0), (3, 5), (4, 4), (2, 2)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_quantise_strides_and_offsets(dtype, offset, extra, fmt):
+    rows, cols = 67, 333
+    room = values(1, offset + rows * (cols + extra) + 64, dtype, 5).view(-1)
+    x = torch.as_strided(room, (rows, cols), (cols + extra, 1), offset)
+    q, q_t = sbc.sbc_fp4_quantise_both(x, fmt)
+    assert same(sbc.sbc_fp4_dequantise(q), plain_round(x, fmt))
+    assert same(sbc.sbc_fp4_dequantise(q_t), plain_round(x.t(), fmt))
+    # a strided output keeps what stands between its rows
+    wide = torch.full((rows, cols + 7), 7.0, device=DEV)
+    sbc.sbc_fp4_dequantise(q, out=wide[:, 3:3 + cols])
+    assert same(wide[:, 3:3 + cols], plain_round(x, fmt))
+    assert bool((wide[:, :3] == 7).all()) and bool((wide[:, 3 + cols:] == 7).all())
+
+
+@pytest.mark.parametrize("fmt", ["e8m0", "e4m3"])
+def test_every_midpoint_and_its_neighbours(fmt):
+    """Blocks whose largest value fixes the scale, the others on and next to the grid's midpoints."""
+    rows = []
+    mids = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0], dtype=torch.float32)
+    for scale in [1.0, 1.125, 1.25, 1.375, 1.5, 1.625, 1.75, 1.875]:
+        at = mids * scale                                     # exact
+        row = torch.cat((at, torch.nextafter(at, torch.tensor(math.inf))))
+        low = torch.nextafter(at, torch.tensor(-math.inf))
+        rows.append(torch.cat((row, torch.tensor([6 * scale, -6 * scale]))))
+        rows.append(torch.cat((-low, low, torch.tensor([6 * scale, 0.0]))))
+    x = torch.stack(rows).to(DEV).repeat(1, 2)
+    x = torch.cat((x, x * 2.0 ** -20, x * 2.0 ** 40 if fmt == "e8m0" else x * 4))
+    assert same(sbc.sbc_fp4_dequantise(sbc.sbc_fp4_quantise(x, fmt)), plain_round(x, fmt))
+
+
+@pytest.mark.parametrize("fmt", ["e8m0", "e4m3"])
+def test_zeros_extremes_and_non_finite_blocks(fmt):
+    x = torch.zeros(12, 96, device=DEV)
+    x[1] = 1e-45
+    x[2, 5] = 3e38
+    x[3, 40:] = torch.linspace(-1e-40, 1e-40, 56, device=DEV)
+    x[4, 3], x[4, 50] = math.inf, 1.0
+    x[5, 70], x[5, 1] = math.nan, -2.0
+    x[6] = -math.inf
+    x[7] = 1.17549435e-38
+    x[8, ::2], x[8, 1::2] = -0.0, 1e-3
+    x[9] = torch.logspace(-44, 38, 96, device=DEV)
+    x[10] = -3.4028234e38
+    if fmt == "e4m3":      # keep g where the small rows still matter, too
+        assert same(sbc.sbc_fp4_dequantise(sbc.sbc_fp4_quantise(x[:2].contiguous(), fmt)), plain_round(x[:2], fmt))
+    assert same(sbc.sbc_fp4_dequantise(sbc.sbc_fp4_quantise(x, fmt)), plain_round(x, fmt))
+    assert same(sbc.sbc_fp4_dequantise(sbc.sbc_fp4_quantise(x, fmt, transposed=True)), plain_round(x.t(), fmt))
+    z = torch.zeros(3, 40, device=DEV)
+    assert not bool(sbc.sbc_fp4_dequantise(sbc.sbc_fp4_quantise(z, fmt)).any())
+
+
+def plain_product(a, b):
+    a, b = sbc.sbc_fp4_dequantise(a).double(), sbc.sbc_fp4_dequantise(b).double()
+    return a @ b.t(), a.abs() @ b.abs().t()
+
+
+def check_product(got, a, b):
+    want, size = plain_product(a, b)
+    allowed = (math.ceil(a.cols / 64) + 4) * 2.0 ** -22 * size + ROUND[got.dtype] * want.abs() + 1e-30
+    assert bool(((got.double() - want).abs() <= allowed).all()), float(((got.double() - want).abs() - allowed).max())
+
+
+PRODUCTS = [(1, 650, 10000), (1, 64, 128), (16, 256, 128), (1, 1, 1), (3, 5, 7), (17, 65, 129), (2, 8192, 256), (35, 650, 1000),
+            (128, 512, 128), (129, 513, 130), (255, 300, 257), (256, 256, 256), (257, 1000, 300), (700, 1300, 2600), (16, 4096, 4096),
+            (513, 96, 33), (64, 2048, 1000)]
+
+
+@pytest.mark.parametrize("fmt", ["e8m0", "e4m3"])
+@pytest.mark.parametrize("shape", PRODUCTS)
+def test_product(shape, fmt):
+    tokens, inner, outer = shape
+    a = sbc.sbc_fp4_quantise(values(tokens, inner, torch.bfloat16, 3), fmt)
+    b = sbc.sbc_fp4_quantise(values(outer, inner, torch.float32, 4), fmt)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for dtype in (torch.float32, torch.bfloat16):
+        check_product(sbc.sbc_fp4_product(a, b, dtype, status=status), a, b)
+    again = sbc.sbc_fp4_product(a, b, torch.float32)
+    assert torch.equal(again, sbc.sbc_fp4_product(a, b, torch.float32))        # same sums every time
+    assert int(status.item()) == 0
+
+
+@pytest.mark.parametrize("fmt", ["e8m0", "e4m3"])
+def test_product_with_exact_small_integers(fmt):
+    """Grid values with scale one everywhere: sums are whole numbers of quarters and must be exact."""
+    g = torch.Generator(device=DEV).manual_seed(11)
+    table = torch.cat((GRID, -GRID)).float()
+    x = table[torch.randint(0, 16, (40, 320), generator=g, device=DEV)]
+    w = table[torch.randint(0, 16, (200, 320), generator=g, device=DEV)]
+    x[:, ::16], w[:, ::16] = 6.0, 6.0
+    a, b = sbc.sbc_fp4_quantise(x, fmt), sbc.sbc_fp4_quantise(w, fmt)
+    assert torch.equal(sbc.sbc_fp4_dequantise(a), x)
+    assert torch.equal(sbc.sbc_fp4_product(a, b, torch.float32).double(), x.double() @ w.double().t())
+
+
+@pytest.mark.parametrize("fmt", ["e8m0", "e4m3"])
+def test_product_writes_only_its_output(fmt):
+    a = sbc.sbc_fp4_quantise(values(21, 200, torch.bfloat16, 3), fmt)
+    b = sbc.sbc_fp4_quantise(values(131, 200, torch.float32, 4), fmt)
+    room = torch.full((23, 140), 7.0, device=DEV, dtype=torch.float16)
+    sbc.sbc_fp4_product(a, b, out=room[1:22, 5:136])
+    check_product(room[1:22, 5:136], a, b)
+    inside = torch.zeros_like(room, dtype=torch.bool)
+    inside[1:22, 5:136] = True
+    assert bool((room[~inside] == 7).all())
+
+
+@pytest.mark.parametrize("fmt", ["e8m0", "e4m3"])
+@pytest.mark.parametrize("tokens", [1, 40, 300])
+def test_nan_blocks_reach_only_their_rows(fmt, tokens):
+    x, w = values(tokens, 700, torch.float32, 3), values(140, 700, torch.float32, 4)
+    x[tokens // 2, 100], w[77, 650] = math.nan, math.inf
+    a, b = sbc.sbc_fp4_quantise(x, fmt), sbc.sbc_fp4_quantise(w, fmt)
+    got = sbc.sbc_fp4_product(a, b, torch.float32)
+    want = torch.zeros_like(got, dtype=torch.bool)
+    want[tokens // 2], want[:, 77] = True, True
+    assert torch.equal(torch.isnan(got), want)
+
+
+def test_refusals():
+    x = values(4, 64, torch.float32, 1)
+    with pytest.raises(TypeError):
+        sbc.sbc_fp4_quantise(x.double())
+    with pytest.raises(TypeError):
+        sbc.sbc_fp4_quantise(x.cpu())
+    with pytest.raises(TypeError):
+        sbc.sbc_fp4_quantise(x[0])
+    with pytest.raises(ValueError):
+        sbc.sbc_fp4_quantise(x.t())
+    with pytest.raises(ValueError):
+        sbc.sbc_fp4_quantise(x, "e5m2")
+    with pytest.raises(ValueError):
+        sbc.sbc_fp4_quantise(x[:0])
+    a, b = sbc.sbc_fp4_quantise(x, "e8m0"), sbc.sbc_fp4_quantise(x, "e4m3")
+    with pytest.raises(ValueError):
+        sbc.sbc_fp4_product(a, b)
+    with pytest.raises(ValueError):
+        sbc.sbc_fp4_product(a, sbc.sbc_fp4_quantise(values(4, 65, torch.float32, 1), "e8m0"))
+    with pytest.raises(ValueError):
+        sbc.sbc_fp4_product(a, a, out=torch.empty(3, 4, device=DEV))
+    with pytest.raises(ValueError):
+        sbc.Fp4Tensor(a.values[:3], a.scales, a.tensor_scale, 4, 64, "e8m0")
+    with pytest.raises(ValueError):
+        sbc.Fp4Tensor(a.values, a.scales[:-512], a.tensor_scale, 4, 64, "e8m0")
+
+
+def test_work_on_another_stream():
+    side = torch.cuda.Stream()
+    x, w = values(33, 650, torch.bfloat16, 3), values(300, 650, torch.float32, 4)
+    torch.cuda.synchronize()
+    a, b = sbc.sbc_fp4_quantise(x, stream=side), sbc.sbc_fp4_quantise(w, stream=side)
+    got = sbc.sbc_fp4_product(a, b, torch.float32, stream=side)
+    side.synchronize()
+    check_product(got, a, b)
