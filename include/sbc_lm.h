@@ -109,6 +109,77 @@ int sbc_fp4_dequantise(const sbc_fp4 *q, void *out, int dtype, int64_t row_strid
 int sbc_fp4_product(const sbc_fp4 *a, const sbc_fp4 *b, void *out, int dtype, int64_t row_stride,
                     uint32_t *status, sbc_cuda_stream_t stream);
 
+/* ---- a teacher's message ------------------------------------------------- */
+
+#define SBC_TOP_MOST 256          /* most logits of a row that sbc_top_logits selects */
+#define SBC_DISTILL_MOST 1024     /* most logits of a row that a loss takes */
+#define SBC_DISTILL_COLS (1 << 20) /* most columns that a loss takes */
+#define SBC_DISTILL_STATS 8       /* floats per row that sbc_distill_loss leaves for sbc_distill_grad */
+
+/*
+ * The k largest logits of every row and the mass of the others:
+ *   values[r, 0..k), indices[r, 0..k)  in descending order, the lower index
+ *                                      first among equals (-0 equals +0)
+ *   rest[r] = log sum_{j not sent} exp(logits[r, j] / temperature), -inf if
+ *             nothing (or nothing but -inf) is left
+ * Logits of -inf (words ruled out) are sent only where fewer than k others
+ * exist.  NaN orders above everything and makes the row's rest NaN if it is
+ * not sent.
+ *
+ * logits  device, dtype, rows x cols; rows may be 0
+ * k       1 .. min(cols, SBC_TOP_MOST); temperature > 0
+ * values float, indices int32: device, rows x k;  rest: device, rows floats
+ */
+int sbc_top_logits(const void *logits, int dtype, int64_t rows, int64_t cols, int64_t row_stride, int k,
+                   float temperature, float *values, int32_t *indices, float *rest, sbc_cuda_stream_t stream);
+
+/*
+ * What a student is taught, per row:
+ *   teacher  p = softmax over (values[r, :] / temperature, rest[r])
+ *   student  q = softmax(logits[r, :] / temperature); q_rest its mass outside
+ *            the sent words
+ *   loss[r] = alpha * temperature^2 * KL(p || q over the same outcomes)
+ *           + (1 - alpha) * cross entropy of softmax(logits[r, :]) and labels[r]
+ * A row whose teacher has no mass, or whose logits are all -inf, has neither
+ * term of that kind; a row without a label has no cross entropy.  A slot of
+ * negative index is not used.  Indices of a row differ from each other.  An
+ * index or label >= cols is ignored and SBC_STATUS_RANGE or-ed into status.
+ *
+ * values   device, rows x k floats
+ * indices  device, rows x k int32
+ * rest     device, rows floats, or NULL: no mass outside (renormalised over k)
+ * labels   device, rows int64, negative: none; or NULL
+ */
+typedef struct sbc_distill {
+    const float *values;
+    const int32_t *indices;
+    const float *rest;
+    const int64_t *labels;
+    int32_t k;         /* 1 .. SBC_DISTILL_MOST */
+    float temperature; /* > 0 */
+    float alpha;       /* 0 .. 1 */
+    int32_t reserved;  /* 0 */
+} sbc_distill;
+
+/* Forward: loss (rows floats) and, unless NULL, stats (rows x SBC_DISTILL_STATS
+ * floats, 16-byte aligned) for the backward call.  status: device, one uint32,
+ * or NULL. */
+int sbc_distill_loss(const void *logits, int dtype, int64_t rows, int64_t cols, int64_t row_stride,
+                     const sbc_distill *d, float *loss, float *stats, uint32_t *status, sbc_cuda_stream_t stream);
+
+/* Backward: grad[r, j] = grad_loss[r] * d loss[r] / d logits[r, j] (dtype of the
+ * logits, rows grad_stride apart; may be the logits themselves).  grad_loss:
+ * device, rows floats, or NULL: ones.  stats: what sbc_distill_loss left for
+ * the same logits and the same d. */
+int sbc_distill_grad(const void *logits, int dtype, int64_t rows, int64_t cols, int64_t row_stride,
+                     const sbc_distill *d, const float *stats, const float *grad_loss, void *grad,
+                     int64_t grad_stride, sbc_cuda_stream_t stream);
+
+/* Both in one reading of the logits, where grad_loss is known beforehand. */
+int sbc_distill_loss_grad(const void *logits, int dtype, int64_t rows, int64_t cols, int64_t row_stride,
+                          const sbc_distill *d, const float *grad_loss, float *loss, void *grad,
+                          int64_t grad_stride, uint32_t *status, sbc_cuda_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

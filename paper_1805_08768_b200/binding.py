@@ -31,7 +31,7 @@ EXPORTS = [
     "sbc_workspace_bytes_sampled", "sbc_encode_sampled", "sbc_decode_accumulate_sized", "sbc_decode_apply_sized",
     "sbc_debug_barrier_timeout",
     "sbc_fp4_row_bytes", "sbc_fp4_scale_bytes", "sbc_fp4_workspace_bytes", "sbc_fp4_quantise", "sbc_fp4_dequantise",
-    "sbc_fp4_product",
+    "sbc_fp4_product", "sbc_top_logits", "sbc_distill_loss", "sbc_distill_grad", "sbc_distill_loss_grad",
 ]
 SIDE_VALUES = 2
 STATIC_WORKSPACE_BYTES = 8 << 20
@@ -71,6 +71,11 @@ class TensorDesc(C.Structure):
 class Fp4Desc(C.Structure):
     _fields_ = [("values", C.c_void_p), ("scales", C.c_void_p), ("tensor_scale", C.c_void_p), ("rows", C.c_int64),
                 ("cols", C.c_int64), ("format", C.c_int32), ("reserved", C.c_int32)]
+
+
+class DistillDesc(C.Structure):
+    _fields_ = [("values", C.c_void_p), ("indices", C.c_void_p), ("rest", C.c_void_p), ("labels", C.c_void_p),
+                ("k", C.c_int32), ("temperature", C.c_float), ("alpha", C.c_float), ("reserved", C.c_int32)]
 
 
 class DecodeDesc(C.Structure):
@@ -171,6 +176,19 @@ def lib() -> C.CDLL:
         L.sbc_fp4_product.restype = C.c_int
         L.sbc_fp4_product.argtypes = [C.POINTER(Fp4Desc), C.POINTER(Fp4Desc), C.c_void_p, C.c_int, C.c_int64,
                                       C.c_void_p, C.c_void_p]
+        L.sbc_top_logits.restype = C.c_int
+        L.sbc_top_logits.argtypes = [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_int, C.c_float,
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.sbc_distill_loss.restype = C.c_int
+        L.sbc_distill_loss.argtypes = [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.POINTER(DistillDesc),
+                                       C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.sbc_distill_grad.restype = C.c_int
+        L.sbc_distill_grad.argtypes = [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.POINTER(DistillDesc),
+                                       C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
+        L.sbc_distill_loss_grad.restype = C.c_int
+        L.sbc_distill_loss_grad.argtypes = [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64,
+                                            C.POINTER(DistillDesc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
+                                            C.c_void_p, C.c_void_p]
         _lib = L
     return _lib
 
@@ -653,3 +671,113 @@ def sbc_fp4_product(a: Fp4Tensor, b: Fp4Tensor, dtype: torch.dtype = torch.bfloa
                                  _row_stride(out), status.data_ptr() if status is not None else None,
                                  _cuda_stream(stream)), "sbc_fp4_product")
     return out
+
+
+TOP_MOST, DISTILL_MOST, DISTILL_COLS, DISTILL_STATS = 256, 1024, 1 << 20, 8
+
+
+def sbc_top_logits(logits: torch.Tensor, k: int, temperature: float = 1.0,
+                   stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """(values float32 [rows, k], indices int32 [rows, k], rest float32 [rows]): every row's k largest
+    logits in descending order and log sum exp(z / temperature) of all the others."""
+    _matrix(logits, "logits")
+    rows, cols = logits.shape
+    if not 1 <= k <= min(cols, TOP_MOST):
+        raise ValueError(f"k must be in 1 .. {min(cols, TOP_MOST)}")
+    with _fresh(stream):
+        values = torch.empty(rows, k, dtype=torch.float32, device=logits.device)
+        indices = torch.empty(rows, k, dtype=torch.int32, device=logits.device)
+        rest = torch.empty(rows, dtype=torch.float32, device=logits.device)
+    _check(lib().sbc_top_logits(logits.data_ptr(), DTYPE_CODES[logits.dtype], rows, cols, _row_stride(logits), k,
+                                float(temperature), values.data_ptr(), indices.data_ptr(), rest.data_ptr(),
+                                _cuda_stream(stream)), "sbc_top_logits")
+    return values, indices, rest
+
+
+def _rows_of(t: Optional[torch.Tensor], rows: int, dtype: torch.dtype, name: str) -> Optional[int]:
+    if t is None:
+        return None
+    if not (t.is_cuda and t.dtype == dtype and t.is_contiguous()):
+        raise TypeError(f"{name} must be a contiguous {dtype} CUDA tensor")
+    if t.numel() != rows:
+        raise ValueError(f"{name} must hold one value per row")
+    return t.data_ptr()
+
+
+def _taught(logits, values, indices, rest, temperature, alpha, labels) -> DistillDesc:
+    _matrix(logits, "logits")
+    rows, cols = logits.shape
+    _dev_f32(values, "values")
+    if not (indices.is_cuda and indices.dtype == torch.int32 and indices.is_contiguous()):
+        raise TypeError("indices must be a contiguous int32 CUDA tensor")
+    if values.dim() != 2 or values.shape != indices.shape or values.shape[0] != rows:
+        raise ValueError("values and indices must be rows x k")
+    if not 1 <= values.shape[1] <= DISTILL_MOST:
+        raise ValueError(f"k must be in 1 .. {DISTILL_MOST}")
+    if not 1 <= cols <= DISTILL_COLS:
+        raise ValueError(f"logits must have 1 .. {DISTILL_COLS} columns")
+    return DistillDesc(values.data_ptr(), indices.data_ptr(), _rows_of(rest, rows, torch.float32, "rest"),
+                       _rows_of(labels, rows, torch.int64, "labels"), values.shape[1], float(temperature),
+                       float(alpha), 0)
+
+
+def _grad_out(logits: torch.Tensor, out: Optional[torch.Tensor], stream) -> torch.Tensor:
+    if out is None:
+        with _fresh(stream):
+            return torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    _matrix(out, "out")
+    if out.shape != logits.shape or out.dtype != logits.dtype:
+        raise ValueError("out must have the logits' shape and type")
+    return out
+
+
+def sbc_distill_loss(logits: torch.Tensor, values: torch.Tensor, indices: torch.Tensor,
+                     rest: Optional[torch.Tensor] = None, temperature: float = 1.0, alpha: float = 1.0,
+                     labels: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                     stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(loss [rows], statistics for sbc_distill_grad): alpha temperature^2 KL(teacher || student) over the
+    sent words and one outcome for all others, plus (1 - alpha) cross entropy of the labels."""
+    d = _taught(logits, values, indices, rest, temperature, alpha, labels)
+    rows, cols = logits.shape
+    with _fresh(stream):
+        loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
+        stats = torch.empty(rows, DISTILL_STATS, dtype=torch.float32, device=logits.device)
+    _check(lib().sbc_distill_loss(logits.data_ptr(), DTYPE_CODES[logits.dtype], rows, cols, _row_stride(logits),
+                                  C.byref(d), loss.data_ptr(), stats.data_ptr(),
+                                  status.data_ptr() if status is not None else None, _cuda_stream(stream)),
+           "sbc_distill_loss")
+    return loss, stats
+
+
+def sbc_distill_grad(logits: torch.Tensor, values: torch.Tensor, indices: torch.Tensor, stats: torch.Tensor,
+                     grad_loss: Optional[torch.Tensor] = None, rest: Optional[torch.Tensor] = None,
+                     temperature: float = 1.0, alpha: float = 1.0, labels: Optional[torch.Tensor] = None,
+                     out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """grad_loss[r] * d loss[r] / d logits[r, :] in the logits' type; ``out`` may be the logits."""
+    d = _taught(logits, values, indices, rest, temperature, alpha, labels)
+    rows, cols = logits.shape
+    out = _grad_out(logits, out, stream)
+    _check(lib().sbc_distill_grad(logits.data_ptr(), DTYPE_CODES[logits.dtype], rows, cols, _row_stride(logits),
+                                  C.byref(d), _rows_of(stats, rows * DISTILL_STATS, torch.float32, "stats"),
+                                  _rows_of(grad_loss, rows, torch.float32, "grad_loss"), out.data_ptr(),
+                                  _row_stride(out), _cuda_stream(stream)), "sbc_distill_grad")
+    return out
+
+
+def sbc_distill_loss_grad(logits: torch.Tensor, values: torch.Tensor, indices: torch.Tensor,
+                          grad_loss: Optional[torch.Tensor] = None, rest: Optional[torch.Tensor] = None,
+                          temperature: float = 1.0, alpha: float = 1.0, labels: Optional[torch.Tensor] = None,
+                          out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                          stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(loss [rows], its gradient times grad_loss) in one reading of the logits; ``out`` may be the logits."""
+    d = _taught(logits, values, indices, rest, temperature, alpha, labels)
+    rows, cols = logits.shape
+    out = _grad_out(logits, out, stream)
+    with _fresh(stream):
+        loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
+    _check(lib().sbc_distill_loss_grad(logits.data_ptr(), DTYPE_CODES[logits.dtype], rows, cols, _row_stride(logits),
+                                       C.byref(d), _rows_of(grad_loss, rows, torch.float32, "grad_loss"),
+                                       loss.data_ptr(), out.data_ptr(), _row_stride(out),
+                                       status.data_ptr() if status is not None else None, _cuda_stream(stream)),
+           "sbc_distill_loss_grad")
+    return loss, out

@@ -1,7 +1,9 @@
 // C entry points of the language-model operators (include/sbc_lm.h).
 #include <algorithm>
+#include <type_traits>
 
 #include "lm_common.cuh"
+#include "lm_logits.cuh"
 #include "lm_product.cuh"
 #include "lm_quantise.cuh"
 
@@ -110,6 +112,75 @@ int launch_product(const CUtensorMap& mw, const CUtensorMap& mx, const ProductAr
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, k_fp4_product<T, FMT>, mw, mx, a) == cudaSuccess ? SBC_OK : SBC_ECUDA;
+}
+
+// A launch of one cluster of `size` blocks per row.
+struct RowLaunch {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    RowLaunch(int64_t rows, int size, int threads, size_t smem, cudaStream_t st) {
+        cfg.gridDim = dim3((unsigned)(rows * size));
+        cfg.blockDim = dim3((unsigned)threads);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = st;
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)size;
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+    }
+};
+
+// Blocks that share a row: as many (up to 8) as keep the GPU busy when there are few rows, each
+// with at least `least` elements.
+int blocks_per_row(int64_t rows, int64_t cols, int64_t least) {
+    int size = 1;
+    while (size < 8 && rows * size * 2 <= 2 * sm_count() && cols >= least * size * 2) size *= 2;
+    return size;
+}
+
+bool distill_ok(const sbc_distill* d, int64_t rows, int64_t cols) {
+    return d && (rows == 0 || (d->values && d->indices)) && aligned(d->values, 4) && aligned(d->indices, 4) && aligned(d->rest, 4) &&
+           aligned(d->labels, 8) && d->k >= 1 && d->k <= SBC_DISTILL_MOST && d->temperature > 0.f && d->temperature <= 1e6f &&
+           d->alpha >= 0.f && d->alpha <= 1.f && d->reserved == 0 && cols <= SBC_DISTILL_COLS && rows <= kMaxDim / 8;
+}
+
+DistillArgs distill_args(const void* logits, int64_t rows, int64_t cols, int64_t stride, const sbc_distill* d) {
+    DistillArgs a = {};
+    a.logits = logits;
+    a.rows = rows;
+    a.stride = stride;
+    a.cols = (int)cols;
+    a.k = d->k;
+    a.temperature = d->temperature;
+    a.alpha = d->alpha;
+    a.values = d->values;
+    a.indices = d->indices;
+    a.rest = d->rest;
+    a.labels = d->alpha < 1.f ? reinterpret_cast<const long long*>(d->labels) : nullptr;
+    return a;
+}
+
+// A second exponential per element where labels are mixed in at another temperature than the teacher's.
+bool second_exponential(const DistillArgs& a) { return a.labels && a.temperature != 1.f; }
+
+int row_threads(int64_t per_block) { return per_block <= 16384 ? 256 : 512; }
+
+template <typename T, bool CE2, bool GRAD> int launch_distill(const DistillArgs& a, cudaStream_t st) {
+    const int size = blocks_per_row(a.rows, a.cols, 2048);
+    const size_t smem = ((size_t)((a.cols + 63) / 64 + size - 1) / size * 64 + 64) / 8 + (size_t)a.k * 12;
+    if (cudaFuncSetAttribute(k_distill<T, CE2, GRAD>, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != cudaSuccess)
+        return SBC_ECUDA;
+    RowLaunch l(a.rows, size, row_threads(a.cols / size), smem, st);
+    return cudaLaunchKernelEx(&l.cfg, k_distill<T, CE2, GRAD>, a) == cudaSuccess ? SBC_OK : SBC_ECUDA;
+}
+
+template <bool GRAD> int distill_by_type(const DistillArgs& a, int dtype, cudaStream_t st) {
+    return by_dtype(dtype, [&](auto* as) {
+        using T = std::remove_pointer_t<decltype(as)>;
+        return second_exponential(a) ? launch_distill<T, true, GRAD>(a, st) : launch_distill<T, false, GRAD>(a, st);
+    });
 }
 
 }  // namespace
@@ -238,6 +309,74 @@ int sbc_fp4_product(const sbc_fp4* a, const sbc_fp4* b, void* out, int dtype, in
         return a->format == SBC_FP4_E4M3 ? launch_product<T, SBC_FP4_E4M3>(mw, mx, p, grid, smem, stream)
                                          : launch_product<T, SBC_FP4_E8M0>(mw, mx, p, grid, smem, stream);
     });
+}
+
+int sbc_top_logits(const void* logits, int dtype, int64_t rows, int64_t cols, int64_t row_stride, int k, float temperature,
+                   float* values, int32_t* indices, float* rest, sbc_cuda_stream_t stream) {
+    if (rows == 0 && width_of(dtype) && cols >= 1) return k >= 1 && k <= std::min<int64_t>(cols, kTopMost) && temperature > 0.f ? SBC_OK : SBC_EINVAL;
+    if (!matrix_ok(logits, dtype, rows, cols, row_stride) || rows > kMaxDim / 8) return SBC_EINVAL;
+    if (k < 1 || k > std::min<int64_t>(cols, kTopMost) || !(temperature > 0.f) || !(temperature <= 1e6f)) return SBC_EINVAL;
+    if (!values || !indices || !rest || !aligned(values, 4) || !aligned(indices, 4) || !aligned(rest, 4)) return SBC_EINVAL;
+    TopArgs a = {logits, rows, row_stride, (int)cols, k, temperature, values, indices, rest};
+    return by_dtype(dtype, [&](auto* as) {
+        using T = std::remove_pointer_t<decltype(as)>;
+        RowLaunch l(rows, blocks_per_row(rows, cols, 2048), kTopThreads, 0, stream);
+        return cudaLaunchKernelEx(&l.cfg, k_top_logits<T>, a) == cudaSuccess ? (int)SBC_OK : (int)SBC_ECUDA;
+    });
+}
+
+int sbc_distill_loss(const void* logits, int dtype, int64_t rows, int64_t cols, int64_t row_stride, const sbc_distill* d, float* loss,
+                     float* stats, uint32_t* status, sbc_cuda_stream_t stream) {
+    if (!distill_ok(d, rows, cols) || !width_of(dtype)) return SBC_EINVAL;
+    if (rows == 0) return SBC_OK;
+    if (!matrix_ok(logits, dtype, rows, cols, row_stride) || !loss || !aligned(loss, 4) || !aligned(stats, 16) || !aligned(status, 4))
+        return SBC_EINVAL;
+    DistillArgs a = distill_args(logits, rows, cols, row_stride, d);
+    a.loss = loss;
+    a.stats = stats;
+    a.status = status;
+    return distill_by_type<false>(a, dtype, stream);
+}
+
+int sbc_distill_grad(const void* logits, int dtype, int64_t rows, int64_t cols, int64_t row_stride, const sbc_distill* d,
+                     const float* stats, const float* grad_loss, void* grad, int64_t grad_stride, sbc_cuda_stream_t stream) {
+    if (!distill_ok(d, rows, cols) || !width_of(dtype)) return SBC_EINVAL;
+    if (rows == 0) return SBC_OK;
+    if (!matrix_ok(logits, dtype, rows, cols, row_stride) || !matrix_ok(grad, dtype, rows, cols, grad_stride) || !stats ||
+        !aligned(stats, 16) || !aligned(grad_loss, 4))
+        return SBC_EINVAL;
+    DistillArgs a = distill_args(logits, rows, cols, row_stride, d);
+    a.stats = const_cast<float*>(stats);
+    a.grad_loss = grad_loss;
+    a.grad = grad;
+    a.grad_stride = grad_stride;
+    return by_dtype(dtype, [&](auto* as) {
+        using T = std::remove_pointer_t<decltype(as)>;
+        const int size = blocks_per_row(rows, cols, 2048), threads = row_threads(cols / size);
+        const size_t smem = (size_t)a.k * 12;
+        if (second_exponential(a))
+            k_distill_grad<T, true><<<(unsigned)(rows * size), threads, smem, stream>>>(a, size);
+        else
+            k_distill_grad<T, false><<<(unsigned)(rows * size), threads, smem, stream>>>(a, size);
+        return launched();
+    });
+}
+
+int sbc_distill_loss_grad(const void* logits, int dtype, int64_t rows, int64_t cols, int64_t row_stride, const sbc_distill* d,
+                          const float* grad_loss, float* loss, void* grad, int64_t grad_stride, uint32_t* status,
+                          sbc_cuda_stream_t stream) {
+    if (!distill_ok(d, rows, cols) || !width_of(dtype)) return SBC_EINVAL;
+    if (rows == 0) return SBC_OK;
+    if (!matrix_ok(logits, dtype, rows, cols, row_stride) || !matrix_ok(grad, dtype, rows, cols, grad_stride) || !loss ||
+        !aligned(loss, 4) || !aligned(grad_loss, 4) || !aligned(status, 4))
+        return SBC_EINVAL;
+    DistillArgs a = distill_args(logits, rows, cols, row_stride, d);
+    a.loss = loss;
+    a.grad_loss = grad_loss;
+    a.grad = grad;
+    a.grad_stride = grad_stride;
+    a.status = status;
+    return distill_by_type<true>(a, dtype, stream);
 }
 
 }  // extern "C"

@@ -119,7 +119,7 @@ __device__ __forceinline__ uint32_t cluster_size() {
     return r;
 }
 __device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
 // Address of `local` (a shared-memory address of this block) in block `rank` of the cluster.
 __device__ __forceinline__ uint32_t map_rank(uint32_t local, uint32_t rank) {
