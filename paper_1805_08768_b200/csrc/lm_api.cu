@@ -132,12 +132,25 @@ struct RowLaunch {
     }
 };
 
-// Blocks that share a row: as many (up to 8) as keep the GPU busy when there are few rows, each
-// with at least `least` elements.
-int blocks_per_row(int64_t rows, int64_t cols, int64_t least) {
-    int size = 1;
-    while (size < 8 && rows * size * 2 <= 2 * sm_count() && cols >= least * size * 2) size *= 2;
-    return size;
+// How a row of logits is cut: blocks that share it, elements a block holds in shared memory at a
+// time, threads of a block.
+struct RowPlan {
+    int size, room, threads;
+};
+
+// A segment is at most kRoomBytes where eight blocks are enough for that; few rows are spread over as
+// many blocks as keep the GPU busy, each with at least 2048 elements.
+constexpr int kRoomBytes = 64 * 1024;
+RowPlan plan_rows(int64_t rows, int64_t cols, int width) {
+    int64_t size = 1;
+    while (size < 8 && cols * width > size * kRoomBytes) size *= 2;
+    while (size < 8 && rows * size * 2 <= 2 * sm_count() && cols >= 2048 * size * 2) size *= 2;
+    const int64_t segment = ceil_div(ceil_div(cols, 64), size) * 64;
+    RowPlan p;
+    p.size = (int)size;
+    p.room = (int)std::min<int64_t>(segment, 2 * kRoomBytes / width);
+    p.threads = segment * width <= 24 * 1024 ? 128 : segment * width <= 48 * 1024 ? 256 : 512;
+    return p;
 }
 
 bool distill_ok(const sbc_distill* d, int64_t rows, int64_t cols) {
@@ -165,14 +178,14 @@ DistillArgs distill_args(const void* logits, int64_t rows, int64_t cols, int64_t
 // A second exponential per element where labels are mixed in at another temperature than the teacher's.
 bool second_exponential(const DistillArgs& a) { return a.labels && a.temperature != 1.f; }
 
-int row_threads(int64_t per_block) { return per_block <= 16384 ? 256 : 512; }
-
-template <typename T, bool CE2, bool GRAD> int launch_distill(const DistillArgs& a, cudaStream_t st) {
-    const int size = blocks_per_row(a.rows, a.cols, 2048);
-    const size_t smem = ((size_t)((a.cols + 63) / 64 + size - 1) / size * 64 + 64) / 8 + (size_t)a.k * 12;
-    if (cudaFuncSetAttribute(k_distill<T, CE2, GRAD>, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != cudaSuccess)
+template <typename T, bool CE2, bool GRAD> int launch_distill(DistillArgs a, cudaStream_t st) {
+    const RowPlan p = plan_rows(a.rows, a.cols, (int)sizeof(T));
+    a.room = p.room;
+    const size_t smem = (size_t)p.room * sizeof(T) + 32 + (size_t)a.k * 12;
+    if (cudaFuncSetAttribute(k_distill<T, CE2, GRAD>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * kRoomBytes + 32 + SBC_DISTILL_MOST * 12) !=
+        cudaSuccess)
         return SBC_ECUDA;
-    RowLaunch l(a.rows, size, row_threads(a.cols / size), smem, st);
+    RowLaunch l(a.rows, p.size, p.threads, smem, st);
     return cudaLaunchKernelEx(&l.cfg, k_distill<T, CE2, GRAD>, a) == cudaSuccess ? SBC_OK : SBC_ECUDA;
 }
 
@@ -313,15 +326,25 @@ int sbc_fp4_product(const sbc_fp4* a, const sbc_fp4* b, void* out, int dtype, in
 
 int sbc_top_logits(const void* logits, int dtype, int64_t rows, int64_t cols, int64_t row_stride, int k, float temperature,
                    float* values, int32_t* indices, float* rest, sbc_cuda_stream_t stream) {
-    if (rows == 0 && width_of(dtype) && cols >= 1) return k >= 1 && k <= std::min<int64_t>(cols, kTopMost) && temperature > 0.f ? SBC_OK : SBC_EINVAL;
-    if (!matrix_ok(logits, dtype, rows, cols, row_stride) || rows > kMaxDim / 8) return SBC_EINVAL;
-    if (k < 1 || k > std::min<int64_t>(cols, kTopMost) || !(temperature > 0.f) || !(temperature <= 1e6f)) return SBC_EINVAL;
+    if (!width_of(dtype) || rows < 0 || rows > kMaxDim / 8 || cols < 1 || cols > kMaxDim) return SBC_EINVAL;
+    if (k < 1 || k > std::min<int64_t>(cols, SBC_TOP_MOST) || !(temperature > 0.f) || !(temperature <= 1e6f)) return SBC_EINVAL;
+    if (rows == 0) return SBC_OK;
+    if (!matrix_ok(logits, dtype, rows, cols, row_stride)) return SBC_EINVAL;
     if (!values || !indices || !rest || !aligned(values, 4) || !aligned(indices, 4) || !aligned(rest, 4)) return SBC_EINVAL;
     TopArgs a = {logits, rows, row_stride, (int)cols, k, temperature, values, indices, rest};
     return by_dtype(dtype, [&](auto* as) {
         using T = std::remove_pointer_t<decltype(as)>;
-        RowLaunch l(rows, blocks_per_row(rows, cols, 2048), kTopThreads, 0, stream);
-        return cudaLaunchKernelEx(&l.cfg, k_top_logits<T>, a) == cudaSuccess ? (int)SBC_OK : (int)SBC_ECUDA;
+        const RowPlan p = plan_rows(rows, cols, (int)sizeof(T));
+        // enough groups of elements that the k-th largest of their maxima bounds tightly: two a thread, four times k
+        const int threads = std::max(p.threads, std::min(256, (int)ceil_div(2 * k, 32) * 32));
+        if (ceil_div(ceil_div(cols, 64), p.size) * 64 > p.room) {   // too long to be held
+            RowLaunch l(rows, p.size, kTopThreads, 0, stream);
+            return cudaLaunchKernelEx(&l.cfg, k_top_logits<T, false>, a) == cudaSuccess ? (int)SBC_OK : (int)SBC_ECUDA;
+        }
+        if (cudaFuncSetAttribute(k_top_logits<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * kRoomBytes + 32) != cudaSuccess)
+            return (int)SBC_ECUDA;
+        RowLaunch l(rows, p.size, threads, (size_t)p.room * sizeof(T) + 32, stream);
+        return cudaLaunchKernelEx(&l.cfg, k_top_logits<T, true>, a) == cudaSuccess ? (int)SBC_OK : (int)SBC_ECUDA;
     });
 }
 
@@ -352,7 +375,8 @@ int sbc_distill_grad(const void* logits, int dtype, int64_t rows, int64_t cols, 
     a.grad_stride = grad_stride;
     return by_dtype(dtype, [&](auto* as) {
         using T = std::remove_pointer_t<decltype(as)>;
-        const int size = blocks_per_row(rows, cols, 2048), threads = row_threads(cols / size);
+        const RowPlan p = plan_rows(rows, cols, (int)sizeof(T));
+        const int size = p.size, threads = p.threads;
         const size_t smem = (size_t)a.k * 12;
         if (second_exponential(a))
             k_distill_grad<T, true><<<(unsigned)(rows * size), threads, smem, stream>>>(a, size);

@@ -1,7 +1,8 @@
 // A teacher's largest logits, and the loss and gradient of a student against them.
 //
-// A row of logits belongs to one block, or to a cluster of blocks where there are few rows (each
-// then takes a segment of the row).  Exponentials are powers of two: c = log2(e) / temperature.
+// A row of logits belongs to one block, or to a cluster of blocks where there are few rows or the row
+// is long; each then takes a segment of the row, which it keeps in shared memory between its passes
+// over it.  Exponentials are powers of two: c = log2(e) / temperature.
 #pragma once
 
 #include "lm_common.cuh"
@@ -41,89 +42,149 @@ __device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigne
     return r;
 }
 
-__device__ __forceinline__ void unpack8(float* x, const Pack8<float>& v) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = v.e[j];
+// A granule: 16 bytes of a row, the unit of loads and stores.
+template <typename T> struct Gran {
+    static constexpr int E = 16 / (int)sizeof(T);
+};
+__device__ __forceinline__ void unpack(float* x, const uint4& q, const float*) {
+    x[0] = __uint_as_float(q.x), x[1] = __uint_as_float(q.y), x[2] = __uint_as_float(q.z), x[3] = __uint_as_float(q.w);
 }
-__device__ __forceinline__ void unpack8(float* x, const Pack8<__nv_bfloat16>& v) {
+__device__ __forceinline__ void unpack(float* x, const uint4& q, const __nv_bfloat16*) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        x[2 * j] = __uint_as_float(v.w[j] << 16);
-        x[2 * j + 1] = __uint_as_float(v.w[j] & 0xffff0000u);
+        x[2 * j] = __uint_as_float(w[j] << 16);
+        x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
     }
 }
-__device__ __forceinline__ void unpack8(float* x, const Pack8<__half>& v) {
+__device__ __forceinline__ void unpack(float* x, const uint4& q, const __half*) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = __half2float(v.e[j]);
-}
-__device__ __forceinline__ float max8(const float* x) {
-    return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-}
-__device__ __forceinline__ bool any_nan8(const float* x) {
-    float s = 0.f;   // a NaN survives a product with zero, infinities become NaN too (and are looked at)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) s = fmaf(x[j], 0.f, s);
-    return s != s;
-}
-
-// Sum of 2^((x - m) c) with the largest x so far, m, as its reference.
-struct Mass {
-    float m, s;
-    __device__ __forceinline__ void clear() { m = -infinity(), s = 0.f; }
-    __device__ __forceinline__ float base() const { return m == -infinity() ? 0.f : m; }
-    __device__ __forceinline__ void add8(const float* x, float c) {
-        const float top = max8(x);
-        if (top > m) {
-            s *= exp2_fast((m - top) * c);
-            m = top;
-        }
-        const float b = base();
-        const unsigned long long off = pair(-b, -b), cc = pair(c, c);
-        unsigned long long sum = 0;
-#pragma unroll
-        for (int j = 0; j < 8; j += 2) {
-            float u, v;
-            unpair(u, v, mul2(add2(pair(x[j], x[j + 1]), off), cc));
-            sum = add2(sum, pair(exp2_fast(u), exp2_fast(v)));
-        }
-        float u, v;
-        unpair(u, v, sum);
-        s += u + v;
+    for (int j = 0; j < 4; ++j) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
+        x[2 * j] = f.x, x[2 * j + 1] = f.y;
     }
-    __device__ __forceinline__ void join(float om, float os, float c) {
-        const float top = fmaxf(m, om), b = top == -infinity() ? 0.f : top;
-        s = s * exp2_fast((m - b) * c) + os * exp2_fast((om - b) * c);
-        m = top;
-    }
-    __device__ __forceinline__ void warp(float c) {   // every lane gets the warp's
+}
+__device__ __forceinline__ uint4 pack(const float* x, const float*) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+}
+template <typename P, typename F> __device__ __forceinline__ uint4 pack_pairs(const float* x, F two) {
+    uint32_t w[4];
 #pragma unroll
-        for (int d = 16; d; d >>= 1) {
-            const float om = __shfl_xor_sync(0xffffffffu, m, d), os = __shfl_xor_sync(0xffffffffu, s, d);
-            join(om, os, c);
-        }
+    for (int j = 0; j < 4; ++j) {
+        const P h = two(x[2 * j], x[2 * j + 1]);
+        w[j] = *reinterpret_cast<const uint32_t*>(&h);
     }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ uint4 pack(const float* x, const __nv_bfloat16*) {
+    return pack_pairs<__nv_bfloat162>(x, [](float a, float b) { return __floats2bfloat162_rn(a, b); });
+}
+__device__ __forceinline__ uint4 pack(const float* x, const __half*) {
+    return pack_pairs<__half2>(x, [](float a, float b) { return __floats2half2_rn(a, b); });
+}
+// Running maxima of granules, two groups of elements apart.  NAN: a NaN is the largest (otherwise it
+// does not count).
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+template <typename T, bool NAN_> struct GranMax;
+template <bool NAN_> struct GranMax<float, NAN_> {
+    float m0 = -__builtin_huge_valf(), m1 = -__builtin_huge_valf();
+    static __device__ __forceinline__ float max2(float a, float b) { return NAN_ ? max_nan(a, b) : fmaxf(a, b); }
+    __device__ __forceinline__ void add(const uint4& q) {
+        m0 = max2(m0, max2(__uint_as_float(q.x), __uint_as_float(q.y)));
+        m1 = max2(m1, max2(__uint_as_float(q.z), __uint_as_float(q.w)));
+    }
+    __device__ __forceinline__ void add(const GranMax& o) { m0 = max2(m0, o.m0), m1 = max2(m1, o.m1); }
+    __device__ __forceinline__ float first() const { return m0; }
+    __device__ __forceinline__ float second() const { return m1; }
+    __device__ __forceinline__ float get() const { return max2(m0, m1); }
+};
+template <typename T2, typename F> __device__ __forceinline__ uint32_t on_words(uint32_t a, uint32_t b, F f) {
+    const T2 r = f(*reinterpret_cast<const T2*>(&a), *reinterpret_cast<const T2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+template <typename T, typename T2, bool NAN_> struct WordMax {
+    uint32_t w;
+    static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+        return on_words<T2>(a, b, [](T2 x, T2 y) { return NAN_ ? __hmax2_nan(x, y) : __hmax2(x, y); });
+    }
+    __device__ __forceinline__ void add(const uint4& q) { w = max2(max2(w, max2(q.x, q.y)), max2(q.z, q.w)); }
+    __device__ __forceinline__ void add(const WordMax& o) { w = max2(w, o.w); }
+    __device__ __forceinline__ float get() const { return NAN_ ? max_nan(first(), second()) : fmaxf(first(), second()); }
+    __device__ __forceinline__ float first() const { return to_float(reinterpret_cast<const T*>(&w)[0]); }
+    __device__ __forceinline__ float second() const { return to_float(reinterpret_cast<const T*>(&w)[1]); }
+};
+template <bool NAN_> struct GranMax<__nv_bfloat16, NAN_> : WordMax<__nv_bfloat16, __nv_bfloat162, NAN_> {
+    __device__ __forceinline__ GranMax() { this->w = 0xff80ff80u; }
+};
+template <bool NAN_> struct GranMax<__half, NAN_> : WordMax<__half, __half2, NAN_> {
+    __device__ __forceinline__ GranMax() { this->w = 0xfc00fc00u; }
 };
 
-// A segment of a row: up to 7 single elements, whole vectors of 8 from a 16-byte boundary on, up to
-// 7 single elements.
-template <typename T> struct Segment {
-    const T* p;
-    int first, n;        // element of the row that p points at, elements
-    int head, vecs;      // single elements in front, vectors
-    __device__ Segment(const T* row, int lo, int hi) : p(row + lo), first(lo), n(hi - lo) {
-        head = min(n, (int)((16u - ((uint32_t)(uintptr_t)p & 15u)) & 15u) / (int)sizeof(T));
-        vecs = (n - head) / 8;
+// x c - m c for x near or below m, ready for 2^: in one rounding of the product's difference where |m c|
+// is moderate (NEAR; what the rounded m c lacks is returned by `lack` and made up for once per sum),
+// else from the difference of the logits, which stays exact for logits of any size (a type's lowest
+// value as a mask).
+constexpr float kNear = 1048576.f;
+template <bool NEAR> struct Scale {
+    unsigned long long mul, off;
+    __device__ __forceinline__ Scale(float m, float c) : mul(pair(c, c)) {
+        const float o = NEAR ? -__fmul_rn(m, c) : -m;
+        off = pair(o, o);
     }
-    __device__ int tail() const { return n - head - 8 * vecs; }
-    __device__ void load(Pack8<T>& v, int i) const {
-        const uint4* q = reinterpret_cast<const uint4*>(p + head + 8LL * i);
+    __device__ __forceinline__ unsigned long long two(unsigned long long x) const {
+        return NEAR ? fma2(x, mul, off) : mul2(add2(x, off), mul);
+    }
+    static __device__ __forceinline__ float lack(float m, float c) { return NEAR ? fmaf(m, c, -__fmul_rn(m, c)) : 0.f; }
+};
+
+// sum += 2^(...) over a granule
+template <int E, bool NEAR> __device__ __forceinline__ void add_powers(unsigned long long& sum, const float* x, const Scale<NEAR>& scale) {
 #pragma unroll
-        for (int j = 0; j < (int)sizeof(T) / 2; ++j) v.q[j] = q[j];   // not the read-only path: a gradient may be written in place
+    for (int j = 0; j < E; j += 2) {
+        float u, v;
+        unpair(u, v, scale.two(pair(x[j], x[j + 1])));
+        sum = add2(sum, pair(exp2_fast(u), exp2_fast(v)));
     }
-    // offset of the single element that thread t takes (threads 0..7 the head, 8..15 the tail), -1: none
-    __device__ int single(int t) const {
-        if (t < 8) return t < head ? t : -1;
-        return t < 16 && t - 8 < tail() ? n - tail() + t - 8 : -1;
+}
+__device__ __forceinline__ float sum_of(unsigned long long p) {
+    float u, v;
+    unpair(u, v, p);
+    return __fadd_rn(u, v);
+}
+__device__ __forceinline__ float warp_max(float v) {
+    float r;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) v = __fadd_rn(v, __shfl_xor_sync(0xffffffffu, v, d));
+    return v;
+}
+
+// Sums of 2^((x - m) c), and with CE2 of 2^((x - m) log2e), with the largest x as their reference.
+// Every operation is rounded by itself wherever this is compiled, so that two calls and one for both
+// give the same bits.
+template <bool CE2> struct Mass {
+    float m = -__builtin_huge_valf(), s = 0.f, s1 = 0.f;
+    __device__ __forceinline__ float base() const { return m == -infinity() ? 0.f : m; }
+    __device__ __forceinline__ void join(float om, float os, float os1, float c) {
+        const float top = fmaxf(m, om), b = top == -infinity() ? 0.f : top;
+        s = fmaf(s, exp2_fast(__fmul_rn(m - b, c)), __fmul_rn(os, exp2_fast(__fmul_rn(om - b, c))));
+        if (CE2) s1 = fmaf(s1, exp2_fast(__fmul_rn(m - b, kLog2e)), __fmul_rn(os1, exp2_fast(__fmul_rn(om - b, kLog2e))));
+        m = top;
+    }
+    // every lane gets the warp's
+    __device__ __forceinline__ void lanes(float c) {
+        const float top = warp_max(m), b = top == -infinity() ? 0.f : top;
+        s = warp_sum(__fmul_rn(s, exp2_fast(__fmul_rn(m - b, c))));
+        if (CE2) s1 = warp_sum(__fmul_rn(s1, exp2_fast(__fmul_rn(m - b, kLog2e))));
+        m = top;
     }
 };
 
@@ -134,6 +195,41 @@ __device__ __forceinline__ int segment_start(int cols, int rank, int size) {
     return min(cols, (int)((long long)units * rank / size) * 64);
 }
 
+// n elements of a row from p on, cut into granules where 16-byte boundaries fall: element i sits in
+// slot `phase` + i, slots that are no elements read as -inf.
+template <typename T> struct Cut {
+    static constexpr int E = Gran<T>::E;
+    const T* p;
+    int n, phase, grans;
+    __device__ __forceinline__ Cut(const T* at, int count) : p(at), n(count) {
+        phase = (int)((uint32_t)(uintptr_t)p & 15u) / (int)sizeof(T);
+        grans = n > 0 ? (phase + n + E - 1) / E : 0;
+    }
+    __device__ __forceinline__ bool whole(int g) const { return g * E >= phase && g * E + E <= phase + n; }
+    // From global memory (not the read-only path: a gradient may be written in place).
+    __device__ __forceinline__ uint4 load(int g) const {
+        if (whole(g)) return *reinterpret_cast<const uint4*>(p - phase + (long long)g * E);
+        uint4 q;
+        T* e = reinterpret_cast<T*>(&q);
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const int i = g * E + j - phase;
+            e[j] = i >= 0 && i < n ? p[i] : from_float<T>(-infinity());
+        }
+        return q;
+    }
+    // Into shared memory, 16 bytes a copy; the copies are waited for by `landed`.
+    __device__ __forceinline__ void stage(T* room) const {
+        for (int g = threadIdx.x; g < grans; g += blockDim.x) {
+            if (whole(g))
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(room + g * E)), "l"(p - phase + (long long)g * E) : "memory");
+            else
+                *reinterpret_cast<uint4*>(room + g * E) = load(g);
+        }
+    }
+};
+__device__ __forceinline__ void landed() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
 // ---- distillation ------------------------------------------------------------------
 
 struct DistillArgs {
@@ -141,6 +237,7 @@ struct DistillArgs {
     void* grad;
     long long rows, stride, grad_stride;
     int cols, k;
+    int room;                  // elements of a row that a block holds at a time
     float temperature, alpha;
     const float* values;       // teacher: rows x k logits
     const int32_t* indices;    // rows x k, negative: slot not used
@@ -162,93 +259,134 @@ struct RowStats {
     float others, log_others, top, log_whole, high, log_total, log_whole1, coef;
 };
 
-struct DistillShared {
-    float m[32], s[32], s1[32];
-    RowStats row;
+// Gradients of a row's elements.
+template <typename T, bool CE2> struct Slope {
+    RowStats r;
+    float c, inv, kl, ce, coef;
+    __device__ __forceinline__ Slope(const DistillArgs& a, const RowStats& stats, float g, bool label) : r(stats) {
+        c = kLog2e / a.temperature, inv = 1.f / a.temperature;
+        kl = __fmul_rn(g, __fmul_rn(a.alpha, a.temperature));
+        ce = label && r.log_whole1 < infinity() ? __fmul_rn(g, 1.f - a.alpha) : 0.f;
+        coef = __fmul_rn(g, r.coef);
+    }
+    __device__ __forceinline__ bool near() const {
+        return fmaxf(fabsf(r.others), fabsf(r.top)) * fmaxf(c, kLog2e) < kNear;
+    }
+    // Elements of granules, two at a time: y = coef 2^(..) / others' sum, + ce 2^(..) / the whole's
+    template <bool NEAR> struct Granules {
+        Scale<NEAR> scale, scale1;
+        unsigned long long by, by1;
+        __device__ __forceinline__ Granules(const Slope& s) : scale(s.r.others, s.c), scale1(s.r.top, kLog2e) {
+            const float k = __fmul_rn(s.coef, exp2_fast(-Scale<NEAR>::lack(s.r.others, s.c) - s.r.log_others));
+            const float k1 = __fmul_rn(s.ce, exp2_fast(-Scale<NEAR>::lack(s.r.top, kLog2e) - s.r.log_whole1));
+            by = pair(k, k), by1 = pair(k1, k1);
+        }
+        __device__ __forceinline__ unsigned long long two(unsigned long long z) const {
+            float u, v;
+            unpair(u, v, scale.two(z));
+            unsigned long long y = mul2(by, pair(exp2_fast(u), exp2_fast(v)));
+            if (CE2) {
+                unpair(u, v, scale1.two(z));
+                y = fma2(by1, pair(exp2_fast(u), exp2_fast(v)), y);
+            }
+            return y;
+        }
+        __device__ __forceinline__ uint4 granule(const uint4& q) const {
+            constexpr int E = Gran<T>::E;
+            float x[E];
+            unpack(x, q, (const T*)nullptr);
+#pragma unroll
+            for (int j = 0; j < E; j += 2) unpair(x[j], x[j + 1], two(pair(x[j], x[j + 1])));
+            return pack(x, (const T*)nullptr);
+        }
+    };
+    template <typename F> __device__ __forceinline__ void granules(F f) const {
+        if (near())
+            f(Granules<true>(*this));
+        else
+            f(Granules<false>(*this));
+    }
+    // The label's, where the teacher did not send it.
+    __device__ __forceinline__ float unsent_label(float z) const {
+        float y = 0.f;
+        granules([&](const auto& g) {
+            float v;
+            unpair(y, v, g.two(pair(z, z)));
+        });
+        return y - ce;
+    }
+    __device__ __forceinline__ float sent(float z, float t, bool is_label) const {
+        const float q = exp2_fast(fmaf(z - r.top, c, -r.log_whole)), p = exp2_fast(fmaf(__fmul_rn(t, inv) - r.high, kLog2e, -r.log_total));
+        float v = __fmul_rn(kl, q - p);
+        if (ce != 0.f) v = fmaf(ce, exp2_fast(fmaf(z - r.top, kLog2e, -r.log_whole1)) - (is_label ? 1.f : 0.f), v);
+        return v;
+    }
 };
 
-// dL/dz of a segment.  sent_*: the row's sent words (shared memory), whose elements are written after all others.
-template <typename T, bool CE2>
-__device__ __forceinline__ void write_gradient(const DistillArgs& a, long long row, const Segment<T>& seg, const RowStats& r, const int* sent_at,
-                                               const float* sent_t, const float* sent_z, int label, float label_z) {
-    const int t = threadIdx.x, threads = blockDim.x;
-    const float g = a.grad_loss ? a.grad_loss[row] : 1.f;
-    const float c = kLog2e / a.temperature, inv = 1.f / a.temperature;
-    const float coef = g * r.coef, kl = g * a.alpha * a.temperature;
-    const float ce = label >= 0 && r.log_whole1 < infinity() ? g * (1.f - a.alpha) : 0.f;
-    T* out = static_cast<T*>(a.grad) + row * a.grad_stride + seg.first;
-    const auto off = [&](float z) {
-        float v = coef * exp2_fast(fmaf(z - r.others, c, -r.log_others));
-        if (CE2) v += ce * exp2_fast(fmaf(z - r.top, kLog2e, -r.log_whole1));
-        return v;
-    };
-    const bool wide = (((uintptr_t)(out + seg.head)) & 15) == 0;
-    for (int i = t; i < seg.vecs; i += threads) {
-        Pack8<T> v;
-        seg.load(v, i);
+// Writes granule g of a cut to `out` (where the cut's first element goes).
+template <typename T> __device__ __forceinline__ void store_granule(T* out, const Cut<T>& cut, int g, const uint4& q, bool wide) {
+    constexpr int E = Gran<T>::E;
+    const int i0 = g * E - cut.phase;
+    if (wide && cut.whole(g)) {
+        *reinterpret_cast<uint4*>(out + i0) = q;
+        return;
+    }
+    const T* e = reinterpret_cast<const T*>(&q);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v.e[j] = from_float<T>(off(to_float(v.e[j])));
-        store8(out + seg.head + 8LL * i, v, 8, wide ? 16 : (int)sizeof(T));
-    }
-    const int one = seg.single(t);
-    if (one >= 0) out[one] = from_float<T>(off(to_float(seg.p[one])));
-    __syncthreads();
-    bool has_label = false;
-    for (int k = t; k < a.k; k += threads) {
-        const int at = sent_at[k];
-        if (at < 0) continue;
-        if (at == label) has_label = true;
-        const int i = at - seg.first;
-        if (i < 0 || i >= seg.n) continue;
-        const float z = sent_z[k];
-        const float q = exp2_fast(fmaf(z - r.top, c, -r.log_whole));
-        const float p = exp2_fast(fmaf(sent_t[k] * inv - r.high, kLog2e, -r.log_total));
-        float v = kl * (q - p);
-        if (ce != 0.f) v += ce * (exp2_fast(fmaf(z - r.top, kLog2e, -r.log_whole1)) - (at == label ? 1.f : 0.f));
-        out[i] = from_float<T>(v);
-    }
-    has_label = __syncthreads_or(has_label);
-    if (t == 0 && label >= seg.first && label < seg.first + seg.n && !has_label && ce != 0.f)
-        out[label - seg.first] = from_float<T>(off(label_z) - ce);
+    for (int j = 0; j < E; ++j)
+        if (i0 + j >= 0 && i0 + j < cut.n) out[i0 + j] = e[j];
+}
+template <typename T> __device__ __forceinline__ bool same_phase(const T* out, const Cut<T>& cut) {
+    return ((uint32_t)(uintptr_t)out & 15u) == (uint32_t)cut.phase * sizeof(T);
 }
 
-// One row per cluster.  Shared memory: a bit per element of the segment that the teacher sent, then the
-// sent words.
-template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(1024) k_distill(DistillArgs a) {
-    extern __shared__ uint32_t dyn[];
+// After all other elements of a segment are written: the sent words', and a label's that was not sent.
+// words: elements of this segment at sent_at (negative: none of this block's).
+template <typename T, typename S>
+__device__ __forceinline__ void write_sent(T* out, const S& slope, int first, int n, int k, const int* sent_at, const float* sent_t,
+                                           const float* sent_z, int label, float label_z) {
+    bool has_label = false;
+    for (int i = threadIdx.x; i < k; i += blockDim.x) {
+        const int at = sent_at[i];
+        if (at < 0) continue;
+        has_label |= at == label;
+        out[at - first] = from_float<T>(slope.sent(sent_z[i], sent_t[i], at == label));
+    }
+    has_label = __syncthreads_or(has_label);
+    if (threadIdx.x == 0 && label >= first && label < first + n && !has_label && slope.ce != 0.f)
+        out[label - first] = from_float<T>(slope.unsent_label(label_z));
+}
+
+constexpr int kDistillThreads = 512, kDistillWarps = kDistillThreads / 32;
+
+struct DistillShared {
+    float om[kDistillWarps], os[kDistillWarps], os1[kDistillWarps];  // a warp's mass of words that were not sent
+    float sm[kDistillWarps], ss[kDistillWarps], ss1[kDistillWarps];  // ... that were
+    float tm[kDistillWarps], ts[kDistillWarps];                      // ... of the teacher's sent words (natural units)
+    float kl[kDistillWarps], kl_block;
+};
+
+// One row per cluster; a block keeps its segment in shared memory, with the sent words taken out (-inf),
+// so the sum over the others is a plain one.  Segments that do not fit are taken in parts, twice.
+template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDistillThreads, 2) k_distill(DistillArgs a) {
+    extern __shared__ __align__(16) uint8_t dyn[];
     __shared__ DistillShared sh;
+    constexpr int E = Gran<T>::E;
     const int t = threadIdx.x, threads = blockDim.x, warp = t >> 5, lane = t & 31, warps = threads >> 5;
     const int size = (int)cluster_size(), rank = (int)cluster_rank();
     const long long row = blockIdx.x / size;
     const T* z = static_cast<const T*>(a.logits) + row * a.stride;
-    const Segment<T> seg(z, segment_start(a.cols, rank, size), segment_start(a.cols, rank + 1, size));
-    const int words = (((a.cols + 63) / 64 + size - 1) / size * 64 + 64) / 32;  // the longest segment's, and the shift of the head
-    uint8_t* bits = reinterpret_cast<uint8_t*>(dyn);
-    int* sent_at = reinterpret_cast<int*>(dyn + words);
-    float* sent_t = reinterpret_cast<float*>(sent_at + a.k);
+    const int first = segment_start(a.cols, rank, size), n = segment_start(a.cols, rank + 1, size) - first;
+    T* held = reinterpret_cast<T*>(dyn);
+    float* sent_t = reinterpret_cast<float*>(dyn + (size_t)(a.room + 2 * E) * sizeof(T));
     float* sent_z = sent_t + a.k;
-    const float c = kLog2e / a.temperature;
+    int* sent_at = reinterpret_cast<int*>(sent_z + a.k);
+    const float c = kLog2e / a.temperature, inv = 1.f / a.temperature;
+    const int parts = n > a.room ? (n + a.room - 1) / a.room : 1;
 
-    for (int i = t; i < words; i += threads) dyn[i] = 0;
-    __syncthreads();
-    for (int k = t; k < a.k; k += threads) {
-        int at = a.indices[row * a.k + k];
-        const float tv = a.values[row * a.k + k];
-        if (at >= a.cols) {
-            if (a.status && rank == 0) atomicOr(a.status, SBC_STATUS_RANGE);
-            at = -1;
-        }
-        float zv = -infinity();
-        if (at >= 0) {
-            zv = to_float(z[at]);
-            const int i = at - seg.first;
-            // bit 8 + (offset from the first vector): a vector's bits are one byte, the head's are byte 0
-            if (i >= 0 && i < seg.n) atomicOr(&dyn[(i - seg.head + 8) >> 5], 1u << ((i - seg.head + 8) & 31));
-        }
-        sent_at[k] = at;
-        sent_t[k] = at >= 0 ? tv : -infinity();
-        sent_z[k] = zv;
-    }
+    Cut<T> cut(z + first, min(n, a.room));
+    cut.stage(held);
+    // the teacher, while the logits are on their way
     long long label_in = a.labels ? a.labels[row] : -1;
     if (label_in >= a.cols) {
         if (a.status && rank == 0 && t == 0) atomicOr(a.status, SBC_STATUS_RANGE);
@@ -256,201 +394,208 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(102
     }
     const int label = label_in < 0 ? -1 : (int)label_in;
     const float label_z = label >= 0 ? to_float(z[label]) : 0.f;
-    __syncthreads();
+    const float rest = a.rest ? a.rest[row] : -infinity();
+    const float g = GRAD && a.grad_loss ? a.grad_loss[row] : 1.f;
+    Mass<false> teacher;
+    for (int i = t; i < a.k; i += threads) {
+        int at = a.indices[row * a.k + i];
+        const float tv = a.values[row * a.k + i];
+        if (at >= a.cols) {
+            if (a.status && rank == 0) atomicOr(a.status, SBC_STATUS_RANGE);
+            at = -1;
+        }
+        const bool here = at >= first && at < first + n;
+        sent_at[i] = here ? at : -1;
+        sent_t[i] = at >= 0 ? tv : -infinity();
+        if (at >= 0) teacher.join(__fmul_rn(tv, inv), 1.f, 0.f, kLog2e);
+    }
+    teacher.lanes(kLog2e);
+    if (lane == 0) sh.tm[warp] = teacher.m, sh.ts[warp] = teacher.s;
 
-    // the student's mass outside the sent words
-    float m = -infinity(), base = 0.f, s = 0.f, s1 = 0.f;
-    const auto take = [&](float* x) {
-        float top = x[0];
-#pragma unroll
-        for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
-        if (top > m) {
-            s *= exp2_fast((m - top) * c);
-            if (CE2) s1 *= exp2_fast((m - top) * kLog2e);
-            m = base = top;
+    Mass<CE2> others, sent;
+    for (int part = 0; part < parts; ++part) {
+        const int lo = part * a.room;
+        if (part > 0) {
+            __syncthreads();
+            cut = Cut<T>(z + first + lo, min(n - lo, a.room));
+            cut.stage(held);
         }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            s += exp2_fast((x[j] - base) * c);
-            if (CE2) s1 += exp2_fast((x[j] - base) * kLog2e);
+        landed();
+        __syncthreads();
+        for (int i = t; i < a.k; i += threads) {
+            const int at = sent_at[i] - first - lo;
+            if (sent_at[i] < 0 || at < 0 || at >= cut.n) continue;
+            const float zv = to_float(held[cut.phase + at]);
+            held[cut.phase + at] = from_float<T>(-infinity());
+            sent_z[i] = zv;
+            sent.join(zv, 1.f, 1.f, c);
         }
-    };
-    for (int i = t; i < seg.vecs; i += threads) {
-        Pack8<T> v;
-        seg.load(v, i);
-        const uint32_t sent = bits[i + 1];
-        float x[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = to_float(v.e[j]);
-        if (sent) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (sent >> j & 1) x[j] = -infinity();
-        }
-        take(x);
+        __syncthreads();
+        GranMax<T, false> top;
+        for (int i = t; i < cut.grans; i += threads) top.add(*reinterpret_cast<const uint4*>(held + i * E));
+        Mass<CE2> mine;
+        mine.m = top.get();
+        const float base = mine.base();
+        const auto add_all = [&](const auto& scale, const auto& scale1) {
+            unsigned long long sum = 0, sum1 = 0;
+            for (int i = t; i < cut.grans; i += threads) {
+                float x[E];
+                unpack(x, *reinterpret_cast<const uint4*>(held + i * E), (const T*)nullptr);
+                add_powers<E>(sum, x, scale);
+                if (CE2) add_powers<E>(sum1, x, scale1);
+            }
+            mine.s = __fmul_rn(sum_of(sum), exp2_fast(-scale.lack(base, c)));
+            if (CE2) mine.s1 = __fmul_rn(sum_of(sum1), exp2_fast(-scale1.lack(base, kLog2e)));
+        };
+        if (fabsf(base) * fmaxf(c, kLog2e) < kNear)
+            add_all(Scale<true>(base, c), Scale<true>(base, kLog2e));
+        else
+            add_all(Scale<false>(base, c), Scale<false>(base, kLog2e));
+        if (parts == 1)
+            others = mine;
+        else
+            others.join(mine.m, mine.s, mine.s1, c);
     }
-    const int one = seg.single(t);
-    if (one >= 0) {
-        const int b = one - seg.head + 8;
-        float x[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = -infinity();
-        if (!(dyn[b >> 5] >> (b & 31) & 1)) x[0] = to_float(seg.p[one]);
-        take(x);
-    }
-    // a warp's, a block's and a cluster's mass
-    const auto join = [&](float om, float os, float os1) {
-        const float top = fmaxf(m, om), base = top == -infinity() ? 0.f : top;
-        s = s * exp2_fast((m - base) * c) + os * exp2_fast((om - base) * c);
-        if (CE2) s1 = s1 * exp2_fast((m - base) * kLog2e) + os1 * exp2_fast((om - base) * kLog2e);
-        m = top;
-    };
-#pragma unroll
-    for (int d = 16; d; d >>= 1) {
-        const float om = __shfl_xor_sync(0xffffffffu, m, d), os = __shfl_xor_sync(0xffffffffu, s, d);
-        join(om, os, CE2 ? __shfl_xor_sync(0xffffffffu, s1, d) : 0.f);
-    }
+    others.lanes(c);
+    sent.lanes(c);
     if (lane == 0) {
-        sh.m[warp] = m;
-        sh.s[warp] = s;
-        sh.s1[warp] = s1;
+        sh.om[warp] = others.m, sh.os[warp] = others.s, sh.os1[warp] = others.s1;
+        sh.sm[warp] = sent.m, sh.ss[warp] = sent.s, sh.ss1[warp] = sent.s1;
     }
     if (size > 1)
         cluster_sync();
     else
         __syncthreads();
-    if (warp == 0) {
-        m = -infinity(), s = 0.f, s1 = 0.f;
-        for (int i = lane; i < warps * size; i += 32) {
-            const uint32_t r = (uint32_t)(i / warps), w = (uint32_t)(i % warps);
-            if (size > 1)
-                join(ld_cluster(map_rank(smem_u32(&sh.m[w]), r)), ld_cluster(map_rank(smem_u32(&sh.s[w]), r)),
-                     ld_cluster(map_rank(smem_u32(&sh.s1[w]), r)));
-            else
-                join(sh.m[w], sh.s[w], sh.s1[w]);
-        }
-#pragma unroll
-        for (int d = 16; d; d >>= 1) {
-            const float om = __shfl_xor_sync(0xffffffffu, m, d), os = __shfl_xor_sync(0xffffffffu, s, d);
-            join(om, os, CE2 ? __shfl_xor_sync(0xffffffffu, s1, d) : 0.f);
-        }
-        // the sent words: maxima, then sums, then the divergence
-        const float inv = 1.f / a.temperature;
-        const float rest = a.rest ? a.rest[row] : -infinity();
-        float top = m, high = rest;
-        for (int k = lane; k < a.k; k += 32) {
-            top = fmaxf(top, sent_z[k]);
-            high = fmaxf(high, sent_t[k] * inv);
-        }
-#pragma unroll
-        for (int d = 16; d; d >>= 1) {
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-            high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, d));
-        }
-        const bool seen = top > -infinity(), taught = high > -infinity();
-        const float top0 = seen ? top : 0.f, high0 = taught ? high : 0.f;
-        float mass = 0.f, mass1 = 0.f, total = 0.f;
-        for (int k = lane; k < a.k; k += 32) {
-            mass += exp2_fast((sent_z[k] - top0) * c);
-            mass1 += exp2_fast((sent_z[k] - top0) * kLog2e);
-            total += exp2_fast((sent_t[k] * inv - high0) * kLog2e);
-        }
-#pragma unroll
-        for (int d = 16; d; d >>= 1) {
-            mass += __shfl_xor_sync(0xffffffffu, mass, d);
-            mass1 += __shfl_xor_sync(0xffffffffu, mass1, d);
-            total += __shfl_xor_sync(0xffffffffu, total, d);
-        }
-        total += exp2_fast((rest - high0) * kLog2e);
-        const float away = s * exp2_fast((m - top0) * c);   // mass outside, below top (none: 0 * 0)
-        const float whole = away + mass;
-        const float whole1 = (CE2 ? s1 * exp2_fast((m - top0) * kLog2e) : s * exp2_fast((m - top0) * kLog2e)) + mass1;
-        const float q_r = away / whole, p_r = exp2_fast((rest - high0) * kLog2e) / total;
-        const float shift = (high0 - top0 * inv) + (logf(total) - logf(whole));
-        // p d - p + q, every term positive; p (exp(-d) - 1 + d) keeps a small d's digits
-        const auto term = [](float p, float q, float d) {
-            if (!(p > 0.f)) return q;
-            return fabsf(d) < 0.5f ? p * (expm1f(-d) + d) : p * d - p + q;
-        };
-        float kl = 0.f;
-        for (int k = lane; k < a.k; k += 32) {
-            if (sent_at[k] < 0) continue;
-            const float p = exp2_fast((sent_t[k] * inv - high0) * kLog2e) / total, q = exp2_fast((sent_z[k] - top0) * c) / whole;
-            kl += term(p, q, (sent_t[k] - sent_z[k]) * inv - shift);
-        }
-#pragma unroll
-        for (int d = 16; d; d >>= 1) kl += __shfl_xor_sync(0xffffffffu, kl, d);
-        kl += term(p_r, q_r, ((rest - m * inv) - logf(s)) - shift);
-        const float ce_weight = label >= 0 && seen ? 1.f - a.alpha : 0.f;
-        const bool live = seen && taught;
-        if (lane == 0) {
-            float loss = live ? a.alpha * a.temperature * a.temperature * kl : (whole != whole || total != total) ? whole + total : 0.f;
-            if (ce_weight != 0.f) loss += ce_weight * (logf(whole1) - (label_z - top0));
-            RowStats r;
-            r.others = m == -infinity() ? 0.f : m;
-            r.log_others = s == 0.f ? infinity() : log2f(s);
-            r.top = top0;
-            r.log_whole = live ? log2f(whole) : infinity();
-            r.high = high0;
-            r.log_total = live ? log2f(total) : infinity();
-            r.log_whole1 = seen ? log2f(whole1) : infinity();
-            r.coef = (live ? a.alpha * a.temperature * (q_r - p_r) : 0.f) + (!CE2 && ce_weight != 0.f ? ce_weight * q_r : 0.f);
-            sh.row = r;
-            if (rank == 0) {
-                if (a.loss) a.loss[row] = loss;
-                if (a.stats) {
-                    float4* st = reinterpret_cast<float4*>(a.stats + row * kDistillStats);
-                    st[0] = make_float4(r.others, r.log_others, r.top, r.log_whole);
-                    st[1] = make_float4(r.high, r.log_total, r.log_whole1, r.coef);
-                }
-            }
-        }
+    // every warp puts the parts together for itself
+    others = Mass<CE2>(), sent = Mass<CE2>(), teacher = Mass<false>();
+    for (int i = lane; i < warps * size; i += 32) {
+        const uint32_t r = (uint32_t)(i / warps), w = (uint32_t)(i % warps);
+        const auto at = [&](float* p) { return size > 1 ? ld_cluster(map_rank(smem_u32(p), r)) : *p; };
+        others.join(at(&sh.om[w]), at(&sh.os[w]), CE2 ? at(&sh.os1[w]) : 0.f, c);
+        sent.join(at(&sh.sm[w]), at(&sh.ss[w]), CE2 ? at(&sh.ss1[w]) : 0.f, c);
     }
+    if (lane < warps) teacher.m = sh.tm[lane], teacher.s = sh.ts[lane];
+    others.lanes(c), sent.lanes(c), teacher.lanes(kLog2e);
+    const float m = others.m, s = others.s;
+    teacher.join(rest, 1.f, 0.f, kLog2e);
+    Mass<CE2> all = others;
+    all.join(sent.m, sent.s, sent.s1, c);
+    const bool seen = all.m > -infinity(), taught = teacher.m > -infinity();
+    const float top = all.base(), high = teacher.base(), whole = all.s, total = teacher.s;
+    const float whole1 = CE2 ? all.s1 : whole;
+    const float q_r = s * exp2_fast((m - top) * c) / whole, p_r = exp2_fast((rest - high) * kLog2e) / total;
+    const float ce_weight = label >= 0 && seen ? 1.f - a.alpha : 0.f;
+    const bool live = seen && taught;
+    RowStats r;
+    r.others = others.base();
+    r.log_others = s == 0.f ? infinity() : log2f(s);
+    r.top = top;
+    r.log_whole = live ? log2f(whole) : infinity();
+    r.high = high;
+    r.log_total = live ? log2f(total) : infinity();
+    r.log_whole1 = seen ? log2f(whole1) : infinity();
+    r.coef = __fadd_rn(live ? __fmul_rn(a.alpha * a.temperature, q_r - p_r) : 0.f, !CE2 && ce_weight != 0.f ? __fmul_rn(ce_weight, q_r) : 0.f);
+    if (s != s) r.coef = s;   // a NaN among the others is everybody's
+    T* out = nullptr;
+    const Slope<T, CE2> slope(a, r, g, label >= 0);
     if (GRAD) {
-        __syncthreads();
-        const RowStats r = sh.row;
-        // an in-place gradient may not overtake another block's reading of the sent words
-        if (size > 1) cluster_sync();
-        write_gradient<T, CE2>(a, row, seg, r, sent_at, sent_t, sent_z, label, label_z);
-    } else if (size > 1) {
-        cluster_sync();   // the blocks' partial sums are read from each other's shared memory
+        out = static_cast<T*>(a.grad) + row * a.grad_stride + first;
+        for (int part = 0; part < parts; ++part) {
+            const int lo = part * a.room;
+            if (parts > 1) {
+                __syncthreads();
+                cut = Cut<T>(z + first + lo, min(n - lo, a.room));
+                cut.stage(held);
+                landed();
+                __syncthreads();
+            }
+            const bool wide = same_phase(out + lo, cut);
+            slope.granules([&](const auto& gr) {
+                for (int i = t; i < cut.grans; i += threads)
+                    store_granule(out + lo, cut, i, gr.granule(*reinterpret_cast<const uint4*>(held + i * E)), wide);
+            });
+        }
     }
+    // the divergence: p d - p + q over the outcomes, d = log p - log q; every term is positive, and
+    // p (exp(-d) - 1 + d) keeps a small d's digits
+    const float shift = (high - top * inv) + (logf(total) - logf(whole));
+    const auto term = [](float p, float q, float d) {
+        if (!(p > 0.f)) return q;
+        return fabsf(d) < 0.5f ? p * (expm1f(-d) + d) : p * d - p + q;
+    };
+    float kl = 0.f;
+    for (int i = t; i < a.k; i += threads) {
+        if (sent_at[i] < 0) continue;
+        const float p = exp2_fast((__fmul_rn(sent_t[i], inv) - high) * kLog2e) / total, q = exp2_fast((sent_z[i] - top) * c) / whole;
+        kl += term(p, q, (sent_t[i] - sent_z[i]) * inv - shift);
+    }
+    kl = warp_sum(kl);
+    if (lane == 0) sh.kl[warp] = kl;
+    __syncthreads();
+    if (size > 1) {
+        if (t == 0) {
+            kl = 0.f;
+            for (int i = 0; i < warps; ++i) kl += sh.kl[i];
+            sh.kl_block = kl;
+        }
+        cluster_sync();
+    }
+    if (rank == 0 && t == 0) {
+        kl = term(p_r, q_r, ((rest - m * inv) - logf(s)) - shift);
+        if (size > 1)
+            for (int i = 0; i < size; ++i) kl += ld_cluster(map_rank(smem_u32(&sh.kl_block), (uint32_t)i));
+        else
+            for (int i = 0; i < warps; ++i) kl += sh.kl[i];
+        float loss = live ? a.alpha * a.temperature * a.temperature * kl : (whole != whole || total != total) ? whole + total : 0.f;
+        if (ce_weight != 0.f) loss += ce_weight * (logf(whole1) - (label_z - top));
+        a.loss[row] = loss;
+        if (a.stats) {
+            float4* st = reinterpret_cast<float4*>(a.stats + row * SBC_DISTILL_STATS);
+            st[0] = make_float4(r.others, r.log_others, r.top, r.log_whole);
+            st[1] = make_float4(r.high, r.log_total, r.log_whole1, r.coef);
+        }
+    }
+    if (GRAD) write_sent(out, slope, first, n, a.k, sent_at, sent_t, sent_z, label, label_z);
+    if (size > 1) cluster_sync();   // blocks read each other's sums up to here
 }
 
 // The backward call: statistics come from the forward one.  `size` blocks share a row, none needs another.
-template <typename T, bool CE2> __global__ void __launch_bounds__(1024) k_distill_grad(DistillArgs a, int size) {
-    extern __shared__ uint32_t dyn[];
+template <typename T, bool CE2> __global__ void __launch_bounds__(kDistillThreads, 2) k_distill_grad(DistillArgs a, int size) {
+    extern __shared__ uint32_t words[];
     const int t = threadIdx.x, threads = blockDim.x;
     const long long row = blockIdx.x / size;
     const int rank = (int)(blockIdx.x % size);
     const T* z = static_cast<const T*>(a.logits) + row * a.stride;
-    const Segment<T> seg(z, segment_start(a.cols, rank, size), segment_start(a.cols, rank + 1, size));
-    int* sent_at = reinterpret_cast<int*>(dyn);
-    float* sent_t = reinterpret_cast<float*>(sent_at + a.k);
+    const int first = segment_start(a.cols, rank, size), n = segment_start(a.cols, rank + 1, size) - first;
+    const Cut<T> cut(z + first, n);
+    float* sent_t = reinterpret_cast<float*>(words);
     float* sent_z = sent_t + a.k;
-    const float4 lo = *reinterpret_cast<const float4*>(a.stats + row * kDistillStats);
-    const float4 hi = *reinterpret_cast<const float4*>(a.stats + row * kDistillStats + 4);
+    int* sent_at = reinterpret_cast<int*>(sent_z + a.k);
+    const float4 lo = *reinterpret_cast<const float4*>(a.stats + row * SBC_DISTILL_STATS);
+    const float4 hi = *reinterpret_cast<const float4*>(a.stats + row * SBC_DISTILL_STATS + 4);
     const RowStats r = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-    // the words of this segment (the label's place among the sent ones is asked for in every segment)
-    for (int k = t; k < a.k; k += threads) {
-        const int at = a.indices[row * a.k + k];
-        const bool here = at >= seg.first && at < seg.first + seg.n;
-        sent_at[k] = at >= 0 && at < a.cols ? at : -1;
-        sent_t[k] = here ? a.values[row * a.k + k] : 0.f;
-        sent_z[k] = here ? to_float(z[at]) : 0.f;
-    }
     const long long label_in = a.labels ? a.labels[row] : -1;
     const int label = label_in >= 0 && label_in < a.cols ? (int)label_in : -1;
-    const float label_z = label >= seg.first && label < seg.first + seg.n ? to_float(z[label]) : 0.f;
+    const float label_z = label >= first && label < first + n ? to_float(z[label]) : 0.f;
+    for (int i = t; i < a.k; i += threads) {
+        const int at = a.indices[row * a.k + i];
+        const bool here = at >= first && at < first + n;
+        sent_at[i] = here ? at : -1;
+        if (here) sent_t[i] = a.values[row * a.k + i], sent_z[i] = to_float(z[at]);
+    }
+    const Slope<T, CE2> slope(a, r, a.grad_loss ? a.grad_loss[row] : 1.f, label >= 0);
+    __syncthreads();   // an in-place gradient comes after the words are read
+    T* out = static_cast<T*>(a.grad) + row * a.grad_stride + first;
+    const bool wide = same_phase(out, cut);
+    slope.granules([&](const auto& gr) {
+#pragma unroll 4
+        for (int i = t; i < cut.grans; i += threads) store_granule(out, cut, i, gr.granule(cut.load(i)), wide);
+    });
     __syncthreads();
-    write_gradient<T, CE2>(a, row, seg, r, sent_at, sent_t, sent_z, label, label_z);
+    write_sent(out, slope, first, n, a.k, sent_at, sent_t, sent_z, label, label_z);
 }
 
 // ---- the largest logits --------------------------------------------------------------
-
-constexpr int kTopMost = SBC_TOP_MOST;
-constexpr int kTopRoom = 2048;     // candidates that are ranked: at least kTopMost from each of 8 blocks
-constexpr int kTopThreads = 256, kTopWarps = kTopThreads / 32;
 
 struct TopArgs {
     const void* logits;
@@ -462,6 +607,10 @@ struct TopArgs {
     float* rest;
 };
 
+constexpr int kTopRoom = 2048;     // candidates that are ranked: at least SBC_TOP_MOST from each of 8 blocks
+constexpr int kTopBins = 512;
+constexpr int kTopThreads = 512, kTopWarps = kTopThreads / 32;
+
 // Order of values as whole numbers: NaN above everything, -0 as +0.
 __device__ __forceinline__ uint32_t order_key(float x) {
     if (x != x) return 0xffffffffu;
@@ -471,6 +620,7 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 __device__ __forceinline__ float key_value(uint32_t k) {
     return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu));
 }
+constexpr uint32_t kLowestKey = 0x00800000u;   // of the lowest finite number: -inf lies below
 // Larger value first, then lower index.
 __device__ __forceinline__ unsigned long long composite(float x, int index) {
     return (unsigned long long)order_key(x) << 32 | (uint32_t)~index;
@@ -478,68 +628,108 @@ __device__ __forceinline__ unsigned long long composite(float x, int index) {
 
 struct TopShared {
     unsigned long long cand[kTopRoom];
-    uint16_t rank[kTopRoom];
-    unsigned long long best[kTopMost];   // this block's largest, in order
+    unsigned long long best[SBC_TOP_MOST];   // this block's largest, in order
+    uint16_t order[kTopRoom];                // candidates by bin
+    uint32_t bins[kTopBins + 1];             // how many a bin holds, then where it starts
+    uint32_t warp_hi[kTopWarps], warp_lo[kTopWarps];
     float warp_m[2][kTopWarps], warp_s[2][kTopWarps];
     uint32_t warp_bound[kTopWarps];
-    float m, s;                          // mass of what this block does not send, s * 2^((x - m) c)
+    float m, s;                              // mass of what this block does not send
     unsigned long long threshold;
     int count, have;
 };
 
-// f(values, index of the first, how many) for a thread's share of a segment.
-template <typename T, typename F> __device__ __forceinline__ void for_each8(const Segment<T>& seg, F f) {
-    for (int i = threadIdx.x; i < seg.vecs; i += kTopThreads) {
-        Pack8<T> v;
-        seg.load(v, i);
-        float x[8];
-        unpack8(x, v);
-        f(x, seg.first + seg.head + 8 * i, 8);
+// A segment's granules, held in shared memory or read from global memory.
+template <typename T, bool HELD> struct Source {
+    const Cut<T>& cut;
+    T* held;
+    __device__ __forceinline__ uint4 get(int g) const {
+        if (HELD) return *reinterpret_cast<const uint4*>(held + g * Gran<T>::E);
+        return cut.load(g);
     }
-    const int one = seg.single(threadIdx.x);
-    if (one >= 0) {
-        float x[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = -infinity();
-        x[0] = to_float(seg.p[one]);
-        f(x, seg.first + one, 1);
-    }
-}
+};
 
 // The block's mass from every thread's; `turn` keeps two uses in a row apart.
-__device__ __forceinline__ void block_mass(Mass& a, TopShared& sh, int turn, float c) {
-    a.warp(c);
+__device__ __forceinline__ void block_mass(Mass<false>& a, TopShared& sh, int turn, float c) {
+    a.lanes(c);
+    const int warps = blockDim.x >> 5;
     if ((threadIdx.x & 31) == 0) {
         sh.warp_m[turn][threadIdx.x >> 5] = a.m;
         sh.warp_s[turn][threadIdx.x >> 5] = a.s;
     }
     __syncthreads();
-    a.clear();
-    for (int i = 0; i < kTopWarps; ++i) a.join(sh.warp_m[turn][i], sh.warp_s[turn][i], c);
+    a = Mass<false>();
+    for (int i = 0; i < warps; ++i) a.join(sh.warp_m[turn][i], sh.warp_s[turn][i], 0.f, c);
 }
 
-// Ranks sh.cand[0, n) (all different): sh.rank, and the first min(k, n) in order to sh.best.
-__device__ __forceinline__ void rank_candidates(TopShared& sh, int n, int k) {
-    for (int i = threadIdx.x; i < n; i += kTopThreads) {
+// Ranks sh.cand[0, n) (all different): the first min(k, n) in order to sh.best, the others join the mass
+// of what is not sent.  The keys' range is cut into equal bins, largest first; a candidate's rank is its
+// bin's start and how many of the same bin are larger.
+__device__ __forceinline__ void rank_candidates(TopShared& sh, int n, int k, Mass<false>& mass, float c) {
+    const int t = threadIdx.x, threads = blockDim.x, lane = t & 31, warps = threads >> 5;
+    uint32_t hi = 0, lo = 0xffffffffu;
+    for (int i = t; i < n; i += threads) {
+        const uint32_t key = (uint32_t)(sh.cand[i] >> 32);
+        hi = max(hi, key), lo = min(lo, key);
+    }
+    hi = __reduce_max_sync(0xffffffffu, hi), lo = __reduce_min_sync(0xffffffffu, lo);
+    if (lane == 0) sh.warp_hi[t >> 5] = hi, sh.warp_lo[t >> 5] = lo;
+    for (int i = t; i <= kTopBins; i += threads) sh.bins[i] = 0;
+    __syncthreads();
+    for (int i = 0; i < warps; ++i) hi = max(hi, sh.warp_hi[i]), lo = min(lo, sh.warp_lo[i]);
+    const int shift = max(0, 32 - __clz((int)(hi - lo)) - 9);   // 2^9 bins
+    uint32_t slot[kTopRoom / 128];
+#pragma unroll
+    for (int j = 0; j < kTopRoom / 128; ++j) {
+        const int i = t + j * threads;
+        if (i < n) slot[j] = atomicAdd(&sh.bins[(hi - (uint32_t)(sh.cand[i] >> 32)) >> shift], 1u);
+    }
+    __syncthreads();
+    if (t < 32) {
+        uint32_t count[kTopBins / 32], sum = 0;
+#pragma unroll
+        for (int b = 0; b < kTopBins / 32; ++b) {
+            count[b] = sum;
+            sum += sh.bins[lane * (kTopBins / 32) + b];
+        }
+        uint32_t upto = sum;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const uint32_t o = __shfl_up_sync(0xffffffffu, upto, d);
+            if (lane >= d) upto += o;
+        }
+#pragma unroll
+        for (int b = 0; b < kTopBins / 32; ++b) sh.bins[lane * (kTopBins / 32) + b] = upto - sum + count[b];
+        if (lane == 31) sh.bins[kTopBins] = upto;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kTopRoom / 128; ++j) {
+        const int i = t + j * threads;
+        if (i < n) sh.order[sh.bins[(hi - (uint32_t)(sh.cand[i] >> 32)) >> shift] + slot[j]] = (uint16_t)i;
+    }
+    __syncthreads();
+    for (int i = t; i < n; i += threads) {
         const unsigned long long mine = sh.cand[i];
-        int r = 0;
-        for (int j = 0; j < n; ++j) r += sh.cand[j] > mine;
-        sh.rank[i] = (uint16_t)r;
-        if (r < k) sh.best[r] = mine;
+        const uint32_t key = (uint32_t)(mine >> 32), bin = (hi - key) >> shift;
+        int r = (int)sh.bins[bin];
+        if (r < k) {
+            const int end = (int)sh.bins[bin + 1];
+            for (int j = (int)sh.bins[bin]; j < end; ++j) r += sh.cand[sh.order[j]] > mine;
+        }
+        if (r < k)
+            sh.best[r] = mine;
+        else
+            mass.join(key_value(key), 1.f, 0.f, c);
     }
     __syncthreads();
 }
 
-// Mass of the ranked candidates that are not sent.
-__device__ __forceinline__ void unsent_mass(Mass& a, const TopShared& sh, int n, int k, float c) {
-    for (int i = threadIdx.x; i < n; i += kTopThreads)
-        if (sh.rank[i] >= k) a.join(key_value((uint32_t)(sh.cand[i] >> 32)), 1.f, c);
-}
-
 // The composite at or above which between k and kTopRoom elements lie: the k-th largest one's leading
 // digits, found digit by digit until few enough elements share them.  For rows whose values crowd at
-// the threshold (ties, masks).
-template <typename T> __device__ __noinline__ unsigned long long exact_threshold(const Segment<T>& seg, TopShared& sh, int k) {
+// the threshold (ties).
+template <typename T> __device__ __noinline__ unsigned long long exact_threshold(const Cut<T>& cut, int first, TopShared& sh, int k) {
+    constexpr int E = Gran<T>::E;
     const int t = threadIdx.x, lane = t & 31;
     uint32_t* hist = reinterpret_cast<uint32_t*>(sh.cand);
     unsigned long long prefix = 0;
@@ -547,14 +737,27 @@ template <typename T> __device__ __noinline__ unsigned long long exact_threshold
     while (shift > 0) {
         const int digit = min(11, shift), upper = shift;
         shift -= digit;
-        for (int i = t; i < 2048; i += kTopThreads) hist[i] = 0;
+        for (int i = t; i < 2048; i += blockDim.x) hist[i] = 0;
         __syncthreads();
-        for_each8(seg, [&](const float* x, int index, int cnt) {
-            for (int j = 0; j < cnt; ++j) {
-                const unsigned long long mine = composite(x[j], index + j);
-                if (upper == 64 || (mine >> upper) == prefix) atomicAdd(&hist[(mine >> shift) & ((1u << digit) - 1)], 1u);
+        for (int g = t; g < cut.grans; g += blockDim.x) {
+            float x[E];
+            unpack(x, cut.load(g), (const T*)nullptr);
+            int bin = -1, times = 0;   // equal neighbours are counted together
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const int i = g * E + j - cut.phase;
+                if (i < 0 || i >= cut.n) continue;
+                const unsigned long long mine = composite(x[j], first + i);
+                if (upper < 64 && (mine >> upper) != prefix) continue;
+                const int b = (int)((mine >> shift) & ((1u << digit) - 1));
+                if (b != bin) {
+                    if (times) atomicAdd(&hist[bin], (uint32_t)times);
+                    bin = b, times = 0;
+                }
+                ++times;
             }
-        });
+            if (times) atomicAdd(&hist[bin], (uint32_t)times);
+        }
         __syncthreads();
         if (t < 32) {
             // 64 bins a lane, from the top
@@ -590,53 +793,93 @@ template <typename T> __device__ __noinline__ unsigned long long exact_threshold
     return prefix << shift;
 }
 
-// Gathers what is at or above the threshold; the mass of everything else.
-template <typename T> __device__ __forceinline__ Mass gather_top(const Segment<T>& seg, TopShared& sh, unsigned long long threshold, float c) {
+// Gathers what is at or above the threshold; returns the thread's mass of everything else.
+template <typename T, bool HELD>
+__device__ __forceinline__ Mass<false> gather_top(const Source<T, HELD>& src, int first, TopShared& sh, unsigned long long threshold, float c) {
+    constexpr int E = Gran<T>::E;
+    const Cut<T>& cut = src.cut;
     const float low = threshold == 0 ? -infinity() : key_value((uint32_t)(threshold >> 32));
-    Mass mass;
-    mass.clear();
-    for_each8(seg, [&](float* x, int index, int n) {
-        if (!(max8(x) < low) || any_nan8(x)) {
+    GranMax<T, true> top;
+    float top_left = -infinity();   // of granules that hold a candidate: what is left
+    for (int g = threadIdx.x; g < cut.grans; g += blockDim.x) {
+        const uint4 q = src.get(g);
+        GranMax<T, true> here;
+        here.add(q);
+        if (here.get() < low) {
+            top.add(here);
+            continue;
+        }
+        float x[E];
+        unpack(x, q, (const T*)nullptr);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (j >= n || x[j] < low) continue;
-                const unsigned long long mine = composite(x[j], index + j);
-                if (mine >= threshold) {
+        for (int j = 0; j < E; ++j) {
+            if (!(x[j] < low)) {
+                const int i = g * E + j - cut.phase;
+                const unsigned long long mine = composite(x[j], first + i);
+                if (mine >= threshold && i >= 0 && i < cut.n) {
                     const int at = atomicAdd(&sh.count, 1);
                     if (at < kTopRoom) sh.cand[at] = mine;
+                    if (HELD) src.held[g * E + j] = from_float<T>(-infinity());
                     x[j] = -infinity();
                 }
             }
+            top_left = fmaxf(top_left, x[j]);
         }
-        mass.add8(x, c);
-    });
+    }
+    Mass<false> mass;
+    mass.m = fmaxf(top.get(), top_left);
+    const float base = mass.base();
+    const auto add_all = [&](const auto& scale) {
+        unsigned long long sum = 0;
+        for (int g = threadIdx.x; g < cut.grans; g += blockDim.x) {
+            const uint4 q = src.get(g);
+            float x[E];
+            unpack(x, q, (const T*)nullptr);
+            if (!HELD) {
+#pragma unroll
+                for (int j = 0; j < E; ++j)
+                    if (!(x[j] < low) && composite(x[j], first + g * E + j - cut.phase) >= threshold) x[j] = -infinity();
+            }
+            add_powers<E>(sum, x, scale);
+        }
+        mass.s = __fmul_rn(sum_of(sum), exp2_fast(-scale.lack(base, c)));
+    };
+    if (fabsf(base) * c < kNear)
+        add_all(Scale<true>(base, c));
+    else
+        add_all(Scale<false>(base, c));
     return mass;
 }
 
-// One row per cluster.  A lower bound of the k-th largest: every warp takes the (k / 8)-th largest of
-// its lanes' maxima (two groups of elements a lane), the least of these has k elements at or above
+// One row per cluster.  A lower bound of the k-th largest: every warp takes the (k / warps)-th largest
+// of its lanes' maxima (two groups of elements a lane), the least of these has k elements at or above
 // it.  What is (little more than k, where values are spread at random) is ranked by comparing all
 // pairs, everything else only adds to the mass.
-template <typename T> __global__ void __launch_bounds__(kTopThreads, 5) k_top_logits(TopArgs a) {
+template <typename T, bool HELD> __global__ void __launch_bounds__(kTopThreads, 2) k_top_logits(TopArgs a) {
+    extern __shared__ __align__(16) uint8_t dyn[];
     __shared__ TopShared sh;
-    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    const int t = threadIdx.x, threads = blockDim.x, lane = t & 31, warp = t >> 5, warps = threads >> 5;
     const int size = (int)cluster_size(), rank = (int)cluster_rank();
     const long long row = blockIdx.x / size;
     const T* z = static_cast<const T*>(a.logits) + row * a.stride;
-    const Segment<T> seg(z, segment_start(a.cols, rank, size), segment_start(a.cols, rank + 1, size));
+    const int first = segment_start(a.cols, rank, size), len = segment_start(a.cols, rank + 1, size) - first;
+    const Cut<T> cut(z + first, len);
+    const Source<T, HELD> src = {cut, reinterpret_cast<T*>(dyn)};
     const float c = kLog2e / a.temperature;
-    const int k = min(a.k, seg.n);
+    const int k = min(a.k, len);
 
     if (t == 0) sh.count = 0;
+    if (HELD) {
+        cut.stage(src.held);
+        landed();
+        __syncthreads();
+    }
     unsigned long long threshold = 0;
-    if (seg.n > kTopThreads) {
-        float m0 = -infinity(), m1 = -infinity();
-        for_each8(seg, [&](const float* x, int, int) {
-            m0 = fmaxf(fmaxf(m0, fmaxf(x[0], x[1])), fmaxf(x[2], x[3]));
-            m1 = fmaxf(fmaxf(m1, fmaxf(x[4], x[5])), fmaxf(x[6], x[7]));
-        });
-        const uint32_t k0 = order_key(m0) >> 16, k1 = order_key(m1) >> 16;
-        const int share = (k + kTopWarps - 1) / kTopWarps;
+    if (len > threads) {
+        GranMax<T, true> top;
+        for (int g = t; g < cut.grans; g += threads) top.add(src.get(g));
+        const uint32_t k0 = order_key(top.first()) >> 16, k1 = order_key(top.second()) >> 16;
+        const int share = (k + warps - 1) / warps;
         uint32_t bound = 0;    // upper half of the threshold's key
         for (uint32_t bit = 0x8000u; bit; bit >>= 1) {
             const uint32_t next = bound | bit;
@@ -644,24 +887,31 @@ template <typename T> __global__ void __launch_bounds__(kTopThreads, 5) k_top_lo
         }
         if (lane == 0) sh.warp_bound[warp] = bound;
         __syncthreads();
-        for (int i = 0; i < kTopWarps; ++i) bound = min(bound, sh.warp_bound[i]);
-        threshold = (unsigned long long)bound << 48;
+        for (int i = 0; i < warps; ++i) bound = min(bound, sh.warp_bound[i]);
+        // -inf is asked for only where nothing else is left
+        threshold = (unsigned long long)max(bound << 16, kLowestKey) << 32;
     }
     __syncthreads();
-    Mass mass = gather_top(seg, sh, threshold, c);
+    Mass<false> mass = gather_top(src, first, sh, threshold, c);
     __syncthreads();
     int n = sh.count;
     if (n > kTopRoom) {
         __syncthreads();
-        threshold = exact_threshold(seg, sh, k);
+        threshold = exact_threshold(cut, first, sh, k);
         if (t == 0) sh.count = 0;
         __syncthreads();
-        mass = gather_top(seg, sh, threshold, c);
+        mass = gather_top(Source<T, false>{cut, nullptr}, first, sh, threshold, c);
+        __syncthreads();
+        n = sh.count;
+    } else if (n < k) {
+        // fewer than k are above -inf, so enough of the first k elements are -inf
+        __syncthreads();
+        for (int i = t; i < k; i += threads)
+            if (to_float(z[first + i]) == -infinity()) sh.cand[atomicAdd(&sh.count, 1)] = composite(-infinity(), first + i);
         __syncthreads();
         n = sh.count;
     }
-    rank_candidates(sh, n, k);
-    unsent_mass(mass, sh, n, k, c);
+    rank_candidates(sh, n, k, mass, c);
     block_mass(mass, sh, 0, c);
     if (size > 1) {
         if (t == 0) {
@@ -675,23 +925,23 @@ template <typename T> __global__ void __launch_bounds__(kTopThreads, 5) k_top_lo
             n = 0;
             for (int b = 0; b < size; ++b) {
                 const int have = (int)__float_as_uint(ld_cluster(map_rank(smem_u32(&sh.have), (uint32_t)b)));
-                for (int i = t; i < have; i += kTopThreads) {
+                for (int i = t; i < have; i += threads) {
                     const uint32_t at = map_rank(smem_u32(&sh.best[i]), (uint32_t)b);
                     sh.cand[n + i] = (unsigned long long)__float_as_uint(ld_cluster(at + 4)) << 32 | __float_as_uint(ld_cluster(at));
                 }
                 n += have;
             }
-            mass.clear();
-            if (t < size) mass.join(ld_cluster(map_rank(smem_u32(&sh.m), (uint32_t)t)), ld_cluster(map_rank(smem_u32(&sh.s), (uint32_t)t)), c);
+            mass = Mass<false>();
+            if (t < size)
+                mass.join(ld_cluster(map_rank(smem_u32(&sh.m), (uint32_t)t)), ld_cluster(map_rank(smem_u32(&sh.s), (uint32_t)t)), 0.f, c);
             __syncthreads();
         }
         cluster_sync();   // nobody reads another block's list any more
         if (rank != 0) return;
-        rank_candidates(sh, n, a.k);
-        unsent_mass(mass, sh, n, a.k, c);
+        rank_candidates(sh, n, a.k, mass, c);
         block_mass(mass, sh, 1, c);
     }
-    for (int i = t; i < a.k; i += kTopThreads) {
+    for (int i = t; i < a.k; i += threads) {
         const unsigned long long mine = sh.best[i];
         a.values[row * a.k + i] = key_value((uint32_t)(mine >> 32));
         a.indices[row * a.k + i] = (int32_t)~(uint32_t)mine;
