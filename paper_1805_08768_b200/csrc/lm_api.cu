@@ -135,12 +135,12 @@ struct RowLaunch {
 // How a row of logits is cut: blocks that share it, elements a block holds in shared memory at a
 // time, threads of a block.
 struct RowPlan {
-    int size, room, threads;
+    int size, shift, room, threads;
 };
 
 // A segment is at most kRoomBytes where eight blocks are enough for that; few rows are spread over as
 // many blocks as keep the GPU busy, each with at least 2048 elements.
-constexpr int kRoomBytes = 64 * 1024;
+constexpr int kRoomBytes = 100 * 1024;
 RowPlan plan_rows(int64_t rows, int64_t cols, int width) {
     int64_t size = 1;
     while (size < 8 && cols * width > size * kRoomBytes) size *= 2;
@@ -148,8 +148,9 @@ RowPlan plan_rows(int64_t rows, int64_t cols, int width) {
     const int64_t segment = ceil_div(ceil_div(cols, 64), size) * 64;
     RowPlan p;
     p.size = (int)size;
-    p.room = (int)std::min<int64_t>(segment, 2 * kRoomBytes / width);
-    p.threads = segment * width <= 24 * 1024 ? 128 : segment * width <= 48 * 1024 ? 256 : 512;
+    p.shift = size == 8 ? 3 : size == 4 ? 2 : size == 2 ? 1 : 0;
+    p.room = (int)std::min<int64_t>(segment, kRoomBytes / width);
+    p.threads = segment * width <= 32 * 1024 ? 128 : 256;
     return p;
 }
 
@@ -181,8 +182,9 @@ bool second_exponential(const DistillArgs& a) { return a.labels && a.temperature
 template <typename T, bool CE2, bool GRAD> int launch_distill(DistillArgs a, cudaStream_t st) {
     const RowPlan p = plan_rows(a.rows, a.cols, (int)sizeof(T));
     a.room = p.room;
+    a.shift = p.shift;
     const size_t smem = (size_t)p.room * sizeof(T) + 32 + (size_t)a.k * 12;
-    if (cudaFuncSetAttribute(k_distill<T, CE2, GRAD>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * kRoomBytes + 32 + SBC_DISTILL_MOST * 12) !=
+    if (cudaFuncSetAttribute(k_distill<T, CE2, GRAD>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRoomBytes + 32 + SBC_DISTILL_MOST * 12) !=
         cudaSuccess)
         return SBC_ECUDA;
     RowLaunch l(a.rows, p.size, p.threads, smem, st);
@@ -331,19 +333,22 @@ int sbc_top_logits(const void* logits, int dtype, int64_t rows, int64_t cols, in
     if (rows == 0) return SBC_OK;
     if (!matrix_ok(logits, dtype, rows, cols, row_stride)) return SBC_EINVAL;
     if (!values || !indices || !rest || !aligned(values, 4) || !aligned(indices, 4) || !aligned(rest, 4)) return SBC_EINVAL;
-    TopArgs a = {logits, rows, row_stride, (int)cols, k, temperature, values, indices, rest};
+    TopArgs a = {logits, rows, row_stride, (int)cols, k, 0, 0, temperature, values, indices, rest};
     return by_dtype(dtype, [&](auto* as) {
         using T = std::remove_pointer_t<decltype(as)>;
         const RowPlan p = plan_rows(rows, cols, (int)sizeof(T));
+        a.shift = p.shift;
         // enough groups of elements that the k-th largest of their maxima bounds tightly: two a thread, four times k
-        const int threads = std::max(p.threads, std::min(256, (int)ceil_div(2 * k, 32) * 32));
+        const int threads = std::max(p.threads, std::min(kTopThreads, (int)ceil_div(2 * k, 32 * p.size) * 32));
+        a.room = std::max(std::max(512, 4 * k), k * p.size);
+        const size_t lists = (size_t)a.room * 10;
         if (ceil_div(ceil_div(cols, 64), p.size) * 64 > p.room) {   // too long to be held
-            RowLaunch l(rows, p.size, kTopThreads, 0, stream);
+            RowLaunch l(rows, p.size, kTopThreads, lists, stream);
             return cudaLaunchKernelEx(&l.cfg, k_top_logits<T, false>, a) == cudaSuccess ? (int)SBC_OK : (int)SBC_ECUDA;
         }
-        if (cudaFuncSetAttribute(k_top_logits<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * kRoomBytes + 32) != cudaSuccess)
+        if (cudaFuncSetAttribute(k_top_logits<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRoomBytes + 32 + 2048 * 10) != cudaSuccess)
             return (int)SBC_ECUDA;
-        RowLaunch l(rows, p.size, threads, (size_t)p.room * sizeof(T) + 32, stream);
+        RowLaunch l(rows, p.size, threads, lists + (size_t)p.room * sizeof(T) + 32, stream);
         return cudaLaunchKernelEx(&l.cfg, k_top_logits<T, true>, a) == cudaSuccess ? (int)SBC_OK : (int)SBC_ECUDA;
     });
 }
@@ -378,10 +383,11 @@ int sbc_distill_grad(const void* logits, int dtype, int64_t rows, int64_t cols, 
         const RowPlan p = plan_rows(rows, cols, (int)sizeof(T));
         const int size = p.size, threads = p.threads;
         const size_t smem = (size_t)a.k * 12;
+        a.shift = p.shift;
         if (second_exponential(a))
-            k_distill_grad<T, true><<<(unsigned)(rows * size), threads, smem, stream>>>(a, size);
+            k_distill_grad<T, true><<<(unsigned)(rows * size), threads, smem, stream>>>(a);
         else
-            k_distill_grad<T, false><<<(unsigned)(rows * size), threads, smem, stream>>>(a, size);
+            k_distill_grad<T, false><<<(unsigned)(rows * size), threads, smem, stream>>>(a);
         return launched();
     });
 }

@@ -188,11 +188,11 @@ template <bool CE2> struct Mass {
     }
 };
 
-// The part of [0, cols) that block `rank` of `size` takes, in whole multiples of 64 elements.
-__device__ __forceinline__ int segment_start(int cols, int rank, int size) {
-    if (rank == size) return cols;
-    const int units = (cols + 63) / 64;
-    return min(cols, (int)((long long)units * rank / size) * 64);
+// The part of [0, cols) that block `rank` of 2^shift takes, in whole multiples of 64 elements.
+__device__ __forceinline__ int segment_start(int cols, int rank, int shift) {
+    if (rank >> shift) return cols;
+    const uint32_t units = ((uint32_t)cols + 63u) / 64u;
+    return min(cols, (int)(units * (uint32_t)rank >> shift) * 64);
 }
 
 // n elements of a row from p on, cut into granules where 16-byte boundaries fall: element i sits in
@@ -218,17 +218,23 @@ template <typename T> struct Cut {
         }
         return q;
     }
-    // Into shared memory, 16 bytes a copy; the copies are waited for by `landed`.
-    __device__ __forceinline__ void stage(T* room) const {
-        for (int g = threadIdx.x; g < grans; g += blockDim.x) {
-            if (whole(g))
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(room + g * E)), "l"(p - phase + (long long)g * E) : "memory");
-            else
-                *reinterpret_cast<uint4*>(room + g * E) = load(g);
+    // Into shared memory: the whole granules by bulk copies that one thread starts (`bar` counts their
+    // bytes), the edges by the threads that hold them.
+    __device__ __forceinline__ void stage(T* room, uint32_t bar) const {
+        const int g0 = phase > 0 ? 1 : 0, g1 = (phase + n) / E;
+        if (threadIdx.x == 0) {
+            const int whole_bytes = max(g1 - g0, 0) * 16;
+            mbar_expect(bar, (uint32_t)whole_bytes);
+            const uint8_t* src = reinterpret_cast<const uint8_t*>(p - phase) + 16LL * g0;
+            for (int at = 0; at < whole_bytes; at += kBulk)
+                bulk_load(smem_u32(room + g0 * E) + (uint32_t)at, src + at, (uint32_t)min(kBulk, whole_bytes - at), bar);
+        } else if (threadIdx.x <= 2) {
+            const int g = threadIdx.x == 1 ? 0 : grans - 1;
+            if (grans > 0 && !whole(g)) *reinterpret_cast<uint4*>(room + g * E) = load(g);
         }
     }
+    static constexpr int kBulk = 16384;
 };
-__device__ __forceinline__ void landed() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // ---- distillation ------------------------------------------------------------------
 
@@ -238,6 +244,7 @@ struct DistillArgs {
     long long rows, stride, grad_stride;
     int cols, k;
     int room;                  // elements of a row that a block holds at a time
+    int shift;                 // 2^shift blocks share a row
     float temperature, alpha;
     const float* values;       // teacher: rows x k logits
     const int32_t* indices;    // rows x k, negative: slot not used
@@ -336,8 +343,22 @@ template <typename T> __device__ __forceinline__ void store_granule(T* out, cons
     for (int j = 0; j < E; ++j)
         if (i0 + j >= 0 && i0 + j < cut.n) out[i0 + j] = e[j];
 }
-template <typename T> __device__ __forceinline__ bool same_phase(const T* out, const Cut<T>& cut) {
-    return ((uint32_t)(uintptr_t)out & 15u) == (uint32_t)cut.phase * sizeof(T);
+// f(granule index) -> 16 bytes, for every granule of a cut: whole ones side by side, then the edges.
+template <typename T, typename F> __device__ __forceinline__ void store_all(T* out, const Cut<T>& cut, F f) {
+    constexpr int E = Gran<T>::E;
+    const int t = threadIdx.x, threads = blockDim.x;
+    if (((uint32_t)(uintptr_t)out & 15u) != (uint32_t)cut.phase * sizeof(T)) {
+        for (int i = t; i < cut.grans; i += threads) store_granule(out, cut, i, f(i), false);
+        return;
+    }
+    const int g0 = cut.phase > 0 ? 1 : 0, g1 = (cut.phase + cut.n) / E;
+    uint4* wide = reinterpret_cast<uint4*>(out - cut.phase);
+#pragma unroll 4
+    for (int i = g0 + t; i < g1; i += threads) wide[i] = f(i);
+    if (t < 2) {
+        const int i = t == 0 ? 0 : cut.grans - 1;
+        if (cut.grans > 0 && !cut.whole(i) && (t == 0 || i > 0)) store_granule(out, cut, i, f(i), false);
+    }
 }
 
 // After all other elements of a segment are written: the sent words', and a label's that was not sent.
@@ -357,26 +378,30 @@ __device__ __forceinline__ void write_sent(T* out, const S& slope, int first, in
         out[label - first] = from_float<T>(slope.unsent_label(label_z));
 }
 
-constexpr int kDistillThreads = 512, kDistillWarps = kDistillThreads / 32;
+constexpr int kDistillThreads = 256, kDistillWarps = kDistillThreads / 32;
 
 struct DistillShared {
+    uint64_t bar;                                                    // the logits' arrival
     float om[kDistillWarps], os[kDistillWarps], os1[kDistillWarps];  // a warp's mass of words that were not sent
     float sm[kDistillWarps], ss[kDistillWarps], ss1[kDistillWarps];  // ... that were
     float tm[kDistillWarps], ts[kDistillWarps];                      // ... of the teacher's sent words (natural units)
     float kl[kDistillWarps], kl_block;
+    RowStats row;
+    float shift, inv_total, inv_whole;                               // for the divergence's terms
+    float rest_term, cross, missing;                                 // the loss's other parts
 };
 
 // One row per cluster; a block keeps its segment in shared memory, with the sent words taken out (-inf),
 // so the sum over the others is a plain one.  Segments that do not fit are taken in parts, twice.
-template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDistillThreads, 2) k_distill(DistillArgs a) {
+template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDistillThreads, 5) k_distill(DistillArgs a) {
     extern __shared__ __align__(16) uint8_t dyn[];
     __shared__ DistillShared sh;
     constexpr int E = Gran<T>::E;
     const int t = threadIdx.x, threads = blockDim.x, warp = t >> 5, lane = t & 31, warps = threads >> 5;
-    const int size = (int)cluster_size(), rank = (int)cluster_rank();
-    const long long row = blockIdx.x / size;
+    const int size = 1 << a.shift, rank = (int)(blockIdx.x & (uint32_t)(size - 1));
+    const long long row = blockIdx.x >> a.shift;
     const T* z = static_cast<const T*>(a.logits) + row * a.stride;
-    const int first = segment_start(a.cols, rank, size), n = segment_start(a.cols, rank + 1, size) - first;
+    const int first = segment_start(a.cols, rank, a.shift), n = segment_start(a.cols, rank + 1, a.shift) - first;
     T* held = reinterpret_cast<T*>(dyn);
     float* sent_t = reinterpret_cast<float*>(dyn + (size_t)(a.room + 2 * E) * sizeof(T));
     float* sent_z = sent_t + a.k;
@@ -384,8 +409,20 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
     const float c = kLog2e / a.temperature, inv = 1.f / a.temperature;
     const int parts = n > a.room ? (n + a.room - 1) / a.room : 1;
 
+    const uint32_t bar = smem_u32(&sh.bar);
+    if (t == 0) {
+        mbar_init(bar, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
     Cut<T> cut(z + first, min(n, a.room));
-    cut.stage(held);
+    cut.stage(held, bar);
+    uint32_t phase = 0;
+    bool late = false;
+    const auto landed = [&] {   // the barrier in front of it is for the edges, and for its own initialisation
+        __syncthreads();
+        late |= !mbar_wait(bar, phase);
+        phase ^= 1;
+    };
     // the teacher, while the logits are on their way
     long long label_in = a.labels ? a.labels[row] : -1;
     if (label_in >= a.cols) {
@@ -418,10 +455,9 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
         if (part > 0) {
             __syncthreads();
             cut = Cut<T>(z + first + lo, min(n - lo, a.room));
-            cut.stage(held);
+            cut.stage(held, bar);
         }
         landed();
-        __syncthreads();
         for (int i = t; i < a.k; i += threads) {
             const int at = sent_at[i] - first - lo;
             if (sent_at[i] < 0 || at < 0 || at >= cut.n) continue;
@@ -432,12 +468,14 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
         }
         __syncthreads();
         GranMax<T, false> top;
+#pragma unroll 4
         for (int i = t; i < cut.grans; i += threads) top.add(*reinterpret_cast<const uint4*>(held + i * E));
         Mass<CE2> mine;
         mine.m = top.get();
         const float base = mine.base();
         const auto add_all = [&](const auto& scale, const auto& scale1) {
             unsigned long long sum = 0, sum1 = 0;
+#pragma unroll 2
             for (int i = t; i < cut.grans; i += threads) {
                 float x[E];
                 unpack(x, *reinterpret_cast<const uint4*>(held + i * E), (const T*)nullptr);
@@ -456,6 +494,7 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
         else
             others.join(mine.m, mine.s, mine.s1, c);
     }
+    if (late) others.s = __uint_as_float(0x7fffffffu);   // the logits never came: everything is NaN
     others.lanes(c);
     sent.lanes(c);
     if (lane == 0) {
@@ -466,36 +505,67 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
         cluster_sync();
     else
         __syncthreads();
-    // every warp puts the parts together for itself
-    others = Mass<CE2>(), sent = Mass<CE2>(), teacher = Mass<false>();
-    for (int i = lane; i < warps * size; i += 32) {
-        const uint32_t r = (uint32_t)(i / warps), w = (uint32_t)(i % warps);
-        const auto at = [&](float* p) { return size > 1 ? ld_cluster(map_rank(smem_u32(p), r)) : *p; };
-        others.join(at(&sh.om[w]), at(&sh.os[w]), CE2 ? at(&sh.os1[w]) : 0.f, c);
-        sent.join(at(&sh.sm[w]), at(&sh.ss[w]), CE2 ? at(&sh.ss1[w]) : 0.f, c);
+    // p d - p + q of an outcome, d = log p - log q: their sum is the divergence, every one is positive, and
+    // p (exp(-d) - 1 + d) keeps a small d's digits
+    const auto term = [](float p, float q, float d) {
+        if (!(p > 0.f)) return q;
+        return fabsf(d) < 0.5f ? p * (expm1f(-d) + d) : p * d - p + q;
+    };
+    if (warp == 0) {
+        others = Mass<CE2>(), sent = Mass<CE2>(), teacher = Mass<false>();
+        for (int i = lane; i < warps * size; i += 32) {
+            const uint32_t r = (uint32_t)(i / warps), w = (uint32_t)(i % warps);
+            const auto at = [&](float* p) { return size > 1 ? ld_cluster(map_rank(smem_u32(p), r)) : *p; };
+            others.join(at(&sh.om[w]), at(&sh.os[w]), CE2 ? at(&sh.os1[w]) : 0.f, c);
+            sent.join(at(&sh.sm[w]), at(&sh.ss[w]), CE2 ? at(&sh.ss1[w]) : 0.f, c);
+        }
+        if (lane < warps) teacher.m = sh.tm[lane], teacher.s = sh.ts[lane];
+        others.lanes(c), sent.lanes(c), teacher.lanes(kLog2e);
+        const float m = others.m, s = others.s;
+        teacher.join(rest, 1.f, 0.f, kLog2e);
+        Mass<CE2> all = others;
+        all.join(sent.m, sent.s, sent.s1, c);
+        const bool seen = all.m > -infinity(), taught = teacher.m > -infinity();
+        const float top = all.base(), high = teacher.base(), whole = all.s, total = teacher.s;
+        const float whole1 = CE2 ? all.s1 : whole;
+        // one logarithm and one division for all of them, a lane each
+        const float arg = lane == 0 ? s : lane == 1 ? whole : lane == 2 ? total : whole1;
+        const float log_arg = log2f(arg), inv_arg = 1.f / arg;
+        const float log_s = __shfl_sync(0xffffffffu, log_arg, 0), log_whole = __shfl_sync(0xffffffffu, log_arg, 1),
+                    log_total = __shfl_sync(0xffffffffu, log_arg, 2), log_whole1 = __shfl_sync(0xffffffffu, log_arg, 3);
+        const float inv_whole = __shfl_sync(0xffffffffu, inv_arg, 1), inv_total = __shfl_sync(0xffffffffu, inv_arg, 2);
+        const float q_r = __fmul_rn(__fmul_rn(s, exp2_fast(__fmul_rn(m - top, c))), inv_whole);
+        const float p_r = __fmul_rn(exp2_fast(__fmul_rn(rest - high, kLog2e)), inv_total);
+        const float ce_weight = label >= 0 && seen ? 1.f - a.alpha : 0.f;
+        const bool live = seen && taught;
+        RowStats r;
+        r.others = others.base();
+        r.log_others = s == 0.f ? infinity() : log_s;
+        r.top = top;
+        r.log_whole = live ? log_whole : infinity();
+        r.high = high;
+        r.log_total = live ? log_total : infinity();
+        r.log_whole1 = seen ? log_whole1 : infinity();
+        r.coef = __fadd_rn(live ? __fmul_rn(a.alpha * a.temperature, q_r - p_r) : 0.f, !CE2 && ce_weight != 0.f ? __fmul_rn(ce_weight, q_r) : 0.f);
+        if (s != s) r.coef = s;   // a NaN among the others is everybody's
+        const float shift = (high - top * inv) + (log_total - log_whole) * kLn2;
+        if (lane == 0) {
+            sh.row = r;
+            sh.shift = shift;
+            sh.inv_total = inv_total;
+            sh.inv_whole = inv_whole;
+            sh.rest_term = live ? term(p_r, q_r, ((rest - m * inv) - log_s * kLn2) - shift) : 0.f;
+            sh.cross = ce_weight != 0.f ? ce_weight * (log_whole1 * kLn2 - (label_z - top)) : 0.f;
+            sh.missing = live ? 1.f : (whole != whole || total != total) ? whole + total : 0.f;   // the divergence's factor
+            if (a.stats && rank == 0) {
+                float4* st = reinterpret_cast<float4*>(a.stats + row * SBC_DISTILL_STATS);
+                st[0] = make_float4(r.others, r.log_others, r.top, r.log_whole);
+                st[1] = make_float4(r.high, r.log_total, r.log_whole1, r.coef);
+            }
+        }
     }
-    if (lane < warps) teacher.m = sh.tm[lane], teacher.s = sh.ts[lane];
-    others.lanes(c), sent.lanes(c), teacher.lanes(kLog2e);
-    const float m = others.m, s = others.s;
-    teacher.join(rest, 1.f, 0.f, kLog2e);
-    Mass<CE2> all = others;
-    all.join(sent.m, sent.s, sent.s1, c);
-    const bool seen = all.m > -infinity(), taught = teacher.m > -infinity();
-    const float top = all.base(), high = teacher.base(), whole = all.s, total = teacher.s;
-    const float whole1 = CE2 ? all.s1 : whole;
-    const float q_r = s * exp2_fast((m - top) * c) / whole, p_r = exp2_fast((rest - high) * kLog2e) / total;
-    const float ce_weight = label >= 0 && seen ? 1.f - a.alpha : 0.f;
-    const bool live = seen && taught;
-    RowStats r;
-    r.others = others.base();
-    r.log_others = s == 0.f ? infinity() : log2f(s);
-    r.top = top;
-    r.log_whole = live ? log2f(whole) : infinity();
-    r.high = high;
-    r.log_total = live ? log2f(total) : infinity();
-    r.log_whole1 = seen ? log2f(whole1) : infinity();
-    r.coef = __fadd_rn(live ? __fmul_rn(a.alpha * a.temperature, q_r - p_r) : 0.f, !CE2 && ce_weight != 0.f ? __fmul_rn(ce_weight, q_r) : 0.f);
-    if (s != s) r.coef = s;   // a NaN among the others is everybody's
+    __syncthreads();
+    const RowStats r = sh.row;
     T* out = nullptr;
     const Slope<T, CE2> slope(a, r, g, label >= 0);
     if (GRAD) {
@@ -505,30 +575,23 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
             if (parts > 1) {
                 __syncthreads();
                 cut = Cut<T>(z + first + lo, min(n - lo, a.room));
-                cut.stage(held);
+                cut.stage(held, bar);
                 landed();
-                __syncthreads();
             }
-            const bool wide = same_phase(out + lo, cut);
             slope.granules([&](const auto& gr) {
-                for (int i = t; i < cut.grans; i += threads)
-                    store_granule(out + lo, cut, i, gr.granule(*reinterpret_cast<const uint4*>(held + i * E)), wide);
+                store_all(out + lo, cut, [&](int i) { return gr.granule(*reinterpret_cast<const uint4*>(held + i * E)); });
             });
         }
     }
-    // the divergence: p d - p + q over the outcomes, d = log p - log q; every term is positive, and
-    // p (exp(-d) - 1 + d) keeps a small d's digits
-    const float shift = (high - top * inv) + (logf(total) - logf(whole));
-    const auto term = [](float p, float q, float d) {
-        if (!(p > 0.f)) return q;
-        return fabsf(d) < 0.5f ? p * (expm1f(-d) + d) : p * d - p + q;
-    };
+    const bool live = sh.missing == 1.f;
     float kl = 0.f;
-    for (int i = t; i < a.k; i += threads) {
-        if (sent_at[i] < 0) continue;
-        const float p = exp2_fast((__fmul_rn(sent_t[i], inv) - high) * kLog2e) / total, q = exp2_fast((sent_z[i] - top) * c) / whole;
-        kl += term(p, q, (sent_t[i] - sent_z[i]) * inv - shift);
-    }
+    if (live)
+        for (int i = t; i < a.k; i += threads) {
+            if (sent_at[i] < 0) continue;
+            const float p = exp2_fast((__fmul_rn(sent_t[i], inv) - r.high) * kLog2e) * sh.inv_total;
+            const float q = exp2_fast((sent_z[i] - r.top) * c) * sh.inv_whole;
+            kl += term(p, q, (sent_t[i] - sent_z[i]) * inv - sh.shift);
+        }
     kl = warp_sum(kl);
     if (lane == 0) sh.kl[warp] = kl;
     __syncthreads();
@@ -540,33 +603,25 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
         }
         cluster_sync();
     }
-    if (rank == 0 && t == 0) {
-        kl = term(p_r, q_r, ((rest - m * inv) - logf(s)) - shift);
-        if (size > 1)
-            for (int i = 0; i < size; ++i) kl += ld_cluster(map_rank(smem_u32(&sh.kl_block), (uint32_t)i));
-        else
-            for (int i = 0; i < warps; ++i) kl += sh.kl[i];
-        float loss = live ? a.alpha * a.temperature * a.temperature * kl : (whole != whole || total != total) ? whole + total : 0.f;
-        if (ce_weight != 0.f) loss += ce_weight * (logf(whole1) - (label_z - top));
-        a.loss[row] = loss;
-        if (a.stats) {
-            float4* st = reinterpret_cast<float4*>(a.stats + row * SBC_DISTILL_STATS);
-            st[0] = make_float4(r.others, r.log_others, r.top, r.log_whole);
-            st[1] = make_float4(r.high, r.log_total, r.log_whole1, r.coef);
-        }
+    if (rank == 0 && warp == 0) {
+        const int parts_of = size > 1 ? size : warps;
+        kl = lane >= parts_of ? 0.f : size > 1 ? ld_cluster(map_rank(smem_u32(&sh.kl_block), (uint32_t)lane)) : sh.kl[lane];
+        kl = warp_sum(kl);
+        if (lane == 0) a.loss[row] = (live ? a.alpha * a.temperature * a.temperature * (kl + sh.rest_term) : sh.missing) + sh.cross;
     }
+    if (late && a.status) atomicOr(a.status, SBC_STATUS_TIMEOUT);
     if (GRAD) write_sent(out, slope, first, n, a.k, sent_at, sent_t, sent_z, label, label_z);
     if (size > 1) cluster_sync();   // blocks read each other's sums up to here
 }
 
-// The backward call: statistics come from the forward one.  `size` blocks share a row, none needs another.
-template <typename T, bool CE2> __global__ void __launch_bounds__(kDistillThreads, 2) k_distill_grad(DistillArgs a, int size) {
+// The backward call: statistics come from the forward one.  Blocks that share a row do not need one another.
+template <typename T, bool CE2> __global__ void __launch_bounds__(kDistillThreads, 4) k_distill_grad(DistillArgs a) {
     extern __shared__ uint32_t words[];
     const int t = threadIdx.x, threads = blockDim.x;
-    const long long row = blockIdx.x / size;
-    const int rank = (int)(blockIdx.x % size);
+    const int rank = (int)(blockIdx.x & ((1u << a.shift) - 1u));
+    const long long row = blockIdx.x >> a.shift;
     const T* z = static_cast<const T*>(a.logits) + row * a.stride;
-    const int first = segment_start(a.cols, rank, size), n = segment_start(a.cols, rank + 1, size) - first;
+    const int first = segment_start(a.cols, rank, a.shift), n = segment_start(a.cols, rank + 1, a.shift) - first;
     const Cut<T> cut(z + first, n);
     float* sent_t = reinterpret_cast<float*>(words);
     float* sent_z = sent_t + a.k;
@@ -586,11 +641,7 @@ template <typename T, bool CE2> __global__ void __launch_bounds__(kDistillThread
     const Slope<T, CE2> slope(a, r, a.grad_loss ? a.grad_loss[row] : 1.f, label >= 0);
     __syncthreads();   // an in-place gradient comes after the words are read
     T* out = static_cast<T*>(a.grad) + row * a.grad_stride + first;
-    const bool wide = same_phase(out, cut);
-    slope.granules([&](const auto& gr) {
-#pragma unroll 4
-        for (int i = t; i < cut.grans; i += threads) store_granule(out, cut, i, gr.granule(cut.load(i)), wide);
-    });
+    slope.granules([&](const auto& gr) { store_all(out, cut, [&](int i) { return gr.granule(cut.load(i)); }); });
     __syncthreads();
     write_sent(out, slope, first, n, a.k, sent_at, sent_t, sent_z, label, label_z);
 }
@@ -601,15 +652,17 @@ struct TopArgs {
     const void* logits;
     long long rows, stride;
     int cols, k;
+    int shift;                 // 2^shift blocks share a row
+    int room;                  // candidates a block can hold: at least 2 k, and k for every block of a row
     float temperature;
     float* values;
     int32_t* indices;
     float* rest;
 };
 
-constexpr int kTopRoom = 2048;     // candidates that are ranked: at least SBC_TOP_MOST from each of 8 blocks
-constexpr int kTopBins = 512;
-constexpr int kTopThreads = 512, kTopWarps = kTopThreads / 32;
+constexpr int kTopPairs = 192;     // so many candidates are ranked by comparing all pairs, more by bins
+constexpr int kTopBins = 256;
+constexpr int kTopThreads = 256, kTopWarps = kTopThreads / 32;
 
 // Order of values as whole numbers: NaN above everything, -0 as +0.
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -627,10 +680,10 @@ __device__ __forceinline__ unsigned long long composite(float x, int index) {
 }
 
 struct TopShared {
-    unsigned long long cand[kTopRoom];
+    uint64_t bar;                            // the logits' arrival
     unsigned long long best[SBC_TOP_MOST];   // this block's largest, in order
-    uint16_t order[kTopRoom];                // candidates by bin
     uint32_t bins[kTopBins + 1];             // how many a bin holds, then where it starts
+    uint32_t next[kTopBins];                 // where a bin's next candidate goes
     uint32_t warp_hi[kTopWarps], warp_lo[kTopWarps];
     float warp_m[2][kTopWarps], warp_s[2][kTopWarps];
     uint32_t warp_bound[kTopWarps];
@@ -638,6 +691,20 @@ struct TopShared {
     unsigned long long threshold;
     int count, have;
 };
+// What a block gathers, behind the logits it holds: larger value first, then lower index.  A candidate is
+// stored as its value's bits and its index, and becomes a composite when it is ranked.
+struct Candidates {
+    unsigned long long* at;
+    uint16_t* order;           // by bin
+    int room;
+};
+
+// (the compiler would gather a warp's additions first, which costs more than these few)
+__device__ __forceinline__ uint32_t add_shared(void* p) {
+    uint32_t r;
+    asm volatile("atom.shared.add.u32 %0, [%1], 1;" : "=r"(r) : "r"(smem_u32(p)) : "memory");
+    return r;
+}
 
 // A segment's granules, held in shared memory or read from global memory.
 template <typename T, bool HELD> struct Source {
@@ -649,41 +716,60 @@ template <typename T, bool HELD> struct Source {
     }
 };
 
-// The block's mass from every thread's; `turn` keeps two uses in a row apart.
+// The block's mass from every thread's, for warp 0; `turn` keeps two uses in a row apart.
 __device__ __forceinline__ void block_mass(Mass<false>& a, TopShared& sh, int turn, float c) {
     a.lanes(c);
-    const int warps = blockDim.x >> 5;
-    if ((threadIdx.x & 31) == 0) {
+    const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
+    if (lane == 0) {
         sh.warp_m[turn][threadIdx.x >> 5] = a.m;
         sh.warp_s[turn][threadIdx.x >> 5] = a.s;
     }
     __syncthreads();
-    a = Mass<false>();
-    for (int i = 0; i < warps; ++i) a.join(sh.warp_m[turn][i], sh.warp_s[turn][i], 0.f, c);
+    if (threadIdx.x < 32) {
+        a = Mass<false>();
+        if (lane < warps) a.m = sh.warp_m[turn][lane], a.s = sh.warp_s[turn][lane];
+        a.lanes(c);
+    }
 }
 
-// Ranks sh.cand[0, n) (all different): the first min(k, n) in order to sh.best, the others join the mass
-// of what is not sent.  The keys' range is cut into equal bins, largest first; a candidate's rank is its
-// bin's start and how many of the same bin are larger.
-__device__ __forceinline__ void rank_candidates(TopShared& sh, int n, int k, Mass<false>& mass, float c) {
+// Ranks the candidates [0, n) (all different): the first min(k, n) in order to sh.best, the others join
+// the mass of what is not sent.  Few are compared with each other; otherwise the keys' range is cut into
+// equal bins, largest first, and a candidate's rank is its bin's start and how many of the same bin are
+// larger.
+__device__ __forceinline__ void rank_candidates(TopShared& sh, const Candidates& cand, int n, int k, Mass<false>& mass, float c) {
     const int t = threadIdx.x, threads = blockDim.x, lane = t & 31, warps = threads >> 5;
+    if (n <= kTopPairs) {
+        for (int i = t; i < n; i += threads) {
+            const unsigned long long mine = cand.at[i];
+            int r = 0;
+            int j = 0;
+            for (; j + 2 <= n; j += 2) {
+                const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(cand.at + j);
+                r += (two.x > mine) + (two.y > mine);
+            }
+            if (j < n) r += cand.at[j] > mine;
+            if (r < k)
+                sh.best[r] = mine;
+            else
+                mass.join(key_value((uint32_t)(mine >> 32)), 1.f, 0.f, c);
+        }
+        __syncthreads();
+        return;
+    }
     uint32_t hi = 0, lo = 0xffffffffu;
     for (int i = t; i < n; i += threads) {
-        const uint32_t key = (uint32_t)(sh.cand[i] >> 32);
+        const uint32_t key = (uint32_t)(cand.at[i] >> 32);
         hi = max(hi, key), lo = min(lo, key);
     }
     hi = __reduce_max_sync(0xffffffffu, hi), lo = __reduce_min_sync(0xffffffffu, lo);
     if (lane == 0) sh.warp_hi[t >> 5] = hi, sh.warp_lo[t >> 5] = lo;
-    for (int i = t; i <= kTopBins; i += threads) sh.bins[i] = 0;
+    for (int i = t; i < kTopBins; i += threads) sh.bins[i] = 0;
     __syncthreads();
-    for (int i = 0; i < warps; ++i) hi = max(hi, sh.warp_hi[i]), lo = min(lo, sh.warp_lo[i]);
-    const int shift = max(0, 32 - __clz((int)(hi - lo)) - 9);   // 2^9 bins
-    uint32_t slot[kTopRoom / 128];
-#pragma unroll
-    for (int j = 0; j < kTopRoom / 128; ++j) {
-        const int i = t + j * threads;
-        if (i < n) slot[j] = atomicAdd(&sh.bins[(hi - (uint32_t)(sh.cand[i] >> 32)) >> shift], 1u);
-    }
+    hi = __reduce_max_sync(0xffffffffu, sh.warp_hi[min(lane, warps - 1)]);
+    lo = __reduce_min_sync(0xffffffffu, sh.warp_lo[min(lane, warps - 1)]);
+    const int shift = max(0, 32 - __clz((int)(hi - lo)) - 8);   // 2^8 bins
+    const auto bin_of = [&](unsigned long long x) { return (hi - (uint32_t)(x >> 32)) >> shift; };
+    for (int i = t; i < n; i += threads) add_shared(&sh.bins[bin_of(cand.at[i])]);
     __syncthreads();
     if (t < 32) {
         uint32_t count[kTopBins / 32], sum = 0;
@@ -699,45 +785,41 @@ __device__ __forceinline__ void rank_candidates(TopShared& sh, int n, int k, Mas
             if (lane >= d) upto += o;
         }
 #pragma unroll
-        for (int b = 0; b < kTopBins / 32; ++b) sh.bins[lane * (kTopBins / 32) + b] = upto - sum + count[b];
+        for (int b = 0; b < kTopBins / 32; ++b) sh.bins[lane * (kTopBins / 32) + b] = sh.next[lane * (kTopBins / 32) + b] = upto - sum + count[b];
         if (lane == 31) sh.bins[kTopBins] = upto;
     }
     __syncthreads();
-#pragma unroll
-    for (int j = 0; j < kTopRoom / 128; ++j) {
-        const int i = t + j * threads;
-        if (i < n) sh.order[sh.bins[(hi - (uint32_t)(sh.cand[i] >> 32)) >> shift] + slot[j]] = (uint16_t)i;
-    }
+    for (int i = t; i < n; i += threads) cand.order[add_shared(&sh.next[bin_of(cand.at[i])])] = (uint16_t)i;
     __syncthreads();
     for (int i = t; i < n; i += threads) {
-        const unsigned long long mine = sh.cand[i];
-        const uint32_t key = (uint32_t)(mine >> 32), bin = (hi - key) >> shift;
+        const unsigned long long mine = cand.at[i];
+        const uint32_t bin = bin_of(mine);
         int r = (int)sh.bins[bin];
         if (r < k) {
             const int end = (int)sh.bins[bin + 1];
-            for (int j = (int)sh.bins[bin]; j < end; ++j) r += sh.cand[sh.order[j]] > mine;
+            for (int j = (int)sh.bins[bin]; j < end; ++j) r += cand.at[cand.order[j]] > mine;
         }
         if (r < k)
             sh.best[r] = mine;
         else
-            mass.join(key_value(key), 1.f, 0.f, c);
+            mass.join(key_value((uint32_t)(mine >> 32)), 1.f, 0.f, c);
     }
     __syncthreads();
 }
 
-// The composite at or above which between k and kTopRoom elements lie: the k-th largest one's leading
+// The composite at or above which between k and `cand.room` elements lie: the k-th largest one's leading
 // digits, found digit by digit until few enough elements share them.  For rows whose values crowd at
 // the threshold (ties).
-template <typename T> __device__ __noinline__ unsigned long long exact_threshold(const Cut<T>& cut, int first, TopShared& sh, int k) {
+template <typename T> __device__ __noinline__ unsigned long long exact_threshold(const Cut<T>& cut, int first, TopShared& sh, const Candidates& cand, int k) {
     constexpr int E = Gran<T>::E;
     const int t = threadIdx.x, lane = t & 31;
-    uint32_t* hist = reinterpret_cast<uint32_t*>(sh.cand);
+    uint32_t* hist = sh.bins;
     unsigned long long prefix = 0;
     int need = k, shift = 64;
     while (shift > 0) {
-        const int digit = min(11, shift), upper = shift;
+        const int digit = 8, upper = shift;
         shift -= digit;
-        for (int i = t; i < 2048; i += blockDim.x) hist[i] = 0;
+        for (int i = t; i < 256; i += blockDim.x) hist[i] = 0;
         __syncthreads();
         for (int g = t; g < cut.grans; g += blockDim.x) {
             float x[E];
@@ -760,9 +842,9 @@ template <typename T> __device__ __noinline__ unsigned long long exact_threshold
         }
         __syncthreads();
         if (t < 32) {
-            // 64 bins a lane, from the top
+            // 8 bins a lane, from the top
             uint32_t sum = 0;
-            for (int b = 0; b < 64; ++b) sum += hist[(31 - lane) * 64 + b];
+            for (int b = 0; b < 8; ++b) sum += hist[(31 - lane) * 8 + b];
             uint32_t upto = sum;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
@@ -771,10 +853,10 @@ template <typename T> __device__ __noinline__ unsigned long long exact_threshold
             }
             uint32_t before = upto - sum;
             if (before < (uint32_t)need && upto >= (uint32_t)need) {
-                for (int b = 63; b >= 0; --b) {
-                    const uint32_t h = hist[(31 - lane) * 64 + b];
+                for (int b = 7; b >= 0; --b) {
+                    const uint32_t h = hist[(31 - lane) * 8 + b];
                     if (before + h >= (uint32_t)need) {
-                        sh.threshold = prefix << digit | (unsigned long long)((31 - lane) * 64 + b);
+                        sh.threshold = prefix << digit | (unsigned long long)((31 - lane) * 8 + b);
                         sh.count = (int)before;
                         sh.have = (int)h;
                         break;
@@ -788,42 +870,49 @@ template <typename T> __device__ __noinline__ unsigned long long exact_threshold
         need -= sh.count;
         const int all = k - need + sh.have;
         __syncthreads();
-        if (all <= kTopRoom) break;
+        if (all <= cand.room) break;
     }
     return prefix << shift;
 }
 
-// Gathers what is at or above the threshold; returns the thread's mass of everything else.
-template <typename T, bool HELD>
-__device__ __forceinline__ Mass<false> gather_top(const Source<T, HELD>& src, int first, TopShared& sh, unsigned long long threshold, float c) {
+// Gathers what is at or above the threshold; returns the thread's mass of everything else.  PLAIN: the
+// threshold is a value's (whole composites need not be compared) above -inf.
+template <typename T, bool HELD, bool PLAIN>
+__device__ __forceinline__ Mass<false> gather_top(const Source<T, HELD>& src, int first, TopShared& sh, const Candidates& cand,
+                                                  unsigned long long threshold, float c) {
     constexpr int E = Gran<T>::E;
     const Cut<T>& cut = src.cut;
-    const float low = threshold == 0 ? -infinity() : key_value((uint32_t)(threshold >> 32));
+    const float low = !PLAIN && threshold == 0 ? -infinity() : key_value((uint32_t)(threshold >> 32));
     GranMax<T, true> top;
     float top_left = -infinity();   // of granules that hold a candidate: what is left
-    for (int g = threadIdx.x; g < cut.grans; g += blockDim.x) {
-        const uint4 q = src.get(g);
-        GranMax<T, true> here;
-        here.add(q);
-        if (here.get() < low) {
-            top.add(here);
-            continue;
+    for (int g0 = threadIdx.x; g0 < cut.grans; g0 += 32 * blockDim.x) {
+        // mark the granules first: a warp then goes through its fullest lane's, not through all that any lane has
+        uint32_t marked = 0, bit = 1;
+#pragma unroll 4
+        for (int g = g0; g < cut.grans && bit; g += blockDim.x, bit <<= 1) {
+            GranMax<T, true> here;
+            here.add(src.get(g));
+            if (here.get() < low)
+                top.add(here);
+            else
+                marked |= bit;
         }
-        float x[E];
-        unpack(x, q, (const T*)nullptr);
+        while (marked) {
+            const int g = g0 + (__ffs((int)marked) - 1) * (int)blockDim.x;
+            marked &= marked - 1;
+            float x[E];
+            unpack(x, src.get(g), (const T*)nullptr);
+            const int i0 = g * E - cut.phase;
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-            if (!(x[j] < low)) {
-                const int i = g * E + j - cut.phase;
-                const unsigned long long mine = composite(x[j], first + i);
-                if (mine >= threshold && i >= 0 && i < cut.n) {
-                    const int at = atomicAdd(&sh.count, 1);
-                    if (at < kTopRoom) sh.cand[at] = mine;
+            for (int j = 0; j < E; ++j) {
+                if (!(x[j] < low) && (PLAIN || (i0 + j >= 0 && i0 + j < cut.n && composite(x[j], first + i0 + j) >= threshold))) {
+                    const uint32_t at = add_shared(&sh.count);
+                    if (at < (uint32_t)cand.room) cand.at[at] = (unsigned long long)__float_as_uint(x[j]) << 32 | (uint32_t)(first + i0 + j);
                     if (HELD) src.held[g * E + j] = from_float<T>(-infinity());
                     x[j] = -infinity();
                 }
+                top_left = fmaxf(top_left, x[j]);
             }
-            top_left = fmaxf(top_left, x[j]);
         }
     }
     Mass<false> mass;
@@ -831,6 +920,7 @@ __device__ __forceinline__ Mass<false> gather_top(const Source<T, HELD>& src, in
     const float base = mass.base();
     const auto add_all = [&](const auto& scale) {
         unsigned long long sum = 0;
+#pragma unroll 2
         for (int g = threadIdx.x; g < cut.grans; g += blockDim.x) {
             const uint4 q = src.get(g);
             float x[E];
@@ -853,98 +943,146 @@ __device__ __forceinline__ Mass<false> gather_top(const Source<T, HELD>& src, in
 
 // One row per cluster.  A lower bound of the k-th largest: every warp takes the (k / warps)-th largest
 // of its lanes' maxima (two groups of elements a lane), the least of these has k elements at or above
-// it.  What is (little more than k, where values are spread at random) is ranked by comparing all
-// pairs, everything else only adds to the mass.
-template <typename T, bool HELD> __global__ void __launch_bounds__(kTopThreads, 2) k_top_logits(TopArgs a) {
+// it.  What is (little more than k, where values are spread at random) is ranked by the cluster's
+// first block, everything else only adds to the mass.
+template <typename T, bool HELD> __global__ void __launch_bounds__(kTopThreads, 4) k_top_logits(TopArgs a) {
     extern __shared__ __align__(16) uint8_t dyn[];
     __shared__ TopShared sh;
     const int t = threadIdx.x, threads = blockDim.x, lane = t & 31, warp = t >> 5, warps = threads >> 5;
-    const int size = (int)cluster_size(), rank = (int)cluster_rank();
-    const long long row = blockIdx.x / size;
+    const int size = 1 << a.shift, rank = (int)(blockIdx.x & (uint32_t)(size - 1));
+    const long long row = blockIdx.x >> a.shift;
     const T* z = static_cast<const T*>(a.logits) + row * a.stride;
-    const int first = segment_start(a.cols, rank, size), len = segment_start(a.cols, rank + 1, size) - first;
+    const int first = segment_start(a.cols, rank, a.shift), len = segment_start(a.cols, rank + 1, a.shift) - first;
     const Cut<T> cut(z + first, len);
-    const Source<T, HELD> src = {cut, reinterpret_cast<T*>(dyn)};
+    Candidates cand;
+    cand.at = reinterpret_cast<unsigned long long*>(dyn);
+    cand.order = reinterpret_cast<uint16_t*>(cand.at + a.room);
+    cand.room = a.room;
+    const Source<T, HELD> src = {cut, reinterpret_cast<T*>(cand.order + a.room)};
     const float c = kLog2e / a.temperature;
-    const int k = min(a.k, len);
+    const int k = a.k;
+    const auto sync = [&] {
+        if (size > 1)
+            cluster_sync();
+        else
+            __syncthreads();
+    };
 
+    bool late = false;
     if (t == 0) sh.count = 0;
     if (HELD) {
-        cut.stage(src.held);
-        landed();
+        const uint32_t bar = smem_u32(&sh.bar);
+        if (t == 0) {
+            mbar_init(bar, 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        cut.stage(src.held, bar);
         __syncthreads();
+        late = !mbar_wait(bar, 0);
     }
     unsigned long long threshold = 0;
-    if (len > threads) {
+    const bool bounded = a.cols > threads;
+    Mass<false> mass;
+    if (bounded) {
         GranMax<T, true> top;
+#pragma unroll 4
         for (int g = t; g < cut.grans; g += threads) top.add(src.get(g));
         const uint32_t k0 = order_key(top.first()) >> 16, k1 = order_key(top.second()) >> 16;
-        const int share = (k + warps - 1) / warps;
-        uint32_t bound = 0;    // upper half of the threshold's key
-        for (uint32_t bit = 0x8000u; bit; bit >>= 1) {
-            const uint32_t next = bound | bit;
+        const int share = (k + warps * size - 1) / (warps * size);
+        // upper half of the threshold's key: what all have in common, then bit by bit
+        const uint32_t all = __reduce_and_sync(0xffffffffu, k0 & k1), any = __reduce_or_sync(0xffffffffu, k0 | k1);
+        const int bits = 32 - __clz((int)(all ^ any));
+        uint32_t bound = all >> bits << bits;
+        for (int b = bits - 1; b >= 0; --b) {
+            const uint32_t next = bound | 1u << b;
             if (__popc(__ballot_sync(0xffffffffu, k0 >= next)) + __popc(__ballot_sync(0xffffffffu, k1 >= next)) >= share) bound = next;
         }
         if (lane == 0) sh.warp_bound[warp] = bound;
-        __syncthreads();
-        for (int i = 0; i < warps; ++i) bound = min(bound, sh.warp_bound[i]);
+        sync();
+        for (int i = lane; i < warps * size; i += 32) {
+            const uint32_t r = (uint32_t)(i / warps), w = (uint32_t)(i % warps);
+            bound = min(bound, size > 1 ? __float_as_uint(ld_cluster(map_rank(smem_u32(&sh.warp_bound[w]), r))) : sh.warp_bound[w]);
+        }
+        bound = __reduce_min_sync(0xffffffffu, bound);
         // -inf is asked for only where nothing else is left
         threshold = (unsigned long long)max(bound << 16, kLowestKey) << 32;
+        mass = gather_top<T, HELD, true>(src, first, sh, cand, threshold, c);
+    } else {
+        __syncthreads();
+        mass = gather_top<T, HELD, false>(src, first, sh, cand, threshold, c);
     }
-    __syncthreads();
-    Mass<false> mass = gather_top(src, first, sh, threshold, c);
-    __syncthreads();
-    int n = sh.count;
-    if (n > kTopRoom) {
-        __syncthreads();
-        threshold = exact_threshold(cut, first, sh, k);
-        if (t == 0) sh.count = 0;
-        __syncthreads();
-        mass = gather_top(Source<T, false>{cut, nullptr}, first, sh, threshold, c);
-        __syncthreads();
-        n = sh.count;
-    } else if (n < k) {
-        // fewer than k are above -inf, so enough of the first k elements are -inf
-        __syncthreads();
-        for (int i = t; i < k; i += threads)
-            if (to_float(z[first + i]) == -infinity()) sh.cand[atomicAdd(&sh.count, 1)] = composite(-infinity(), first + i);
-        __syncthreads();
-        n = sh.count;
-    }
-    rank_candidates(sh, n, k, mass, c);
-    block_mass(mass, sh, 0, c);
-    if (size > 1) {
-        if (t == 0) {
-            sh.m = mass.m;
-            sh.s = mass.s;
-            sh.have = k;
+    if (late) mass.s = __uint_as_float(0x7fffffffu);   // the logits never came
+    sync();
+    // how many candidates the cluster has
+    const auto have = [&](int b) { return size > 1 ? (int)__float_as_uint(ld_cluster(map_rank(smem_u32(&sh.count), (uint32_t)b))) : sh.count; };
+    int n = 0;
+    for (int b = 0; b < size; ++b) n += min(have(b), a.room + 1);
+    const auto compose = [&](int count) {
+        for (int i = t; i < count; i += threads) {
+            const unsigned long long raw = cand.at[i];
+            cand.at[i] = composite(__uint_as_float((uint32_t)(raw >> 32)), (int)(uint32_t)raw);
         }
+        __syncthreads();
+    };
+    if (n > a.room) {
+        // more than can be ranked: every block keeps no more than k
+        sync();
+        const int most = min(k, len);
+        if (most > 0) {
+            threshold = exact_threshold(cut, first, sh, cand, most);
+            if (t == 0) sh.count = 0;
+            __syncthreads();
+            mass = gather_top<T, false, false>(Source<T, false>{cut, nullptr}, first, sh, cand, threshold, c);
+            __syncthreads();
+            compose(sh.count);
+            if (size > 1) {
+                rank_candidates(sh, cand, sh.count, most, mass, c);
+                for (int i = t; i < most; i += threads) cand.at[i] = sh.best[i];
+                if (t == 0) sh.count = most;
+            }
+        }
+        sync();
+        n = 0;
+        for (int b = 0; b < size; ++b) n += have(b);
+    } else {
+        compose(sh.count);
+    }
+    if (size > 1) {
+        block_mass(mass, sh, 0, c);
+        if (t == 0) sh.m = mass.m, sh.s = mass.s;
         cluster_sync();
         if (rank == 0) {
-            // the blocks' lists, ranked together
-            n = 0;
-            for (int b = 0; b < size; ++b) {
-                const int have = (int)__float_as_uint(ld_cluster(map_rank(smem_u32(&sh.have), (uint32_t)b)));
-                for (int i = t; i < have; i += threads) {
-                    const uint32_t at = map_rank(smem_u32(&sh.best[i]), (uint32_t)b);
-                    sh.cand[n + i] = (unsigned long long)__float_as_uint(ld_cluster(at + 4)) << 32 | __float_as_uint(ld_cluster(at));
+            n = sh.count;
+            for (int b = 1; b < size; ++b) {
+                const int count = have(b);
+                for (int i = t; i < count; i += threads) {
+                    const uint32_t at = map_rank(smem_u32(&cand.at[i]), (uint32_t)b);
+                    cand.at[n + i] = (unsigned long long)__float_as_uint(ld_cluster(at + 4)) << 32 | __float_as_uint(ld_cluster(at));
                 }
-                n += have;
+                n += count;
             }
             mass = Mass<false>();
-            if (t < size)
-                mass.join(ld_cluster(map_rank(smem_u32(&sh.m), (uint32_t)t)), ld_cluster(map_rank(smem_u32(&sh.s), (uint32_t)t)), 0.f, c);
-            __syncthreads();
+            if (t < size) mass.m = ld_cluster(map_rank(smem_u32(&sh.m), (uint32_t)t)), mass.s = ld_cluster(map_rank(smem_u32(&sh.s), (uint32_t)t));
         }
-        cluster_sync();   // nobody reads another block's list any more
+        cluster_sync();   // nobody reads another block's candidates any more
         if (rank != 0) return;
-        rank_candidates(sh, n, a.k, mass, c);
-        block_mass(mass, sh, 1, c);
     }
-    for (int i = t; i < a.k; i += threads) {
+    if (n < k) {
+        // fewer than k are above -inf, so enough of the first k elements are -inf
+        if (t == 0) sh.count = n;
+        __syncthreads();
+        for (int i = t; i < k; i += threads)
+            if (to_float(z[i]) == -infinity()) cand.at[add_shared(&sh.count)] = composite(-infinity(), i);
+        __syncthreads();
+        n = sh.count;
+        __syncthreads();
+    }
+    rank_candidates(sh, cand, n, k, mass, c);
+    block_mass(mass, sh, 1, c);
+    for (int i = t; i < k; i += threads) {
         const unsigned long long mine = sh.best[i];
-        a.values[row * a.k + i] = key_value((uint32_t)(mine >> 32));
-        a.indices[row * a.k + i] = (int32_t)~(uint32_t)mine;
+        a.values[row * k + i] = key_value((uint32_t)(mine >> 32));
+        a.indices[row * k + i] = (int32_t)~(uint32_t)mine;
     }
     if (t == 0) a.rest[row] = mass.s == 0.f ? -infinity() : mass.m / a.temperature + logf(mass.s);
 }
