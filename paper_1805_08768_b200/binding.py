@@ -7,7 +7,6 @@ is loaded on first use; if it is missing or cannot be loaded the call raises
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 import os
 from typing import List, Optional, Sequence, Tuple
@@ -198,9 +197,18 @@ def _check(code: int, where: str) -> None:
         raise SbcError(code, where)
 
 
+def _current_stream() -> int:
+    return torch.cuda.current_stream().cuda_stream
+
+
+if hasattr(torch._C, "_cuda_getCurrentRawStream"):   # the same handle without the Stream object around it
+    def _current_stream() -> int:  # noqa: F811
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
 def _cuda_stream(stream) -> int:
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -538,15 +546,20 @@ def sbc_encode_sampled(update: torch.Tensor, residual: torch.Tensor, p: float, s
 # ---- language-model operators (include/sbc_lm.h) -----------------------------------
 
 DTYPE_CODES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+FP4_WORKSPACE_BYTES = 4096   # what sbc_fp4_workspace_bytes says for any matrix
 FP4_FORMATS = {"e8m0": 0, "e4m3": 1}   # block scales: powers of two for 32 elements, 8-bit floats for 16
 
 
 def _matrix(t: torch.Tensor, name: str) -> None:
     if not (t.is_cuda and t.dim() == 2 and t.dtype in DTYPE_CODES):
         raise TypeError(f"{name} must be a float32, bfloat16 or float16 CUDA matrix")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    rows, cols = t.shape
+    across, along = t.stride()
+    if cols > 1 and along != 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
-    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+    if rows > 1 and across < cols:
         raise ValueError(f"{name}: rows must not overlap")
 
 
@@ -554,12 +567,23 @@ def _row_stride(t: torch.Tensor) -> int:
     return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
 
 
-def _fresh(stream):
-    """Context in which new buffers belong to the stream that the work is enqueued on."""
+def _empty(stream, shape, dtype, device) -> torch.Tensor:
+    """A new buffer that belongs to the stream which the work is enqueued on."""
     if stream is None:
-        return contextlib.nullcontext()
+        return torch.empty(shape, dtype=dtype, device=device)
     s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_cuda_stream(stream))
-    return torch.cuda.stream(s)
+    with torch.cuda.stream(s):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _fp4_sizes(rows: int, cols: int, format: str) -> Tuple[int, int]:
+    """(bytes of the elements, bytes of the scales), as the header lays them out."""
+    if format not in FP4_FORMATS:
+        raise ValueError(f"unknown 4-bit format {format!r}")
+    if rows < 1 or cols < 1:
+        raise ValueError("an Fp4Tensor has at least one row and one column")
+    tiles = (cols + 127) // 128 if format == "e8m0" else (cols + 63) // 64
+    return rows * ((cols + 31) // 32 * 16), (rows + 127) // 128 * tiles * 512
 
 
 class Fp4Tensor:
@@ -567,65 +591,81 @@ class Fp4Tensor:
     header's.  ``values`` uint8 [rows, row bytes], ``scales`` uint8 (flat), ``tensor_scale`` float32 [1];
     ``format`` is "e8m0" or "e4m3"."""
 
-    __slots__ = ("values", "scales", "tensor_scale", "rows", "cols", "format", "desc")
+    __slots__ = ("rows", "cols", "format", "desc", "_room", "_at", "_parts")
 
     def __init__(self, values: torch.Tensor, scales: torch.Tensor, tensor_scale: torch.Tensor, rows: int, cols: int,
                  format: str):
-        if format not in FP4_FORMATS:
-            raise ValueError(f"unknown 4-bit format {format!r}")
-        row_bytes = int(lib().sbc_fp4_row_bytes(cols))
-        scale_bytes = int(lib().sbc_fp4_scale_bytes(rows, cols, FP4_FORMATS[format]))
-        for t, name, n in ((values, "values", rows * row_bytes), (scales, "scales", scale_bytes)):
+        value_bytes, scale_bytes = _fp4_sizes(rows, cols, format)
+        for t, name, n in ((values, "values", value_bytes), (scales, "scales", scale_bytes)):
             if not (t.is_cuda and t.dtype == torch.uint8 and t.is_contiguous()):
                 raise TypeError(f"{name} must be a contiguous uint8 CUDA tensor")
-            if n == 0 or t.numel() != n:
+            if t.numel() != n:
                 raise ValueError(f"{name}: {n} bytes needed for {rows} x {cols}, got {t.numel()}")
         _dev_f32(tensor_scale, "tensor_scale")
         if tensor_scale.numel() < 1:
             raise ValueError("tensor_scale must hold one value")
-        self._set(values, scales, tensor_scale, rows, cols, format)
-
-    def _set(self, values, scales, tensor_scale, rows, cols, format):
-        self.values, self.scales, self.tensor_scale = values, scales, tensor_scale
         self.rows, self.cols, self.format = rows, cols, format
+        self._room, self._at, self._parts = None, 0, (values, scales, tensor_scale)
         self.desc = Fp4Desc(values.data_ptr(), scales.data_ptr(), tensor_scale.data_ptr(), rows, cols,
                             FP4_FORMATS[format], 0)
 
     @classmethod
-    def empty(cls, rows: int, cols: int, format: str, device) -> "Fp4Tensor":
-        """Room for a rows x cols matrix, contents undefined."""
-        if format not in FP4_FORMATS:
-            raise ValueError(f"unknown 4-bit format {format!r}")
-        if rows < 1 or cols < 1:
-            raise ValueError("an Fp4Tensor has at least one row and one column")
-        row_bytes = (cols + 31) // 32 * 16
-        scale_bytes = int(lib().sbc_fp4_scale_bytes(rows, cols, FP4_FORMATS[format]))
-        room = torch.empty(rows * row_bytes + scale_bytes + 16, dtype=torch.uint8, device=device)
+    def _in_room(cls, room: torch.Tensor, at: int, value_bytes: int, scale_bytes: int, rows: int, cols: int,
+                 format: str) -> "Fp4Tensor":
+        """Elements, scales and tensor scale one behind the other in a byte buffer."""
         self = cls.__new__(cls)
-        self._set(room[:rows * row_bytes].view(rows, row_bytes), room[rows * row_bytes:-16],
-                  room[-16:-12].view(torch.float32), rows, cols, format)
+        self.rows, self.cols, self.format = rows, cols, format
+        self._room, self._at, self._parts = room, at, None
+        base = room.data_ptr() + at
+        self.desc = Fp4Desc(base, base + value_bytes, base + value_bytes + scale_bytes, rows, cols,
+                            FP4_FORMATS[format], 0)
         return self
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, format: str, device, stream=None) -> "Fp4Tensor":
+        """Room for a rows x cols matrix, contents undefined."""
+        value_bytes, scale_bytes = _fp4_sizes(rows, cols, format)
+        room = _empty(stream, value_bytes + scale_bytes + 16, torch.uint8, device)
+        return cls._in_room(room, 0, value_bytes, scale_bytes, rows, cols, format)
+
+    def _views(self):
+        if self._parts is None:
+            value_bytes, scale_bytes = _fp4_sizes(self.rows, self.cols, self.format)
+            a, b = self._at, self._at + value_bytes
+            self._parts = (self._room[a:b].view(self.rows, -1), self._room[b:b + scale_bytes],
+                           self._room[b + scale_bytes:b + scale_bytes + 4].view(torch.float32))
+        return self._parts
+
+    values = property(lambda self: self._views()[0])
+    scales = property(lambda self: self._views()[1])
+    tensor_scale = property(lambda self: self._views()[2])
+
+    @property
+    def device(self) -> torch.device:
+        return (self._room if self._parts is None else self._parts[0]).device
 
     @property
     def nbytes(self) -> int:
-        return self.values.numel() + self.scales.numel() + 4
+        return sum(_fp4_sizes(self.rows, self.cols, self.format)) + 4
 
 
 def _quantise(x, format, along_rows, along_cols, stream):
     _matrix(x, "x")
-    if format not in FP4_FORMATS:
-        raise ValueError(f"unknown 4-bit format {format!r}")
     rows, cols = x.shape
-    with _fresh(stream):
-        q = Fp4Tensor.empty(rows, cols, format, x.device) if along_rows else None
-        q_t = Fp4Tensor.empty(cols, rows, format, x.device) if along_cols else None
-        ws = torch.empty(int(lib().sbc_fp4_workspace_bytes(rows, cols, FP4_FORMATS[format])), dtype=torch.uint8,
-                         device=x.device)
+    v, s = _fp4_sizes(rows, cols, format) if along_rows else (0, 0)
+    v_t, s_t = _fp4_sizes(cols, rows, format) if along_cols else (0, 0)
+    # one buffer: both tensors and, in front, the scratch of the call
+    ws = FP4_WORKSPACE_BYTES
+    at_t = ws + (v + s + 16 if along_rows else 0)
+    room = _empty(stream, at_t + (v_t + s_t + 16 if along_cols else 0), torch.uint8, x.device)
+    q = Fp4Tensor._in_room(room, ws, v, s, rows, cols, format) if along_rows else None
+    q_t = Fp4Tensor._in_room(room, at_t, v_t, s_t, cols, rows, format) if along_cols else None
     code = lib().sbc_fp4_quantise(x.data_ptr(), DTYPE_CODES[x.dtype], rows, cols, _row_stride(x),
                                   C.byref(q.desc) if q is not None else None,
-                                  C.byref(q_t.desc) if q_t is not None else None, ws.data_ptr(), ws.numel(),
+                                  C.byref(q_t.desc) if q_t is not None else None, room.data_ptr(), ws,
                                   _cuda_stream(stream))
-    _check(code, "sbc_fp4_quantise")
+    if code:
+        _check(code, "sbc_fp4_quantise")
     return q, q_t
 
 
@@ -645,13 +685,14 @@ def sbc_fp4_dequantise(q: Fp4Tensor, dtype: torch.dtype = torch.float32, out: Op
                        stream=None) -> torch.Tensor:
     """The values that q stands for (rows x cols)."""
     if out is None:
-        with _fresh(stream):
-            out = torch.empty(q.rows, q.cols, dtype=dtype, device=q.values.device)
+        out = _empty(stream, (q.rows, q.cols), dtype, q.device)
     _matrix(out, "out")
     if tuple(out.shape) != (q.rows, q.cols):
         raise ValueError(f"out must be {q.rows} x {q.cols}")
-    _check(lib().sbc_fp4_dequantise(C.byref(q.desc), out.data_ptr(), DTYPE_CODES[out.dtype], _row_stride(out),
-                                    _cuda_stream(stream)), "sbc_fp4_dequantise")
+    code = lib().sbc_fp4_dequantise(C.byref(q.desc), out.data_ptr(), DTYPE_CODES[out.dtype], _row_stride(out),
+                                    _cuda_stream(stream))
+    if code:
+        _check(code, "sbc_fp4_dequantise")
     return out
 
 
@@ -662,14 +703,15 @@ def sbc_fp4_product(a: Fp4Tensor, b: Fp4Tensor, dtype: torch.dtype = torch.bfloa
     if a.format != b.format or a.cols != b.cols:
         raise ValueError(f"operands differ: {a.cols} columns of {a.format}, {b.cols} of {b.format}")
     if out is None:
-        with _fresh(stream):
-            out = torch.empty(a.rows, b.rows, dtype=dtype, device=a.values.device)
+        out = _empty(stream, (a.rows, b.rows), dtype, a.device)
     _matrix(out, "out")
     if tuple(out.shape) != (a.rows, b.rows):
         raise ValueError(f"out must be {a.rows} x {b.rows}")
-    _check(lib().sbc_fp4_product(C.byref(a.desc), C.byref(b.desc), out.data_ptr(), DTYPE_CODES[out.dtype],
+    code = lib().sbc_fp4_product(C.byref(a.desc), C.byref(b.desc), out.data_ptr(), DTYPE_CODES[out.dtype],
                                  _row_stride(out), status.data_ptr() if status is not None else None,
-                                 _cuda_stream(stream)), "sbc_fp4_product")
+                                 _cuda_stream(stream))
+    if code:
+        _check(code, "sbc_fp4_product")
     return out
 
 
@@ -684,10 +726,9 @@ def sbc_top_logits(logits: torch.Tensor, k: int, temperature: float = 1.0,
     rows, cols = logits.shape
     if not 1 <= k <= min(cols, TOP_MOST):
         raise ValueError(f"k must be in 1 .. {min(cols, TOP_MOST)}")
-    with _fresh(stream):
-        values = torch.empty(rows, k, dtype=torch.float32, device=logits.device)
-        indices = torch.empty(rows, k, dtype=torch.int32, device=logits.device)
-        rest = torch.empty(rows, dtype=torch.float32, device=logits.device)
+    values = _empty(stream, (rows, k), torch.float32, logits.device)
+    indices = _empty(stream, (rows, k), torch.int32, logits.device)
+    rest = _empty(stream, (rows,), torch.float32, logits.device)
     _check(lib().sbc_top_logits(logits.data_ptr(), DTYPE_CODES[logits.dtype], rows, cols, _row_stride(logits), k,
                                 float(temperature), values.data_ptr(), indices.data_ptr(), rest.data_ptr(),
                                 _cuda_stream(stream)), "sbc_top_logits")
@@ -723,8 +764,7 @@ def _taught(logits, values, indices, rest, temperature, alpha, labels) -> Distil
 
 def _grad_out(logits: torch.Tensor, out: Optional[torch.Tensor], stream) -> torch.Tensor:
     if out is None:
-        with _fresh(stream):
-            return torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        return _empty(stream, logits.shape, logits.dtype, logits.device)
     _matrix(out, "out")
     if out.shape != logits.shape or out.dtype != logits.dtype:
         raise ValueError("out must have the logits' shape and type")
@@ -739,9 +779,8 @@ def sbc_distill_loss(logits: torch.Tensor, values: torch.Tensor, indices: torch.
     sent words and one outcome for all others, plus (1 - alpha) cross entropy of the labels."""
     d = _taught(logits, values, indices, rest, temperature, alpha, labels)
     rows, cols = logits.shape
-    with _fresh(stream):
-        loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
-        stats = torch.empty(rows, DISTILL_STATS, dtype=torch.float32, device=logits.device)
+    loss = _empty(stream, (rows,), torch.float32, logits.device)
+    stats = _empty(stream, (rows, DISTILL_STATS), torch.float32, logits.device)
     _check(lib().sbc_distill_loss(logits.data_ptr(), DTYPE_CODES[logits.dtype], rows, cols, _row_stride(logits),
                                   C.byref(d), loss.data_ptr(), stats.data_ptr(),
                                   status.data_ptr() if status is not None else None, _cuda_stream(stream)),
@@ -773,8 +812,7 @@ def sbc_distill_loss_grad(logits: torch.Tensor, values: torch.Tensor, indices: t
     d = _taught(logits, values, indices, rest, temperature, alpha, labels)
     rows, cols = logits.shape
     out = _grad_out(logits, out, stream)
-    with _fresh(stream):
-        loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
+    loss = _empty(stream, (rows,), torch.float32, logits.device)
     _check(lib().sbc_distill_loss_grad(logits.data_ptr(), DTYPE_CODES[logits.dtype], rows, cols, _row_stride(logits),
                                        C.byref(d), _rows_of(grad_loss, rows, torch.float32, "grad_loss"),
                                        loss.data_ptr(), out.data_ptr(), _row_stride(out),

@@ -1,5 +1,6 @@
 // C entry points of the language-model operators (include/sbc_lm.h).
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "lm_common.cuh"
@@ -55,6 +56,18 @@ template <typename F> int by_dtype(int dtype, F f) {
     return SBC_EINVAL;
 }
 
+// Raises a kernel's limit of dynamic shared memory, once per device.
+template <auto Kernel> bool allow_smem(int bytes) {
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return false;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (dev < 64 && (done.load(std::memory_order_relaxed) & bit)) return true;
+    if (cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return true;
+}
+
 int launched() { return cudaGetLastError() == cudaSuccess ? SBC_OK : SBC_ECUDA; }
 
 template <typename T, int FMT> void launch_quantise(const QuantiseArgs& a, bool rows, bool cols, unsigned grid, cudaStream_t st) {
@@ -97,8 +110,7 @@ constexpr int kSmemMost = 227 * 1024;
 
 template <typename T, int FMT>
 int launch_product(const CUtensorMap& mw, const CUtensorMap& mx, const ProductArgs& a, dim3 grid, int smem, cudaStream_t st) {
-    if (cudaFuncSetAttribute(k_fp4_product<T, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - 1024) != cudaSuccess)
-        return SBC_ECUDA;
+    if (!allow_smem<k_fp4_product<T, FMT>>(kSmemMost - 1024)) return SBC_ECUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(kPThreads);
@@ -184,9 +196,7 @@ template <typename T, bool CE2, bool GRAD> int launch_distill(DistillArgs a, cud
     a.room = p.room;
     a.shift = p.shift;
     const size_t smem = (size_t)p.room * sizeof(T) + 32 + (size_t)a.k * 12;
-    if (cudaFuncSetAttribute(k_distill<T, CE2, GRAD>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRoomBytes + 32 + SBC_DISTILL_MOST * 12) !=
-        cudaSuccess)
-        return SBC_ECUDA;
+    if (!allow_smem<k_distill<T, CE2, GRAD>>(kRoomBytes + 32 + SBC_DISTILL_MOST * 12)) return SBC_ECUDA;
     RowLaunch l(a.rows, p.size, p.threads, smem, st);
     return cudaLaunchKernelEx(&l.cfg, k_distill<T, CE2, GRAD>, a) == cudaSuccess ? SBC_OK : SBC_ECUDA;
 }
@@ -210,7 +220,7 @@ size_t sbc_fp4_scale_bytes(int64_t rows, int64_t cols, int format) {
 }
 
 size_t sbc_fp4_workspace_bytes(int64_t rows, int64_t cols, int format) {
-    return sbc_fp4_scale_bytes(rows, cols, format) ? 256 : 0;
+    return sbc_fp4_scale_bytes(rows, cols, format) ? kAmaxBlocks * 4 : 0;
 }
 
 int sbc_fp4_quantise(const void* x, int dtype, int64_t rows, int64_t cols, int64_t row_stride, const sbc_fp4* along_rows,
@@ -251,9 +261,10 @@ int sbc_fp4_quantise(const void* x, int dtype, int64_t rows, int64_t cols, int64
         using T = std::remove_pointer_t<decltype(as)>;
         cudaStream_t st = stream;
         if (format == SBC_FP4_E4M3) {
-            if (cudaMemsetAsync(workspace, 0, 4, st) != cudaSuccess) return (int)SBC_ECUDA;
-            const int64_t blocks = std::min<int64_t>(ceil_div(rows * ceil_div(cols, 8), kQThreads), sm_count() * 8);
-            k_fp4_amax<T><<<(unsigned)blocks, kQThreads, 0, st>>>(a, static_cast<uint32_t*>(workspace));
+            if (rows * cols > kAmaxAlone) {
+                a.amax_blocks = (int)std::min<int64_t>(ceil_div(rows * ceil_div(cols, 8), kQThreads * 4), kAmaxBlocks);
+                k_fp4_amax<T><<<(unsigned)a.amax_blocks, kQThreads, 0, st>>>(a, static_cast<uint32_t*>(workspace));
+            }
             launch_quantise<T, SBC_FP4_E4M3>(a, along_rows, along_cols, (unsigned)(row_tiles * col_tiles), st);
         } else {
             launch_quantise<T, SBC_FP4_E8M0>(a, along_rows, along_cols, (unsigned)(row_tiles * col_tiles), st);
@@ -346,8 +357,7 @@ int sbc_top_logits(const void* logits, int dtype, int64_t rows, int64_t cols, in
             RowLaunch l(rows, p.size, kTopThreads, lists, stream);
             return cudaLaunchKernelEx(&l.cfg, k_top_logits<T, false>, a) == cudaSuccess ? (int)SBC_OK : (int)SBC_ECUDA;
         }
-        if (cudaFuncSetAttribute(k_top_logits<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRoomBytes + 32 + 2048 * 10) != cudaSuccess)
-            return (int)SBC_ECUDA;
+        if (!allow_smem<k_top_logits<T, true>>(kRoomBytes + 32 + 2048 * 10)) return (int)SBC_ECUDA;
         RowLaunch l(rows, p.size, threads, lists + (size_t)p.room * sizeof(T) + 32, stream);
         return cudaLaunchKernelEx(&l.cfg, k_top_logits<T, true>, a) == cudaSuccess ? (int)SBC_OK : (int)SBC_ECUDA;
     });

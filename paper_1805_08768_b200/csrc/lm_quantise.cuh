@@ -70,7 +70,8 @@ struct QuantiseArgs {
     long long rows, cols, stride;
     int align;                    // every row starts at a multiple of this many bytes
     uint32_t col_tiles;           // blocks are numbered row tile by row tile
-    const uint32_t* amax;         // E4M3: bits of the tensor's largest finite magnitude
+    const uint32_t* amax;         // E4M3: bits of the largest finite magnitudes that the blocks of k_fp4_amax found
+    int amax_blocks;              // ... how many; 0: the tensor is small, every block looks for itself
     float* tensor_r;              // where the tensor scale goes (either may be null)
     float* tensor_c;
     uint8_t *values_r, *scales_r; // along the rows: rows x cols
@@ -79,14 +80,17 @@ struct QuantiseArgs {
     long long ktiles_r, ktiles_c; // scale tiles per 128 rows
 };
 
-// Largest finite magnitude of the tensor, as float bits (whole numbers: the maximum does not
-// depend on the order).
-template <typename T> __global__ void __launch_bounds__(kQThreads) k_fp4_amax(QuantiseArgs a, uint32_t* amax) {
+constexpr int kAmaxBlocks = 1024;
+constexpr long long kAmaxAlone = 32768;   // elements up to which every block finds the maximum itself, instead of a launch in front
+
+// Largest finite magnitude of the elements that threads [at, at + step, ...) of the tensor take, over the
+// block, as float bits (whole numbers: the maximum does not depend on the order).
+template <typename T> __device__ __forceinline__ uint32_t amax_over(const QuantiseArgs& a, long long at, long long step, uint32_t* room) {
     const T* x = static_cast<const T*>(a.x);
     const long long per_row = (a.cols + 7) / 8, all = per_row * a.rows;
     uint32_t top = 0;
-    for (long long i = (long long)blockIdx.x * kQThreads + threadIdx.x; i < all; i += (long long)gridDim.x * kQThreads) {
-        const long long r = i / per_row, c = (i - r * per_row) * 8;
+    for (long long i = at; i < all; i += step) {
+        const long long r = all < (1ll << 31) ? (long long)((uint32_t)i / (uint32_t)per_row) : i / per_row, c = (i - r * per_row) * 8;
         Pack8<T> v;
         load8(v, x + r * a.stride + c, (int)min(8LL, a.cols - c), a.align);
 #pragma unroll
@@ -96,7 +100,27 @@ template <typename T> __global__ void __launch_bounds__(kQThreads) k_fp4_amax(Qu
         }
     }
     top = __reduce_max_sync(0xffffffffu, top);
-    if ((threadIdx.x & 31) == 0 && top) atomicMax(amax, top);
+    if ((threadIdx.x & 31) == 0) room[threadIdx.x >> 5] = top;
+    __syncthreads();
+    return __reduce_max_sync(0xffffffffu, room[threadIdx.x & (kQThreads / 32 - 1)]);
+}
+
+template <typename T> __global__ void __launch_bounds__(kQThreads) k_fp4_amax(QuantiseArgs a, uint32_t* amax) {
+    __shared__ uint32_t room[kQThreads / 32];
+    const uint32_t top = amax_over<T>(a, (long long)blockIdx.x * kQThreads + threadIdx.x, (long long)gridDim.x * kQThreads, room);
+    if (threadIdx.x == 0) amax[blockIdx.x] = top;
+}
+
+// The tensor's, in every block of the quantising kernel.
+template <typename T> __device__ __forceinline__ uint32_t tensor_amax(const QuantiseArgs& a) {
+    __shared__ uint32_t room[kQThreads / 32];
+    if (a.amax_blocks == 0) return amax_over<T>(a, threadIdx.x, kQThreads, room);
+    uint32_t top = 0;
+    for (int i = threadIdx.x; i < a.amax_blocks; i += kQThreads) top = max(top, a.amax[i]);
+    top = __reduce_max_sync(0xffffffffu, top);
+    if ((threadIdx.x & 31) == 0) room[threadIdx.x >> 5] = top;
+    __syncthreads();
+    return __reduce_max_sync(0xffffffffu, room[threadIdx.x & (kQThreads / 32 - 1)]);
 }
 
 // One block takes a 128 x 128 tile, which is whole scale tiles of either orientation.
@@ -112,7 +136,7 @@ template <typename T, int FMT, bool ROWS, bool COLS> __global__ void __launch_bo
     const uint32_t row_tile = blockIdx.x / a.col_tiles, col_tile = blockIdx.x % a.col_tiles;
     const long long row0 = (long long)row_tile * kQTile, col0 = (long long)col_tile * kQTile;
     float tensor = 1.f;
-    if (FMT == SBC_FP4_E4M3) tensor = tensor_scale_of(*a.amax);
+    if (FMT == SBC_FP4_E4M3) tensor = tensor_scale_of(tensor_amax<T>(a));
     if (blockIdx.x == 0 && t == 0) {
         if (ROWS) *a.tensor_r = tensor;
         if (COLS) *a.tensor_c = tensor;

@@ -208,6 +208,32 @@ def test_nan_blocks_reach_only_their_rows(fmt, tokens):
     assert torch.equal(torch.isnan(got), want)
 
 
+def test_sizes_agree_with_the_library():
+    for rows in (1, 127, 128, 129, 5000):
+        for cols in (1, 31, 32, 33, 64, 65, 128, 129, 4097):
+            for fmt, code in sbc.FP4_FORMATS.items():
+                values, scales = sbc._fp4_sizes(rows, cols, fmt)
+                assert values == rows * sbc.lib().sbc_fp4_row_bytes(cols)
+                assert scales == sbc.lib().sbc_fp4_scale_bytes(rows, cols, code)
+                assert sbc.lib().sbc_fp4_workspace_bytes(rows, cols, code) == sbc.FP4_WORKSPACE_BYTES
+                q = sbc.Fp4Tensor.empty(rows, cols, fmt, DEV)
+                assert q.values.shape == (rows, values // rows) and q.scales.numel() == scales and q.nbytes == values + scales + 4
+                assert q.values.data_ptr() == q.desc.values and q.scales.data_ptr() == q.desc.scales
+                assert q.tensor_scale.data_ptr() == q.desc.tensor_scale and q.tensor_scale.shape == (1,)
+
+
+@pytest.mark.parametrize("shape", [(40, 800), (41, 799), (32768, 1), (300, 400)])
+def test_the_tensor_scale_looks_at_every_element(shape):
+    """On both sides of the size from which a kernel of its own finds the largest magnitude."""
+    rows, cols = shape
+    for r, c in ((0, 0), (rows - 1, cols - 1), (rows // 2, cols // 3)):
+        x = torch.full(shape, 1.0, device=DEV)
+        x[r, c] = -1000.0
+        q = sbc.sbc_fp4_quantise(x, "e4m3")
+        assert float(q.tensor_scale) == 0.5          # 2^(9 - 10)
+        assert same(sbc.sbc_fp4_dequantise(q), plain_round(x, "e4m3"))
+
+
 def test_refusals():
     x = values(4, 64, torch.float32, 1)
     with pytest.raises(TypeError):
