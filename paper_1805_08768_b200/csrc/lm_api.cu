@@ -208,6 +208,49 @@ template <bool GRAD> int distill_by_type(const DistillArgs& a, int dtype, cudaSt
     });
 }
 
+template <typename T, int FMT>
+int launch_wide(const CUtensorMap& mw, const CUtensorMap& mx, const WideArgs& a, unsigned blocks, int smem, cudaStream_t st) {
+    if (!allow_smem<k_fp4_product_wide<T, FMT>>(kSmemMost - 1024)) return SBC_ECUDA;
+    k_fp4_product_wide<T, FMT><<<blocks, kWThreads, (size_t)smem, st>>>(mw, mx, a);
+    return launched();
+}
+
+// More than 128 tokens: pairs of blocks that stay.  Tiles of 256 tokens where that makes two rounds of
+// tiles or more, of 128 (twice as many, and the accumulator twice) below.
+int product_wide(const sbc_fp4* a, const sbc_fp4* b, void* out, int dtype, int64_t row_stride, uint32_t* status, cudaStream_t st) {
+    WideArgs p = {};
+    p.scales_w = static_cast<const uint8_t*>(b->scales);
+    p.scales_x = static_cast<const uint8_t*>(a->scales);
+    p.tensor_w = b->tensor_scale;
+    p.tensor_x = a->tensor_scale;
+    p.out = out;
+    p.status = status;
+    p.rows_w = b->rows;
+    p.rows_x = a->rows;
+    p.stride = row_stride;
+    p.ktiles = ktiles_of(a->cols, a->format);
+    p.chunks = (int)ceil_div(a->cols, 256);
+    p.steps = (int)ceil_div(a->cols, 64);
+    const int64_t pairs = std::max(1, sm_count() / 2), tiles_w = ceil_div(b->rows, 256);
+    p.nt = tiles_w * ceil_div(a->rows, 256) >= 2 * pairs ? 256 : 128;
+    const int64_t tiles = tiles_w * ceil_div(a->rows, p.nt);
+    if (tiles > kMaxDim / 2) return SBC_EINVAL;
+    p.tiles_w = (int)tiles_w;
+    p.tiles = (int)tiles;
+    const int tiles_k = a->format == SBC_FP4_E8M0 ? 2 : 4;
+    const int stage = kPRows * kPBytes + p.nt / 2 * kPBytes + tiles_k * 512 * (1 + p.nt / 128);
+    p.stages = std::min(std::min(kWMaxStages, 220 * 1024 / stage), 256 / (4 * tiles_k * (1 + p.nt / 128)));
+    CUtensorMap mw, mx;
+    if (!values_map(&mw, b, kPRows) || !values_map(&mx, a, p.nt / 2)) return SBC_ECUDA;
+    const unsigned blocks = (unsigned)(2 * std::min(pairs, tiles));
+    const int smem = std::max(p.stages * stage + 1024, kSmemMost / 2 + 1024);   // one block per SM: it takes all of tensor memory
+    return by_dtype(dtype, [&](auto* as) {
+        using T = std::remove_pointer_t<decltype(as)>;
+        return a->format == SBC_FP4_E4M3 ? launch_wide<T, SBC_FP4_E4M3>(mw, mx, p, blocks, smem, st)
+                                         : launch_wide<T, SBC_FP4_E8M0>(mw, mx, p, blocks, smem, st);
+    });
+}
+
 }  // namespace
 
 extern "C" {
@@ -301,6 +344,7 @@ int sbc_fp4_product(const sbc_fp4* a, const sbc_fp4* b, void* out, int dtype, in
                     sbc_cuda_stream_t stream) {
     if (!fp4_ok(a) || !fp4_ok(b) || a->format != b->format || a->cols != b->cols) return SBC_EINVAL;
     if (!matrix_ok(out, dtype, a->rows, b->rows, row_stride) || !aligned(status, 4)) return SBC_EINVAL;
+    if (a->rows > 128) return product_wide(a, b, out, dtype, row_stride, status, stream);
     ProductArgs p = {};
     p.scales_w = static_cast<const uint8_t*>(b->scales);
     p.scales_x = static_cast<const uint8_t*>(a->scales);
@@ -314,7 +358,7 @@ int sbc_fp4_product(const sbc_fp4* a, const sbc_fp4* b, void* out, int dtype, in
     p.ktiles = ktiles_of(a->cols, a->format);
     p.chunks = (int)ceil_div(a->cols, 256);
     p.steps = (int)ceil_div(a->cols, 64);
-    p.nt = a->rows >= 256 ? 256 : (int)ceil_div(a->rows, 16) * 16;
+    p.nt = (int)ceil_div(a->rows, 16) * 16;
     const int row_tiles = (p.nt + 127) / 128, tiles_k = a->format == SBC_FP4_E8M0 ? 2 : 4;
     const int stage = (kPRows * kPBytes + p.nt * kPBytes + tiles_k * 512 * (1 + row_tiles) + 1023) / 1024 * 1024;
     p.stages = p.nt > 128 ? 4 : std::min(4, 110 * 1024 / stage);

@@ -174,6 +174,7 @@ __global__ void __launch_bounds__(kPThreads) k_fp4_product(const __grid_constant
         }
         commit(done);
         if (!ok) gave_up = 1;
+        mbar_wait(done, 0);   // no product may be running when tensor memory is given back
     }
     __syncwarp();
     // every block of a cluster has at least one chunk, so `done` always means a whole partial sum
@@ -227,6 +228,272 @@ __global__ void __launch_bounds__(kPThreads) k_fp4_product(const __grid_constant
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     if (warp == 5) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(a.tmem_cols));
+}
+
+// ---- many tokens ----------------------------------------------------------------------
+//
+// Pairs of blocks on neighbouring SMs share a tile of 256 weights x `nt` (256 or 128) tokens: each
+// loads its 128 weights and half of the tokens, the tensor cores of both read both halves, so an SM
+// loads 0.58 bytes per thousand products where a block alone would load 0.82.  Blocks stay and take
+// tile after tile; loads run ahead across tiles.
+//
+// Scales reach tensor memory through registers (four warps that do nothing else): copies by the tensor
+// unit (tcgen05.cp) take turns with the products there, about 100 cycles each against 128 of a product.
+//
+// Warps: 0..3 accumulator to memory, 4..7 scales, 8 loads, 9 multiplies (in the first block of the pair).
+
+constexpr int kWThreads = 320;
+constexpr int kWMaxStages = 8;
+
+struct WideArgs {
+    const uint8_t *scales_w, *scales_x;
+    const float *tensor_w, *tensor_x;
+    void* out;
+    uint32_t* status;
+    long long rows_w, rows_x, stride, ktiles;
+    int chunks, steps, nt, stages;
+    int tiles_w, tiles;   // tiles along the weights, all tiles
+};
+
+template <int FMT>
+__device__ __forceinline__ void multiply2(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t add) {
+    if (FMT == SBC_FP4_E8M0)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(add)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(add)
+            : "memory");
+}
+// Arrives at the barrier of this address in both blocks when all products so far are done.
+__device__ __forceinline__ void commit2(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+                 "h"((uint16_t)3)
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_load32(float* v, uint32_t addr) {
+    uint32_t* u = reinterpret_cast<uint32_t*>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]),
+          "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]), "=r"(u[17]), "=r"(u[18]),
+          "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]), "=r"(u[25]), "=r"(u[26]), "=r"(u[27]),
+          "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
+        : "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_store4(uint32_t addr, const uint4& q) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w) : "memory");
+}
+__device__ __forceinline__ uint4 ld_shared16(uint32_t addr) {
+    uint4 q;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(addr) : "memory");
+    return q;
+}
+
+template <typename T, int FMT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWThreads, 1)
+    k_fp4_product_wide(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, WideArgs a) {
+    using S = ProductShape<FMT>;
+    extern __shared__ uint8_t raw[];
+    __shared__ uint64_t bars[3 * kWMaxStages + 5];
+    __shared__ uint32_t tmem_slot, gave_up;
+    const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+    const uint32_t rank = cluster_rank();
+    const uint32_t smem = (smem_u32(raw) + 1023u) & ~1023u;
+    const int nt = a.nt, row_tiles = nt / 128, buffers = nt == 128 ? 2 : 1;
+    const uint32_t bytes_w = kPRows * kPBytes, bytes_x = (uint32_t)(nt / 2) * kPBytes, bytes_sc = S::kTiles * 512u;
+    const uint32_t stage_bytes = bytes_w + bytes_x + bytes_sc * (1 + row_tiles);   // a multiple of 1024
+    const uint32_t bar0 = smem_u32(bars);
+    const auto full = [&](int s) { return bar0 + 24u * s; };           // this block's loads of a stage have landed
+    const auto ready = [&](int s) { return bar0 + 24u * s + 8; };      // both blocks' loads have, and their scales are in tensor memory
+    const auto empty = [&](int s) { return bar0 + 24u * s + 16; };     // the products that read a stage are done
+    const auto acc_full = [&](int b) { return bar0 + 24u * kWMaxStages + 8u * b; };
+    const auto acc_empty = [&](int b) { return bar0 + 24u * kWMaxStages + 16 + 8u * b; };
+    const uint32_t drained = bar0 + 24u * kWMaxStages + 32;
+    const uint32_t acc_cols = 256, sc_cols = 4u * S::kTiles * (1 + row_tiles);
+    const int pairs = (int)(gridDim.x / 2), pair = (int)(blockIdx.x / 2);
+
+    if (t == 0) {
+        gave_up = 0;
+        for (int s = 0; s < a.stages; ++s) {
+            mbar_init(full(s), 1);
+            mbar_init(ready(s), 8);
+            mbar_init(empty(s), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(acc_full(b), 1);
+            mbar_init(acc_empty(b), 8);
+        }
+        mbar_init(drained, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_sync();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = tmem_slot;
+    const float nan = __uint_as_float(0x7fffffffu);
+
+    if (warp == 8) {
+        if (lane == 0) {
+            bool ok = true;
+            int i = 0;
+            for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
+                const long long w0 = (long long)(tile % a.tiles_w) * 256 + rank * 128, x0 = (long long)(tile / a.tiles_w) * nt;
+                const long long x1 = x0 + rank * (nt / 2);
+                const bool has_w = w0 < a.rows_w;
+                const int x_tiles = (int)min((long long)row_tiles, (a.rows_x + 127) / 128 - x0 / 128);
+                for (int c = 0; c < a.chunks; ++c, ++i) {
+                    const int s = i % a.stages;
+                    ok = mbar_wait(empty(s), ((i / a.stages) & 1) ^ 1);
+                    if (!ok) break;
+                    const long long k0 = (long long)c * S::kTiles;
+                    const uint32_t sc = (uint32_t)min((long long)S::kTiles, a.ktiles - k0) * 512u;
+                    const uint32_t at = smem + (uint32_t)s * stage_bytes, at_x = at + bytes_w, at_sc = at_x + bytes_x;
+                    mbar_expect(full(s), bytes_w + bytes_x + sc * ((has_w ? 1 : 0) + x_tiles));
+                    tma_load_2d(at, &map_w, c * kPBytes, (int)w0, full(s));
+                    tma_load_2d(at_x, &map_x, c * kPBytes, (int)x1, full(s));
+                    if (has_w) bulk_load(at_sc, a.scales_w + (w0 / 128 * a.ktiles + k0) * 512, sc, full(s));
+                    for (int j = 0; j < x_tiles; ++j)
+                        bulk_load(at_sc + bytes_sc * (1 + j), a.scales_x + ((x0 / 128 + j) * a.ktiles + k0) * 512, sc, full(s));
+                }
+            }
+            if (!ok) gave_up = 1;
+            // no copy and no arrival at a barrier may be on its way when the block ends
+            for (int j = max(0, i - a.stages); j < i; ++j) {
+                mbar_wait(full(j % a.stages), (j / a.stages) & 1);
+                mbar_wait(empty(j % a.stages), (j / a.stages) & 1);
+            }
+        }
+    } else if (warp == 9) {
+        if (lane == 0 && rank != 0) mbar_wait(drained, 0);
+        if (lane == 0 && rank == 0) {
+            bool ok = true;
+            const uint32_t idesc = (1u << 7) | (1u << 10) | (FMT == SBC_FP4_E8M0 ? 1u << 23 : 0u) | (2u << 27) | ((uint32_t)(nt >> 3) << 17);
+            int i = 0, n = 0;
+            for (int tile = pair; tile < a.tiles && ok; tile += pairs, ++n) {
+                const int b = n % buffers;
+                ok = mbar_wait_cluster(acc_empty(b), ((n / buffers) & 1) ^ 1);
+                if (!ok) break;
+                const uint32_t acc = tmem + (uint32_t)b * 128u;
+                for (int c = 0; c < a.chunks; ++c, ++i) {
+                    const int s = i % a.stages;
+                    ok = mbar_wait_cluster(ready(s), (i / a.stages) & 1);
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t at = smem + (uint32_t)s * stage_bytes, at_x = at + bytes_w;
+                    const uint32_t sf_w = tmem + acc_cols + (uint32_t)s * sc_cols, sf_x = sf_w + 4 * S::kTiles;
+                    const int steps = min(4, a.steps - c * 4);
+                    for (int k = 0; k < steps; ++k) {
+                        // E8M0: two steps share a scale tile, each takes its half of every word
+                        const int tile_k = FMT == SBC_FP4_E8M0 ? k / 2 : k;
+                        const uint32_t half = FMT == SBC_FP4_E8M0 ? (uint32_t)(k & 1) * 2u : 0u;
+                        multiply2<FMT>(acc, operand_desc(at + 32 * k), operand_desc(at_x + 32 * k), idesc | (half << 4) | (half << 29),
+                                       sf_w + 4 * tile_k, sf_x + 4 * tile_k * row_tiles, (uint32_t)(c > 0 || k > 0));
+                    }
+                    commit2(empty(s));
+                }
+                if (ok) commit2(acc_full(b));
+            }
+            if (!ok) gave_up = 1;
+            // no product may be running when tensor memory is given back
+            commit2(drained);
+            mbar_wait(drained, 0);
+        }
+    } else if (warp >= 4) {
+        bool ok = true;
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;
+        int i = 0;
+        for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
+            for (int c = 0; c < a.chunks; ++c, ++i) {
+                const int s = i % a.stages;
+                ok = __all_sync(0xffffffffu, mbar_wait(full(s), (i / a.stages) & 1));
+                if (!ok) break;
+                const uint32_t at = smem + (uint32_t)s * stage_bytes + bytes_w + bytes_x + 16u * lane;
+                const uint32_t sf = tmem + acc_cols + (uint32_t)s * sc_cols + lanes;
+                uint4 q[S::kTiles * 3];
+#pragma unroll
+                for (int k = 0; k < S::kTiles; ++k) q[k] = ld_shared16(at + 512u * k);
+#pragma unroll
+                for (int k = 0; k < S::kTiles; ++k) {
+                    q[S::kTiles + 2 * k] = ld_shared16(at + bytes_sc + 512u * k);
+                    if (row_tiles == 2) q[S::kTiles + 2 * k + 1] = ld_shared16(at + 2 * bytes_sc + 512u * k);
+                }
+#pragma unroll
+                for (int k = 0; k < S::kTiles; ++k) tmem_store4(sf + 4u * k, q[k]);
+#pragma unroll
+                for (int k = 0; k < S::kTiles; ++k) {
+                    const uint32_t to = sf + 4u * S::kTiles + 4u * k * row_tiles;
+                    tmem_store4(to, q[S::kTiles + 2 * k]);
+                    if (row_tiles == 2) tmem_store4(to + 4u, q[S::kTiles + 2 * k + 1]);
+                }
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive_remote(map_rank(ready(s), 0));
+            }
+        }
+        if (!ok) gave_up = 1;
+    } else {
+        bool ok = true;
+        const float scale = FMT == SBC_FP4_E4M3 ? *a.tensor_w * *a.tensor_x : 1.f;
+        int n = 0;
+        for (int tile = pair; tile < a.tiles; tile += pairs, ++n) {
+            const int b = n % buffers;
+            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(acc_full(b), (n / buffers) & 1));
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const long long j = (long long)(tile % a.tiles_w) * 256 + rank * 128 + warp * 32 + lane, x0 = (long long)(tile / a.tiles_w) * nt;
+            const int tokens = (int)min((long long)nt, a.rows_x - x0);
+            T* out = static_cast<T*>(a.out) + x0 * a.stride + j;
+            const bool mine = j < a.rows_w;
+            const uint32_t acc = tmem + (uint32_t)b * 128u + ((uint32_t)warp << 21);
+            for (int n0 = 0; n0 < nt; n0 += 32) {
+                float v[32];
+                __syncwarp();
+                tmem_load32(v, acc + n0);
+                if (n0 + 32 >= nt) {
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_remote(map_rank(acc_empty(b), 0));
+                }
+                const float by = ok ? scale : nan;
+                if (mine && n0 + 32 <= tokens) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        *out = from_float<T>(v[i] * by);
+                        out += a.stride;
+                    }
+                } else if (mine) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (n0 + i < tokens) {
+                            *out = from_float<T>(v[i] * by);
+                            out += a.stride;
+                        }
+                }
+            }
+        }
+        if (!ok) gave_up = 1;
+    }
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (t == 0 && gave_up && a.status) atomicOr(a.status, SBC_STATUS_TIMEOUT);
+    cluster_sync();   // the other block's barriers and tensor memory are used up to here
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
 }
 
 }  // namespace sbclm
