@@ -37,6 +37,16 @@ template <int FMT> struct ProductShape {
         (1u << 7) | (1u << 10) | (FMT == SBC_FP4_E8M0 ? 1u << 23 : 0u) | (1u << 27);
 };
 
+// A place in the ring of stages and the parity its barriers have there (no divisions: every role goes
+// around it with one thread, whose own latency would otherwise be what a stage costs).
+struct Ring {
+    int s = 0;
+    uint32_t turn = 0;
+    __device__ __forceinline__ void next(int stages) {
+        if (++s == stages) s = 0, turn ^= 1;
+    }
+};
+
 __device__ __forceinline__ uint64_t operand_desc(uint32_t smem) {  // 128-byte swizzle, 8 rows of 128 bytes per group
     return (uint64_t)((smem & 0x3ffff) >> 4) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
@@ -119,41 +129,43 @@ __global__ void __launch_bounds__(kPThreads) k_fp4_product(const __grid_constant
     const uint32_t sc_cols = 4u * S::kTiles * (1 + row_tiles);     // scale columns per stage
 
     if (warp == 4 && lane == 0) {
-        int issued = first;
         bool ok = true;
-        for (int c = first; c < last && ok; ++c) {
-            const int i = c - first, s = i % a.stages;
-            const uint32_t full = bar0 + 16 * s, empty = full + 8;
-            ok = mbar_wait(empty, ((i / a.stages) & 1) ^ 1);
+        Ring at;
+        // a token tile's last 128 rows may lie beyond the scales' last tile
+        const int x_tiles = (int)min((long long)row_tiles, (a.rows_x + 127) / 128 - x0 / 128);
+        const uint8_t* sw = a.scales_w + (w0 / 128 * a.ktiles + (long long)first * S::kTiles) * 512;
+        const uint8_t* sx = a.scales_x + (x0 / 128 * a.ktiles + (long long)first * S::kTiles) * 512;
+        const long long sx_tile = a.ktiles * 512;
+        int left = (int)(a.ktiles - (long long)first * S::kTiles);
+        int c = first;
+        for (; c < last; ++c) {
+            const uint32_t full = bar0 + 16 * at.s;
+            ok = mbar_wait(full + 8, at.turn ^ 1);
             if (!ok) break;
-            const long long k0 = (long long)c * S::kTiles;
-            const uint32_t sc = (uint32_t)min((long long)S::kTiles, a.ktiles - k0) * 512u;
-            const uint32_t at = smem + (uint32_t)s * stage_room, at_x = at + bytes_w, at_sc = at_x + bytes_x_room;
-            // a token tile's last 128 rows may lie beyond the scales' last tile
-            const int x_tiles = (int)min((long long)row_tiles, (a.rows_x + 127) / 128 - x0 / 128);
+            const uint32_t sc = (uint32_t)min(S::kTiles, left) * 512u;
+            const uint32_t to = smem + (uint32_t)at.s * stage_room, to_x = to + bytes_w, to_sc = to_x + bytes_x_room;
             mbar_expect(full, bytes_w + bytes_x + sc * (1 + x_tiles));
-            tma_load_2d(at, &map_w, c * kPBytes, (int)w0, full);
-            tma_load_2d(at_x, &map_x, c * kPBytes, (int)x0, full);
-            bulk_load(at_sc, a.scales_w + (w0 / 128 * a.ktiles + k0) * 512, sc, full);
-            for (int j = 0; j < x_tiles; ++j)
-                bulk_load(at_sc + bytes_sc * (1 + j), a.scales_x + ((x0 / 128 + j) * a.ktiles + k0) * 512, sc, full);
-            issued = c + 1;
+            tma_load_2d(to, &map_w, c * kPBytes, (int)w0, full);
+            tma_load_2d(to_x, &map_x, c * kPBytes, (int)x0, full);
+            bulk_load(to_sc, sw, sc, full);
+            for (int j = 0; j < x_tiles; ++j) bulk_load(to_sc + bytes_sc * (1 + j), sx + sx_tile * j, sc, full);
+            sw += S::kTiles * 512, sx += S::kTiles * 512, left -= S::kTiles;
+            at.next(a.stages);
         }
         if (!ok) gave_up = 1;
         // no copy may be in flight when the block ends
-        for (int c = max(first, issued - a.stages); c < issued; ++c)
-            mbar_wait(bar0 + 16 * ((c - first) % a.stages), ((c - first) / a.stages) & 1);
+        for (int j = max(0, c - first - a.stages); j < c - first; ++j) mbar_wait(bar0 + 16 * (j % a.stages), (j / a.stages) & 1);
     } else if (warp == 5 && lane == 0) {
         bool ok = true;
         const uint32_t idesc = S::kIdesc | ((uint32_t)(a.nt >> 3) << 17);
+        Ring ring;
         for (int c = first; c < last; ++c) {
-            const int i = c - first, s = i % a.stages;
-            const uint32_t full = bar0 + 16 * s, empty = full + 8;
-            ok = mbar_wait(full, (i / a.stages) & 1);
+            const uint32_t full = bar0 + 16 * ring.s, empty = full + 8;
+            ok = mbar_wait(full, ring.turn);
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t at = smem + (uint32_t)s * stage_room, at_x = at + bytes_w, at_sc = at_x + bytes_x_room;
-            const uint32_t sf_w = tmem + acc_cols + (uint32_t)s * sc_cols, sf_x = sf_w + 4 * S::kTiles;
+            const uint32_t at = smem + (uint32_t)ring.s * stage_room, at_x = at + bytes_w, at_sc = at_x + bytes_x_room;
+            const uint32_t sf_w = tmem + acc_cols + (uint32_t)ring.s * sc_cols, sf_x = sf_w + 4 * S::kTiles;
             const int steps = min(4, a.steps - c * 4);
             // scales: a step's tiles of 128 rows stand in neighbouring columns
 #pragma unroll
@@ -168,9 +180,10 @@ __global__ void __launch_bounds__(kPThreads) k_fp4_product(const __grid_constant
                 const int tile = FMT == SBC_FP4_E8M0 ? k / 2 : k;
                 const uint32_t half = FMT == SBC_FP4_E8M0 ? (uint32_t)(k & 1) * 2u : 0u;
                 multiply<FMT>(tmem, operand_desc(at + 32 * k), operand_desc(at_x + 32 * k), idesc | (half << 4) | (half << 29),
-                              sf_w + 4 * tile, sf_x + 4 * tile * row_tiles, (uint32_t)(i > 0 || k > 0));
+                              sf_w + 4 * tile, sf_x + 4 * tile * row_tiles, (uint32_t)(c > first || k > 0));
             }
             commit(empty);
+            ring.next(a.stages);
         }
         commit(done);
         if (!ok) gave_up = 1;
@@ -349,32 +362,41 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWThreads, 1)
     if (warp == 8) {
         if (lane == 0) {
             bool ok = true;
-            int i = 0;
+            Ring ring;
+            int issued = 0;
             for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
-                const long long w0 = (long long)(tile % a.tiles_w) * 256 + rank * 128, x0 = (long long)(tile / a.tiles_w) * nt;
-                const long long x1 = x0 + rank * (nt / 2);
+                const int w0 = tile % a.tiles_w * 256 + (int)rank * 128;
+                const int x0 = tile / a.tiles_w * nt, x1 = x0 + (int)rank * (nt / 2);
                 const bool has_w = w0 < a.rows_w;
                 const int x_tiles = (int)min((long long)row_tiles, (a.rows_x + 127) / 128 - x0 / 128);
-                for (int c = 0; c < a.chunks; ++c, ++i) {
-                    const int s = i % a.stages;
-                    ok = mbar_wait(empty(s), ((i / a.stages) & 1) ^ 1);
+                const uint8_t* sw = a.scales_w + w0 / 128 * a.ktiles * 512;
+                const uint8_t* sx = a.scales_x + x0 / 128 * a.ktiles * 512;
+                const uint8_t* sx2 = sx + a.ktiles * 512;
+                int left = (int)a.ktiles;
+                for (int c = 0; c < a.chunks; ++c) {
+                    const uint32_t bar = full(ring.s);
+                    ok = mbar_wait(bar + 16, ring.turn ^ 1);
                     if (!ok) break;
-                    const long long k0 = (long long)c * S::kTiles;
-                    const uint32_t sc = (uint32_t)min((long long)S::kTiles, a.ktiles - k0) * 512u;
-                    const uint32_t at = smem + (uint32_t)s * stage_bytes, at_x = at + bytes_w, at_sc = at_x + bytes_x;
-                    mbar_expect(full(s), bytes_w + bytes_x + sc * ((has_w ? 1 : 0) + x_tiles));
-                    tma_load_2d(at, &map_w, c * kPBytes, (int)w0, full(s));
-                    tma_load_2d(at_x, &map_x, c * kPBytes, (int)x1, full(s));
-                    if (has_w) bulk_load(at_sc, a.scales_w + (w0 / 128 * a.ktiles + k0) * 512, sc, full(s));
-                    for (int j = 0; j < x_tiles; ++j)
-                        bulk_load(at_sc + bytes_sc * (1 + j), a.scales_x + ((x0 / 128 + j) * a.ktiles + k0) * 512, sc, full(s));
+                    const uint32_t sc = (uint32_t)min(S::kTiles, left) * 512u;
+                    const uint32_t at = smem + (uint32_t)ring.s * stage_bytes, at_x = at + bytes_w, at_sc = at_x + bytes_x;
+                    mbar_expect(bar, bytes_w + bytes_x + sc * ((has_w ? 1 : 0) + x_tiles));
+                    tma_load_2d(at, &map_w, c * kPBytes, w0, bar);
+                    tma_load_2d(at_x, &map_x, c * kPBytes, x1, bar);
+                    if (has_w) bulk_load(at_sc, sw, sc, bar);
+                    bulk_load(at_sc + bytes_sc, sx, sc, bar);
+                    if (x_tiles > 1) bulk_load(at_sc + 2 * bytes_sc, sx2, sc, bar);
+                    sw += S::kTiles * 512, sx += S::kTiles * 512, sx2 += S::kTiles * 512, left -= S::kTiles;
+                    ring.next(a.stages);
+                    issued = min(issued + 1, a.stages);
                 }
             }
             if (!ok) gave_up = 1;
-            // no copy and no arrival at a barrier may be on its way when the block ends
-            for (int j = max(0, i - a.stages); j < i; ++j) {
-                mbar_wait(full(j % a.stages), (j / a.stages) & 1);
-                mbar_wait(empty(j % a.stages), (j / a.stages) & 1);
+            // no copy and no arrival at a barrier may be on its way when the block ends: every stage's last turn
+            for (int j = 0; j < issued; ++j) {
+                const int s = ring.s - 1 - j < 0 ? ring.s - 1 - j + a.stages : ring.s - 1 - j;
+                const uint32_t turn = ring.s - 1 - j < 0 ? ring.turn ^ 1 : ring.turn;
+                mbar_wait(full(s), turn);
+                mbar_wait(empty(s), turn);
             }
         }
     } else if (warp == 9) {
@@ -382,19 +404,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWThreads, 1)
         if (lane == 0 && rank == 0) {
             bool ok = true;
             const uint32_t idesc = (1u << 7) | (1u << 10) | (FMT == SBC_FP4_E8M0 ? 1u << 23 : 0u) | (2u << 27) | ((uint32_t)(nt >> 3) << 17);
-            int i = 0, n = 0;
-            for (int tile = pair; tile < a.tiles && ok; tile += pairs, ++n) {
-                const int b = n % buffers;
-                ok = mbar_wait_cluster(acc_empty(b), ((n / buffers) & 1) ^ 1);
+            Ring ring, accs;
+            for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
+                const int b = accs.s;
+                ok = mbar_wait_cluster(acc_empty(b), accs.turn ^ 1);
                 if (!ok) break;
                 const uint32_t acc = tmem + (uint32_t)b * 128u;
-                for (int c = 0; c < a.chunks; ++c, ++i) {
-                    const int s = i % a.stages;
-                    ok = mbar_wait_cluster(ready(s), (i / a.stages) & 1);
+                for (int c = 0; c < a.chunks; ++c) {
+                    ok = mbar_wait_cluster(ready(ring.s), ring.turn);
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t at = smem + (uint32_t)s * stage_bytes, at_x = at + bytes_w;
-                    const uint32_t sf_w = tmem + acc_cols + (uint32_t)s * sc_cols, sf_x = sf_w + 4 * S::kTiles;
+                    const uint32_t at = smem + (uint32_t)ring.s * stage_bytes, at_x = at + bytes_w;
+                    const uint32_t sf_w = tmem + acc_cols + (uint32_t)ring.s * sc_cols, sf_x = sf_w + 4 * S::kTiles;
                     const int steps = min(4, a.steps - c * 4);
                     for (int k = 0; k < steps; ++k) {
                         // E8M0: two steps share a scale tile, each takes its half of every word
@@ -403,9 +424,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWThreads, 1)
                         multiply2<FMT>(acc, operand_desc(at + 32 * k), operand_desc(at_x + 32 * k), idesc | (half << 4) | (half << 29),
                                        sf_w + 4 * tile_k, sf_x + 4 * tile_k * row_tiles, (uint32_t)(c > 0 || k > 0));
                     }
-                    commit2(empty(s));
+                    commit2(empty(ring.s));
+                    ring.next(a.stages);
                 }
                 if (ok) commit2(acc_full(b));
+                accs.next(buffers);
             }
             if (!ok) gave_up = 1;
             // no product may be running when tensor memory is given back
@@ -415,14 +438,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWThreads, 1)
     } else if (warp >= 4) {
         bool ok = true;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;
-        int i = 0;
+        Ring ring;
         for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
-            for (int c = 0; c < a.chunks; ++c, ++i) {
-                const int s = i % a.stages;
-                ok = __all_sync(0xffffffffu, mbar_wait(full(s), (i / a.stages) & 1));
+            for (int c = 0; c < a.chunks; ++c) {
+                ok = __all_sync(0xffffffffu, mbar_wait(full(ring.s), ring.turn));
                 if (!ok) break;
-                const uint32_t at = smem + (uint32_t)s * stage_bytes + bytes_w + bytes_x + 16u * lane;
-                const uint32_t sf = tmem + acc_cols + (uint32_t)s * sc_cols + lanes;
+                const uint32_t at = smem + (uint32_t)ring.s * stage_bytes + bytes_w + bytes_x + 16u * lane;
+                const uint32_t sf = tmem + acc_cols + (uint32_t)ring.s * sc_cols + lanes;
                 uint4 q[S::kTiles * 3];
 #pragma unroll
                 for (int k = 0; k < S::kTiles; ++k) q[k] = ld_shared16(at + 512u * k);
@@ -442,17 +464,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWThreads, 1)
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) mbar_arrive_remote(map_rank(ready(s), 0));
+                if (lane == 0) mbar_arrive_remote(map_rank(ready(ring.s), 0));
+                ring.next(a.stages);
             }
         }
         if (!ok) gave_up = 1;
     } else {
         bool ok = true;
         const float scale = FMT == SBC_FP4_E4M3 ? *a.tensor_w * *a.tensor_x : 1.f;
-        int n = 0;
-        for (int tile = pair; tile < a.tiles; tile += pairs, ++n) {
-            const int b = n % buffers;
-            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(acc_full(b), (n / buffers) & 1));
+        Ring accs;
+        for (int tile = pair; tile < a.tiles; tile += pairs, accs.next(buffers)) {
+            const int b = accs.s;
+            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(acc_full(b), accs.turn));
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const long long j = (long long)(tile % a.tiles_w) * 256 + rank * 128 + warp * 32 + lane, x0 = (long long)(tile / a.tiles_w) * nt;
             const int tokens = (int)min((long long)nt, a.rows_x - x0);
