@@ -100,9 +100,10 @@ int sbc_fp4_dequantise(const sbc_fp4 *q, void *out, int dtype, int64_t row_strid
  * out[i, j] = sum_k a[i, k] * b[j, k]   (a.rows x b.rows, dtype), products and
  * sums in 32 bits on the tensor cores, rounded once at the end.
  *
- * a  activations: rows are tokens; b  weights: rows are output channels.  Both
- *    of the same format and the same cols.  The kernel reads whole weights and
- *    as many token rows as there are, so few tokens cost the weights' bytes.
+ * a  activations: rows are tokens; b  weights: rows are output channels (each
+ *    at most 2^31-513 rows).  Both of the same format and the same cols.  The
+ *    kernel reads whole weights and as many token rows as there are, so few
+ *    tokens cost the weights' bytes.
  * status  device, one uint32 (may be NULL): SBC_STATUS_TIMEOUT is or-ed in if a
  *    bounded device-side wait gave up; the affected outputs are then NaN.
  */

@@ -208,15 +208,26 @@ template <bool GRAD> int distill_by_type(const DistillArgs& a, int dtype, cudaSt
     });
 }
 
-template <typename T, int FMT>
-int launch_wide(const CUtensorMap& mw, const CUtensorMap& mx, const WideArgs& a, unsigned blocks, int smem, cudaStream_t st) {
-    if (!allow_smem<k_fp4_product_wide<T, FMT>>(kSmemMost - 1024)) return SBC_ECUDA;
-    k_fp4_product_wide<T, FMT><<<blocks, kWThreads, (size_t)smem, st>>>(mw, mx, a);
+template <typename T, int FMT, int NT>
+int launch_wide(const sbc_fp4* a, const sbc_fp4* b, WideArgs p, int64_t tiles, cudaStream_t st) {
+    using Shape = ProductShape<FMT>;
+    if (tiles > kMaxDim / 2) return SBC_EINVAL;
+    p.nt = NT;
+    p.tiles = (int)tiles;
+    const int stage = kPRows * kPBytes + NT / 2 * kPBytes, scales = kWScales * Shape::kTiles * 512 * (1 + NT / 128);
+    p.stages = std::min(std::min(kWMaxStages, (224 * 1024 - scales) / stage), 256 / (4 * Shape::kTiles * (1 + NT / 128)));
+    CUtensorMap mw, mx;
+    if (!values_map(&mw, b, kPRows) || !values_map(&mx, a, NT / 2)) return SBC_ECUDA;
+    if (!allow_smem<k_fp4_product_wide<T, FMT, NT>>(kSmemMost - 1024)) return SBC_ECUDA;
+    const unsigned blocks = (unsigned)(2 * std::min<int64_t>(std::max(1, sm_count() / 2), tiles));
+    // (always more than half of an SM's shared memory: a block takes all of its tensor memory)
+    k_fp4_product_wide<T, FMT, NT><<<blocks, kWThreads, (size_t)(p.stages * stage + scales + 1024), st>>>(mw, mx, p);
     return launched();
 }
 
 // More than 128 tokens: pairs of blocks that stay.  Tiles of 256 tokens where that makes two rounds of
-// tiles or more, of 128 (twice as many, and the accumulator twice) below.
+// tiles or more; else, and for 32-bit results (which do not fit in registers until they are stored),
+// tiles of 128 with two accumulators.
 int product_wide(const sbc_fp4* a, const sbc_fp4* b, void* out, int dtype, int64_t row_stride, uint32_t* status, cudaStream_t st) {
     WideArgs p = {};
     p.scales_w = static_cast<const uint8_t*>(b->scales);
@@ -231,23 +242,18 @@ int product_wide(const sbc_fp4* a, const sbc_fp4* b, void* out, int dtype, int64
     p.ktiles = ktiles_of(a->cols, a->format);
     p.chunks = (int)ceil_div(a->cols, 256);
     p.steps = (int)ceil_div(a->cols, 64);
-    const int64_t pairs = std::max(1, sm_count() / 2), tiles_w = ceil_div(b->rows, 256);
-    p.nt = tiles_w * ceil_div(a->rows, 256) >= 2 * pairs ? 256 : 128;
-    const int64_t tiles = tiles_w * ceil_div(a->rows, p.nt);
-    if (tiles > kMaxDim / 2) return SBC_EINVAL;
+    const int64_t tiles_w = ceil_div(b->rows, 256), tiles256 = tiles_w * ceil_div(a->rows, 256), tiles128 = tiles_w * ceil_div(a->rows, 128);
     p.tiles_w = (int)tiles_w;
-    p.tiles = (int)tiles;
-    const int tiles_k = a->format == SBC_FP4_E8M0 ? 2 : 4;
-    const int stage = kPRows * kPBytes + p.nt / 2 * kPBytes + tiles_k * 512 * (1 + p.nt / 128);
-    p.stages = std::min(std::min(kWMaxStages, 220 * 1024 / stage), 256 / (4 * tiles_k * (1 + p.nt / 128)));
-    CUtensorMap mw, mx;
-    if (!values_map(&mw, b, kPRows) || !values_map(&mx, a, p.nt / 2)) return SBC_ECUDA;
-    const unsigned blocks = (unsigned)(2 * std::min(pairs, tiles));
-    const int smem = std::max(p.stages * stage + 1024, kSmemMost / 2 + 1024);   // one block per SM: it takes all of tensor memory
+    const bool big = tiles256 >= sm_count();
     return by_dtype(dtype, [&](auto* as) {
         using T = std::remove_pointer_t<decltype(as)>;
-        return a->format == SBC_FP4_E4M3 ? launch_wide<T, SBC_FP4_E4M3>(mw, mx, p, blocks, smem, st)
-                                         : launch_wide<T, SBC_FP4_E8M0>(mw, mx, p, blocks, smem, st);
+        if constexpr (sizeof(T) == 2) {
+            if (big)
+                return a->format == SBC_FP4_E4M3 ? launch_wide<T, SBC_FP4_E4M3, 256>(a, b, p, tiles256, st)
+                                                 : launch_wide<T, SBC_FP4_E8M0, 256>(a, b, p, tiles256, st);
+        }
+        return a->format == SBC_FP4_E4M3 ? launch_wide<T, SBC_FP4_E4M3, 128>(a, b, p, tiles128, st)
+                                         : launch_wide<T, SBC_FP4_E8M0, 128>(a, b, p, tiles128, st);
     });
 }
 
@@ -343,6 +349,7 @@ int sbc_fp4_dequantise(const sbc_fp4* q, void* out, int dtype, int64_t row_strid
 int sbc_fp4_product(const sbc_fp4* a, const sbc_fp4* b, void* out, int dtype, int64_t row_stride, uint32_t* status,
                     sbc_cuda_stream_t stream) {
     if (!fp4_ok(a) || !fp4_ok(b) || a->format != b->format || a->cols != b->cols) return SBC_EINVAL;
+    if (a->rows > kMaxDim - 512 || b->rows > kMaxDim - 512) return SBC_EINVAL;
     if (!matrix_ok(out, dtype, a->rows, b->rows, row_stride) || !aligned(status, 4)) return SBC_EINVAL;
     if (a->rows > 128) return product_wide(a, b, out, dtype, row_stride, status, stream);
     ProductArgs p = {};

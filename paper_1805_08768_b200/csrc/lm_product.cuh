@@ -250,13 +250,18 @@ __global__ void __launch_bounds__(kPThreads) k_fp4_product(const __grid_constant
 // loads 0.58 bytes per thousand products where a block alone would load 0.82.  Blocks stay and take
 // tile after tile; loads run ahead across tiles.
 //
-// Scales reach tensor memory through registers (four warps that do nothing else): copies by the tensor
-// unit (tcgen05.cp) take turns with the products there, about 100 cycles each against 128 of a product.
+// What a stage costs is its way around the ring (products done, load, products) over the number of
+// stages, so nothing else is on that way: both blocks' loads count at the first block's barrier, and
+// the scales come through a deeper ring of their own.  They reach tensor memory through registers (four
+// warps that do nothing else): copies by the tensor unit (tcgen05.cp) take turns with the products
+// there, about 100 cycles each against 128 of a product.
 //
-// Warps: 0..3 accumulator to memory, 4..7 scales, 8 loads, 9 multiplies (in the first block of the pair).
+// Warps: 0..3 accumulator to memory, 4..7 scales, 8 loads, 9 multiplies (in the first block of the
+// pair), 10 loads scales.
 
-constexpr int kWThreads = 320;
+constexpr int kWThreads = 352;
 constexpr int kWMaxStages = 8;
+constexpr int kWScales = 8;   // stages of the scales' ring
 
 struct WideArgs {
     const uint8_t *scales_w, *scales_x;
@@ -311,27 +316,83 @@ __device__ __forceinline__ uint4 ld_shared16(uint32_t addr) {
     return q;
 }
 
-template <typename T, int FMT>
+__device__ __forceinline__ uint32_t pack2(float a, float b, const __nv_bfloat16*) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b, const __half*) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+__device__ __forceinline__ void store_half(void* p, uint32_t v) {
+    asm volatile("{\n\t.reg .b16 h, r;\n\tmov.b32 {h, r}, %1;\n\tst.global.b16 [%0], h;\n\t}" ::"l"(p), "r"(v) : "memory");
+}
+
+// A tile's accumulator, NT columns of this warp's 32 lanes, to `out` (one row per column); `free` is
+// called when it has left tensor memory.  16-bit results wait in registers, two to a word, so that the
+// next tile's products can begin before the stores have.
+template <typename T, int NT, typename F>
+__device__ __forceinline__ void store_tile(uint32_t acc, T* out, long long stride, int tokens, bool mine, float by, F free) {
+    if constexpr (sizeof(T) == 2) {
+        uint32_t w[NT / 2];
+#pragma unroll
+        for (int n0 = 0; n0 < NT; n0 += 16) {
+            float v[16];
+            tmem_load16(v, acc + n0);
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) w[(n0 + i) / 2] = pack2(v[i] * by, v[i + 1] * by, (const T*)nullptr);
+        }
+        free();
+        if (!mine) return;
+        // one store behind the other (volatile: the addresses would otherwise all be formed in front)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            if (n < tokens) store_half(out, n & 1 ? w[n / 2] >> 16 : w[n / 2]);
+            out += stride;
+        }
+    } else {
+#pragma unroll 1
+        for (int n0 = 0; n0 < NT; n0 += 32) {
+            float v[32];
+            __syncwarp();
+            tmem_load32(v, acc + n0);
+            if (n0 + 32 == NT) free();
+            if (!mine) continue;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                if (n0 + i < tokens) *out = from_float<T>(v[i] * by);
+                out += stride;
+            }
+        }
+    }
+}
+
+template <typename T, int FMT, int NT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWThreads, 1)
     k_fp4_product_wide(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, WideArgs a) {
     using S = ProductShape<FMT>;
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t bars[3 * kWMaxStages + 5];
+    __shared__ uint64_t bars[3 * kWMaxStages + 2 * kWScales + 5];
     __shared__ uint32_t tmem_slot, gave_up;
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
     const uint32_t rank = cluster_rank();
     const uint32_t smem = (smem_u32(raw) + 1023u) & ~1023u;
-    const int nt = a.nt, row_tiles = nt / 128, buffers = nt == 128 ? 2 : 1;
-    const uint32_t bytes_w = kPRows * kPBytes, bytes_x = (uint32_t)(nt / 2) * kPBytes, bytes_sc = S::kTiles * 512u;
-    const uint32_t stage_bytes = bytes_w + bytes_x + bytes_sc * (1 + row_tiles);   // a multiple of 1024
+    constexpr int row_tiles = NT / 128, buffers = NT == 128 ? 2 : 1;
+    constexpr uint32_t bytes_w = kPRows * kPBytes, bytes_x = NT / 2 * kPBytes, bytes_sc = S::kTiles * 512u;
+    constexpr uint32_t stage_bytes = bytes_w + bytes_x, scale_bytes = bytes_sc * (1 + row_tiles);
+    const uint32_t scales0 = smem + (uint32_t)a.stages * stage_bytes;
     const uint32_t bar0 = smem_u32(bars);
-    const auto full = [&](int s) { return bar0 + 24u * s; };           // this block's loads of a stage have landed
-    const auto ready = [&](int s) { return bar0 + 24u * s + 8; };      // both blocks' loads have, and their scales are in tensor memory
+    const auto full = [&](int s) { return bar0 + 24u * s; };           // (first block) both blocks' loads of a stage have landed
+    const auto ready = [&](int s) { return bar0 + 24u * s + 8; };      // (first block) both blocks' scales of it are in tensor memory
     const auto empty = [&](int s) { return bar0 + 24u * s + 16; };     // the products that read a stage are done
-    const auto acc_full = [&](int b) { return bar0 + 24u * kWMaxStages + 8u * b; };
-    const auto acc_empty = [&](int b) { return bar0 + 24u * kWMaxStages + 16 + 8u * b; };
-    const uint32_t drained = bar0 + 24u * kWMaxStages + 32;
-    const uint32_t acc_cols = 256, sc_cols = 4u * S::kTiles * (1 + row_tiles);
+    const auto sc_full = [&](int s) { return bar0 + 24u * kWMaxStages + 16u * s; };       // this block's scales have landed
+    const auto sc_empty = [&](int s) { return bar0 + 24u * kWMaxStages + 16u * s + 8; };  // ... are in registers
+    const uint32_t bar1 = bar0 + 24u * kWMaxStages + 16u * kWScales;
+    const auto acc_full = [&](int b) { return bar1 + 8u * b; };
+    const auto acc_empty = [&](int b) { return bar1 + 16 + 8u * b; };  // (first block)
+    const uint32_t drained = bar1 + 32;
+    constexpr uint32_t acc_cols = 256, sc_cols = 4u * S::kTiles * (1 + row_tiles);
     const int pairs = (int)(gridDim.x / 2), pair = (int)(blockIdx.x / 2);
 
     if (t == 0) {
@@ -340,6 +401,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWThreads, 1)
             mbar_init(full(s), 1);
             mbar_init(ready(s), 8);
             mbar_init(empty(s), 1);
+        }
+        for (int s = 0; s < kWScales; ++s) {
+            mbar_init(sc_full(s), 1);
+            mbar_init(sc_empty(s), 4);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(acc_full(b), 1);
@@ -357,7 +422,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWThreads, 1)
     cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_slot;
-    const float nan = __uint_as_float(0x7fffffffu);
 
     if (warp == 8) {
         if (lane == 0) {
@@ -366,26 +430,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWThreads, 1)
             int issued = 0;
             for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
                 const int w0 = tile % a.tiles_w * 256 + (int)rank * 128;
-                const int x0 = tile / a.tiles_w * nt, x1 = x0 + (int)rank * (nt / 2);
-                const bool has_w = w0 < a.rows_w;
-                const int x_tiles = (int)min((long long)row_tiles, (a.rows_x + 127) / 128 - x0 / 128);
-                const uint8_t* sw = a.scales_w + w0 / 128 * a.ktiles * 512;
-                const uint8_t* sx = a.scales_x + x0 / 128 * a.ktiles * 512;
-                const uint8_t* sx2 = sx + a.ktiles * 512;
-                int left = (int)a.ktiles;
+                const int x1 = tile / a.tiles_w * NT + (int)rank * (NT / 2);
                 for (int c = 0; c < a.chunks; ++c) {
-                    const uint32_t bar = full(ring.s);
-                    ok = mbar_wait(bar + 16, ring.turn ^ 1);
+                    ok = mbar_wait(empty(ring.s), ring.turn ^ 1);
                     if (!ok) break;
-                    const uint32_t sc = (uint32_t)min(S::kTiles, left) * 512u;
-                    const uint32_t at = smem + (uint32_t)ring.s * stage_bytes, at_x = at + bytes_w, at_sc = at_x + bytes_x;
-                    mbar_expect(bar, bytes_w + bytes_x + sc * ((has_w ? 1 : 0) + x_tiles));
-                    tma_load_2d(at, &map_w, c * kPBytes, w0, bar);
-                    tma_load_2d(at_x, &map_x, c * kPBytes, x1, bar);
-                    if (has_w) bulk_load(at_sc, sw, sc, bar);
-                    bulk_load(at_sc + bytes_sc, sx, sc, bar);
-                    if (x_tiles > 1) bulk_load(at_sc + 2 * bytes_sc, sx2, sc, bar);
-                    sw += S::kTiles * 512, sx += S::kTiles * 512, sx2 += S::kTiles * 512, left -= S::kTiles;
+                    const uint32_t at = smem + (uint32_t)ring.s * stage_bytes, bar = map_rank(full(ring.s), 0);
+                    // the second block's bytes may arrive before they are announced: the turn ends with the announcement
+                    if (rank == 0) mbar_expect(full(ring.s), 2 * stage_bytes);
+                    tma_load_2d_pair(at, &map_w, c * kPBytes, w0, bar);
+                    tma_load_2d_pair(at + bytes_w, &map_x, c * kPBytes, x1, bar);
                     ring.next(a.stages);
                     issued = min(issued + 1, a.stages);
                 }
@@ -395,29 +448,64 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWThreads, 1)
             for (int j = 0; j < issued; ++j) {
                 const int s = ring.s - 1 - j < 0 ? ring.s - 1 - j + a.stages : ring.s - 1 - j;
                 const uint32_t turn = ring.s - 1 - j < 0 ? ring.turn ^ 1 : ring.turn;
-                mbar_wait(full(s), turn);
+                if (rank == 0) mbar_wait(full(s), turn);
                 mbar_wait(empty(s), turn);
+            }
+        }
+    } else if (warp == 10) {
+        if (lane == 0) {
+            bool ok = true;
+            Ring ring;
+            int issued = 0;
+            for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
+                const int w0 = tile % a.tiles_w * 256 + (int)rank * 128, x0 = tile / a.tiles_w * NT;
+                const bool has_w = w0 < a.rows_w;
+                const int x_tiles = (int)min((long long)row_tiles, (a.rows_x + 127) / 128 - x0 / 128);
+                const uint8_t* sw = a.scales_w + w0 / 128 * a.ktiles * 512;
+                const uint8_t* sx = a.scales_x + x0 / 128 * a.ktiles * 512;
+                const uint8_t* sx2 = sx + a.ktiles * 512;
+                int left = (int)a.ktiles;
+                for (int c = 0; c < a.chunks; ++c) {
+                    const uint32_t bar = sc_full(ring.s);
+                    ok = mbar_wait(bar + 8, ring.turn ^ 1);
+                    if (!ok) break;
+                    const uint32_t sc = (uint32_t)min(S::kTiles, left) * 512u, at = scales0 + (uint32_t)ring.s * scale_bytes;
+                    mbar_expect(bar, sc * ((has_w ? 1 : 0) + x_tiles));
+                    if (has_w) bulk_load(at, sw, sc, bar);
+                    bulk_load(at + bytes_sc, sx, sc, bar);
+                    if (x_tiles > 1) bulk_load(at + 2 * bytes_sc, sx2, sc, bar);
+                    sw += S::kTiles * 512, sx += S::kTiles * 512, sx2 += S::kTiles * 512, left -= S::kTiles;
+                    ring.next(kWScales);
+                    issued = min(issued + 1, kWScales);
+                }
+            }
+            if (!ok) gave_up = 1;
+            for (int j = 0; j < issued; ++j) {
+                const int s = ring.s - 1 - j < 0 ? ring.s - 1 - j + kWScales : ring.s - 1 - j;
+                mbar_wait(sc_full(s), ring.s - 1 - j < 0 ? ring.turn ^ 1 : ring.turn);
             }
         }
     } else if (warp == 9) {
         if (lane == 0 && rank != 0) mbar_wait(drained, 0);
         if (lane == 0 && rank == 0) {
             bool ok = true;
-            const uint32_t idesc = (1u << 7) | (1u << 10) | (FMT == SBC_FP4_E8M0 ? 1u << 23 : 0u) | (2u << 27) | ((uint32_t)(nt >> 3) << 17);
+            const uint32_t idesc = (1u << 7) | (1u << 10) | (FMT == SBC_FP4_E8M0 ? 1u << 23 : 0u) | (2u << 27) | ((uint32_t)(NT >> 3) << 17);
             Ring ring, accs;
             for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
                 const int b = accs.s;
-                ok = mbar_wait_cluster(acc_empty(b), accs.turn ^ 1);
+                ok = mbar_wait(acc_empty(b), accs.turn ^ 1);
                 if (!ok) break;
                 const uint32_t acc = tmem + (uint32_t)b * 128u;
                 for (int c = 0; c < a.chunks; ++c) {
-                    ok = mbar_wait_cluster(ready(ring.s), ring.turn);
+                    ok = mbar_wait(ready(ring.s), ring.turn) && mbar_wait(full(ring.s), ring.turn);
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t at = smem + (uint32_t)ring.s * stage_bytes, at_x = at + bytes_w;
                     const uint32_t sf_w = tmem + acc_cols + (uint32_t)ring.s * sc_cols, sf_x = sf_w + 4 * S::kTiles;
                     const int steps = min(4, a.steps - c * 4);
-                    for (int k = 0; k < steps; ++k) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (k >= steps) break;
                         // E8M0: two steps share a scale tile, each takes its half of every word
                         const int tile_k = FMT == SBC_FP4_E8M0 ? k / 2 : k;
                         const uint32_t half = FMT == SBC_FP4_E8M0 ? (uint32_t)(k & 1) * 2u : 0u;
@@ -438,34 +526,35 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWThreads, 1)
     } else if (warp >= 4) {
         bool ok = true;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;
-        Ring ring;
+        Ring ring, from;
         for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
             for (int c = 0; c < a.chunks; ++c) {
-                ok = __all_sync(0xffffffffu, mbar_wait(full(ring.s), ring.turn));
+                ok = __all_sync(0xffffffffu, mbar_wait(sc_full(from.s), from.turn));
                 if (!ok) break;
-                const uint32_t at = smem + (uint32_t)ring.s * stage_bytes + bytes_w + bytes_x + 16u * lane;
+                const uint32_t at = scales0 + (uint32_t)from.s * scale_bytes + 16u * lane;
                 const uint32_t sf = tmem + acc_cols + (uint32_t)ring.s * sc_cols + lanes;
-                uint4 q[S::kTiles * 3];
-#pragma unroll
-                for (int k = 0; k < S::kTiles; ++k) q[k] = ld_shared16(at + 512u * k);
+                uint4 q[S::kTiles * (1 + row_tiles)];
 #pragma unroll
                 for (int k = 0; k < S::kTiles; ++k) {
-                    q[S::kTiles + 2 * k] = ld_shared16(at + bytes_sc + 512u * k);
-                    if (row_tiles == 2) q[S::kTiles + 2 * k + 1] = ld_shared16(at + 2 * bytes_sc + 512u * k);
-                }
+                    q[k] = ld_shared16(at + 512u * k);
 #pragma unroll
-                for (int k = 0; k < S::kTiles; ++k) tmem_store4(sf + 4u * k, q[k]);
-#pragma unroll
-                for (int k = 0; k < S::kTiles; ++k) {
-                    const uint32_t to = sf + 4u * S::kTiles + 4u * k * row_tiles;
-                    tmem_store4(to, q[S::kTiles + 2 * k]);
-                    if (row_tiles == 2) tmem_store4(to + 4u, q[S::kTiles + 2 * k + 1]);
+                    for (int j = 0; j < row_tiles; ++j) q[S::kTiles + k * row_tiles + j] = ld_shared16(at + bytes_sc * (1 + j) + 512u * k);
                 }
+                // the stage's columns of tensor memory are free when its last products are done
+                ok = __all_sync(0xffffffffu, mbar_wait(empty(ring.s), ring.turn ^ 1));
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                for (int k = 0; k < S::kTiles * (1 + row_tiles); ++k) tmem_store4(sf + 4u * k, q[k]);
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) mbar_arrive_remote(map_rank(ready(ring.s), 0));
+                if (lane == 0) {
+                    mbar_arrive_remote(map_rank(ready(ring.s), 0));
+                    mbar_arrive_remote(map_rank(sc_empty(from.s), rank));
+                }
                 ring.next(a.stages);
+                from.next(kWScales);
             }
         }
         if (!ok) gave_up = 1;
@@ -477,36 +566,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWThreads, 1)
             const int b = accs.s;
             if (ok) ok = __all_sync(0xffffffffu, mbar_wait(acc_full(b), accs.turn));
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const long long j = (long long)(tile % a.tiles_w) * 256 + rank * 128 + warp * 32 + lane, x0 = (long long)(tile / a.tiles_w) * nt;
-            const int tokens = (int)min((long long)nt, a.rows_x - x0);
-            T* out = static_cast<T*>(a.out) + x0 * a.stride + j;
-            const bool mine = j < a.rows_w;
-            const uint32_t acc = tmem + (uint32_t)b * 128u + ((uint32_t)warp << 21);
-            for (int n0 = 0; n0 < nt; n0 += 32) {
-                float v[32];
-                __syncwarp();
-                tmem_load32(v, acc + n0);
-                if (n0 + 32 >= nt) {
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_remote(map_rank(acc_empty(b), 0));
-                }
-                const float by = ok ? scale : nan;
-                if (mine && n0 + 32 <= tokens) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        *out = from_float<T>(v[i] * by);
-                        out += a.stride;
-                    }
-                } else if (mine) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (n0 + i < tokens) {
-                            *out = from_float<T>(v[i] * by);
-                            out += a.stride;
-                        }
-                }
-            }
+            const long long j = (long long)(tile % a.tiles_w) * 256 + rank * 128 + warp * 32 + lane, x0 = (long long)(tile / a.tiles_w) * NT;
+            store_tile<T, NT>(tmem + (uint32_t)b * 128u + ((uint32_t)warp << 21), static_cast<T*>(a.out) + x0 * a.stride + j, a.stride,
+                              (int)min((long long)NT, a.rows_x - x0), j < a.rows_w, ok ? scale : __uint_as_float(0x7fffffffu), [&] {
+                                  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                                  __syncwarp();
+                                  if (lane == 0) mbar_arrive_remote(map_rank(acc_empty(b), 0));
+                              });
+            __syncwarp();
         }
         if (!ok) gave_up = 1;
     }
