@@ -256,10 +256,10 @@ __global__ void __launch_bounds__(kPThreads) k_fp4_product(const __grid_constant
 // warps that do nothing else): copies by the tensor unit (tcgen05.cp) take turns with the products
 // there, about 100 cycles each against 128 of a product.
 //
-// Warps: 0..3 accumulator to memory, 4..7 scales, 8 loads, 9 multiplies (in the first block of the
-// pair), 10 loads scales.
+// Warps: 0..3 and 12..15 accumulator to memory (half of the columns each), 4..7 scales, 8 loads, 9
+// multiplies (in the first block of the pair), 10 loads scales.
 
-constexpr int kWThreads = 352;
+constexpr int kWThreads = 512;
 constexpr int kWMaxStages = 8;
 constexpr int kWScales = 8;   // stages of the scales' ring
 
@@ -329,41 +329,54 @@ __device__ __forceinline__ void store_half(void* p, uint32_t v) {
     asm volatile("{\n\t.reg .b16 h, r;\n\tmov.b32 {h, r}, %1;\n\tst.global.b16 [%0], h;\n\t}" ::"l"(p), "r"(v) : "memory");
 }
 
-// A tile's accumulator, NT columns of this warp's 32 lanes, to `out` (one row per column); `free` is
-// called when it has left tensor memory.  16-bit results wait in registers, two to a word, so that the
-// next tile's products can begin before the stores have.
-template <typename T, int NT, typename F>
+__device__ __forceinline__ void store_word(void* p, uint32_t v) { asm volatile("st.global.b32 [%0], %1;" ::"l"(p), "r"(v) : "memory"); }
+
+// COLS columns of an accumulator, this warp's 32 lanes, to `out` (this lane's weight of the first
+// token); `free` is called when they have left tensor memory: results wait in registers (16-bit ones
+// two to a word), so that the next tile's products can begin before the stores have.  Stores follow
+// one another (volatile: their addresses would otherwise all be formed in front).
+// PAIRS: 16-bit results whose even places are 4-byte aligned.  Neighbouring lanes swap halves, so that
+// one has two weights of a token and the other the same two of the next.
+template <typename T, int COLS, bool PAIRS, typename F>
 __device__ __forceinline__ void store_tile(uint32_t acc, T* out, long long stride, int tokens, bool mine, float by, F free) {
     if constexpr (sizeof(T) == 2) {
-        uint32_t w[NT / 2];
+        uint32_t w[COLS / 2];
 #pragma unroll
-        for (int n0 = 0; n0 < NT; n0 += 16) {
-            float v[16];
-            tmem_load16(v, acc + n0);
+        for (int n0 = 0; n0 < COLS; n0 += 32) {
+            float v[32];
+            tmem_load32(v, acc + n0);
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) w[(n0 + i) / 2] = pack2(v[i] * by, v[i + 1] * by, (const T*)nullptr);
+            for (int i = 0; i < 32; i += 2) w[(n0 + i) / 2] = pack2(v[i] * by, v[i + 1] * by, (const T*)nullptr);
         }
         free();
-        if (!mine) return;
-        // one store behind the other (volatile: the addresses would otherwise all be formed in front)
+        if (PAIRS) {
+            const bool odd = threadIdx.x & 1;
+            T* to = odd ? out - 1 + stride : out;
+            const int most = mine ? tokens - (odd ? 1 : 0) : 0;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            if (n < tokens) store_half(out, n & 1 ? w[n / 2] >> 16 : w[n / 2]);
-            out += stride;
-        }
-    } else {
-#pragma unroll 1
-        for (int n0 = 0; n0 < NT; n0 += 32) {
-            float v[32];
-            __syncwarp();
-            tmem_load32(v, acc + n0);
-            if (n0 + 32 == NT) free();
-            if (!mine) continue;
+            for (int n = 0; n < COLS; n += 2) {
+                const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? w[n / 2] : w[n / 2] >> 16, 1);
+                if (n < most) store_word(to, odd ? __byte_perm(other, w[n / 2], 0x7610) : __byte_perm(w[n / 2], other, 0x5410));
+                to += 2 * stride;
+            }
+        } else {
+            const int most = mine ? tokens : 0;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                if (n0 + i < tokens) *out = from_float<T>(v[i] * by);
+            for (int n = 0; n < COLS; ++n) {
+                if (n < most) store_half(out, n & 1 ? w[n / 2] >> 16 : w[n / 2]);
                 out += stride;
             }
+        }
+    } else {
+        float v[COLS];
+#pragma unroll
+        for (int n0 = 0; n0 < COLS; n0 += 32) tmem_load32(v + n0, acc + n0);
+        free();
+        const int most = mine ? tokens : 0;
+#pragma unroll
+        for (int n = 0; n < COLS; ++n) {
+            if (n < most) store_word(out, __float_as_uint(v[n] * by));
+            out += stride;
         }
     }
 }
@@ -408,7 +421,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWThreads, 1)
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(acc_full(b), 1);
-            mbar_init(acc_empty(b), 8);
+            mbar_init(acc_empty(b), 16);
         }
         mbar_init(drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -523,7 +536,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWThreads, 1)
             commit2(drained);
             mbar_wait(drained, 0);
         }
-    } else if (warp >= 4) {
+    } else if (warp >= 4 && warp < 8) {
         bool ok = true;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;
         Ring ring, from;
@@ -558,21 +571,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWThreads, 1)
             }
         }
         if (!ok) gave_up = 1;
-    } else {
+    } else if (warp < 4 || warp >= 12) {
         bool ok = true;
         const float scale = FMT == SBC_FP4_E4M3 ? *a.tensor_w * *a.tensor_x : 1.f;
+        constexpr int kCols = NT / 2;
+        const int col0 = warp < 4 ? 0 : kCols, sub = warp & 3;
+        const bool pairs_ok = sizeof(T) == 2 && ((a.stride | a.rows_w) & 1) == 0 && ((uintptr_t)a.out & 3) == 0;
         Ring accs;
         for (int tile = pair; tile < a.tiles; tile += pairs, accs.next(buffers)) {
             const int b = accs.s;
             if (ok) ok = __all_sync(0xffffffffu, mbar_wait(acc_full(b), accs.turn));
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const long long j = (long long)(tile % a.tiles_w) * 256 + rank * 128 + warp * 32 + lane, x0 = (long long)(tile / a.tiles_w) * NT;
-            store_tile<T, NT>(tmem + (uint32_t)b * 128u + ((uint32_t)warp << 21), static_cast<T*>(a.out) + x0 * a.stride + j, a.stride,
-                              (int)min((long long)NT, a.rows_x - x0), j < a.rows_w, ok ? scale : __uint_as_float(0x7fffffffu), [&] {
-                                  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                                  __syncwarp();
-                                  if (lane == 0) mbar_arrive_remote(map_rank(acc_empty(b), 0));
-                              });
+            const long long j = (long long)(tile % a.tiles_w) * 256 + rank * 128 + sub * 32 + lane, x0 = (long long)(tile / a.tiles_w) * NT + col0;
+            const uint32_t acc = tmem + (uint32_t)b * 128u + (uint32_t)col0 + ((uint32_t)sub << 21);
+            T* out = static_cast<T*>(a.out) + x0 * a.stride + j;
+            const int tokens = (int)min((long long)kCols, a.rows_x - x0);
+            const float by = ok ? scale : __uint_as_float(0x7fffffffu);
+            const auto free = [&] {
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive_remote(map_rank(acc_empty(b), 0));
+            };
+            if (pairs_ok)
+                store_tile<T, kCols, true>(acc, out, a.stride, tokens, j < a.rows_w, by, free);
+            else
+                store_tile<T, kCols, false>(acc, out, a.stride, tokens, j < a.rows_w, by, free);
             __syncwarp();
         }
         if (!ok) gave_up = 1;
