@@ -68,6 +68,12 @@ template <auto Kernel> bool allow_smem(int bytes) {
     return true;
 }
 
+// Blocks that have a piece of a matrix for every warp.
+int64_t pieces(int64_t rows, int64_t cols, bool flat) {
+    const int64_t n = flat ? ceil_div(rows * cols, kPiece) : rows * ceil_div(cols, kPiece);
+    return ceil_div(n, kQThreads / 32);
+}
+
 int launched() { return cudaGetLastError() == cudaSuccess ? SBC_OK : SBC_ECUDA; }
 
 template <typename T, int FMT> void launch_quantise(const QuantiseArgs& a, bool rows, bool cols, unsigned grid, cudaStream_t st) {
@@ -311,7 +317,7 @@ int sbc_fp4_quantise(const void* x, int dtype, int64_t rows, int64_t cols, int64
         cudaStream_t st = stream;
         if (format == SBC_FP4_E4M3) {
             if (rows * cols > kAmaxAlone) {
-                a.amax_blocks = (int)std::min<int64_t>(ceil_div(rows * ceil_div(cols, 8), kQThreads * 4), kAmaxBlocks);
+                a.amax_blocks = (int)std::min<int64_t>(pieces(rows, cols, row_stride == cols), kAmaxBlocks);
                 k_fp4_amax<T><<<(unsigned)a.amax_blocks, kQThreads, 0, st>>>(a, static_cast<uint32_t*>(workspace));
             }
             launch_quantise<T, SBC_FP4_E4M3>(a, along_rows, along_cols, (unsigned)(row_tiles * col_tiles), st);
@@ -335,7 +341,7 @@ int sbc_fp4_dequantise(const sbc_fp4* q, void* out, int dtype, int64_t row_strid
     a.pitch = (long long)sbc_fp4_row_bytes(q->cols);
     a.ktiles = ktiles_of(q->cols, q->format);
     a.align = row_align(out, row_stride, width_of(dtype));
-    const int64_t blocks = std::min<int64_t>(ceil_div(q->rows * ceil_div(q->cols, 8), kQThreads), sm_count() * 16);
+    const int64_t blocks = std::min<int64_t>(pieces(q->rows, q->cols, false), sm_count() * 8);
     return by_dtype(dtype, [&](auto* as) {
         using T = std::remove_pointer_t<decltype(as)>;
         if (q->format == SBC_FP4_E4M3)

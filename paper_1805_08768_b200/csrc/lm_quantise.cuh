@@ -6,6 +6,9 @@
 // that decides like the exact one: a grid midpoint m has at most 3 significant bits, m * s is a
 // float, so an x that is not m * s differs from it by at least one unit in the last place, and the
 // rounded quotient then is not m either.  The same holds for the block scale, amax / (6 * 2^g).
+// The quotient comes from the block's rounded reciprocal r: q = x r, and one correction by the residual
+// x - q s, which a fused operation gives exactly (Markstein 1990); the power of two is taken off first,
+// so s is in [2^-9, 448] and nothing over- or underflows that could matter.
 #pragma once
 
 #include "lm_common.cuh"
@@ -29,27 +32,33 @@ __device__ __forceinline__ float tensor_scale_of(uint32_t amax_bits) {
     return pow2(max(e - 127 - 10, -126));
 }
 
-// A block's scale code, and the factor or divisor its elements take.
-template <int FMT> __device__ __forceinline__ uint32_t scale_code(uint32_t amax_bits, float tensor, float* by) {
-    if (amax_bits >= 0x7f800000u) {
-        *by = 0.f;
-        return Fp4<FMT>::kNanScale;
+// A block's scale, ready for its elements.
+template <int FMT> struct BlockScale {
+    uint32_t code;
+    float by, inv;   // E8M0: by = 1 / scale.  E4M3: by = the code's value, inv its rounded reciprocal.  0: the block is zeros
+    __device__ __forceinline__ BlockScale(uint32_t amax_bits, float tensor, float inv_tensor) : inv(0.f) {
+        if (FMT == SBC_FP4_E8M0) {
+            code = (uint32_t)max((int)(amax_bits >> 23) - 2, 0);
+            by = __uint_as_float((254u - code) << 23);
+        } else {
+            const float want = __uint_as_float(amax_bits) / (6.f * tensor);
+            code = __nv_cvt_float_to_fp8(want, __NV_SATFINITE, __NV_E4M3);
+            by = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3)));
+            inv = by > 0.f ? 1.f / by : 0.f;
+        }
+        if (amax_bits >= 0x7f800000u) {
+            code = Fp4<FMT>::kNanScale;
+            by = inv = 0.f;
+        }
     }
-    if (FMT == SBC_FP4_E8M0) {
-        const uint32_t code = (uint32_t)max((int)(amax_bits >> 23) - 2, 0);
-        *by = __uint_as_float((254u - code) << 23);  // 1 / scale, exact
-        return code;
+    __device__ __forceinline__ bool zero() const { return by == 0.f; }
+    // quotient of x (E4M3: of x already divided by the tensor's scale)
+    __device__ __forceinline__ float over(float x) const {
+        if (FMT == SBC_FP4_E8M0) return x * by;
+        const float q = __fmul_rn(x, inv);
+        return fmaf(fmaf(-q, by, x), inv, q);
     }
-    const float want = __uint_as_float(amax_bits) / (6.f * tensor);
-    const uint32_t code = __nv_cvt_float_to_fp8(want, __NV_SATFINITE, __NV_E4M3);
-    *by = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3))) * tensor;
-    return code;
-}
-
-template <int FMT> __device__ __forceinline__ float scaled(float x, float by) {
-    if (FMT == SBC_FP4_E8M0) return x * by;
-    return by > 0.f ? x / by : 0.f;
-}
+};
 
 // Eight values to eight nibbles, the first one lowest.
 __device__ __forceinline__ uint32_t pack_nibbles(const float* y) {
@@ -63,6 +72,34 @@ __device__ __forceinline__ uint32_t pack_nibbles(const float* y) {
         : "=r"(w)
         : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
     return w;
+}
+
+// Eight values, and the bits of the largest magnitude among them (as a float's; whole numbers, so a NaN
+// is above an infinity is above all else).
+__device__ __forceinline__ uint32_t unpack_max(float* y, const Pack8<float>& v) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        y[j] = v.e[j];
+        top = max(top, __float_as_uint(y[j]) & 0x7fffffffu);
+    }
+    return top;
+}
+__device__ __forceinline__ uint32_t max_halves(const uint32_t* w, int n) {
+    uint32_t top = w[0] & 0x7fff7fffu;
+#pragma unroll
+    for (int j = 1; j < n; ++j) top = __vmaxu2(top, w[j] & 0x7fff7fffu);
+    return top;
+}
+__device__ __forceinline__ uint32_t float_bits_of(uint32_t half_bits, const __nv_bfloat16*) { return half_bits << 16; }
+__device__ __forceinline__ uint32_t float_bits_of(uint32_t half_bits, const __half*) {
+    return __float_as_uint(__half2float(__ushort_as_half((unsigned short)half_bits)));
+}
+template <typename T> __device__ __forceinline__ uint32_t unpack_max(float* y, const Pack8<T>& v) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = to_float(v.e[j]);
+    const uint32_t top = max_halves(v.w, 4);
+    return float_bits_of(max(top & 0xffffu, top >> 16), (const T*)nullptr);
 }
 
 struct QuantiseArgs {
@@ -83,22 +120,47 @@ struct QuantiseArgs {
 constexpr int kAmaxBlocks = 1024;
 constexpr long long kAmaxAlone = 32768;   // elements up to which every block finds the maximum itself, instead of a launch in front
 
-// Largest finite magnitude of the elements that threads [at, at + step, ...) of the tensor take, over the
-// block, as float bits (whole numbers: the maximum does not depend on the order).
-template <typename T> __device__ __forceinline__ uint32_t amax_over(const QuantiseArgs& a, long long at, long long step, uint32_t* room) {
-    const T* x = static_cast<const T*>(a.x);
-    const long long per_row = (a.cols + 7) / 8, all = per_row * a.rows;
-    uint32_t top = 0;
-    for (long long i = at; i < all; i += step) {
-        const long long r = all < (1ll << 31) ? (long long)((uint32_t)i / (uint32_t)per_row) : i / per_row, c = (i - r * per_row) * 8;
-        Pack8<T> v;
-        load8(v, x + r * a.stride + c, (int)min(8LL, a.cols - c), a.align);
+// A warp's share of a matrix: rows in pieces of 2048 elements, 256 at a time.  f(row, column) for eight
+// elements a lane.
+constexpr int kPiece = 2048;
+template <typename F> __device__ __forceinline__ void warp_pieces(long long rows, long long cols, uint32_t warp, uint32_t warps, F f) {
+    const uint32_t per_row = (uint32_t)((cols + kPiece - 1) / kPiece);
+    const long long all = rows * per_row;
+    for (long long i = warp; i < all; i += warps) {
+        const long long r = all < (1ll << 32) ? (long long)((uint32_t)i / per_row) : i / per_row;
+        const long long c0 = (i - r * per_row) * kPiece + (threadIdx.x & 31) * 8;
+        if (c0 + kPiece - 256 + 8 <= cols) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t b = __float_as_uint(to_float(v.e[j])) & 0x7fffffffu;
-            top = max(top, b < 0x7f800000u ? b : 0u);
+            for (int k = 0; k < kPiece; k += 256) f(r, c0 + k);
+        } else {
+            for (int k = 0; k < kPiece && c0 + k < cols; k += 256) f(r, c0 + k);
         }
     }
+}
+
+// Largest finite magnitude of the warps' shares, over the block, as float bits (whole numbers: the
+// maximum does not depend on the order).
+template <typename T> __device__ __forceinline__ uint32_t amax_over(const QuantiseArgs& a, uint32_t warp, uint32_t warps, uint32_t* room) {
+    const T* x = static_cast<const T*>(a.x);
+    // rows without gaps are one long row
+    const bool flat = a.stride == a.cols;
+    const long long rows = flat ? 1 : a.rows, cols = flat ? a.rows * a.cols : a.cols;
+    uint32_t top = 0;
+    warp_pieces(rows, cols, warp, warps, [&](long long r, long long c) {
+        Pack8<T> v;
+        load8(v, x + r * a.stride + c, (int)min(8LL, cols - c), a.align);
+        float y[8];
+        const uint32_t m = unpack_max(y, v);
+        if (m < 0x7f800000u) {
+            top = max(top, m);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t b = __float_as_uint(y[j]) & 0x7fffffffu;
+                top = max(top, b < 0x7f800000u ? b : 0u);
+            }
+        }
+    });
     top = __reduce_max_sync(0xffffffffu, top);
     if ((threadIdx.x & 31) == 0) room[threadIdx.x >> 5] = top;
     __syncthreads();
@@ -107,14 +169,14 @@ template <typename T> __device__ __forceinline__ uint32_t amax_over(const Quanti
 
 template <typename T> __global__ void __launch_bounds__(kQThreads) k_fp4_amax(QuantiseArgs a, uint32_t* amax) {
     __shared__ uint32_t room[kQThreads / 32];
-    const uint32_t top = amax_over<T>(a, (long long)blockIdx.x * kQThreads + threadIdx.x, (long long)gridDim.x * kQThreads, room);
+    const uint32_t top = amax_over<T>(a, blockIdx.x * (kQThreads / 32) + threadIdx.x / 32, gridDim.x * (kQThreads / 32), room);
     if (threadIdx.x == 0) amax[blockIdx.x] = top;
 }
 
 // The tensor's, in every block of the quantising kernel.
 template <typename T> __device__ __forceinline__ uint32_t tensor_amax(const QuantiseArgs& a) {
     __shared__ uint32_t room[kQThreads / 32];
-    if (a.amax_blocks == 0) return amax_over<T>(a, threadIdx.x, kQThreads, room);
+    if (a.amax_blocks == 0) return amax_over<T>(a, threadIdx.x / 32, kQThreads / 32, room);
     uint32_t top = 0;
     for (int i = threadIdx.x; i < a.amax_blocks; i += kQThreads) top = max(top, a.amax[i]);
     top = __reduce_max_sync(0xffffffffu, top);
@@ -123,20 +185,94 @@ template <typename T> __device__ __forceinline__ uint32_t tensor_amax(const Quan
     return __reduce_max_sync(0xffffffffu, room[threadIdx.x & (kQThreads / 32 - 1)]);
 }
 
+// N (16 or 32, a block's elements) values down a column to nibbles and the block's scale code.
+template <int FMT, int N> __device__ __forceinline__ uint32_t quantise_run(uint32_t* nibbles, float* y, uint32_t top, float tensor, float inv_tensor) {
+    const BlockScale<FMT> scale(top, tensor, inv_tensor);
+#pragma unroll
+    for (int j = 0; j < N; ++j) y[j] = scale.over(FMT == SBC_FP4_E4M3 ? y[j] * inv_tensor : y[j]);
+#pragma unroll
+    for (int j = 0; j < N / 8; ++j) nibbles[j] = scale.zero() ? 0u : pack_nibbles(y + 8 * j);
+    return scale.code;
+}
+
+// 32 rows of a column (16 bytes of nibbles, one or two scales) to the transpose.
+template <int FMT>
+__device__ __forceinline__ void store_column(const QuantiseArgs& a, long long out_row, long long row, const uint32_t* n, uint32_t codes) {
+    if (out_row < a.cols && row / 2 < a.pitch_c) *reinterpret_cast<uint4*>(a.values_c + out_row * a.pitch_c + row / 2) = make_uint4(n[0], n[1], n[2], n[3]);
+    const long long block = row / Fp4<FMT>::kBlock, k = block / 4;   // block % 4 is even for two scales
+    if (k < a.ktiles_c) {
+        uint8_t* p = a.scales_c + (out_row / 128 * a.ktiles_c + k) * 512 + (out_row % 32) * 16 + (out_row % 128 / 32) * 4 + block % 4;
+        if (FMT == SBC_FP4_E8M0)
+            *p = (uint8_t)codes;
+        else
+            *reinterpret_cast<uint16_t*>(p) = (uint16_t)codes;
+    }
+}
+
+// The columns of a pass (128 rows of 16-bit elements, two columns and 32 rows a thread; 64 rows of floats,
+// one column and 32 rows a thread) to the transpose.
+template <typename T, int FMT>
+__device__ __forceinline__ void quantise_columns(const QuantiseArgs& a, const T* tile, int stride, uint32_t row_tile, uint32_t col_tile, int pass,
+                                                 float tensor, float inv_tensor) {
+    constexpr int kB = Fp4<FMT>::kBlock;
+    const int t = threadIdx.x;
+    if constexpr (sizeof(T) == 2) {
+        const int c = t % 64 * 2, r0 = t / 64 * 32;
+        uint32_t w[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) w[j] = *reinterpret_cast<const uint32_t*>(tile + (r0 + j) * stride + c);
+        const long long row = (long long)row_tile * kQTile + pass + r0, out_row = (long long)col_tile * kQTile + c;
+        uint32_t top[32 / kB];
+#pragma unroll
+        for (int b = 0; b < 32 / kB; ++b) top[b] = max_halves(w + b * kB, kB);
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+            uint32_t n[4], codes = 0;
+#pragma unroll
+            for (int b = 0; b < 32 / kB; ++b) {
+                float y[kB];
+#pragma unroll
+                for (int j = 0; j < kB; ++j) y[j] = to_float(reinterpret_cast<const T*>(&w[b * kB + j])[side]);
+                codes |= quantise_run<FMT, kB>(n + b * (kB / 8), y, float_bits_of(side ? top[b] >> 16 : top[b] & 0xffffu, (const T*)nullptr), tensor, inv_tensor)
+                         << (8 * b);
+            }
+            store_column<FMT>(a, out_row + side, row, n, codes);
+        }
+    } else {
+        const int c = t % kQTile, r0 = t / kQTile * 32;
+        const long long row = (long long)row_tile * kQTile + pass + r0;
+        uint32_t n[4], codes = 0;
+#pragma unroll
+        for (int b = 0; b < 32 / kB; ++b) {
+            float y[kB];
+            uint32_t top = 0;
+#pragma unroll
+            for (int j = 0; j < kB; ++j) {
+                y[j] = tile[(r0 + b * kB + j) * stride + c];
+                top = max(top, __float_as_uint(y[j]) & 0x7fffffffu);
+            }
+            codes |= quantise_run<FMT, kB>(n + b * (kB / 8), y, top, tensor, inv_tensor) << (8 * b);
+        }
+        store_column<FMT>(a, (long long)col_tile * kQTile + c, row, n, codes);
+    }
+}
+
 // One block takes a 128 x 128 tile, which is whole scale tiles of either orientation.
 template <typename T, int FMT, bool ROWS, bool COLS> __global__ void __launch_bounds__(kQThreads) k_fp4_quantise(QuantiseArgs a) {
     constexpr int kB = Fp4<FMT>::kBlock, kBlocks = kQTile / kB;  // blocks along a tile's side
     constexpr int kPad = 16 / (int)sizeof(T);
     constexpr int kPass = COLS ? 256 / (int)sizeof(T) : kQTile;  // rows held in shared memory at a time (up to 34 KB)
-    constexpr int kHalf = kPass / 2;                             // rows of a column that one thread takes
     __shared__ uint32_t codes[kQTile][kBlocks / 4];              // a row's scale bytes, four to a word
     __shared__ alignas(16) T tile[COLS ? kPass : 1][COLS ? kQTile + kPad : 8];
     const T* x = static_cast<const T*>(a.x);
     const int t = threadIdx.x, lane = t & 31;
     const uint32_t row_tile = blockIdx.x / a.col_tiles, col_tile = blockIdx.x % a.col_tiles;
     const long long row0 = (long long)row_tile * kQTile, col0 = (long long)col_tile * kQTile;
-    float tensor = 1.f;
-    if (FMT == SBC_FP4_E4M3) tensor = tensor_scale_of(tensor_amax<T>(a));
+    float tensor = 1.f, inv_tensor = 1.f;
+    if (FMT == SBC_FP4_E4M3) {
+        tensor = tensor_scale_of(tensor_amax<T>(a));
+        inv_tensor = 1.f / tensor;
+    }
     if (blockIdx.x == 0 && t == 0) {
         if (ROWS) *a.tensor_r = tensor;
         if (COLS) *a.tensor_c = tensor;
@@ -156,66 +292,20 @@ template <typename T, int FMT, bool ROWS, bool COLS> __global__ void __launch_bo
             }
             if (ROWS) {
                 float y[8];
-                uint32_t top = 0;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    y[j] = to_float(v.e[j]);
-                    top = max(top, __float_as_uint(y[j]) & 0x7fffffffu);
-                }
+                uint32_t top = unpack_max(y, v);
 #pragma unroll
                 for (int d = 1; d < kB / 8; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
-                float by;
-                const uint32_t code = scale_code<FMT>(top, tensor, &by);
+                const BlockScale<FMT> scale(top, tensor, inv_tensor);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] = scaled<FMT>(y[j], by);
+                for (int j = 0; j < 8; ++j) y[j] = scale.over(FMT == SBC_FP4_E4M3 ? y[j] * inv_tensor : y[j]);
                 if (r < a.rows && (col0 + cc) / 2 < a.pitch_r)
-                    *reinterpret_cast<uint32_t*>(a.values_r + r * a.pitch_r + (col0 + cc) / 2) = by > 0.f ? pack_nibbles(y) : 0u;
-                if (lane % (kB / 8) == 0) reinterpret_cast<uint8_t*>(codes[pass + rr])[cc / kB] = (uint8_t)code;
+                    *reinterpret_cast<uint32_t*>(a.values_r + r * a.pitch_r + (col0 + cc) / 2) = scale.zero() ? 0u : pack_nibbles(y);
+                if (lane % (kB / 8) == 0) reinterpret_cast<uint8_t*>(codes[pass + rr])[cc / kB] = (uint8_t)scale.code;
             }
         }
         if (!COLS) continue;
         __syncthreads();
-        {
-            const int c = t % kQTile, r0 = (t / kQTile) * kHalf;
-            const long long out_row = col0 + c;
-            uint32_t word = 0;
-#pragma unroll
-            for (int b = 0; b < kHalf / kB; ++b) {
-                float y[kB];
-                uint32_t top = 0;
-#pragma unroll
-                for (int j = 0; j < kB; ++j) {
-                    y[j] = to_float(tile[COLS ? r0 + b * kB + j : 0][COLS ? c : 0]);
-                    top = max(top, __float_as_uint(y[j]) & 0x7fffffffu);
-                }
-                float by;
-                word |= scale_code<FMT>(top, tensor, &by) << (8 * b);
-                uint32_t n[kB / 8];
-#pragma unroll
-                for (int j = 0; j < kB; ++j) y[j] = scaled<FMT>(y[j], by);
-#pragma unroll
-                for (int j = 0; j < kB / 8; ++j) n[j] = by > 0.f ? pack_nibbles(y + 8 * j) : 0u;
-                const long long at = (row0 + pass + r0 + b * kB) / 2;
-                if (out_row < a.cols && at < a.pitch_c) {
-                    uint8_t* p = a.values_c + out_row * a.pitch_c + at;
-                    if (FMT == SBC_FP4_E8M0)
-                        *reinterpret_cast<uint4*>(p) = make_uint4(n[0], n[1], n[kB / 8 - 2], n[kB / 8 - 1]);
-                    else
-                        *reinterpret_cast<uint2*>(p) = make_uint2(n[0], n[1]);
-                }
-            }
-            const int first = (pass + r0) / kB;  // the thread's first block within the tile's rows
-            const long long k = (long long)row_tile * (kBlocks / 4) + first / 4;
-            if (k < a.ktiles_c) {
-                uint8_t* p = a.scales_c + ((long long)col_tile * a.ktiles_c + k) * 512 + (c % 32) * 16 + (c / 32) * 4 + first % 4;
-                if (kHalf / kB == 4)
-                    *reinterpret_cast<uint32_t*>(p) = word;
-                else if (kHalf / kB == 2)
-                    *reinterpret_cast<uint16_t*>(p) = (uint16_t)word;
-                else
-                    *p = (uint8_t)word;
-            }
-        }
+        quantise_columns<T, FMT>(a, &tile[0][0], kQTile + kPad, row_tile, col_tile, pass, tensor, inv_tensor);
         __syncthreads();
     }
     if (ROWS) {
@@ -238,12 +328,20 @@ struct DequantiseArgs {
     int align;
 };
 
-// The grid value of nibble i of `w`, exact.
-__device__ __forceinline__ float grid_value(uint32_t w, int i) {
-    const uint32_t n = w >> (4 * i), m = n & 7u;
-    // 0, 0.5: m / 2; above: exponent m >> 1, fraction m & 1
-    const float v = m < 2 ? 0.5f * (float)m : __uint_as_float(((m >> 1) + 126u) << 23 | (m & 1u) << 22);
-    return (n & 8u) ? -v : v;
+// The grid values of eight nibbles, exact.  A bfloat16 holds them, its two bytes come from tables that
+// a byte permutation looks up, four at a time.
+__device__ __forceinline__ void grid_values(float* x, uint32_t w) {
+    const uint32_t m = w & 0x77777777u;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t hi = __byte_perm(0x3f3f3f00u, 0x40404040u, m >> (16 * h)), lo = __byte_perm(0xc0800000u, 0xc0804000u, m >> (16 * h));
+        const uint32_t a = __byte_perm(lo, hi, 0x5140), b = __byte_perm(lo, hi, 0x7362);   // values 0, 1 and 2, 3
+        const uint32_t s = w >> (16 * h);
+        x[4 * h + 0] = __uint_as_float((a << 16) | (s << 28 & 0x80000000u));
+        x[4 * h + 1] = __uint_as_float((a & 0xffff0000u) | (s << 24 & 0x80000000u));
+        x[4 * h + 2] = __uint_as_float((b << 16) | (s << 20 & 0x80000000u));
+        x[4 * h + 3] = __uint_as_float((b & 0xffff0000u) | (s << 16 & 0x80000000u));
+    }
 }
 
 template <int FMT> __device__ __forceinline__ float scale_value(uint32_t code) {
@@ -252,22 +350,21 @@ template <int FMT> __device__ __forceinline__ float scale_value(uint32_t code) {
     return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3)));
 }
 
-// Eight elements a thread.
 template <typename T, int FMT> __global__ void __launch_bounds__(kQThreads) k_fp4_dequantise(DequantiseArgs a) {
     constexpr int kB = Fp4<FMT>::kBlock;
     T* out = static_cast<T*>(a.out);
-    const long long per_row = (a.cols + 7) / 8, all = per_row * a.rows;
     const float tensor = FMT == SBC_FP4_E4M3 ? *a.tensor : 1.f;
-    for (long long i = (long long)blockIdx.x * kQThreads + threadIdx.x; i < all; i += (long long)gridDim.x * kQThreads) {
-        const long long r = i / per_row, c = (i - r * per_row) * 8, b = c / kB;
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(a.values + r * a.pitch + c / 2);
+    warp_pieces(a.rows, a.cols, blockIdx.x * (kQThreads / 32) + threadIdx.x / 32, gridDim.x * (kQThreads / 32), [&](long long r, long long c) {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(a.values + r * a.pitch + c / 2), b = (uint32_t)(c / kB);
         const uint32_t code = a.scales[((r / 128) * a.ktiles + b / 4) * 512 + (r % 32) * 16 + (r % 128 / 32) * 4 + b % 4];
         const float s = scale_value<FMT>(code) * tensor;
+        float x[8];
+        grid_values(x, w);
         Pack8<T> v;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v.e[j] = from_float<T>(grid_value(w, j) * s);
+        for (int j = 0; j < 8; ++j) v.e[j] = from_float<T>(x[j] * s);
         store8(out + r * a.stride + c, v, (int)min(8LL, a.cols - c), a.align);
-    }
+    });
 }
 
 }  // namespace sbclm

@@ -154,7 +154,7 @@ def check_product(got, a, b):
 
 PRODUCTS = [(1, 650, 10000), (1, 64, 128), (16, 256, 128), (1, 1, 1), (3, 5, 7), (17, 65, 129), (2, 8192, 256), (35, 650, 1000),
             (128, 512, 128), (129, 513, 130), (255, 300, 257), (256, 256, 256), (257, 1000, 300), (700, 1300, 2600), (16, 4096, 4096),
-            (513, 96, 33), (64, 2048, 1000)]
+            (513, 96, 33), (64, 2048, 1000), (5000, 300, 1024), (4097, 128, 9000), (129, 70, 5)]
 
 
 @pytest.mark.parametrize("fmt", ["e8m0", "e4m3"])
@@ -185,14 +185,19 @@ def test_product_with_exact_small_integers(fmt):
 
 
 @pytest.mark.parametrize("fmt", ["e8m0", "e4m3"])
-def test_product_writes_only_its_output(fmt):
-    a = sbc.sbc_fp4_quantise(values(21, 200, torch.bfloat16, 3), fmt)
-    b = sbc.sbc_fp4_quantise(values(131, 200, torch.float32, 4), fmt)
-    room = torch.full((23, 140), 7.0, device=DEV, dtype=torch.float16)
-    sbc.sbc_fp4_product(a, b, out=room[1:22, 5:136])
-    check_product(room[1:22, 5:136], a, b)
+@pytest.mark.parametrize("tokens", [21, 201, 513])
+@pytest.mark.parametrize("outer,stride,at", [(131, 140, 5), (130, 140, 5), (130, 140, 4), (130, 141, 4), (131, 142, 2)])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+def test_product_writes_only_its_output(fmt, tokens, outer, stride, at, dtype):
+    """Odd and even row lengths, strides and offsets: where words of two results are stored, and where not."""
+    a = sbc.sbc_fp4_quantise(values(tokens, 200, torch.bfloat16, 3) / 16, fmt)
+    b = sbc.sbc_fp4_quantise(values(outer, 200, torch.float32, 4) / 16, fmt)
+    room = torch.full((tokens + 2, stride), 7.0, device=DEV, dtype=dtype)
+    out = room[1:tokens + 1, at:at + outer]
+    sbc.sbc_fp4_product(a, b, out=out)
+    check_product(out, a, b)
     inside = torch.zeros_like(room, dtype=torch.bool)
-    inside[1:22, 5:136] = True
+    inside[1:tokens + 1, at:at + outer] = True
     assert bool((room[~inside] == 7).all())
 
 
