@@ -120,20 +120,24 @@ struct QuantiseArgs {
 constexpr int kAmaxBlocks = 1024;
 constexpr long long kAmaxAlone = 32768;   // elements up to which every block finds the maximum itself, instead of a launch in front
 
-// A warp's share of a matrix: rows in pieces of 2048 elements, 256 at a time.  f(row, column) for eight
-// elements a lane.
+// A warp's share of a matrix: rows in pieces of 2048 elements, 256 at a time.  at(row, column) is told
+// where a lane's first eight elements of a piece are, f(k, have) is called for the `have` elements that
+// lie k further.
 constexpr int kPiece = 2048;
-template <typename F> __device__ __forceinline__ void warp_pieces(long long rows, long long cols, uint32_t warp, uint32_t warps, F f) {
+template <typename A, typename F> __device__ __forceinline__ void warp_pieces(long long rows, long long cols, uint32_t warp, uint32_t warps, A at, F f) {
     const uint32_t per_row = (uint32_t)((cols + kPiece - 1) / kPiece);
     const long long all = rows * per_row;
     for (long long i = warp; i < all; i += warps) {
         const long long r = all < (1ll << 32) ? (long long)((uint32_t)i / per_row) : i / per_row;
-        const long long c0 = (i - r * per_row) * kPiece + (threadIdx.x & 31) * 8;
-        if (c0 + kPiece - 256 + 8 <= cols) {
+        const long long p0 = (i - r * per_row) * kPiece, c0 = p0 + (threadIdx.x & 31) * 8;
+        at(r, c0);
+        if (p0 + kPiece <= cols) {
 #pragma unroll
-            for (int k = 0; k < kPiece; k += 256) f(r, c0 + k);
+            for (int k = 0; k < kPiece; k += 256) f(k, 8);
         } else {
-            for (int k = 0; k < kPiece && c0 + k < cols; k += 256) f(r, c0 + k);
+            const int left = (int)(cols - c0);
+#pragma unroll 4
+            for (int k = 0; k < left; k += 256) f(k, min(8, left - k));
         }
     }
 }
@@ -146,9 +150,10 @@ template <typename T> __device__ __forceinline__ uint32_t amax_over(const Quanti
     const bool flat = a.stride == a.cols;
     const long long rows = flat ? 1 : a.rows, cols = flat ? a.rows * a.cols : a.cols;
     uint32_t top = 0;
-    warp_pieces(rows, cols, warp, warps, [&](long long r, long long c) {
+    const T* p = nullptr;
+    warp_pieces(rows, cols, warp, warps, [&](long long r, long long c) { p = x + r * a.stride + c; }, [&](int k, int have) {
         Pack8<T> v;
-        load8(v, x + r * a.stride + c, (int)min(8LL, cols - c), a.align);
+        load8(v, p + k, have, a.align);
         float y[8];
         const uint32_t m = unpack_max(y, v);
         if (m < 0x7f800000u) {
@@ -280,27 +285,36 @@ template <typename T, int FMT, bool ROWS, bool COLS> __global__ void __launch_bo
     // sixteen threads to a row, eight elements each, sixteen rows at a time
     const int cc = (t & 15) * 8;
     const int have = (int)max(0LL, min(8LL, a.cols - (col0 + cc)));
+    constexpr int kStep = kQThreads / 16, kBatch = 16 / (int)sizeof(T);   // rows a step, steps whose loads are under way together (32 registers)
     for (int pass = 0; pass < kQTile; pass += kPass) {
-#pragma unroll 2
-        for (int rr = t >> 4; rr < kPass; rr += kQThreads / 16) {
-            const long long r = row0 + pass + rr;
-            Pack8<T> v;
-            load8(v, x + r * a.stride + col0 + cc, r < a.rows ? have : 0, a.align);
-            if (COLS) {
+#pragma unroll 1
+        for (int r1 = 0; r1 < kPass; r1 += kStep * kBatch) {
+            Pack8<T> v[kBatch];
 #pragma unroll
-                for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(&tile[rr][cc])[i] = v.q[i];
+            for (int i = 0; i < kBatch; ++i) {
+                const long long r = row0 + pass + r1 + i * kStep + (t >> 4);
+                load8(v[i], x + r * a.stride + col0 + cc, r < a.rows ? have : 0, a.align);
             }
-            if (ROWS) {
-                float y[8];
-                uint32_t top = unpack_max(y, v);
 #pragma unroll
-                for (int d = 1; d < kB / 8; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
-                const BlockScale<FMT> scale(top, tensor, inv_tensor);
+            for (int i = 0; i < kBatch; ++i) {
+                const int rr = r1 + i * kStep + (t >> 4);
+                const long long r = row0 + pass + rr;
+                if (COLS) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] = scale.over(FMT == SBC_FP4_E4M3 ? y[j] * inv_tensor : y[j]);
-                if (r < a.rows && (col0 + cc) / 2 < a.pitch_r)
-                    *reinterpret_cast<uint32_t*>(a.values_r + r * a.pitch_r + (col0 + cc) / 2) = scale.zero() ? 0u : pack_nibbles(y);
-                if (lane % (kB / 8) == 0) reinterpret_cast<uint8_t*>(codes[pass + rr])[cc / kB] = (uint8_t)scale.code;
+                    for (int q = 0; q < (int)sizeof(T) / 2; ++q) reinterpret_cast<uint4*>(&tile[COLS ? rr : 0][COLS ? cc : 0])[q] = v[i].q[q];
+                }
+                if (ROWS) {
+                    float y[8];
+                    uint32_t top = unpack_max(y, v[i]);
+#pragma unroll
+                    for (int d = 1; d < kB / 8; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+                    const BlockScale<FMT> scale(top, tensor, inv_tensor);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) y[j] = scale.over(FMT == SBC_FP4_E4M3 ? y[j] * inv_tensor : y[j]);
+                    if (r < a.rows && (col0 + cc) / 2 < a.pitch_r)
+                        *reinterpret_cast<uint32_t*>(a.values_r + r * a.pitch_r + (col0 + cc) / 2) = scale.zero() ? 0u : pack_nibbles(y);
+                    if (lane % (kB / 8) == 0) reinterpret_cast<uint8_t*>(codes[pass + rr])[cc / kB] = (uint8_t)scale.code;
+                }
             }
         }
         if (!COLS) continue;
@@ -354,16 +368,24 @@ template <typename T, int FMT> __global__ void __launch_bounds__(kQThreads) k_fp
     constexpr int kB = Fp4<FMT>::kBlock;
     T* out = static_cast<T*>(a.out);
     const float tensor = FMT == SBC_FP4_E4M3 ? *a.tensor : 1.f;
-    warp_pieces(a.rows, a.cols, blockIdx.x * (kQThreads / 32) + threadIdx.x / 32, gridDim.x * (kQThreads / 32), [&](long long r, long long c) {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(a.values + r * a.pitch + c / 2), b = (uint32_t)(c / kB);
-        const uint32_t code = a.scales[((r / 128) * a.ktiles + b / 4) * 512 + (r % 32) * 16 + (r % 128 / 32) * 4 + b % 4];
-        const float s = scale_value<FMT>(code) * tensor;
+    // a step of 256 elements is 128 bytes of nibbles and whole scale tiles
+    constexpr int kTileStep = 256 / kB / 4 * 512;
+    const uint8_t *values = nullptr, *scales = nullptr;
+    T* to = nullptr;
+    const auto at = [&](long long r, long long c) {
+        values = a.values + r * a.pitch + c / 2;
+        scales = a.scales + (r / 128 * a.ktiles + c / (4 * kB)) * 512 + (r % 32) * 16 + (r % 128 / 32) * 4 + c / kB % 4;
+        to = out + r * a.stride + c;
+    };
+    warp_pieces(a.rows, a.cols, blockIdx.x * (kQThreads / 32) + threadIdx.x / 32, gridDim.x * (kQThreads / 32), at, [&](int k, int have) {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(values + k / 2);
+        const float s = scale_value<FMT>(scales[k / 256 * kTileStep]) * tensor;
         float x[8];
         grid_values(x, w);
         Pack8<T> v;
 #pragma unroll
         for (int j = 0; j < 8; ++j) v.e[j] = from_float<T>(x[j] * s);
-        store8(out + r * a.stride + c, v, (int)min(8LL, a.cols - c), a.align);
+        store8(to + k, v, have, a.align);
     });
 }
 
