@@ -6,9 +6,10 @@
 // that decides like the exact one: a grid midpoint m has at most 3 significant bits, m * s is a
 // float, so an x that is not m * s differs from it by at least one unit in the last place, and the
 // rounded quotient then is not m either.  The same holds for the block scale, amax / (6 * 2^g).
-// The quotient comes from the block's rounded reciprocal r: q = x r, and one correction by the residual
-// x - q s, which a fused operation gives exactly (Markstein 1990); the power of two is taken off first,
-// so s is in [2^-9, 448] and nothing over- or underflows that could matter.
+// The quotient comes from an approximate reciprocal r: q = x r, then one correction by the residual
+// x - q s, which a fused operation gives exactly (Markstein 1990).  What that can be off by is far below
+// the 7 % of half a unit by which x / s stays clear of rounding to a midpoint it is not.  The power of
+// two is taken off first, so s is in [2^-9, 448] and nothing over- or underflows that could matter.
 #pragma once
 
 #include "lm_common.cuh"
@@ -32,31 +33,47 @@ __device__ __forceinline__ float tensor_scale_of(uint32_t amax_bits) {
     return pow2(max(e - 127 - 10, -126));
 }
 
+// x / d, corrected (see above), for r near 1 / d.
+__device__ __forceinline__ float quotient(float x, float d, float r) {
+    const float q = __fmul_rn(x, r);
+    return fmaf(fmaf(-q, d, x), r, q);
+}
+
 // A block's scale, ready for its elements.
 template <int FMT> struct BlockScale {
     uint32_t code;
-    float by, inv;   // E8M0: by = 1 / scale.  E4M3: by = the code's value, inv its rounded reciprocal.  0: the block is zeros
-    __device__ __forceinline__ BlockScale(uint32_t amax_bits, float tensor, float inv_tensor) : inv(0.f) {
+    float by, inv;   // E8M0: by = 1 / scale.  E4M3: by = the code's value, inv near its reciprocal.  0: the block is zeros
+    __device__ __forceinline__ BlockScale(uint32_t amax_bits, float inv_tensor) : inv(0.f) {
         if (FMT == SBC_FP4_E8M0) {
             code = (uint32_t)max((int)(amax_bits >> 23) - 2, 0);
             by = __uint_as_float((254u - code) << 23);
         } else {
-            const float want = __uint_as_float(amax_bits) / (6.f * tensor);
+            const float want = quotient(__uint_as_float(amax_bits) * inv_tensor, 6.f, 1.f / 6.f);
             code = __nv_cvt_float_to_fp8(want, __NV_SATFINITE, __NV_E4M3);
             by = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3)));
-            inv = by > 0.f ? 1.f / by : 0.f;
+            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(by));
         }
         if (amax_bits >= 0x7f800000u) {
             code = Fp4<FMT>::kNanScale;
-            by = inv = 0.f;
+            by = 0.f;
         }
     }
     __device__ __forceinline__ bool zero() const { return by == 0.f; }
-    // quotient of x (E4M3: of x already divided by the tensor's scale)
-    __device__ __forceinline__ float over(float x) const {
-        if (FMT == SBC_FP4_E8M0) return x * by;
-        const float q = __fmul_rn(x, inv);
-        return fmaf(fmaf(-q, by, x), inv, q);
+    // N quotients, in place (E4M3: of values divided by the tensor's scale on the way)
+    template <int N> __device__ __forceinline__ void over(float* y, float inv_tensor) const {
+        const unsigned long long b = pair(by, by), minus = pair(-by, -by), r = pair(inv, inv), t = pair(inv_tensor, inv_tensor);
+#pragma unroll
+        for (int j = 0; j < N; j += 2) {
+            unsigned long long x = pair(y[j], y[j + 1]);
+            if (FMT == SBC_FP4_E8M0) {
+                x = mul2(x, b);
+            } else {
+                x = mul2(x, t);
+                const unsigned long long q = mul2(x, r);
+                x = fma2(fma2(q, minus, x), r, q);
+            }
+            unpair(y[j], y[j + 1], x);
+        }
     }
 };
 
@@ -122,9 +139,10 @@ constexpr long long kAmaxAlone = 32768;   // elements up to which every block fi
 
 // A warp's share of a matrix: rows in pieces of 2048 elements, 256 at a time.  at(row, column) is told
 // where a lane's first eight elements of a piece are, f(k, have) is called for the `have` elements that
-// lie k further.
+// lie k further, or whole() for a piece that is all there.
 constexpr int kPiece = 2048;
-template <typename A, typename F> __device__ __forceinline__ void warp_pieces(long long rows, long long cols, uint32_t warp, uint32_t warps, A at, F f) {
+template <typename A, typename F, typename W>
+__device__ __forceinline__ void warp_pieces(long long rows, long long cols, uint32_t warp, uint32_t warps, A at, F f, W whole) {
     const uint32_t per_row = (uint32_t)((cols + kPiece - 1) / kPiece);
     const long long all = rows * per_row;
     for (long long i = warp; i < all; i += warps) {
@@ -132,8 +150,7 @@ template <typename A, typename F> __device__ __forceinline__ void warp_pieces(lo
         const long long p0 = (i - r * per_row) * kPiece, c0 = p0 + (threadIdx.x & 31) * 8;
         at(r, c0);
         if (p0 + kPiece <= cols) {
-#pragma unroll
-            for (int k = 0; k < kPiece; k += 256) f(k, 8);
+            whole();
         } else {
             const int left = (int)(cols - c0);
 #pragma unroll 4
@@ -151,9 +168,7 @@ template <typename T> __device__ __forceinline__ uint32_t amax_over(const Quanti
     const long long rows = flat ? 1 : a.rows, cols = flat ? a.rows * a.cols : a.cols;
     uint32_t top = 0;
     const T* p = nullptr;
-    warp_pieces(rows, cols, warp, warps, [&](long long r, long long c) { p = x + r * a.stride + c; }, [&](int k, int have) {
-        Pack8<T> v;
-        load8(v, p + k, have, a.align);
+    const auto look = [&](const Pack8<T>& v) {
         float y[8];
         const uint32_t m = unpack_max(y, v);
         if (m < 0x7f800000u) {
@@ -165,7 +180,25 @@ template <typename T> __device__ __forceinline__ uint32_t amax_over(const Quanti
                 top = max(top, b < 0x7f800000u ? b : 0u);
             }
         }
-    });
+    };
+    warp_pieces(
+        rows, cols, warp, warps, [&](long long r, long long c) { p = x + r * a.stride + c; },
+        [&](int k, int have) {
+            Pack8<T> v;
+            load8(v, p + k, have, a.align);
+            look(v);
+        },
+        [&] {
+            constexpr int kAhead = 16 / (int)sizeof(T);   // 32 registers of loads under way
+#pragma unroll
+            for (int k = 0; k < kPiece; k += 256 * kAhead) {
+                Pack8<T> v[kAhead];
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) load8(v[i], p + k + 256 * i, 8, a.align);
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) look(v[i]);
+            }
+        });
     top = __reduce_max_sync(0xffffffffu, top);
     if ((threadIdx.x & 31) == 0) room[threadIdx.x >> 5] = top;
     __syncthreads();
@@ -191,10 +224,9 @@ template <typename T> __device__ __forceinline__ uint32_t tensor_amax(const Quan
 }
 
 // N (16 or 32, a block's elements) values down a column to nibbles and the block's scale code.
-template <int FMT, int N> __device__ __forceinline__ uint32_t quantise_run(uint32_t* nibbles, float* y, uint32_t top, float tensor, float inv_tensor) {
-    const BlockScale<FMT> scale(top, tensor, inv_tensor);
-#pragma unroll
-    for (int j = 0; j < N; ++j) y[j] = scale.over(FMT == SBC_FP4_E4M3 ? y[j] * inv_tensor : y[j]);
+template <int FMT, int N> __device__ __forceinline__ uint32_t quantise_run(uint32_t* nibbles, float* y, uint32_t top, float inv_tensor) {
+    const BlockScale<FMT> scale(top, inv_tensor);
+    scale.template over<N>(y, inv_tensor);
 #pragma unroll
     for (int j = 0; j < N / 8; ++j) nibbles[j] = scale.zero() ? 0u : pack_nibbles(y + 8 * j);
     return scale.code;
@@ -218,7 +250,7 @@ __device__ __forceinline__ void store_column(const QuantiseArgs& a, long long ou
 // one column and 32 rows a thread) to the transpose.
 template <typename T, int FMT>
 __device__ __forceinline__ void quantise_columns(const QuantiseArgs& a, const T* tile, int stride, uint32_t row_tile, uint32_t col_tile, int pass,
-                                                 float tensor, float inv_tensor) {
+                                                 float inv_tensor) {
     constexpr int kB = Fp4<FMT>::kBlock;
     const int t = threadIdx.x;
     if constexpr (sizeof(T) == 2) {
@@ -238,7 +270,7 @@ __device__ __forceinline__ void quantise_columns(const QuantiseArgs& a, const T*
                 float y[kB];
 #pragma unroll
                 for (int j = 0; j < kB; ++j) y[j] = to_float(reinterpret_cast<const T*>(&w[b * kB + j])[side]);
-                codes |= quantise_run<FMT, kB>(n + b * (kB / 8), y, float_bits_of(side ? top[b] >> 16 : top[b] & 0xffffu, (const T*)nullptr), tensor, inv_tensor)
+                codes |= quantise_run<FMT, kB>(n + b * (kB / 8), y, float_bits_of(side ? top[b] >> 16 : top[b] & 0xffffu, (const T*)nullptr), inv_tensor)
                          << (8 * b);
             }
             store_column<FMT>(a, out_row + side, row, n, codes);
@@ -256,7 +288,7 @@ __device__ __forceinline__ void quantise_columns(const QuantiseArgs& a, const T*
                 y[j] = tile[(r0 + b * kB + j) * stride + c];
                 top = max(top, __float_as_uint(y[j]) & 0x7fffffffu);
             }
-            codes |= quantise_run<FMT, kB>(n + b * (kB / 8), y, top, tensor, inv_tensor) << (8 * b);
+            codes |= quantise_run<FMT, kB>(n + b * (kB / 8), y, top, inv_tensor) << (8 * b);
         }
         store_column<FMT>(a, (long long)col_tile * kQTile + c, row, n, codes);
     }
@@ -308,9 +340,8 @@ template <typename T, int FMT, bool ROWS, bool COLS> __global__ void __launch_bo
                     uint32_t top = unpack_max(y, v[i]);
 #pragma unroll
                     for (int d = 1; d < kB / 8; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
-                    const BlockScale<FMT> scale(top, tensor, inv_tensor);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) y[j] = scale.over(FMT == SBC_FP4_E4M3 ? y[j] * inv_tensor : y[j]);
+                    const BlockScale<FMT> scale(top, inv_tensor);
+                    scale.template over<8>(y, inv_tensor);
                     if (r < a.rows && (col0 + cc) / 2 < a.pitch_r)
                         *reinterpret_cast<uint32_t*>(a.values_r + r * a.pitch_r + (col0 + cc) / 2) = scale.zero() ? 0u : pack_nibbles(y);
                     if (lane % (kB / 8) == 0) reinterpret_cast<uint8_t*>(codes[pass + rr])[cc / kB] = (uint8_t)scale.code;
@@ -319,7 +350,7 @@ template <typename T, int FMT, bool ROWS, bool COLS> __global__ void __launch_bo
         }
         if (!COLS) continue;
         __syncthreads();
-        quantise_columns<T, FMT>(a, &tile[0][0], kQTile + kPad, row_tile, col_tile, pass, tensor, inv_tensor);
+        quantise_columns<T, FMT>(a, &tile[0][0], kQTile + kPad, row_tile, col_tile, pass, inv_tensor);
         __syncthreads();
     }
     if (ROWS) {
@@ -377,16 +408,33 @@ template <typename T, int FMT> __global__ void __launch_bounds__(kQThreads) k_fp
         scales = a.scales + (r / 128 * a.ktiles + c / (4 * kB)) * 512 + (r % 32) * 16 + (r % 128 / 32) * 4 + c / kB % 4;
         to = out + r * a.stride + c;
     };
-    warp_pieces(a.rows, a.cols, blockIdx.x * (kQThreads / 32) + threadIdx.x / 32, gridDim.x * (kQThreads / 32), at, [&](int k, int have) {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(values + k / 2);
-        const float s = scale_value<FMT>(scales[k / 256 * kTileStep]) * tensor;
+    const auto expand = [&](int k, int have, uint32_t w, uint32_t code) {
+        const float s = scale_value<FMT>(code) * tensor;
         float x[8];
         grid_values(x, w);
         Pack8<T> v;
 #pragma unroll
         for (int j = 0; j < 8; ++j) v.e[j] = from_float<T>(x[j] * s);
         store8(to + k, v, have, a.align);
-    });
+    };
+    // a whole piece's loads go ahead of its stores
+    uint32_t w[kPiece / 256], code[kPiece / 256];
+    warp_pieces(
+        a.rows, a.cols, blockIdx.x * (kQThreads / 32) + threadIdx.x / 32, gridDim.x * (kQThreads / 32), at,
+        [&](int k, int have) {
+            w[0] = *reinterpret_cast<const uint32_t*>(values + k / 2);
+            code[0] = scales[k / 256 * kTileStep];
+            expand(k, have, w[0], code[0]);
+        },
+        [&] {
+#pragma unroll
+            for (int i = 0; i < kPiece / 256; ++i) {
+                w[i] = *reinterpret_cast<const uint32_t*>(values + i * 128);
+                code[i] = scales[i * kTileStep];
+            }
+#pragma unroll
+            for (int i = 0; i < kPiece / 256; ++i) expand(i * 256, 8, w[i], code[i]);
+        });
 }
 
 }  // namespace sbclm
