@@ -74,15 +74,30 @@ int64_t pieces(int64_t rows, int64_t cols, bool flat) {
     return ceil_div(n, kQThreads / 32);
 }
 
-int launched() { return cudaGetLastError() == cudaSuccess ? SBC_OK : SBC_ECUDA; }
+// One launch: `cluster` blocks along `axis` (0: x, 2: z) together, allowed to start while the kernel in
+// front ends (the kernels wait for it themselves).
+template <typename... P, typename... A>
+int launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, int cluster, int axis, const A&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = axis == 0 ? (unsigned)cluster : 1;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = axis == 2 ? (unsigned)cluster : 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 0 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, P(args)...) == cudaSuccess ? SBC_OK : SBC_ECUDA;
+}
 
-template <typename T, int FMT> void launch_quantise(const QuantiseArgs& a, bool rows, bool cols, unsigned grid, cudaStream_t st) {
-    if (rows && cols)
-        k_fp4_quantise<T, FMT, true, true><<<grid, kQThreads, 0, st>>>(a);
-    else if (rows)
-        k_fp4_quantise<T, FMT, true, false><<<grid, kQThreads, 0, st>>>(a);
-    else
-        k_fp4_quantise<T, FMT, false, true><<<grid, kQThreads, 0, st>>>(a);
+template <typename T, int FMT> int launch_quantise(const QuantiseArgs& a, bool rows, bool cols, unsigned grid, cudaStream_t st) {
+    const auto kernel = rows && cols ? k_fp4_quantise<T, FMT, true, true> : rows ? k_fp4_quantise<T, FMT, true, false> : k_fp4_quantise<T, FMT, false, true>;
+    return launch(kernel, grid, kQThreads, 0, st, 0, 0, a);
 }
 
 typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -117,38 +132,8 @@ constexpr int kSmemMost = 227 * 1024;
 template <typename T, int FMT>
 int launch_product(const CUtensorMap& mw, const CUtensorMap& mx, const ProductArgs& a, dim3 grid, int smem, cudaStream_t st) {
     if (!allow_smem<k_fp4_product<T, FMT>>(kSmemMost - 1024)) return SBC_ECUDA;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(kPThreads);
-    cfg.dynamicSmemBytes = (size_t)smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 1;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = grid.z;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, k_fp4_product<T, FMT>, mw, mx, a) == cudaSuccess ? SBC_OK : SBC_ECUDA;
+    return launch(k_fp4_product<T, FMT>, grid, kPThreads, (size_t)smem, st, (int)grid.z, 2, mw, mx, a);
 }
-
-// A launch of one cluster of `size` blocks per row.
-struct RowLaunch {
-    cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[1];
-    RowLaunch(int64_t rows, int size, int threads, size_t smem, cudaStream_t st) {
-        cfg.gridDim = dim3((unsigned)(rows * size));
-        cfg.blockDim = dim3((unsigned)threads);
-        cfg.dynamicSmemBytes = smem;
-        cfg.stream = st;
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = (unsigned)size;
-        attr[0].val.clusterDim.y = 1;
-        attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-    }
-};
 
 // How a row of logits is cut: blocks that share it, elements a block holds in shared memory at a
 // time, threads of a block.
@@ -203,8 +188,7 @@ template <typename T, bool CE2, bool GRAD> int launch_distill(DistillArgs a, cud
     a.shift = p.shift;
     const size_t smem = (size_t)p.room * sizeof(T) + 32 + (size_t)a.k * 12;
     if (!allow_smem<k_distill<T, CE2, GRAD>>(kRoomBytes + 32 + SBC_DISTILL_MOST * 12)) return SBC_ECUDA;
-    RowLaunch l(a.rows, p.size, p.threads, smem, st);
-    return cudaLaunchKernelEx(&l.cfg, k_distill<T, CE2, GRAD>, a) == cudaSuccess ? SBC_OK : SBC_ECUDA;
+    return launch(k_distill<T, CE2, GRAD>, dim3((unsigned)(a.rows * p.size)), p.threads, smem, st, p.size, 0, a);
 }
 
 template <bool GRAD> int distill_by_type(const DistillArgs& a, int dtype, cudaStream_t st) {
@@ -227,8 +211,7 @@ int launch_wide(const sbc_fp4* a, const sbc_fp4* b, WideArgs p, int64_t tiles, c
     if (!allow_smem<k_fp4_product_wide<T, FMT, NT>>(kSmemMost - 1024)) return SBC_ECUDA;
     const unsigned blocks = (unsigned)(2 * std::min<int64_t>(std::max(1, sm_count() / 2), tiles));
     // (always more than half of an SM's shared memory: a block takes all of its tensor memory)
-    k_fp4_product_wide<T, FMT, NT><<<blocks, kWThreads, (size_t)(p.stages * stage + scales + 1024), st>>>(mw, mx, p);
-    return launched();
+    return launch(k_fp4_product_wide<T, FMT, NT>, dim3(blocks), kWThreads, (size_t)(p.stages * stage + scales + 1024), st, 2, 0, mw, mx, p);
 }
 
 // More than 128 tokens: pairs of blocks that stay.  Tiles of 256 tokens where that makes two rounds of
@@ -296,6 +279,7 @@ int sbc_fp4_quantise(const void* x, int dtype, int64_t rows, int64_t cols, int64
     a.cols = cols;
     a.stride = row_stride;
     a.align = row_align(x, row_stride, width_of(dtype));
+    a.base_align = row_align(x, 0, 1);
     a.col_tiles = (uint32_t)col_tiles;
     a.amax = static_cast<const uint32_t*>(workspace);
     if (along_rows) {
@@ -318,13 +302,12 @@ int sbc_fp4_quantise(const void* x, int dtype, int64_t rows, int64_t cols, int64
         if (format == SBC_FP4_E4M3) {
             if (rows * cols > kAmaxAlone) {
                 a.amax_blocks = (int)std::min<int64_t>(pieces(rows, cols, row_stride == cols), kAmaxBlocks);
-                k_fp4_amax<T><<<(unsigned)a.amax_blocks, kQThreads, 0, st>>>(a, static_cast<uint32_t*>(workspace));
+                const int rc = launch(k_fp4_amax<T>, dim3((unsigned)a.amax_blocks), kQThreads, 0, st, 0, 0, a, static_cast<uint32_t*>(workspace));
+                if (rc != SBC_OK) return rc;
             }
-            launch_quantise<T, SBC_FP4_E4M3>(a, along_rows, along_cols, (unsigned)(row_tiles * col_tiles), st);
-        } else {
-            launch_quantise<T, SBC_FP4_E8M0>(a, along_rows, along_cols, (unsigned)(row_tiles * col_tiles), st);
+            return launch_quantise<T, SBC_FP4_E4M3>(a, along_rows, along_cols, (unsigned)(row_tiles * col_tiles), st);
         }
-        return launched();
+        return launch_quantise<T, SBC_FP4_E8M0>(a, along_rows, along_cols, (unsigned)(row_tiles * col_tiles), st);
     });
 }
 
@@ -344,11 +327,8 @@ int sbc_fp4_dequantise(const sbc_fp4* q, void* out, int dtype, int64_t row_strid
     const int64_t blocks = std::min<int64_t>(pieces(q->rows, q->cols, false), sm_count() * 8);
     return by_dtype(dtype, [&](auto* as) {
         using T = std::remove_pointer_t<decltype(as)>;
-        if (q->format == SBC_FP4_E4M3)
-            k_fp4_dequantise<T, SBC_FP4_E4M3><<<(unsigned)blocks, kQThreads, 0, stream>>>(a);
-        else
-            k_fp4_dequantise<T, SBC_FP4_E8M0><<<(unsigned)blocks, kQThreads, 0, stream>>>(a);
-        return launched();
+        const auto kernel = q->format == SBC_FP4_E4M3 ? k_fp4_dequantise<T, SBC_FP4_E4M3> : k_fp4_dequantise<T, SBC_FP4_E8M0>;
+        return launch(kernel, dim3((unsigned)blocks), kQThreads, 0, stream, 0, 0, a);
     });
 }
 
@@ -410,13 +390,12 @@ int sbc_top_logits(const void* logits, int dtype, int64_t rows, int64_t cols, in
         const int threads = std::max(p.threads, std::min(kTopThreads, (int)ceil_div(2 * k, 32 * p.size) * 32));
         a.room = std::max(std::max(512, 4 * k), k * p.size);
         const size_t lists = (size_t)a.room * 10;
+        const dim3 grid((unsigned)(rows * p.size));
         if (ceil_div(ceil_div(cols, 64), p.size) * 64 > p.room) {   // too long to be held
-            RowLaunch l(rows, p.size, kTopThreads, lists, stream);
-            return cudaLaunchKernelEx(&l.cfg, k_top_logits<T, false>, a) == cudaSuccess ? (int)SBC_OK : (int)SBC_ECUDA;
+            return launch(k_top_logits<T, false>, grid, kTopThreads, lists, stream, p.size, 0, a);
         }
         if (!allow_smem<k_top_logits<T, true>>(kRoomBytes + 32 + 2048 * 10)) return (int)SBC_ECUDA;
-        RowLaunch l(rows, p.size, threads, lists + (size_t)p.room * sizeof(T) + 32, stream);
-        return cudaLaunchKernelEx(&l.cfg, k_top_logits<T, true>, a) == cudaSuccess ? (int)SBC_OK : (int)SBC_ECUDA;
+        return launch(k_top_logits<T, true>, grid, threads, lists + (size_t)p.room * sizeof(T) + 32, stream, p.size, 0, a);
     });
 }
 
@@ -451,11 +430,8 @@ int sbc_distill_grad(const void* logits, int dtype, int64_t rows, int64_t cols, 
         const int size = p.size, threads = p.threads;
         const size_t smem = (size_t)a.k * 12;
         a.shift = p.shift;
-        if (second_exponential(a))
-            k_distill_grad<T, true><<<(unsigned)(rows * size), threads, smem, stream>>>(a);
-        else
-            k_distill_grad<T, false><<<(unsigned)(rows * size), threads, smem, stream>>>(a);
-        return launched();
+        const auto kernel = second_exponential(a) ? k_distill_grad<T, true> : k_distill_grad<T, false>;
+        return launch(kernel, dim3((unsigned)(rows * size)), threads, smem, stream, 0, 0, a);
     });
 }
 

@@ -87,6 +87,15 @@ template <typename T> __device__ __forceinline__ void store8(T* p, const Pack8<T
     }
 }
 
+// Every kernel here is launched so that its blocks may start while the kernel in front of it on the
+// stream ends (its own preparation, barriers and tensor memory, then costs nothing).  This waits until
+// everything in front is done and visible; nothing in global memory is touched before it.  The next
+// kernel may start from here on.
+__device__ __forceinline__ void after_earlier_kernels() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 // ---- shared-memory barriers and bulk copies ------------------------------------
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }

@@ -391,6 +391,7 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
         mbar_init(bar, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    after_earlier_kernels();
     Cut<T> cut(z + first, min(n, a.room));
     cut.stage(held, bar);
     uint32_t phase = 0;
@@ -603,6 +604,7 @@ template <typename T, bool CE2> __global__ void __launch_bounds__(kDistillThread
     float* sent_t = reinterpret_cast<float*>(words);
     float* sent_z = sent_t + a.k;
     int* sent_at = reinterpret_cast<int*>(sent_z + a.k);
+    after_earlier_kernels();
     const float4 lo = *reinterpret_cast<const float4*>(a.stats + row * SBC_DISTILL_STATS);
     const float4 hi = *reinterpret_cast<const float4*>(a.stats + row * SBC_DISTILL_STATS + 4);
     const RowStats r = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
@@ -947,12 +949,13 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(kTopThreads, 
 
     bool late = false;
     if (t == 0) sh.count = 0;
+    const uint32_t bar = smem_u32(&sh.bar);
+    if (HELD && t == 0) {
+        mbar_init(bar, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    after_earlier_kernels();
     if (HELD) {
-        const uint32_t bar = smem_u32(&sh.bar);
-        if (t == 0) {
-            mbar_init(bar, 1);
-            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        }
         cut.stage(src.held, bar);
         __syncthreads();
         late = !mbar_wait(bar, 0);

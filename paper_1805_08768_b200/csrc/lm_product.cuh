@@ -125,6 +125,7 @@ __global__ void __launch_bounds__(kPThreads) k_fp4_product(const __grid_constant
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_slot;
+    after_earlier_kernels();
     const uint32_t acc_cols = (uint32_t)(a.nt + 31) & ~31u;
     const uint32_t sc_cols = 4u * S::kTiles * (1 + row_tiles);     // scale columns per stage
 
@@ -382,7 +383,7 @@ __device__ __forceinline__ void store_tile(uint32_t acc, T* out, long long strid
 }
 
 template <typename T, int FMT, int NT>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWThreads, 1)
+__global__ void __launch_bounds__(kWThreads, 1)
     k_fp4_product_wide(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, WideArgs a) {
     using S = ProductShape<FMT>;
     extern __shared__ uint8_t raw[];
@@ -435,6 +436,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWThreads, 1)
     cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_slot;
+    after_earlier_kernels();
 
     if (warp == 8) {
         if (lane == 0) {

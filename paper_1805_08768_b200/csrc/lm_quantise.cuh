@@ -122,7 +122,7 @@ template <typename T> __device__ __forceinline__ uint32_t unpack_max(float* y, c
 struct QuantiseArgs {
     const void* x;
     long long rows, cols, stride;
-    int align;                    // every row starts at a multiple of this many bytes
+    int align, base_align;        // every row, and the first one, starts at a multiple of this many bytes
     uint32_t col_tiles;           // blocks are numbered row tile by row tile
     const uint32_t* amax;         // E4M3: bits of the largest finite magnitudes that the blocks of k_fp4_amax found
     int amax_blocks;              // ... how many; 0: the tensor is small, every block looks for itself
@@ -137,25 +137,16 @@ struct QuantiseArgs {
 constexpr int kAmaxBlocks = 1024;
 constexpr long long kAmaxAlone = 32768;   // elements up to which every block finds the maximum itself, instead of a launch in front
 
-// A warp's share of a matrix: rows in pieces of 2048 elements, 256 at a time.  at(row, column) is told
-// where a lane's first eight elements of a piece are, f(k, have) is called for the `have` elements that
-// lie k further, or whole() for a piece that is all there.
-constexpr int kPiece = 2048;
-template <typename A, typename F, typename W>
-__device__ __forceinline__ void warp_pieces(long long rows, long long cols, uint32_t warp, uint32_t warps, A at, F f, W whole) {
+// A warp's share of a matrix: rows in pieces of 2048 elements, eight steps of 256.  f(row, column, left):
+// where a lane's first eight elements of a piece are, and how many elements the row has from there on.
+constexpr int kPiece = 2048, kSteps = kPiece / 256;
+template <typename F> __device__ __forceinline__ void warp_pieces(long long rows, long long cols, uint32_t warp, uint32_t warps, F f) {
     const uint32_t per_row = (uint32_t)((cols + kPiece - 1) / kPiece);
     const long long all = rows * per_row;
     for (long long i = warp; i < all; i += warps) {
         const long long r = all < (1ll << 32) ? (long long)((uint32_t)i / per_row) : i / per_row;
-        const long long p0 = (i - r * per_row) * kPiece, c0 = p0 + (threadIdx.x & 31) * 8;
-        at(r, c0);
-        if (p0 + kPiece <= cols) {
-            whole();
-        } else {
-            const int left = (int)(cols - c0);
-#pragma unroll 4
-            for (int k = 0; k < left; k += 256) f(k, min(8, left - k));
-        }
+        const long long c = (i - r * per_row) * kPiece + (threadIdx.x & 31) * 8;
+        f(r, c, (int)min(cols - c, (long long)kPiece));
     }
 }
 
@@ -167,7 +158,6 @@ template <typename T> __device__ __forceinline__ uint32_t amax_over(const Quanti
     const bool flat = a.stride == a.cols;
     const long long rows = flat ? 1 : a.rows, cols = flat ? a.rows * a.cols : a.cols;
     uint32_t top = 0;
-    const T* p = nullptr;
     const auto look = [&](const Pack8<T>& v) {
         float y[8];
         const uint32_t m = unpack_max(y, v);
@@ -181,24 +171,19 @@ template <typename T> __device__ __forceinline__ uint32_t amax_over(const Quanti
             }
         }
     };
-    warp_pieces(
-        rows, cols, warp, warps, [&](long long r, long long c) { p = x + r * a.stride + c; },
-        [&](int k, int have) {
-            Pack8<T> v;
-            load8(v, p + k, have, a.align);
-            look(v);
-        },
-        [&] {
-            constexpr int kAhead = 16 / (int)sizeof(T);   // 32 registers of loads under way
+    const int align = flat ? a.base_align : a.align;
+    warp_pieces(rows, cols, warp, warps, [&](long long r, long long c, int left) {
+        const T* p = x + r * a.stride + c;
+        constexpr int kAhead = 16 / (int)sizeof(T);   // 32 registers of loads under way
 #pragma unroll
-            for (int k = 0; k < kPiece; k += 256 * kAhead) {
-                Pack8<T> v[kAhead];
+        for (int k = 0; k < kSteps; k += kAhead) {
+            Pack8<T> v[kAhead];
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) load8(v[i], p + k + 256 * i, 8, a.align);
+            for (int i = 0; i < kAhead; ++i) load8(v[i], p + 256 * (k + i), min(8, left - 256 * (k + i)), align);
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) look(v[i]);
-            }
-        });
+            for (int i = 0; i < kAhead; ++i) look(v[i]);
+        }
+    });
     top = __reduce_max_sync(0xffffffffu, top);
     if ((threadIdx.x & 31) == 0) room[threadIdx.x >> 5] = top;
     __syncthreads();
@@ -207,6 +192,7 @@ template <typename T> __device__ __forceinline__ uint32_t amax_over(const Quanti
 
 template <typename T> __global__ void __launch_bounds__(kQThreads) k_fp4_amax(QuantiseArgs a, uint32_t* amax) {
     __shared__ uint32_t room[kQThreads / 32];
+    after_earlier_kernels();
     const uint32_t top = amax_over<T>(a, blockIdx.x * (kQThreads / 32) + threadIdx.x / 32, gridDim.x * (kQThreads / 32), room);
     if (threadIdx.x == 0) amax[blockIdx.x] = top;
 }
@@ -295,7 +281,7 @@ __device__ __forceinline__ void quantise_columns(const QuantiseArgs& a, const T*
 }
 
 // One block takes a 128 x 128 tile, which is whole scale tiles of either orientation.
-template <typename T, int FMT, bool ROWS, bool COLS> __global__ void __launch_bounds__(kQThreads) k_fp4_quantise(QuantiseArgs a) {
+template <typename T, int FMT, bool ROWS, bool COLS> __global__ void __launch_bounds__(kQThreads, 4) k_fp4_quantise(QuantiseArgs a) {
     constexpr int kB = Fp4<FMT>::kBlock, kBlocks = kQTile / kB;  // blocks along a tile's side
     constexpr int kPad = 16 / (int)sizeof(T);
     constexpr int kPass = COLS ? 256 / (int)sizeof(T) : kQTile;  // rows held in shared memory at a time (up to 34 KB)
@@ -303,6 +289,7 @@ template <typename T, int FMT, bool ROWS, bool COLS> __global__ void __launch_bo
     __shared__ alignas(16) T tile[COLS ? kPass : 1][COLS ? kQTile + kPad : 8];
     const T* x = static_cast<const T*>(a.x);
     const int t = threadIdx.x, lane = t & 31;
+    after_earlier_kernels();
     const uint32_t row_tile = blockIdx.x / a.col_tiles, col_tile = blockIdx.x % a.col_tiles;
     const long long row0 = (long long)row_tile * kQTile, col0 = (long long)col_tile * kQTile;
     float tensor = 1.f, inv_tensor = 1.f;
@@ -398,43 +385,34 @@ template <int FMT> __device__ __forceinline__ float scale_value(uint32_t code) {
 template <typename T, int FMT> __global__ void __launch_bounds__(kQThreads) k_fp4_dequantise(DequantiseArgs a) {
     constexpr int kB = Fp4<FMT>::kBlock;
     T* out = static_cast<T*>(a.out);
+    after_earlier_kernels();
     const float tensor = FMT == SBC_FP4_E4M3 ? *a.tensor : 1.f;
     // a step of 256 elements is 128 bytes of nibbles and whole scale tiles
     constexpr int kTileStep = 256 / kB / 4 * 512;
-    const uint8_t *values = nullptr, *scales = nullptr;
-    T* to = nullptr;
-    const auto at = [&](long long r, long long c) {
-        values = a.values + r * a.pitch + c / 2;
-        scales = a.scales + (r / 128 * a.ktiles + c / (4 * kB)) * 512 + (r % 32) * 16 + (r % 128 / 32) * 4 + c / kB % 4;
-        to = out + r * a.stride + c;
-    };
-    const auto expand = [&](int k, int have, uint32_t w, uint32_t code) {
-        const float s = scale_value<FMT>(code) * tensor;
-        float x[8];
-        grid_values(x, w);
-        Pack8<T> v;
+    warp_pieces(a.rows, a.cols, blockIdx.x * (kQThreads / 32) + threadIdx.x / 32, gridDim.x * (kQThreads / 32), [&](long long r, long long c, int left) {
+        const uint8_t* values = a.values + r * a.pitch + c / 2;
+        const uint8_t* scales = a.scales + (r / 128 * a.ktiles + c / (4 * kB)) * 512 + (r % 32) * 16 + (r % 128 / 32) * 4 + c / kB % 4;
+        T* to = out + r * a.stride + c;
+        // a piece's loads go ahead of its stores
+        uint32_t w[kSteps], code[kSteps];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v.e[j] = from_float<T>(x[j] * s);
-        store8(to + k, v, have, a.align);
-    };
-    // a whole piece's loads go ahead of its stores
-    uint32_t w[kPiece / 256], code[kPiece / 256];
-    warp_pieces(
-        a.rows, a.cols, blockIdx.x * (kQThreads / 32) + threadIdx.x / 32, gridDim.x * (kQThreads / 32), at,
-        [&](int k, int have) {
-            w[0] = *reinterpret_cast<const uint32_t*>(values + k / 2);
-            code[0] = scales[k / 256 * kTileStep];
-            expand(k, have, w[0], code[0]);
-        },
-        [&] {
+        for (int i = 0; i < kSteps; ++i) {
+            if (left <= 256 * i) break;
+            w[i] = *reinterpret_cast<const uint32_t*>(values + i * 128);
+            code[i] = scales[i * kTileStep];
+        }
 #pragma unroll
-            for (int i = 0; i < kPiece / 256; ++i) {
-                w[i] = *reinterpret_cast<const uint32_t*>(values + i * 128);
-                code[i] = scales[i * kTileStep];
-            }
+        for (int i = 0; i < kSteps; ++i) {
+            if (left <= 256 * i) break;
+            const float s = scale_value<FMT>(code[i]) * tensor;
+            float x[8];
+            grid_values(x, w[i]);
+            Pack8<T> v;
 #pragma unroll
-            for (int i = 0; i < kPiece / 256; ++i) expand(i * 256, 8, w[i], code[i]);
-        });
+            for (int j = 0; j < 8; ++j) v.e[j] = from_float<T>(x[j] * s);
+            store8(to + 256 * i, v, min(8, left - 256 * i), a.align);
+        }
+    });
 }
 
 }  // namespace sbclm
