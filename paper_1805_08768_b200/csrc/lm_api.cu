@@ -386,6 +386,12 @@ int sbc_top_logits(const void* logits, int dtype, int64_t rows, int64_t cols, in
         using T = std::remove_pointer_t<decltype(as)>;
         const RowPlan p = plan_rows(rows, cols, (int)sizeof(T));
         a.shift = p.shift;
+        // many rows that would take four blocks each: 2048 x 131072 bfloat16 232 us streamed, 299 us in clusters
+        // (65536: 133 and 132, 32000: 84 and 59)
+        if (rows >= sm_count() && cols * (int64_t)sizeof(T) > 2 * kRoomBytes) {
+            a.room = kStreamRoom;
+            return launch(k_top_stream<T>, dim3((unsigned)rows), kStreamThreads, 2 * kStreamBytes + (size_t)a.room * 10, stream, 0, 0, a);
+        }
         // enough groups of elements that the k-th largest of their maxima bounds tightly: two a thread, four times k
         const int threads = std::max(p.threads, std::min(kTopThreads, (int)ceil_div(2 * k, 32 * p.size) * 32));
         a.room = std::max(std::max(512, 4 * k), k * p.size);

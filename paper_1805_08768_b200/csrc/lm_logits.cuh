@@ -320,21 +320,29 @@ template <typename T> __device__ __forceinline__ void store_granule(T* out, cons
     for (int j = 0; j < E; ++j)
         if (i0 + j >= 0 && i0 + j < cut.n) out[i0 + j] = e[j];
 }
-// f(granule index) -> 16 bytes, for every granule of a cut: whole ones side by side, then the edges.
-template <typename T, typename F> __device__ __forceinline__ void store_all(T* out, const Cut<T>& cut, F f) {
-    constexpr int E = Gran<T>::E;
+// make(load(i)) for every granule i of a cut: whole ones side by side, four loads ahead of their stores
+// (a gradient written in place only replaces what its own thread has read), then the edges.
+template <typename T, typename L, typename M> __device__ __forceinline__ void store_all(T* out, const Cut<T>& cut, L load, M make) {
+    constexpr int E = Gran<T>::E, kAhead = 4;
     const int t = threadIdx.x, threads = blockDim.x;
     if (((uint32_t)(uintptr_t)out & 15u) != (uint32_t)cut.phase * sizeof(T)) {
-        for (int i = t; i < cut.grans; i += threads) store_granule(out, cut, i, f(i), false);
+        for (int i = t; i < cut.grans; i += threads) store_granule(out, cut, i, make(load(i)), false);
         return;
     }
     const int g0 = cut.phase > 0 ? 1 : 0, g1 = (cut.phase + cut.n) / E;
     uint4* wide = reinterpret_cast<uint4*>(out - cut.phase);
-#pragma unroll 4
-    for (int i = g0 + t; i < g1; i += threads) wide[i] = f(i);
+    int i = g0 + t;
+    for (; i + (kAhead - 1) * threads < g1; i += kAhead * threads) {
+        uint4 q[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) q[j] = load(i + j * threads);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) wide[i + j * threads] = make(q[j]);
+    }
+    for (; i < g1; i += threads) wide[i] = make(load(i));
     if (t < 2) {
-        const int i = t == 0 ? 0 : cut.grans - 1;
-        if (cut.grans > 0 && !cut.whole(i) && (t == 0 || i > 0)) store_granule(out, cut, i, f(i), false);
+        const int e = t == 0 ? 0 : cut.grans - 1;
+        if (cut.grans > 0 && !cut.whole(e) && (t == 0 || e > 0)) store_granule(out, cut, e, make(load(e)), false);
     }
 }
 
@@ -431,6 +439,7 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
     for (int part = 0; part < parts; ++part) {
         const int lo = part * a.room;
         if (part > 0) {
+            before_copies();
             __syncthreads();
             cut = Cut<T>(z + first + lo, min(n - lo, a.room));
             cut.stage(held, bar);
@@ -551,13 +560,14 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
         for (int part = 0; part < parts; ++part) {
             const int lo = part * a.room;
             if (parts > 1) {
+                before_copies();
                 __syncthreads();
                 cut = Cut<T>(z + first + lo, min(n - lo, a.room));
                 cut.stage(held, bar);
                 landed();
             }
             slope.granules([&](const auto& gr) {
-                store_all(out + lo, cut, [&](int i) { return gr.granule(*reinterpret_cast<const uint4*>(held + i * E)); });
+                store_all(out + lo, cut, [&](int i) { return *reinterpret_cast<const uint4*>(held + i * E); }, [&](const uint4& q) { return gr.granule(q); });
             });
         }
     }
@@ -620,7 +630,12 @@ template <typename T, bool CE2> __global__ void __launch_bounds__(kDistillThread
     const Slope<T, CE2> slope(a, r, a.grad_loss ? a.grad_loss[row] : 1.f, label >= 0);
     __syncthreads();   // an in-place gradient comes after the words are read
     T* out = static_cast<T*>(a.grad) + row * a.grad_stride + first;
-    slope.granules([&](const auto& gr) { store_all(out, cut, [&](int i) { return gr.granule(cut.load(i)); }); });
+    slope.granules([&](const auto& gr) {
+        store_all(
+            out, cut,
+            [&](int i) { return cut.whole(i) ? *reinterpret_cast<const uint4*>(cut.p - cut.phase + (long long)i * Gran<T>::E) : cut.load(i); },
+            [&](const uint4& q) { return gr.granule(q); });
+    });
     __syncthreads();
     write_sent(out, slope, first, n, a.k, sent_at, sent_t, sent_z, label, label_z);
 }
@@ -679,9 +694,9 @@ struct Candidates {
 };
 
 // (the compiler would gather a warp's additions first, which costs more than these few)
-__device__ __forceinline__ uint32_t add_shared(void* p) {
+__device__ __forceinline__ uint32_t add_shared(void* p, uint32_t n = 1) {
     uint32_t r;
-    asm volatile("atom.shared.add.u32 %0, [%1], 1;" : "=r"(r) : "r"(smem_u32(p)) : "memory");
+    asm volatile("atom.shared.add.u32 %0, [%1], %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(n) : "memory");
     return r;
 }
 
@@ -710,6 +725,24 @@ __device__ __forceinline__ void block_mass(Mass<false>& a, TopShared& sh, int tu
         a.lanes(c);
     }
 }
+
+// Bins for keys between lo and hi, the largest in bin 0: equal parts of the values' range where that is
+// finite (logits crowd around zero only in their keys), else of the keys'.  A larger key is never in a
+// later bin.
+struct KeyBins {
+    uint32_t hi;
+    int shift;
+    float top, scale;
+    __device__ __forceinline__ KeyBins(uint32_t hi_key, uint32_t lo_key) : hi(hi_key), top(key_value(hi_key)) {
+        shift = max(0, 32 - __clz((int)(hi_key - lo_key)) - 8);   // 2^8 bins
+        const float range = top - key_value(lo_key);
+        scale = range > 1e-30f && range < 1e30f ? ((float)kTopBins - 0.5f) / range : 0.f;
+    }
+    __device__ __forceinline__ uint32_t of(uint32_t key) const {
+        if (scale > 0.f) return min((uint32_t)kTopBins - 1u, (uint32_t)((top - key_value(key)) * scale));
+        return (hi - key) >> shift;
+    }
+};
 
 // Ranks the candidates [0, n) (all different): the first min(k, n) in order to sh.best, the others join
 // the mass of what is not sent.  Few are compared with each other; otherwise the keys' range is cut into
@@ -746,8 +779,8 @@ __device__ __forceinline__ void rank_candidates(TopShared& sh, const Candidates&
     __syncthreads();
     hi = __reduce_max_sync(0xffffffffu, sh.warp_hi[min(lane, warps - 1)]);
     lo = __reduce_min_sync(0xffffffffu, sh.warp_lo[min(lane, warps - 1)]);
-    const int shift = max(0, 32 - __clz((int)(hi - lo)) - 8);   // 2^8 bins
-    const auto bin_of = [&](unsigned long long x) { return (hi - (uint32_t)(x >> 32)) >> shift; };
+    const KeyBins bins(hi, lo);
+    const auto bin_of = [&](unsigned long long x) { return bins.of((uint32_t)(x >> 32)); };
     for (int i = t; i < n; i += threads) add_shared(&sh.bins[bin_of(cand.at[i])]);
     __syncthreads();
     if (t < 32) {
@@ -864,33 +897,54 @@ __device__ __forceinline__ Mass<false> gather_top(const Source<T, HELD>& src, in
     const float low = !PLAIN && threshold == 0 ? -infinity() : key_value((uint32_t)(threshold >> 32));
     GranMax<T, true> top;
     float top_left = -infinity();   // of granules that hold a candidate: what is left
-    for (int g0 = threadIdx.x; g0 < cut.grans; g0 += 32 * blockDim.x) {
+    const int threads = blockDim.x;
+    // (all lanes of a warp go around together: apart, each would take its own turns)
+    for (int gw = threadIdx.x & ~31; gw < cut.grans; gw += 32 * threads) {
+        const int g0 = gw + (threadIdx.x & 31);
         // mark the granules first: a warp then goes through its fullest lane's, not through all that any lane has
-        uint32_t marked = 0, bit = 1;
+        uint32_t marked = 0;
 #pragma unroll 4
-        for (int g = g0; g < cut.grans && bit; g += blockDim.x, bit <<= 1) {
+        for (int j = 0; j < 32; ++j) {
+            const int g = g0 + j * threads;
+            if (gw + j * threads >= cut.grans) break;
+            if (g >= cut.grans) continue;
             GranMax<T, true> here;
             here.add(src.get(g));
             if (here.get() < low)
                 top.add(here);
             else
-                marked |= bit;
+                marked |= 1u << j;
         }
-        while (marked) {
-            const int g = g0 + (__ffs((int)marked) - 1) * (int)blockDim.x;
+        while (__any_sync(0xffffffffu, marked != 0)) {
+            const bool any = marked != 0;
+            const int g = any ? g0 + (__ffs((int)marked) - 1) * threads : 0;
             marked &= marked - 1;
             float x[E];
             unpack(x, src.get(g), (const T*)nullptr);
             const int i0 = g * E - cut.phase;
+            uint32_t hits = 0;
 #pragma unroll
             for (int j = 0; j < E; ++j) {
-                if (!(x[j] < low) && (PLAIN || (i0 + j >= 0 && i0 + j < cut.n && composite(x[j], first + i0 + j) >= threshold))) {
-                    const uint32_t at = add_shared(&sh.count);
-                    if (at < (uint32_t)cand.room) cand.at[at] = (unsigned long long)__float_as_uint(x[j]) << 32 | (uint32_t)(first + i0 + j);
+                bool hit = !(x[j] < low);
+                if (!PLAIN) hit = hit && i0 + j >= 0 && i0 + j < cut.n && composite(x[j], first + i0 + j) >= threshold;
+                hits |= hit ? 1u << j : 0u;
+            }
+            if (!any) hits = 0;
+#pragma unroll
+            for (int j = 0; j < E; ++j) top_left = any && !(hits >> j & 1) ? fmaxf(top_left, x[j]) : top_left;
+            uint32_t at = 0;
+            if (hits) at = add_shared(&sh.count, (uint32_t)__popc(hits));
+            __syncwarp();
+            while (__any_sync(0xffffffffu, hits != 0)) {
+                const int j = __ffs((int)hits) - 1;
+                if (hits) {
+                    const float v = to_float(HELD ? src.held[g * E + j] : cut.p[i0 + j]);
+                    if (at < (uint32_t)cand.room) cand.at[at] = (unsigned long long)__float_as_uint(v) << 32 | (uint32_t)(first + i0 + j);
                     if (HELD) src.held[g * E + j] = from_float<T>(-infinity());
-                    x[j] = -infinity();
                 }
-                top_left = fmaxf(top_left, x[j]);
+                ++at;
+                hits &= hits - 1;
+                __syncwarp();
             }
         }
     }
@@ -1047,6 +1101,204 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(kTopThreads, 
         cluster_sync();   // nobody reads another block's candidates any more
         if (rank != 0) return;
     }
+    if (n < k) {
+        // fewer than k are above -inf, so enough of the first k elements are -inf
+        if (t == 0) sh.count = n;
+        __syncthreads();
+        for (int i = t; i < k; i += threads)
+            if (to_float(z[i]) == -infinity()) cand.at[add_shared(&sh.count)] = composite(-infinity(), i);
+        __syncthreads();
+        n = sh.count;
+        __syncthreads();
+    }
+    rank_candidates(sh, cand, n, k, mass, c);
+    block_mass(mass, sh, 1, c);
+    for (int i = t; i < k; i += threads) {
+        const unsigned long long mine = sh.best[i];
+        a.values[row * k + i] = key_value((uint32_t)(mine >> 32));
+        a.indices[row * k + i] = (int32_t)~(uint32_t)mine;
+    }
+    if (t == 0) a.rest[row] = mass.s == 0.f ? -infinity() : mass.m / a.temperature + logf(mass.s);
+}
+
+// ---- long rows, one block each --------------------------------------------------------
+//
+// A block streams its row through two buffers in shared memory and reads it once.  The first part's
+// group maxima bound the k-th largest from below; whenever many candidates have come together the bound
+// is raised to (about) their own k-th largest, so a part of a long row adds few.
+
+constexpr int kStreamBytes = 16384;
+constexpr int kStreamThreads = 256, kStreamRoom = 1024;   // threads of a block, candidates it can hold
+
+template <typename T> struct StreamShared {
+    uint64_t bar[2];
+    TopShared top;
+};
+
+// Keeps about the k largest of the candidates: those in the bins (of equal parts of the keys' range) down
+// to the k-th largest's.  Returns the smallest key kept; the others join the mass.
+__device__ __forceinline__ uint32_t keep_largest(TopShared& sh, const Candidates& cand, int n, int k, Mass<false>& mass, float c) {
+    const int t = threadIdx.x, threads = blockDim.x, lane = t & 31, warps = threads >> 5;
+    constexpr int kMost = kStreamRoom / kStreamThreads;   // candidates a thread holds
+    unsigned long long mine[kMost];
+    uint32_t hi = 0, lo = 0xffffffffu;
+#pragma unroll
+    for (int j = 0; j < kMost; ++j) {
+        const int i = t + j * threads;
+        mine[j] = i < n ? cand.at[i] : 0;
+        if (i < n) {
+            const uint32_t key = order_key(__uint_as_float((uint32_t)(mine[j] >> 32)));
+            hi = max(hi, key), lo = min(lo, key);
+        }
+    }
+    hi = __reduce_max_sync(0xffffffffu, hi), lo = __reduce_min_sync(0xffffffffu, lo);
+    if (lane == 0) sh.warp_hi[t >> 5] = hi, sh.warp_lo[t >> 5] = lo;
+    for (int i = t; i < kTopBins; i += threads) sh.bins[i] = 0;
+    __syncthreads();
+    hi = __reduce_max_sync(0xffffffffu, sh.warp_hi[min(lane, warps - 1)]);
+    lo = __reduce_min_sync(0xffffffffu, sh.warp_lo[min(lane, warps - 1)]);
+    const KeyBins bins(hi, lo);
+#pragma unroll
+    for (int j = 0; j < kMost; ++j)
+        if (t + j * threads < n) add_shared(&sh.bins[bins.of(order_key(__uint_as_float((uint32_t)(mine[j] >> 32))))]);
+    if (t == 0) sh.count = 0;
+    __syncthreads();
+    if (t < 32) {
+        uint32_t sum = 0;
+#pragma unroll
+        for (int b = 0; b < kTopBins / 32; ++b) sum += sh.bins[lane * (kTopBins / 32) + b];
+        uint32_t upto = sum;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const uint32_t o = __shfl_up_sync(0xffffffffu, upto, d);
+            if (lane >= d) upto += o;
+        }
+        uint32_t before = upto - sum;
+        if (before < (uint32_t)k && upto >= (uint32_t)k) {
+            int b = 0;
+            for (; before + sh.bins[lane * (kTopBins / 32) + b] < (uint32_t)k; ++b) before += sh.bins[lane * (kTopBins / 32) + b];
+            sh.have = lane * (kTopBins / 32) + b;
+        }
+    }
+    __syncthreads();
+    const uint32_t bin = (uint32_t)sh.have;
+    uint32_t least = 0xffffffffu;
+#pragma unroll
+    for (int j = 0; j < kMost; ++j) {
+        if (t + j * threads >= n) continue;
+        const float x = __uint_as_float((uint32_t)(mine[j] >> 32));
+        const uint32_t key = order_key(x);
+        if (bins.of(key) <= bin) {
+            cand.at[add_shared(&sh.count)] = mine[j];
+            least = min(least, key);
+        } else {
+            mass.join(x, 1.f, 0.f, c);
+        }
+    }
+    least = __reduce_min_sync(0xffffffffu, least);
+    __syncthreads();
+    if (lane == 0) sh.warp_lo[t >> 5] = least;
+    __syncthreads();
+    return __reduce_min_sync(0xffffffffu, sh.warp_lo[min(lane, warps - 1)]);
+}
+
+template <typename T> __global__ void __launch_bounds__(kStreamThreads, 4) k_top_stream(TopArgs a) {
+    extern __shared__ __align__(16) uint8_t dyn[];
+    __shared__ StreamShared<T> shared;
+    TopShared& sh = shared.top;
+    constexpr int E = Gran<T>::E, kGrans = kStreamBytes / 16;
+    const int t = threadIdx.x, threads = blockDim.x, lane = t & 31, warp = t >> 5, warps = threads >> 5;
+    const long long row = blockIdx.x;
+    const T* z = static_cast<const T*>(a.logits) + row * a.stride;
+    const Cut<T> cut(z, a.cols);
+    T* const buffer = reinterpret_cast<T*>(dyn);
+    Candidates cand;
+    cand.at = reinterpret_cast<unsigned long long*>(dyn + 2 * kStreamBytes);
+    cand.order = reinterpret_cast<uint16_t*>(cand.at + a.room);
+    cand.room = a.room;
+    const float c = kLog2e / a.temperature;
+    const int k = a.k, parts = (cut.grans + kGrans - 1) / kGrans;
+
+    if (t == 0) {
+        sh.count = 0;
+        mbar_init(smem_u32(&shared.bar[0]), 1);
+        mbar_init(smem_u32(&shared.bar[1]), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    after_earlier_kernels();
+    // part p of the row into its buffer: whole granules by a bulk copy, the row's edges by hand
+    const auto part_of = [&](int p) {
+        const int g0 = p * kGrans;
+        const int from = max(0, g0 * E - cut.phase), to = min(cut.n, g0 * E + kGrans * E - cut.phase);
+        return Cut<T>(z + from, to - from);
+    };
+    const auto fetch = [&](int p) { part_of(p).stage(buffer + (p & 1) * (kGrans * E), smem_u32(&shared.bar[p & 1])); };
+    fetch(0);
+    if (parts > 1) fetch(1);
+
+    Mass<false> mass;
+    uint32_t least = 0;   // key of the bound
+    bool late = false, crowded = false;
+    int p = 0;
+    for (; p < parts; ++p) {
+        __syncthreads();
+        late |= !mbar_wait(smem_u32(&shared.bar[p & 1]), (uint32_t)(p >> 1) & 1);
+        const Cut<T> part = part_of(p);
+        const Source<T, true> src = {part, buffer + (p & 1) * (kGrans * E)};
+        if (p == 0) {
+            GranMax<T, true> top;
+#pragma unroll 4
+            for (int g = t; g < part.grans; g += threads) top.add(src.get(g));
+            const uint32_t k0 = order_key(top.first()) >> 16, k1 = order_key(top.second()) >> 16;
+            const int share = (k + warps - 1) / warps;
+            const uint32_t all = __reduce_and_sync(0xffffffffu, k0 & k1), any = __reduce_or_sync(0xffffffffu, k0 | k1);
+            const int bits = 32 - __clz((int)(all ^ any));
+            uint32_t bound = all >> bits << bits;
+            for (int b = bits - 1; b >= 0; --b) {
+                const uint32_t next = bound | 1u << b;
+                if (__popc(__ballot_sync(0xffffffffu, k0 >= next)) + __popc(__ballot_sync(0xffffffffu, k1 >= next)) >= share) bound = next;
+            }
+            if (lane == 0) sh.warp_bound[warp] = bound;
+            __syncthreads();
+            least = max(__reduce_min_sync(0xffffffffu, sh.warp_bound[min(lane, warps - 1)]) << 16, kLowestKey);
+        }
+        const Mass<false> more = gather_top<T, true, true>(src, part.p - z, sh, cand, (unsigned long long)least << 32, c);
+        mass.join(more.m, more.s, 0.f, c);
+        before_copies();
+        __syncthreads();
+        if (p + 2 < parts) fetch(p + 2);
+        const int n = sh.count;
+        if (n > a.room) {
+            crowded = true;
+            break;
+        }
+        if (n > a.room / 2 && p + 1 < parts) {
+            least = keep_largest(sh, cand, n, k, mass, c);
+            if (sh.count > a.room / 2) {
+                crowded = true;
+                break;
+            }
+        }
+    }
+    int n = sh.count;
+    __syncthreads();
+    if (crowded) {
+        // values crowd at the bound: an exact one, from the whole row once more (what is on its way is not used)
+        for (int q = p + 1; q < min(p + 3, parts); ++q) late |= !mbar_wait(smem_u32(&shared.bar[q & 1]), (uint32_t)(q >> 1) & 1);
+        const unsigned long long threshold = exact_threshold(cut, 0, sh, cand, k);
+        if (t == 0) sh.count = 0;
+        __syncthreads();
+        mass = gather_top<T, false, false>(Source<T, false>{cut, nullptr}, 0, sh, cand, threshold, c);
+        __syncthreads();
+        n = sh.count;
+        __syncthreads();
+    }
+    if (late) mass.s = __uint_as_float(0x7fffffffu);   // the logits never came
+    for (int i = t; i < n; i += threads) {
+        const unsigned long long raw = cand.at[i];
+        cand.at[i] = composite(__uint_as_float((uint32_t)(raw >> 32)), (int)(uint32_t)raw);
+    }
+    __syncthreads();
     if (n < k) {
         // fewer than k are above -inf, so enough of the first k elements are -inf
         if (t == 0) sh.count = n;

@@ -61,7 +61,8 @@ def check_top(z, k, tau):
 
 TOPS = [(1, 1, 1), (3, 2, 1), (2, 2, 2), (5, 7, 3), (4, 8, 8), (3, 9, 4), (2, 63, 63), (2, 65, 17), (3, 255, 100), (3, 256, 256), (2, 257, 256),
         (2, 300, 256), (3, 1000, 1), (2, 1023, 200), (3, 2049, 256), (1, 4099, 64), (40, 5000, 30), (1, 10000, 32), (700, 10000, 64),
-        (2, 50001, 128), (1, 131072, 256), (1, 262147, 5), (300, 20011, 128)]
+        (2, 50001, 128), (1, 131072, 256), (1, 262147, 5), (300, 20011, 128),
+        (160, 131072, 256), (150, 110003, 1), (149, 102401, 40)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
@@ -71,7 +72,7 @@ def test_top_logits(rows, cols, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("rows,cols,k", [(3, 40, 7), (2, 700, 64), (1, 10000, 64), (320, 10000, 200), (2, 40000, 256)])
+@pytest.mark.parametrize("rows,cols,k", [(3, 40, 7), (2, 700, 64), (1, 10000, 64), (320, 10000, 200), (2, 40000, 256), (148, 104003, 100)])
 @pytest.mark.parametrize("kind", ["equal", "zeros", "few_values", "masked", "nearly_all_masked", "empty", "steps", "huge", "nan"])
 def test_top_logits_ties_and_masks(kind, rows, cols, k, dtype):
     g = gen(7)
