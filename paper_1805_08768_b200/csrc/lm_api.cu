@@ -144,14 +144,17 @@ struct RowPlan {
 // A segment is at most kRoomBytes where eight blocks are enough for that; few rows are spread over as
 // many blocks as keep the GPU busy, each with at least 2048 elements.
 constexpr int kRoomBytes = 100 * 1024;
+int spread(int64_t rows, int64_t cols, int shift) {
+    while (shift < 3 && rows * (2 << shift) <= 2 * sm_count() && cols >= 2048 * (2 << shift)) ++shift;
+    return shift;
+}
 RowPlan plan_rows(int64_t rows, int64_t cols, int width) {
-    int64_t size = 1;
-    while (size < 8 && cols * width > size * kRoomBytes) size *= 2;
-    while (size < 8 && rows * size * 2 <= 2 * sm_count() && cols >= 2048 * size * 2) size *= 2;
-    const int64_t segment = ceil_div(ceil_div(cols, 64), size) * 64;
+    int shift = 0;
+    while (shift < 3 && cols * width > ((int64_t)kRoomBytes << shift)) ++shift;
     RowPlan p;
-    p.size = (int)size;
-    p.shift = size == 8 ? 3 : size == 4 ? 2 : size == 2 ? 1 : 0;
+    p.shift = spread(rows, cols, shift);
+    p.size = 1 << p.shift;
+    const int64_t segment = ceil_div(ceil_div(cols, 64), p.size) * 64;
     p.room = (int)std::min<int64_t>(segment, kRoomBytes / width);
     p.threads = segment * width <= 32 * 1024 ? 128 : 256;
     return p;
@@ -182,13 +185,19 @@ DistillArgs distill_args(const void* logits, int64_t rows, int64_t cols, int64_t
 // A second exponential per element where labels are mixed in at another temperature than the teacher's.
 bool second_exponential(const DistillArgs& a) { return a.labels && a.temperature != 1.f; }
 
+// Bytes of a segment that a block of k_distill holds at a time.  Nine to ten blocks fit an SM for the word
+// model's rows, five for longer ones; us for loss / loss and gradient with parts of 24, 32, 40 and 48 KB:
+// 4095 x 50001 bfloat16 91, 92, 94, 105 / 201, 194, 189, 200; 4480 x 10000 float32 - / 76, 81, 70, 70;
+// 4096 x 32000 bfloat16 - / 121, 114, 117, 126.
+constexpr int kPartBytes = 40 * 1024;
+
 template <typename T, bool CE2, bool GRAD> int launch_distill(DistillArgs a, cudaStream_t st) {
-    const RowPlan p = plan_rows(a.rows, a.cols, (int)sizeof(T));
-    a.room = p.room;
-    a.shift = p.shift;
-    const size_t smem = (size_t)p.room * sizeof(T) + 32 + (size_t)a.k * 12;
-    if (!allow_smem<k_distill<T, CE2, GRAD>>(kRoomBytes + 32 + SBC_DISTILL_MOST * 12)) return SBC_ECUDA;
-    return launch(k_distill<T, CE2, GRAD>, dim3((unsigned)(a.rows * p.size)), p.threads, smem, st, p.size, 0, a);
+    a.shift = spread(a.rows, a.cols, 0);
+    const int64_t segment = ceil_div(ceil_div(a.cols, 64), 1 << a.shift) * 64 + 8;   // with the row's offset from a granule
+    a.part = (int)std::min<int64_t>(segment, kPartBytes / (int)sizeof(T));
+    const size_t smem = (size_t)a.part * sizeof(T) + (size_t)a.k * 12;
+    if (!allow_smem<k_distill<T, CE2, GRAD>>(kPartBytes + SBC_DISTILL_MOST * 12)) return SBC_ECUDA;
+    return launch(k_distill<T, CE2, GRAD>, dim3((unsigned)(a.rows << a.shift)), kDistillThreads, smem, st, 1 << a.shift, 0, a);
 }
 
 template <bool GRAD> int distill_by_type(const DistillArgs& a, int dtype, cudaStream_t st) {

@@ -220,7 +220,7 @@ struct DistillArgs {
     void* grad;
     long long rows, stride, grad_stride;
     int cols, k;
-    int room;                  // elements of a row that a block holds at a time
+    int part;                  // elements of a segment that a block holds at a time (a multiple of 8)
     int shift;                 // 2^shift blocks share a row
     float temperature, alpha;
     const float* values;       // teacher: rows x k logits
@@ -363,7 +363,7 @@ __device__ __forceinline__ void write_sent(T* out, const S& slope, int first, in
         out[label - first] = from_float<T>(slope.unsent_label(label_z));
 }
 
-constexpr int kDistillThreads = 256, kDistillWarps = kDistillThreads / 32;
+constexpr int kDistillThreads = 128, kDistillWarps = kDistillThreads / 32;
 
 struct DistillShared {
     uint64_t bar;                                                    // the logits' arrival
@@ -377,8 +377,9 @@ struct DistillShared {
 };
 
 // One row per cluster; a block keeps its segment in shared memory, with the sent words taken out (-inf),
-// so the sum over the others is a plain one.  Segments that do not fit are taken in parts, twice.
-template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDistillThreads, 5) k_distill(DistillArgs a) {
+// so the sum over the others is a plain one.  Longer segments are taken in parts, for a gradient twice
+// (the forward call sums in the same order, so two calls and one give the same bits).
+template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDistillThreads, 10) k_distill(DistillArgs a) {
     extern __shared__ __align__(16) uint8_t dyn[];
     __shared__ DistillShared sh;
     constexpr int E = Gran<T>::E;
@@ -388,11 +389,10 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
     const T* z = static_cast<const T*>(a.logits) + row * a.stride;
     const int first = segment_start(a.cols, rank, a.shift), n = segment_start(a.cols, rank + 1, a.shift) - first;
     T* held = reinterpret_cast<T*>(dyn);
-    float* sent_t = reinterpret_cast<float*>(dyn + (size_t)(a.room + 2 * E) * sizeof(T));
+    float* sent_t = reinterpret_cast<float*>(dyn + (size_t)a.part * sizeof(T));
     float* sent_z = sent_t + a.k;
     int* sent_at = reinterpret_cast<int*>(sent_z + a.k);
     const float c = kLog2e / a.temperature, inv = 1.f / a.temperature;
-    const int parts = n > a.room ? (n + a.room - 1) / a.room : 1;
 
     const uint32_t bar = smem_u32(&sh.bar);
     if (t == 0) {
@@ -400,7 +400,13 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     after_earlier_kernels();
-    Cut<T> cut(z + first, min(n, a.room));
+    const Cut<T> segment(z + first, n);
+    const int part_grans = a.part / E, parts = max(1, (segment.grans + part_grans - 1) / part_grans);   // whole granules
+    const auto part_of = [&](int part) {
+        const int slot = part * part_grans * E, from = max(0, slot - segment.phase), to = min(n, slot + part_grans * E - segment.phase);
+        return Cut<T>(segment.p + from, max(0, to - from));
+    };
+    Cut<T> cut = part_of(0);
     cut.stage(held, bar);
     uint32_t phase = 0;
     bool late = false;
@@ -437,16 +443,16 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
 
     Mass<CE2> others, sent;
     for (int part = 0; part < parts; ++part) {
-        const int lo = part * a.room;
         if (part > 0) {
             before_copies();
             __syncthreads();
-            cut = Cut<T>(z + first + lo, min(n - lo, a.room));
+            cut = part_of(part);
             cut.stage(held, bar);
         }
         landed();
+        const int lo = first + (int)(cut.p - segment.p);
         for (int i = t; i < a.k; i += threads) {
-            const int at = sent_at[i] - first - lo;
+            const int at = sent_at[i] - lo;
             if (sent_at[i] < 0 || at < 0 || at >= cut.n) continue;
             const float zv = to_float(held[cut.phase + at]);
             held[cut.phase + at] = from_float<T>(-infinity());
@@ -558,14 +564,14 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
     if (GRAD) {
         out = static_cast<T*>(a.grad) + row * a.grad_stride + first;
         for (int part = 0; part < parts; ++part) {
-            const int lo = part * a.room;
             if (parts > 1) {
                 before_copies();
                 __syncthreads();
-                cut = Cut<T>(z + first + lo, min(n - lo, a.room));
+                cut = part_of(part);
                 cut.stage(held, bar);
                 landed();
             }
+            const int lo = (int)(cut.p - segment.p);
             slope.granules([&](const auto& gr) {
                 store_all(out + lo, cut, [&](int i) { return *reinterpret_cast<const uint4*>(held + i * E); }, [&](const uint4& q) { return gr.granule(q); });
             });
@@ -603,7 +609,7 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
 }
 
 // The backward call: statistics come from the forward one.  Blocks that share a row do not need one another.
-template <typename T, bool CE2> __global__ void __launch_bounds__(kDistillThreads, 4) k_distill_grad(DistillArgs a) {
+template <typename T, bool CE2> __global__ void __launch_bounds__(256, 4) k_distill_grad(DistillArgs a) {
     extern __shared__ uint32_t words[];
     const int t = threadIdx.x, threads = blockDim.x;
     const int rank = (int)(blockIdx.x & ((1u << a.shift) - 1u));
