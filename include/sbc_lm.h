@@ -128,7 +128,7 @@ int sbc_fp4_product(const sbc_fp4 *a, const sbc_fp4 *b, void *out, int dtype, in
  * not sent.
  *
  * logits  device, dtype, rows x cols; rows may be 0
- * k       1 .. min(cols, SBC_TOP_MOST); temperature > 0
+ * k       1 .. min(cols, SBC_TOP_MOST); temperature 1e-6 .. 1e6
  * values float, indices int32: device, rows x k;  rest: device, rows floats
  */
 int sbc_top_logits(const void *logits, int dtype, int64_t rows, int64_t cols, int64_t row_stride, int k,
@@ -157,7 +157,7 @@ typedef struct sbc_distill {
     const float *rest;
     const int64_t *labels;
     int32_t k;         /* 1 .. SBC_DISTILL_MOST */
-    float temperature; /* > 0 */
+    float temperature; /* 1e-6 .. 1e6 */
     float alpha;       /* 0 .. 1 */
     int32_t reserved;  /* 0 */
 } sbc_distill;

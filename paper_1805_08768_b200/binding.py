@@ -197,13 +197,16 @@ def _check(code: int, where: str) -> None:
         raise SbcError(code, where)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _current_stream() -> int:
     return torch.cuda.current_stream().cuda_stream
 
 
 if hasattr(torch._C, "_cuda_getCurrentRawStream"):   # the same handle without the Stream object around it
     def _current_stream() -> int:  # noqa: F811
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        return torch._C._cuda_getCurrentRawStream(_current_device())
 
 
 def _cuda_stream(stream) -> int:
@@ -553,14 +556,28 @@ FP4_FORMATS = {"e8m0": 0, "e4m3": 1}   # block scales: powers of two for 32 elem
 def _matrix(t: torch.Tensor, name: str) -> None:
     if not (t.is_cuda and t.dim() == 2 and t.dtype in DTYPE_CODES):
         raise TypeError(f"{name} must be a float32, bfloat16 or float16 CUDA matrix")
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    if t.get_device() != _current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{_current_device()}")
     rows, cols = t.shape
     across, along = t.stride()
     if cols > 1 and along != 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
     if rows > 1 and across < cols:
         raise ValueError(f"{name}: rows must not overlap")
+
+
+def _beside(t: torch.Tensor, other: torch.Tensor, name: str) -> None:
+    if t.get_device() != other.get_device():
+        raise ValueError(f"{name} is on {t.device}, not on {other.device}")
+
+
+def _status(status: Optional[torch.Tensor], other: torch.Tensor) -> Optional[int]:
+    if status is None:
+        return None
+    if not (status.is_cuda and status.dtype == torch.int32 and status.numel() >= 1):
+        raise TypeError("status must be an int32 CUDA tensor")
+    _beside(status, other, "status")
+    return status.data_ptr()
 
 
 def _row_stride(t: torch.Tensor) -> int:
@@ -602,6 +619,8 @@ class Fp4Tensor:
             if t.numel() != n:
                 raise ValueError(f"{name}: {n} bytes needed for {rows} x {cols}, got {t.numel()}")
         _dev_f32(tensor_scale, "tensor_scale")
+        _beside(scales, values, "scales")
+        _beside(tensor_scale, values, "tensor_scale")
         if tensor_scale.numel() < 1:
             raise ValueError("tensor_scale must hold one value")
         self.rows, self.cols, self.format = rows, cols, format
@@ -641,8 +660,12 @@ class Fp4Tensor:
     tensor_scale = property(lambda self: self._views()[2])
 
     @property
+    def _any(self) -> torch.Tensor:
+        return self._room if self._room is not None else self._parts[0]
+
+    @property
     def device(self) -> torch.device:
-        return (self._room if self._parts is None else self._parts[0]).device
+        return self._any.device
 
     @property
     def nbytes(self) -> int:
@@ -689,6 +712,7 @@ def sbc_fp4_dequantise(q: Fp4Tensor, dtype: torch.dtype = torch.float32, out: Op
     _matrix(out, "out")
     if tuple(out.shape) != (q.rows, q.cols):
         raise ValueError(f"out must be {q.rows} x {q.cols}")
+    _beside(out, q._any, "out")
     code = lib().sbc_fp4_dequantise(C.byref(q.desc), out.data_ptr(), DTYPE_CODES[out.dtype], _row_stride(out),
                                     _cuda_stream(stream))
     if code:
@@ -707,9 +731,10 @@ def sbc_fp4_product(a: Fp4Tensor, b: Fp4Tensor, dtype: torch.dtype = torch.bfloa
     _matrix(out, "out")
     if tuple(out.shape) != (a.rows, b.rows):
         raise ValueError(f"out must be {a.rows} x {b.rows}")
+    if not out.get_device() == a._any.get_device() == b._any.get_device():
+        raise ValueError("operands and result must be on one device")
     code = lib().sbc_fp4_product(C.byref(a.desc), C.byref(b.desc), out.data_ptr(), DTYPE_CODES[out.dtype],
-                                 _row_stride(out), status.data_ptr() if status is not None else None,
-                                 _cuda_stream(stream))
+                                 _row_stride(out), _status(status, out), _cuda_stream(stream))
     if code:
         _check(code, "sbc_fp4_product")
     return out
@@ -735,13 +760,14 @@ def sbc_top_logits(logits: torch.Tensor, k: int, temperature: float = 1.0,
     return values, indices, rest
 
 
-def _rows_of(t: Optional[torch.Tensor], rows: int, dtype: torch.dtype, name: str) -> Optional[int]:
+def _rows_of(t: Optional[torch.Tensor], rows: int, dtype: torch.dtype, name: str, other: torch.Tensor) -> Optional[int]:
     if t is None:
         return None
     if not (t.is_cuda and t.dtype == dtype and t.is_contiguous()):
         raise TypeError(f"{name} must be a contiguous {dtype} CUDA tensor")
     if t.numel() != rows:
         raise ValueError(f"{name} must hold one value per row")
+    _beside(t, other, name)
     return t.data_ptr()
 
 
@@ -753,12 +779,14 @@ def _taught(logits, values, indices, rest, temperature, alpha, labels) -> Distil
         raise TypeError("indices must be a contiguous int32 CUDA tensor")
     if values.dim() != 2 or values.shape != indices.shape or values.shape[0] != rows:
         raise ValueError("values and indices must be rows x k")
+    _beside(values, logits, "values")
+    _beside(indices, logits, "indices")
     if not 1 <= values.shape[1] <= DISTILL_MOST:
         raise ValueError(f"k must be in 1 .. {DISTILL_MOST}")
     if not 1 <= cols <= DISTILL_COLS:
         raise ValueError(f"logits must have 1 .. {DISTILL_COLS} columns")
-    return DistillDesc(values.data_ptr(), indices.data_ptr(), _rows_of(rest, rows, torch.float32, "rest"),
-                       _rows_of(labels, rows, torch.int64, "labels"), values.shape[1], float(temperature),
+    return DistillDesc(values.data_ptr(), indices.data_ptr(), _rows_of(rest, rows, torch.float32, "rest", logits),
+                       _rows_of(labels, rows, torch.int64, "labels", logits), values.shape[1], float(temperature),
                        float(alpha), 0)
 
 
@@ -768,6 +796,7 @@ def _grad_out(logits: torch.Tensor, out: Optional[torch.Tensor], stream) -> torc
     _matrix(out, "out")
     if out.shape != logits.shape or out.dtype != logits.dtype:
         raise ValueError("out must have the logits' shape and type")
+    _beside(out, logits, "out")
     return out
 
 
@@ -783,7 +812,7 @@ def sbc_distill_loss(logits: torch.Tensor, values: torch.Tensor, indices: torch.
     stats = _empty(stream, (rows, DISTILL_STATS), torch.float32, logits.device)
     _check(lib().sbc_distill_loss(logits.data_ptr(), DTYPE_CODES[logits.dtype], rows, cols, _row_stride(logits),
                                   C.byref(d), loss.data_ptr(), stats.data_ptr(),
-                                  status.data_ptr() if status is not None else None, _cuda_stream(stream)),
+                                  _status(status, logits), _cuda_stream(stream)),
            "sbc_distill_loss")
     return loss, stats
 
@@ -797,8 +826,8 @@ def sbc_distill_grad(logits: torch.Tensor, values: torch.Tensor, indices: torch.
     rows, cols = logits.shape
     out = _grad_out(logits, out, stream)
     _check(lib().sbc_distill_grad(logits.data_ptr(), DTYPE_CODES[logits.dtype], rows, cols, _row_stride(logits),
-                                  C.byref(d), _rows_of(stats, rows * DISTILL_STATS, torch.float32, "stats"),
-                                  _rows_of(grad_loss, rows, torch.float32, "grad_loss"), out.data_ptr(),
+                                  C.byref(d), _rows_of(stats, rows * DISTILL_STATS, torch.float32, "stats", logits),
+                                  _rows_of(grad_loss, rows, torch.float32, "grad_loss", logits), out.data_ptr(),
                                   _row_stride(out), _cuda_stream(stream)), "sbc_distill_grad")
     return out
 
@@ -814,8 +843,8 @@ def sbc_distill_loss_grad(logits: torch.Tensor, values: torch.Tensor, indices: t
     out = _grad_out(logits, out, stream)
     loss = _empty(stream, (rows,), torch.float32, logits.device)
     _check(lib().sbc_distill_loss_grad(logits.data_ptr(), DTYPE_CODES[logits.dtype], rows, cols, _row_stride(logits),
-                                       C.byref(d), _rows_of(grad_loss, rows, torch.float32, "grad_loss"),
+                                       C.byref(d), _rows_of(grad_loss, rows, torch.float32, "grad_loss", logits),
                                        loss.data_ptr(), out.data_ptr(), _row_stride(out),
-                                       status.data_ptr() if status is not None else None, _cuda_stream(stream)),
+                                       _status(status, logits), _cuda_stream(stream)),
            "sbc_distill_loss_grad")
     return loss, out

@@ -160,9 +160,12 @@ RowPlan plan_rows(int64_t rows, int64_t cols, int width) {
     return p;
 }
 
+// Beyond these the scaled logits would leave 32 bits.
+bool temperature_ok(float t) { return t >= 1e-6f && t <= 1e6f; }
+
 bool distill_ok(const sbc_distill* d, int64_t rows, int64_t cols) {
     return d && (rows == 0 || (d->values && d->indices)) && aligned(d->values, 4) && aligned(d->indices, 4) && aligned(d->rest, 4) &&
-           aligned(d->labels, 8) && d->k >= 1 && d->k <= SBC_DISTILL_MOST && d->temperature > 0.f && d->temperature <= 1e6f &&
+           aligned(d->labels, 8) && d->k >= 1 && d->k <= SBC_DISTILL_MOST && temperature_ok(d->temperature) &&
            d->alpha >= 0.f && d->alpha <= 1.f && d->reserved == 0 && cols <= SBC_DISTILL_COLS && rows <= kMaxDim / 8;
 }
 
@@ -386,7 +389,7 @@ int sbc_fp4_product(const sbc_fp4* a, const sbc_fp4* b, void* out, int dtype, in
 int sbc_top_logits(const void* logits, int dtype, int64_t rows, int64_t cols, int64_t row_stride, int k, float temperature,
                    float* values, int32_t* indices, float* rest, sbc_cuda_stream_t stream) {
     if (!width_of(dtype) || rows < 0 || rows > kMaxDim / 8 || cols < 1 || cols > kMaxDim) return SBC_EINVAL;
-    if (k < 1 || k > std::min<int64_t>(cols, SBC_TOP_MOST) || !(temperature > 0.f) || !(temperature <= 1e6f)) return SBC_EINVAL;
+    if (k < 1 || k > std::min<int64_t>(cols, SBC_TOP_MOST) || !temperature_ok(temperature)) return SBC_EINVAL;
     if (rows == 0) return SBC_OK;
     if (!matrix_ok(logits, dtype, rows, cols, row_stride)) return SBC_EINVAL;
     if (!values || !indices || !rest || !aligned(values, 4) || !aligned(indices, 4) || !aligned(rest, 4)) return SBC_EINVAL;

@@ -262,6 +262,8 @@ def test_refusals():
         sbc.sbc_fp4_product(a, a, out=torch.empty(3, 4, device=DEV))
     with pytest.raises(ValueError):
         sbc.Fp4Tensor(a.values[:3], a.scales, a.tensor_scale, 4, 64, "e8m0")
+    with pytest.raises(TypeError):
+        sbc.sbc_fp4_product(a, a, status=torch.zeros(1, device=DEV))
     with pytest.raises(ValueError):
         sbc.Fp4Tensor(a.values, a.scales[:-512], a.tensor_scale, 4, 64, "e8m0")
 
@@ -274,3 +276,43 @@ def test_work_on_another_stream():
     got = sbc.sbc_fp4_product(a, b, torch.float32, stream=side)
     side.synchronize()
     check_product(got, a, b)
+
+
+def test_matrices_of_more_than_2_31_elements():
+    """The last rows and columns of a long matrix come out as those of a matrix of their own."""
+    rows, cols = 66000, 32800
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device=DEV)
+    for lo in range(0, rows, 6600):
+        x[lo:lo + 6600] = torch.randn(6600, cols, generator=torch.Generator(device=DEV).manual_seed(lo), device=DEV)
+    assert x.numel() > 2 ** 31
+    q, q_t = sbc.sbc_fp4_quantise_both(x, "e8m0")
+    out = sbc.sbc_fp4_dequantise(q, torch.bfloat16)
+    assert same(out[-300:], plain_round(x[-300:], "e8m0")) and same(out[:10], plain_round(x[:10], "e8m0"))
+    out_t = sbc.sbc_fp4_dequantise(q_t, torch.bfloat16)
+    last = x[:, -40:].t().contiguous()
+    assert same(out_t[-40:], plain_round(last, "e8m0"))
+    del out, out_t, q_t
+    x[rows - 1, cols - 1] = 4096.0        # the tensor's largest is its last element
+    e = sbc.sbc_fp4_quantise(x, "e4m3")
+    assert float(e.tensor_scale) == 4.0
+    # a product whose result has more than 2^31 elements
+    del x, e
+    a = sbc.sbc_fp4_quantise(values(66000, 64, torch.bfloat16, 1) / 16, "e8m0")
+    b = sbc.sbc_fp4_quantise(values(32800, 64, torch.bfloat16, 2) / 16, "e8m0")
+    y = sbc.sbc_fp4_product(a, b, torch.bfloat16)
+    tail = sbc.Fp4Tensor(a.values[65920:].contiguous(), a.scales[65920 // 128 * 512:].contiguous(), a.tensor_scale, 80, 64, "e8m0")
+    check_product(y[65920:].contiguous(), tail, b)
+
+
+def test_calls_in_a_graph():
+    """A recorded sequence of calls runs again on new inputs."""
+    x, w = values(200, 650, torch.bfloat16, 3), values(300, 650, torch.float32, 4)
+    w4 = sbc.sbc_fp4_quantise(w, "e4m3")
+    sbc.sbc_fp4_product(sbc.sbc_fp4_quantise(x, "e4m3"), w4, torch.float32)      # kernels loaded before the recording
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = sbc.sbc_fp4_product(sbc.sbc_fp4_quantise(x, "e4m3"), w4, torch.float32)
+    for seed in (7, 8):
+        x.copy_(values(200, 650, torch.bfloat16, seed))
+        graph.replay()
+        assert torch.equal(y, sbc.sbc_fp4_product(sbc.sbc_fp4_quantise(x, "e4m3"), w4, torch.float32))

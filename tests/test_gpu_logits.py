@@ -401,3 +401,39 @@ def test_work_on_another_stream():
     side.synchronize()
     again, grad2 = sbc.sbc_distill_loss_grad(z, values, indices, rest=rest, temperature=2.0)
     assert torch.equal(loss, again) and torch.equal(grad, grad2)
+
+
+def test_logits_of_more_than_2_31_elements():
+    """The last rows of a long matrix come out as those of a matrix of their own."""
+    rows, cols, k = 33000, 66000, 20
+    z = torch.empty(rows, cols, dtype=torch.bfloat16, device=DEV)
+    for lo in range(0, rows, 3300):
+        z[lo:lo + 3300] = 3 * torch.randn(3300, cols, generator=gen(lo), device=DEV)
+    assert z.numel() > 2 ** 31
+    values, indices, rest = sbc.sbc_top_logits(z, k, 2.0)
+    few = z[-200:].contiguous()
+    part = sbc.sbc_top_logits(few, k, 2.0)
+    assert torch.equal(values[-200:], part[0]) and torch.equal(indices[-200:], part[1])
+    check_top(few[-3:], k, 2.0)
+    values += torch.randn(values.shape, generator=gen(1), device=DEV)
+    loss, stats = sbc.sbc_distill_loss(z, values, indices, rest, 2.0)
+    grad = sbc.sbc_distill_grad(z, values, indices, stats, rest=rest, temperature=2.0)
+    one, one_grad = sbc.sbc_distill_loss_grad(few, values[-200:].contiguous(), indices[-200:].contiguous(), rest=rest[-200:].contiguous(), temperature=2.0)
+    want, want_grad, size = plain(few[-4:], values[-4:], indices[-4:], rest[-4:], 2.0, 1.0, None, None)
+    delta = (cols / 256 + 64 + 4 * 40) * U
+    assert bool(((loss[-4:] - want).abs() <= 4 * 10 * delta).all()) and bool(((loss[-200:] - one).abs() <= 4 * 10 * delta).all())
+    allowed = 4 * delta * size + ROUND[z.dtype] * want_grad.abs() + 1e-37
+    assert bool(((grad[-4:].double() - want_grad).abs() <= allowed).all())
+
+
+def test_calls_in_a_graph():
+    z = logits(64, 5000, torch.bfloat16, 3)
+    run = lambda: sbc.sbc_distill_loss_grad(z, *sbc.sbc_top_logits(z, 16, 2.0)[:2], temperature=2.0)   # noqa: E731
+    run()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loss, grad = run()
+    z.copy_(logits(64, 5000, torch.bfloat16, 9))
+    graph.replay()
+    again, grad2 = run()
+    assert torch.equal(loss, again) and torch.equal(grad, grad2)
