@@ -335,11 +335,12 @@ int sbc_fp4_dequantise(const sbc_fp4* q, void* out, int dtype, int64_t row_strid
     a.stride = row_stride;
     a.pitch = (long long)sbc_fp4_row_bytes(q->cols);
     a.ktiles = ktiles_of(q->cols, q->format);
-    a.align = row_align(out, row_stride, width_of(dtype));
     const int64_t blocks = std::min<int64_t>(pieces(q->rows, q->cols, false), sm_count() * 8);
     return by_dtype(dtype, [&](auto* as) {
         using T = std::remove_pointer_t<decltype(as)>;
-        const auto kernel = q->format == SBC_FP4_E4M3 ? k_fp4_dequantise<T, SBC_FP4_E4M3> : k_fp4_dequantise<T, SBC_FP4_E8M0>;
+        const bool shift = row_align(out, row_stride, width_of(dtype)) < 16, e4m3 = q->format == SBC_FP4_E4M3;
+        const auto kernel = shift ? (e4m3 ? k_fp4_dequantise<T, SBC_FP4_E4M3, true> : k_fp4_dequantise<T, SBC_FP4_E8M0, true>)
+                                  : (e4m3 ? k_fp4_dequantise<T, SBC_FP4_E4M3, false> : k_fp4_dequantise<T, SBC_FP4_E8M0, false>);
         return launch(kernel, dim3((unsigned)blocks), kQThreads, 0, stream, 0, 0, a);
     });
 }

@@ -357,15 +357,14 @@ struct DequantiseArgs {
     const float* tensor;
     void* out;
     long long rows, cols, stride, pitch, ktiles;
-    int align;
 };
 
-// The grid values of eight nibbles, exact.  A bfloat16 holds them, its two bytes come from tables that
-// a byte permutation looks up, four at a time.
-__device__ __forceinline__ void grid_values(float* x, uint32_t w) {
+// The grid values of N (4 or 8) nibbles, exact.  A bfloat16 holds them, its two bytes come from tables
+// that a byte permutation looks up, four at a time.
+template <int N> __device__ __forceinline__ void grid_values(float* x, uint32_t w) {
     const uint32_t m = w & 0x77777777u;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < N / 4; ++h) {
         const uint32_t hi = __byte_perm(0x3f3f3f00u, 0x40404040u, m >> (16 * h)), lo = __byte_perm(0xc0800000u, 0xc0804000u, m >> (16 * h));
         const uint32_t a = __byte_perm(lo, hi, 0x5140), b = __byte_perm(lo, hi, 0x7362);   // values 0, 1 and 2, 3
         const uint32_t s = w >> (16 * h);
@@ -382,37 +381,95 @@ template <int FMT> __device__ __forceinline__ float scale_value(uint32_t code) {
     return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3)));
 }
 
-template <typename T, int FMT> __global__ void __launch_bounds__(kQThreads) k_fp4_dequantise(DequantiseArgs a) {
-    constexpr int kB = Fp4<FMT>::kBlock;
-    T* out = static_cast<T*>(a.out);
+// A warp's rows in pieces of 2048 elements, cut where the output's 16-byte granules fall: stores are whole
+// granules at any alignment.  SHIFT: rows start inside a granule, so what moves is the nibbles (a funnel
+// shift of two words) and the place in a granule where a block ends.  (With stores as wide as an odd
+// row's alignment 16384 x 4095 bfloat16 took 196 us.)
+template <typename T, int FMT, bool SHIFT> __global__ void __launch_bounds__(kQThreads, 4) k_fp4_dequantise(DequantiseArgs a) {
+    constexpr int kB = Fp4<FMT>::kBlock, E = 16 / (int)sizeof(T), kAhead = SHIFT ? 4 : 8;
     after_earlier_kernels();
     const float tensor = FMT == SBC_FP4_E4M3 ? *a.tensor : 1.f;
-    // a step of 256 elements is 128 bytes of nibbles and whole scale tiles
-    constexpr int kTileStep = 256 / kB / 4 * 512;
-    warp_pieces(a.rows, a.cols, blockIdx.x * (kQThreads / 32) + threadIdx.x / 32, gridDim.x * (kQThreads / 32), [&](long long r, long long c, int left) {
-        const uint8_t* values = a.values + r * a.pitch + c / 2;
-        const uint8_t* scales = a.scales + (r / 128 * a.ktiles + c / (4 * kB)) * 512 + (r % 32) * 16 + (r % 128 / 32) * 4 + c / kB % 4;
-        T* to = out + r * a.stride + c;
-        // a piece's loads go ahead of its stores
-        uint32_t w[kSteps], code[kSteps];
+    const int lane = threadIdx.x & 31;
+    const uint32_t warp = blockIdx.x * (kQThreads / 32) + threadIdx.x / 32, warps = gridDim.x * (kQThreads / 32);
+    const uint32_t per_row = (uint32_t)((a.cols + (SHIFT ? E - 1 : 0) + kPiece - 1) / kPiece);
+    const long long all = a.rows * per_row;
+    for (long long i = warp; i < all; i += warps) {
+        const long long r = all < (1ll << 32) ? (long long)((uint32_t)i / per_row) : i / per_row;
+        T* const row = static_cast<T*>(a.out) + r * a.stride;
+        const int phase = SHIFT ? (int)((uint32_t)(uintptr_t)row & 15u) / (int)sizeof(T) : 0;
+        // this lane's first granule (the next ones are 32 lanes apart), and how many elements there are from it on
+        const long long first = (i - r * per_row) * kPiece - phase + lane * E;
+        const int left = (int)min(a.cols - first, (long long)kPiece + E);
+        const int most = SHIFT ? __shfl_sync(0xffffffffu, left, 0) : left;   // lane 0 has most
+        if (most <= 0) continue;
+        const int e0 = (int)first, end = (int)a.cols - 1;
+        const uint8_t* const values = a.values + r * a.pitch;
+        const uint8_t* const scales = a.scales + r / 128 * a.ktiles * 512 + (r % 32) * 16 + (r % 128 / 32) * 4;
+        const auto code_of = [&](uint32_t e) { return (uint32_t)scales[(size_t)(e / (4 * kB)) * 512 + e / kB % 4]; };
+        T* const to = row + e0;
+        constexpr int kGrans = kPiece / (32 * E);
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            if (left <= 256 * i) break;
-            w[i] = *reinterpret_cast<const uint32_t*>(values + i * 128);
-            code[i] = scales[i * kTileStep];
+        for (int g0 = 0; g0 < kGrans; g0 += kAhead) {
+            uint32_t lo[kAhead], hi[kAhead], c0[kAhead], c1[kAhead];
+#pragma unroll
+            for (int g = 0; g < kAhead; ++g) {
+                const int at = (g0 + g) * 32 * E;
+                if ((SHIFT ? most : left) <= at) break;
+                if (SHIFT) {
+                    // what follows a lane's word and block is the next lane's
+                    const uint32_t f = (uint32_t)min(max(e0 + at, 0), end);
+                    lo[g] = reinterpret_cast<const uint32_t*>(values)[f / 8];
+                    c0[g] = code_of(f);
+                    hi[g] = c1[g] = 0;
+                    if (lane == 31) {
+                        const uint32_t next = (uint32_t)min((int)f + E, end);
+                        hi[g] = reinterpret_cast<const uint32_t*>(values)[next / 8];
+                        c1[g] = code_of(next);
+                    }
+                } else {
+                    // (a step of 32 granules is whole scale tiles, or half of one for 32 x 4 elements of 32-element blocks)
+                    if (E == 8) lo[g] = *reinterpret_cast<const uint32_t*>(values + (uint32_t)(e0 + at) / 2);
+                    if (E == 4) lo[g] = *reinterpret_cast<const uint16_t*>(values + (uint32_t)(e0 + at) / 2);
+                    c0[g] = code_of((uint32_t)(e0 + at));
+                }
+            }
+#pragma unroll
+            for (int g = 0; g < kAhead; ++g) {
+                const int at = (g0 + g) * 32 * E;
+                if ((SHIFT ? most : left) <= at) break;
+                if (SHIFT) {
+                    const uint32_t word = __shfl_down_sync(0xffffffffu, lo[g], 1), code = __shfl_down_sync(0xffffffffu, c0[g], 1);
+                    if (lane < 31) hi[g] = word, c1[g] = code;
+                }
+                if (SHIFT && left <= at) continue;
+                float x[E];
+                const float s0 = scale_value<FMT>(c0[g]) * tensor;
+                uint4 q;
+                T* v = reinterpret_cast<T*>(&q);
+                int skip = 0;
+                if (SHIFT) {
+                    const uint32_t f = (uint32_t)max(e0 + at, 0);
+                    skip = (int)f - (e0 + at);
+                    grid_values<E>(x, __funnelshift_r(lo[g], hi[g], 4 * (f & 7u)));
+                    const float s1 = scale_value<FMT>(c1[g]) * tensor;
+                    const int split = kB - (int)(f % kB);   // elements of the granule that belong to the first block
+#pragma unroll
+                    for (int j = 0; j < E; ++j) v[j] = from_float<T>(x[j] * (j < split ? s0 : s1));
+                } else {
+                    grid_values<E>(x, lo[g]);
+#pragma unroll
+                    for (int j = 0; j < E; ++j) v[j] = from_float<T>(x[j] * s0);
+                }
+                if (skip == 0 && left >= at + E) {
+                    *reinterpret_cast<uint4*>(to + at) = q;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < E; ++j)
+                        if (j + skip < E && at + skip + j < left) to[at + skip + j] = v[j];
+                }
+            }
         }
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            if (left <= 256 * i) break;
-            const float s = scale_value<FMT>(code[i]) * tensor;
-            float x[8];
-            grid_values(x, w[i]);
-            Pack8<T> v;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v.e[j] = from_float<T>(x[j] * s);
-            store8(to + 256 * i, v, min(8, left - 256 * i), a.align);
-        }
-    });
+    }
 }
 
 }  // namespace sbclm
