@@ -18,10 +18,14 @@ int width_of(int dtype) { return dtype == SBC_F32 ? 4 : (dtype == SBC_BF16 || dt
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
+// SMs of the current device (asked for once per device: the question costs as much as half a launch).
 int sm_count() {
+    static std::atomic<int> known[64];
     int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0)
-        return 148;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 148;
+    if (dev < 64 && (n = known[dev].load(std::memory_order_relaxed)) > 0) return n;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) return 148;
+    if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
     return n;
 }
 
@@ -145,7 +149,8 @@ struct RowPlan {
 // many blocks as keep the GPU busy, each with at least 2048 elements.
 constexpr int kRoomBytes = 100 * 1024;
 int spread(int64_t rows, int64_t cols, int shift) {
-    while (shift < 3 && rows * (2 << shift) <= 2 * sm_count() && cols >= 2048 * (2 << shift)) ++shift;
+    const int64_t blocks = 2 * sm_count();
+    while (shift < 3 && rows * (2 << shift) <= blocks && cols >= 2048 * (2 << shift)) ++shift;
     return shift;
 }
 RowPlan plan_rows(int64_t rows, int64_t cols, int width) {
