@@ -553,8 +553,10 @@ FP4_WORKSPACE_BYTES = 4096   # what sbc_fp4_workspace_bytes says for any matrix
 FP4_FORMATS = {"e8m0": 0, "e4m3": 1}   # block scales: powers of two for 32 elements, 8-bit floats for 16
 
 
-def _matrix(t: torch.Tensor, name: str) -> None:
-    if not (t.is_cuda and t.dim() == 2 and t.dtype in DTYPE_CODES):
+def _matrix(t: torch.Tensor, name: str) -> Tuple[int, int, int, int]:
+    """(rows, columns, elements between rows, type code) of a matrix argument."""
+    code = DTYPE_CODES.get(t.dtype)
+    if code is None or not t.is_cuda or t.dim() != 2:
         raise TypeError(f"{name} must be a float32, bfloat16 or float16 CUDA matrix")
     if t.get_device() != _current_device():
         raise ValueError(f"{name} is on {t.device}, the current device is cuda:{_current_device()}")
@@ -562,8 +564,11 @@ def _matrix(t: torch.Tensor, name: str) -> None:
     across, along = t.stride()
     if cols > 1 and along != 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
-    if rows > 1 and across < cols:
+    if rows <= 1:
+        across = max(cols, 1)
+    elif across < cols:
         raise ValueError(f"{name}: rows must not overlap")
+    return rows, cols, across, code
 
 
 def _beside(t: torch.Tensor, other: torch.Tensor, name: str) -> None:
@@ -580,17 +585,13 @@ def _status(status: Optional[torch.Tensor], other: torch.Tensor) -> Optional[int
     return status.data_ptr()
 
 
-def _row_stride(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
-
-
-def _empty(stream, shape, dtype, device) -> torch.Tensor:
-    """A new buffer that belongs to the stream which the work is enqueued on."""
+def _empty(stream, shape, dtype, like: torch.Tensor) -> torch.Tensor:
+    """A new buffer beside `like` that belongs to the stream which the work is enqueued on."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
     s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_cuda_stream(stream))
     with torch.cuda.stream(s):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
 
 
 def _fp4_sizes(rows: int, cols: int, format: str) -> Tuple[int, int]:
@@ -608,7 +609,7 @@ class Fp4Tensor:
     header's.  ``values`` uint8 [rows, row bytes], ``scales`` uint8 (flat), ``tensor_scale`` float32 [1];
     ``format`` is "e8m0" or "e4m3"."""
 
-    __slots__ = ("rows", "cols", "format", "desc", "_room", "_at", "_parts")
+    __slots__ = ("rows", "cols", "format", "desc", "_room", "_at", "_parts", "_device")
 
     def __init__(self, values: torch.Tensor, scales: torch.Tensor, tensor_scale: torch.Tensor, rows: int, cols: int,
                  format: str):
@@ -625,6 +626,7 @@ class Fp4Tensor:
             raise ValueError("tensor_scale must hold one value")
         self.rows, self.cols, self.format = rows, cols, format
         self._room, self._at, self._parts = None, 0, (values, scales, tensor_scale)
+        self._device = values.get_device()
         self.desc = Fp4Desc(values.data_ptr(), scales.data_ptr(), tensor_scale.data_ptr(), rows, cols,
                             FP4_FORMATS[format], 0)
 
@@ -635,6 +637,7 @@ class Fp4Tensor:
         self = cls.__new__(cls)
         self.rows, self.cols, self.format = rows, cols, format
         self._room, self._at, self._parts = room, at, None
+        self._device = room.get_device()
         base = room.data_ptr() + at
         self.desc = Fp4Desc(base, base + value_bytes, base + value_bytes + scale_bytes, rows, cols,
                             FP4_FORMATS[format], 0)
@@ -644,7 +647,10 @@ class Fp4Tensor:
     def empty(cls, rows: int, cols: int, format: str, device, stream=None) -> "Fp4Tensor":
         """Room for a rows x cols matrix, contents undefined."""
         value_bytes, scale_bytes = _fp4_sizes(rows, cols, format)
-        room = _empty(stream, value_bytes + scale_bytes + 16, torch.uint8, device)
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return cls.empty(rows, cols, format, device)
+        room = torch.empty(value_bytes + scale_bytes + 16, dtype=torch.uint8, device=device)
         return cls._in_room(room, 0, value_bytes, scale_bytes, rows, cols, format)
 
     def _views(self):
@@ -673,22 +679,22 @@ class Fp4Tensor:
 
 
 def _quantise(x, format, along_rows, along_cols, stream):
-    _matrix(x, "x")
-    rows, cols = x.shape
-    v, s = _fp4_sizes(rows, cols, format) if along_rows else (0, 0)
-    v_t, s_t = _fp4_sizes(cols, rows, format) if along_cols else (0, 0)
+    rows, cols, across, code = _matrix(x, "x")
     # one buffer: both tensors and, in front, the scratch of the call
-    ws = FP4_WORKSPACE_BYTES
-    at_t = ws + (v + s + 16 if along_rows else 0)
-    room = _empty(stream, at_t + (v_t + s_t + 16 if along_cols else 0), torch.uint8, x.device)
+    at_t = ws = FP4_WORKSPACE_BYTES
+    v = s = v_t = s_t = 0
+    if along_rows:
+        v, s = _fp4_sizes(rows, cols, format)
+        at_t += v + s + 16
+    if along_cols:
+        v_t, s_t = _fp4_sizes(cols, rows, format)
+    room = _empty(stream, at_t + (v_t + s_t + 16 if along_cols else 0), torch.uint8, x)
     q = Fp4Tensor._in_room(room, ws, v, s, rows, cols, format) if along_rows else None
     q_t = Fp4Tensor._in_room(room, at_t, v_t, s_t, cols, rows, format) if along_cols else None
-    code = lib().sbc_fp4_quantise(x.data_ptr(), DTYPE_CODES[x.dtype], rows, cols, _row_stride(x),
-                                  C.byref(q.desc) if q is not None else None,
-                                  C.byref(q_t.desc) if q_t is not None else None, room.data_ptr(), ws,
-                                  _cuda_stream(stream))
-    if code:
-        _check(code, "sbc_fp4_quantise")
+    rc = lib().sbc_fp4_quantise(x.data_ptr(), code, rows, cols, across, C.byref(q.desc) if along_rows else None,
+                                C.byref(q_t.desc) if along_cols else None, room.data_ptr(), ws, _cuda_stream(stream))
+    if rc:
+        _check(rc, "sbc_fp4_quantise")
     return q, q_t
 
 
@@ -708,15 +714,15 @@ def sbc_fp4_dequantise(q: Fp4Tensor, dtype: torch.dtype = torch.float32, out: Op
                        stream=None) -> torch.Tensor:
     """The values that q stands for (rows x cols)."""
     if out is None:
-        out = _empty(stream, (q.rows, q.cols), dtype, q.device)
-    _matrix(out, "out")
-    if tuple(out.shape) != (q.rows, q.cols):
+        out = _empty(stream, (q.rows, q.cols), dtype, q._any)
+    rows, cols, across, code = _matrix(out, "out")
+    if (rows, cols) != (q.rows, q.cols):
         raise ValueError(f"out must be {q.rows} x {q.cols}")
-    _beside(out, q._any, "out")
-    code = lib().sbc_fp4_dequantise(C.byref(q.desc), out.data_ptr(), DTYPE_CODES[out.dtype], _row_stride(out),
-                                    _cuda_stream(stream))
-    if code:
-        _check(code, "sbc_fp4_dequantise")
+    if q._device != out.get_device():
+        raise ValueError("out must be on the tensor's device")
+    rc = lib().sbc_fp4_dequantise(C.byref(q.desc), out.data_ptr(), code, across, _cuda_stream(stream))
+    if rc:
+        _check(rc, "sbc_fp4_dequantise")
     return out
 
 
@@ -727,16 +733,16 @@ def sbc_fp4_product(a: Fp4Tensor, b: Fp4Tensor, dtype: torch.dtype = torch.bfloa
     if a.format != b.format or a.cols != b.cols:
         raise ValueError(f"operands differ: {a.cols} columns of {a.format}, {b.cols} of {b.format}")
     if out is None:
-        out = _empty(stream, (a.rows, b.rows), dtype, a.device)
-    _matrix(out, "out")
-    if tuple(out.shape) != (a.rows, b.rows):
+        out = _empty(stream, (a.rows, b.rows), dtype, a._any)
+    rows, cols, across, code = _matrix(out, "out")
+    if (rows, cols) != (a.rows, b.rows):
         raise ValueError(f"out must be {a.rows} x {b.rows}")
-    if not out.get_device() == a._any.get_device() == b._any.get_device():
+    if not out.get_device() == a._device == b._device:
         raise ValueError("operands and result must be on one device")
-    code = lib().sbc_fp4_product(C.byref(a.desc), C.byref(b.desc), out.data_ptr(), DTYPE_CODES[out.dtype],
-                                 _row_stride(out), _status(status, out), _cuda_stream(stream))
-    if code:
-        _check(code, "sbc_fp4_product")
+    rc = lib().sbc_fp4_product(C.byref(a.desc), C.byref(b.desc), out.data_ptr(), code, across, _status(status, out),
+                               _cuda_stream(stream))
+    if rc:
+        _check(rc, "sbc_fp4_product")
     return out
 
 
@@ -747,16 +753,16 @@ def sbc_top_logits(logits: torch.Tensor, k: int, temperature: float = 1.0,
                    stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """(values float32 [rows, k], indices int32 [rows, k], rest float32 [rows]): every row's k largest
     logits in descending order and log sum exp(z / temperature) of all the others."""
-    _matrix(logits, "logits")
-    rows, cols = logits.shape
+    rows, cols, across, code = _matrix(logits, "logits")
     if not 1 <= k <= min(cols, TOP_MOST):
         raise ValueError(f"k must be in 1 .. {min(cols, TOP_MOST)}")
-    values = _empty(stream, (rows, k), torch.float32, logits.device)
-    indices = _empty(stream, (rows, k), torch.int32, logits.device)
-    rest = _empty(stream, (rows,), torch.float32, logits.device)
-    _check(lib().sbc_top_logits(logits.data_ptr(), DTYPE_CODES[logits.dtype], rows, cols, _row_stride(logits), k,
-                                float(temperature), values.data_ptr(), indices.data_ptr(), rest.data_ptr(),
-                                _cuda_stream(stream)), "sbc_top_logits")
+    values = _empty(stream, (rows, k), torch.float32, logits)
+    indices = _empty(stream, (rows, k), torch.int32, logits)
+    rest = _empty(stream, rows, torch.float32, logits)
+    rc = lib().sbc_top_logits(logits.data_ptr(), code, rows, cols, across, k, temperature, values.data_ptr(),
+                              indices.data_ptr(), rest.data_ptr(), _cuda_stream(stream))
+    if rc:
+        _check(rc, "sbc_top_logits")
     return values, indices, rest
 
 
@@ -771,33 +777,34 @@ def _rows_of(t: Optional[torch.Tensor], rows: int, dtype: torch.dtype, name: str
     return t.data_ptr()
 
 
-def _taught(logits, values, indices, rest, temperature, alpha, labels) -> DistillDesc:
-    _matrix(logits, "logits")
-    rows, cols = logits.shape
+def _taught(logits, values, indices, rest, temperature, alpha, labels):
+    """(rows, columns, elements between rows, type code, the teacher's side) of a loss's arguments."""
+    rows, cols, across, code = _matrix(logits, "logits")
     _dev_f32(values, "values")
     if not (indices.is_cuda and indices.dtype == torch.int32 and indices.is_contiguous()):
         raise TypeError("indices must be a contiguous int32 CUDA tensor")
-    if values.dim() != 2 or values.shape != indices.shape or values.shape[0] != rows:
+    shape = values.shape
+    if len(shape) != 2 or shape != indices.shape or shape[0] != rows:
         raise ValueError("values and indices must be rows x k")
     _beside(values, logits, "values")
     _beside(indices, logits, "indices")
-    if not 1 <= values.shape[1] <= DISTILL_MOST:
+    if not 1 <= shape[1] <= DISTILL_MOST:
         raise ValueError(f"k must be in 1 .. {DISTILL_MOST}")
     if not 1 <= cols <= DISTILL_COLS:
         raise ValueError(f"logits must have 1 .. {DISTILL_COLS} columns")
-    return DistillDesc(values.data_ptr(), indices.data_ptr(), _rows_of(rest, rows, torch.float32, "rest", logits),
-                       _rows_of(labels, rows, torch.int64, "labels", logits), values.shape[1], float(temperature),
-                       float(alpha), 0)
+    d = DistillDesc(values.data_ptr(), indices.data_ptr(), _rows_of(rest, rows, torch.float32, "rest", logits),
+                    _rows_of(labels, rows, torch.int64, "labels", logits), shape[1], temperature, alpha, 0)
+    return rows, cols, across, code, d
 
 
-def _grad_out(logits: torch.Tensor, out: Optional[torch.Tensor], stream) -> torch.Tensor:
+def _grad_out(logits: torch.Tensor, out: Optional[torch.Tensor], stream) -> Tuple[torch.Tensor, int]:
+    """(the gradient's buffer, elements between its rows)"""
     if out is None:
-        return _empty(stream, logits.shape, logits.dtype, logits.device)
-    _matrix(out, "out")
+        return _empty(stream, logits.shape, logits.dtype, logits), max(logits.shape[1], 1)
+    across = _matrix(out, "out")[2]
     if out.shape != logits.shape or out.dtype != logits.dtype:
         raise ValueError("out must have the logits' shape and type")
-    _beside(out, logits, "out")
-    return out
+    return out, across
 
 
 def sbc_distill_loss(logits: torch.Tensor, values: torch.Tensor, indices: torch.Tensor,
@@ -806,14 +813,13 @@ def sbc_distill_loss(logits: torch.Tensor, values: torch.Tensor, indices: torch.
                      stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(loss [rows], statistics for sbc_distill_grad): alpha temperature^2 KL(teacher || student) over the
     sent words and one outcome for all others, plus (1 - alpha) cross entropy of the labels."""
-    d = _taught(logits, values, indices, rest, temperature, alpha, labels)
-    rows, cols = logits.shape
-    loss = _empty(stream, (rows,), torch.float32, logits.device)
-    stats = _empty(stream, (rows, DISTILL_STATS), torch.float32, logits.device)
-    _check(lib().sbc_distill_loss(logits.data_ptr(), DTYPE_CODES[logits.dtype], rows, cols, _row_stride(logits),
-                                  C.byref(d), loss.data_ptr(), stats.data_ptr(),
-                                  _status(status, logits), _cuda_stream(stream)),
-           "sbc_distill_loss")
+    rows, cols, across, code, d = _taught(logits, values, indices, rest, temperature, alpha, labels)
+    loss = _empty(stream, rows, torch.float32, logits)
+    stats = _empty(stream, (rows, DISTILL_STATS), torch.float32, logits)
+    rc = lib().sbc_distill_loss(logits.data_ptr(), code, rows, cols, across, C.byref(d), loss.data_ptr(),
+                                stats.data_ptr(), _status(status, logits), _cuda_stream(stream))
+    if rc:
+        _check(rc, "sbc_distill_loss")
     return loss, stats
 
 
@@ -822,13 +828,14 @@ def sbc_distill_grad(logits: torch.Tensor, values: torch.Tensor, indices: torch.
                      temperature: float = 1.0, alpha: float = 1.0, labels: Optional[torch.Tensor] = None,
                      out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """grad_loss[r] * d loss[r] / d logits[r, :] in the logits' type; ``out`` may be the logits."""
-    d = _taught(logits, values, indices, rest, temperature, alpha, labels)
-    rows, cols = logits.shape
-    out = _grad_out(logits, out, stream)
-    _check(lib().sbc_distill_grad(logits.data_ptr(), DTYPE_CODES[logits.dtype], rows, cols, _row_stride(logits),
-                                  C.byref(d), _rows_of(stats, rows * DISTILL_STATS, torch.float32, "stats", logits),
-                                  _rows_of(grad_loss, rows, torch.float32, "grad_loss", logits), out.data_ptr(),
-                                  _row_stride(out), _cuda_stream(stream)), "sbc_distill_grad")
+    rows, cols, across, code, d = _taught(logits, values, indices, rest, temperature, alpha, labels)
+    out, out_across = _grad_out(logits, out, stream)
+    rc = lib().sbc_distill_grad(logits.data_ptr(), code, rows, cols, across, C.byref(d),
+                                _rows_of(stats, rows * DISTILL_STATS, torch.float32, "stats", logits),
+                                _rows_of(grad_loss, rows, torch.float32, "grad_loss", logits), out.data_ptr(),
+                                out_across, _cuda_stream(stream))
+    if rc:
+        _check(rc, "sbc_distill_grad")
     return out
 
 
@@ -838,13 +845,12 @@ def sbc_distill_loss_grad(logits: torch.Tensor, values: torch.Tensor, indices: t
                           out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
                           stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(loss [rows], its gradient times grad_loss) in one reading of the logits; ``out`` may be the logits."""
-    d = _taught(logits, values, indices, rest, temperature, alpha, labels)
-    rows, cols = logits.shape
-    out = _grad_out(logits, out, stream)
-    loss = _empty(stream, (rows,), torch.float32, logits.device)
-    _check(lib().sbc_distill_loss_grad(logits.data_ptr(), DTYPE_CODES[logits.dtype], rows, cols, _row_stride(logits),
-                                       C.byref(d), _rows_of(grad_loss, rows, torch.float32, "grad_loss", logits),
-                                       loss.data_ptr(), out.data_ptr(), _row_stride(out),
-                                       _status(status, logits), _cuda_stream(stream)),
-           "sbc_distill_loss_grad")
+    rows, cols, across, code, d = _taught(logits, values, indices, rest, temperature, alpha, labels)
+    out, out_across = _grad_out(logits, out, stream)
+    loss = _empty(stream, rows, torch.float32, logits)
+    rc = lib().sbc_distill_loss_grad(logits.data_ptr(), code, rows, cols, across, C.byref(d),
+                                     _rows_of(grad_loss, rows, torch.float32, "grad_loss", logits), loss.data_ptr(),
+                                     out.data_ptr(), out_across, _status(status, logits), _cuda_stream(stream))
+    if rc:
+        _check(rc, "sbc_distill_loss_grad")
     return loss, out
