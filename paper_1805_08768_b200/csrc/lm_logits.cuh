@@ -577,18 +577,27 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
             });
         }
     }
+    if (GRAD) __syncthreads();   // the sent words' gradients come after all others'
     const bool live = sh.missing == 1.f;
     float kl = 0.f;
-    if (live)
-        for (int i = t; i < a.k; i += threads) {
-            if (sent_at[i] < 0) continue;
-            const float p = exp2_fast((__fmul_rn(sent_t[i], inv) - r.high) * kLog2e) * sh.inv_total;
-            const float q = exp2_fast((sent_z[i] - r.top) * c) * sh.inv_whole;
-            kl += term(p, q, (sent_t[i] - sent_z[i]) * inv - sh.shift);
+    bool has_label = false;
+    for (int i = t; i < a.k; i += threads) {
+        const int at = sent_at[i];
+        if (at < 0) continue;
+        const float zv = sent_z[i], tv = sent_t[i];
+        if (live) {
+            const float p = exp2_fast((__fmul_rn(tv, inv) - r.high) * kLog2e) * sh.inv_total;
+            const float q = exp2_fast((zv - r.top) * c) * sh.inv_whole;
+            kl += term(p, q, (tv - zv) * inv - sh.shift);
         }
+        if (GRAD) {
+            has_label |= at == label;
+            out[at - first] = from_float<T>(slope.sent(zv, tv, at == label));
+        }
+    }
     kl = warp_sum(kl);
     if (lane == 0) sh.kl[warp] = kl;
-    __syncthreads();
+    has_label = __syncthreads_or(has_label);
     if (size > 1) {
         if (t == 0) {
             kl = 0.f;
@@ -604,7 +613,8 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
         if (lane == 0) a.loss[row] = (live ? a.alpha * a.temperature * a.temperature * (kl + sh.rest_term) : sh.missing) + sh.cross;
     }
     if (late && a.status) atomicOr(a.status, SBC_STATUS_TIMEOUT);
-    if (GRAD) write_sent(out, slope, first, n, a.k, sent_at, sent_t, sent_z, label, label_z);
+    if (GRAD && t == 0 && label >= first && label < first + n && !has_label && slope.ce != 0.f)
+        out[label - first] = from_float<T>(slope.unsent_label(label_z));
     if (size > 1) cluster_sync();   // blocks read each other's sums up to here
 }
 
@@ -902,7 +912,7 @@ __device__ __forceinline__ Mass<false> gather_top(const Source<T, HELD>& src, in
     const Cut<T>& cut = src.cut;
     const float low = !PLAIN && threshold == 0 ? -infinity() : key_value((uint32_t)(threshold >> 32));
     GranMax<T, true> top;
-    float top_left = -infinity();   // of granules that hold a candidate: what is left
+    float top_left = -infinity();   // of granules that hold a candidate, where they are not held: what is left
     const int threads = blockDim.x;
     // (all lanes of a warp go around together: apart, each would take its own turns)
     for (int gw = threadIdx.x & ~31; gw < cut.grans; gw += 32 * threads) {
@@ -936,8 +946,10 @@ __device__ __forceinline__ Mass<false> gather_top(const Source<T, HELD>& src, in
                 hits |= hit ? 1u << j : 0u;
             }
             if (!any) hits = 0;
+            if (!HELD) {
 #pragma unroll
-            for (int j = 0; j < E; ++j) top_left = any && !(hits >> j & 1) ? fmaxf(top_left, x[j]) : top_left;
+                for (int j = 0; j < E; ++j) top_left = any && !(hits >> j & 1) ? fmaxf(top_left, x[j]) : top_left;
+            }
             uint32_t at = 0;
             if (hits) at = add_shared(&sh.count, (uint32_t)__popc(hits));
             __syncwarp();
@@ -952,6 +964,7 @@ __device__ __forceinline__ Mass<false> gather_top(const Source<T, HELD>& src, in
                 hits &= hits - 1;
                 __syncwarp();
             }
+            if (HELD && any) top.add(src.get(g));
         }
     }
     Mass<false> mass;
