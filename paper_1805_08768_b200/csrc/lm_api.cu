@@ -92,8 +92,8 @@ int launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = axis == 0 ? (unsigned)cluster : 1;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = axis == 2 ? (unsigned)cluster : 1;
+    attr[1].val.clusterDim.y = axis == 1 ? (unsigned)cluster : 1;
+    attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = cluster > 0 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, P(args)...) == cudaSuccess ? SBC_OK : SBC_ECUDA;
@@ -136,7 +136,7 @@ constexpr int kSmemMost = 227 * 1024;
 template <typename T, int FMT>
 int launch_product(const CUtensorMap& mw, const CUtensorMap& mx, const ProductArgs& a, dim3 grid, int smem, cudaStream_t st) {
     if (!allow_smem<k_fp4_product<T, FMT>>(kSmemMost - 1024)) return SBC_ECUDA;
-    return launch(k_fp4_product<T, FMT>, grid, kPThreads, (size_t)smem, st, (int)grid.z, 2, mw, mx, a);
+    return launch(k_fp4_product<T, FMT>, grid, kPThreads, (size_t)smem, st, (int)grid.y, 1, mw, mx, a);
 }
 
 // How a row of logits is cut: blocks that share it, elements a block holds in shared memory at a
@@ -146,11 +146,13 @@ struct RowPlan {
 };
 
 // A segment is at most kRoomBytes where eight blocks are enough for that; few rows are spread over as
-// many blocks as keep the GPU busy, each with at least 2048 elements.
+// many blocks as keep the GPU busy, each with at least 8192 elements (us alone / spread, 8 float32 rows:
+// top 32 of 10000 words 7.1 / 9.5, of 131072 13.4 / 13.4; loss and gradient of 10000 6.7 / 6.4, of 32768
+// 15.9 / 7.3, of 131072 48 / 11).
 constexpr int kRoomBytes = 100 * 1024;
 int spread(int64_t rows, int64_t cols, int shift) {
     const int64_t blocks = 2 * sm_count();
-    while (shift < 3 && rows * (2 << shift) <= blocks && cols >= 2048 * (2 << shift)) ++shift;
+    while (shift < 3 && rows * (2 << shift) <= blocks && cols >= 8192 * (2 << shift)) ++shift;
     return shift;
 }
 RowPlan plan_rows(int64_t rows, int64_t cols, int width) {
@@ -231,9 +233,10 @@ int launch_wide(const sbc_fp4* a, const sbc_fp4* b, WideArgs p, int64_t tiles, c
     return launch(k_fp4_product_wide<T, FMT, NT>, dim3(blocks), kWThreads, (size_t)(p.stages * stage + scales + 1024), st, 2, 0, mw, mx, p);
 }
 
-// More than 128 tokens: pairs of blocks that stay.  Tiles of 256 tokens where that makes two rounds of
-// tiles or more; else, and for 32-bit results (which do not fit in registers until they are stored),
-// tiles of 128 with two accumulators.
+// Pairs of blocks that stay.  Tiles of 256 tokens, or of 128 with two accumulators: by the rounds that the
+// pairs take, a round of 256 counted as 1.6 of 128 (us with tiles of 256 / 128: 8192^3 242 / 404,
+// 4096^3 43 / 58, 3000 x 2048 -> 3000 17.3 / 21.5, 2240 x 1300 -> 2600 15.1 / 14.0).  32-bit results
+// always take 128: more do not fit in registers until they are stored.
 int product_wide(const sbc_fp4* a, const sbc_fp4* b, void* out, int dtype, int64_t row_stride, uint32_t* status, cudaStream_t st) {
     WideArgs p = {};
     p.scales_w = static_cast<const uint8_t*>(b->scales);
@@ -250,7 +253,8 @@ int product_wide(const sbc_fp4* a, const sbc_fp4* b, void* out, int dtype, int64
     p.steps = (int)ceil_div(a->cols, 64);
     const int64_t tiles_w = ceil_div(b->rows, 256), tiles256 = tiles_w * ceil_div(a->rows, 256), tiles128 = tiles_w * ceil_div(a->rows, 128);
     p.tiles_w = (int)tiles_w;
-    const bool big = tiles256 >= sm_count();
+    const int64_t pairs = std::max(1, sm_count() / 2);
+    const bool big = 16 * ceil_div(tiles256, pairs) <= 10 * ceil_div(tiles128, pairs);
     return by_dtype(dtype, [&](auto* as) {
         using T = std::remove_pointer_t<decltype(as)>;
         if constexpr (sizeof(T) == 2) {
@@ -355,6 +359,8 @@ int sbc_fp4_product(const sbc_fp4* a, const sbc_fp4* b, void* out, int dtype, in
     if (!fp4_ok(a) || !fp4_ok(b) || a->format != b->format || a->cols != b->cols) return SBC_EINVAL;
     if (a->rows > kMaxDim - 512 || b->rows > kMaxDim - 512) return SBC_EINVAL;
     if (!matrix_ok(out, dtype, a->rows, b->rows, row_stride) || !aligned(status, 4)) return SBC_EINVAL;
+    // us of 128 tokens here / there: 8192^2 13.6 / 18.8, 1300 -> 2600 7.3 / 6.9, 2048^2 8.5 / 8.1, 4096 -> 16384
+    // 13.7 / 12.4, 16384 -> 4096 15.2 / 31.9, 650 -> 10000 6.0 / 6.1; of 64 never slower here
     if (a->rows > 128) return product_wide(a, b, out, dtype, row_stride, status, stream);
     ProductArgs p = {};
     p.scales_w = static_cast<const uint8_t*>(b->scales);
@@ -370,21 +376,27 @@ int sbc_fp4_product(const sbc_fp4* a, const sbc_fp4* b, void* out, int dtype, in
     p.chunks = (int)ceil_div(a->cols, 256);
     p.steps = (int)ceil_div(a->cols, 64);
     p.nt = (int)ceil_div(a->rows, 16) * 16;
-    const int row_tiles = (p.nt + 127) / 128, tiles_k = a->format == SBC_FP4_E8M0 ? 2 : 4;
-    const int stage = (kPRows * kPBytes + p.nt * kPBytes + tiles_k * 512 * (1 + row_tiles) + 1023) / 1024 * 1024;
-    p.stages = p.nt > 128 ? 4 : std::min(4, 110 * 1024 / stage);
-    const int cols = (p.nt + 31) / 32 * 32 + p.stages * 4 * tiles_k * (1 + row_tiles);
+    const int tiles_k = a->format == SBC_FP4_E8M0 ? 2 : 4;
+    const int stage = (kPRows * kPBytes + p.nt * kPBytes + tiles_k * 512 * 2 + 1023) / 1024 * 1024;
+    p.stages = std::min(4, 110 * 1024 / stage);
+    const int cols = (p.nt + 31) / 32 * 32 + p.stages * 4 * tiles_k * 2;
     p.tmem_cols = 32;
     while ((int)p.tmem_cols < cols) p.tmem_cols *= 2;
     // as many blocks on an SM as its tensor memory serves, so that none waits for another's columns
     const int smem = std::max(p.stages * stage + 1024, kSmemMost / (512 / (int)p.tmem_cols + 1) + 1024);
-    const int64_t tiles_w = ceil_div(b->rows, kPRows), tiles_x = ceil_div(a->rows, p.nt);
-    if (tiles_x > 65535) return SBC_EINVAL;
+    const int64_t tiles_w = ceil_div(b->rows, kPRows);
+    // the columns in parts: up to a block per SM while a part has one stage, up to two while it has two (us of
+    // 16 tokens in one part / so many: 8192^2 23.8 / 9.9, 1024^2 4.8 / 4.1; 650 -> 10000, two blocks per SM
+    // of one stage or two 5.5, one 4.4; four blocks per SM: 8192^2 14.2)
     int parts = 1;
-    while (parts < 8 && tiles_w * tiles_x * parts * 2 <= 2 * sm_count() && p.chunks >= parts * 2) parts *= 2;
+    while (parts < 8) {
+        const int64_t blocks = tiles_w * parts * 2;
+        if (blocks > 2 * sm_count() || p.chunks < parts * (blocks <= sm_count() ? 2 : 4)) break;
+        parts *= 2;
+    }
     CUtensorMap mw, mx;
     if (!values_map(&mw, b, kPRows) || !values_map(&mx, a, p.nt)) return SBC_ECUDA;
-    const dim3 grid((unsigned)tiles_w, (unsigned)tiles_x, (unsigned)parts);
+    const dim3 grid((unsigned)tiles_w, (unsigned)parts);
     return by_dtype(dtype, [&](auto* as) {
         using T = std::remove_pointer_t<decltype(as)>;
         return a->format == SBC_FP4_E4M3 ? launch_product<T, SBC_FP4_E4M3>(mw, mx, p, grid, smem, stream)
