@@ -167,6 +167,11 @@ RowPlan plan_rows(int64_t rows, int64_t cols, int width) {
     return p;
 }
 
+// Candidates that a block of k_top_logits has room for, where `size` blocks share a row.  In whole eights:
+// the row that the block holds lies behind the two lists and starts at a multiple of 16 bytes.
+constexpr int candidate_room(int k, int size) { return (std::max(std::max(512, 4 * k), k * size) + 7) / 8 * 8; }
+static_assert(8 * kCandidateBytes % 16 == 0 && kStreamRoom % 8 == 0, "what lies behind the lists is read 16 bytes at a time");
+
 // Beyond these the scaled logits would leave 32 bits.
 bool temperature_ok(float t) { return t >= 1e-6f && t <= 1e6f; }
 
@@ -420,17 +425,17 @@ int sbc_top_logits(const void* logits, int dtype, int64_t rows, int64_t cols, in
         // (65536: 133 and 132, 32000: 84 and 59)
         if (rows >= sm_count() && cols * (int64_t)sizeof(T) > 2 * kRoomBytes) {
             a.room = kStreamRoom;
-            return launch(k_top_stream<T>, dim3((unsigned)rows), kStreamThreads, 2 * kStreamBytes + (size_t)a.room * 10, stream, 0, 0, a);
+            return launch(k_top_stream<T>, dim3((unsigned)rows), kStreamThreads, 2 * kStreamBytes + (size_t)a.room * kCandidateBytes, stream, 0, 0, a);
         }
         // enough groups of elements that the k-th largest of their maxima bounds tightly: two a thread, four times k
         const int threads = std::max(p.threads, std::min(kTopThreads, (int)ceil_div(2 * k, 32 * p.size) * 32));
-        a.room = std::max(std::max(512, 4 * k), k * p.size);
-        const size_t lists = (size_t)a.room * 10;
+        a.room = candidate_room(k, p.size);
+        const size_t lists = (size_t)a.room * kCandidateBytes;
         const dim3 grid((unsigned)(rows * p.size));
         if (ceil_div(ceil_div(cols, 64), p.size) * 64 > p.room) {   // too long to be held
             return launch(k_top_logits<T, false>, grid, kTopThreads, lists, stream, p.size, 0, a);
         }
-        if (!allow_smem<k_top_logits<T, true>>(kRoomBytes + 32 + 2048 * 10)) return (int)SBC_ECUDA;
+        if (!allow_smem<k_top_logits<T, true>>(kRoomBytes + 32 + candidate_room(SBC_TOP_MOST, 8) * kCandidateBytes)) return (int)SBC_ECUDA;
         return launch(k_top_logits<T, true>, grid, threads, lists + (size_t)p.room * sizeof(T) + 32, stream, p.size, 0, a);
     });
 }

@@ -672,7 +672,7 @@ struct TopArgs {
     long long rows, stride;
     int cols, k;
     int shift;                 // 2^shift blocks share a row
-    int room;                  // candidates a block can hold: at least 2 k, and k for every block of a row
+    int room;                  // candidates a block can hold: at least 2 k, and k for every block of a row; whole eights
     float temperature;
     float* values;
     int32_t* indices;
@@ -714,6 +714,7 @@ struct TopShared {
 };
 // What a block gathers, behind the logits it holds: larger value first, then lower index.  A candidate is
 // stored as its value's bits and its index, and becomes a composite when it is ranked.
+constexpr int kCandidateBytes = 8 + 2;   // in the list and in its order
 struct Candidates {
     unsigned long long* at;
     uint16_t* order;           // by bin

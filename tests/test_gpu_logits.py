@@ -71,6 +71,14 @@ def test_top_logits(rows, cols, k, dtype):
     check_top(logits(rows, cols, dtype, rows + cols), k, 1.0 if cols % 2 else 2.5)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows,cols", [(3, 300), (2, 1000), (300, 10000), (3, 20000), (3, 40000), (1, 131072), (150, 110003)])
+@pytest.mark.parametrize("k", [127, 129, 131, 201, 255])
+def test_top_logits_of_odd_counts(rows, cols, k, dtype):
+    """Lists of any length in front of the row that a block holds: one, two, four and eight blocks a row, and streamed."""
+    check_top(logits(rows, cols, dtype, rows + k), k, 1.5)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("rows,cols,k", [(3, 40, 7), (2, 700, 64), (1, 10000, 64), (320, 10000, 200), (2, 40000, 256), (148, 104003, 100)])
 @pytest.mark.parametrize("kind", ["equal", "zeros", "few_values", "masked", "nearly_all_masked", "empty", "steps", "huge", "nan"])
