@@ -415,11 +415,14 @@ template <typename T, int FMT, bool SHIFT> __global__ void __launch_bounds__(kQT
         const int left = (int)min(a.cols - first, (long long)kPiece + E);
         const int most = SHIFT ? __shfl_sync(0xffffffffu, left, 0) : left;   // lane 0 has most
         if (most <= 0) continue;
-        const int e0 = (int)first, end = (int)a.cols - 1;
+        // positions are counted from the granule that the row starts in (32 bits without a sign: a row may have 2^31 - 1
+        // elements, and a piece goes on behind them); element e of the row is at e + phase
+        const uint32_t p0 = (uint32_t)(first + phase), end = (uint32_t)a.cols - 1;
+        const auto element = [&](uint32_t p) { return max(p, (uint32_t)phase) - (uint32_t)phase; };   // the first one at or behind p
         const uint8_t* const values = a.values + r * a.pitch;
         const uint8_t* const scales = a.scales + r / 128 * a.ktiles * 512 + (r % 32) * 16 + (r % 128 / 32) * 4;
         const auto code_of = [&](uint32_t e) { return (uint32_t)scales[(size_t)(e / (4 * kB)) * 512 + e / kB % 4]; };
-        T* const to = row + e0;
+        T* const to = row + first;
         constexpr int kGrans = kPiece / (32 * E);
 #pragma unroll
         for (int g0 = 0; g0 < kGrans; g0 += kAhead) {
@@ -430,20 +433,20 @@ template <typename T, int FMT, bool SHIFT> __global__ void __launch_bounds__(kQT
                 if ((SHIFT ? most : left) <= at) break;
                 if (SHIFT) {
                     // what follows a lane's word and block is the next lane's
-                    const uint32_t f = (uint32_t)min(max(e0 + at, 0), end);
+                    const uint32_t f = min(element(p0 + at), end);
                     lo[g] = reinterpret_cast<const uint32_t*>(values)[f / 8];
                     c0[g] = code_of(f);
                     hi[g] = c1[g] = 0;
                     if (lane == 31) {
-                        const uint32_t next = (uint32_t)min((int)f + E, end);
+                        const uint32_t next = min(f + E, end);
                         hi[g] = reinterpret_cast<const uint32_t*>(values)[next / 8];
                         c1[g] = code_of(next);
                     }
                 } else {
                     // (a step of 32 granules is whole scale tiles, or half of one for 32 x 4 elements of 32-element blocks)
-                    if (E == 8) lo[g] = *reinterpret_cast<const uint32_t*>(values + (uint32_t)(e0 + at) / 2);
-                    if (E == 4) lo[g] = *reinterpret_cast<const uint16_t*>(values + (uint32_t)(e0 + at) / 2);
-                    c0[g] = code_of((uint32_t)(e0 + at));
+                    if (E == 8) lo[g] = *reinterpret_cast<const uint32_t*>(values + (p0 + at) / 2);
+                    if (E == 4) lo[g] = *reinterpret_cast<const uint16_t*>(values + (p0 + at) / 2);
+                    c0[g] = code_of(p0 + at);
                 }
             }
 #pragma unroll
@@ -461,8 +464,8 @@ template <typename T, int FMT, bool SHIFT> __global__ void __launch_bounds__(kQT
                 T* v = reinterpret_cast<T*>(&q);
                 int skip = 0;
                 if (SHIFT) {
-                    const uint32_t f = (uint32_t)max(e0 + at, 0);
-                    skip = (int)f - (e0 + at);
+                    const uint32_t f = element(p0 + at);
+                    skip = (int)(f + (uint32_t)phase - (p0 + at));
                     grid_values<E>(x, __funnelshift_r(lo[g], hi[g], 4 * (f & 7u)));
                     const float s1 = scale_value<FMT>(c1[g]) * tensor;
                     const int split = kB - (int)(f % kB);   // elements of the granule that belong to the first block

@@ -316,3 +316,26 @@ def test_calls_in_a_graph():
         x.copy_(values(200, 650, torch.bfloat16, seed))
         graph.replay()
         assert torch.equal(y, sbc.sbc_fp4_product(sbc.sbc_fp4_quantise(x, "e4m3"), w4, torch.float32))
+
+
+@pytest.mark.parametrize("fmt", ["e8m0", "e4m3"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_row_of_the_largest_length(dtype, fmt):
+    """2^31 - 1 columns, the largest a header's matrix has, expanded to rows at every kind of offset: its
+    last blocks come out as those of a short row."""
+    cols, tail = 2 ** 31 - 1, 32 * 20 - 1
+    x = torch.ones(1, cols, dtype=dtype, device=DEV)
+    x[0, -tail:] = values(1, tail, dtype, 6)[0].clamp(-64, 64)
+    x[0, -1] = 448.0
+    q = sbc.sbc_fp4_quantise(x, fmt)
+    short = plain_round(x[:, -tail - 64:], fmt)       # holds the tensor's largest, so its tensor scale
+    one, want = short[:, :64].to(dtype), short[:, 64:]
+    del x
+    room = torch.empty(cols + 16, dtype=dtype, device=DEV)
+    for offset in (0, 1, 16 // dtype.itemsize - 1):
+        room.fill_(7.0)
+        out = room[offset:offset + cols].view(1, cols)
+        sbc.sbc_fp4_dequantise(q, out=out)
+        assert same(out[:, -tail:], want)
+        assert torch.equal(out[:, :64], one) and bool((out[:, :-tail:2 ** 20 + 1] == one[0, 0]).all())
+        assert bool((room[:offset] == 7).all()) and bool((room[offset + cols:] == 7).all())
