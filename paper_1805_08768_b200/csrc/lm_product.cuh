@@ -38,6 +38,24 @@ template <int FMT> struct ProductShape {
         (1u << 7) | (1u << 10) | (FMT == SBC_FP4_E8M0 ? 1u << 23 : 0u) | (1u << 27);
 };
 
+// The two tensor scales, applied to a sum.  Their product may leave 32 bits (2^-252 .. 2^234) where the result does
+// not, so the sum meets one after the other, the larger first: two small ones then round once, since a sum
+// is 0 or at least 2^-20 (grid values 0.5, block scales 2^-9), and two large ones leave 32 bits only if the result does.
+template <int FMT> struct ResultScale {
+    float first = 1.f, second = 1.f;
+    __device__ __forceinline__ ResultScale(const float* tensor_w, const float* tensor_x) {
+        if (FMT == SBC_FP4_E4M3) {
+            const float w = *tensor_w, x = *tensor_x;
+            const bool larger = fabsf(w) > fabsf(x);
+            first = larger ? w : x, second = larger ? x : w;
+        }
+    }
+    __device__ __forceinline__ float of(float sum) const {
+        const float v = __fmul_rn(sum, first);
+        return FMT == SBC_FP4_E4M3 ? __fmul_rn(v, second) : v;
+    }
+};
+
 // A place in the ring of stages and the parity its barriers have there (no divisions: every role goes
 // around it with one thread, whose own latency would otherwise be what a stage costs).
 struct Ring {
@@ -201,7 +219,7 @@ __global__ void __launch_bounds__(kPThreads) k_fp4_product(const __grid_constant
     if (bad && t == 0 && a.status) atomicOr(a.status, SBC_STATUS_TIMEOUT);
     const float nan = __uint_as_float(0x7fffffffu);
     T* out = static_cast<T*>(a.out);
-    const float scale = FMT == SBC_FP4_E4M3 ? *a.tensor_w * *a.tensor_x : 1.f;
+    const ResultScale<FMT> scale(a.tensor_w, a.tensor_x);
     const int tokens = (int)a.rows_x;
     const long long j = w0 + warp * 32 + lane;
     if (parts == 1) {
@@ -214,7 +232,7 @@ __global__ void __launch_bounds__(kPThreads) k_fp4_product(const __grid_constant
                 tmem_load16(v, tmem + ((uint32_t)warp << 21) + n0);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    if (n0 + i < most) *to = from_float<T>(bad ? nan : v[i] * scale);
+                    if (n0 + i < most) *to = from_float<T>(bad ? nan : scale.of(v[i]));
                     to += a.stride;
                 }
             }
@@ -246,8 +264,8 @@ __global__ void __launch_bounds__(kPThreads) k_fp4_product(const __grid_constant
                 if (p < parts) sum.x += v[p].x, sum.y += v[p].y, sum.z += v[p].z, sum.w += v[p].w;
             const long long w = w0 + i % 32 * 4;
             T* to = out + i / 32 * a.stride + w;
-            alignas(16) const T four[4] = {from_float<T>(sum.x * scale), from_float<T>(sum.y * scale), from_float<T>(sum.z * scale),
-                                           from_float<T>(sum.w * scale)};
+            alignas(16) const T four[4] = {from_float<T>(scale.of(sum.x)), from_float<T>(scale.of(sum.y)), from_float<T>(scale.of(sum.z)),
+                                           from_float<T>(scale.of(sum.w))};
             if (wide && w + 4 <= a.rows_w) {
                 if constexpr (sizeof(T) == 2)
                     *reinterpret_cast<uint2*>(to) = *reinterpret_cast<const uint2*>(four);
@@ -365,8 +383,8 @@ __device__ __forceinline__ void store_word(void* p, uint32_t v) { asm volatile("
 // one another (volatile: their addresses would otherwise all be formed in front).
 // PAIRS: 16-bit results whose even places are 4-byte aligned.  Neighbouring lanes swap halves, so that
 // one has two weights of a token and the other the same two of the next.
-template <typename T, int COLS, bool PAIRS, typename F>
-__device__ __forceinline__ void store_tile(uint32_t acc, T* out, long long stride, int tokens, bool mine, float by, F free) {
+template <typename T, int FMT, int COLS, bool PAIRS, typename F>
+__device__ __forceinline__ void store_tile(uint32_t acc, T* out, long long stride, int tokens, bool mine, const ResultScale<FMT>& scale, F free) {
     if constexpr (sizeof(T) == 2) {
         uint32_t w[COLS / 2];
 #pragma unroll
@@ -374,7 +392,7 @@ __device__ __forceinline__ void store_tile(uint32_t acc, T* out, long long strid
             float v[32];
             tmem_load32(v, acc + n0);
 #pragma unroll
-            for (int i = 0; i < 32; i += 2) w[(n0 + i) / 2] = pack2(v[i] * by, v[i + 1] * by, (const T*)nullptr);
+            for (int i = 0; i < 32; i += 2) w[(n0 + i) / 2] = pack2(scale.of(v[i]), scale.of(v[i + 1]), (const T*)nullptr);
         }
         free();
         if (PAIRS) {
@@ -403,7 +421,7 @@ __device__ __forceinline__ void store_tile(uint32_t acc, T* out, long long strid
         const int most = mine ? tokens : 0;
 #pragma unroll
         for (int n = 0; n < COLS; ++n) {
-            if (n < most) store_word(out, __float_as_uint(v[n] * by));
+            if (n < most) store_word(out, __float_as_uint(scale.of(v[n])));
             out += stride;
         }
     }
@@ -602,7 +620,7 @@ __global__ void __launch_bounds__(kWThreads, 1)
         if (!ok) gave_up = 1;
     } else if (warp < 4 || warp >= 12) {
         bool ok = true;
-        const float scale = FMT == SBC_FP4_E4M3 ? *a.tensor_w * *a.tensor_x : 1.f;
+        ResultScale<FMT> scale(a.tensor_w, a.tensor_x);
         constexpr int kCols = NT / 2;
         const int col0 = warp < 4 ? 0 : kCols, sub = warp & 3;
         const bool pairs_ok = sizeof(T) == 2 && ((a.stride | a.rows_w) & 1) == 0 && ((uintptr_t)a.out & 3) == 0;
@@ -615,16 +633,16 @@ __global__ void __launch_bounds__(kWThreads, 1)
             const uint32_t acc = tmem + (uint32_t)b * 128u + (uint32_t)col0 + ((uint32_t)sub << 21);
             T* out = static_cast<T*>(a.out) + x0 * a.stride + j;
             const int tokens = (int)min((long long)kCols, a.rows_x - x0);
-            const float by = ok ? scale : __uint_as_float(0x7fffffffu);
+            if (!ok) scale.first = __uint_as_float(0x7fffffffu);
             const auto free = [&] {
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive_remote(map_rank(acc_empty(b), 0));
             };
             if (pairs_ok)
-                store_tile<T, kCols, true>(acc, out, a.stride, tokens, j < a.rows_w, by, free);
+                store_tile<T, FMT, kCols, true>(acc, out, a.stride, tokens, j < a.rows_w, scale, free);
             else
-                store_tile<T, kCols, false>(acc, out, a.stride, tokens, j < a.rows_w, by, free);
+                store_tile<T, FMT, kCols, false>(acc, out, a.stride, tokens, j < a.rows_w, scale, free);
             __syncwarp();
         }
         if (!ok) gave_up = 1;

@@ -339,3 +339,40 @@ def test_a_row_of_the_largest_length(dtype, fmt):
         assert same(out[:, -tail:], want)
         assert torch.equal(out[:, :64], one) and bool((out[:, :-tail:2 ** 20 + 1] == one[0, 0]).all())
         assert bool((room[:offset] == 7).all()) and bool((room[offset + cols:] == 7).all())
+
+
+SMALLEST = {torch.float32: 2.0 ** -149, torch.bfloat16: 2.0 ** -133}
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tokens,inner,outer", [(1, 650, 300), (16, 8192, 300), (128, 300, 131), (129, 70, 130), (300, 4096, 300)])
+@pytest.mark.parametrize("size_a,size_b", [(1e-20, 1e-20), (1e-21, 3e-18), (1e-30, 1e-10), (1e-36, 1.0), (1e-30, 1e25), (1e25, 1e-35), (1e18, 1e17),
+                                           (1e30, 1e5)])
+def test_product_of_tensor_scales_beyond_32_bits(size_a, size_b, tokens, inner, outer, dtype):
+    """Tensor scales whose product alone is below the smallest or above the largest number; the result counts.
+    Tolerance as above, and half of the smallest number for results that are not normal ones."""
+    a = sbc.sbc_fp4_quantise(torch.randn(tokens, inner, generator=torch.Generator(device=DEV).manual_seed(5), device=DEV) * size_a, "e4m3")
+    b = sbc.sbc_fp4_quantise(torch.randn(outer, inner, generator=torch.Generator(device=DEV).manual_seed(6), device=DEV) * size_b, "e4m3")
+    want, size = plain_product(a, b)
+    got = sbc.sbc_fp4_product(a, b, dtype)
+    allowed = (math.ceil(inner / 64) + 4) * 2.0 ** -22 * size + ROUND[dtype] * want.abs() + SMALLEST[dtype] / 2
+    assert bool(((got.double() - want).abs() <= allowed).all())
+    assert bool(torch.isfinite(got).all()) and bool((got != 0).any())
+
+
+@pytest.mark.parametrize("tokens", [3, 40, 300])
+def test_huge_tensor_scales_and_rows_of_zeros(tokens):
+    """One value near the type's largest on each side fixes the tensor scales; rows of zeros stay zeros, and so do
+    products of rows that the scale rounds to zero."""
+    x, w = torch.zeros(tokens, 200, device=DEV), torch.zeros(150, 200, device=DEV)
+    x[1, 7], w[70, 9] = 2e38, -3e38                  # in different places: their product with everything is 0
+    x[2, 100], w[3, 100] = 1.0, 1.0                  # far below the smallest block scale
+    a, b = sbc.sbc_fp4_quantise(x, "e4m3"), sbc.sbc_fp4_quantise(w, "e4m3")
+    assert float(a.tensor_scale) * float(b.tensor_scale) > 2.0 ** 200
+    for dtype in (torch.float32, torch.bfloat16):
+        assert not bool(sbc.sbc_fp4_product(a, b, dtype).any())
+    x[1, 9] = 2e38                                   # now one result is beyond the largest number, the others are not
+    got = sbc.sbc_fp4_product(sbc.sbc_fp4_quantise(x, "e4m3"), b, torch.float32)
+    assert float(got[1, 70]) == -math.inf
+    got[1, 70] = 0
+    assert not bool(got.any())
