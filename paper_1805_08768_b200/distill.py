@@ -6,7 +6,8 @@ teacher's knowledge arrives as the k largest logits of every position and the ma
 and the gradients that the loss against them gives are what the client's weight update is made of.
 
 Everything that computes is the CUDA library's (``binding.sbc_fp4_*``, ``sbc_top_logits``,
-``sbc_distill_*``); this module puts it behind torch's autograd and moves arguments.
+``sbc_distill_*``); this module puts it behind torch's autograd and moves arguments.  Gradients are
+first ones: differentiating them again raises.
 ``ToyDistillation`` is a small seeded model that runs all of it inside ``DelayedSGD``.
 """
 from __future__ import annotations
@@ -35,24 +36,42 @@ def teach(logits: torch.Tensor, k: int, temperature: float = 1.0) -> TeacherMess
     return TeacherMessage(*binding.sbc_top_logits(logits, k, temperature), temperature)
 
 
+class _FirstOnly(torch.autograd.Function):
+    """A gradient as it is, tied to what it was made of: differentiating it again raises.  (Kernels leave no
+    trace, so without the tie it would pass for a constant, and only this part of a sum would be lost.)"""
+
+    @staticmethod
+    def forward(ctx, grad, *sources):
+        return grad.view_as(grad)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("fp4_linear and distill_loss have no second derivatives")
+
+
+def _first_only(grad, *sources):
+    """The tie is needed only where a graph of the gradients is asked for."""
+    return _FirstOnly.apply(grad, *sources) if grad is not None and torch.is_grad_enabled() else grad
+
+
 class _DistillLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, values, indices, rest, temperature, alpha, labels):
-        logits = logits.detach()
-        if logits.stride(-1) != 1:
-            logits = logits.contiguous()
-        loss, stats = binding.sbc_distill_loss(logits, values, indices, rest, temperature, alpha, labels)
-        ctx.save_for_backward(logits, values, indices, rest, labels, stats)
+        flat = logits.detach()
+        if flat.stride(-1) != 1:
+            flat = flat.contiguous()
+        loss, stats = binding.sbc_distill_loss(flat, values, indices, rest, temperature, alpha, labels)
+        ctx.save_for_backward(logits, flat, values, indices, rest, labels, stats)
         ctx.about = (temperature, alpha)
         return loss
 
     @staticmethod
     def backward(ctx, grad_loss):
-        logits, values, indices, rest, labels, stats = ctx.saved_tensors
+        logits, flat, values, indices, rest, labels, stats = ctx.saved_tensors
         temperature, alpha = ctx.about
-        grad = binding.sbc_distill_grad(logits, values, indices, stats, grad_loss.float().contiguous(), rest,
+        grad = binding.sbc_distill_grad(flat, values, indices, stats, grad_loss.float().contiguous(), rest,
                                         temperature, alpha, labels)
-        return grad, None, None, None, None, None, None
+        return _first_only(grad, logits, grad_loss), None, None, None, None, None, None
 
 
 def distill_loss(logits: torch.Tensor, message: TeacherMessage, alpha: float = 1.0,
@@ -64,10 +83,11 @@ def distill_loss(logits: torch.Tensor, message: TeacherMessage, alpha: float = 1
 
 class _Fp4Linear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w, format):
+    def forward(ctx, x, w, format, tie):
         flat = x.detach().reshape(-1, x.shape[-1])
         need_x, need_w = ctx.needs_input_grad[0], ctx.needs_input_grad[1]
         ctx.about = (x.shape, x.dtype, w.dtype, format)
+        ctx.tie = tie
         if flat.shape[0] == 0:
             ctx.save_for_backward(w)
             return x.new_zeros(*x.shape[:-1], w.shape[0])
@@ -82,7 +102,8 @@ class _Fp4Linear(torch.autograd.Function):
         shape, x_dtype, w_dtype, format = ctx.about
         if dy.numel() == 0:
             (w,) = ctx.saved_tensors
-            return dy.new_zeros(shape, dtype=x_dtype), torch.zeros_like(w), None
+            return dy.new_zeros(shape, dtype=x_dtype), torch.zeros_like(w), None, None
+        sources = (dy, *ctx.tie)
         dy = dy.reshape(-1, dy.shape[-1])
         need_x, need_w = ctx.needs_input_grad[0], ctx.needs_input_grad[1]
         dx = dw = None
@@ -95,7 +116,7 @@ class _Fp4Linear(torch.autograd.Function):
             dx = binding.sbc_fp4_product(dy4, ctx.w4_t, x_dtype).view(shape)
         if need_w:
             dw = binding.sbc_fp4_product(dy4_t, ctx.x4_t, w_dtype)
-        return dx, dw, None
+        return _first_only(dx, *sources), _first_only(dw, *sources), None, None
 
 
 def fp4_linear(x: torch.Tensor, w: torch.Tensor, format: str = "e8m0") -> torch.Tensor:
@@ -103,7 +124,10 @@ def fp4_linear(x: torch.Tensor, w: torch.Tensor, format: str = "e8m0") -> torch.
     axis that a product contracts; w [out, in] stays a master copy and gets a gradient in its own type."""
     if x.shape[-1] != w.shape[1]:
         raise ValueError(f"x has {x.shape[-1]} features, w takes {w.shape[1]}")
-    return _Fp4Linear.apply(x, w, format)
+    # what was rounded to 4 bits is kept for the backward pass, not x itself: an empty tensor stands for both in _first_only
+    # (in a list: it is no input of the product)
+    tie = [_FirstOnly.apply(x.new_empty(0), x, w)] if torch.is_grad_enabled() and (x.requires_grad or w.requires_grad) else []
+    return _Fp4Linear.apply(x, w, format, tie)
 
 
 def fp4_apply(x: torch.Tensor, w: binding.Fp4Tensor) -> torch.Tensor:

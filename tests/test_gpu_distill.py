@@ -103,3 +103,41 @@ def test_toy_runs_repeat_exactly():
         updates = [u for c in range(2) for u in toy.local_update(c, toy.weights, 3)]
         results.append(updates)
     assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+def test_second_derivatives_are_refused():
+    """A gradient that is differentiated again raises, instead of leaving out these functions' part of a sum."""
+    z = torch.randn(4, 200, generator=gen(1), device=DEV).requires_grad_(True)
+    message = distill.teach(z.detach() + torch.randn(4, 200, generator=gen(2), device=DEV), 8)
+    for logits in (z, z.t().contiguous().t()):
+        for total in (lambda t: t.sum(), lambda t: t.square().sum()):
+            loss = total(distill.distill_loss(logits, message)) + (z ** 2).sum()
+            (plain,) = torch.autograd.grad(loss, z, retain_graph=True)
+            (grad,) = torch.autograd.grad(loss, z, create_graph=True)
+            assert torch.equal(grad, plain)             # asking for the graph alone changes nothing
+            with pytest.raises(RuntimeError, match="second derivatives"):
+                torch.autograd.grad(grad.square().sum(), z)
+    x = torch.randn(6, 64, generator=gen(3), device=DEV).requires_grad_(True)
+    w = torch.randn(10, 64, generator=gen(4), device=DEV).requires_grad_(True)
+    for total in (lambda t: (t * t.detach()).sum(), lambda t: t.square().sum()):
+        loss = total(distill.fp4_linear(x, w)) + (x ** 2).sum() + (w ** 2).sum()
+        plain = torch.autograd.grad(loss, (x, w), retain_graph=True)
+        grads = torch.autograd.grad(loss, (x, w), create_graph=True)
+        assert all(torch.equal(a, b) for a, b in zip(grads, plain))
+        for g, of in ((grads[0], w), (grads[1], x), (grads[0], x), (grads[1], w)):
+            with pytest.raises(RuntimeError, match="second derivatives"):
+                torch.autograd.grad(g.square().sum(), of, retain_graph=True)
+
+
+def test_the_product_keeps_its_input_in_four_bits_only():
+    """Nothing of the forward call holds on to x between the two passes."""
+    w = torch.randn(32, 4096, generator=gen(4), device=DEV).requires_grad_(True)
+    start = torch.randn(4096, 4096, generator=gen(3), device=DEV).requires_grad_(True)
+    base = torch.cuda.memory_allocated()
+    x = start + 1.0
+    size = x.numel() * 4
+    y = distill.fp4_linear(x, w)
+    del x
+    assert torch.cuda.memory_allocated() - base < size / 2
+    (y * y).sum().backward()
+    assert start.grad.shape == start.shape and w.grad.shape == w.shape
