@@ -31,9 +31,16 @@ class TeacherMessage(NamedTuple):
         return sum(t.numel() * t.element_size() for t in (self.values, self.indices, self.rest))
 
 
+def _rows(t: torch.Tensor) -> torch.Tensor:
+    """A matrix as the calls take one: contiguous along its rows, which do not overlap.  Transposes and
+    broadcast values (what a sum's gradient is) are copied."""
+    across, along = t.stride()
+    return t if (along == 1 or t.shape[1] == 1) and (across >= t.shape[1] or t.shape[0] == 1) else t.contiguous()
+
+
 def teach(logits: torch.Tensor, k: int, temperature: float = 1.0) -> TeacherMessage:
     """The message for a teacher's logits [positions, words]."""
-    return TeacherMessage(*binding.sbc_top_logits(logits, k, temperature), temperature)
+    return TeacherMessage(*binding.sbc_top_logits(_rows(logits), k, temperature), temperature)
 
 
 class _FirstOnly(torch.autograd.Function):
@@ -57,9 +64,7 @@ def _first_only(grad, *sources):
 class _DistillLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, values, indices, rest, temperature, alpha, labels):
-        flat = logits.detach()
-        if flat.stride(-1) != 1:
-            flat = flat.contiguous()
+        flat = _rows(logits.detach())
         loss, stats = binding.sbc_distill_loss(flat, values, indices, rest, temperature, alpha, labels)
         ctx.save_for_backward(logits, flat, values, indices, rest, labels, stats)
         ctx.about = (temperature, alpha)
@@ -84,7 +89,7 @@ def distill_loss(logits: torch.Tensor, message: TeacherMessage, alpha: float = 1
 class _Fp4Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, format, tie):
-        flat = x.detach().reshape(-1, x.shape[-1])
+        flat, master = _rows(x.detach().reshape(-1, x.shape[-1])), _rows(w.detach())
         need_x, need_w = ctx.needs_input_grad[0], ctx.needs_input_grad[1]
         ctx.about = (x.shape, x.dtype, w.dtype, format)
         ctx.tie = tie
@@ -93,8 +98,8 @@ class _Fp4Linear(torch.autograd.Function):
             return x.new_zeros(*x.shape[:-1], w.shape[0])
         # along the rows for this product; along the columns, still in 4 bits, for the backward ones
         x4, ctx.x4_t = binding.sbc_fp4_quantise_both(flat, format) if need_w else (binding.sbc_fp4_quantise(flat, format), None)
-        w4, ctx.w4_t = (binding.sbc_fp4_quantise_both(w.detach(), format) if need_x
-                        else (binding.sbc_fp4_quantise(w.detach(), format), None))
+        w4, ctx.w4_t = (binding.sbc_fp4_quantise_both(master, format) if need_x
+                        else (binding.sbc_fp4_quantise(master, format), None))
         return binding.sbc_fp4_product(x4, w4, x.dtype).view(*x.shape[:-1], w4.rows)
 
     @staticmethod
@@ -104,7 +109,7 @@ class _Fp4Linear(torch.autograd.Function):
             (w,) = ctx.saved_tensors
             return dy.new_zeros(shape, dtype=x_dtype), torch.zeros_like(w), None, None
         sources = (dy, *ctx.tie)
-        dy = dy.reshape(-1, dy.shape[-1])
+        dy = _rows(dy.reshape(-1, dy.shape[-1]))
         need_x, need_w = ctx.needs_input_grad[0], ctx.needs_input_grad[1]
         dx = dw = None
         if need_x and need_w:
@@ -132,7 +137,7 @@ def fp4_linear(x: torch.Tensor, w: torch.Tensor, format: str = "e8m0") -> torch.
 
 def fp4_apply(x: torch.Tensor, w: binding.Fp4Tensor) -> torch.Tensor:
     """x w^T for weights that are held in 4 bits (no gradients): a token or a batch."""
-    flat = x.reshape(-1, x.shape[-1])
+    flat = _rows(x.reshape(-1, x.shape[-1]))
     if flat.shape[0] == 0:
         return x.new_zeros(*x.shape[:-1], w.rows)
     y = binding.sbc_fp4_product(binding.sbc_fp4_quantise(flat, w.format), w, x.dtype)

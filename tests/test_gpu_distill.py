@@ -141,3 +141,65 @@ def test_the_product_keeps_its_input_in_four_bits_only():
     assert torch.cuda.memory_allocated() - base < size / 2
     (y * y).sum().backward()
     assert start.grad.shape == start.shape and w.grad.shape == w.shape
+
+
+ORDERS = {"transposed": lambda t: t.t().contiguous().t(), "every second": lambda t: t.repeat_interleave(2, 1)[:, ::2],
+          "padded": lambda t: torch.nn.functional.pad(t, (3, 2))[:, 3:-2], "one row": lambda t: t[:1].expand(t.shape),
+          "one column": lambda t: t[:, :1].expand(t.shape), "one value": lambda t: t[:1, :1].expand(t.shape)}
+
+
+@pytest.mark.parametrize("fmt", ["e8m0", "e4m3"])
+@pytest.mark.parametrize("order", list(ORDERS))
+@pytest.mark.parametrize("tokens", [1, 37])
+def test_fp4_linear_of_any_order(order, tokens, fmt):
+    """Inputs, weights and gradients that are transposes, slices or broadcast give what their copies give."""
+    make = ORDERS[order]
+    x = torch.randn(tokens, 70, generator=gen(1), device=DEV)
+    w = torch.randn(45, 70, generator=gen(2), device=DEV)
+    dy = torch.randn(tokens, 45, generator=gen(3), device=DEV)
+
+    def call(x, w, dy):
+        x, w = x.detach().requires_grad_(True), w.detach().requires_grad_(True)
+        y = distill.fp4_linear(x, w, fmt)
+        return (y, *torch.autograd.grad(y, (x, w), dy))
+
+    for xs, ws, dys in ((make(x), w, dy), (x, make(w), dy), (x, w, make(dy)), (make(x), make(w), make(dy))):
+        for a, b in zip(call(xs, ws, dys), call(xs.contiguous(), ws.contiguous(), dys.contiguous())):
+            assert torch.equal(a, b)
+    held = sbc.sbc_fp4_quantise(w, fmt)
+    assert torch.equal(distill.fp4_apply(make(x), held), distill.fp4_apply(make(x).contiguous(), held))
+
+
+@pytest.mark.parametrize("total", [lambda y: y.sum(), lambda y: y.mean(), lambda y: y.sum(0)[3], lambda y: y.mean(0).sum(), lambda y: y[:, 0].sum(),
+                                   lambda y: (y.t() @ torch.ones(y.shape[0], 2, device=DEV)).sum(), lambda y: y.t().contiguous().sum()])
+def test_fp4_linear_under_ordinary_reductions(total):
+    """The gradient that autograd hands over, whatever its strides, against the same one as a matrix of its own."""
+    x = torch.randn(2, 9, 64, generator=gen(1), device=DEV).requires_grad_(True)
+    w = torch.randn(24, 64, generator=gen(2), device=DEV).requires_grad_(True)
+    y = distill.fp4_linear(x, w)
+    got = torch.autograd.grad(total(y.view(18, 24)), (x, w), retain_graph=True)
+    leaf = y.detach().view(18, 24).clone().requires_grad_(True)
+    (dy,) = torch.autograd.grad(total(leaf), leaf)
+    want = torch.autograd.grad(y, (x, w), dy.contiguous().view(2, 9, 24))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("order", list(ORDERS))
+def test_distill_loss_of_any_order(order):
+    z = ORDERS[order](2 * torch.randn(10, 300, generator=gen(1), device=DEV))
+    message = distill.teach(z, 12, 2.0)
+    for a, b in zip(message[:3], distill.teach(z.contiguous(), 12, 2.0)[:3]):
+        assert torch.equal(a, b)
+    message = distill.teach(z + torch.randn(10, 300, generator=gen(2), device=DEV), 12, 2.0)
+    results = []
+    for logits in (z, z.contiguous()):
+        logits = logits.detach().requires_grad_(True)
+        loss = distill.distill_loss(logits, message)
+        results.append((loss, *torch.autograd.grad(loss.sum(), logits)))
+    (loss, grad), (want, want_grad) = results
+    if order == "padded":    # such rows are read where they are and cut into vectors elsewhere: sums in another order
+        delta = (300 / 256 + 64 + 4 * 30) * 2.0 ** -24
+        assert bool(((loss - want).abs() <= 4 * delta * 2.0 ** 2).all())
+        assert bool(((grad - want_grad).abs() <= 8 * delta + 2 * 2.0 ** -24 * want_grad.abs()).all())
+    else:
+        assert torch.equal(loss, want) and torch.equal(grad, want_grad)
