@@ -122,7 +122,7 @@ int sbc_fp4_product(const sbc_fp4 *a, const sbc_fp4 *b, void *out, int dtype, in
  *   values[r, 0..k), indices[r, 0..k)  in descending order, the lower index
  *                                      first among equals (-0 equals +0)
  *   rest[r] = log sum_{j not sent} exp(logits[r, j] / temperature), -inf if
- *             nothing (or nothing but -inf) is left
+ *             nothing (or nothing but -inf) is left, +inf if a +inf is
  * Logits of -inf (words ruled out) are sent only where fewer than k others
  * exist.  NaN orders above everything and makes the row's rest NaN if it is
  * not sent.

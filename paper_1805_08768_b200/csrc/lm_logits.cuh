@@ -119,8 +119,19 @@ template <bool NEAR> struct Scale {
     static __device__ __forceinline__ float lack(float m, float c) { return NEAR ? fmaf(m, c, -__fmul_rn(m, c)) : 0.f; }
 };
 
+// The same for an infinite reference.
+struct InfiniteScale {
+    static __device__ __forceinline__ float one(float x) { return x == __builtin_huge_valf() ? 0.f : x != x ? x : -__builtin_huge_valf(); }
+    __device__ __forceinline__ unsigned long long two(unsigned long long x) const {
+        float u, v;
+        unpair(u, v, x);
+        return pair(one(u), one(v));
+    }
+    static __device__ __forceinline__ float lack(float, float) { return 0.f; }
+};
+
 // sum += 2^(...) over a granule
-template <int E, bool NEAR> __device__ __forceinline__ void add_powers(unsigned long long& sum, const float* x, const Scale<NEAR>& scale) {
+template <int E, typename S> __device__ __forceinline__ void add_powers(unsigned long long& sum, const float* x, const S& scale) {
 #pragma unroll
     for (int j = 0; j < E; j += 2) {
         float u, v;
@@ -146,24 +157,26 @@ __device__ __forceinline__ float warp_sum(float v) {
 
 // Sums of 2^((x - m) c), and with CE2 of 2^((x - m) log2e), with the largest x as their reference.
 // Every operation is rounded by itself wherever this is compiled, so that two calls and one for both
-// give the same bits.
-template <bool CE2> struct Mass {
+// give the same bits.  INF: infinities count, each as the reference itself (2^0); otherwise they make a NaN.
+template <bool CE2, bool INF = false> struct Mass {
     float m = -__builtin_huge_valf(), s = 0.f, s1 = 0.f;
     __device__ __forceinline__ float base() const { return m == -infinity() ? 0.f : m; }
+    static __device__ __forceinline__ float gap(float x, float base) { return INF && x == base ? 0.f : x - base; }
     __device__ __forceinline__ void join(float om, float os, float os1, float c) {
         const float top = fmaxf(m, om), b = top == -infinity() ? 0.f : top;
-        s = fmaf(s, exp2_fast(__fmul_rn(m - b, c)), __fmul_rn(os, exp2_fast(__fmul_rn(om - b, c))));
-        if (CE2) s1 = fmaf(s1, exp2_fast(__fmul_rn(m - b, kLog2e)), __fmul_rn(os1, exp2_fast(__fmul_rn(om - b, kLog2e))));
+        s = fmaf(s, exp2_fast(__fmul_rn(gap(m, b), c)), __fmul_rn(os, exp2_fast(__fmul_rn(gap(om, b), c))));
+        if (CE2) s1 = fmaf(s1, exp2_fast(__fmul_rn(gap(m, b), kLog2e)), __fmul_rn(os1, exp2_fast(__fmul_rn(gap(om, b), kLog2e))));
         m = top;
     }
     // every lane gets the warp's
     __device__ __forceinline__ void lanes(float c) {
         const float top = warp_max(m), b = top == -infinity() ? 0.f : top;
-        s = warp_sum(__fmul_rn(s, exp2_fast(__fmul_rn(m - b, c))));
-        if (CE2) s1 = warp_sum(__fmul_rn(s1, exp2_fast(__fmul_rn(m - b, kLog2e))));
+        s = warp_sum(__fmul_rn(s, exp2_fast(__fmul_rn(gap(m, b), c))));
+        if (CE2) s1 = warp_sum(__fmul_rn(s1, exp2_fast(__fmul_rn(gap(m, b), kLog2e))));
         m = top;
     }
 };
+using RestMass = Mass<false, true>;   // of what is not sent
 
 // The part of [0, cols) that block `rank` of 2^shift takes, in whole multiples of 64 elements.
 __device__ __forceinline__ int segment_start(int cols, int rank, int shift) {
@@ -739,7 +752,7 @@ template <typename T, bool HELD> struct Source {
 };
 
 // The block's mass from every thread's, for warp 0; `turn` keeps two uses in a row apart.
-__device__ __forceinline__ void block_mass(Mass<false>& a, TopShared& sh, int turn, float c) {
+__device__ __forceinline__ void block_mass(RestMass& a, TopShared& sh, int turn, float c) {
     a.lanes(c);
     const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
     if (lane == 0) {
@@ -748,7 +761,7 @@ __device__ __forceinline__ void block_mass(Mass<false>& a, TopShared& sh, int tu
     }
     __syncthreads();
     if (threadIdx.x < 32) {
-        a = Mass<false>();
+        a = RestMass();
         if (lane < warps) a.m = sh.warp_m[turn][lane], a.s = sh.warp_s[turn][lane];
         a.lanes(c);
     }
@@ -776,7 +789,7 @@ struct KeyBins {
 // the mass of what is not sent.  Few are compared with each other; otherwise the keys' range is cut into
 // equal bins, largest first, and a candidate's rank is its bin's start and how many of the same bin are
 // larger.
-__device__ __forceinline__ void rank_candidates(TopShared& sh, const Candidates& cand, int n, int k, Mass<false>& mass, float c) {
+__device__ __forceinline__ void rank_candidates(TopShared& sh, const Candidates& cand, int n, int k, RestMass& mass, float c) {
     const int t = threadIdx.x, threads = blockDim.x, lane = t & 31, warps = threads >> 5;
     if (n <= kTopPairs) {
         for (int i = t; i < n; i += threads) {
@@ -918,7 +931,7 @@ template <typename T> __device__ __noinline__ unsigned long long exact_threshold
 // Gathers what is at or above the threshold; returns the thread's mass of everything else.  PLAIN: the
 // threshold is a value's (whole composites need not be compared) above -inf.
 template <typename T, bool HELD, bool PLAIN>
-__device__ __forceinline__ Mass<false> gather_top(const Source<T, HELD>& src, int first, TopShared& sh, const Candidates& cand,
+__device__ __forceinline__ RestMass gather_top(const Source<T, HELD>& src, int first, TopShared& sh, const Candidates& cand,
                                                   unsigned long long threshold, float c) {
     constexpr int E = Gran<T>::E;
     const Cut<T>& cut = src.cut;
@@ -979,7 +992,7 @@ __device__ __forceinline__ Mass<false> gather_top(const Source<T, HELD>& src, in
             if (HELD && any) top.add(src.get(g));
         }
     }
-    Mass<false> mass;
+    RestMass mass;
     mass.m = fmaxf(top.get(), top_left);
     const float base = mass.base();
     const auto add_all = [&](const auto& scale) {
@@ -1000,8 +1013,10 @@ __device__ __forceinline__ Mass<false> gather_top(const Source<T, HELD>& src, in
     };
     if (fabsf(base) * c < kNear)
         add_all(Scale<true>(base, c));
-    else
+    else if (PLAIN || base != infinity())   // (no infinity is below a value's threshold)
         add_all(Scale<false>(base, c));
+    else
+        add_all(InfiniteScale());
     return mass;
 }
 
@@ -1051,7 +1066,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(kTopThreads, 
     }
     unsigned long long threshold = 0;
     const bool bounded = a.cols > threads;
-    Mass<false> mass;
+    RestMass mass;
     if (bounded) {
         GranMax<T, true> top;
 #pragma unroll 4
@@ -1130,7 +1145,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(kTopThreads, 
                 }
                 n += count;
             }
-            mass = Mass<false>();
+            mass = RestMass();
             if (t < size) mass.m = ld_cluster(map_rank(smem_u32(&sh.m), (uint32_t)t)), mass.s = ld_cluster(map_rank(smem_u32(&sh.s), (uint32_t)t));
         }
         cluster_sync();   // nobody reads another block's candidates any more
@@ -1174,7 +1189,7 @@ template <typename T> struct StreamShared {
 
 // Keeps about the k largest of the candidates: those in the bins (of equal parts of the keys' range) down
 // to the k-th largest's.  Returns the smallest key kept; the others join the mass.
-__device__ __forceinline__ uint32_t keep_largest(TopShared& sh, const Candidates& cand, int n, int k, Mass<false>& mass, float c) {
+__device__ __forceinline__ uint32_t keep_largest(TopShared& sh, const Candidates& cand, int n, int k, RestMass& mass, float c) {
     const int t = threadIdx.x, threads = blockDim.x, lane = t & 31, warps = threads >> 5;
     constexpr int kMost = kStreamRoom / kStreamThreads;   // candidates a thread holds
     unsigned long long mine[kMost];
@@ -1273,7 +1288,7 @@ template <typename T> __global__ void __launch_bounds__(kStreamThreads, 4) k_top
     fetch(0);
     if (parts > 1) fetch(1);
 
-    Mass<false> mass;
+    RestMass mass;
     uint32_t least = 0;   // key of the bound
     bool late = false, crowded = false;
     int p = 0;
@@ -1299,7 +1314,7 @@ template <typename T> __global__ void __launch_bounds__(kStreamThreads, 4) k_top
             __syncthreads();
             least = max(__reduce_min_sync(0xffffffffu, sh.warp_bound[min(lane, warps - 1)]) << 16, kLowestKey);
         }
-        const Mass<false> more = gather_top<T, true, true>(src, part.p - z, sh, cand, (unsigned long long)least << 32, c);
+        const RestMass more = gather_top<T, true, true>(src, part.p - z, sh, cand, (unsigned long long)least << 32, c);
         mass.join(more.m, more.s, 0.f, c);
         before_copies();
         __syncthreads();

@@ -114,6 +114,27 @@ def test_top_logits_ties_and_masks(kind, rows, cols, k, dtype):
     check_top(z, k, 1.0)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows,cols,k", [(8, 40, 7), (8, 700, 64), (8, 3000, 33), (7, 40000, 200), (8, 450000, 5), (150, 110003, 100)])
+def test_top_logits_with_infinities(rows, cols, k, dtype):
+    """More infinities than are sent leave an infinite rest, a NaN that is left makes it a NaN."""
+    z = logits(rows, cols, dtype, 3)
+    places = torch.randperm(cols, generator=gen(8), device=DEV)
+    z[0, places[:k + 1]] = INF
+    z[1, places[:k]] = INF                       # all of them are sent
+    z[2, places[:min(2 * k + 500, cols)]] = INF
+    z[3] = INF
+    z[4, places[:k]], z[4, places[k]] = math.nan, INF
+    z[5, places[:k + 1]], z[5, places[k + 1]] = math.nan, INF
+    z[6, places[:3]], z[6, places[3:k + 2]], z[6, places[k + 2:]] = math.nan, INF, -INF
+    check_top(z, k, 2.0)
+    rest = sbc.sbc_top_logits(z, k, 2.0)[2]
+    want = torch.full((7,), INF, device=DEV)
+    want[5] = math.nan
+    assert bool(((rest[:7] == want) | (torch.isnan(rest[:7]) & torch.isnan(want)))[[0, 2, 3, 4, 5, 6]].all())
+    assert bool(torch.isfinite(rest[1]))
+
+
 def test_top_logits_strides_and_empty():
     room = logits(1, 200_000, torch.bfloat16, 9).view(-1)
     for offset, stride in ((1, 5003), (3, 5010), (0, 5001), (7, 6000)):
