@@ -569,7 +569,8 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
             sh.inv_whole = inv_whole;
             sh.rest_term = live ? term(p_r, q_r, ((rest - m * inv) - log_s * kLn2) - shift) : 0.f;
             sh.cross = ce_weight != 0.f ? ce_weight * (log_whole1 * kLn2 - (label_z - top)) : 0.f;
-            sh.missing = live ? 1.f : (whole != whole || total != total) ? whole + total : 0.f;   // the divergence's factor
+            // (without weight it is left out, not multiplied by 0: it may be infinite)
+            sh.missing = live && a.alpha > 0.f ? 1.f : (whole != whole || total != total) ? whole + total : 0.f;   // the divergence's factor
             if (a.stats && rank == 0) {
                 float4* st = reinterpret_cast<float4*>(a.stats + row * SBC_DISTILL_STATS);
                 st[0] = make_float4(r.others, r.log_others, r.top, r.log_whole);

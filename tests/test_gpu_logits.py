@@ -291,6 +291,35 @@ def test_masks_of_the_types_lowest_value(dtype, tau):
     assert torch.equal(loss[keep], other) and torch.equal(grad[keep], other_grad)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tau", [1.0, 2.0])
+@pytest.mark.parametrize("rows,cols,k", [(6, 50, 8), (4, 3000, 64), (2, 40000, 32)])
+def test_divergence_without_weight(rows, cols, k, tau, dtype):
+    """alpha = 0 leaves the cross entropy alone, also where the student rules out what the teacher sent (an infinite
+    divergence); a NaN among the logits still makes the row's loss NaN."""
+    z = logits(rows, cols, dtype, 11)
+    values, indices, rest = message(z, k, tau, 5)
+    z.scatter_(1, indices[:, 1::2].long(), -INF)
+    labels = z.argmax(1)
+    labels[0] = -1
+    about = dict(rest=rest, temperature=tau, alpha=0.0, labels=labels)
+    x = z.double().requires_grad_(True)
+    log_q = torch.log_softmax(x, 1)
+    want = -log_q.gather(1, labels.clamp(min=0)[:, None])[:, 0] * (labels >= 0)
+    (want_grad,) = torch.autograd.grad(want.sum(), x)
+    size = (log_q.detach().exp() + torch.zeros_like(z).double().scatter(1, labels.clamp(min=0)[:, None], 1.0)) * (labels >= 0)[:, None]
+    finite = torch.where(torch.isfinite(z), z.double().abs(), torch.zeros_like(z).double())
+    delta = (cols / 256 + 64) * U + 4 * U * (float(finite.max()) + math.log(cols) + 1)
+    loss, stats = sbc.sbc_distill_loss(z, values, indices, **about)
+    assert bool(((loss.double() - want.detach()).abs() <= 2 * delta + 8 * U * want.detach().abs()).all()) and float(loss[0]) == 0
+    for grad in (sbc.sbc_distill_grad(z, values, indices, stats, **about), sbc.sbc_distill_loss_grad(z, values, indices, **about)[1]):
+        assert bool(((grad.double() - want_grad).abs() <= 4 * delta * size + ROUND[dtype] * want_grad.abs() + 1e-37).all())
+    assert torch.equal(sbc.sbc_distill_loss_grad(z, values, indices, **about)[0], loss)
+    z[rows - 1, int(indices[rows - 1, 0])] = math.nan
+    again = sbc.sbc_distill_loss(z, values, indices, **about)[0]
+    assert bool(torch.isnan(again[-1])) and torch.equal(again[:-1], loss[:-1])
+
+
 def test_distill_everything_sent_and_nothing_left():
     z = logits(5, 100, torch.float32, 3)
     values, indices, rest = message(z, 100, 1.0, 2)
