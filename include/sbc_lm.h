@@ -125,7 +125,8 @@ int sbc_fp4_product(const sbc_fp4 *a, const sbc_fp4 *b, void *out, int dtype, in
  *             nothing (or nothing but -inf) is left, +inf if a +inf is
  * Logits of -inf (words ruled out) are sent only where fewer than k others
  * exist.  NaN orders above everything and makes the row's rest NaN if it is
- * not sent.
+ * not sent.  If a bounded device-side wait gave up, rest is NaN and the row's
+ * values and indices say nothing.
  *
  * logits  device, dtype, rows x cols; rows may be 0
  * k       1 .. min(cols, SBC_TOP_MOST); temperature 1e-6 .. 1e6
@@ -164,7 +165,8 @@ typedef struct sbc_distill {
 
 /* Forward: loss (rows floats) and, unless NULL, stats (rows x SBC_DISTILL_STATS
  * floats, 16-byte aligned) for the backward call.  status: device, one uint32,
- * or NULL. */
+ * or NULL; SBC_STATUS_TIMEOUT is or-ed in if a bounded device-side wait gave
+ * up, what it was for is then NaN. */
 int sbc_distill_loss(const void *logits, int dtype, int64_t rows, int64_t cols, int64_t row_stride,
                      const sbc_distill *d, float *loss, float *stats, uint32_t *status, sbc_cuda_stream_t stream);
 

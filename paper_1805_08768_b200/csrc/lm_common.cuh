@@ -126,6 +126,14 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
     return false;
 }
 
+// Waits for copies into shared memory; true if they are late.  Late ones still write, so they are waited for as long
+// again before anything takes their place or the block ends.
+__device__ __forceinline__ bool copies_late(uint32_t bar, uint32_t parity) {
+    uint32_t i = 0;
+    while (i < 2 * kWaitTries && !mbar_try(bar, parity)) ++i;
+    return i >= kWaitTries;
+}
+
 // Arrives at a barrier of a block of the cluster (`bar` from map_rank).  It orders this thread's tensor
 // memory accesses only (behind tcgen05.wait and tcgen05.fence); a release to the whole cluster would
 // wait for every earlier write, which cost more than the rest of a stage.

@@ -430,9 +430,11 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
     cut.stage(held, bar);
     uint32_t phase = 0;
     bool late = false;
-    const auto landed = [&] {   // the barrier in front of it is for the edges, and for its own initialisation
+    // the barrier in front of it is for the edges, and for its own initialisation; a thread that was late once waits no
+    // more, and the one that starts the copies starts no more
+    const auto landed = [&] {
         __syncthreads();
-        late |= !mbar_wait(bar, phase);
+        if (!late) late = copies_late(bar, phase);
         phase ^= 1;
     };
     // the teacher, while the logits are on their way
@@ -467,7 +469,7 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
             before_copies();
             __syncthreads();
             cut = part_of(part);
-            cut.stage(held, bar);
+            if (!late) cut.stage(held, bar);
         }
         landed();
         const int lo = first + (int)(cut.p - segment.p);
@@ -581,7 +583,7 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
     __syncthreads();
     const RowStats r = sh.row;
     T* out = nullptr;
-    const Slope<T, CE2> slope(a, r, g, label >= 0);
+    Slope<T, CE2> slope(a, r, g, label >= 0);
     if (GRAD) {
         out = static_cast<T*>(a.grad) + row * a.grad_stride + first;
         for (int part = 0; part < parts; ++part) {
@@ -589,8 +591,9 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
                 before_copies();
                 __syncthreads();
                 cut = part_of(part);
-                cut.stage(held, bar);
+                if (!late) cut.stage(held, bar);
                 landed();
+                if (late) slope.coef = __uint_as_float(0x7fffffffu);   // this thread's granules become NaN
             }
             const int lo = (int)(cut.p - segment.p);
             slope.granules([&](const auto& gr) {
@@ -1063,7 +1066,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(kTopThreads, 
     if (HELD) {
         cut.stage(src.held, bar);
         __syncthreads();
-        late = !mbar_wait(bar, 0);
+        late = copies_late(bar, 0);
     }
     unsigned long long threshold = 0;
     const bool bounded = a.cols > threads;
@@ -1182,6 +1185,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(kTopThreads, 
 
 constexpr int kStreamBytes = 16384;
 constexpr int kStreamThreads = 256, kStreamRoom = 1024;   // threads of a block, candidates it can hold
+constexpr int kLate = 1 << 20;                            // added to their number when a part's copies came late
 
 template <typename T> struct StreamShared {
     uint64_t bar[2];
@@ -1291,11 +1295,12 @@ template <typename T> __global__ void __launch_bounds__(kStreamThreads, 4) k_top
 
     RestMass mass;
     uint32_t least = 0;   // key of the bound
-    bool late = false, crowded = false;
+    bool crowded = false;
+    int on_way = 1;   // parts on their way when the loop ends early
     int p = 0;
     for (; p < parts; ++p) {
         __syncthreads();
-        late |= !mbar_wait(smem_u32(&shared.bar[p & 1]), (uint32_t)(p >> 1) & 1);
+        if (copies_late(smem_u32(&shared.bar[p & 1]), (uint32_t)(p >> 1) & 1)) add_shared(&sh.count, kLate);   // ends the loop
         const Cut<T> part = part_of(p);
         const Source<T, true> src = {part, buffer + (p & 1) * (kGrans * E)};
         if (p == 0) {
@@ -1319,25 +1324,27 @@ template <typename T> __global__ void __launch_bounds__(kStreamThreads, 4) k_top
         mass.join(more.m, more.s, 0.f, c);
         before_copies();
         __syncthreads();
-        if (p + 2 < parts) fetch(p + 2);
         const int n = sh.count;
         if (n > a.room) {
             crowded = true;
             break;
         }
+        if (p + 2 < parts) fetch(p + 2);
         if (n > a.room / 2 && p + 1 < parts) {
             least = keep_largest(sh, cand, n, k, mass, c);
             if (sh.count > a.room / 2) {
                 crowded = true;
+                ++on_way;
                 break;
             }
         }
     }
     int n = sh.count;
+    bool late = n >= kLate;
     __syncthreads();
     if (crowded) {
         // values crowd at the bound: an exact one, from the whole row once more (what is on its way is not used)
-        for (int q = p + 1; q < min(p + 3, parts); ++q) late |= !mbar_wait(smem_u32(&shared.bar[q & 1]), (uint32_t)(q >> 1) & 1);
+        for (int q = p + 1; q <= min(p + on_way, parts - 1); ++q) late |= copies_late(smem_u32(&shared.bar[q & 1]), (uint32_t)(q >> 1) & 1);
         const unsigned long long threshold = exact_threshold(cut, 0, sh, cand, k);
         if (t == 0) sh.count = 0;
         __syncthreads();
