@@ -226,7 +226,6 @@ template <typename T, int FMT, int NT>
 int launch_wide(const sbc_fp4* a, const sbc_fp4* b, WideArgs p, int64_t tiles, cudaStream_t st) {
     using Shape = ProductShape<FMT>;
     if (tiles > kMaxDim / 2) return SBC_EINVAL;
-    p.nt = NT;
     p.tiles = (int)tiles;
     const int stage = kPRows * kPBytes + NT / 2 * kPBytes, scales = kWScales * Shape::kTiles * 512 * (1 + NT / 128);
     p.stages = std::min(std::min(kWMaxStages, (224 * 1024 - scales) / stage), 256 / (4 * Shape::kTiles * (1 + NT / 128)));

@@ -70,23 +70,6 @@ template <typename T> __device__ __forceinline__ void load8(Pack8<T>& v, const T
     }
 }
 
-template <typename T> __device__ __forceinline__ void store8(T* p, const Pack8<T>& v, int have, int align) {
-    if (have >= 8 && align >= 16) {
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(p)[i] = v.q[i];
-    } else if (have >= 8 && align >= 8) {
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T); ++i) reinterpret_cast<uint2*>(p)[i] = v.d[i];
-    } else if (have >= 8 && align >= 4) {
-#pragma unroll
-        for (int i = 0; i < 2 * (int)sizeof(T); ++i) reinterpret_cast<uint32_t*>(p)[i] = v.w[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < have) p[i] = v.e[i];
-    }
-}
-
 // Every kernel here is launched so that its blocks may start while the kernel in front of it on the
 // stream ends (its own preparation, barriers and tensor memory, then costs nothing).  This waits until
 // everything in front is done and visible; nothing in global memory is touched before it.  The next
@@ -169,11 +152,6 @@ __device__ __forceinline__ void before_copies() { asm volatile("fence.proxy.asyn
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t cluster_size() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
     return r;
 }
 __device__ __forceinline__ void cluster_sync() {

@@ -10,7 +10,6 @@
 namespace sbclm {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kDistillStats = 8;   // floats per row that the forward call leaves for the backward one
 
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;

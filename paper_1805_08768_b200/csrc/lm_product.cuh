@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(kPThreads) k_fp4_product(const __grid_constant
 
 // ---- many tokens ----------------------------------------------------------------------
 //
-// Pairs of blocks on neighbouring SMs share a tile of 256 weights x `nt` (256 or 128) tokens: each
+// Pairs of blocks on neighbouring SMs share a tile of 256 weights x NT (256 or 128) tokens: each
 // loads its 128 weights and half of the tokens, the tensor cores of both read both halves, so an SM
 // loads 0.58 bytes per thousand products where a block alone would load 0.82.  Blocks stay and take
 // tile after tile; loads run ahead across tiles.
@@ -315,7 +315,7 @@ struct WideArgs {
     void* out;
     uint32_t* status;
     long long rows_w, rows_x, stride, ktiles;
-    int chunks, steps, nt, stages;
+    int chunks, steps, stages;
     int tiles_w, tiles;   // tiles along the weights, all tiles
 };
 
