@@ -325,8 +325,9 @@ int sbc_fp4_quantise(const void* x, int dtype, int64_t rows, int64_t cols, int64
         using T = std::remove_pointer_t<decltype(as)>;
         cudaStream_t st = stream;
         if (format == SBC_FP4_E4M3) {
-            if (rows * cols > kAmaxAlone) {
-                a.amax_blocks = (int)std::min<int64_t>(pieces(rows, cols, row_stride == cols), kAmaxBlocks);
+            const int64_t blocks = pieces(rows, cols, row_stride == cols);
+            if (blocks > kAmaxAlone) {
+                a.amax_blocks = (int)std::min<int64_t>(blocks, kAmaxBlocks);
                 const int rc = launch(k_fp4_amax<T>, dim3((unsigned)a.amax_blocks), kQThreads, 0, st, 0, 0, a, static_cast<uint32_t*>(workspace));
                 if (rc != SBC_OK) return rc;
             }

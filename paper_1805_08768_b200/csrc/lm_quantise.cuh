@@ -135,9 +135,11 @@ struct QuantiseArgs {
 };
 
 constexpr int kAmaxBlocks = 1024;
-// Elements up to which every block finds the maximum itself, instead of a launch in front (us without / with
-// the launch: 1 x 650 4.4 / 5.7, 16 x 2048 5.4 / 5.2, 64 x 4096 18.8 / 5.2).
-constexpr long long kAmaxAlone = 32768;
+// Turns of a block's warps (a piece of a row each; rows without gaps are one long row) up to which every block finds
+// the maximum itself, instead of a launch in front.  us without / with the launch, float32: rows without gaps 1 x 650
+// 4.4 / 5.7, 16 x 2048 (two turns) 5.4 / 5.2, 64 x 4096 18.8 / 5.2; with gaps 16 x 64 (two turns) 5.2, 17 x 64 6.2 / 5.3,
+// 64 x 64 12.3 / 5.5, 40 x 650 9.1 / 5.3, 32768 x 1 6118 / 25.
+constexpr long long kAmaxAlone = 2;
 
 // A warp's share of a matrix: rows in pieces of 2048 elements, eight steps of 256.  f(row, column, left):
 // where a lane's first eight elements of a piece are, and how many elements the row has from there on.

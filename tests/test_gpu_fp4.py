@@ -376,3 +376,29 @@ def test_huge_tensor_scales_and_rows_of_zeros(tokens):
     assert float(got[1, 70]) == -math.inf
     got[1, 70] = 0
     assert not bool(got.any())
+
+
+@pytest.mark.parametrize("rows,cols,gap", [(16, 64, 64), (17, 64, 64), (512, 64, 64), (40, 650, 14), (32768, 1, 7)])
+def test_the_tensor_scale_of_rows_with_gaps(rows, cols, gap):
+    """Slices on both sides of the rule by which a kernel of its own finds the largest magnitude.  A slice may not take
+    20 times what its copy takes (a block that walks all rows by itself takes hundreds of times as long)."""
+    x = torch.full((rows, cols + gap), 5000.0, device=DEV)[:, :cols]
+    x.fill_(1.0)
+    x[rows - 1, cols - 1] = -1000.0
+    q = sbc.sbc_fp4_quantise(x, "e4m3")
+    assert float(q.tensor_scale) == 0.5
+    assert same(sbc.sbc_fp4_dequantise(q), plain_round(x, "e4m3"))
+
+    def least(t):
+        times = []
+        for _ in range(7):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            start.record()
+            for _ in range(4):
+                sbc.sbc_fp4_quantise(t, "e4m3")
+            end.record()
+            end.synchronize()
+            times.append(start.elapsed_time(end))
+        return min(times)
+
+    assert least(x) <= 20 * least(x.contiguous())
