@@ -90,7 +90,8 @@ class _Fp4Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, format, tie):
         flat, master = _rows(x.detach().reshape(-1, x.shape[-1])), _rows(w.detach())
-        need_x, need_w = ctx.needs_input_grad[0], ctx.needs_input_grad[1]
+        # (an input that asks for gradients does so under no_grad, too; there is no tie then)
+        need_x, need_w = (bool(tie) and needed for needed in ctx.needs_input_grad[:2])
         ctx.about = (x.shape, x.dtype, w.dtype, format)
         ctx.tie = tie
         if flat.shape[0] == 0:

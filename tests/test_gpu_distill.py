@@ -203,3 +203,16 @@ def test_distill_loss_of_any_order(order):
         assert bool(((grad - want_grad).abs() <= 8 * delta + 2 * 2.0 ** -24 * want_grad.abs()).all())
     else:
         assert torch.equal(loss, want) and torch.equal(grad, want_grad)
+
+
+def test_evaluation_rounds_one_way(monkeypatch):
+    """Without gradients nothing is quantised along the columns, whatever the weights ask for."""
+    x = torch.randn(5, 64, generator=gen(1), device=DEV)
+    w = torch.randn(24, 64, generator=gen(2), device=DEV).requires_grad_(True)
+    want = distill.fp4_linear(x, w).detach()
+    monkeypatch.setattr(distill.binding, "sbc_fp4_quantise_both", None)
+    with torch.no_grad():
+        assert torch.equal(distill.fp4_linear(x, w), want)
+    with torch.inference_mode():
+        assert torch.equal(distill.fp4_linear(x, w), want)
+    assert torch.equal(distill.fp4_linear(x, w.detach()), want)
