@@ -562,13 +562,15 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
         r.log_whole1 = seen ? log_whole1 : infinity();
         r.coef = __fadd_rn(live ? __fmul_rn(a.alpha * a.temperature, q_r - p_r) : 0.f, !CE2 && ce_weight != 0.f ? __fmul_rn(ce_weight, q_r) : 0.f);
         if (s != s) r.coef = s;   // a NaN among the others is everybody's
-        const float shift = (high - top * inv) + (log_total - log_whole) * kLn2;
+        // log p - log q: differences from the largest first, so that logits of any size (a type's lowest value as a mask) leave
+        // the logarithms their digits
+        const float shift = (log_total - log_whole) * kLn2;
         if (lane == 0) {
             sh.row = r;
             sh.shift = shift;
             sh.inv_total = inv_total;
             sh.inv_whole = inv_whole;
-            sh.rest_term = live ? term(p_r, q_r, ((rest - m * inv) - log_s * kLn2) - shift) : 0.f;
+            sh.rest_term = live ? term(p_r, q_r, fmaf(-log_s, kLn2, fmaf(top - m, inv, rest - high)) - shift) : 0.f;
             sh.cross = ce_weight != 0.f ? ce_weight * (log_whole1 * kLn2 - (label_z - top)) : 0.f;
             // (without weight it is left out, not multiplied by 0: it may be infinite)
             sh.missing = live && a.alpha > 0.f ? 1.f : (whole != whole || total != total) ? whole + total : 0.f;   // the divergence's factor
@@ -609,9 +611,9 @@ template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDi
         if (at < 0) continue;
         const float zv = sent_z[i], tv = sent_t[i];
         if (live) {
-            const float p = exp2_fast((__fmul_rn(tv, inv) - r.high) * kLog2e) * sh.inv_total;
-            const float q = exp2_fast((zv - r.top) * c) * sh.inv_whole;
-            kl += term(p, q, (tv - zv) * inv - sh.shift);
+            const float over = __fmul_rn(tv, inv) - r.high, under = zv - r.top;
+            const float p = exp2_fast(over * kLog2e) * sh.inv_total, q = exp2_fast(under * c) * sh.inv_whole;
+            kl += term(p, q, fmaf(-under, inv, over) - sh.shift);
         }
         if (GRAD) {
             has_label |= at == label;

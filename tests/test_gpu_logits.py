@@ -320,6 +320,33 @@ def test_divergence_without_weight(rows, cols, k, tau, dtype):
     assert bool(torch.isnan(again[-1])) and torch.equal(again[:-1], loss[:-1])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("tau", [0.5, 1.0, 2.0])
+@pytest.mark.parametrize("rows,cols,k", [(5, 900, 40), (2, 40000, 16)])
+def test_one_side_of_the_types_lowest_value(rows, cols, k, tau, dtype):
+    """A student whose words are all ruled out by the lowest value is uniform, whatever the teacher says; a teacher of
+    lowest values is uniform over its words, whatever the student says.  All distances on that side are zero, so only
+    the other side's logits enter the tolerance."""
+    low = torch.finfo(dtype).min
+    usual = logits(rows, cols, dtype, 11)
+    values, indices, rest = message(usual, k, tau, 4)
+    size = float(usual.double().abs().max()) + float(values.abs().max())
+    delta = (cols / 256 + 64) * U + 4 * U * (size / min(tau, 1.0) + math.log(cols) + 1)
+    lowest = torch.full_like(usual, low)
+    quiet = torch.full_like(values, low)
+    cases = [(lowest, values, rest), (lowest, values, None)]
+    if tau >= 1.0:      # (beyond it the lowest value divided by the temperature is -inf: such a teacher says nothing)
+        cases += [(usual, quiet, None), (lowest, quiet, None)]
+    for z, v, r in cases:
+        want, want_grad, parts = plain(z, v, indices, r, tau, 1.0, None, None)
+        loss, grad = sbc.sbc_distill_loss_grad(z, v, indices, rest=r, temperature=tau)
+        assert bool(((loss.double() - want).abs() <= tau * tau * 6 * delta + 8 * U * want.abs()).all()), (loss, want)
+        tiny = 1e-37 if dtype != torch.float16 else 2.0 ** -25
+        assert bool(((grad.double() - want_grad).abs() <= 4 * delta * parts + ROUND[dtype] * want_grad.abs() + tiny).all())
+        again, stats = sbc.sbc_distill_loss(z, v, indices, r, tau)
+        assert torch.equal(again, loss) and torch.equal(sbc.sbc_distill_grad(z, v, indices, stats, rest=r, temperature=tau), grad)
+
+
 def test_distill_everything_sent_and_nothing_left():
     z = logits(5, 100, torch.float32, 3)
     values, indices, rest = message(z, 100, 1.0, 2)
