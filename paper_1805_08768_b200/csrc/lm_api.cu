@@ -364,8 +364,10 @@ int sbc_fp4_product(const sbc_fp4* a, const sbc_fp4* b, void* out, int dtype, in
     if (!fp4_ok(a) || !fp4_ok(b) || a->format != b->format || a->cols != b->cols) return SBC_EINVAL;
     if (a->rows > kMaxDim - 512 || b->rows > kMaxDim - 512) return SBC_EINVAL;
     if (!matrix_ok(out, dtype, a->rows, b->rows, row_stride) || !aligned(status, 4)) return SBC_EINVAL;
-    // us of 128 tokens here / there: 8192^2 13.6 / 18.8, 1300 -> 2600 7.3 / 6.9, 2048^2 8.5 / 8.1, 4096 -> 16384
-    // 13.7 / 12.4, 16384 -> 4096 15.2 / 31.9, 650 -> 10000 6.0 / 6.1; of 64 never slower here
+    // This kernel holds 128 tokens.  us of 128 here / there: 8192^2 13.6 / 18.8, 1300 -> 2600 7.3 / 6.9, 2048^2 8.5 / 8.1,
+    // 4096 -> 16384 13.7 / 12.4, 16384 -> 4096 15.2 / 31.9, 650 -> 10000 6.0 / 6.1: three shapes would gain up to 1.3 us
+    // there, one would take twice as long; of 64 never slower here.  128 here, 129 there: 8192^2 13.3, 19.5;
+    // 16384 -> 4096 15.0, 32.0 (few tiles, long columns, which are not split there); 4096 -> 16384 13.3, 15.4
     if (a->rows > 128) return product_wide(a, b, out, dtype, row_stride, status, stream);
     ProductArgs p = {};
     p.scales_w = static_cast<const uint8_t*>(b->scales);

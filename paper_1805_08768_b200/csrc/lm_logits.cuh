@@ -394,8 +394,8 @@ struct DistillShared {
 //
 // log q = z c ln 2 - logZ with logZ from a running maximum and sum; the loss is the sum of p d - p + q over
 // sent words and the rest, d = log p - log q, times alpha tau^2; its gradient is alpha tau (q - p) at a sent
-// word, alpha tau q (1 - p_rest / q_rest) at another.  4480 x 10000 bfloat16 with its gradient 49 us,
-// 3.7 TB/s; its bytes alone take 28 us.  Bound by the latency between a block's steps (load, maximum and
+// word, alpha tau q (1 - p_rest / q_rest) at another.  4480 x 10000 bfloat16 with its gradient 48 us,
+// 3.8 TB/s; its bytes alone take 28 us.  Bound by the latency between a block's steps (load, maximum and
 // sum, join, statistics, store), so small blocks of which many share an SM.
 // 4095 x 50001 bfloat16 forward 92 us, 4.4 TB/s: parts of 40 KB leave five blocks on an SM.
 template <typename T, bool CE2, bool GRAD> __global__ void __launch_bounds__(kDistillThreads, 10) k_distill(DistillArgs a) {
@@ -1030,6 +1030,11 @@ __device__ __forceinline__ RestMass gather_top(const Source<T, HELD>& src, int f
 // it.  What is (little more than k, where values are spread at random) is ranked by the cluster's
 // first block, everything else only adds to the mass.
 //
+// A warp that owns fewer groups than its share bounds nothing, and rows of more columns than there is room for
+// candidates then always take exact_threshold: 16-bit rows of 513 to 768 columns (k up to 8), to 824 (64), to
+// 1912 (256); float32 rows of 513 to 944 (k of 100 to 200).  2240 bfloat16 rows for 64: 512 columns 23 us, 768 33 us,
+// 1000 18 us; for 128: 512 36 us, 1848 67 us, 2000 36 us.
+//
 // rest = log of the sum of exp(z / tau) over what is not sent, from a running maximum and sum.  2240 x 10000
 // bfloat16 for 64: 29 us, 1.6 TB/s; its bytes alone take 7 us.  Bound by instructions and the latency between a row's
 // steps (0.62 a cycle and scheduler): a quarter exponentials, a fifth ranking, a sixth the bound.
@@ -1181,7 +1186,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(kTopThreads, 
 // A block streams its row through two buffers in shared memory and reads it once.  The first part's
 // group maxima bound the k-th largest from below; whenever many candidates have come together the bound
 // is raised to (about) their own k-th largest, so a part of a long row adds few.  2048 x 131072 bfloat16 for
-// 128: 220 us, 2.4 TB/s.  Bound by instructions, 0.71 a cycle and scheduler, 5700 a part: unpacking,
+// 128: 223 us, 2.4 TB/s.  Bound by instructions, 0.71 a cycle and scheduler, 5700 a part: unpacking,
 // comparing with the bound and an exponential for every element.
 
 constexpr int kStreamBytes = 16384;

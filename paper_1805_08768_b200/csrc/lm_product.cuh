@@ -309,8 +309,10 @@ __global__ void __launch_bounds__(kPThreads) k_fp4_product(const __grid_constant
 // warps that do nothing else): copies by the tensor unit (tcgen05.cp) take turns with the products
 // there, about 100 cycles each against 128 of a product.
 //
-// 8192^3: E8M0 223 us, 4.9 PFLOP/s; E4M3 235 us, 4.7 PFLOP/s: bound by loads from L2, the tensor pipe is
-// busy half of the time.  4096^3 40 us, 3.4 PFLOP/s (256 tiles for 74 pairs: four rounds, the last half full);
+// 8192^3: E8M0 223 us, 4.9 PFLOP/s; E4M3 235 us, 4.7 PFLOP/s: stages wait for their loads.  The tensor pipe is busy half
+// of the time and L2 at 36 % of its peak, so neither bounds it; whether the way into the SMs or the ring of stages does
+// was not measured.  Tiles below half of the pairs leave the rest idle, the columns are not split here (16384 -> 4096:
+// 129 to 512 tokens 32 to 33 us).  4096^3 40 us, 3.4 PFLOP/s (256 tiles for 74 pairs: four rounds, the last half full);
 // 2240 x 1300 -> 2600 14 us, ramp and drain.
 //
 // Warps: 0..3 and 12..15 accumulator to memory (half of the columns each), 4..7 scales, 8 loads, 9
