@@ -1,4 +1,4 @@
-"""Thin ctypes binding over the C ABI declared in include/sbc.h.
+"""Thin ctypes binding over the C ABI declared in include/sbc.h, sbc_lm.h and sbc_block.h.
 
 Argument marshalling only: torch supplies device memory and the current CUDA
 stream, every step of the method runs in the library's kernels.  The library
@@ -31,6 +31,9 @@ EXPORTS = [
     "sbc_debug_barrier_timeout",
     "sbc_fp4_row_bytes", "sbc_fp4_scale_bytes", "sbc_fp4_workspace_bytes", "sbc_fp4_quantise", "sbc_fp4_dequantise",
     "sbc_fp4_product", "sbc_top_logits", "sbc_distill_loss", "sbc_distill_grad", "sbc_distill_loss_grad",
+    "sbc_layer_norm", "sbc_layer_norm_workspace_bytes", "sbc_layer_norm_grad", "sbc_dropout", "sbc_gated_kept_bytes",
+    "sbc_gated_workspace_bytes", "sbc_gated", "sbc_gated_grad", "sbc_adapter_plan_bytes", "sbc_adapter_plan", "sbc_adapter",
+    "sbc_adapter_grad",
 ]
 SIDE_VALUES = 2
 STATIC_WORKSPACE_BYTES = 8 << 20
@@ -75,6 +78,16 @@ class Fp4Desc(C.Structure):
 class DistillDesc(C.Structure):
     _fields_ = [("values", C.c_void_p), ("indices", C.c_void_p), ("rest", C.c_void_p), ("labels", C.c_void_p),
                 ("k", C.c_int32), ("temperature", C.c_float), ("alpha", C.c_float), ("reserved", C.c_int32)]
+
+
+class GatedDesc(C.Structure):
+    _fields_ = [("gate", C.c_void_p), ("up", C.c_void_p), ("gate_stride", C.c_int64), ("up_stride", C.c_int64),
+                ("hidden", C.c_int64), ("inner", C.c_int64), ("dtype", C.c_int32), ("act", C.c_int32)]
+
+
+class AdaptersDesc(C.Structure):
+    _fields_ = [("down", C.c_void_p), ("up", C.c_void_p), ("count", C.c_int64), ("rank", C.c_int64), ("inner", C.c_int64),
+                ("outer", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
 
 
 class DecodeDesc(C.Structure):
@@ -188,6 +201,21 @@ def lib() -> C.CDLL:
         L.sbc_distill_loss_grad.argtypes = [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64,
                                             C.POINTER(DistillDesc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
                                             C.c_void_p, C.c_void_p]
+        p, i32, i64, f32, size = C.c_void_p, C.c_int, C.c_int64, C.c_float, C.c_size_t
+        for name, result, args in (
+                ("sbc_layer_norm", i32, [p, i32, i64, i64, i64, p, p, i32, f32, p, i64, p, p]),
+                ("sbc_layer_norm_workspace_bytes", size, [i64, i64]),
+                ("sbc_layer_norm_grad", i32, [p, i64, p, i64, i32, i64, i64, p, p, i32, p, i64, p, p, p, size, p]),
+                ("sbc_dropout", i32, [p, i32, i64, i64, i64, p, i64, C.c_double, p, i64, p, i64, p]),
+                ("sbc_gated_kept_bytes", size, [i64, i64]),
+                ("sbc_gated_workspace_bytes", size, [p, i64, p, i64, i32, i32]),
+                ("sbc_gated", i32, [p, p, i64, i64, p, i64, p, p, size, p, p]),
+                ("sbc_gated_grad", i32, [p, p, i64, i64, p, i64, p, p, i64, p, p, i32, i64, p, size, p, p]),
+                ("sbc_adapter_plan_bytes", size, [i64, i64]),
+                ("sbc_adapter_plan", i32, [p, i64, i64, p, size, p, p]),
+                ("sbc_adapter", i32, [p, p, i32, i64, i64, p, p, f32, p, i64, p, i64, p, p, p]),
+                ("sbc_adapter_grad", i32, [p, p, i64, p, i64, i32, i64, p, p, f32, p, i64, p, i64, p, p, p, p])):
+            getattr(L, name).restype, getattr(L, name).argtypes = result, args
         _lib = L
     return _lib
 
@@ -854,3 +882,306 @@ def sbc_distill_loss_grad(logits: torch.Tensor, values: torch.Tensor, indices: t
     if rc:
         _check(rc, "sbc_distill_loss_grad")
     return loss, out
+
+
+# ---- operators of a client's own layers (include/sbc_block.h) ------------------------
+
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}
+ADAPTER_RANK, ADAPTER_FEW, ADAPTER_COUNT = 256, 64, 32768
+
+
+def _same(t: torch.Tensor, like: torch.Tensor, name: str, shape=None) -> int:
+    """Elements between the rows of a matrix of another one's type and device (and shape)."""
+    rows, cols, across, _ = _matrix(t, name)
+    if t.dtype != like.dtype:
+        raise TypeError(f"{name} must be {like.dtype}")
+    if (rows, cols) != tuple(like.shape if shape is None else shape):
+        raise ValueError(f"{name} must be {' x '.join(str(n) for n in (like.shape if shape is None else shape))}")
+    return across
+
+
+def _out(out: Optional[torch.Tensor], shape, like: torch.Tensor, stream) -> Tuple[torch.Tensor, int]:
+    """(a result's buffer, elements between its rows)"""
+    if out is None:
+        return _empty(stream, shape, like.dtype, like), max(shape[1], 1)
+    return out, _same(out, like, "out", shape)
+
+
+def _vector(t: Optional[torch.Tensor], n: int, x: torch.Tensor, name: str) -> Tuple[Optional[int], Optional[int]]:
+    """(address, type code) of a weight vector: float32 or the matrix's type."""
+    if t is None:
+        return None, None
+    if not (t.is_cuda and t.dim() == 1 and t.is_contiguous() and t.dtype in (torch.float32, x.dtype)):
+        raise TypeError(f"{name} must be a contiguous float32 or {x.dtype} CUDA vector")
+    if t.numel() != n:
+        raise ValueError(f"{name} must hold {n} values")
+    _beside(t, x, name)
+    return t.data_ptr(), DTYPE_CODES[t.dtype]
+
+
+def sbc_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                   eps: float = 1e-5, out: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(rows of x normalised, times weight plus bias; statistics [rows, 2] for sbc_layer_norm_grad).  The vectors
+    are float32 or of x's type, both alike; ``out`` may be x."""
+    rows, cols, across, code = _matrix(x, "x")
+    w, w_code = _vector(weight, cols, x, "weight")
+    b, b_code = _vector(bias, cols, x, "bias")
+    if w is not None and b is not None and w_code != b_code:
+        raise TypeError("weight and bias must be of one type")
+    out, out_across = _out(out, x.shape, x, stream)
+    stats = _empty(stream, (rows, 2), torch.float32, x)
+    rc = lib().sbc_layer_norm(x.data_ptr(), code, rows, cols, across, w, b, w_code if w is not None else b_code or 0, eps,
+                              out.data_ptr(), out_across, stats.data_ptr(), _cuda_stream(stream))
+    if rc:
+        _check(rc, "sbc_layer_norm")
+    return out, stats
+
+
+def sbc_layer_norm_grad(dy: torch.Tensor, x: torch.Tensor, stats: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                        need_input: bool = True, need_weights: bool = True, out: Optional[torch.Tensor] = None,
+                        weight_dtype: Optional[torch.dtype] = None, stream=None):
+    """(dx, dweight, dbias), each None where it is not asked for; ``out`` (for dx) may be dy or x.  dweight and dbias
+    are of the weight's type (``weight_dtype``, else float32, without a weight)."""
+    rows, cols, across, code = _matrix(x, "x")
+    dy_across = _same(dy, x, "dy")
+    w, w_code = _vector(weight, cols, x, "weight")
+    if w is None:
+        weight_dtype = torch.float32 if weight_dtype is None else weight_dtype
+        if weight_dtype not in (torch.float32, x.dtype):
+            raise TypeError(f"weight_dtype must be float32 or {x.dtype}")
+        w_code = DTYPE_CODES[weight_dtype]
+    elif weight_dtype not in (None, weight.dtype):
+        raise TypeError("weight_dtype must be the weight's type")
+    else:
+        weight_dtype = weight.dtype
+    if not (need_input or need_weights):
+        return None, None, None
+    st = _rows_of(stats, rows * 2, torch.float32, "stats", x)
+    dx = dx_across = dweight = dbias = room = None
+    if need_input:
+        dx, dx_across = _out(out, x.shape, x, stream)
+    size = 0
+    if need_weights:
+        dweight, dbias = _empty(stream, cols, weight_dtype, x), _empty(stream, cols, weight_dtype, x)
+        size = int(lib().sbc_layer_norm_workspace_bytes(rows, cols))
+        room = _empty(stream, size, torch.uint8, x)
+    rc = lib().sbc_layer_norm_grad(dy.data_ptr(), dy_across, x.data_ptr(), across, code, rows, cols, st, w, w_code,
+                                   dx.data_ptr() if need_input else None, dx_across or 0,
+                                   dweight.data_ptr() if need_weights else None, dbias.data_ptr() if need_weights else None,
+                                   room.data_ptr() if need_weights else None, size, _cuda_stream(stream))
+    if rc:
+        _check(rc, "sbc_layer_norm_grad")
+    return dx, dweight, dbias
+
+
+def sbc_dropout(x: torch.Tensor, p: float, rng: torch.Tensor, at: int = 0, residual: Optional[torch.Tensor] = None,
+                out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """residual + x with elements dropped with probability p (a multiple of 2^-16) and the others scaled up.  ``rng``:
+    int64 [2] on the GPU, a key and a step; ``at``: where in the step's numbers this matrix begins, in groups of eight
+    elements.  The same call on the gradient (without a residual) is the backward pass.  ``out`` may be x or the residual."""
+    rows, cols, across, code = _matrix(x, "x")
+    if not (rng.is_cuda and rng.dtype == torch.int64 and rng.is_contiguous()):
+        raise TypeError("rng must be a contiguous int64 CUDA tensor")
+    if rng.numel() != 2:
+        raise ValueError("rng must hold a key and a step")
+    _beside(rng, x, "rng")
+    if not 0.0 <= p <= 1.0:
+        raise ValueError("p must be in 0 .. 1")
+    if not 0 <= at <= 1 << 62:
+        raise ValueError("at must be in 0 .. 2^62")
+    res, res_across = (None, 0) if residual is None else (residual.data_ptr(), _same(residual, x, "residual"))
+    out, out_across = _out(out, x.shape, x, stream)
+    rc = lib().sbc_dropout(x.data_ptr(), code, rows, cols, across, res, res_across, p, rng.data_ptr(), at, out.data_ptr(),
+                           out_across, _cuda_stream(stream))
+    if rc:
+        _check(rc, "sbc_dropout")
+    return out
+
+
+def _gated_desc(x, gate, up, act):
+    tokens, inner, across, code = _matrix(x, "x")
+    if code == 0:
+        raise TypeError("x must be bfloat16 or float16")
+    if act not in ACTIVATIONS:
+        raise ValueError(f"unknown activation {act!r}")
+    hidden = gate.shape[0] if gate.dim() == 2 else 0
+    gate_across, up_across = _same(gate, x, "gate", (hidden, inner)), _same(up, x, "up", (hidden, inner))
+    if hidden < 1 or inner < 1:
+        raise ValueError("gate and up must have at least one row and one column")
+    return tokens, inner, hidden, across, GatedDesc(gate.data_ptr(), up.data_ptr(), gate_across, up_across, hidden, inner, code,
+                                                    ACTIVATIONS[act])
+
+
+def sbc_gated(x: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, act: str = "silu", keep: bool = False,
+              out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
+    """act(x gate^T) * (x up^T), bfloat16 or float16, one token or many; with ``keep`` (that, what sbc_gated_grad takes:
+    float32, a pair for every token and hidden unit).  ``act``: silu, gelu, gelu_tanh, relu or sigmoid."""
+    tokens, inner, hidden, across, d = _gated_desc(x, gate, up, act)
+    out, out_across = _out(out, (tokens, hidden), x, stream)
+    kept = _empty(stream, (tokens, (hidden + 1) // 2 * 2, 2), torch.float32, x) if keep else None
+    size = int(lib().sbc_gated_workspace_bytes(C.byref(d), tokens, x.data_ptr(), across, keep, 0))
+    room = _empty(stream, size, torch.uint8, x) if size else None
+    rc = lib().sbc_gated(C.byref(d), x.data_ptr(), tokens, across, out.data_ptr(), out_across, kept.data_ptr() if keep else None,
+                         room.data_ptr() if size else None, size, _status(status, x), _cuda_stream(stream))
+    if rc:
+        _check(rc, "sbc_gated")
+    return (out, kept) if keep else out
+
+
+def sbc_gated_grad(dh: torch.Tensor, x: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, kept: torch.Tensor,
+                   need_input: bool = True, need_weights: bool = True, grad_dtype: Optional[torch.dtype] = None,
+                   status: Optional[torch.Tensor] = None, stream=None):
+    """(dx, dgate, dup), None where not asked for; the weights' gradients in their type or, by ``grad_dtype``, float32."""
+    tokens, inner, hidden, across, d = _gated_desc(x, gate, up, "silu")
+    dh_across = _same(dh, x, "dh", (tokens, hidden))
+    if not (kept.is_cuda and kept.dtype == torch.float32 and kept.is_contiguous()):
+        raise TypeError("kept must be a contiguous float32 CUDA tensor")
+    if kept.numel() != tokens * ((hidden + 1) // 2 * 4):
+        raise ValueError("kept is not of these sizes")
+    _beside(kept, x, "kept")
+    grad_dtype = x.dtype if grad_dtype is None else grad_dtype
+    if grad_dtype not in (x.dtype, torch.float32):
+        raise TypeError(f"grad_dtype must be float32 or {x.dtype}")
+    if not (need_input or need_weights):
+        return None, None, None
+    dx = _empty(stream, (tokens, inner), x.dtype, x) if need_input else None
+    dgate = dup = None
+    if need_weights:
+        dgate, dup = _empty(stream, (hidden, inner), grad_dtype, x), _empty(stream, (hidden, inner), grad_dtype, x)
+    size = int(lib().sbc_gated_workspace_bytes(C.byref(d), tokens, x.data_ptr(), across, 0, 1))
+    room = _empty(stream, size, torch.uint8, x) if size else None
+    rc = lib().sbc_gated_grad(C.byref(d), x.data_ptr(), tokens, across, dh.data_ptr(), dh_across, kept.data_ptr(),
+                              dx.data_ptr() if need_input else None, inner, dgate.data_ptr() if need_weights else None,
+                              dup.data_ptr() if need_weights else None, DTYPE_CODES[grad_dtype], inner,
+                              room.data_ptr() if size else None, size, _status(status, x), _cuda_stream(stream))
+    if rc:
+        _check(rc, "sbc_gated_grad")
+    return dx, dgate, dup
+
+
+class AdapterPlan:
+    """A batch's tokens grouped by their adapters: made once, for all layers that the batch goes through."""
+
+    __slots__ = ("room", "tokens", "count")
+
+    def __init__(self, room: torch.Tensor, tokens: int, count: int):
+        self.room, self.tokens, self.count = room, tokens, count
+
+
+class AdapterKept:
+    """What a forward call leaves for sbc_adapter_grad: x down^T in float32 [tokens, rank], and the plan."""
+
+    __slots__ = ("mid", "plan")
+
+    def __init__(self, mid: torch.Tensor, plan: AdapterPlan):
+        self.mid, self.plan = mid, plan
+
+
+def _ids(ids: torch.Tensor, tokens: Optional[int]) -> int:
+    if not (ids.is_cuda and ids.dtype == torch.int32 and ids.dim() == 1 and ids.is_contiguous()):
+        raise TypeError("ids must be a contiguous int32 CUDA vector")
+    if tokens is not None and ids.numel() != tokens:
+        raise ValueError("ids must hold one adapter per token")
+    return ids.data_ptr()
+
+
+def sbc_adapter_plan(ids: torch.Tensor, count: int, status: Optional[torch.Tensor] = None, stream=None) -> AdapterPlan:
+    """The plan of a batch whose token t has adapter ids[t] of ``count`` (negative: none; one that is not there counts as none,
+    and STATUS_RANGE is or-ed into ``status``)."""
+    at, tokens = _ids(ids, None), ids.numel()
+    if ids.get_device() != _current_device():
+        raise ValueError(f"ids is on {ids.device}, the current device is cuda:{_current_device()}")
+    size = int(lib().sbc_adapter_plan_bytes(tokens, count))
+    if not size:
+        raise ValueError(f"a plan takes up to 2^24 tokens and 1 .. {ADAPTER_COUNT} adapters")
+    room = _empty(stream, size, torch.uint8, ids)
+    rc = lib().sbc_adapter_plan(at, tokens, count, room.data_ptr(), size, _status(status, ids), _cuda_stream(stream))
+    if rc:
+        _check(rc, "sbc_adapter_plan")
+    return AdapterPlan(room, tokens, count)
+
+
+def _adapters(x: torch.Tensor, down: torch.Tensor, up: torch.Tensor):
+    for t, name in ((down, "down"), (up, "up")):
+        if not (t.is_cuda and t.dim() == 3 and t.is_contiguous() and t.dtype in (torch.float32, x.dtype)):
+            raise TypeError(f"{name} must be a contiguous float32 or {x.dtype} CUDA tensor [adapters, rank, features]")
+        _beside(t, x, name)
+    if down.dtype != up.dtype:
+        raise TypeError("down and up must be of one type")
+    count, rank, inner = down.shape
+    outer = up.shape[2]
+    if up.shape[:2] != down.shape[:2]:
+        raise ValueError("down and up must be [adapters, rank, features] with the same adapters and rank")
+    if not (1 <= count <= ADAPTER_COUNT and 1 <= rank <= ADAPTER_RANK and inner >= 1 and outer >= 1):
+        raise ValueError(f"1 .. {ADAPTER_COUNT} adapters of rank 1 .. {ADAPTER_RANK}")
+    return count, rank, inner, outer, AdaptersDesc(down.data_ptr(), up.data_ptr(), count, rank, inner, outer, DTYPE_CODES[down.dtype], 0)
+
+
+def _planned(plan: AdapterPlan, tokens: int, count: int, x: torch.Tensor) -> int:
+    if plan.tokens != tokens or plan.count != count:
+        raise ValueError(f"the plan is of {plan.tokens} tokens and {plan.count} adapters, not of {tokens} and {count}")
+    _beside(plan.room, x, "plan")
+    return plan.room.data_ptr()
+
+
+def sbc_adapter(x: torch.Tensor, down: torch.Tensor, up: torch.Tensor, ids: Optional[torch.Tensor], scale: float = 1.0,
+                base: Optional[torch.Tensor] = None, plan: Optional[AdapterPlan] = None, keep: bool = False,
+                out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
+    """base + scale (x down_i^T) up_i with i = ids[t] the adapter of token t (negative: none).  ``down`` [adapters, rank, in],
+    ``up`` [adapters, rank, out], float32 or of x's type; ``base`` is what the shared projection gave (None: zeros), ``out``
+    may be it.  ``plan`` (sbc_adapter_plan) saves grouping the tokens again for each layer, ids are then not read.  With
+    ``keep`` (that, AdapterKept)."""
+    tokens, cols, across, code = _matrix(x, "x")
+    count, rank, inner, outer, d = _adapters(x, down, up)
+    if cols != inner:
+        raise ValueError(f"x has {cols} features, down takes {inner}")
+    at = None
+    if plan is None:
+        if ids is None:
+            raise ValueError("ids or a plan")
+        at = _ids(ids, tokens)
+        _beside(ids, x, "ids")
+        if tokens > ADAPTER_FEW or keep:
+            plan = sbc_adapter_plan(ids, count, status, stream)
+    planned = None if plan is None else _planned(plan, tokens, count, x)
+    res, res_across = (None, 0) if base is None else (base.data_ptr(), _same(base, x, "base", (tokens, outer)))
+    out, out_across = _out(out, (tokens, outer), x, stream)
+    mid = None if plan is None else _empty(stream, (tokens, rank), torch.float32, x)
+    rc = lib().sbc_adapter(C.byref(d), x.data_ptr(), code, tokens, across, at, planned, scale, res, res_across, out.data_ptr(),
+                           out_across, None if mid is None else mid.data_ptr(), _status(status, x), _cuda_stream(stream))
+    if rc:
+        _check(rc, "sbc_adapter")
+    return (out, AdapterKept(mid, plan)) if keep else out
+
+
+def sbc_adapter_grad(dy: torch.Tensor, x: torch.Tensor, down: torch.Tensor, up: torch.Tensor, kept: AdapterKept,
+                     scale: float = 1.0, base: Optional[torch.Tensor] = None, need_input: bool = True,
+                     need_adapters: bool = True, out: Optional[torch.Tensor] = None, stream=None):
+    """(dx, ddown, dup), None where not asked for: dx = base + what the adapters give (``base``: the input's gradient through
+    the shared projection; ``out`` may be it), the adapters' gradients in their type, zeros for adapters without tokens."""
+    tokens, cols, across, code = _matrix(x, "x")
+    count, rank, inner, outer, d = _adapters(x, down, up)
+    if cols != inner:
+        raise ValueError(f"x has {cols} features, down takes {inner}")
+    dy_across = _same(dy, x, "dy", (tokens, outer))
+    planned = _planned(kept.plan, tokens, count, x)
+    mid = _rows_of(kept.mid, tokens * rank, torch.float32, "mid", x)
+    if not (need_input or need_adapters):
+        return None, None, None
+    dx = ddown = dup = None
+    dx_across = res_across = 0
+    res = None
+    if need_input:
+        if base is not None:
+            res, res_across = base.data_ptr(), _same(base, x, "base")
+        dx, dx_across = _out(out, (tokens, inner), x, stream)
+    if need_adapters:
+        ddown, dup = _empty(stream, down.shape, down.dtype, x), _empty(stream, up.shape, up.dtype, x)
+    dmid = _empty(stream, (tokens, rank), torch.float32, x)
+    rc = lib().sbc_adapter_grad(C.byref(d), dy.data_ptr(), dy_across, x.data_ptr(), across, code, tokens, planned, mid, scale, res,
+                                res_across, dx.data_ptr() if need_input else None, dx_across,
+                                ddown.data_ptr() if need_adapters else None, dup.data_ptr() if need_adapters else None,
+                                dmid.data_ptr(), _cuda_stream(stream))
+    if rc:
+        _check(rc, "sbc_adapter_grad")
+    return dx, ddown, dup

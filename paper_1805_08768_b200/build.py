@@ -16,7 +16,7 @@ NVCC_FLAGS = [
 ]
 # The method's kernels take their arithmetic as written (they are checked bit for bit): no fused
 # multiply-add contraction.  The language-model operators are held to tolerances and may fuse.
-SOURCES = {"sbc_api.cu": ["-fmad=false"], "lm_api.cu": []}
+SOURCES = {"sbc_api.cu": ["-fmad=false"], "lm_api.cu": [], "lm_block_api.cu": []}
 
 
 def _nvcc() -> str:

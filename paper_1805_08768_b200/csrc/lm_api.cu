@@ -1,9 +1,5 @@
 // C entry points of the language-model operators (include/sbc_lm.h).
-#include <algorithm>
-#include <atomic>
-#include <type_traits>
-
-#include "lm_common.cuh"
+#include "lm_host.cuh"
 #include "lm_logits.cuh"
 #include "lm_product.cuh"
 #include "lm_quantise.cuh"
@@ -11,36 +7,6 @@
 using namespace sbclm;
 
 namespace {
-
-constexpr int64_t kMaxDim = 0x7fffffff;
-
-int width_of(int dtype) { return dtype == SBC_F32 ? 4 : (dtype == SBC_BF16 || dtype == SBC_F16) ? 2 : 0; }
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
-
-// SMs of the current device (asked for once per device: the question costs as much as half a launch).
-int sm_count() {
-    static std::atomic<int> known[64];
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return 148;
-    if (dev < 64 && (n = known[dev].load(std::memory_order_relaxed)) > 0) return n;
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) return 148;
-    if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
-    return n;
-}
-
-// What every row of a matrix starts at a multiple of, at most 16 bytes.
-int row_align(const void* p, int64_t stride, int width) {
-    const uintptr_t bits = (uintptr_t)p | (uintptr_t)(stride * width) | 16u;
-    return (int)(bits & (~bits + 1));
-}
-
-// A matrix argument: base, type and stride fit together.
-bool matrix_ok(const void* p, int dtype, int64_t rows, int64_t cols, int64_t stride) {
-    const int width = width_of(dtype);
-    return p && width && aligned(p, (uintptr_t)width) && rows >= 0 && rows <= kMaxDim && cols >= 1 && cols <= kMaxDim && stride >= cols &&
-           stride <= (int64_t)1 << 40;
-}
 
 int64_t ktiles_of(int64_t cols, int format) { return ceil_div(cols, format == SBC_FP4_E8M0 ? 128 : 64); }
 
@@ -50,74 +16,15 @@ bool fp4_ok(const sbc_fp4* q) {
            (q->format == SBC_FP4_E8M0 || q->format == SBC_FP4_E4M3);
 }
 
-// dtype -> element type
-template <typename F> int by_dtype(int dtype, F f) {
-    switch (dtype) {
-        case SBC_F32: return f((float*)nullptr);
-        case SBC_BF16: return f((__nv_bfloat16*)nullptr);
-        case SBC_F16: return f((__half*)nullptr);
-    }
-    return SBC_EINVAL;
-}
-
-// Raises a kernel's limit of dynamic shared memory, once per device.
-template <auto Kernel> bool allow_smem(int bytes) {
-    static std::atomic<uint64_t> done{0};
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return false;
-    const uint64_t bit = 1ull << (dev & 63);
-    if (dev < 64 && (done.load(std::memory_order_relaxed) & bit)) return true;
-    if (cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
-    done.fetch_or(bit, std::memory_order_relaxed);
-    return true;
-}
-
 // Blocks that have a piece of a matrix for every warp.
 int64_t pieces(int64_t rows, int64_t cols, bool flat) {
     const int64_t n = flat ? ceil_div(rows * cols, kPiece) : rows * ceil_div(cols, kPiece);
     return ceil_div(n, kQThreads / 32);
 }
 
-// One launch: `cluster` blocks along `axis` (0: x, 2: z) together, allowed to start while the kernel in
-// front ends (the kernels wait for it themselves).
-template <typename... P, typename... A>
-int launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, int cluster, int axis, const A&... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = axis == 0 ? (unsigned)cluster : 1;
-    attr[1].val.clusterDim.y = axis == 1 ? (unsigned)cluster : 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = cluster > 0 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, P(args)...) == cudaSuccess ? SBC_OK : SBC_ECUDA;
-}
-
 template <typename T, int FMT> int launch_quantise(const QuantiseArgs& a, bool rows, bool cols, unsigned grid, cudaStream_t st) {
     const auto kernel = rows && cols ? k_fp4_quantise<T, FMT, true, true> : rows ? k_fp4_quantise<T, FMT, true, false> : k_fp4_quantise<T, FMT, false, true>;
     return launch(kernel, grid, kQThreads, 0, st, 0, 0, a);
-}
-
-typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiled encode_tiled() {
-    static const EncodeTiled fn = [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-            found != cudaDriverEntryPointSuccess)
-            p = nullptr;
-        return (EncodeTiled)p;
-    }();
-    return fn;
 }
 
 // Boxes of 128 bytes x `rows` of the elements' bytes, in the swizzle that the tensor cores read.
@@ -130,8 +37,6 @@ bool values_map(CUtensorMap* map, const sbc_fp4* q, int rows) {
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, q->values, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-
-constexpr int kSmemMost = 227 * 1024;
 
 template <typename T, int FMT>
 int launch_product(const CUtensorMap& mw, const CUtensorMap& mx, const ProductArgs& a, dim3 grid, int smem, cudaStream_t st) {

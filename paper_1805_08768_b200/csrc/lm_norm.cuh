@@ -1,0 +1,408 @@
+// Layer norm of rows, forward and backward.
+//
+//   y = h w + b with h = (x - m) s, m the row's mean, s = 1 / sqrt(mean((x - m)^2) + eps)
+//   dx = s (t - mean(t) - h mean(t h)) with t = dy w;  dw = sum over rows of dy h,  db = sum of dy
+//
+// Bound by memory: forward reads x and writes y, backward reads x and dy and writes dx.  A group of
+// threads holds a row in registers, so each is touched once; the variance is the second pass over those
+// registers (no difference of large sums).  Groups stay and take row after row, so the weights, and in the
+// backward pass the sums over rows, stay in registers too.  A row is cut into granules of eight elements
+// whose boundaries in memory are multiples of 16 bytes, wherever the row begins: rows of odd lengths load
+// and store whole granules, only the first and the last one element by element.  All rows of a group
+// begin at the same place within 16 bytes (their distance is a multiple of eight rows), so an element's
+// column, weight and sum never change registers.
+#pragma once
+
+#include "lm_common.cuh"
+
+namespace sbclm {
+
+constexpr int kNormThreads = 512;   // most threads of a group of the kernels that hold a row
+constexpr int kNormLong = 1024;     // threads of the kernels for longer rows
+
+struct NormArgs {
+    const void *x, *dy;
+    void* out;               // y or dx (NULL: not asked for)
+    const void *weight, *bias;
+    float2* stats;
+    float* partial;          // backward: sums of blocks, [block][2][cols]; NULL: not asked for
+    long long rows, x_stride, dy_stride, out_stride;
+    int cols, group, groups;  // threads that share a row, such groups in a block
+    int weight_f32;
+    float eps;
+};
+
+// Sum over the threads of a group, the same bits in all of them.  `buf` alternates between two places, so one barrier
+// separates a sum's reads from the next but one's writes.  All threads of the block take part.
+__device__ __forceinline__ float2 group_sum(float2 v, float2* red, int group_warps) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        v.x += __shfl_xor_sync(0xffffffffu, v.x, d);
+        v.y += __shfl_xor_sync(0xffffffffu, v.y, d);
+    }
+    if (group_warps == 1) return v;
+    const int warp = threadIdx.x >> 5, first = warp / group_warps * group_warps;
+    if ((threadIdx.x & 31) == 0) red[warp] = v;
+    __syncthreads();
+    float2 s = red[first];
+    for (int i = 1; i < group_warps; ++i) s.x += red[first + i].x, s.y += red[first + i].y;
+    return s;
+}
+
+__device__ __forceinline__ float weight_at(const void* p, long long i, int f32, const float*) { return static_cast<const float*>(p)[i]; }
+template <typename T> __device__ __forceinline__ float weight_at(const void* p, long long i, int f32, const T*) {
+    return f32 ? static_cast<const float*>(p)[i] : to_float(static_cast<const T*>(p)[i]);
+}
+
+// Where a granule of a row lies: elements lo .. hi of its eight are in the row, the first of which (lo = 0)
+// would be column `col`.
+struct Granule {
+    long long col;
+    int lo, hi;
+    __device__ __forceinline__ Granule(int i, int phase, int cols) {
+        col = 8ll * i - phase;
+        lo = (int)max(0ll, -col);
+        hi = (int)min(8ll, cols - col);
+    }
+    __device__ __forceinline__ bool whole() const { return lo == 0 && hi == 8; }
+};
+
+// `vec`: whole granules of these rows begin at multiples of 16 bytes.
+template <typename T> __device__ __forceinline__ void load_granule(Pack8<T>& v, const T* row, const Granule& g, bool vec) {
+    if (vec && g.whole()) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) v.q[i] = reinterpret_cast<const uint4*>(row + g.col)[i];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v.e[e] = e >= g.lo && e < g.hi ? row[g.col + e] : from_float<T>(0.f);
+    }
+}
+template <typename T> __device__ __forceinline__ void store_granule(T* row, const Pack8<T>& v, const Granule& g, bool vec) {
+    if (vec && g.whole()) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(row + g.col)[i] = v.q[i];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e >= g.lo && e < g.hi) row[g.col + e] = v.e[e];
+    }
+}
+
+template <typename T> __device__ __forceinline__ int phase_of(const T* row) { return (int)((uintptr_t)row / sizeof(T) % (16 / sizeof(T))); }
+
+// Whole granules of one row are whole granules of the other's memory too (for all rows of a group, if for its first).
+__device__ __forceinline__ bool same_phase(const void* p, const void* q) { return ((uintptr_t)p - (uintptr_t)q) % 16 == 0; }
+
+template <typename T, int NV> __global__ void __launch_bounds__(kNormThreads) k_norm(NormArgs a) {
+    __shared__ float2 red[2][kNormThreads / 32];
+    after_earlier_kernels();
+    const int t = threadIdx.x % a.group, warps = a.group / 32;
+    const long long all = (long long)gridDim.x * a.groups, first = (long long)blockIdx.x * a.groups + threadIdx.x / a.group;
+    const T* x = static_cast<const T*>(a.x) + first * a.x_stride;
+    T* y = static_cast<T*>(a.out) + first * a.out_stride;
+    const int phase = phase_of(x);
+    const bool vec = same_phase(x, y);
+    const float share = 1.f / (float)a.cols;
+    float w[NV * 8], b[NV * 8];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const Granule g(t + v * a.group, phase, a.cols);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const bool in = e >= g.lo && e < g.hi;
+            w[v * 8 + e] = !in ? 0.f : a.weight ? weight_at(a.weight, g.col + e, a.weight_f32, (const T*)nullptr) : 1.f;
+            b[v * 8 + e] = in && a.bias ? weight_at(a.bias, g.col + e, a.weight_f32, (const T*)nullptr) : 0.f;
+        }
+    }
+    Pack8<T> next[NV];
+    const auto fetch = [&](const T* row, bool live) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const Granule g(t + v * a.group, phase, a.cols);
+            if (live && g.hi > g.lo)
+                load_granule(next[v], row, g, true);
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e) next[v].e[e] = from_float<T>(0.f);
+        }
+    };
+    fetch(x, first < a.rows);
+    for (long long base = (long long)blockIdx.x * a.groups, r = first; base < a.rows; base += all, r += all, y += all * a.out_stride) {
+        float f[NV * 8];
+        float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < NV * 8; ++i) {
+            f[i] = to_float(next[i / 8].e[i % 8]);
+            sum.x += f[i];
+        }
+        x += all * a.x_stride;
+        fetch(x, r + all < a.rows);
+        const float mean = group_sum(sum, red[0], warps).x * share;
+        sum.x = 0.f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const Granule g(t + v * a.group, phase, a.cols);
+            if (!g.whole()) {   // what is not in the row is no distance from the mean
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (e < g.lo || e >= g.hi) f[v * 8 + e] = mean;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                f[v * 8 + e] -= mean;
+                sum.x = fmaf(f[v * 8 + e], f[v * 8 + e], sum.x);
+            }
+        }
+        const float rstd = 1.f / sqrtf(group_sum(sum, red[1], warps).x * share + a.eps);
+        if (r >= a.rows) continue;
+        if (t == 0 && a.stats) a.stats[r] = make_float2(mean, rstd);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const Granule g(t + v * a.group, phase, a.cols);
+            if (g.hi <= g.lo) continue;
+            Pack8<T> o;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o.e[e] = from_float<T>(fmaf(f[v * 8 + e] * rstd, w[v * 8 + e], b[v * 8 + e]));
+            store_granule(y, o, g, vec);
+        }
+    }
+}
+
+// The sums over rows stay in the registers of the threads that hold the columns until the block's last row.
+template <typename T, int NV> __global__ void __launch_bounds__(kNormThreads) k_norm_grad(NormArgs a) {
+    __shared__ float2 red[2][kNormThreads / 32];
+    after_earlier_kernels();
+    const int t = threadIdx.x % a.group, warps = a.group / 32;
+    const long long all = (long long)gridDim.x * a.groups, first = (long long)blockIdx.x * a.groups + threadIdx.x / a.group;
+    const T* x = static_cast<const T*>(a.x) + first * a.x_stride;
+    const T* dy = static_cast<const T*>(a.dy) + first * a.dy_stride;
+    T* dx = a.out ? static_cast<T*>(a.out) + first * a.out_stride : nullptr;
+    const int phase = phase_of(x);
+    const bool vec = same_phase(x, dx), vec_dy = same_phase(x, dy);
+    const float share = 1.f / (float)a.cols;
+    float w[NV * 8], dw[NV * 8], db[NV * 8];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const Granule g(t + v * a.group, phase, a.cols);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            w[v * 8 + e] = !(e >= g.lo && e < g.hi) ? 0.f : a.weight ? weight_at(a.weight, g.col + e, a.weight_f32, (const T*)nullptr) : 1.f;
+            dw[v * 8 + e] = db[v * 8 + e] = 0.f;
+        }
+    }
+    Pack8<T> next_x[NV], next_dy[NV];
+    float2 next_st = make_float2(0.f, 0.f);
+    const auto fetch = [&](const T* row, const T* dy_row, long long r) {
+        if (r < a.rows) next_st = a.stats[r];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const Granule g(t + v * a.group, phase, a.cols);
+            if (r < a.rows && g.hi > g.lo) {
+                load_granule(next_x[v], row, g, true);
+                load_granule(next_dy[v], dy_row, g, vec_dy);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) next_x[v].e[e] = next_dy[v].e[e] = from_float<T>(0.f);
+            }
+        }
+    };
+    fetch(x, dy, first);
+    int turn = 0;
+    for (long long base = (long long)blockIdx.x * a.groups, r = first; base < a.rows; base += all, r += all, dx += all * a.out_stride, turn ^= 1) {
+        const float2 st = next_st;
+        float h[NV * 8], d[NV * 8];
+        float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < NV * 8; ++i) {
+            // (a place outside of the row has dy = w = 0, and no h of it is used)
+            d[i] = to_float(next_dy[i / 8].e[i % 8]);
+            h[i] = (to_float(next_x[i / 8].e[i % 8]) - st.x) * st.y;
+            dw[i] = fmaf(d[i], h[i], dw[i]);
+            db[i] += d[i];
+            d[i] *= w[i];
+            sum.x += d[i];
+            sum.y = fmaf(d[i], h[i], sum.y);
+        }
+        x += all * a.x_stride;
+        dy += all * a.dy_stride;
+        fetch(x, dy, r + all);
+        if (!a.out) continue;
+        const float2 s = group_sum(sum, red[turn], warps);
+        if (r >= a.rows) continue;
+        const float mean = s.x * share, dot = s.y * share;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const Granule g(t + v * a.group, phase, a.cols);
+            if (g.hi <= g.lo) continue;
+            Pack8<T> o;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o.e[e] = from_float<T>(st.y * (d[v * 8 + e] - mean - h[v * 8 + e] * dot));
+            store_granule(dx, o, g, vec);
+        }
+    }
+    if (!a.partial) return;
+    // groups may have their granules at other places of a row, so they meet in shared memory, one after the other
+    extern __shared__ float sums[];
+    float* to = a.partial + (long long)blockIdx.x * 2 * a.cols;
+    for (int i = 0; i < a.groups; ++i) {
+        if (threadIdx.x / a.group == i) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const Granule g(t + v * a.group, phase, a.cols);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (e < g.lo || e >= g.hi) continue;
+                    const long long c = g.col + e;
+                    float p = dw[v * 8 + e], q = db[v * 8 + e];
+                    if (i > 0) p += sums[c], q += sums[a.cols + c];
+                    if (i + 1 < a.groups)
+                        sums[c] = p, sums[a.cols + c] = q;
+                    else
+                        to[c] = p, to[a.cols + c] = q;
+                }
+            }
+        }
+        if (i + 1 < a.groups) __syncthreads();
+    }
+}
+
+// Rows that no group holds: a block reads its row three times (the second and third time from the caches).
+template <typename T> __global__ void __launch_bounds__(kNormLong) k_norm_long(NormArgs a) {
+    __shared__ float2 red[2][kNormLong / 32];
+    after_earlier_kernels();
+    const float share = 1.f / (float)a.cols;
+    for (long long r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        const T* x = static_cast<const T*>(a.x) + r * a.x_stride;
+        T* y = static_cast<T*>(a.out) + r * a.out_stride;
+        const int phase = phase_of(x), n = (int)(((long long)a.cols + phase + 7) / 8);
+        const bool vec = same_phase(x, y);
+        float2 sum = make_float2(0.f, 0.f);
+        for (int i = threadIdx.x; i < n; i += kNormLong) {
+            const Granule g(i, phase, a.cols);
+            Pack8<T> v;
+            load_granule(v, x, g, true);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum.x += to_float(v.e[e]);
+        }
+        const float mean = group_sum(sum, red[0], kNormLong / 32).x * share;
+        sum.x = 0.f;
+        for (int i = threadIdx.x; i < n; i += kNormLong) {
+            const Granule g(i, phase, a.cols);
+            Pack8<T> v;
+            load_granule(v, x, g, true);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float d = e >= g.lo && e < g.hi ? to_float(v.e[e]) - mean : 0.f;
+                sum.x = fmaf(d, d, sum.x);
+            }
+        }
+        const float rstd = 1.f / sqrtf(group_sum(sum, red[1], kNormLong / 32).x * share + a.eps);
+        if (threadIdx.x == 0 && a.stats) a.stats[r] = make_float2(mean, rstd);
+        for (int i = threadIdx.x; i < n; i += kNormLong) {
+            const Granule g(i, phase, a.cols);
+            Pack8<T> v;
+            load_granule(v, x, g, true);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e >= g.lo && e < g.hi) {
+                    const float w = a.weight ? weight_at(a.weight, g.col + e, a.weight_f32, (const T*)nullptr) : 1.f;
+                    const float b = a.bias ? weight_at(a.bias, g.col + e, a.weight_f32, (const T*)nullptr) : 0.f;
+                    v.e[e] = from_float<T>(fmaf((to_float(v.e[e]) - mean) * rstd, w, b));
+                }
+            store_granule(y, v, g, vec);
+        }
+    }
+}
+
+// The block's sums over rows are in its part of `partial`, read and written by the thread that has the column: granules
+// here begin at column 0, so rows that begin elsewhere than at 16 bytes are taken element by element.
+template <typename T> __global__ void __launch_bounds__(kNormLong) k_norm_grad_long(NormArgs a) {
+    __shared__ float2 red[2][kNormLong / 32];
+    after_earlier_kernels();
+    const float share = 1.f / (float)a.cols;
+    const int n = (int)(((long long)a.cols + 7) / 8);
+    float* sums = a.partial ? a.partial + (long long)blockIdx.x * 2 * a.cols : nullptr;
+    int turn = 0;
+    for (long long r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
+        const T* x = static_cast<const T*>(a.x) + r * a.x_stride;
+        const T* dy = static_cast<const T*>(a.dy) + r * a.dy_stride;
+        T* dx = a.out ? static_cast<T*>(a.out) + r * a.out_stride : nullptr;
+        const bool vec_x = (uintptr_t)x % 16 == 0, vec_dy = (uintptr_t)dy % 16 == 0, vec = (uintptr_t)dx % 16 == 0;
+        const float2 st = a.stats[r];
+        float2 sum = make_float2(0.f, 0.f);
+        for (int i = threadIdx.x; i < n; i += kNormLong) {
+            const Granule g(i, 0, a.cols);
+            Pack8<T> v, d;
+            load_granule(v, x, g, vec_x);
+            load_granule(d, dy, g, vec_dy);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (e >= g.hi) break;
+                const float h = (to_float(v.e[e]) - st.x) * st.y, u = to_float(d.e[e]);
+                const float w = a.weight ? weight_at(a.weight, g.col + e, a.weight_f32, (const T*)nullptr) : 1.f;
+                sum.x = fmaf(u, w, sum.x);
+                sum.y = fmaf(u * w, h, sum.y);
+                if (sums) {
+                    float &dw = sums[g.col + e], &db = sums[a.cols + g.col + e];
+                    const bool begun = r != blockIdx.x;
+                    dw = fmaf(u, h, begun ? dw : 0.f);
+                    db = u + (begun ? db : 0.f);
+                }
+            }
+        }
+        if (!a.out) continue;
+        const float2 s = group_sum(sum, red[turn], kNormLong / 32);
+        const float mean = s.x * share, dot = s.y * share;
+        for (int i = threadIdx.x; i < n; i += kNormLong) {
+            const Granule g(i, 0, a.cols);
+            Pack8<T> v, d;
+            load_granule(v, x, g, vec_x);
+            load_granule(d, dy, g, vec_dy);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (e >= g.hi) break;
+                const float h = (to_float(v.e[e]) - st.x) * st.y;
+                const float w = a.weight ? weight_at(a.weight, g.col + e, a.weight_f32, (const T*)nullptr) : 1.f;
+                v.e[e] = from_float<T>(st.y * (to_float(d.e[e]) * w - mean - h * dot));
+            }
+            store_granule(dx, v, g, vec);
+        }
+    }
+}
+
+// The blocks' sums of a column: each row of threads takes every sixteenth block's, then one adds up the rows.
+constexpr int kNormSumCols = 32, kNormSumRows = 16;
+struct NormSumArgs {
+    const float* partial;
+    void *dweight, *dbias;
+    int cols, parts, f32, dtype;
+};
+__device__ __forceinline__ void store_as(void* p, long long i, float v, int dtype) {
+    if (dtype == SBC_F32) static_cast<float*>(p)[i] = v;
+    else if (dtype == SBC_BF16) static_cast<__nv_bfloat16*>(p)[i] = from_float<__nv_bfloat16>(v);
+    else static_cast<__half*>(p)[i] = from_float<__half>(v);
+}
+__global__ void __launch_bounds__(kNormSumCols * kNormSumRows) k_norm_sum(NormSumArgs a) {
+    __shared__ float part[kNormSumRows][kNormSumCols + 1];
+    after_earlier_kernels();
+    const int lane = threadIdx.x % kNormSumCols, row = threadIdx.x / kNormSumCols;
+    const long long c = (long long)blockIdx.x * kNormSumCols + lane;   // both rows of sums, one behind the other
+    float s = 0.f;
+    if (c < 2ll * a.cols) {
+        const float* p = a.partial + c;
+#pragma unroll 8
+        for (int i = row; i < a.parts; i += kNormSumRows) s += p[(long long)i * 2 * a.cols];
+    }
+    part[row][lane] = s;
+    __syncthreads();
+    if (row != 0 || c >= 2ll * a.cols) return;
+#pragma unroll
+    for (int i = 1; i < kNormSumRows; ++i) s += part[i][lane];
+    if (c < a.cols) {
+        if (a.dweight) store_as(a.dweight, c, s, a.dtype);
+    } else if (a.dbias) {
+        store_as(a.dbias, c - a.cols, s, a.dtype);
+    }
+}
+
+}  // namespace sbclm
