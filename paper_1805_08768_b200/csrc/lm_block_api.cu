@@ -133,11 +133,12 @@ int launch_mm(const CUtensorMap& r, const CUtensorMap& r2, const CUtensorMap& c,
     if (tiles > kMaxDim / 2) return SBC_EINVAL;
     a.tiles = (int)tiles;
     const int stage = (128 + NT / 2) * kMBytes;
-    a.stages = std::min(kMStages, (kSmemMost - 3 * 1024) / stage);
+    constexpr int swap = MODE == kForward || MODE == kForwardKeep ? kMSwap : 0;
+    a.stages = std::min(kMStages, (kSmemMost - 2 * 1024 - swap) / stage);
     if (!allow_smem<k_mm<T, O, MODE, NT>>(kSmemMost - 1024)) return SBC_ECUDA;
     const unsigned blocks = (unsigned)(2 * std::min<int64_t>(std::max(1, sm_count() / 2), tiles));
     // (always more than half of an SM's shared memory: a block takes up to all of its tensor memory)
-    return launch(k_mm<T, O, MODE, NT>, dim3(blocks), kMThreads, (size_t)(a.stages * stage + 1024), st, 2, 0, r, r2, c, c2, a);
+    return launch(k_mm<T, O, MODE, NT>, dim3(blocks), kMThreads, (size_t)(a.stages * stage + swap + 1024), st, 2, 0, r, r2, c, c2, a);
 }
 
 template <typename T> int lay_rows(const GatedLayout& l, cudaStream_t st) {
@@ -155,7 +156,7 @@ template <typename T, int MODE> int gated_forward(const sbc_gated_weights* w, co
     const bool wide = wide_columns(a.tiles_m, tokens, 1);
     a.tiles_n = (int)ceil_div(tokens, wide ? 256 : 128);
     CUtensorMap r, r2, c;
-    if (!half_map(&r, l.gate, w->hidden, w->inner, 16) || !half_map(&r2, l.up, w->hidden, w->inner, 16) ||
+    if (!half_map(&r, l.gate, w->hidden, w->inner, 64) || !half_map(&r2, l.up, w->hidden, w->inner, 64) ||
         !half_map(&c, l.x, tokens, w->inner, wide ? 128 : 64))
         return SBC_ECUDA;
     const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;

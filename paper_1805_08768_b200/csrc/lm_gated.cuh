@@ -20,13 +20,13 @@ namespace sbclm {
 // ---- activations ------------------------------------------------------------------------
 
 // act(g) and its derivative.  Sigmoids by exp(-g), so that small ones keep their digits.
-template <bool SLOPE> __device__ __forceinline__ void activate(float g, int act, float& value, float& slope) {
-    if (act == SBC_ACT_RELU) {
+template <int ACT, bool SLOPE> __device__ __forceinline__ void activate(float g, float& value, float& slope) {
+    if (ACT == SBC_ACT_RELU) {
         value = g < 0.f ? 0.f : g;   // (a NaN stays one)
         if (SLOPE) slope = g > 0.f ? 1.f : 0.f;
         return;
     }
-    if (act == SBC_ACT_GELU) {
+    if (ACT == SBC_ACT_GELU) {
         const float p = normcdff(g);
         value = g * p;
         if (SLOPE) slope = fmaf(g * 0.3989422804f, __expf(-0.5f * g * g), p);
@@ -34,18 +34,30 @@ template <bool SLOPE> __device__ __forceinline__ void activate(float g, int act,
     }
     // share = 1 / (1 + exp(-z))
     float z = g, dz = 1.f;
-    if (act == SBC_ACT_GELU_TANH) {
+    if (ACT == SBC_ACT_GELU_TANH) {
         z = 1.5957691216f * g * fmaf(0.044715f, g * g, 1.f);
         if (SLOPE) dz = 1.5957691216f * fmaf(3.f * 0.044715f, g * g, 1.f);
     }
     const float e = __expf(-z), share = __fdividef(1.f, 1.f + e);
     const float other = z > 0.f ? e * share : 1.f - share;
-    if (act == SBC_ACT_SIGMOID) {
+    if (ACT == SBC_ACT_SIGMOID) {
         value = share;
         if (SLOPE) slope = share * other;
     } else {
         value = g * share;
         if (SLOPE) slope = share * fmaf(g * dz, other, 1.f);
+    }
+}
+
+// f(constant) with the activation of that number: asked once for many elements.
+template <int N> struct Act { static constexpr int n = N; };
+template <typename F> __device__ __forceinline__ void by_act(int act, F f) {
+    switch (act) {
+        case SBC_ACT_SILU: return f(Act<SBC_ACT_SILU>());
+        case SBC_ACT_GELU: return f(Act<SBC_ACT_GELU>());
+        case SBC_ACT_GELU_TANH: return f(Act<SBC_ACT_GELU_TANH>());
+        case SBC_ACT_RELU: return f(Act<SBC_ACT_RELU>());
+        default: return f(Act<SBC_ACT_SIGMOID>());
     }
 }
 
@@ -58,15 +70,17 @@ template <bool SLOPE> __device__ __forceinline__ void activate(float g, int act,
 // it is high and its operands stay in L2 (one row of tiles at a time would read all of a large R from memory
 // for every 256 tokens).
 //
-// Forward: R is made of both weights, sixteen rows of G, the same sixteen of U, and so on, so the
-// two factors of a hidden unit are sixteen lanes apart in one warp.  Lanes below sixteen give their g of every
-// other token for the u of the tokens between: each ends with both factors of one token.
+// Forward: R is made of both weights, a block's lanes 0..63 are rows of G and 64..127 the same rows of U.  Of the two
+// warps that hold the two factors of the same units, each gives the other half of its tokens through shared memory and ends
+// with both factors of the rest.  (Sixteen rows of each in turn would leave both in one warp, but eight small boxes
+// a stage are slower to load than two: 8192 x 4096 -> 8192 without kept factors 964 us.)
 //
 // Warps: 0..7 accumulator to memory (half of the columns each four), 8 loads, 9 multiplies (in the pair's first block).
 
 constexpr int kMThreads = 320;
 constexpr int kMStages = 8;
 constexpr int kMBytes = 128;    // bytes of a row of a box: 64 elements
+constexpr int kMSwap = 8 * 2 * 16 * 32 * 4;   // bytes that eight warps swap factors through, twice sixteen tokens each
 enum { kForward, kForwardKeep, kInputGrad, kWeightGrad };
 
 struct MmArgs {
@@ -218,11 +232,8 @@ __global__ void __launch_bounds__(kMThreads, 1)
                     const bool next = i >= a.chunks;
                     const int k0 = (next ? i - a.chunks : i) * 64;
                     if (gated) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            tma_load_2d_pair(to + 4096u * j, &map_r, k0, m0 + 16 * j, bar);
-                            tma_load_2d_pair(to + 4096u * j + 2048u, &map_r2, k0, m0 + 16 * j, bar);
-                        }
+                        tma_load_2d_pair(to, &map_r, k0, m0, bar);
+                        tma_load_2d_pair(to + 8192u, &map_r2, k0, m0, bar);
                     } else {
                         const CUtensorMap* r = next ? &map_r2 : &map_r;
                         tma_load_2d_pair(to, r, m0, k0, bar);
@@ -301,30 +312,49 @@ __global__ void __launch_bounds__(kMThreads, 1)
                 if (lane == 0) mbar_arrive_remote(map_rank(acc_empty(b), 0));
             };
             if constexpr (gated) {
-                const long long unit = (long long)at.m * 128 + rank * 64 + sub * 16 + (lane & 15);
-                const bool up = lane >= 16;
-                const int have = unit < a.rows_m ? most - (up ? 1 : 0) : 0;
-                T* out = static_cast<T*>(a.out) + (n0 + (up ? 1 : 0)) * a.out_stride + unit;
-                float2* kept = MODE == kForwardKeep ? a.kept + (n0 + (up ? 1 : 0)) * a.kept_stride + unit : nullptr;
+                const long long unit = (long long)at.m * 128 + rank * 64 + (sub & 1) * 32 + lane;
+                const bool up = sub >= 2;
+                // this warp's half of every 32 tokens; the other's go to the partner's place
+                const int have = unit < a.rows_m ? most - (up ? 16 : 0) : 0;
+                T* out = static_cast<T*>(a.out) + (n0 + (up ? 16 : 0)) * a.out_stride + unit;
+                float2* kept = MODE == kForwardKeep ? a.kept + (n0 + (up ? 16 : 0)) * a.kept_stride + unit : nullptr;
+                const uint32_t swap = smem + (uint32_t)a.stages * stage_bytes + (uint32_t)lane * 4u;
+                const uint32_t give = swap + (uint32_t)(warp ^ 2) * 2048u, take = swap + (uint32_t)warp * 2048u;
+                const int meet = 1 + (warp >> 2) * 2 + (sub & 1);
 #pragma unroll 1
                 for (int c0 = 0; c0 < kCols; c0 += 32) {
+                    const uint32_t half = (uint32_t)(c0 & 32) * (kMSwap / 64);
                     float v[32];
                     tmem_load32(v, acc + c0);
                     if (c0 + 32 == kCols) free();
 #pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        const float got = __shfl_xor_sync(0xffffffffu, up ? v[i] : v[i + 1], 16);
-                        float value, slope = 0.f;
-                        const float g = up ? got : v[i], u = up ? v[i + 1] : got;
-                        activate<MODE == kForwardKeep>(g, a.act, value, slope);
-                        if (!ok) value = slope = __uint_as_float(0x7fffffffu);
-                        if (c0 + i < have) {
-                            *out = from_float<T>(value * u);
-                            if (MODE == kForwardKeep) *kept = make_float2(u * slope, value);
-                        }
-                        out += 2 * a.out_stride;
-                        if (MODE == kForwardKeep) kept += 2 * a.kept_stride;
+                    for (int i = 0; i < 16; ++i)
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(give + half + 128u * i), "f"(up ? v[i] : v[16 + i]) : "memory");
+                    asm volatile("bar.sync %0, 64;" ::"r"(meet) : "memory");
+                    float g[16], u[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float got;
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(got) : "r"(take + half + 128u * i) : "memory");
+                        g[i] = up ? got : v[i];
+                        u[i] = up ? v[16 + i] : got;
+                        if (!ok) g[i] = u[i] = __uint_as_float(0x7fffffffu);
                     }
+                    by_act(a.act, [&](auto which) {
+                        T* to = out + c0 * a.out_stride;
+                        float2* keep = kept + c0 * a.kept_stride;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            float value, slope = 0.f;
+                            activate<decltype(which)::n, MODE == kForwardKeep>(g[i], value, slope);
+                            if (c0 + i < have) {
+                                *to = from_float<T>(value * u[i]);
+                                if (MODE == kForwardKeep) *keep = make_float2(u[i] * slope, value);
+                            }
+                            to += a.out_stride;
+                            if (MODE == kForwardKeep) keep += a.kept_stride;
+                        }
+                    });
                 }
             } else {
                 const long long m = (long long)at.m * 256 + rank * 128 + sub * 32 + lane;
@@ -441,7 +471,7 @@ template <typename T, int TT, int UT> __global__ void __launch_bounds__(kFThread
         const long long unit = unit0 + 8 * i + (at >> 2);
         const int tok = 8 * j + (at & 3) * 2 + e;
         float value, slope;
-        activate<false>(gs, a.act, value, slope);
+        by_act(a.act, [&](auto which) { activate<decltype(which)::n, false>(gs, value, slope); });
         if (unit < a.hidden && tok < a.tokens) static_cast<T*>(a.h)[tok * a.h_stride + unit] = from_float<T>(value * us);
     }
 }
