@@ -148,7 +148,7 @@ int sbc_gated_grad(const sbc_gated_weights *w, const void *x, int64_t tokens, in
 
 /* ---- low-rank adapters ---------------------------------------------------------- */
 
-#define SBC_ADAPTER_RANK 256   /* largest rank */
+#define SBC_ADAPTER_RANK 128   /* largest rank */
 #define SBC_ADAPTER_FEW 64     /* most tokens of a call without a plan */
 #define SBC_ADAPTER_COUNT 32768 /* most adapters */
 

@@ -887,7 +887,7 @@ def sbc_distill_loss_grad(logits: torch.Tensor, values: torch.Tensor, indices: t
 # ---- operators of a client's own layers (include/sbc_block.h) ------------------------
 
 ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}
-ADAPTER_RANK, ADAPTER_FEW, ADAPTER_COUNT = 256, 64, 32768
+ADAPTER_RANK, ADAPTER_FEW, ADAPTER_COUNT = 128, 64, 32768
 
 
 def _same(t: torch.Tensor, like: torch.Tensor, name: str, shape=None) -> int:

@@ -21,15 +21,14 @@
 
 #include "../../include/sbc_block.h"
 #include "lm_common.cuh"
+#include "lm_product.cuh"
 
 namespace sbclm {
 
 constexpr int kATile = 64;        // tokens of a tile
 constexpr int kAThreads = 256;
 constexpr int kAFewThreads = 256;
-constexpr int kAGradThreads = 128;
 constexpr int kAPlanThreads = 1024;
-constexpr int kARank = 64;        // rank rows that a block takes at a time
 
 // ---- plan -----------------------------------------------------------------------------------
 
@@ -62,14 +61,21 @@ __global__ void __launch_bounds__(kAPlanThreads) k_adapter_plan(PlanArgs a) {
     const int first = (int)min((long long)a.tokens, (long long)warp * run), last = warp < a.warps ? (int)min((long long)a.tokens, (long long)first + run) : first;
     int* mine = counters + (long long)min(warp, a.warps - 1) * bins;
     bool beyond = false;
-    for (int t0 = first; t0 < last; t0 += 32) {
-        const bool in = t0 + lane < last;
-        const int id = in ? a.ids[t0 + lane] : -1;
-        beyond |= id >= a.count;
-        const int bin = in ? adapter_of(id, a.count) : -1;
-        const unsigned same = __match_any_sync(0xffffffffu, bin);
-        if (in && (same & ((1u << lane) - 1)) == 0) mine[bin] += __popc(same);
-        __syncwarp();
+    constexpr int kSteps = 8;   // ids of so many steps are loaded together
+    for (int t0 = first; t0 < last; t0 += 32 * kSteps) {
+        int ids[kSteps];
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) ids[i] = t0 + 32 * i + lane < last ? a.ids[t0 + 32 * i + lane] : -1;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            if (t0 + 32 * i >= last) break;
+            const bool in = t0 + 32 * i + lane < last;
+            beyond |= ids[i] >= a.count;
+            const int bin = in ? adapter_of(ids[i], a.count) : -1;
+            const unsigned same = __match_any_sync(0xffffffffu, bin);
+            if (in && (same & ((1u << lane) - 1)) == 0) mine[bin] += __popc(same);
+            __syncwarp();
+        }
     }
     if (beyond && a.status) atomicOr(a.status, SBC_STATUS_RANGE);
     __syncthreads();
@@ -110,18 +116,25 @@ __global__ void __launch_bounds__(kAPlanThreads) k_adapter_plan(PlanArgs a) {
         a.plan.offsets[bins] = a.tokens;
         a.plan.tiles[0] = make_int4(before.y, 0, 0, 0);
     }
-    for (int t0 = first; t0 < last; t0 += 32) {
-        const bool in = t0 + lane < last;
-        const int bin = in ? adapter_of(a.ids[t0 + lane], a.count) : -1;
-        const unsigned same = __match_any_sync(0xffffffffu, bin), ahead = same & ((1u << lane) - 1);
-        int at = 0;
-        if (in && ahead == 0) {
-            at = mine[bin];
-            mine[bin] = at + __popc(same);
+    for (int t0 = first; t0 < last; t0 += 32 * kSteps) {
+        int ids[kSteps];
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) ids[i] = t0 + 32 * i + lane < last ? a.ids[t0 + 32 * i + lane] : -1;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            if (t0 + 32 * i >= last) break;
+            const bool in = t0 + 32 * i + lane < last;
+            const int bin = in ? adapter_of(ids[i], a.count) : -1;
+            const unsigned same = __match_any_sync(0xffffffffu, bin), ahead = same & ((1u << lane) - 1);
+            int at = 0;
+            if (in && ahead == 0) {
+                at = mine[bin];
+                mine[bin] = at + __popc(same);
+            }
+            at = __shfl_sync(0xffffffffu, at, __ffs(same) - 1) + __popc(ahead);
+            if (in) a.plan.order[at] = t0 + 32 * i + lane;
+            __syncwarp();
         }
-        at = __shfl_sync(0xffffffffu, at, __ffs(same) - 1) + __popc(ahead);
-        if (in) a.plan.order[at] = t0 + lane;
-        __syncwarp();
     }
 }
 
@@ -217,14 +230,77 @@ __device__ __forceinline__ void add_products(float (*acc)[4], const uint16_t* p,
     }
 }
 
-// (plain loads: what they read may be written in place)
-template <typename T> __device__ __forceinline__ void read8(Pack8<T>& v, const T* p, int have, bool vec) {
-    if (have >= 8 && vec) {
+// ---- a thread's own ring in shared memory ---------------------------------------------------
+//
+// Loads run ahead of the products by stages of such a ring: a thread copies eight elements at a time to places that it alone reads,
+// so nothing but its own wait stands between the two, registers hold only what the products take next, and an
+// SM has 100 KB and more under way.  A pack's granules of 16 bytes are 512 bytes apart: a warp's are side by side.
+
+// Copies `have` elements (at most 8, zeros behind them) whose address is a multiple of `align`.  VEC: of 16 bytes, and all
+// eight or none.  SHARED: other warps load the same, so it may stay in the first-level cache.
+template <bool VEC, bool SHARED, typename T> __device__ __forceinline__ void ring_load(uint32_t to, const T* p, int have, int align) {
+    constexpr int kEach = 16 / (int)sizeof(T);
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) v.q[i] = reinterpret_cast<const uint4*>(p)[i];
-    } else {
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i, to += 512, p += kEach, have -= kEach) {
+        if (VEC) {
+            const int bytes = have > 0 ? 16 : 0;
+            if (SHARED)
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(p), "r"(bytes) : "memory");
+            else
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(p), "r"(bytes) : "memory");
+            continue;
+        }
+        const int bytes = max(0, min(16, have * (int)sizeof(T)));
+        if (align >= 4) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v.e[e] = e < have ? p[e] : from_float<T>(0.f);
+            for (int k = 0; k < 4; ++k)
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + 4 * k), "l"(reinterpret_cast<const char*>(p) + 4 * k),
+                             "r"(max(0, min(4, bytes - 4 * k)))
+                             : "memory");
+        } else {
+            union {
+                T e[kEach];
+                uint4 q;
+            } v;
+            v.q = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int k = 0; k < kEach; ++k)
+                if (k * (int)sizeof(T) < bytes) v.e[k] = p[k];
+            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(v.q.x), "r"(v.q.y), "r"(v.q.z), "r"(v.q.w) : "memory");
+        }
+    }
+}
+template <typename T> __device__ __forceinline__ void ring_read(Pack8<T>& v, uint32_t from) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(v.q[i].x), "=r"(v.q[i].y), "=r"(v.q[i].z), "=r"(v.q[i].w)
+                     : "r"(from + 512 * i)
+                     : "memory");
+}
+template <typename T> constexpr uint32_t kPackBytes = 32 * 8 * sizeof(T);   // of a warp
+__device__ __forceinline__ void ring_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// Waits until at most `left` (0 .. 7) of this thread's groups of copies are under way.
+__device__ __forceinline__ void ring_wait(int left) {
+    switch (left) {
+        case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
+        case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+        case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+        case 3: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+        case 4: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
+        case 5: asm volatile("cp.async.wait_group 5;" ::: "memory"); break;
+        case 6: asm volatile("cp.async.wait_group 6;" ::: "memory"); break;
+        default: asm volatile("cp.async.wait_group 7;" ::: "memory"); break;
+    }
+}
+
+template <typename T> __device__ __forceinline__ void pack8(Pack8<T>& v, const float* f) {
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        if constexpr (sizeof(T) == 4)
+            v.e[e] = f[e], v.e[e + 1] = f[e + 1];
+        else
+            v.w[e / 2] = pack2(f[e], f[e + 1], (const T*)nullptr);
     }
 }
 template <typename T> __device__ __forceinline__ void write8(T* p, const Pack8<T>& v, int have, bool vec) {
@@ -239,96 +315,154 @@ template <typename T> __device__ __forceinline__ void write8(T* p, const Pack8<T
 }
 
 struct AdapterArgs {
-    const void* x;          // the wide input (x or dy) of mid, or what is added up over tokens
+    const void* x;          // the wide input (x or dy)
     const void* factor;     // [count][rank][wide]
     const void* base;
-    void* out;              // y or dx; [count][rank][wide] gradients
+    void* out;              // y or dx
     float* mid;             // [tokens][rank]
     AdapterPlan plan;
     long long x_stride, base_stride, out_stride;
     int count, rank, wide, parts;
-    int align_x, align_factor;
+    int align_x, align_base, align_out, align_factor;
     float scale;
 };
 
 // ---- into the rank ------------------------------------------------------------------------------
 
 // mid[t][j] = scale sum_k x[t][k] factor[i][j][k] for a tile of tokens and up to 8 JT rows.  A thread takes eight neighbours
-// of a row, its four k's of two products (which element is which k is free as long as both operands agree).  Warps are
-// two halves of the tokens and four runs of the wide axis, blocks of a cluster share it further; sums meet
-// in shared memory in a fixed order.
-template <typename T, typename W, int JT> __global__ void __launch_bounds__(kAThreads) k_adapter_in(AdapterArgs a) {
-    constexpr int X = Terms<T>::n, Y = Terms<W>::n, MT = 2, kPer = MT * JT * 4;
-    extern __shared__ float sums[];   // [8 warps][kPer][32]
+// of a row, its four k's of two products (which element is which k is free as long as both operands agree).  A warp has half
+// of the tokens, so that two blocks fit an SM's registers; warps, and blocks of a cluster, take the wide axis in turns.  Their
+// sums meet in shared memory in a fixed order.  VEC: all rows begin at multiples of 16 bytes.
+template <typename T, typename W, int JT> struct InShape {
+    static constexpr int MT = 2, kHalves = 4 / MT, kRuns = 8 / kHalves, kPer = MT * JT * 4;
+    static constexpr int kStage = MT * 2 * (int)kPackBytes<T> + JT * (int)kPackBytes<W>;   // of a warp
+    // two blocks of an SM share it while each has two stages
+    static constexpr int kFit = 108 * 1024 / (8 * kStage), kStages = kFit >= 4 ? 4 : kFit >= 2 ? kFit : 200 * 1024 / (8 * kStage) >= 3 ? 3 : 2;
+    static constexpr int kSmem = 8 * (kStages * kStage > kPer * 128 ? kStages * kStage : kPer * 128);
+};
+template <typename T, typename W, int JT, bool VEC>
+__global__ void __launch_bounds__(kAThreads, Terms<T>::n + Terms<W>::n <= 3 ? 2 : 1) k_adapter_in(AdapterArgs a) {
+    using S = InShape<T, W, JT>;
+    constexpr int X = Terms<T>::n, Y = Terms<W>::n, MT = S::MT, kPer = S::kPer;
+    extern __shared__ __align__(16) uint8_t raw[];   // rings of the warps; in the end sums [8 warps][kPer][32]
     __shared__ int tokens[kATile];
     after_earlier_kernels();
     const int part = (int)blockIdx.x % a.parts, tile = (int)blockIdx.x / a.parts;
     if (tile >= a.plan.tiles[0].x) return;
     const int4 at = a.plan.tiles[1 + tile];
     if (at.x >= a.count) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3, half = warp & 1, run = warp >> 1;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3, half = warp % S::kHalves, run = warp / S::kHalves;
     const int j0 = (int)blockIdx.y * 8 * JT;
     if (threadIdx.x < kATile) tokens[threadIdx.x] = threadIdx.x < at.z ? a.plan.order[at.y + threadIdx.x] : -1;
     __syncthreads();
     const T* x[MT][2];
-    bool live[MT][2];
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int t = tokens[half * 32 + m * 16 + h * 8 + g];
-            live[m][h] = t >= 0;
-            x[m][h] = static_cast<const T*>(a.x) + (long long)max(t, 0) * a.x_stride;
+            x[m][h] = t < 0 ? nullptr : static_cast<const T*>(a.x) + (long long)t * a.x_stride;
         }
-    const W* f[JT];
-#pragma unroll
-    for (int j = 0; j < JT; ++j) f[j] = static_cast<const W*>(a.factor) + ((long long)at.x * a.rank + min(j0 + 8 * j + g, a.rank - 1)) * a.wide;
+    const W* factor = static_cast<const W*>(a.factor) + ((long long)at.x * a.rank + j0 + g) * a.wide;
+    const int rows = a.rank - j0 - g;   // of the factor, this thread's first among them
+    const uint32_t ring = smem_u32(raw) + (uint32_t)(warp * S::kStages * S::kStage) + 16u * lane;
     float acc[MT][JT][4] = {};
-    if (half * 32 < at.z) {
-        const int units = (a.wide + 31) / 32;   // of 32 elements; this block's run of them
-        const int u0 = (int)((long long)units * part / a.parts), u1 = (int)((long long)units * (part + 1) / a.parts);
-        for (int u = u0 + run; u < u1; u += 4) {
+    const int left = at.z - half * 32;   // tokens of this warp
+    const int units = (a.wide + 31) / 32;   // of 32 elements; this block's run of them
+    const int u0 = (int)((long long)units * part / a.parts), u1 = left > 0 ? (int)((long long)units * (part + 1) / a.parts) : u0;
+    const auto fill = [&](int u, int stage) {
+        if (u < u1) {
             const int k = u * 32 + q * 8, have = a.wide - k;
-            Pack8<T> xs[MT][2];
-            Pack8<W> fs[JT];
+            uint32_t to = ring + (uint32_t)(stage * S::kStage);
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+            for (int m = 0; m < MT; ++m) {
+                if (m * 16 >= left) break;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) load8(xs[m][h], x[m][h] + k, live[m][h] ? have : 0, a.align_x);
-#pragma unroll
-            for (int j = 0; j < JT; ++j) load8(fs[j], f[j] + k, j0 + 8 * j + g < a.rank ? have : 0, a.align_factor);
-            uint32_t xt[MT][2][X][4];
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) cut_row<X>(xt[m][h], xs[m][h]);
+                for (int h = 0; h < 2; ++h)
+                    ring_load<VEC, false>(to + (m * 2 + h) * kPackBytes<T>, x[m][h] ? x[m][h] + k : static_cast<const T*>(a.x), x[m][h] ? have : 0, a.align_x);
+            }
+            to += MT * 2 * kPackBytes<T>;
 #pragma unroll
             for (int j = 0; j < JT; ++j) {
-                uint32_t ft[Y][4];
-                cut_row<Y>(ft, fs[j]);
+                const bool in = 8 * j < rows;
+                ring_load<VEC, true>(to + j * kPackBytes<W>, in ? factor + (long long)(8 * j) * a.wide + k : static_cast<const W*>(a.factor), in ? have : 0, a.align_factor);
+            }
+        }
+        ring_commit();
+    };
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    float part[4] = {};
-                    float* d = sizeof(W) == 4 ? part : acc[m][j];
+    for (int s = 0; s < S::kStages - 1; ++s) fill(u0 + run + s * S::kRuns, s);
+    int stage = 0;
+    for (int u = u0 + run; u < u1; u += S::kRuns) {
+        fill(u + (S::kStages - 1) * S::kRuns, stage == 0 ? S::kStages - 1 : stage - 1);
+        ring_wait(S::kStages - 1);
+        const uint32_t from = ring + (uint32_t)(stage * S::kStage);
+        if (++stage == S::kStages) stage = 0;
+        // all of the factor's terms where they are few, otherwise all of x's
+        constexpr bool kHold = JT * Y <= MT * 2 * X;
+        uint32_t held[kHold ? JT : MT * 2][kHold ? Y : X][4];
+        if constexpr (kHold) {
 #pragma unroll
-                    for (int order = 2; order >= 0; --order)   // the small products first
+            for (int j = 0; j < JT; ++j) {
+                Pack8<W> v;
+                ring_read(v, from + MT * 2 * kPackBytes<T> + j * kPackBytes<W>);
+                cut_row<Y>(held[j], v);
+            }
+        } else {
 #pragma unroll
-                        for (int n = 0; n < X; ++n) {
-                            const int o = order - n;
-                            if (o < 0 || o >= Y) continue;
+            for (int m = 0; m < MT * 2; ++m) {
+                if (m * 8 >= left) break;
+                Pack8<T> v;
+                ring_read(v, from + m * kPackBytes<T>);
+                cut_row<X>(held[m], v);
+            }
+        }
 #pragma unroll
-                            for (int s = 0; s < 4; s += 2) {
-                                const uint32_t w[4] = {xt[m][0][n][s], xt[m][1][n][s], xt[m][0][n][s + 1], xt[m][1][n][s + 1]};
-                                mma_terms(d, w, ft[o][s], ft[o][s + 1]);
-                            }
-                        }
-                    if (sizeof(W) == 4)
+        for (int outer = 0; outer < (kHold ? MT : JT); ++outer) {
+            uint32_t now[kHold ? 2 : 1][kHold ? X : Y][4];
+            if constexpr (kHold) {
+                if (outer * 16 >= left) break;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[m][j][e] += part[e];
+                for (int h = 0; h < 2; ++h) {
+                    Pack8<T> v;
+                    ring_read(v, from + (outer * 2 + h) * kPackBytes<T>);
+                    cut_row<X>(now[h], v);
                 }
+            } else {
+                Pack8<W> v;
+                ring_read(v, from + MT * 2 * kPackBytes<T> + outer * kPackBytes<W>);
+                cut_row<Y>(now[0], v);
+            }
+#pragma unroll
+            for (int inner = 0; inner < (kHold ? JT : MT); ++inner) {
+                const int m = kHold ? outer : inner, j = kHold ? inner : outer;
+                if (!kHold && m * 16 >= left) break;
+                float part_sum[4] = {};
+                float* d = sizeof(W) == 4 ? part_sum : acc[m][j];
+#pragma unroll
+                for (int order = 2; order >= 0; --order)   // the small products first
+#pragma unroll
+                    for (int n = 0; n < X; ++n) {
+                        const int o = order - n;
+                        if (o < 0 || o >= Y) continue;
+#pragma unroll
+                        for (int s = 0; s < 4; s += 2) {
+                            const uint32_t(&r0)[4] = kHold ? now[0][n] : held[m * 2 % (kHold ? JT : MT * 2)][n];
+                            const uint32_t(&r1)[4] = kHold ? now[kHold ? 1 : 0][n] : held[(m * 2 + 1) % (kHold ? JT : MT * 2)][n];
+                            const uint32_t(&f)[4] = kHold ? held[j % (kHold ? JT : MT * 2)][o] : now[0][o];
+                            const uint32_t w[4] = {r0[s], r1[s], r0[s + 1], r1[s + 1]};
+                            mma_terms(d, w, f[s], f[s + 1]);
+                        }
+                    }
+                if (sizeof(W) == 4)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[m][j][e] += part_sum[e];
             }
         }
     }
+    ring_wait(0);
+    __syncthreads();   // all rings are read: sums take their place
+    float* sums = reinterpret_cast<float*>(raw);
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -336,26 +470,26 @@ template <typename T, typename W, int JT> __global__ void __launch_bounds__(kATh
 #pragma unroll
             for (int e = 0; e < 4; ++e) sums[(warp * kPer + (m * JT + j) * 4 + e) * 32 + lane] = acc[m][j][e];
     __syncthreads();
-    // [2 halves][kPer][32] sums of four warps, left in the first ones' places for the cluster
-    const auto place = [&](int i, int w) { return (((i / (kPer * 32)) + 2 * w) * kPer * 32) + i % (kPer * 32); };
+    // [halves][kPer][32] sums of kRuns warps, left in the first ones' places for the cluster
+    constexpr int kSums = S::kHalves * kPer * 32;
     const auto store = [&](int i, float v) {
         const int n = i % 32, e = i / 32 % 4, j = i / 128 % JT, m = i / (128 * JT);   // m: halves and their tiles
         const int t = m * 16 + (e >> 1) * 8 + (n >> 2), r = j0 + 8 * j + (n & 3) * 2 + (e & 1);
         if (t < at.z && r < a.rank) a.mid[(long long)tokens[t] * a.rank + r] = v * a.scale;
     };
-    for (int i = threadIdx.x; i < 2 * kPer * 32; i += kAThreads) {
-        float v = sums[place(i, 0)];
+    for (int i = threadIdx.x; i < kSums; i += kAThreads) {
+        float v = sums[i];
 #pragma unroll
-        for (int w = 1; w < 4; ++w) v += sums[place(i, w)];
+        for (int w = 1; w < S::kRuns; ++w) v += sums[i + w * kSums];
         if (a.parts == 1)
             store(i, v);
         else
-            sums[place(i, 0)] = v;
+            sums[i] = v;
     }
     if (a.parts == 1) return;
     cluster_sync();
-    for (int i = part * kAThreads + threadIdx.x; i < 2 * kPer * 32; i += a.parts * kAThreads) {
-        const uint32_t from = smem_u32(&sums[place(i, 0)]);
+    for (int i = part * kAThreads + threadIdx.x; i < kSums; i += a.parts * kAThreads) {
+        const uint32_t from = smem_u32(&sums[i]);
         float v = 0.f;
         for (int p = 0; p < a.parts; ++p) v += ld_cluster(map_rank(from, (uint32_t)p));
         store(i, v);
@@ -365,12 +499,25 @@ template <typename T, typename W, int JT> __global__ void __launch_bounds__(kATh
 
 // ---- out of the rank ------------------------------------------------------------------------------
 
-// out[t][c] = base[t][c] + scale sum_j mid[t][j] factor[i][j][c].  A warp has 32 tokens x 64 columns at a time.  mid's terms
-// wait in shared memory; a thread loads eight neighbours of four rows of the factor, whose pairs are the products' words (which
-// column is which of a product's eight is free, too), and ends with sixteen neighbours of four rows of out.
-template <typename T, typename W> __global__ void __launch_bounds__(kAThreads) k_adapter_out(AdapterArgs a) {
+// out[t][c] = base[t][c] + scale sum_j mid[t][j] factor[i][j][c].  A warp has 32 tokens x 64 columns at a
+// time.  mid's terms wait in shared memory; a thread loads eight neighbours of four rows of the factor, whose pairs are
+// the products' words (which column is which of a product's eight is free, too), and ends with sixteen
+// neighbours of each of its rows of out.
+template <typename T, typename W> struct OutShape {
     // 16-bit results: what lies 2^-16 below a factor does not reach them
-    constexpr int X = sizeof(T) == 4 ? 3 : 2, Y = sizeof(T) == 4 ? Terms<W>::n : (Terms<W>::n < 2 ? Terms<W>::n : 2), MT = 2;
+    static constexpr int X = sizeof(T) == 4 ? 3 : 2, Y = sizeof(T) == 4 ? Terms<W>::n : (Terms<W>::n < 2 ? Terms<W>::n : 2);
+    static constexpr int MT = 2, kHalves = 4 / MT, kColumns = 8 / kHalves * 64;   // of a block at a time
+    static constexpr int kBase = MT * 4 * (int)kPackBytes<T>, kStage = 4 * (int)kPackBytes<W>;   // of a warp
+    // base: one buffer, loaded while the tile's products are made, or, where those are a single step, two
+    static __host__ __device__ constexpr int pitch(int rank) { return (rank + 15) / 16 * 16 + 8; }
+    static __host__ __device__ constexpr int buffers(int rank) { return rank <= 16 ? 2 : 1; }
+    static __host__ __device__ constexpr int stages(int rank) { return rank <= 16 ? 2 : 3; }
+    static __host__ __device__ constexpr int smem(int rank) { return 8 * (buffers(rank) * kBase + stages(rank) * kStage) + X * kATile * pitch(rank) * 2; }
+};
+template <typename T, typename W, bool VEC>
+__global__ void __launch_bounds__(kAThreads, sizeof(W) == 2 ? 2 : 1) k_adapter_out(AdapterArgs a) {
+    using S = OutShape<T, W>;
+    constexpr int X = S::X, Y = S::Y, MT = S::MT;
     extern __shared__ __align__(16) uint8_t raw[];
     __shared__ int tokens[kATile];
     after_earlier_kernels();
@@ -378,12 +525,64 @@ template <typename T, typename W> __global__ void __launch_bounds__(kAThreads) k
     const int4 at = a.plan.tiles[1 + blockIdx.x];
     const bool none = at.x >= a.count;
     if (none && a.base == a.out) return;
-    const int steps = none ? 0 : (a.rank + 15) / 16, pitch = (a.rank + 15) / 16 * 16 + 8;
-    uint16_t* terms = reinterpret_cast<uint16_t*>(raw);   // [X][kATile][pitch]
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3, half = warp & 1;
+    const int pitch = S::pitch(a.rank), steps = none ? 1 : (a.rank + 15) / 16, buffers = S::buffers(a.rank), stages = S::stages(a.rank);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3, half = warp % S::kHalves;
+    const uint32_t base_ring = smem_u32(raw) + (uint32_t)(warp * buffers * S::kBase) + 16u * lane;
+    const uint32_t ring = smem_u32(raw) + (uint32_t)(8 * buffers * S::kBase + warp * stages * S::kStage) + 16u * lane;
+    uint16_t* terms = reinterpret_cast<uint16_t*>(raw + 8 * (buffers * S::kBase + stages * S::kStage));   // [X][kATile][pitch]
     if (threadIdx.x < kATile) tokens[threadIdx.x] = threadIdx.x < at.z ? a.plan.order[at.y + threadIdx.x] : -1;
     __syncthreads();
-    for (int i = threadIdx.x; i < kATile * steps * 16; i += kAThreads) {
+    const int left = at.z - half * 32;
+    int row[MT][2];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) row[m][h] = tokens[half * 32 + m * 16 + h * 8 + g];
+    const W* factor = static_cast<const W*>(a.factor) + (long long)(none ? 0 : at.x) * a.rank * a.wide;
+    const int first = ((int)blockIdx.y * (8 / S::kHalves) + warp / S::kHalves) * 64, across = (int)gridDim.y * S::kColumns;
+    const int mine = left > 0 && first < a.wide ? (a.wide - first + across - 1) / across : 0;   // this warp's tiles of columns
+    const auto fill_base = [&](int n) {
+        const int col = first + n * across + 16 * q;
+        const uint32_t to = base_ring + (uint32_t)((buffers == 2 ? n & 1 : 0) * S::kBase);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            if (m * 16 >= left) break;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    const int have = a.base && row[m][h] >= 0 ? a.wide - col - 8 * p : 0;
+                    const T* from = static_cast<const T*>(have > 0 ? a.base : a.x);
+                    ring_load<VEC, false>(to + ((m * 2 + h) * 2 + p) * kPackBytes<T>, have > 0 ? from + (long long)row[m][h] * a.base_stride + col + 8 * p : from, have, a.align_base);
+                }
+        }
+    };
+    const auto fill_factor = [&](int n, int s, int stage) {
+        const int fc = first + n * across + 8 * g;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int j = s * 16 + 2 * q + (k & 1) + (k >> 1) * 8, have = !none && j < a.rank ? a.wide - fc : 0;
+            ring_load<VEC, true>(ring + (uint32_t)(stage * S::kStage) + k * kPackBytes<W>, have > 0 ? factor + (long long)j * a.wide + fc : factor, have, a.align_factor);
+        }
+    };
+    // `ahead` steps of the factor are under way; one group of copies a step
+    const int ahead = min(steps, stages - 1);
+    int fn = 0, fs = 0, fstage = 0;   // the step that is loaded next
+    const auto fill = [&]() {
+        if (fn < mine) {
+            if (buffers == 2) fill_base(fn);   // (a single step: base comes with it)
+            fill_factor(fn, fs, fstage);
+        }
+        if (++fs == steps) fs = 0, ++fn;
+        if (++fstage == stages) fstage = 0;
+        ring_commit();
+    };
+    if (buffers == 2) {
+        fill();   // (a second one would need a third buffer)
+    } else {
+        for (int i = 0; i < ahead; ++i) fill();
+    }
+    for (int i = threadIdx.x; !none && i < kATile * steps * 16; i += kAThreads) {
         const int t = i / (steps * 16), j = i - t * steps * 16;
         uint32_t w[X];
         cut<X>(w, tokens[t] >= 0 && j < a.rank ? a.mid[(long long)tokens[t] * a.rank + j] : 0.f);
@@ -391,41 +590,35 @@ template <typename T, typename W> __global__ void __launch_bounds__(kAThreads) k
         for (int n = 0; n < X; ++n) terms[(n * kATile + t) * pitch + j] = (uint16_t)(w[n] >> 16);
     }
     __syncthreads();
-    if (half * 32 >= at.z) return;
-    const W* factor = static_cast<const W*>(a.factor) + (long long)at.x * a.rank * a.wide;
-    const bool vec_base = a.align_x >= 16;   // (align_x: of base and out)
-    int row[MT][2];
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) row[m][h] = tokens[half * 32 + m * 16 + h * 8 + g];
-    for (int c0 = ((int)blockIdx.y * 4 + (warp >> 1)) * 64; c0 < a.wide; c0 += (int)gridDim.y * 256) {
-        const int col = c0 + 16 * q;     // of base and out
-        Pack8<T> b[MT][2][2];
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int p = 0; p < 2; ++p)
-                    read8(b[m][h][p], static_cast<const T*>(a.base) + (a.base ? (long long)row[m][h] * a.base_stride + col + 8 * p : 0),
-                          a.base && row[m][h] >= 0 ? a.wide - col - 8 * p : 0, vec_base);
+    int stage = 0;
+    for (int n = 0; n < mine; ++n) {
         float acc[MT][8][4] = {};
-        const int fc = c0 + 8 * g, have = a.wide - fc;   // of the factor
+        if (buffers == 1) fill_base(n);   // (with the next group)
         for (int s = 0; s < steps; ++s) {
-            Pack8<W> f[4];
+            fill();
+            ring_wait(buffers == 2 ? 1 : ahead);
+            if (!none) {
+                const uint32_t from = ring + (uint32_t)(stage * S::kStage);
+                uint32_t lo[Y][8], hi[Y][8];
+                Pack8<W> f, f2;
+                ring_read(f, from);
+                ring_read(f2, from + kPackBytes<W>);
+                cut_rows<Y>(lo, f, f2);
+                ring_read(f, from + 2 * kPackBytes<W>);
+                ring_read(f2, from + 3 * kPackBytes<W>);
+                cut_rows<Y>(hi, f, f2);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int j = s * 16 + 2 * q + (k & 1) + (k >> 1) * 8;
-                load8(f[k], factor + (long long)min(j, a.rank - 1) * a.wide + fc, j < a.rank ? have : 0, a.align_factor);
+                for (int m = 0; m < MT; ++m) {
+                    if (m * 16 >= left) break;
+                    add_products<X, Y, sizeof(T) == 4>(acc[m], terms + (half * 32 + m * 16 + g) * pitch + s * 16 + 2 * q, kATile * pitch, pitch, lo, hi);
+                }
             }
-            uint32_t lo[Y][8], hi[Y][8];
-            cut_rows<Y>(lo, f[0], f[1]);
-            cut_rows<Y>(hi, f[2], f[3]);
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-                add_products<X, Y, sizeof(T) == 4>(acc[m], terms + (half * 32 + m * 16 + g) * pitch + s * 16 + 2 * q, kATile * pitch, pitch, lo, hi);
+            if (++stage == stages) stage = 0;
         }
+        // base came with the group of the tile's first step
+        if (buffers == 1) ring_wait(min(ahead, steps - 1));
+        const uint32_t from = base_ring + (uint32_t)((buffers == 2 ? n & 1 : 0) * S::kBase);
+        const int col = first + n * across + 16 * q;
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -434,99 +627,167 @@ template <typename T, typename W> __global__ void __launch_bounds__(kAThreads) k
 #pragma unroll
                 for (int p = 0; p < 2; ++p) {
                     Pack8<T> v;
+                    ring_read(v, from + ((m * 2 + h) * 2 + p) * kPackBytes<T>);
+                    if (!none) {
+                        float f[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v.e[e] = none ? b[m][h][p].e[e] : from_float<T>(fmaf(a.scale, acc[m][e][2 * h + p], to_float(b[m][h][p].e[e])));
-                    write8(static_cast<T*>(a.out) + (long long)row[m][h] * a.out_stride + col + 8 * p, v, a.wide - col - 8 * p, vec_base);
+                        for (int e = 0; e < 8; ++e) f[e] = fmaf(a.scale, acc[m][e][2 * h + p], to_float(v.e[e]));
+                        pack8(v, f);
+                    }
+                    write8(static_cast<T*>(a.out) + (long long)row[m][h] * a.out_stride + col + 8 * p, v, a.wide - col - 8 * p, VEC || a.align_out >= 16);
                 }
             }
     }
+    ring_wait(0);
 }
 
 // ---- over tokens ------------------------------------------------------------------------------------
 
-// out[i][j][c] = scale sum over the tokens t of adapter i of mid[t][j] x[t][c].  A warp has 64 columns and up to 16 RT rows; 64
-// tokens' terms of mid are laid out in shared memory with the tokens as the contiguous axis, x is loaded as the factor above.
-// Blocks of a cluster share an adapter's tokens, and add their sums in their order.
-template <typename T, typename W, int RT> __global__ void __launch_bounds__(kAGradThreads) k_adapter_grad(AdapterArgs a) {
-    constexpr int X = sizeof(W) == 4 ? 3 : 2, Y = sizeof(W) == 4 ? Terms<T>::n : (Terms<T>::n < 2 ? Terms<T>::n : 2), pitch = kATile + 8;
-    extern __shared__ __align__(16) uint8_t raw[];
-    __shared__ int tokens[kATile];
-    uint16_t* terms = reinterpret_cast<uint16_t*>(raw);   // [X][16 RT][pitch], and in the end sums [32 RT][threads]
-    float* sums = reinterpret_cast<float*>(raw);
+// out[i][j][c] = scale sum over the tokens t of adapter i of mid[t][j] x[t][c], for one or two such sums in a launch.  A warp
+// has 64 columns and 16 RT rows, the warps of a block 512 columns and, for ranks above 32, twice as many rows.  64 tokens' terms of mid are laid out in shared memory with the tokens as the
+// contiguous axis, x is loaded as the factor above.  Blocks of a cluster share an adapter's tokens, and add their sums in their order.
+struct AdapterSum {
+    const void* x;
+    const float* mid;
+    void* out;             // [count][rank][wide]
+    long long x_stride;
+    int wide, columns;     // blocks of columns
+    int align_x, align_out;
+    float scale;
+};
+struct AdapterGradArgs {
+    AdapterSum sums[2];
+    AdapterPlan plan;
+    int count, rank, parts;
+    int first;             // blocks of the first sum
+};
+template <typename T, typename W, int RT, int RH> struct GradShape {
+    static constexpr int X = sizeof(W) == 4 ? 3 : 2, Y = sizeof(W) == 4 ? Terms<T>::n : (Terms<T>::n < 2 ? Terms<T>::n : 2), kPitch = kATile + 8;
+    static constexpr int kThreads = kAThreads * RH, kRows = 16 * RT * RH;
+    static constexpr int kStage = 4 * (int)kPackBytes<T>, kStages = sizeof(T) == 4 ? 3 : 5;   // of a warp
+    static constexpr int kRings = 8 * RH * kStages * kStage, kTerms = X * kRows * kPitch * 2, kSums = RT * 32 * kThreads * 4;
+    static constexpr int kSmem = kRings + kTerms > kSums ? kRings + kTerms : kSums;
+};
+template <typename T, typename W, int RT, int RH, bool VEC>
+__global__ void __launch_bounds__(kAThreads * RH, RH == 1 && Terms<T>::n + Terms<W>::n <= 3 ? 2 : 1) k_adapter_grad(const __grid_constant__ AdapterGradArgs b) {
+    using S = GradShape<T, W, RT, RH>;
+    constexpr int X = S::X, Y = S::Y, pitch = S::kPitch, kRows = S::kRows, kThreads = S::kThreads;
+    extern __shared__ __align__(16) uint8_t raw[];   // rings of the warps, terms [X][kRows][pitch]; in the end sums [32 RT][threads]
     after_earlier_kernels();
-    const int part = (int)(blockIdx.x % a.parts), blocks = (a.rank + 16 * RT - 1) / (16 * RT);
-    const int columns = (int)(((long long)a.wide + kAGradThreads * 2 - 1) / (kAGradThreads * 2)), at_row = (int)(blockIdx.x / a.parts / columns);
-    const int i = at_row / blocks, j0 = at_row % blocks * 16 * RT, ranks = min(16 * RT, a.rank - j0);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-    const long long cb = (long long)(blockIdx.x / a.parts % columns) * (kAGradThreads * 2);
-    const long long c0 = cb + warp * 64 + 8 * g;
+    const bool second = (int)blockIdx.x >= b.first;
+    const AdapterSum& a = b.sums[second ? 1 : 0];
+    const int block = (int)blockIdx.x - (second ? b.first : 0);
+    const int part = block % b.parts, blocks = (b.rank + kRows - 1) / kRows, at_row = block / b.parts / a.columns;
+    const int i = at_row / blocks, j0 = at_row % blocks * kRows, ranks = min(kRows, b.rank - j0);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3, group = warp % 8, row0 = warp / 8 * 16 * RT;
+    const long long cb = (long long)(block / b.parts % a.columns) * (kAThreads * 2);
+    const long long c0 = cb + group * 64 + 8 * g;
     const int have = (int)max(0ll, min(8ll, a.wide - c0));
-    const int begin = a.plan.offsets[i], groups = (a.plan.offsets[i + 1] - begin + 15) / 16, end = a.plan.offsets[i + 1];
-    const int g0 = (int)((long long)groups * part / a.parts), g1 = (int)((long long)groups * (part + 1) / a.parts);
+    const bool idle = cb + group * 64 >= a.wide || row0 >= ranks;
+    const int begin = b.plan.offsets[i], end = b.plan.offsets[i + 1], groups = (end - begin + 15) / 16;
+    const int t_first = begin + (int)((long long)groups * part / b.parts) * 16, t_last = min(end, begin + (int)((long long)groups * (part + 1) / b.parts) * 16);
+    uint16_t* terms = reinterpret_cast<uint16_t*>(raw + S::kRings);
+    const uint32_t ring = smem_u32(raw) + (uint32_t)(warp * S::kStages * S::kStage) + 16u * lane;
     float acc[RT][8][4] = {};
-    for (int t0 = begin + g0 * 16; t0 < min(end, begin + g1 * 16); t0 += kATile) {
-        const int n_tokens = min(kATile, min(end, begin + g1 * 16) - t0);
-        __syncthreads();
-        if (threadIdx.x < kATile) tokens[threadIdx.x] = threadIdx.x < n_tokens ? a.plan.order[t0 + threadIdx.x] : -1;
-        __syncthreads();
-        for (int n = threadIdx.x; n < kATile * 16 * RT; n += kAGradThreads) {
-            const int t = n / (16 * RT), j = n % (16 * RT);
-            uint32_t w[X];
-            cut<X>(w, tokens[t] >= 0 && j < ranks ? a.mid[(long long)tokens[t] * a.rank + j0 + j] : 0.f);
-#pragma unroll
-            for (int k = 0; k < X; ++k) terms[(k * 16 * RT + j) * pitch + t] = (uint16_t)(w[k] >> 16);
-        }
-        Pack8<T> next[4];
-        const auto fetch = [&](int s) {
+    if (t_first < t_last) {   // (the same in all threads)
+        const T* x = static_cast<const T*>(a.x) + c0;
+        // this thread's rows of sixteen tokens, asked for a step before their copies
+        int rows[4];
+        const auto ask = [&](int t0) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int t = tokens[s * 16 + 2 * q + (k & 1) + (k >> 1) * 8];
-                load8(next[k], static_cast<const T*>(a.x) + (long long)max(t, 0) * a.x_stride + c0, t >= 0 ? have : 0, a.align_x);
+                const int t = t0 + 2 * q + (k & 1) + (k >> 1) * 8;
+                rows[k] = t < t_last && have > 0 ? b.plan.order[t] : -1;
             }
         };
-        fetch(0);
-        __syncthreads();
-#pragma unroll 1
-        for (int s = 0; s * 16 < n_tokens; ++s) {
-            uint32_t lo[Y][8], hi[Y][8];
-            cut_rows<Y>(lo, next[0], next[1]);
-            cut_rows<Y>(hi, next[2], next[3]);
-            if ((s + 1) * 16 < n_tokens) fetch(s + 1);
+        int t_next = t_first, fstage = 0;
+        const auto fill = [&]() {
+            if (t_next < t_last && !idle)
 #pragma unroll
-            for (int m = 0; m < RT; ++m)
-                add_products<X, Y, sizeof(W) == 4>(acc[m], terms + (m * 16 + g) * pitch + s * 16 + 2 * q, 16 * RT * pitch, pitch, lo, hi);
+                for (int k = 0; k < 4; ++k)
+                    ring_load<VEC, (RH > 1)>(ring + (uint32_t)(fstage * S::kStage) + k * kPackBytes<T>, rows[k] >= 0 ? x + (long long)rows[k] * a.x_stride : static_cast<const T*>(a.x),
+                              rows[k] >= 0 ? have : 0, a.align_x);
+            ring_commit();
+            if (++fstage == S::kStages) fstage = 0;
+            t_next += 16;
+            ask(t_next);
+        };
+        ask(t_first);
+        for (int s = 0; s < S::kStages - 1; ++s) fill();
+        int stage = 0;
+        for (int t0 = t_first; t0 < t_last; t0 += kATile) {
+            const int n_tokens = min(kATile, t_last - t0);
+            __syncthreads();   // the terms before are read
+            // two tokens and four rows of mid a thread: words of two tokens' terms
+            for (int n = threadIdx.x; n < kATile / 2 * kRows / 4; n += kThreads) {
+                const int j = n % 4 + n / 128 * 4, t = n / 4 % 32 * 2;   // j: fours of rows
+                uint32_t w[2][4][X];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int tok = t + h < n_tokens ? b.plan.order[t0 + t + h] : -1;
+                    const float* p = a.mid + (long long)max(tok, 0) * b.rank + j0 + 4 * j;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) cut<X>(w[h][k], tok >= 0 && 4 * j + k < ranks ? p[k] : 0.f);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int m = 0; m < X; ++m) *reinterpret_cast<uint32_t*>(terms + (m * kRows + 4 * j + k) * pitch + t) = halves(w[0][k][m], w[1][k][m]);
+            }
+            __syncthreads();
+#pragma unroll 1
+            for (int s = 0; s * 16 < n_tokens; ++s) {
+                fill();
+                ring_wait(S::kStages - 1);
+                if (!idle) {
+                    const uint32_t from = ring + (uint32_t)(stage * S::kStage);
+                    uint32_t lo[Y][8], hi[Y][8];
+                    Pack8<T> f, f2;
+                    ring_read(f, from);
+                    ring_read(f2, from + kPackBytes<T>);
+                    cut_rows<Y>(lo, f, f2);
+                    ring_read(f, from + 2 * kPackBytes<T>);
+                    ring_read(f2, from + 3 * kPackBytes<T>);
+                    cut_rows<Y>(hi, f, f2);
+#pragma unroll
+                    for (int m = 0; m < RT; ++m)
+                        add_products<X, Y, sizeof(W) == 4>(acc[m], terms + (row0 + m * 16 + g) * pitch + s * 16 + 2 * q, kRows * pitch, pitch, lo, hi);
+                }
+                if (++stage == S::kStages) stage = 0;
+            }
         }
+        ring_wait(0);
+        __syncthreads();
     }
-    __syncthreads();
+    float* sums = reinterpret_cast<float*>(raw);
 #pragma unroll
     for (int m = 0; m < RT; ++m)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
 #pragma unroll
-            for (int n = 0; n < 4; ++n) sums[((m * 8 + e) * 4 + n) * kAGradThreads + threadIdx.x] = acc[m][e][n];
-    if (a.parts > 1)
+            for (int n = 0; n < 4; ++n) sums[((m * 8 + e) * 4 + n) * kThreads + threadIdx.x] = acc[m][e][n];
+    if (b.parts > 1)
         cluster_sync();
     else
         __syncthreads();
     // a thread: eight neighbours of a row, summed over the cluster's blocks
-    W* out = static_cast<W*>(a.out) + ((long long)i * a.rank + j0) * a.wide;
-    const bool vec = a.align_factor >= 16;
-    for (int n = part * kAGradThreads + threadIdx.x; n < 16 * RT * 32; n += a.parts * kAGradThreads) {
-        const int j = n / 32, w = n % 32 / 8, qq = n % 8 / 2, r8 = j % 16;
-        const int at = (j / 16 * 32 + (n & 1) + (r8 >> 3) * 2) * kAGradThreads + w * 32 + (r8 & 7) * 4 + qq;
+    W* out = static_cast<W*>(a.out) + ((long long)i * b.rank + j0) * a.wide;
+    for (int n = part * kThreads + threadIdx.x; n < kRows * 64; n += b.parts * kThreads) {
+        const int j = n / 64, w = n % 64 / 8, qq = n % 8 / 2, r8 = j % 16;
+        const int at = (j / 16 % RT * 32 + (n & 1) + (r8 >> 3) * 2) * kThreads + (j / (16 * RT) * 8 + w) * 32 + (r8 & 7) * 4 + qq;
         const long long c = cb + w * 64 + 8 * (n % 8);
         if (j >= ranks || c >= a.wide) continue;
         Pack8<W> v;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const uint32_t from = smem_u32(&sums[at + e * 4 * kAGradThreads]);
+            const uint32_t from = smem_u32(&sums[at + e * 4 * kThreads]);
             float s = 0.f;
-            for (int p = 0; p < a.parts; ++p) s += a.parts > 1 ? ld_cluster(map_rank(from, (uint32_t)p)) : sums[at + e * 4 * kAGradThreads];
+            for (int p = 0; p < b.parts; ++p) s += b.parts > 1 ? ld_cluster(map_rank(from, (uint32_t)p)) : sums[at + e * 4 * kThreads];
             v.e[e] = from_float<W>(s * a.scale);
         }
-        write8(out + (long long)j * a.wide + c, v, (int)min(8ll, a.wide - c), vec);
+        write8(out + (long long)j * a.wide + c, v, (int)min(8ll, a.wide - c), a.align_out >= 16);
     }
-    if (a.parts > 1) cluster_sync();
+    if (b.parts > 1) cluster_sync();
 }
 
 // ---- single tokens -------------------------------------------------------------------------------------

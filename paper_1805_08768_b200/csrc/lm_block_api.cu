@@ -243,19 +243,24 @@ template <typename F> int by_types(int dtype, int weights, F f) {
     });
 }
 
-// Blocks of a cluster that share a sum, where there are fewer pieces of work than keep the GPU busy; a block keeps `least` of `length`.
-int shares(int64_t pieces, int64_t length, int64_t least) {
+template <typename F> int by_vec(bool vec, F f) { return vec ? f(std::true_type()) : f(std::false_type()); }
+
+// Blocks of a cluster that share a sum, while there are fewer pieces of work than `most` blocks; each has at least `least` of `length`.
+int shares(int64_t pieces, int64_t most, int64_t length, int64_t least) {
     int parts = 1;
-    while (parts < 8 && pieces * parts < 2 * sm_count() && length >= least * parts * 2) parts *= 2;
+    while (parts < 8 && pieces * parts * 2 <= most && length >= least * parts * 2) parts *= 2;
     return parts;
 }
 
 template <typename T, typename W, int JT> int launch_in(AdapterArgs a, int64_t tiles, cudaStream_t st) {
+    using S = InShape<T, W, JT>;
     const int64_t blocks = ceil_div(a.rank, 8 * JT);
-    const int smem = 8 * 2 * JT * 4 * 32 * 4;
-    if (!allow_smem<k_adapter_in<T, W, JT>>(smem)) return SBC_ECUDA;
-    a.parts = shares(tiles * blocks, a.wide, 256);
-    return launch(k_adapter_in<T, W, JT>, dim3((unsigned)(tiles * a.parts), (unsigned)blocks), kAThreads, (size_t)smem, st, a.parts, 0, a);
+    a.parts = shares(tiles * blocks, 4 * sm_count(), a.wide, 512);
+    return by_vec(a.align_x >= 16 && a.align_factor >= 16, [&](auto vec) {
+        constexpr auto kernel = k_adapter_in<T, W, JT, decltype(vec)::value>;
+        if (!allow_smem<kernel>(S::kSmem)) return (int)SBC_ECUDA;
+        return launch(kernel, dim3((unsigned)(tiles * a.parts), (unsigned)blocks), kAThreads, S::kSmem, st, a.parts, 0, a);
+    });
 }
 
 // mid = scale x factor^T
@@ -274,38 +279,54 @@ int adapter_in(AdapterArgs a, int dtype, int weights, int64_t tokens, cudaStream
 // out = base + scale mid factor
 int adapter_out(AdapterArgs a, int dtype, int weights, int64_t tokens, cudaStream_t st) {
     const int width = width_of(dtype);
-    a.align_x = std::min(a.base ? row_align(a.base, a.base_stride, width) : 16, row_align(a.out, a.out_stride, width));
+    a.align_base = a.base ? row_align(a.base, a.base_stride, width) : 16;
+    a.align_out = row_align(a.out, a.out_stride, width);
     a.align_factor = row_align(a.factor, a.wide, width_of(weights));
     const int64_t tiles = most_tiles(tokens, a.count);
     return by_types(dtype, weights, [&](auto* t, auto* w) {
         using T = std::remove_pointer_t<decltype(t)>;
         using W = std::remove_pointer_t<decltype(w)>;
-        const int pitch = (int)ceil_div(a.rank, 16) * 16 + 8, smem = 3 * kATile * pitch * 2;
-        if (!allow_smem<k_adapter_out<T, W>>(3 * kATile * (SBC_ADAPTER_RANK + 8) * 2)) return (int)SBC_ECUDA;
+        using S = OutShape<T, W>;
+        constexpr int most = std::max(S::smem(16), S::smem(SBC_ADAPTER_RANK));
+        static_assert(most <= kSmemMost - 1024, "a block's shared memory");
         // four blocks an SM, each with mid's terms once
-        const int64_t columns = std::min<int64_t>(ceil_div(a.wide, 256), std::max<int64_t>(1, ceil_div((int64_t)sm_count() * 4, tiles)));
-        return launch(k_adapter_out<T, W>, dim3((unsigned)tiles, (unsigned)columns), kAThreads, (size_t)smem, st, 0, 0, a);
+        const int64_t columns = std::min<int64_t>(ceil_div(a.wide, S::kColumns), std::max<int64_t>(1, ceil_div((int64_t)sm_count() * 4, tiles)));
+        return by_vec(a.align_base >= 16 && a.align_out >= 16 && a.align_factor >= 16, [&](auto vec) {
+            constexpr auto kernel = k_adapter_out<T, W, decltype(vec)::value>;
+            if (!allow_smem<kernel>(most)) return (int)SBC_ECUDA;
+            return launch(kernel, dim3((unsigned)tiles, (unsigned)columns), kAThreads, (size_t)S::smem(a.rank), st, 0, 0, a);
+        });
     });
 }
 
-template <typename T, typename W, int RT> int launch_adapter_grad(AdapterArgs a, int64_t tokens, cudaStream_t st) {
-    const int64_t columns = ceil_div(a.wide, kAGradThreads * 2), rows = ceil_div(a.rank, 16 * RT) * a.count;
-    if (columns * rows > kMaxDim / 8) return SBC_EINVAL;
-    const int smem = std::max(RT * 32 * kAGradThreads * 4, 3 * 16 * RT * (kATile + 8) * 2);
-    if (!allow_smem<k_adapter_grad<T, W, RT>>(smem)) return SBC_ECUDA;
-    a.parts = shares(columns * rows, tokens, 64);
-    return launch(k_adapter_grad<T, W, RT>, dim3((unsigned)(columns * rows * a.parts)), kAGradThreads, (size_t)smem, st, a.parts, 0, a);
+template <typename T, typename W, int RT, int RH> int launch_adapter_grad(AdapterGradArgs a, int64_t tokens, cudaStream_t st) {
+    using S = GradShape<T, W, RT, RH>;
+    static_assert(S::kSmem <= kSmemMost - 1024, "a block's shared memory");
+    const int64_t rows = ceil_div(a.rank, S::kRows) * a.count;
+    int64_t blocks[2];
+    for (int i = 0; i < 2; ++i) blocks[i] = a.sums[i].out ? rows * (a.sums[i].columns = (int)ceil_div(a.sums[i].wide, kAThreads * 2)) : 0;
+    if (blocks[0] + blocks[1] > kMaxDim / 8) return SBC_EINVAL;
+    a.parts = shares(blocks[0] + blocks[1], 4 * sm_count(), tokens, 64);
+    a.first = (int)(blocks[0] * a.parts);
+    const auto vec_one = [&](const AdapterSum& s) { return !s.out || (s.align_x >= 16 && s.wide % 8 == 0); };
+    return by_vec(vec_one(a.sums[0]) && vec_one(a.sums[1]), [&](auto vec) {
+        constexpr auto kernel = k_adapter_grad<T, W, RT, RH, decltype(vec)::value>;
+        if (!allow_smem<kernel>(S::kSmem)) return (int)SBC_ECUDA;
+        return launch(kernel, dim3((unsigned)((blocks[0] + blocks[1]) * a.parts)), S::kThreads, S::kSmem, st, a.parts, 0, a);
+    });
 }
 
-// out = scale mid^T x
-int adapter_grad(AdapterArgs a, int dtype, int weights, int64_t tokens, cudaStream_t st) {
-    a.align_x = row_align(a.x, a.x_stride, width_of(dtype));
-    a.align_factor = row_align(a.out, a.wide, width_of(weights));
+// out = scale mid^T x of one sum or both
+int adapter_grad(AdapterGradArgs a, int dtype, int weights, int64_t tokens, cudaStream_t st) {
+    for (AdapterSum& s : a.sums) {
+        s.align_x = row_align(s.x, s.x_stride, width_of(dtype));
+        s.align_out = row_align(s.out, s.wide, width_of(weights));
+    }
     return by_types(dtype, weights, [&](auto* t, auto* w) {
         using T = std::remove_pointer_t<decltype(t)>;
         using W = std::remove_pointer_t<decltype(w)>;
-        return a.rank <= 16 ? launch_adapter_grad<T, W, 1>(a, tokens, st) : a.rank <= 32 ? launch_adapter_grad<T, W, 2>(a, tokens, st)
-                                                                                          : launch_adapter_grad<T, W, 4>(a, tokens, st);
+        return a.rank <= 16 ? launch_adapter_grad<T, W, 1, 1>(a, tokens, st) : a.rank <= 32 ? launch_adapter_grad<T, W, 2, 1>(a, tokens, st)
+                                                                                             : launch_adapter_grad<T, W, 2, 2>(a, tokens, st);
     });
 }
 
@@ -568,7 +589,7 @@ int sbc_adapter(const sbc_adapters* w, const void* x, int dtype, int64_t tokens,
         a.align_x = row_align(x, tokens > 1 ? x_stride : 8, width_of(dtype));
         a.align_down = row_align(w->down, w->inner, width_of(w->dtype));
         a.pairs = w->outer % 2 == 0 && aligned(w->up, (uintptr_t)(2 * width_of(w->dtype)));
-        a.parts = shares(tokens, std::min(w->inner, w->outer), 128);
+        a.parts = shares(tokens, 4 * sm_count(), std::min(w->inner, w->outer), 128);
         return by_types(dtype, w->dtype, [&](auto* t, auto* ws) {
             using T = std::remove_pointer_t<decltype(t)>;
             using W = std::remove_pointer_t<decltype(ws)>;
@@ -636,22 +657,14 @@ int sbc_adapter_grad(const sbc_adapters* w, const void* dy, int64_t dy_stride, c
         a.scale = 1.f;
         rc = adapter_out(a, dtype, w->dtype, tokens, stream);
     }
-    if (rc == SBC_OK && ddown) {
-        a.x = x;
-        a.x_stride = x_stride;
-        a.wide = (int)w->inner;
-        a.out = ddown;
-        a.scale = 1.f;
-        rc = adapter_grad(a, dtype, w->dtype, tokens, stream);
-    }
-    if (rc == SBC_OK && dup) {
-        a.mid = const_cast<float*>(mid);
-        a.x = dy;
-        a.x_stride = dy_stride;
-        a.wide = (int)w->outer;
-        a.out = dup;
-        a.scale = scale;
-        rc = adapter_grad(a, dtype, w->dtype, tokens, stream);
+    if (rc == SBC_OK && (ddown || dup)) {
+        AdapterGradArgs g = {};
+        g.plan = a.plan;
+        g.count = a.count;
+        g.rank = a.rank;
+        g.sums[0] = {x, dmid, ddown, x_stride, (int)w->inner, 0, 0, 0, 1.f};
+        g.sums[1] = {dy, mid, dup, dy_stride, (int)w->outer, 0, 0, 0, scale};
+        rc = adapter_grad(g, dtype, w->dtype, tokens, stream);
     }
     return rc;
 }
