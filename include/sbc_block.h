@@ -177,6 +177,9 @@ size_t sbc_adapter_plan_bytes(int64_t tokens, int64_t count);
 int sbc_adapter_plan(const int32_t *ids, int64_t tokens, int64_t count, void *plan, size_t plan_bytes,
                      uint32_t *status, sbc_cuda_stream_t stream);
 
+/* Bytes of x down_i^T for a batch.  Host only; 0 on bad arguments. */
+size_t sbc_adapter_mid_bytes(int64_t tokens, int64_t rank);
+
 /*
  * out[t, :] = base[t, :] + scale * (x[t, :] down_i^T) up_i,  i = ids[t]; sums in
  * 32 bits, operands of any type exact, rounded once.  Tokens without an adapter
@@ -187,14 +190,15 @@ int sbc_adapter_plan(const int32_t *ids, int64_t tokens, int64_t count, void *pl
  *       (at most SBC_ADAPTER_FEW tokens, and mid is NULL).  With a plan ids may be NULL.
  * base  device, dtype, tokens x outer: what the shared projection gave; NULL: zeros
  * out   device, dtype; may be base with base's stride
- * mid   with a plan: device, 16-byte aligned, tokens * rank floats, which hold
- *       x down_i^T in the end (rows of tokens without an adapter are undefined):
- *       sbc_adapter_grad takes them.  Otherwise NULL.
+ * mid   with a plan: device, 16-byte aligned, sbc_adapter_mid_bytes(tokens, rank) bytes for
+ *       x down_i^T, which sbc_adapter_grad takes (each value as three bfloat16 whose sum it is:
+ *       [3][tokens][rank in whole sixteens]; rows of tokens without an adapter are
+ *       undefined).  Otherwise NULL.
  * status  device, one uint32, or NULL: as above, where ids are read
  */
 int sbc_adapter(const sbc_adapters *w, const void *x, int dtype, int64_t tokens, int64_t x_stride, const int32_t *ids,
                 const void *plan, float scale, const void *base, int64_t base_stride, void *out, int64_t out_stride,
-                float *mid, uint32_t *status, sbc_cuda_stream_t stream);
+                void *mid, uint32_t *status, sbc_cuda_stream_t stream);
 
 /*
  * Backward:
@@ -207,11 +211,11 @@ int sbc_adapter(const sbc_adapters *w, const void *x, int dtype, int64_t tokens,
  * base   device, dtype, tokens x inner: the input's gradient through the shared
  *        projection; NULL: zeros
  * dx, ddown, dup  each may be NULL (not all); dx may be base with base's stride
- * dmid   device, 16-byte aligned, tokens * rank floats of scratch
+ * dmid   device, 16-byte aligned, sbc_adapter_mid_bytes(tokens, rank) bytes of scratch
  */
 int sbc_adapter_grad(const sbc_adapters *w, const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, int dtype,
-                     int64_t tokens, const void *plan, const float *mid, float scale, const void *base,
-                     int64_t base_stride, void *dx, int64_t dx_stride, void *ddown, void *dup, float *dmid,
+                     int64_t tokens, const void *plan, const void *mid, float scale, const void *base,
+                     int64_t base_stride, void *dx, int64_t dx_stride, void *ddown, void *dup, void *dmid,
                      sbc_cuda_stream_t stream);
 
 #ifdef __cplusplus

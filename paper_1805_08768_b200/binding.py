@@ -32,7 +32,7 @@ EXPORTS = [
     "sbc_fp4_row_bytes", "sbc_fp4_scale_bytes", "sbc_fp4_workspace_bytes", "sbc_fp4_quantise", "sbc_fp4_dequantise",
     "sbc_fp4_product", "sbc_top_logits", "sbc_distill_loss", "sbc_distill_grad", "sbc_distill_loss_grad",
     "sbc_layer_norm", "sbc_layer_norm_workspace_bytes", "sbc_layer_norm_grad", "sbc_dropout", "sbc_gated_kept_bytes",
-    "sbc_gated_workspace_bytes", "sbc_gated", "sbc_gated_grad", "sbc_adapter_plan_bytes", "sbc_adapter_plan", "sbc_adapter",
+    "sbc_gated_workspace_bytes", "sbc_gated", "sbc_gated_grad", "sbc_adapter_mid_bytes", "sbc_adapter_plan_bytes", "sbc_adapter_plan", "sbc_adapter",
     "sbc_adapter_grad",
 ]
 SIDE_VALUES = 2
@@ -211,6 +211,7 @@ def lib() -> C.CDLL:
                 ("sbc_gated_workspace_bytes", size, [p, i64, p, i64, i32, i32]),
                 ("sbc_gated", i32, [p, p, i64, i64, p, i64, p, p, size, p, p]),
                 ("sbc_gated_grad", i32, [p, p, i64, i64, p, i64, p, p, i64, p, p, i32, i64, p, size, p, p]),
+                ("sbc_adapter_mid_bytes", size, [i64, i64]),
                 ("sbc_adapter_plan_bytes", size, [i64, i64]),
                 ("sbc_adapter_plan", i32, [p, i64, i64, p, size, p, p]),
                 ("sbc_adapter", i32, [p, p, i32, i64, i64, p, p, f32, p, i64, p, i64, p, p, p]),
@@ -1069,7 +1070,8 @@ class AdapterPlan:
 
 
 class AdapterKept:
-    """What a forward call leaves for sbc_adapter_grad: x down^T in float32 [tokens, rank], and the plan."""
+    """What a forward call leaves for sbc_adapter_grad: x down^T (three bfloat16 terms of each value, [3, tokens, rank in whole
+    sixteens]), and the plan."""
 
     __slots__ = ("mid", "plan")
 
@@ -1146,7 +1148,7 @@ def sbc_adapter(x: torch.Tensor, down: torch.Tensor, up: torch.Tensor, ids: Opti
     planned = None if plan is None else _planned(plan, tokens, count, x)
     res, res_across = (None, 0) if base is None else (base.data_ptr(), _same(base, x, "base", (tokens, outer)))
     out, out_across = _out(out, (tokens, outer), x, stream)
-    mid = None if plan is None else _empty(stream, (tokens, rank), torch.float32, x)
+    mid = None if plan is None else _empty(stream, (3, tokens, (rank + 15) // 16 * 16), torch.bfloat16, x)
     rc = lib().sbc_adapter(C.byref(d), x.data_ptr(), code, tokens, across, at, planned, scale, res, res_across, out.data_ptr(),
                            out_across, None if mid is None else mid.data_ptr(), _status(status, x), _cuda_stream(stream))
     if rc:
@@ -1165,7 +1167,8 @@ def sbc_adapter_grad(dy: torch.Tensor, x: torch.Tensor, down: torch.Tensor, up: 
         raise ValueError(f"x has {cols} features, down takes {inner}")
     dy_across = _same(dy, x, "dy", (tokens, outer))
     planned = _planned(kept.plan, tokens, count, x)
-    mid = _rows_of(kept.mid, tokens * rank, torch.float32, "mid", x)
+    shape = (3, tokens, (rank + 15) // 16 * 16)
+    mid = _rows_of(kept.mid, shape[1] * shape[2] * 3, torch.bfloat16, "mid", x)
     if not (need_input or need_adapters):
         return None, None, None
     dx = ddown = dup = None
@@ -1177,7 +1180,7 @@ def sbc_adapter_grad(dy: torch.Tensor, x: torch.Tensor, down: torch.Tensor, up: 
         dx, dx_across = _out(out, (tokens, inner), x, stream)
     if need_adapters:
         ddown, dup = _empty(stream, down.shape, down.dtype, x), _empty(stream, up.shape, up.dtype, x)
-    dmid = _empty(stream, (tokens, rank), torch.float32, x)
+    dmid = _empty(stream, shape, torch.bfloat16, x)
     rc = lib().sbc_adapter_grad(C.byref(d), dy.data_ptr(), dy_across, x.data_ptr(), across, code, tokens, planned, mid, scale, res,
                                 res_across, dx.data_ptr() if need_input else None, dx_across,
                                 ddown.data_ptr() if need_adapters else None, dup.data_ptr() if need_adapters else None,

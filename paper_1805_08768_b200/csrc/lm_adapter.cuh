@@ -11,7 +11,7 @@
 //
 // As good as 32-bit arithmetic whatever the types: an operand goes into the products as the bfloat16 terms that it is the sum of (one
 // for bfloat16, two for float16, three for float32, cut off rather than rounded, so that none overflows),
-// and of the terms' products those count that are not below 2^-24 of the first.  mid and dmid are floats.  Where a result
+// and of the terms' products those count that are not below 2^-24 of the first.  mid and dmid are kept as three terms.  Where a result
 // has 32 bits, a product's sum starts from zero and is added by an ordinary addition: the tensor cores cut off what they
 // align to a running sum, which over 4096 elements came to 1.6e-6 of the result instead of 1e-7.
 //
@@ -200,34 +200,29 @@ __device__ __forceinline__ void mma_terms(float* d, const uint32_t* a, uint32_t 
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Products of sixteen rows of X terms in shared memory (`p`: this thread's place in the first, `next` from term to term) with
-// eight tiles of eight columns of Y terms in registers.
+// Sixteen rows x sixteen k of terms in shared memory as the products take them: from rows, or (TRANS) from columns.  `from`: this
+// lane's row and half of sixteen elements.
+template <bool TRANS> __device__ __forceinline__ void load_terms(uint32_t* w, uint32_t from) {
+    if (TRANS)
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(from) : "memory");
+    else
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(from) : "memory");
+}
+// Products of sixteen rows of X terms with eight columns of Y terms (at a time: b0[o * next], b1[o * next]).
 template <int X, int Y, bool APART>
-__device__ __forceinline__ void add_products(float (*acc)[4], const uint16_t* p, int next, int pitch, const uint32_t (*lo)[8], const uint32_t (*hi)[8]) {
-    uint32_t w[X][4];
+__device__ __forceinline__ void add_products(float* acc, const uint32_t (*w)[4], const uint32_t* b0, const uint32_t* b1, int next) {
+    float part[4] = {};
+    float* d = APART ? part : acc;
 #pragma unroll
-    for (int n = 0; n < X; ++n) {
-        const uint16_t* from = p + n * next;
-        w[n][0] = *reinterpret_cast<const uint32_t*>(from);
-        w[n][1] = *reinterpret_cast<const uint32_t*>(from + 8 * pitch);
-        w[n][2] = *reinterpret_cast<const uint32_t*>(from + 8);
-        w[n][3] = *reinterpret_cast<const uint32_t*>(from + 8 * pitch + 8);
-    }
+    for (int order = X - 1; order >= 0; --order)   // the small products first
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        float part[4] = {};
-        float* d = APART ? part : acc[e];
+        for (int n = 0; n < X; ++n) {
+            const int o = order - n;
+            if (o >= 0 && o < Y) mma_terms(d, w[n], b0[o * next], b1[o * next]);
+        }
+    if (APART)
 #pragma unroll
-        for (int order = X - 1; order >= 0; --order)   // the small products first
-#pragma unroll
-            for (int n = 0; n < X; ++n) {
-                const int o = order - n;
-                if (o >= 0 && o < Y) mma_terms(d, w[n], lo[o][e], hi[o][e]);
-            }
-        if (APART)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) acc[e][k] += part[k];
-    }
+        for (int k = 0; k < 4; ++k) acc[k] += part[k];
 }
 
 // ---- a thread's own ring in shared memory ---------------------------------------------------
@@ -236,27 +231,33 @@ __device__ __forceinline__ void add_products(float (*acc)[4], const uint16_t* p,
 // so nothing but its own wait stands between the two, registers hold only what the products take next, and an
 // SM has 100 KB and more under way.  A pack's granules of 16 bytes are 512 bytes apart: a warp's are side by side.
 
-// Copies `have` elements (at most 8, zeros behind them) whose address is a multiple of `align`.  VEC: of 16 bytes, and all
-// eight or none.  SHARED: other warps load the same, so it may stay in the first-level cache.
-template <bool VEC, bool SHARED, typename T> __device__ __forceinline__ void ring_load(uint32_t to, const T* p, int have, int align) {
-    constexpr int kEach = 16 / (int)sizeof(T);
+// Copies eight elements at a multiple of 16 bytes, or zeros (p is then not read).  SHARED: other warps load the same, so it may
+// stay in the first-level cache.  (Zeros by a predicate: a number of bytes in a register costs tens of instructions.)
+template <bool SHARED, typename T> __device__ __forceinline__ void ring_load8(uint32_t to, const T* p, bool zeros = false) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+        const char* from = reinterpret_cast<const char*>(p) + 16 * i;
+        if (SHARED)
+            asm volatile("{\n\t.reg .pred z;\n\tsetp.ne.u32 z, %2, 0;\n\tcp.async.ca.shared.global [%0], [%1], 16, z;\n\t}" ::"r"(to + 512 * i), "l"(from), "r"((uint32_t)zeros) : "memory");
+        else
+            asm volatile("{\n\t.reg .pred z;\n\tsetp.ne.u32 z, %2, 0;\n\tcp.async.cg.shared.global [%0], [%1], 16, z;\n\t}" ::"r"(to + 512 * i), "l"(from), "r"((uint32_t)zeros) : "memory");
+    }
+}
+// Copies `have` elements (at most 8, zeros behind them) whose address is a multiple of `align`.
+template <typename T> __device__ __forceinline__ void ring_load(uint32_t to, const T* p, int have, int align) {
+    constexpr int kEach = 16 / (int)sizeof(T), kWord = 4 / (int)sizeof(T);
 #pragma unroll
     for (int i = 0; i < (int)sizeof(T) / 2; ++i, to += 512, p += kEach, have -= kEach) {
-        if (VEC) {
-            const int bytes = have > 0 ? 16 : 0;
-            if (SHARED)
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(p), "r"(bytes) : "memory");
-            else
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(p), "r"(bytes) : "memory");
-            continue;
-        }
-        const int bytes = max(0, min(16, have * (int)sizeof(T)));
         if (align >= 4) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + 4 * k), "l"(reinterpret_cast<const char*>(p) + 4 * k),
-                             "r"(max(0, min(4, bytes - 4 * k)))
-                             : "memory");
+            for (int k = 0; k < 4; ++k) {
+                if (kWord == 2 && have == 2 * k + 1)   // half a word
+                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(to + 4 * k), "r"((uint32_t)reinterpret_cast<const uint16_t*>(p)[2 * k]) : "memory");
+                else
+                    asm volatile("{\n\t.reg .pred z;\n\tsetp.le.s32 z, %2, %3;\n\tcp.async.ca.shared.global [%0], [%1], 4, z;\n\t}" ::"r"(to + 4 * k),
+                                 "l"(reinterpret_cast<const char*>(p) + 4 * k), "r"(have), "r"(kWord * k)
+                                 : "memory");
+            }
         } else {
             union {
                 T e[kEach];
@@ -265,7 +266,7 @@ template <bool VEC, bool SHARED, typename T> __device__ __forceinline__ void rin
             v.q = make_uint4(0, 0, 0, 0);
 #pragma unroll
             for (int k = 0; k < kEach; ++k)
-                if (k * (int)sizeof(T) < bytes) v.e[k] = p[k];
+                if (k < have) v.e[k] = p[k];
             asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(v.q.x), "r"(v.q.y), "r"(v.q.z), "r"(v.q.w) : "memory");
         }
     }
@@ -319,13 +320,14 @@ struct AdapterArgs {
     const void* factor;     // [count][rank][wide]
     const void* base;
     void* out;              // y or dx
-    float* mid;             // [tokens][rank]
+    uint16_t* mid;          // terms, [3][tokens][rank in whole sixteens, zeros behind the rank]
     AdapterPlan plan;
     long long x_stride, base_stride, out_stride;
-    int count, rank, wide, parts;
+    int tokens, count, rank, wide, parts;
     int align_x, align_base, align_out, align_factor;
     float scale;
 };
+__host__ __device__ constexpr int sixteens(int rank) { return (rank + 15) / 16 * 16; }
 
 // ---- into the rank ------------------------------------------------------------------------------
 
@@ -355,15 +357,16 @@ __global__ void __launch_bounds__(kAThreads, Terms<T>::n + Terms<W>::n <= 3 ? 2 
     const int j0 = (int)blockIdx.y * 8 * JT;
     if (threadIdx.x < kATile) tokens[threadIdx.x] = threadIdx.x < at.z ? a.plan.order[at.y + threadIdx.x] : -1;
     __syncthreads();
+    // (a row that is none has no sums that are used: nothing is loaded for it where others' places cannot be mistaken for it)
     const T* x[MT][2];
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int t = tokens[half * 32 + m * 16 + h * 8 + g];
-            x[m][h] = t < 0 ? nullptr : static_cast<const T*>(a.x) + (long long)t * a.x_stride;
+            x[m][h] = t < 0 ? nullptr : static_cast<const T*>(a.x) + (long long)t * a.x_stride + q * 8;
         }
-    const W* factor = static_cast<const W*>(a.factor) + ((long long)at.x * a.rank + j0 + g) * a.wide;
+    const W* factor = static_cast<const W*>(a.factor) + ((long long)at.x * a.rank + j0 + g) * a.wide + q * 8;
     const int rows = a.rank - j0 - g;   // of the factor, this thread's first among them
     const uint32_t ring = smem_u32(raw) + (uint32_t)(warp * S::kStages * S::kStage) + 16u * lane;
     float acc[MT][JT][4] = {};
@@ -372,20 +375,28 @@ __global__ void __launch_bounds__(kAThreads, Terms<T>::n + Terms<W>::n <= 3 ? 2 
     const int u0 = (int)((long long)units * part / a.parts), u1 = left > 0 ? (int)((long long)units * (part + 1) / a.parts) : u0;
     const auto fill = [&](int u, int stage) {
         if (u < u1) {
-            const int k = u * 32 + q * 8, have = a.wide - k;
-            uint32_t to = ring + (uint32_t)(stage * S::kStage);
+            const int k = u * 32, have = a.wide - k - q * 8;
+            const uint32_t to = ring + (uint32_t)(stage * S::kStage), to_f = to + MT * 2 * kPackBytes<T>;
+            if (VEC) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                if (m * 16 >= left) break;
+                for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    ring_load<VEC, false>(to + (m * 2 + h) * kPackBytes<T>, x[m][h] ? x[m][h] + k : static_cast<const T*>(a.x), x[m][h] ? have : 0, a.align_x);
-            }
-            to += MT * 2 * kPackBytes<T>;
+                    for (int h = 0; h < 2; ++h)
+                        if (x[m][h]) ring_load8<false>(to + (m * 2 + h) * kPackBytes<T>, x[m][h] + k, have <= 0);
+                const W* f = factor + k;
 #pragma unroll
-            for (int j = 0; j < JT; ++j) {
-                const bool in = 8 * j < rows;
-                ring_load<VEC, true>(to + j * kPackBytes<W>, in ? factor + (long long)(8 * j) * a.wide + k : static_cast<const W*>(a.factor), in ? have : 0, a.align_factor);
+                for (int j = 0; j < JT; ++j, f += 8ll * a.wide)
+                    if (8 * j < rows) ring_load8<true>(to_f + j * kPackBytes<W>, f, have <= 0);
+            } else {
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        if (x[m][h]) ring_load(to + (m * 2 + h) * kPackBytes<T>, x[m][h] + k, have, a.align_x);
+                const W* f = factor + k;
+#pragma unroll
+                for (int j = 0; j < JT; ++j, f += 8ll * a.wide)
+                    if (8 * j < rows) ring_load(to_f + j * kPackBytes<W>, f, have, a.align_factor);
             }
         }
         ring_commit();
@@ -411,7 +422,6 @@ __global__ void __launch_bounds__(kAThreads, Terms<T>::n + Terms<W>::n <= 3 ? 2 
         } else {
 #pragma unroll
             for (int m = 0; m < MT * 2; ++m) {
-                if (m * 8 >= left) break;
                 Pack8<T> v;
                 ring_read(v, from + m * kPackBytes<T>);
                 cut_row<X>(held[m], v);
@@ -421,7 +431,6 @@ __global__ void __launch_bounds__(kAThreads, Terms<T>::n + Terms<W>::n <= 3 ? 2 
         for (int outer = 0; outer < (kHold ? MT : JT); ++outer) {
             uint32_t now[kHold ? 2 : 1][kHold ? X : Y][4];
             if constexpr (kHold) {
-                if (outer * 16 >= left) break;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     Pack8<T> v;
@@ -436,7 +445,6 @@ __global__ void __launch_bounds__(kAThreads, Terms<T>::n + Terms<W>::n <= 3 ? 2 
 #pragma unroll
             for (int inner = 0; inner < (kHold ? JT : MT); ++inner) {
                 const int m = kHold ? outer : inner, j = kHold ? inner : outer;
-                if (!kHold && m * 16 >= left) break;
                 float part_sum[4] = {};
                 float* d = sizeof(W) == 4 ? part_sum : acc[m][j];
 #pragma unroll
@@ -472,10 +480,19 @@ __global__ void __launch_bounds__(kAThreads, Terms<T>::n + Terms<W>::n <= 3 ? 2 
     __syncthreads();
     // [halves][kPer][32] sums of kRuns warps, left in the first ones' places for the cluster
     constexpr int kSums = S::kHalves * kPer * 32;
+    const int wide_rank = sixteens(a.rank);
     const auto store = [&](int i, float v) {
         const int n = i % 32, e = i / 32 % 4, j = i / 128 % JT, m = i / (128 * JT);   // m: halves and their tiles
         const int t = m * 16 + (e >> 1) * 8 + (n >> 2), r = j0 + 8 * j + (n & 3) * 2 + (e & 1);
-        if (t < at.z && r < a.rank) a.mid[(long long)tokens[t] * a.rank + r] = v * a.scale;
+        if (t >= at.z || r >= wide_rank) return;
+        uint32_t w[3];
+        cut<3>(w, r < a.rank ? v * a.scale : 0.f);
+        uint16_t* to = a.mid + (long long)tokens[t] * wide_rank + r;
+#pragma unroll
+        for (int k = 0; k < 3; ++k, to += (long long)a.tokens * wide_rank) {
+            *to = (uint16_t)(w[k] >> 16);
+            if (JT == 1) to[8] = 0;
+        }
     };
     for (int i = threadIdx.x; i < kSums; i += kAThreads) {
         float v = sums[i];
@@ -499,144 +516,173 @@ __global__ void __launch_bounds__(kAThreads, Terms<T>::n + Terms<W>::n <= 3 ? 2 
 
 // ---- out of the rank ------------------------------------------------------------------------------
 
-// out[t][c] = base[t][c] + scale sum_j mid[t][j] factor[i][j][c].  A warp has 32 tokens x 64 columns at a
-// time.  mid's terms wait in shared memory; a thread loads eight neighbours of four rows of the factor, whose pairs are
-// the products' words (which column is which of a product's eight is free, too), and ends with sixteen
-// neighbours of each of its rows of out.
-template <typename T, typename W> struct OutShape {
+// out[t][c] = base[t][c] + scale sum_j mid[t][j] factor[i][j][c].  A block has CB columns, whose factor waits in shared memory as
+// terms (again only where the adapter changes), and takes a run of the tiles of tokens: base and mid's terms of the next
+// tile are on their way while this one's products are made.  A warp has 64 columns and as many tokens as leaves eight
+// warps busy.  The factor's columns are so placed that a thread ends with eight neighbours of a row, twice.
+template <typename T, typename W, int CB> struct OutShape {
     // 16-bit results: what lies 2^-16 below a factor does not reach them
     static constexpr int X = sizeof(T) == 4 ? 3 : 2, Y = sizeof(T) == 4 ? Terms<W>::n : (Terms<W>::n < 2 ? Terms<W>::n : 2);
-    static constexpr int MT = 2, kHalves = 4 / MT, kColumns = 8 / kHalves * 64;   // of a block at a time
-    static constexpr int kBase = MT * 4 * (int)kPackBytes<T>, kStage = 4 * (int)kPackBytes<W>;   // of a warp
-    // base: one buffer, loaded while the tile's products are made, or, where those are a single step, two
-    static __host__ __device__ constexpr int pitch(int rank) { return (rank + 15) / 16 * 16 + 8; }
-    static __host__ __device__ constexpr int buffers(int rank) { return rank <= 16 ? 2 : 1; }
-    static __host__ __device__ constexpr int stages(int rank) { return rank <= 16 ? 2 : 3; }
-    static __host__ __device__ constexpr int smem(int rank) { return 8 * (buffers(rank) * kBase + stages(rank) * kStage) + X * kATile * pitch(rank) * 2; }
+    static constexpr int kGroups = CB / 64, MT = kGroups / 2, kBase = MT * 4 * (int)kPackBytes<T>, kFactorPitch = CB + 8;
+    static __host__ __device__ constexpr int pitch(int rank) { return sixteens(rank) + 8; }
+    static __host__ __device__ constexpr int factor_bytes(int rank) { return Y * sixteens(rank) * kFactorPitch * 2; }
+    static __host__ __device__ constexpr int terms_bytes(int rank) { return X * kATile * pitch(rank) * 2; }
+    static constexpr int kMost = 225 * 1024;
+    // mid's terms of two tiles, where they fit
+    static __host__ __device__ constexpr int buffers(int rank) { return 8 * kBase + factor_bytes(rank) + 2 * terms_bytes(rank) <= kMost ? 2 : 1; }
+    static __host__ __device__ constexpr int smem(int rank) { return 8 * kBase + factor_bytes(rank) + buffers(rank) * terms_bytes(rank); }
 };
-template <typename T, typename W, bool VEC>
-__global__ void __launch_bounds__(kAThreads, sizeof(W) == 2 ? 2 : 1) k_adapter_out(AdapterArgs a) {
-    using S = OutShape<T, W>;
+template <typename T, typename W, int CB, bool VEC>
+__global__ void __launch_bounds__(kAThreads, sizeof(T) == 2 && Terms<W>::n == 1 ? 2 : 1) k_adapter_out(AdapterArgs a) {
+    using S = OutShape<T, W, CB>;
     constexpr int X = S::X, Y = S::Y, MT = S::MT;
-    extern __shared__ __align__(16) uint8_t raw[];
-    __shared__ int tokens[kATile];
+    extern __shared__ __align__(16) uint8_t raw[];   // rings of base, the factor's terms [Y][ranks][pitch], mid's [2][X][kATile][pitch]
+    __shared__ int tokens[3][kATile];
     after_earlier_kernels();
-    if ((int)blockIdx.x >= a.plan.tiles[0].x) return;
-    const int4 at = a.plan.tiles[1 + blockIdx.x];
-    const bool none = at.x >= a.count;
-    if (none && a.base == a.out) return;
-    const int pitch = S::pitch(a.rank), steps = none ? 1 : (a.rank + 15) / 16, buffers = S::buffers(a.rank), stages = S::stages(a.rank);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3, half = warp % S::kHalves;
-    const uint32_t base_ring = smem_u32(raw) + (uint32_t)(warp * buffers * S::kBase) + 16u * lane;
-    const uint32_t ring = smem_u32(raw) + (uint32_t)(8 * buffers * S::kBase + warp * stages * S::kStage) + 16u * lane;
-    uint16_t* terms = reinterpret_cast<uint16_t*>(raw + 8 * (buffers * S::kBase + stages * S::kStage));   // [X][kATile][pitch]
-    if (threadIdx.x < kATile) tokens[threadIdx.x] = threadIdx.x < at.z ? a.plan.order[at.y + threadIdx.x] : -1;
-    __syncthreads();
-    const int left = at.z - half * 32;
-    int row[MT][2];
+    const int all = a.plan.tiles[0].x, ranks = sixteens(a.rank), steps = ranks / 16, pitch = S::pitch(a.rank);
+    const bool two = S::buffers(a.rank) == 2;
+    const int first = (int)((long long)all * blockIdx.y / gridDim.y), last = (int)((long long)all * (blockIdx.y + 1) / gridDim.y);
+    if (first == last) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+    const int group = warp % S::kGroups, row0 = warp / S::kGroups * 16 * MT;
+    const int cb = (int)blockIdx.x * CB, col = cb + group * 64;
+    const uint32_t ring = smem_u32(raw) + (uint32_t)(warp * S::kBase) + 16u * lane;
+    uint16_t* factor = reinterpret_cast<uint16_t*>(raw + 8 * S::kBase);
+    const uint32_t terms = smem_u32(raw) + (uint32_t)(8 * S::kBase + S::factor_bytes(a.rank));
+    // The plan is asked for ahead of its use: a tile's place for five tiles later, its tokens for four, and in shared memory three.
+    const auto place = [&](int tile) { return tile < last ? a.plan.tiles[1 + tile] : make_int4(0, 0, 0, 0); };
+    const auto token = [&](const int4& at) { return (int)threadIdx.x < at.z ? a.plan.order[at.y + threadIdx.x] : -1; };   // (a tile has at most kATile)
+    const auto fill_terms = [&](int tile) {
+        const int* t = tokens[tile % 3];
+        const uint32_t to = terms + (uint32_t)((two ? tile & 1 : 0) * S::terms_bytes(a.rank));
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+        for (int row = (int)threadIdx.x / 8; row < kATile; row += kAThreads / 8) {
+            const int tok = t[row];
+            for (int c = (int)threadIdx.x % 8 * 8; c < ranks; c += 64) {
+                const uint16_t* from = a.mid + (long long)max(tok, 0) * ranks + c;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) row[m][h] = tokens[half * 32 + m * 16 + h * 8 + g];
-    const W* factor = static_cast<const W*>(a.factor) + (long long)(none ? 0 : at.x) * a.rank * a.wide;
-    const int first = ((int)blockIdx.y * (8 / S::kHalves) + warp / S::kHalves) * 64, across = (int)gridDim.y * S::kColumns;
-    const int mine = left > 0 && first < a.wide ? (a.wide - first + across - 1) / across : 0;   // this warp's tiles of columns
-    const auto fill_base = [&](int n) {
-        const int col = first + n * across + 16 * q;
-        const uint32_t to = base_ring + (uint32_t)((buffers == 2 ? n & 1 : 0) * S::kBase);
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            if (m * 16 >= left) break;
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    const int have = a.base && row[m][h] >= 0 ? a.wide - col - 8 * p : 0;
-                    const T* from = static_cast<const T*>(have > 0 ? a.base : a.x);
-                    ring_load<VEC, false>(to + ((m * 2 + h) * 2 + p) * kPackBytes<T>, have > 0 ? from + (long long)row[m][h] * a.base_stride + col + 8 * p : from, have, a.align_base);
-                }
-        }
-    };
-    const auto fill_factor = [&](int n, int s, int stage) {
-        const int fc = first + n * across + 8 * g;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int j = s * 16 + 2 * q + (k & 1) + (k >> 1) * 8, have = !none && j < a.rank ? a.wide - fc : 0;
-            ring_load<VEC, true>(ring + (uint32_t)(stage * S::kStage) + k * kPackBytes<W>, have > 0 ? factor + (long long)j * a.wide + fc : factor, have, a.align_factor);
-        }
-    };
-    // `ahead` steps of the factor are under way; one group of copies a step
-    const int ahead = min(steps, stages - 1);
-    int fn = 0, fs = 0, fstage = 0;   // the step that is loaded next
-    const auto fill = [&]() {
-        if (fn < mine) {
-            if (buffers == 2) fill_base(fn);   // (a single step: base comes with it)
-            fill_factor(fn, fs, fstage);
-        }
-        if (++fs == steps) fs = 0, ++fn;
-        if (++fstage == stages) fstage = 0;
-        ring_commit();
-    };
-    if (buffers == 2) {
-        fill();   // (a second one would need a third buffer)
-    } else {
-        for (int i = 0; i < ahead; ++i) fill();
-    }
-    for (int i = threadIdx.x; !none && i < kATile * steps * 16; i += kAThreads) {
-        const int t = i / (steps * 16), j = i - t * steps * 16;
-        uint32_t w[X];
-        cut<X>(w, tokens[t] >= 0 && j < a.rank ? a.mid[(long long)tokens[t] * a.rank + j] : 0.f);
-#pragma unroll
-        for (int n = 0; n < X; ++n) terms[(n * kATile + t) * pitch + j] = (uint16_t)(w[n] >> 16);
-    }
-    __syncthreads();
-    int stage = 0;
-    for (int n = 0; n < mine; ++n) {
-        float acc[MT][8][4] = {};
-        if (buffers == 1) fill_base(n);   // (with the next group)
-        for (int s = 0; s < steps; ++s) {
-            fill();
-            ring_wait(buffers == 2 ? 1 : ahead);
-            if (!none) {
-                const uint32_t from = ring + (uint32_t)(stage * S::kStage);
-                uint32_t lo[Y][8], hi[Y][8];
-                Pack8<W> f, f2;
-                ring_read(f, from);
-                ring_read(f2, from + kPackBytes<W>);
-                cut_rows<Y>(lo, f, f2);
-                ring_read(f, from + 2 * kPackBytes<W>);
-                ring_read(f2, from + 3 * kPackBytes<W>);
-                cut_rows<Y>(hi, f, f2);
-#pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    if (m * 16 >= left) break;
-                    add_products<X, Y, sizeof(T) == 4>(acc[m], terms + (half * 32 + m * 16 + g) * pitch + s * 16 + 2 * q, kATile * pitch, pitch, lo, hi);
-                }
+                for (int n = 0; n < X; ++n)
+                    ring_load8<false>(to + (uint32_t)(((n * kATile + row) * pitch + c) * 2), reinterpret_cast<const __nv_bfloat16*>(from + (long long)n * a.tokens * ranks), tok < 0);
             }
-            if (++stage == stages) stage = 0;
         }
-        // base came with the group of the tile's first step
-        if (buffers == 1) ring_wait(min(ahead, steps - 1));
-        const uint32_t from = base_ring + (uint32_t)((buffers == 2 ? n & 1 : 0) * S::kBase);
-        const int col = first + n * across + 16 * q;
+    };
+    const auto fill_base = [&](int tile) {
+        if (!a.base) return;
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                if (row[m][h] < 0) continue;
+                const int t = tokens[tile % 3][row0 + m * 16 + h * 8 + g];
+                const T* from = static_cast<const T*>(a.base) + (long long)t * a.base_stride + col + 8 * q;
 #pragma unroll
                 for (int p = 0; p < 2; ++p) {
-                    Pack8<T> v;
-                    ring_read(v, from + ((m * 2 + h) * 2 + p) * kPackBytes<T>);
+                    const int have = a.wide - col - 32 * p - 8 * q;
+                    if (t < 0 || have <= 0) continue;
+                    if (VEC)
+                        ring_load8<false>(ring + ((m * 2 + h) * 2 + p) * kPackBytes<T>, from + 32 * p);
+                    else
+                        ring_load(ring + ((m * 2 + h) * 2 + p) * kPackBytes<T>, from + 32 * p, have, a.align_base);
+                }
+            }
+    };
+    const int4 at0 = place(first), at1 = place(first + 1), at2 = place(first + 2);
+    int4 at4 = place(first + 4);
+    int token3 = token(place(first + 3));
+    if (threadIdx.x < kATile) {
+        tokens[first % 3][threadIdx.x] = token(at0);
+        tokens[(first + 1) % 3][threadIdx.x] = token(at1);
+        tokens[(first + 2) % 3][threadIdx.x] = token(at2);
+    }
+    __syncthreads();
+    fill_base(first);
+    if (at0.x < a.count) fill_terms(first);
+    ring_commit();
+    int adapter = -1, now = at0.x, after = at1.x;   // this tile's adapter, and the next one's
+    for (int tile = first; tile < last; ++tile) {
+        const int later = place(tile + 2).x;
+        const bool none = now >= a.count;
+        if (now != adapter && !none) {
+            // (the tile before has been read behind the barrier at its end)
+            adapter = now;
+            const W* f = static_cast<const W*>(a.factor) + (long long)now * a.rank * a.wide;
+            for (int i = threadIdx.x; i < ranks * (CB / 8); i += kAThreads) {
+                const int j = i / (CB / 8), pack = i % (CB / 8), c = cb + 8 * pack;
+                Pack8<W> v;
+                load8(v, f + (long long)min(j, a.rank - 1) * a.wide + c, j < a.rank ? a.wide - c : 0, VEC ? 16 : a.align_factor);
+                // neighbour e of these eight is column 2 (place of the eight in its 32) + (which 32) of tile e
+                uint16_t* to = factor + j * S::kFactorPitch + pack / 8 * 64 + (pack & 3) * 2 + (pack >> 2 & 1);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    uint32_t w[Y];
+                    cut<Y>(w, to_float(v.e[e]));
+#pragma unroll
+                    for (int o = 0; o < Y; ++o) to[o * ranks * S::kFactorPitch + 8 * e] = (uint16_t)(w[o] >> 16);
+                }
+            }
+        }
+        ring_wait(0);
+        Pack8<T> b[MT][2][2];
+#pragma unroll
+        for (int i = 0; i < MT * 4; ++i) ring_read(b[i / 4][i / 2 % 2][i % 2], ring + i * kPackBytes<T>);
+        __syncthreads();   // this tile's terms, the factor and the tokens of the next are there
+        if (tile + 1 < last) {
+            fill_base(tile + 1);
+            if (two && after < a.count) fill_terms(tile + 1);
+        }
+        ring_commit();
+        float acc[MT][8][4] = {};
+        if (!none) {
+            const uint32_t terms_at = terms + (uint32_t)((two ? tile & 1 : 0) * S::terms_bytes(a.rank) + ((row0 + (lane & 15)) * pitch + (lane >> 4) * 8) * 2);
+            const uint32_t factor_at = smem_u32(factor) + (uint32_t)(((lane & 15) * S::kFactorPitch + group * 64 + (lane >> 4) * 8) * 2);
+            for (int s = 0; s < steps; ++s) {
+                uint32_t w[MT][X][4];
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int n = 0; n < X; ++n) load_terms<false>(w[m][n], terms_at + (uint32_t)(((n * kATile + m * 16) * pitch + s * 16) * 2));
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    uint32_t f[Y][4];
+#pragma unroll
+                    for (int o = 0; o < Y; ++o) load_terms<true>(f[o], factor_at + (uint32_t)(((o * ranks + s * 16) * S::kFactorPitch + e * 8) * 2));
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) {
+                        add_products<X, Y, sizeof(T) == 4>(acc[m][e], w[m], &f[0][0], &f[0][1], 4);
+                        add_products<X, Y, sizeof(T) == 4>(acc[m][e + 1], w[m], &f[0][2], &f[0][3], 4);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int t = tokens[tile % 3][row0 + m * 16 + h * 8 + g];
+                if (t < 0 || (none && a.base == a.out)) continue;
+                T* out = static_cast<T*>(a.out) + (long long)t * a.out_stride + col + 8 * q;
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    Pack8<T> v = b[m][h][p];
+                    if (!a.base) v = {};
                     if (!none) {
                         float f[8];
 #pragma unroll
                         for (int e = 0; e < 8; ++e) f[e] = fmaf(a.scale, acc[m][e][2 * h + p], to_float(v.e[e]));
                         pack8(v, f);
                     }
-                    write8(static_cast<T*>(a.out) + (long long)row[m][h] * a.out_stride + col + 8 * p, v, a.wide - col - 8 * p, VEC || a.align_out >= 16);
+                    write8(out + 32 * p, v, a.wide - col - 32 * p - 8 * q, VEC || a.align_out >= 16);
                 }
             }
+        __syncthreads();   // this tile's terms and tokens, and the factor, are read
+        if (!two && tile + 1 < last && after < a.count) {
+            fill_terms(tile + 1);
+            ring_commit();
+        }
+        if (threadIdx.x < kATile) tokens[tile % 3][threadIdx.x] = token3;   // of tile + 3
+        token3 = token(at4);
+        at4 = place(tile + 5);
+        now = after;
+        after = later;
     }
     ring_wait(0);
 }
@@ -644,11 +690,11 @@ __global__ void __launch_bounds__(kAThreads, sizeof(W) == 2 ? 2 : 1) k_adapter_o
 // ---- over tokens ------------------------------------------------------------------------------------
 
 // out[i][j][c] = scale sum over the tokens t of adapter i of mid[t][j] x[t][c], for one or two such sums in a launch.  A warp
-// has 64 columns and 16 RT rows, the warps of a block 512 columns and, for ranks above 32, twice as many rows.  64 tokens' terms of mid are laid out in shared memory with the tokens as the
-// contiguous axis, x is loaded as the factor above.  Blocks of a cluster share an adapter's tokens, and add their sums in their order.
+// has 64 columns and 16 RT rows, the warps of a block 512 columns and, for ranks above 32, twice as many rows.  64 tokens' terms of mid wait in
+// shared memory; of x, a thread loads eight neighbours of four rows, whose pairs are the products' words.  Blocks of a cluster share an adapter's tokens, and add their sums in their order.
 struct AdapterSum {
     const void* x;
-    const float* mid;
+    const uint16_t* mid;   // terms
     void* out;             // [count][rank][wide]
     long long x_stride;
     int wide, columns;     // blocks of columns
@@ -658,21 +704,20 @@ struct AdapterSum {
 struct AdapterGradArgs {
     AdapterSum sums[2];
     AdapterPlan plan;
-    int count, rank, parts;
+    int tokens, count, rank, parts;
     int first;             // blocks of the first sum
 };
 template <typename T, typename W, int RT, int RH> struct GradShape {
-    static constexpr int X = sizeof(W) == 4 ? 3 : 2, Y = sizeof(W) == 4 ? Terms<T>::n : (Terms<T>::n < 2 ? Terms<T>::n : 2), kPitch = kATile + 8;
-    static constexpr int kThreads = kAThreads * RH, kRows = 16 * RT * RH;
-    static constexpr int kStage = 4 * (int)kPackBytes<T>, kStages = sizeof(T) == 4 ? 3 : 5;   // of a warp
-    static constexpr int kRings = 8 * RH * kStages * kStage, kTerms = X * kRows * kPitch * 2, kSums = RT * 32 * kThreads * 4;
+    static constexpr int X = sizeof(W) == 4 ? 3 : 2, Y = sizeof(W) == 4 ? Terms<T>::n : (Terms<T>::n < 2 ? Terms<T>::n : 2), kThreads = kAThreads * RH, kRows = 16 * RT * RH, kPitch = kRows + 8;
+    static constexpr int kStage = 4 * (int)kPackBytes<T>, kStages = sizeof(T) == 4 ? (RH == 2 ? 2 : 3) : 5;   // of a warp: at most a tile ahead
+    static constexpr int kRings = 8 * RH * kStages * kStage, kTerms = 2 * X * kATile * kPitch * 2, kSums = RT * 32 * kThreads * 4;
     static constexpr int kSmem = kRings + kTerms > kSums ? kRings + kTerms : kSums;
 };
 template <typename T, typename W, int RT, int RH, bool VEC>
 __global__ void __launch_bounds__(kAThreads * RH, RH == 1 && Terms<T>::n + Terms<W>::n <= 3 ? 2 : 1) k_adapter_grad(const __grid_constant__ AdapterGradArgs b) {
     using S = GradShape<T, W, RT, RH>;
     constexpr int X = S::X, Y = S::Y, pitch = S::kPitch, kRows = S::kRows, kThreads = S::kThreads;
-    extern __shared__ __align__(16) uint8_t raw[];   // rings of the warps, terms [X][kRows][pitch]; in the end sums [32 RT][threads]
+    extern __shared__ __align__(16) uint8_t raw[];   // rings of the warps, terms [2][X][kATile][pitch]; in the end sums [32 RT][threads]
     after_earlier_kernels();
     const bool second = (int)blockIdx.x >= b.first;
     const AdapterSum& a = b.sums[second ? 1 : 0];
@@ -687,54 +732,73 @@ __global__ void __launch_bounds__(kAThreads * RH, RH == 1 && Terms<T>::n + Terms
     const int begin = b.plan.offsets[i], end = b.plan.offsets[i + 1], groups = (end - begin + 15) / 16;
     const int t_first = begin + (int)((long long)groups * part / b.parts) * 16, t_last = min(end, begin + (int)((long long)groups * (part + 1) / b.parts) * 16);
     uint16_t* terms = reinterpret_cast<uint16_t*>(raw + S::kRings);
-    const uint32_t ring = smem_u32(raw) + (uint32_t)(warp * S::kStages * S::kStage) + 16u * lane;
+    __shared__ int order[3 * kATile];
+    __shared__ long long offset[3 * kATile];   // of the tokens' rows
+    const uint32_t ring = smem_u32(raw) + (uint32_t)(warp * S::kStages * S::kStage) + 16u * (q * 8 + g);   // (requests are rows of 128 bytes)
     float acc[RT][8][4] = {};
     if (t_first < t_last) {   // (the same in all threads)
         const T* x = static_cast<const T*>(a.x) + c0;
-        // this thread's rows of sixteen tokens, asked for a step before their copies
-        int rows[4];
-        const auto ask = [&](int t0) {
+        const uint32_t terms_at = smem_u32(terms) + (uint32_t)((((lane & 7) + (lane >> 4) * 8) * pitch + row0 + (lane >> 3 & 1) * 8) * 2);
+        const bool loads = !idle && have > 0;   // (a column that is none has no sum that is used)
+        // which tokens: those of three tiles, asked for another tile ahead
+        const auto token = [&](int tile) {
+            const int at = t_first + tile * kATile + (int)threadIdx.x;
+            return threadIdx.x < kATile && at < t_last ? b.plan.order[at] : -1;
+        };
+        const auto keep = [&](int tile, int row) {
+            if (threadIdx.x >= kATile) return;
+            order[tile % 3 * kATile + threadIdx.x] = row;
+            offset[tile % 3 * kATile + threadIdx.x] = row * a.x_stride;
+        };
+        const int ranks_all = sixteens(b.rank);
+        const auto fill_terms = [&](int tile) {
+            const uint32_t to = smem_u32(terms) + (uint32_t)((tile & 1) * X * kATile * pitch * 2);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int t = t0 + 2 * q + (k & 1) + (k >> 1) * 8;
-                rows[k] = t < t_last && have > 0 ? b.plan.order[t] : -1;
+            for (int row = (int)threadIdx.x / (kRows / 8); row < kATile; row += kThreads / (kRows / 8)) {
+                const int tok = order[tile % 3 * kATile + row], c = (int)threadIdx.x % (kRows / 8) * 8;
+                const bool zeros = tok < 0 || j0 + c >= ranks_all;
+                const uint16_t* from = a.mid + (zeros ? 0 : (long long)tok * ranks_all + j0 + c);
+#pragma unroll
+                for (int n = 0; n < X; ++n)
+                    ring_load8<false>(to + (uint32_t)(((n * kATile + row) * pitch + c) * 2), reinterpret_cast<const __nv_bfloat16*>(from + (long long)n * b.tokens * ranks_all), zeros);
             }
         };
-        int t_next = t_first, fstage = 0;
+        int t_next = t_first, next = 0, fstage = 0;   // next: t_next's place in `order`
         const auto fill = [&]() {
-            if (t_next < t_last && !idle)
+            if (t_next < t_last && loads) {
+                const uint32_t to = ring + (uint32_t)(fstage * S::kStage);
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    ring_load<VEC, (RH > 1)>(ring + (uint32_t)(fstage * S::kStage) + k * kPackBytes<T>, rows[k] >= 0 ? x + (long long)rows[k] * a.x_stride : static_cast<const T*>(a.x),
-                              rows[k] >= 0 ? have : 0, a.align_x);
+                for (int k = 0; k < 4; ++k) {
+                    // tokens behind the last are zeros: their terms are, and zero times a NaN is none
+                    const long long row = offset[next + 2 * q + (k & 1) + (k >> 1) * 8];
+                    if (VEC)
+                        ring_load8<(RH > 1)>(to + k * kPackBytes<T>, x + row, row < 0);
+                    else
+                        ring_load(to + k * kPackBytes<T>, x + row, row >= 0 ? have : 0, a.align_x);
+                }
+            }
+            t_next += 16;
+            next += 16;
+            if (next == 3 * kATile) next = 0;
             ring_commit();
             if (++fstage == S::kStages) fstage = 0;
-            t_next += 16;
-            ask(t_next);
         };
-        ask(t_first);
+        keep(0, token(0));
+        keep(1, token(1));
+        int row2 = token(2);
+        __syncthreads();
+        fill_terms(0);
         for (int s = 0; s < S::kStages - 1; ++s) fill();
-        int stage = 0;
-        for (int t0 = t_first; t0 < t_last; t0 += kATile) {
+        int stage = 0, tile = 0;
+        for (int t0 = t_first; t0 < t_last; t0 += kATile, ++tile) {
             const int n_tokens = min(kATile, t_last - t0);
-            __syncthreads();   // the terms before are read
-            // two tokens and four rows of mid a thread: words of two tokens' terms
-            for (int n = threadIdx.x; n < kATile / 2 * kRows / 4; n += kThreads) {
-                const int j = n % 4 + n / 128 * 4, t = n / 4 % 32 * 2;   // j: fours of rows
-                uint32_t w[2][4][X];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int tok = t + h < n_tokens ? b.plan.order[t0 + t + h] : -1;
-                    const float* p = a.mid + (long long)max(tok, 0) * b.rank + j0 + 4 * j;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) cut<X>(w[h][k], tok >= 0 && 4 * j + k < ranks ? p[k] : 0.f);
-                }
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-#pragma unroll
-                    for (int m = 0; m < X; ++m) *reinterpret_cast<uint32_t*>(terms + (m * kRows + 4 * j + k) * pitch + t) = halves(w[0][k][m], w[1][k][m]);
-            }
-            __syncthreads();
+            // this tile's terms came with the first group of the tile before, or the first of all
+            ring_wait(tile == 0 ? S::kStages - 2 : min(S::kStages - 1, 3));
+            const uint32_t terms_now = terms_at + (uint32_t)((tile & 1) * X * kATile * pitch * 2);
+            __syncthreads();   // ... for all, and the tile before's are read, its tokens, too
+            keep(tile + 2, row2);
+            row2 = token(tile + 3);
+            if (t0 + kATile < t_last) fill_terms(tile + 1);
 #pragma unroll 1
             for (int s = 0; s * 16 < n_tokens; ++s) {
                 fill();
@@ -750,8 +814,13 @@ __global__ void __launch_bounds__(kAThreads * RH, RH == 1 && Terms<T>::n + Terms
                     ring_read(f2, from + 3 * kPackBytes<T>);
                     cut_rows<Y>(hi, f, f2);
 #pragma unroll
-                    for (int m = 0; m < RT; ++m)
-                        add_products<X, Y, sizeof(W) == 4>(acc[m], terms + (row0 + m * 16 + g) * pitch + s * 16 + 2 * q, kRows * pitch, pitch, lo, hi);
+                    for (int m = 0; m < RT; ++m) {
+                        uint32_t w[X][4];
+#pragma unroll
+                        for (int n = 0; n < X; ++n) load_terms<true>(w[n], terms_now + (uint32_t)(((n * kATile + s * 16) * pitch + m * 16) * 2));
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) add_products<X, Y, sizeof(W) == 4>(acc[m][e], w, &lo[0][e], &hi[0][e], 8);
+                    }
                 }
                 if (++stage == S::kStages) stage = 0;
             }

@@ -255,7 +255,7 @@ int shares(int64_t pieces, int64_t most, int64_t length, int64_t least) {
 template <typename T, typename W, int JT> int launch_in(AdapterArgs a, int64_t tiles, cudaStream_t st) {
     using S = InShape<T, W, JT>;
     const int64_t blocks = ceil_div(a.rank, 8 * JT);
-    a.parts = shares(tiles * blocks, 4 * sm_count(), a.wide, 512);
+    a.parts = shares(tiles * blocks, 2 * sm_count(), a.wide, 256);
     return by_vec(a.align_x >= 16 && a.align_factor >= 16, [&](auto vec) {
         constexpr auto kernel = k_adapter_in<T, W, JT, decltype(vec)::value>;
         if (!allow_smem<kernel>(S::kSmem)) return (int)SBC_ECUDA;
@@ -276,6 +276,19 @@ int adapter_in(AdapterArgs a, int dtype, int weights, int64_t tokens, cudaStream
     });
 }
 
+template <typename T, typename W, int CB> int launch_out(const AdapterArgs& a, int64_t tiles, bool vec, cudaStream_t st) {
+    using S = OutShape<T, W, CB>;
+    constexpr int largest = std::min(SBC_ADAPTER_RANK, CB == 256 ? 128 / S::Y / 16 * 16 : SBC_ADAPTER_RANK);
+    static_assert(S::smem(largest) <= S::kMost, "a block's shared memory");
+    // about two blocks an SM, each with a run of the tiles
+    const int64_t columns = ceil_div(a.wide, CB), runs = std::min<int64_t>(tiles, std::max<int64_t>(1, (int64_t)sm_count() * 2 / columns));
+    return by_vec(vec, [&](auto v) {
+        constexpr auto kernel = k_adapter_out<T, W, CB, decltype(v)::value>;
+        if (!allow_smem<kernel>(S::kMost)) return (int)SBC_ECUDA;
+        return launch(kernel, dim3((unsigned)columns, (unsigned)runs), kAThreads, (size_t)S::smem(a.rank), st, 0, 0, a);
+    });
+}
+
 // out = base + scale mid factor
 int adapter_out(AdapterArgs a, int dtype, int weights, int64_t tokens, cudaStream_t st) {
     const int width = width_of(dtype);
@@ -286,16 +299,10 @@ int adapter_out(AdapterArgs a, int dtype, int weights, int64_t tokens, cudaStrea
     return by_types(dtype, weights, [&](auto* t, auto* w) {
         using T = std::remove_pointer_t<decltype(t)>;
         using W = std::remove_pointer_t<decltype(w)>;
-        using S = OutShape<T, W>;
-        constexpr int most = std::max(S::smem(16), S::smem(SBC_ADAPTER_RANK));
-        static_assert(most <= kSmemMost - 1024, "a block's shared memory");
-        // four blocks an SM, each with mid's terms once
-        const int64_t columns = std::min<int64_t>(ceil_div(a.wide, S::kColumns), std::max<int64_t>(1, ceil_div((int64_t)sm_count() * 4, tiles)));
-        return by_vec(a.align_base >= 16 && a.align_out >= 16 && a.align_factor >= 16, [&](auto vec) {
-            constexpr auto kernel = k_adapter_out<T, W, decltype(vec)::value>;
-            if (!allow_smem<kernel>(most)) return (int)SBC_ECUDA;
-            return launch(kernel, dim3((unsigned)tiles, (unsigned)columns), kAThreads, (size_t)S::smem(a.rank), st, 0, 0, a);
-        });
+        // the factor's terms leave two blocks of 16-bit ones on an SM, and fit one block otherwise
+        constexpr int terms = OutShape<T, W, 256>::Y;
+        const bool vec = a.align_base >= 16 && a.align_out >= 16 && a.align_factor >= 16;
+        return terms * sixteens(a.rank) <= 128 ? launch_out<T, W, 256>(a, tiles, vec, st) : launch_out<T, W, 128>(a, tiles, vec, st);
     });
 }
 
@@ -543,6 +550,11 @@ int sbc_gated_grad(const sbc_gated_weights* w, const void* x, int64_t tokens, in
     });
 }
 
+size_t sbc_adapter_mid_bytes(int64_t tokens, int64_t rank) {
+    if (tokens < 0 || tokens > kAdapterTokens || rank < 1 || rank > SBC_ADAPTER_RANK) return 0;
+    return (size_t)tokens * (size_t)sixteens((int)rank) * 6;
+}
+
 size_t sbc_adapter_plan_bytes(int64_t tokens, int64_t count) {
     if (tokens < 0 || tokens > kAdapterTokens || count < 1 || count > SBC_ADAPTER_COUNT) return 0;
     return (size_t)(ceil_div(16 * (1 + most_tiles(tokens, count)) + 4 * (count + 2 + tokens), 16) * 16);
@@ -561,7 +573,7 @@ int sbc_adapter_plan(const int32_t* ids, int64_t tokens, int64_t count, void* pl
 }
 
 int sbc_adapter(const sbc_adapters* w, const void* x, int dtype, int64_t tokens, int64_t x_stride, const int32_t* ids, const void* plan,
-                float scale, const void* base, int64_t base_stride, void* out, int64_t out_stride, float* mid, uint32_t* status,
+                float scale, const void* base, int64_t base_stride, void* out, int64_t out_stride, void* mid, uint32_t* status,
                 sbc_cuda_stream_t stream) {
     if (!adapters_ok(w, dtype) || tokens < 0 || tokens > kAdapterTokens || !aligned(status, 4)) return SBC_EINVAL;
     if (tokens == 0) return SBC_OK;
@@ -600,7 +612,8 @@ int sbc_adapter(const sbc_adapters* w, const void* x, int dtype, int64_t tokens,
     a.plan = plan_at(plan, tokens, w->count);
     a.count = (int)w->count;
     a.rank = (int)w->rank;
-    a.mid = mid;
+    a.mid = static_cast<uint16_t*>(mid);
+    a.tokens = (int)tokens;
     a.x = x;
     a.x_stride = x_stride;
     a.factor = w->down;
@@ -619,8 +632,8 @@ int sbc_adapter(const sbc_adapters* w, const void* x, int dtype, int64_t tokens,
 }
 
 int sbc_adapter_grad(const sbc_adapters* w, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, int dtype, int64_t tokens,
-                     const void* plan, const float* mid, float scale, const void* base, int64_t base_stride, void* dx, int64_t dx_stride,
-                     void* ddown, void* dup, float* dmid, sbc_cuda_stream_t stream) {
+                     const void* plan, const void* mid, float scale, const void* base, int64_t base_stride, void* dx, int64_t dx_stride,
+                     void* ddown, void* dup, void* dmid, sbc_cuda_stream_t stream) {
     if (!adapters_ok(w, dtype) || tokens < 0 || tokens > kAdapterTokens || (!dx && !ddown && !dup)) return SBC_EINVAL;
     const int width = width_of(w->dtype);
     if (!aligned(ddown, (uintptr_t)width) || !aligned(dup, (uintptr_t)width)) return SBC_EINVAL;
@@ -639,7 +652,8 @@ int sbc_adapter_grad(const sbc_adapters* w, const void* dy, int64_t dy_stride, c
     a.rank = (int)w->rank;
     int rc = SBC_OK;
     if (dx || ddown) {
-        a.mid = dmid;
+        a.mid = static_cast<uint16_t*>(dmid);
+        a.tokens = (int)tokens;
         a.x = dy;
         a.x_stride = dy_stride;
         a.factor = w->up;
@@ -660,10 +674,11 @@ int sbc_adapter_grad(const sbc_adapters* w, const void* dy, int64_t dy_stride, c
     if (rc == SBC_OK && (ddown || dup)) {
         AdapterGradArgs g = {};
         g.plan = a.plan;
+        g.tokens = (int)tokens;
         g.count = a.count;
         g.rank = a.rank;
-        g.sums[0] = {x, dmid, ddown, x_stride, (int)w->inner, 0, 0, 0, 1.f};
-        g.sums[1] = {dy, mid, dup, dy_stride, (int)w->outer, 0, 0, 0, scale};
+        g.sums[0] = {x, static_cast<const uint16_t*>(dmid), ddown, x_stride, (int)w->inner, 0, 0, 0, 1.f};
+        g.sums[1] = {dy, static_cast<const uint16_t*>(mid), dup, dy_stride, (int)w->outer, 0, 0, 0, scale};
         rc = adapter_grad(g, dtype, w->dtype, tokens, stream);
     }
     return rc;
