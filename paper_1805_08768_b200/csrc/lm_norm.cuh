@@ -375,7 +375,7 @@ constexpr int kNormSumCols = 32, kNormSumRows = 16;
 struct NormSumArgs {
     const float* partial;
     void *dweight, *dbias;
-    int cols, parts, f32, dtype;
+    int cols, parts, dtype;
 };
 __device__ __forceinline__ void store_as(void* p, long long i, float v, int dtype) {
     if (dtype == SBC_F32) static_cast<float*>(p)[i] = v;

@@ -53,7 +53,7 @@ class _FirstOnly(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, *grads):
-        raise RuntimeError("fp4_linear and distill_loss have no second derivatives")
+        raise RuntimeError("the library's operators have no second derivatives")
 
 
 def _first_only(grad, *sources):
