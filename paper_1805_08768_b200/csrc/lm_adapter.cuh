@@ -334,7 +334,7 @@ __host__ __device__ constexpr int sixteens(int rank) { return (rank + 15) / 16 *
 // mid[t][j] = scale sum_k x[t][k] factor[i][j][k] for a tile of tokens and up to 8 JT rows.  A thread takes eight neighbours
 // of a row, its four k's of two products (which element is which k is free as long as both operands agree).  A warp has half
 // of the tokens, so that two blocks fit an SM's registers; warps, and blocks of a cluster, take the wide axis in turns.  Their
-// sums meet in shared memory in a fixed order.  VEC: all rows begin at multiples of 16 bytes.
+// sums meet in shared memory in a fixed order.  VEC: all rows are whole eights that begin at multiples of 16 bytes.
 template <typename T, typename W, int JT> struct InShape {
     static constexpr int MT = 2, kHalves = 4 / MT, kRuns = 8 / kHalves, kPer = MT * JT * 4;
     static constexpr int kStage = MT * 2 * (int)kPackBytes<T> + JT * (int)kPackBytes<W>;   // of a warp

@@ -256,7 +256,7 @@ template <typename T, typename W, int JT> int launch_in(AdapterArgs a, int64_t t
     using S = InShape<T, W, JT>;
     const int64_t blocks = ceil_div(a.rank, 8 * JT);
     a.parts = shares(tiles * blocks, 2 * sm_count(), a.wide, 256);
-    return by_vec(a.align_x >= 16 && a.align_factor >= 16, [&](auto vec) {
+    return by_vec(a.wide % 8 == 0 && a.align_x >= 16 && a.align_factor >= 16, [&](auto vec) {
         constexpr auto kernel = k_adapter_in<T, W, JT, decltype(vec)::value>;
         if (!allow_smem<kernel>(S::kSmem)) return (int)SBC_ECUDA;
         return launch(kernel, dim3((unsigned)(tiles * a.parts), (unsigned)blocks), kAThreads, S::kSmem, st, a.parts, 0, a);
@@ -301,7 +301,7 @@ int adapter_out(AdapterArgs a, int dtype, int weights, int64_t tokens, cudaStrea
         using W = std::remove_pointer_t<decltype(w)>;
         // the factor's terms leave two blocks of 16-bit ones on an SM, and fit one block otherwise
         constexpr int terms = OutShape<T, W, 256>::Y;
-        const bool vec = a.align_base >= 16 && a.align_out >= 16 && a.align_factor >= 16;
+        const bool vec = a.wide % 8 == 0 && a.align_base >= 16 && a.align_out >= 16 && a.align_factor >= 16;
         return terms * sixteens(a.rank) <= 128 ? launch_out<T, W, 256>(a, tiles, vec, st) : launch_out<T, W, 128>(a, tiles, vec, st);
     });
 }
