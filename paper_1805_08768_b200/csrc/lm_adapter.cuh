@@ -22,6 +22,7 @@
 #include "../../include/sbc_block.h"
 #include "lm_common.cuh"
 #include "lm_product.cuh"
+#include "lm_ring.cuh"
 
 namespace sbclm {
 
@@ -225,23 +226,15 @@ __device__ __forceinline__ void add_products(float* acc, const uint32_t (*w)[4],
         for (int k = 0; k < 4; ++k) acc[k] += part[k];
 }
 
-// ---- a thread's own ring in shared memory ---------------------------------------------------
+// ---- packs in a thread's ring -----------------------------------------------------------
 //
-// Loads run ahead of the products by stages of such a ring: a thread copies eight elements at a time to places that it alone reads,
-// so nothing but its own wait stands between the two, registers hold only what the products take next, and an
-// SM has 100 KB and more under way.  A pack's granules of 16 bytes are 512 bytes apart: a warp's are side by side.
+// A pack's granules of 16 bytes are 512 bytes apart: a warp's are side by side.
 
 // Copies eight elements at a multiple of 16 bytes, or zeros (p is then not read).  SHARED: other warps load the same, so it may
 // stay in the first-level cache.  (Zeros by a predicate: a number of bytes in a register costs tens of instructions.)
 template <bool SHARED, typename T> __device__ __forceinline__ void ring_load8(uint32_t to, const T* p, bool zeros = false) {
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-        const char* from = reinterpret_cast<const char*>(p) + 16 * i;
-        if (SHARED)
-            asm volatile("{\n\t.reg .pred z;\n\tsetp.ne.u32 z, %2, 0;\n\tcp.async.ca.shared.global [%0], [%1], 16, z;\n\t}" ::"r"(to + 512 * i), "l"(from), "r"((uint32_t)zeros) : "memory");
-        else
-            asm volatile("{\n\t.reg .pred z;\n\tsetp.ne.u32 z, %2, 0;\n\tcp.async.cg.shared.global [%0], [%1], 16, z;\n\t}" ::"r"(to + 512 * i), "l"(from), "r"((uint32_t)zeros) : "memory");
-    }
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) ring_copy16<SHARED>(to + 512 * i, reinterpret_cast<const uint4*>(p) + i, zeros);
 }
 // Copies `have` elements (at most 8, zeros behind them) whose address is a multiple of `align`.
 template <typename T> __device__ __forceinline__ void ring_load(uint32_t to, const T* p, int have, int align) {
@@ -267,34 +260,15 @@ template <typename T> __device__ __forceinline__ void ring_load(uint32_t to, con
 #pragma unroll
             for (int k = 0; k < kEach; ++k)
                 if (k < have) v.e[k] = p[k];
-            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(v.q.x), "r"(v.q.y), "r"(v.q.z), "r"(v.q.w) : "memory");
+            ring_store16(to, v.q);
         }
     }
 }
 template <typename T> __device__ __forceinline__ void ring_read(Pack8<T>& v, uint32_t from) {
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i)
-        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
-                     : "=r"(v.q[i].x), "=r"(v.q[i].y), "=r"(v.q[i].z), "=r"(v.q[i].w)
-                     : "r"(from + 512 * i)
-                     : "memory");
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) v.q[i] = ring_read16(from + 512 * i);
 }
 template <typename T> constexpr uint32_t kPackBytes = 32 * 8 * sizeof(T);   // of a warp
-__device__ __forceinline__ void ring_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-// Waits until at most `left` (0 .. 7) of this thread's groups of copies are under way.
-__device__ __forceinline__ void ring_wait(int left) {
-    switch (left) {
-        case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
-        case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
-        case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
-        case 3: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
-        case 4: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
-        case 5: asm volatile("cp.async.wait_group 5;" ::: "memory"); break;
-        case 6: asm volatile("cp.async.wait_group 6;" ::: "memory"); break;
-        default: asm volatile("cp.async.wait_group 7;" ::: "memory"); break;
-    }
-}
-
 template <typename T> __device__ __forceinline__ void pack8(Pack8<T>& v, const float* f) {
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {

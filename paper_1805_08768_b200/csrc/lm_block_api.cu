@@ -21,14 +21,12 @@ struct NormPlan {
     int64_t blocks;
 };
 
-// `moved`: rows may begin off a multiple of 16 bytes and then touch one granule more.
-NormPlan plan_norm(int64_t rows, int64_t cols, bool moved, int most_granules) {
+// Backward.  `moved`: rows may begin off a multiple of 16 bytes and then touch one granule more.  Two blocks an SM stay, the
+// same number whatever the alignment (the sums of blocks have room by it).
+NormPlan plan_norm_grad(int64_t rows, int64_t cols, bool moved) {
     NormPlan p = {};
-    const int64_t n = ceil_div(cols + (moved ? 7 : 0), 8);
-    // blocks that stay, the same number whatever the alignment (the sums of blocks have room by it)
-    const int64_t most = std::max<int64_t>(8, sm_count() * 2);
-    p.granules = 1;
-    while (p.granules < most_granules && n > 256 * p.granules) p.granules *= 2;
+    const int64_t n = ceil_div(cols + (moved ? 7 : 0), 8), most = std::max<int64_t>(8, sm_count() * 2);
+    p.granules = n > 256 ? 2 : 1;
     if (n > (int64_t)kNormThreads * p.granules) {
         p.blocks = std::min(rows, std::min<int64_t>(most, std::max<int64_t>(1, ((int64_t)1 << 25) / cols)));
         return p;
@@ -38,6 +36,30 @@ NormPlan plan_norm(int64_t rows, int64_t cols, bool moved, int most_granules) {
     // rows of a group are a multiple of eight rows apart
     p.blocks = std::min(ceil_div(ceil_div(rows, p.groups), 8) * 8, most / 8 * 8);
     return p;
+}
+
+// Forward: as few threads a row as hold it, but enough rows or threads of one for the GPU.
+NormPlan plan_norm(int64_t rows, int64_t cols, bool moved, int width) {
+    NormPlan p = {};
+    const int64_t n = ceil_div(cols + (moved ? 7 : 0), 8), most_granules = 16 / width;
+    int64_t group = 32;
+    while (group < kNormThreads && (n > group * most_granules || (rows * group < (int64_t)sm_count() * 512 && n > group))) group *= 2;
+    if (n > group * most_granules || n * 64 > 96 * 1024) {   // (the weights leave room for two blocks on an SM)
+        p.blocks = std::min<int64_t>(rows, std::max(8, sm_count() * 2));
+        return p;
+    }
+    p.granules = 1;
+    while (p.granules < ceil_div(n, group)) p.granules *= 2;
+    p.group = (int)group;
+    p.groups = std::max(1, 256 / p.group);
+    // a block's rows are eight apart
+    p.blocks = std::min(ceil_div(ceil_div(rows, p.groups), 8) * 8, (int64_t)std::max(8, sm_count() * 2) / 8 * 8);
+    return p;
+}
+
+template <auto Kernel> int launch_norm(const NormArgs& a, const NormPlan& p, int smem, cudaStream_t st) {
+    if (!allow_smem<Kernel>(200 * 1024)) return SBC_ECUDA;
+    return launch(Kernel, dim3((unsigned)p.blocks), p.group * p.groups, (size_t)smem, st, 0, 0, a);
 }
 
 bool moved(const void* p, int64_t stride, int width) { return row_align(p, stride, width) < 16; }
@@ -359,20 +381,23 @@ int sbc_layer_norm(const void* x, int dtype, int64_t rows, int64_t cols, int64_t
     a.x_stride = x_stride;
     a.out_stride = y_stride;
     a.eps = eps;
-    const NormPlan p = plan_norm(rows, cols, moved(x, x_stride, width_of(dtype)), 4);
+    const NormPlan p = plan_norm(rows, cols, moved(x, x_stride, width_of(dtype)), width_of(dtype));
     a.group = p.group;
     a.groups = p.groups;
     return by_dtype(dtype, [&](auto* as) {
         using T = std::remove_pointer_t<decltype(as)>;
         if (!p.group) return launch(k_norm_long<T>, dim3((unsigned)p.blocks), kNormLong, 0, stream, 0, 0, a);
-        const auto kernel = p.granules == 1 ? k_norm<T, 1> : p.granules == 2 ? k_norm<T, 2> : k_norm<T, 4>;
-        return launch(kernel, dim3((unsigned)p.blocks), p.group * p.groups, 0, stream, 0, 0, a);
+        const int smem = (int)ceil_div(cols + 7, 8) * 64;
+        if constexpr (sizeof(T) == 2)
+            if (p.granules == 8) return launch_norm<k_norm<T, 8>>(a, p, smem, stream);
+        return p.granules == 1 ? launch_norm<k_norm<T, 1>>(a, p, smem, stream) : p.granules == 2 ? launch_norm<k_norm<T, 2>>(a, p, smem, stream)
+                                                                                                  : launch_norm<k_norm<T, 4>>(a, p, smem, stream);
     });
 }
 
 size_t sbc_layer_norm_workspace_bytes(int64_t rows, int64_t cols) {
     if (rows < 0 || rows > kMaxDim || cols < 1 || cols > kMaxDim) return 0;
-    const int64_t blocks = std::max(plan_norm(rows, cols, false, 2).blocks, plan_norm(rows, cols, true, 2).blocks);
+    const int64_t blocks = std::max(plan_norm_grad(rows, cols, false).blocks, plan_norm_grad(rows, cols, true).blocks);
     return (size_t)(ceil_div(blocks * 2 * cols * 4, 16) * 16 + 16);
 }
 
@@ -402,15 +427,15 @@ int sbc_layer_norm_grad(const void* dy, int64_t dy_stride, const void* x, int64_
     a.x_stride = x_stride;
     a.dy_stride = dy_stride;
     a.out_stride = dx_stride;
-    const NormPlan p = plan_norm(rows, cols, moved(x, x_stride, width_of(dtype)), 2);
+    const NormPlan p = plan_norm_grad(rows, cols, moved(x, x_stride, width_of(dtype)));
     a.group = p.group;
     a.groups = p.groups;
     if (rows > 0) {
         const int rc = by_dtype(dtype, [&](auto* as) {
             using T = std::remove_pointer_t<decltype(as)>;
             if (!p.group) return launch(k_norm_grad_long<T>, dim3((unsigned)p.blocks), kNormLong, 0, stream, 0, 0, a);
-            const size_t smem = sums && p.groups > 1 ? (size_t)cols * 8 : 0;
-            return launch(p.granules == 1 ? k_norm_grad<T, 1> : k_norm_grad<T, 2>, dim3((unsigned)p.blocks), p.group * p.groups, smem, stream, 0, 0, a);
+            const int smem = sums && p.groups > 1 ? (int)cols * 8 : 0;
+            return p.granules == 1 ? launch_norm<k_norm_grad<T, 1>>(a, p, smem, stream) : launch_norm<k_norm_grad<T, 2>>(a, p, smem, stream);
         });
         if (rc != SBC_OK) return rc;
     }

@@ -6,14 +6,17 @@
 // Bound by memory: forward reads x and writes y, backward reads x and dy and writes dx.  A group of
 // threads holds a row in registers, so each is touched once; the variance is the second pass over those
 // registers (no difference of large sums).  Groups stay and take row after row, so the weights, and in the
-// backward pass the sums over rows, stay in registers too.  A row is cut into granules of eight elements
+// backward pass the sums over rows, stay too.  A row is cut into granules of eight elements
 // whose boundaries in memory are multiples of 16 bytes, wherever the row begins: rows of odd lengths load
 // and store whole granules, only the first and the last one element by element.  All rows of a group
 // begin at the same place within 16 bytes (their distance is a multiple of eight rows), so an element's
 // column, weight and sum never change registers.
 #pragma once
 
+#include <type_traits>
+
 #include "lm_common.cuh"
+#include "lm_product.cuh"
 
 namespace sbclm {
 
@@ -93,77 +96,140 @@ template <typename T> __device__ __forceinline__ int phase_of(const T* row) { re
 // Whole granules of one row are whole granules of the other's memory too (for all rows of a group, if for its first).
 __device__ __forceinline__ bool same_phase(const void* p, const void* q) { return ((uintptr_t)p - (uintptr_t)q) % 16 == 0; }
 
-template <typename T, int NV> __global__ void __launch_bounds__(kNormThreads) k_norm(NormArgs a) {
+// Arithmetic is on two neighbours at a time (one instruction does both): with sixteen elements of a row a thread, instructions
+// are what these kernels are short of before memory is.
+typedef unsigned long long Two;
+__device__ __forceinline__ Two both(float v) { return pair(v, v); }
+template <typename T> __device__ __forceinline__ void as_pairs(Two* to, const Pack8<T>& v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (std::is_same<T, __nv_bfloat16>::value)
+            to[i] = pair(__uint_as_float(v.w[i] << 16), __uint_as_float(v.w[i] & 0xffff0000u));
+        else
+            to[i] = pair(to_float(v.e[2 * i]), to_float(v.e[2 * i + 1]));
+    }
+}
+__device__ __forceinline__ float sum_of(Two v) {
+    float a, b;
+    unpair(a, b, v);
+    return a + b;
+}
+// What of a thread's eight elements is not in the row becomes zero.
+__device__ __forceinline__ void clear_outside(Two* v, const Granule& g) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a, b;
+        unpair(a, b, v[i]);
+        v[i] = pair(2 * i < g.lo || 2 * i >= g.hi ? 0.f : a, 2 * i + 1 < g.lo || 2 * i + 1 >= g.hi ? 0.f : b);
+    }
+}
+
+
+// Eight results of a row; the first of them would be column `col`.
+template <typename T> __device__ __forceinline__ void store_row(T* row, const float* f, int col, bool whole, const Granule& g) {
+    if (whole) {
+        Pack8<T> v;
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            if constexpr (sizeof(T) == 4)
+                v.e[e] = f[e], v.e[e + 1] = f[e + 1];
+            else
+                v.w[e / 2] = pack2(f[e], f[e + 1], (const T*)nullptr);
+        }
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(row + col)[i] = v.q[i];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e >= g.lo && e < g.hi) row[col + e] = from_float<T>(f[e]);
+    }
+}
+
+// Few threads hold a row, each up to 64 elements of it, since sums over threads are what most instructions go into.  The weights
+// wait in shared memory as fours, so placed that a row's granules begin at them: all rows of a block begin at the same
+// place within 16 bytes.
+
+template <typename T, int NV> __global__ void __maxnreg__(NV * sizeof(T) <= 8 ? 80 : 128) k_norm(NormArgs a) {
     __shared__ float2 red[2][kNormThreads / 32];
-    after_earlier_kernels();
+    extern __shared__ __align__(16) uint8_t raw[];   // weights [w of the first four, of the last four, b likewise][granules] of four floats
     const int t = threadIdx.x % a.group, warps = a.group / 32;
-    const long long all = (long long)gridDim.x * a.groups, first = (long long)blockIdx.x * a.groups + threadIdx.x / a.group;
+    after_earlier_kernels();
+    const long long all = (long long)gridDim.x * a.groups;
+    const long long begin = blockIdx.x % 8 + 8ll * a.groups * (blockIdx.x / 8), first = begin + 8 * (threadIdx.x / a.group);
     const T* x = static_cast<const T*>(a.x) + first * a.x_stride;
     T* y = static_cast<T*>(a.out) + first * a.out_stride;
-    const int phase = phase_of(x);
+    const int phase = phase_of(x), n = (a.cols + phase + 7) / 8, last = (n - 1) / a.group;   // (last: granule of a thread that may be the row's last)
     const bool vec = same_phase(x, y);
-    const float share = 1.f / (float)a.cols;
-    float w[NV * 8], b[NV * 8];
+    float4* weights = reinterpret_cast<float4*>(raw);
+    for (int i = threadIdx.x; i < n * 2; i += blockDim.x) {
+        float w[4], b[4];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const Granule g(t + v * a.group, phase, a.cols);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const bool in = e >= g.lo && e < g.hi;
-            w[v * 8 + e] = !in ? 0.f : a.weight ? weight_at(a.weight, g.col + e, a.weight_f32, (const T*)nullptr) : 1.f;
-            b[v * 8 + e] = in && a.bias ? weight_at(a.bias, g.col + e, a.weight_f32, (const T*)nullptr) : 0.f;
+        for (int e = 0; e < 4; ++e) {
+            const int c = 4 * i + e - phase;
+            const bool is = c >= 0 && c < a.cols;
+            w[e] = !is ? 0.f : a.weight ? weight_at(a.weight, c, a.weight_f32, (const T*)nullptr) : 1.f;
+            b[e] = is && a.bias ? weight_at(a.bias, c, a.weight_f32, (const T*)nullptr) : 0.f;
         }
+        weights[(i & 1) * n + i / 2] = make_float4(w[0], w[1], w[2], w[3]);
+        weights[(2 + (i & 1)) * n + i / 2] = make_float4(b[0], b[1], b[2], b[3]);
     }
-    Pack8<T> next[NV];
-    const auto fetch = [&](const T* row, bool live) {
+    __syncthreads();
+    const float share = 1.f / (float)a.cols;
+    const bool ends = (phase | (a.cols & 7)) != 0;   // a row has granules that are not whole
+    for (long long base = begin, r = first; base < a.rows; base += all, r += all, x += all * a.x_stride, y += all * a.out_stride) {
+        Pack8<T> p[NV];
+        if (r < a.rows && (!ends || (r > 0 && r < a.rows - 1))) {   // (rows before and behind: whole granules are within the matrix)
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+                if (t + v * a.group < n)
+#pragma unroll
+                    for (int i = 0; i < (int)sizeof(T) / 2; ++i) p[v].q[i] = reinterpret_cast<const uint4*>(x + (8 * (t + v * a.group) - phase))[i];
+        } else if (r < a.rows) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+                if (t + v * a.group < n) load_granule(p[v], x, Granule(t + v * a.group, phase, a.cols), true);
+        }
+        // pairs of granule v, what is not in the row as zeros
+        const auto pairs_of = [&](Two* f, int v, float mean) {
+            as_pairs(f, p[v]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[i] = add2(f[i], both(-mean));
+            if ((v == 0 && ends) || v == last) clear_outside(f, Granule(t + v * a.group, phase, a.cols));
+        };
+        Two total = 0ull, f[4];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const Granule g(t + v * a.group, phase, a.cols);
-            if (live && g.hi > g.lo)
-                load_granule(next[v], row, g, true);
-            else
+            if (v > last) break;
+            pairs_of(f, v, 0.f);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) next[v].e[e] = from_float<T>(0.f);
+            for (int i = 0; i < 4; ++i) total = add2(total, f[i]);
         }
-    };
-    fetch(x, first < a.rows);
-    for (long long base = (long long)blockIdx.x * a.groups, r = first; base < a.rows; base += all, r += all, y += all * a.out_stride) {
-        float f[NV * 8];
-        float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-        for (int i = 0; i < NV * 8; ++i) {
-            f[i] = to_float(next[i / 8].e[i % 8]);
-            sum.x += f[i];
-        }
-        x += all * a.x_stride;
-        fetch(x, r + all < a.rows);
-        const float mean = group_sum(sum, red[0], warps).x * share;
-        sum.x = 0.f;
+        const float mean = group_sum(make_float2(sum_of(total), 0.f), red[0], warps).x * share;
+        total = 0ull;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const Granule g(t + v * a.group, phase, a.cols);
-            if (!g.whole()) {   // what is not in the row is no distance from the mean
+            if (v > last) break;
+            pairs_of(f, v, mean);
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (e < g.lo || e >= g.hi) f[v * 8 + e] = mean;
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                f[v * 8 + e] -= mean;
-                sum.x = fmaf(f[v * 8 + e], f[v * 8 + e], sum.x);
-            }
+            for (int i = 0; i < 4; ++i) total = fma2(f[i], f[i], total);
         }
-        const float rstd = 1.f / sqrtf(group_sum(sum, red[1], warps).x * share + a.eps);
+        const float rstd = rsqrtf(group_sum(make_float2(sum_of(total), 0.f), red[1], warps).x * share + a.eps);
         if (r >= a.rows) continue;
         if (t == 0 && a.stats) a.stats[r] = make_float2(mean, rstd);
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const Granule g(t + v * a.group, phase, a.cols);
-            if (g.hi <= g.lo) continue;
-            Pack8<T> o;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) o.e[e] = from_float<T>(fmaf(f[v * 8 + e] * rstd, w[v * 8 + e], b[v * 8 + e]));
-            store_granule(y, o, g, vec);
+            const int at = t + v * a.group;
+            if (v > last) break;
+            if (at >= n) continue;
+            const float4 w0 = weights[at], w1 = weights[n + at], b0 = weights[2 * n + at], b1 = weights[3 * n + at];
+            pairs_of(f, v, mean);
+            float o[8];
+            unpair(o[0], o[1], fma2(mul2(f[0], both(rstd)), pair(w0.x, w0.y), pair(b0.x, b0.y)));
+            unpair(o[2], o[3], fma2(mul2(f[1], both(rstd)), pair(w0.z, w0.w), pair(b0.z, b0.w)));
+            unpair(o[4], o[5], fma2(mul2(f[2], both(rstd)), pair(w1.x, w1.y), pair(b1.x, b1.y)));
+            unpair(o[6], o[7], fma2(mul2(f[3], both(rstd)), pair(w1.z, w1.w), pair(b1.z, b1.w)));
+            const Granule g(at, phase, a.cols);
+            store_row(y, o, 8 * at - phase, vec && ((v > 0 || !ends) && v < last ? true : g.whole()), g);
         }
     }
 }
