@@ -681,15 +681,18 @@ struct AdapterGradArgs {
     int tokens, count, rank, parts;
     int first;             // blocks of the first sum
 };
-template <typename T, typename W, int RT, int RH> struct GradShape {
+template <typename T, typename W, int RT, int RH, bool VEC> struct GradShape {
     static constexpr int X = sizeof(W) == 4 ? 3 : 2, Y = sizeof(W) == 4 ? Terms<T>::n : (Terms<T>::n < 2 ? Terms<T>::n : 2), kThreads = kAThreads * RH, kRows = 16 * RT * RH, kPitch = kRows + 8;
     static constexpr int kStage = 4 * (int)kPackBytes<T>, kStages = sizeof(T) == 4 ? (RH == 2 ? 2 : 3) : 5;   // of a warp: at most a tile ahead
-    static constexpr int kRings = 8 * RH * kStages * kStage, kTerms = 2 * X * kATile * kPitch * 2, kSums = RT * 32 * kThreads * 4;
+    // x comes as a tile's rows by bulk copies (two tiles have room), or through the warps' rings
+    static constexpr bool kBulk = VEC && sizeof(T) == 2;
+    static constexpr int kRowPitch = 512 * (int)sizeof(T) + 16;
+    static constexpr int kRings = kBulk ? 2 * kATile * kRowPitch : 8 * RH * kStages * kStage, kTerms = 2 * X * kATile * kPitch * 2, kSums = RT * 32 * kThreads * 4;
     static constexpr int kSmem = kRings + kTerms > kSums ? kRings + kTerms : kSums;
 };
 template <typename T, typename W, int RT, int RH, bool VEC>
 __global__ void __launch_bounds__(kAThreads * RH, RH == 1 && Terms<T>::n + Terms<W>::n <= 3 ? 2 : 1) k_adapter_grad(const __grid_constant__ AdapterGradArgs b) {
-    using S = GradShape<T, W, RT, RH>;
+    using S = GradShape<T, W, RT, RH, VEC>;
     constexpr int X = S::X, Y = S::Y, pitch = S::kPitch, kRows = S::kRows, kThreads = S::kThreads;
     extern __shared__ __align__(16) uint8_t raw[];   // rings of the warps, terms [2][X][kATile][pitch]; in the end sums [32 RT][threads]
     after_earlier_kernels();
@@ -708,8 +711,10 @@ __global__ void __launch_bounds__(kAThreads * RH, RH == 1 && Terms<T>::n + Terms
     uint16_t* terms = reinterpret_cast<uint16_t*>(raw + S::kRings);
     __shared__ int order[3 * kATile];
     __shared__ long long offset[3 * kATile];   // of the tokens' rows
+    __shared__ uint64_t bars[2];
     const uint32_t ring = smem_u32(raw) + (uint32_t)(warp * S::kStages * S::kStage) + 16u * (q * 8 + g);   // (requests are rows of 128 bytes)
     float acc[RT][8][4] = {};
+    bool late = false;
     if (t_first < t_last) {   // (the same in all threads)
         const T* x = static_cast<const T*>(a.x) + c0;
         const uint32_t terms_at = smem_u32(terms) + (uint32_t)((((lane & 7) + (lane >> 4) * 8) * pitch + row0 + (lane >> 3 & 1) * 8) * 2);
@@ -757,36 +762,80 @@ __global__ void __launch_bounds__(kAThreads * RH, RH == 1 && Terms<T>::n + Terms
             ring_commit();
             if (++fstage == S::kStages) fstage = 0;
         };
+        const uint32_t bar = smem_u32(bars), rows0 = smem_u32(raw);
+        const uint32_t row_bytes = (uint32_t)min((long long)kAThreads * 2, a.wide - cb) * (uint32_t)sizeof(T);
+        const auto fill_rows = [&](int tile) {   // a thread a row; rows that fill up the last sixteen are zeros
+            const int n = min(kATile, t_last - (t_first + tile * kATile));
+            const uint32_t to = rows0 + (uint32_t)((tile & 1) * kATile * S::kRowPitch);
+            for (int i = threadIdx.x; i < ((n + 15) / 16 * 16 - n) * (S::kRowPitch / 16); i += kThreads)
+                ring_store16(to + (uint32_t)((n + i / (S::kRowPitch / 16)) * S::kRowPitch + i % (S::kRowPitch / 16) * 16), make_uint4(0, 0, 0, 0));
+            before_copies();
+            if (threadIdx.x == 0) mbar_expect(bar + 8 * (tile & 1), (uint32_t)n * row_bytes);
+            if ((int)threadIdx.x < n)
+                bulk_load(to + threadIdx.x * S::kRowPitch, static_cast<const T*>(a.x) + offset[tile % 3 * kATile + threadIdx.x] + cb, row_bytes, bar + 8 * (tile & 1));
+        };
+        if (S::kBulk && threadIdx.x == 0) {
+            mbar_init(bar, 1);
+            mbar_init(bar + 8, 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
         keep(0, token(0));
         keep(1, token(1));
         int row2 = token(2);
         __syncthreads();
         fill_terms(0);
-        for (int s = 0; s < S::kStages - 1; ++s) fill();
+        if constexpr (S::kBulk) {
+            ring_commit();
+            fill_rows(0);
+        } else {
+            for (int s = 0; s < S::kStages - 1; ++s) fill();
+        }
         int stage = 0, tile = 0;
         for (int t0 = t_first; t0 < t_last; t0 += kATile, ++tile) {
             const int n_tokens = min(kATile, t_last - t0);
-            // this tile's terms came with the first group of the tile before, or the first of all
-            ring_wait(tile == 0 ? S::kStages - 2 : min(S::kStages - 1, 3));
+            if constexpr (S::kBulk) {
+                ring_wait(0);
+                late = !__syncthreads_and(!copies_late(bar + 8 * (tile & 1), (uint32_t)(tile >> 1) & 1));   // ... and the tile before is read
+                if (late) break;
+            } else {
+                // this tile's terms came with the first group of the tile before, or the first of all
+                ring_wait(tile == 0 ? S::kStages - 2 : min(S::kStages - 1, 3));
+                __syncthreads();   // ... for all, and the tile before's are read, its tokens, too
+            }
             const uint32_t terms_now = terms_at + (uint32_t)((tile & 1) * X * kATile * pitch * 2);
-            __syncthreads();   // ... for all, and the tile before's are read, its tokens, too
             keep(tile + 2, row2);
             row2 = token(tile + 3);
-            if (t0 + kATile < t_last) fill_terms(tile + 1);
+            if (t0 + kATile < t_last) {
+                fill_terms(tile + 1);
+                if constexpr (S::kBulk) fill_rows(tile + 1);
+            }
+            if constexpr (S::kBulk) ring_commit();
 #pragma unroll 1
             for (int s = 0; s * 16 < n_tokens; ++s) {
-                fill();
-                ring_wait(S::kStages - 1);
+                if constexpr (!S::kBulk) {
+                    fill();
+                    ring_wait(S::kStages - 1);
+                }
                 if (!idle) {
-                    const uint32_t from = ring + (uint32_t)(stage * S::kStage);
                     uint32_t lo[Y][8], hi[Y][8];
                     Pack8<T> f, f2;
-                    ring_read(f, from);
-                    ring_read(f2, from + kPackBytes<T>);
-                    cut_rows<Y>(lo, f, f2);
-                    ring_read(f, from + 2 * kPackBytes<T>);
-                    ring_read(f2, from + 3 * kPackBytes<T>);
-                    cut_rows<Y>(hi, f, f2);
+                    if constexpr (S::kBulk) {
+                        const uint32_t from = rows0 + (uint32_t)(((tile & 1) * kATile + s * 16 + 2 * q) * S::kRowPitch + (group * 64 + 8 * g) * (int)sizeof(T));
+                        f.q[0] = ring_read16(from);
+                        f2.q[0] = ring_read16(from + S::kRowPitch);
+                        cut_rows<Y>(lo, f, f2);
+                        f.q[0] = ring_read16(from + 8 * S::kRowPitch);
+                        f2.q[0] = ring_read16(from + 9 * S::kRowPitch);
+                        cut_rows<Y>(hi, f, f2);
+                    } else {
+                        const uint32_t from = ring + (uint32_t)(stage * S::kStage);
+                        ring_read(f, from);
+                        ring_read(f2, from + kPackBytes<T>);
+                        cut_rows<Y>(lo, f, f2);
+                        ring_read(f, from + 2 * kPackBytes<T>);
+                        ring_read(f2, from + 3 * kPackBytes<T>);
+                        cut_rows<Y>(hi, f, f2);
+                    }
 #pragma unroll
                     for (int m = 0; m < RT; ++m) {
                         uint32_t w[X][4];
@@ -808,7 +857,7 @@ __global__ void __launch_bounds__(kAThreads * RH, RH == 1 && Terms<T>::n + Terms
 #pragma unroll
         for (int e = 0; e < 8; ++e)
 #pragma unroll
-            for (int n = 0; n < 4; ++n) sums[((m * 8 + e) * 4 + n) * kThreads + threadIdx.x] = acc[m][e][n];
+            for (int n = 0; n < 4; ++n) sums[((m * 8 + e) * 4 + n) * kThreads + threadIdx.x] = late ? __uint_as_float(0x7fffffffu) : acc[m][e][n];
     if (b.parts > 1)
         cluster_sync();
     else

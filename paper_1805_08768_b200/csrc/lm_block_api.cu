@@ -328,21 +328,19 @@ int adapter_out(AdapterArgs a, int dtype, int weights, int64_t tokens, cudaStrea
     });
 }
 
-template <typename T, typename W, int RT, int RH> int launch_adapter_grad(AdapterGradArgs a, int64_t tokens, cudaStream_t st) {
-    using S = GradShape<T, W, RT, RH>;
-    static_assert(S::kSmem <= kSmemMost - 1024, "a block's shared memory");
+template <typename T, typename W, int RT, int RH, bool VEC> int launch_adapter_grad(AdapterGradArgs a, int64_t tokens, cudaStream_t st) {
+    using S = GradShape<T, W, RT, RH, VEC>;
+    static_assert(S::kSmem <= kSmemMost - 4096, "a block's shared memory");
     const int64_t rows = ceil_div(a.rank, S::kRows) * a.count;
     int64_t blocks[2];
     for (int i = 0; i < 2; ++i) blocks[i] = a.sums[i].out ? rows * (a.sums[i].columns = (int)ceil_div(a.sums[i].wide, kAThreads * 2)) : 0;
     if (blocks[0] + blocks[1] > kMaxDim / 8) return SBC_EINVAL;
-    a.parts = shares(blocks[0] + blocks[1], 4 * sm_count(), tokens, 64);
+    constexpr auto kernel = k_adapter_grad<T, W, RT, RH, VEC>;
+    if (!allow_smem<kernel>(S::kSmem)) return SBC_ECUDA;
+    // adapters differ in their tokens: about two blocks for each that an SM holds
+    a.parts = shares(blocks[0] + blocks[1], 2 * sm_count(), tokens, 64);
     a.first = (int)(blocks[0] * a.parts);
-    const auto vec_one = [&](const AdapterSum& s) { return !s.out || (s.align_x >= 16 && s.wide % 8 == 0); };
-    return by_vec(vec_one(a.sums[0]) && vec_one(a.sums[1]), [&](auto vec) {
-        constexpr auto kernel = k_adapter_grad<T, W, RT, RH, decltype(vec)::value>;
-        if (!allow_smem<kernel>(S::kSmem)) return (int)SBC_ECUDA;
-        return launch(kernel, dim3((unsigned)((blocks[0] + blocks[1]) * a.parts)), S::kThreads, S::kSmem, st, a.parts, 0, a);
-    });
+    return launch(kernel, dim3((unsigned)((blocks[0] + blocks[1]) * a.parts)), S::kThreads, S::kSmem, st, a.parts, 0, a);
 }
 
 // out = scale mid^T x of one sum or both
@@ -354,8 +352,12 @@ int adapter_grad(AdapterGradArgs a, int dtype, int weights, int64_t tokens, cuda
     return by_types(dtype, weights, [&](auto* t, auto* w) {
         using T = std::remove_pointer_t<decltype(t)>;
         using W = std::remove_pointer_t<decltype(w)>;
-        return a.rank <= 16 ? launch_adapter_grad<T, W, 1, 1>(a, tokens, st) : a.rank <= 32 ? launch_adapter_grad<T, W, 2, 1>(a, tokens, st)
-                                                                                             : launch_adapter_grad<T, W, 2, 2>(a, tokens, st);
+        const auto vec_one = [&](const AdapterSum& s) { return !s.out || (s.align_x >= 16 && s.wide % 8 == 0); };
+        return by_vec(vec_one(a.sums[0]) && vec_one(a.sums[1]), [&](auto vec) {
+            constexpr bool v = decltype(vec)::value;
+            return a.rank <= 16 ? launch_adapter_grad<T, W, 1, 1, v>(a, tokens, st) : a.rank <= 32 ? launch_adapter_grad<T, W, 2, 1, v>(a, tokens, st)
+                                                                                                    : launch_adapter_grad<T, W, 2, 2, v>(a, tokens, st);
+        });
     });
 }
 
