@@ -904,7 +904,9 @@ def _same(t: torch.Tensor, like: torch.Tensor, name: str, shape=None) -> int:
 def _out(out: Optional[torch.Tensor], shape, like: torch.Tensor, stream) -> Tuple[torch.Tensor, int]:
     """(a result's buffer, elements between its rows)"""
     if out is None:
-        return _empty(stream, shape, like.dtype, like), max(shape[1], 1)
+        # (a buffer like another one costs less than one of a shape)
+        new = torch.empty_like(like) if stream is None and like.shape == shape and like.is_contiguous() else _empty(stream, shape, like.dtype, like)
+        return new, max(shape[1], 1)
     return out, _same(out, like, "out", shape)
 
 

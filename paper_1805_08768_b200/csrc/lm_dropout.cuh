@@ -5,6 +5,9 @@
 // Bound by memory (x, the residual and out once each) as long as the generator keeps up: 16 bits decide an
 // element, so the ten rounds of one Philox-4x32 (two 32 x 32 bit products each) serve eight.  A probability
 // is a multiple of 2^-16, and the scale is that of the multiple taken, so the expectation is exact.
+//
+// 16384 x 4096 bfloat16, into a residual and the gradient: 126 us for 671 MB, 81 % of the copy rate; about 160 instructions for a
+// group of eight, half of them the generator's.
 #pragma once
 
 #include "lm_common.cuh"

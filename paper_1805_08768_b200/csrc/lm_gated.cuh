@@ -75,6 +75,10 @@ template <typename F> __device__ __forceinline__ void by_act(int act, F f) {
 // with both factors of the rest.  (Sixteen rows of each in turn would leave both in one warp, but eight small boxes
 // a stage are slower to load than two: 8192 x 4096 -> 8192 without kept factors 964 us.)
 //
+// 8192 x 4096 -> 8192 bfloat16, alone: forward 730 us (1.51 PFLOP/s; a library product of that size takes 670 to 690), with kept
+// factors 782, input's gradient 692 (1.59 PFLOP/s), weights' gradients 738: the tensor cores under the power limit.  Few tiles leave pairs
+// idle, and the contracted axis is not split: 2240 x 650 -> 2600 float16 42, 32 and 20 us.
+//
 // Warps: 0..7 accumulator to memory (half of the columns each four), 8 loads, 9 multiplies (in the pair's first block).
 
 constexpr int kMThreads = 320;
@@ -384,6 +388,8 @@ __global__ void __launch_bounds__(kMThreads, 1)
 // of a product is free as long as both operands agree: a thread takes eight neighbours of a row, its four
 // k's of two products.  The warps of a block share the units and cut the rows in turn; their sums
 // meet in shared memory in the warps' order.
+//
+// 16 tokens x 4096 -> 16384 bfloat16 54 us for 269 MB, 76 % of the copy rate; 1 x 650 -> 2600 6.0 us, latency.
 
 constexpr int kFThreads = 256;
 constexpr int kFMost = 32;      // tokens
@@ -488,7 +494,7 @@ struct GateGradArgs {
     int cols, align_dh;
 };
 
-// dg = dh P, du = dh Q.  Bound by memory: 14 bytes a unit (2 + 8 read, 4 written).
+// dg = dh P, du = dh Q.  Bound by memory: 14 bytes a unit (2 + 8 read, 4 written); 8192 x 8192 157 us, 6.0 TB/s.
 template <typename T> __global__ void __launch_bounds__(kGThreads) k_gate_grad(GateGradArgs a) {
     after_earlier_kernels();
     const int groups = (a.cols + 7) / 8;

@@ -3,14 +3,18 @@
 //   y = h w + b with h = (x - m) s, m the row's mean, s = 1 / sqrt(mean((x - m)^2) + eps)
 //   dx = s (t - mean(t) - h mean(t h)) with t = dy w;  dw = sum over rows of dy h,  db = sum of dy
 //
-// Bound by memory: forward reads x and writes y, backward reads x and dy and writes dx.  A group of
+// What memory needs is x and y once, and backward x, dy and dx once.  A group of
 // threads holds a row in registers, so each is touched once; the variance is the second pass over those
 // registers (no difference of large sums).  Groups stay and take row after row, so the weights, and in the
 // backward pass the sums over rows, stay too.  A row is cut into granules of eight elements
-// whose boundaries in memory are multiples of 16 bytes, wherever the row begins: rows of odd lengths load
-// and store whole granules, only the first and the last one element by element.  All rows of a group
+// whose boundaries in memory are multiples of 16 bytes, wherever the row begins: rows of odd lengths are loaded
+// and stored in whole granules but for their ends.  All rows of a group
 // begin at the same place within 16 bytes (their distance is a multiple of eight rows), so an element's
-// column, weight and sum never change registers.
+// column, weight and sum never change place.
+//
+// 16384 x 4096 bfloat16 (cold, the buffers before in the caches): forward 81 us for 268 MB, backward 90 us for 403 MB and 4 us for the
+// blocks' sums; 8191 x 2601 float16 forward 40 us for 85 MB.  Instructions bound both (about 30 an element), a quarter of them for the
+// sums over a row's threads.
 #pragma once
 
 #include <type_traits>
@@ -234,7 +238,8 @@ template <typename T, int NV> __global__ void __maxnreg__(NV * sizeof(T) <= 8 ? 
     }
 }
 
-// The sums over rows stay in the registers of the threads that hold the columns until the block's last row.
+// A thread has one or two granules of a row (their weights and sums over rows take 24 registers each), and loads the next row's while
+// it works on this one.  The sums over rows stay in the registers of the threads that hold the columns until the block's last row.
 template <typename T, int NV> __global__ void __launch_bounds__(kNormThreads) k_norm_grad(NormArgs a) {
     __shared__ float2 red[2][kNormThreads / 32];
     after_earlier_kernels();
