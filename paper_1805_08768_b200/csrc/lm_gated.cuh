@@ -45,7 +45,8 @@ template <int ACT, bool SLOPE> __device__ __forceinline__ void activate(float g,
         if (SLOPE) slope = share * other;
     } else {
         value = g * share;
-        if (SLOPE) slope = share * fmaf(g * dz, other, 1.f);
+        // (far out g dz leaves 32 bits where what it is multiplied by has become zero)
+        if (SLOPE) slope = share == 0.f ? 0.f : ACT == SBC_ACT_GELU_TANH && other == 0.f ? share : share * fmaf(g * dz, other, 1.f);
     }
 }
 

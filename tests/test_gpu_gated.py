@@ -133,6 +133,22 @@ def test_gated_activations(act, tokens):
     check_backward(*sbc.sbc_gated_grad(dh, x, gate, up, kept), dh, x, gate, up, act)
 
 
+@pytest.mark.parametrize("act", list(sbc.ACTIVATIONS))
+@pytest.mark.parametrize("tokens", [5, 150])
+def test_gated_far_tails(act, tokens):
+    """Projections of 1e13 and more, of either sign: the activations are what they tend to, and no gradient becomes a NaN."""
+    x, gate, up, dh = problem(tokens, 64, 96, torch.bfloat16)
+    x = x * 1e14
+    up = up * 1e-14
+    h, kept = sbc.sbc_gated(x, gate, up, act, keep=True)
+    assert bool(torch.isfinite(h).all()) and bool(torch.isfinite(kept).all()) and bool(torch.isfinite(sbc.sbc_gated(x, gate, up, act)).all())
+    g = x.double() @ gate.double().t()
+    far = g.abs() > 1e12
+    limit = torch.where(g > 0, 1.0 if act == "sigmoid" else g, 0.0)
+    assert bool(((kept[:, :, 1].double() - limit).abs() <= 2.0 ** -15 * limit.abs())[far].all())
+    assert all(bool(torch.isfinite(t).all()) for t in sbc.sbc_gated_grad(dh, x, gate, up, kept))
+
+
 def test_gated_gradients_of_32_bits_and_parts():
     x, gate, up, dh = problem(300, 130, 260, torch.bfloat16)
     h, kept = sbc.sbc_gated(x, gate, up, keep=True)
