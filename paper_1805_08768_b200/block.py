@@ -14,7 +14,7 @@ from typing import List, Optional, Sequence, Tuple
 import torch
 
 from . import binding
-from .distill import TeacherMessage, _first_only, _rows, distill_loss, fp4_apply, fp4_linear, teach
+from .distill import _FirstOnly, _first_only, _rows, distill_loss, fp4_apply, fp4_linear, teach
 
 
 def _flat(t: torch.Tensor) -> torch.Tensor:
@@ -68,27 +68,30 @@ class DropoutNumbers:
 
 class _Dropout(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, residual, p, rng, at):
+    def forward(ctx, x, residual, p, rng, at, tie):
         y = binding.sbc_dropout(_flat(x.detach()), p, rng, at, None if residual is None else _flat(residual.detach()))
-        ctx.save_for_backward(x, rng)   # (changed in place before the backward pass, autograd raises)
-        ctx.about = (p, at, residual is not None)
+        ctx.save_for_backward(rng)   # (changed in place before the backward pass, autograd raises); x itself is not kept
+        ctx.about = (p, at, residual is not None, x.shape, x.dtype)
+        ctx.tie = tie
         return y.view(x.shape)
 
     @staticmethod
     def backward(ctx, dy):
-        x, rng = ctx.saved_tensors
-        p, at, added = ctx.about
+        (rng,) = ctx.saved_tensors
+        p, at, added, shape, dtype = ctx.about
         dx = None
         if ctx.needs_input_grad[0]:
-            dx = _first_only(binding.sbc_dropout(_flat(dy.to(x.dtype)), p, rng, at).view(x.shape), dy, x)
-        return dx, dy if added and ctx.needs_input_grad[1] else None, None, None, None
+            dx = _first_only(binding.sbc_dropout(_flat(dy.to(dtype)), p, rng, at).view(shape), dy, *ctx.tie)
+        return dx, dy if added and ctx.needs_input_grad[1] else None, None, None, None, None
 
 
 def dropout(x: torch.Tensor, p: float, numbers: DropoutNumbers, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """residual + x, elements of x dropped with probability p and the others scaled up; no mask is kept."""
+    """residual + x, elements of x dropped with probability p and the others scaled up; neither a mask nor x is kept."""
     if residual is not None and (residual.shape != x.shape or residual.dtype != x.dtype):
         raise ValueError("the residual must have x's shape and type")
-    return _Dropout.apply(x, residual, p, numbers.rng, numbers.take(x.numel()))
+    # an empty tensor stands for x where a gradient's gradient is asked for (in a list: it is no input)
+    tie = [_FirstOnly.apply(x.new_empty(0), x)] if torch.is_grad_enabled() and x.requires_grad else []
+    return _Dropout.apply(x, residual, p, numbers.rng, numbers.take(x.numel()), tie)
 
 
 class _Gated(torch.autograd.Function):

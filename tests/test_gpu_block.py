@@ -66,6 +66,18 @@ def test_dropout_under_autograd():
         block.dropout(x, 0.4, numbers, r[:2])
 
 
+def test_dropout_keeps_nothing():
+    """Between the passes there is the output and nothing else: the input's memory is free once its owner lets go of it."""
+    numbers = block.DropoutNumbers(11, DEV)
+    leaf = randn(1, 64, seed=1).requires_grad_(True)
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    y = block.dropout(leaf.expand(1 << 14, 64) * 2.0, 0.5, numbers)   # (4 MB made and dropped, 4 MB out; a constant's product keeps no operand)
+    assert torch.cuda.memory_allocated() - before < 5 << 20
+    (grad,) = torch.autograd.grad(y.sum(), leaf)
+    assert grad.shape == leaf.shape
+
+
 @pytest.mark.parametrize("master", [torch.bfloat16, torch.float32])
 def test_gated_under_autograd(master):
     x = randn(2, 25, 48, seed=1, dtype=torch.bfloat16).requires_grad_(True)
