@@ -149,6 +149,12 @@ template <typename T> __device__ __forceinline__ void store_row(T* row, const fl
     }
 }
 
+// Whether all of a row's granules may be loaded whole: rows that are whole granules themselves (no `ends`), or whose neighbours,
+// eight elements or more each, cover what a granule reaches beyond the row (at most seven elements on either side).
+__host__ __device__ constexpr bool whole_granules_within(long long r, long long rows, int cols, bool ends) {
+    return !ends || (cols >= 8 && r > 0 && r < rows - 1);
+}
+
 // Few threads hold a row, each up to 64 elements of it, since sums over threads are what most instructions go into.  The weights
 // wait in shared memory as fours, so placed that a row's granules begin at them: all rows of a block begin at the same
 // place within 16 bytes.
@@ -182,7 +188,7 @@ template <typename T, int NV> __global__ void __maxnreg__(NV * sizeof(T) <= 8 ? 
     const bool ends = (phase | (a.cols & 7)) != 0;   // a row has granules that are not whole
     for (long long base = begin, r = first; base < a.rows; base += all, r += all, x += all * a.x_stride, y += all * a.out_stride) {
         Pack8<T> p[NV];
-        if (r < a.rows && (!ends || (r > 0 && r < a.rows - 1))) {   // (rows before and behind: whole granules are within the matrix)
+        if (r < a.rows && whole_granules_within(r, a.rows, a.cols, ends)) {
 #pragma unroll
             for (int v = 0; v < NV; ++v)
                 if (t + v * a.group < n)
