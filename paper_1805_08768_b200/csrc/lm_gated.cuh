@@ -436,11 +436,14 @@ template <typename T, int TT, int UT> __global__ void __launch_bounds__(kFThread
         x[i] = static_cast<const T*>(a.x) + (token[i] ? 8 * i + g : 0) * a.x_stride;
     }
     float acc[UT][TT][4] = {};
-    for (int k0 = warp * 32 + q * 8; k0 - q * 8 < a.inner; k0 += kWarps * 32 * kAhead) {
+    // (places are unsigned: the widest rows end less than a step of this loop below 2^31)
+    const uint32_t inner = (uint32_t)a.inner;
+    for (uint32_t k0 = warp * 32 + q * 8; k0 - q * 8 < inner; k0 += kWarps * 32 * kAhead) {
         Pack8<T> wg[kAhead][UT], wu[kAhead][UT], xs[kAhead][TT];
 #pragma unroll
         for (int s = 0; s < kAhead; ++s) {
-            const int k = k0 + s * kWarps * 32, have = a.inner - k;
+            const uint32_t k = k0 + s * kWarps * 32;
+            const int have = (int)(inner - k);
 #pragma unroll
             for (int i = 0; i < UT; ++i) {
                 load8(wg[s][i], gate[i] + k, has[i] ? have : 0, a.align_w);
