@@ -130,8 +130,8 @@ class _Adapter(torch.autograd.Function):
     def forward(ctx, x, base, down, up, ids, plan, scale, keep):
         flat, d, u = _flat(x.detach()), down.detach().contiguous(), up.detach().contiguous()
         shared = None if base is None else _flat(base.detach())
-        if not keep:
-            ctx.save_for_backward(x)
+        ctx.keep = keep
+        if not keep:   # (at most the base asks for a gradient, which is the output's)
             return binding.sbc_adapter(flat, d, u, ids, scale, shared, plan).view(*x.shape[:-1], u.shape[2])
         y, kept = binding.sbc_adapter(flat, d, u, ids, scale, shared, plan, keep=True)
         ctx.save_for_backward(x, down, up, flat, d, u, kept.mid, kept.plan.room)
@@ -140,6 +140,8 @@ class _Adapter(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dy):
+        if not ctx.keep:
+            return None, dy, None, None, None, None, None, None
         x, down, up, flat, d, u, mid, room = ctx.saved_tensors
         scale, tokens, count, shared = ctx.about
         need_x, need_base, need_d, need_u = ctx.needs_input_grad[:4]
