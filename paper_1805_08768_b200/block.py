@@ -130,25 +130,25 @@ class _Adapter(torch.autograd.Function):
     def forward(ctx, x, base, down, up, ids, plan, scale, keep):
         flat, d, u = _flat(x.detach()), down.detach().contiguous(), up.detach().contiguous()
         shared = None if base is None else _flat(base.detach())
-        ctx.keep = keep
+        ctx.keep, ctx.base = keep, None if base is None else base.shape
         if not keep:   # (at most the base asks for a gradient, which is the output's)
             return binding.sbc_adapter(flat, d, u, ids, scale, shared, plan).view(*x.shape[:-1], u.shape[2])
         y, kept = binding.sbc_adapter(flat, d, u, ids, scale, shared, plan, keep=True)
         ctx.save_for_backward(x, down, up, flat, d, u, kept.mid, kept.plan.room)
-        ctx.about = (scale, kept.plan.tokens, kept.plan.count, base is not None)
+        ctx.about = (scale, kept.plan.tokens, kept.plan.count)
         return y.view(*x.shape[:-1], u.shape[2])
 
     @staticmethod
     def backward(ctx, dy):
         if not ctx.keep:
-            return None, dy, None, None, None, None, None, None
+            return None, dy.reshape(ctx.base), None, None, None, None, None, None
         x, down, up, flat, d, u, mid, room = ctx.saved_tensors
-        scale, tokens, count, shared = ctx.about
+        scale, tokens, count = ctx.about
         need_x, need_base, need_d, need_u = ctx.needs_input_grad[:4]
         kept = binding.AdapterKept(mid, binding.AdapterPlan(room, tokens, count))
         dx, dd, du = binding.sbc_adapter_grad(_flat(dy.to(flat.dtype)), flat, d, u, kept, scale, None, need_x, need_d or need_u)
         sources = (dy, x, down, up)
-        return (_first_only(dx.view(x.shape), *sources) if need_x else None, dy if shared and need_base else None,
+        return (_first_only(dx.view(x.shape), *sources) if need_x else None, dy.reshape(ctx.base) if need_base else None,
                 _first_only(dd, *sources) if need_d else None, _first_only(du, *sources) if need_u else None, None, None, None, None)
 
 

@@ -50,3 +50,15 @@ def test_adapter_gives_every_gradient_that_is_asked_for(plain, asked):
     got = torch.autograd.grad(y, leaves, dy)
     assert all(torch.equal(a, b) for a, b in zip(got, [w for w, a in zip(want, asked) if a]))
     assert torch.equal(want[1], dy)
+
+
+@pytest.mark.parametrize("fixed", [False, True])
+def test_adapter_takes_a_base_of_any_leading_dimensions(plain, fixed):
+    """The base's rows are x's whatever dimensions they are in (what a projection of the flattened tokens gave), and so are its gradient's."""
+    g = torch.Generator().manual_seed(1)
+    x, base = torch.randn(2, 3, 4, generator=g), torch.randn(6, 5, generator=g).requires_grad_(True)
+    down, up = torch.randn(3, 2, 4, generator=g).requires_grad_(not fixed), torch.randn(3, 2, 5, generator=g)
+    y = block.adapter(x, down, up, torch.tensor([0, 2, -1, 1, 2, 0], dtype=torch.int32), 1.0, base)
+    dy = torch.randn(y.shape, generator=g)
+    (got,) = torch.autograd.grad(y, base, dy)
+    assert torch.equal(got, dy.view(6, 5))
