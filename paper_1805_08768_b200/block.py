@@ -14,7 +14,7 @@ from typing import List, Optional, Sequence, Tuple
 import torch
 
 from . import binding
-from .distill import _FirstOnly, _first_only, _rows, distill_loss, fp4_apply, fp4_linear, teach
+from .distill import TeacherMessage, _FirstOnly, _first_only, _rows, distill_loss, fp4_apply, fp4_linear, teach
 
 
 def _flat(t: torch.Tensor) -> torch.Tensor:
@@ -197,7 +197,7 @@ class AdaptedBlock:
 
 class ToyAdapters:
     """Clients that learn a teacher's logits by low-rank adapters alone.  Feeds ``DelayedSGD``: ``weights`` (one adapter, the
-    server's) and ``local_update``; all clients' iterations of a round run in one batch, from the first one's call on."""
+    server's) and ``local_updates``, which runs all clients' iterations of a round in one batch, or ``local_update`` for one client."""
 
     def __init__(self, n_clients: int, device: torch.device, width: int = 96, hidden: int = 160, words: int = 200, positions: int = 96,
                  rank: int = 4, k: int = 16, temperature: float = 2.0, lr: float = 4.0, seed: int = 0):
@@ -209,37 +209,51 @@ class ToyAdapters:
         self.x = torch.randn(n_clients * positions, width, generator=g).to(device, torch.bfloat16)
         self.ids = torch.arange(n_clients, device=device, dtype=torch.int32).repeat_interleave(positions)
         self.plan = binding.sbc_adapter_plan(self.ids, n_clients)
+        self.positions, self.alone = positions, binding.sbc_adapter_plan(torch.zeros_like(self.ids[:positions]), 1)
         # the teacher: the same block with an adapter that is not known to the clients
         taught = [torch.randn(1, *w.shape, generator=g).to(device) / w.shape[1] ** 0.5 for w in self.weights]
         y = self.block.serve(self.x, taught[0], 4 * taught[1], torch.zeros_like(self.ids))
         self.message = teach(fp4_linear(y, self.head), k, temperature)
         self.numbers = DropoutNumbers(seed + 3, device)
-        self._updates: List[List[torch.Tensor]] = []
 
-    def _loss(self, y: torch.Tensor) -> torch.Tensor:
-        return distill_loss(fp4_linear(y, self.head), self.message)
+    def _loss(self, y: torch.Tensor, message: Optional[TeacherMessage] = None) -> torch.Tensor:
+        return distill_loss(fp4_linear(y, self.head), self.message if message is None else message)
 
     def loss(self, weights: Optional[Sequence[torch.Tensor]] = None) -> float:
         down, up = (w[None] for w in (self.weights if weights is None else weights))
         with torch.no_grad():
             return float(self._loss(self.block.serve(self.x, down, up, torch.zeros_like(self.ids))).mean())
 
-    def step(self, down: torch.Tensor, up: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
-        """The gradients of all clients' adapters ([clients, rank, ...]) on their tokens."""
-        y = self.block.train(self.x, down, up, self.plan, self.numbers)
-        loss = self._loss(y).view(self.n_clients, -1).mean(1).sum()
+    def _grads(self, x: torch.Tensor, message: TeacherMessage, plan: binding.AdapterPlan, down: torch.Tensor,
+               up: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+        y = self.block.train(x, down, up, plan, self.numbers)
+        loss = self._loss(y, message).view(plan.count, -1).mean(1).sum()
         grads = torch.autograd.grad(loss, (down, up))
         self.numbers.next_step()
         return grads
 
+    def step(self, down: torch.Tensor, up: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+        """The gradients of all clients' adapters ([clients, rank, ...]) on their tokens."""
+        return self._grads(self.x, self.message, self.plan, down, up)
+
+    def _updates(self, step, clients: int, weights: Sequence[torch.Tensor], delay: int) -> List[List[torch.Tensor]]:
+        params = [w.detach().repeat(clients, 1, 1).requires_grad_(True) for w in weights]   # (copies: one client's, too)
+        for _ in range(delay):
+            grads = step(*params)
+            with torch.no_grad():
+                for w, g in zip(params, grads):
+                    w -= self.lr * g
+        return [[(w[c].detach() - w0).contiguous() for w, w0 in zip(params, weights)] for c in range(clients)]
+
+    def local_updates(self, weights: Sequence[torch.Tensor], delay: int) -> List[List[torch.Tensor]]:
+        """``delay`` SGD iterations of every client from ``weights``, in one batch; returns W_after - W of each."""
+        return self._updates(self.step, self.n_clients, weights, delay)
+
     def local_update(self, client: int, weights: Sequence[torch.Tensor], delay: int) -> List[torch.Tensor]:
-        """``delay`` SGD iterations from ``weights``; returns W_after - W of this client."""
-        if client == 0:
-            params = [w.detach().expand(self.n_clients, *w.shape).contiguous().requires_grad_(True) for w in weights]
-            for _ in range(delay):
-                grads = self.step(*params)
-                with torch.no_grad():
-                    for w, g in zip(params, grads):
-                        w -= self.lr * g
-            self._updates = [[(w[c].detach() - w0).contiguous() for w, w0 in zip(params, weights)] for c in range(self.n_clients)]
-        return self._updates[client]
+        """The same for one client, on its tokens alone."""
+        if not 0 <= client < self.n_clients:
+            raise IndexError(f"client {client} of {self.n_clients}")
+        rows = slice(client * self.positions, (client + 1) * self.positions)
+        values, indices, rest, temperature = self.message
+        message = TeacherMessage(values[rows], indices[rows], rest[rows], temperature)
+        return self._updates(lambda down, up: self._grads(self.x[rows], message, self.alone, down, up), 1, weights, delay)[0]

@@ -33,18 +33,23 @@ class DelayedSGD:
     ``weights``: list of float32 CUDA tensors (updated in place by every round).
     ``local_update(client, weights, delay) -> list of tensors``: runs ``delay`` SGD iterations for
     that client starting from ``weights`` (without changing them) and returns W_after - W per tensor.
+    ``local_updates(weights, delay) -> one such list per client``: in its place, for models that train
+    all clients of a round in one batch; called once a round.
     ``momenta``: optional per-tensor momentum buffers of the caller's optimiser; zeroed at every
     transmitted position (momentum masking, Supplement)."""
 
     def __init__(self, weights: Sequence[torch.Tensor], n_clients: int, p: float, delay: int,
-                 local_update: Callable[[int, Sequence[torch.Tensor], int], List[torch.Tensor]],
-                 momenta: Optional[Sequence[torch.Tensor]] = None):
+                 local_update: Optional[Callable[[int, Sequence[torch.Tensor], int], List[torch.Tensor]]] = None,
+                 momenta: Optional[Sequence[torch.Tensor]] = None,
+                 local_updates: Optional[Callable[[Sequence[torch.Tensor], int], List[List[torch.Tensor]]]] = None):
         if n_clients < 1 or delay < 1:
             raise ValueError("need at least one client and a delay of at least one iteration")
+        if (local_update is None) == (local_updates is None):
+            raise ValueError("either local_update or local_updates")
         self.weights = list(weights)
         self.flat = [w.view(-1) for w in self.weights]
         self.n_clients, self.p, self.delay = n_clients, float(p), int(delay)
-        self.local_update = local_update
+        self.local_update, self.local_updates = local_update, local_updates
         self.momenta = [m.view(-1) for m in momenta] if momenta is not None else None
         dev = self.weights[0].device
         sizes = [w.numel() for w in self.weights]
@@ -63,8 +68,12 @@ class DelayedSGD:
     def round(self) -> None:
         """One communication round of Algorithm 1 for all clients."""
         self.last_updates = []
+        together = None if self.local_updates is None else self.local_updates(self.weights, self.delay)
+        if together is not None and len(together) != self.n_clients:
+            raise ValueError(f"local_updates gave {len(together)} clients' updates, not {self.n_clients}")
         for c in range(self.n_clients):
-            upd = [u.contiguous().view(-1) for u in self.local_update(c, self.weights, self.delay)]
+            own = self.local_update(c, self.weights, self.delay) if together is None else together[c]
+            upd = [u.contiguous().view(-1) for u in own]
             self.last_updates.append(upd)
             binding.sbc_encode_batch(upd, self.residuals[c], self.ps, self.messages[c], self.mus[c], self.workspace)
         scale = 1.0 / self.n_clients

@@ -9,6 +9,7 @@ if not torch.cuda.is_available():  # pragma: no cover
 
 from paper_1805_08768_b200 import binding as sbc
 from paper_1805_08768_b200 import block, distill
+from paper_1805_08768_b200.dsgd import DelayedSGD
 
 DEV = torch.device("cuda:0")
 
@@ -30,3 +31,55 @@ def test_fixed_adapters_beside_a_trained_projection(tokens):
         (got,) = torch.autograd.grad(y, w, dy)
         (want,) = torch.autograd.grad(distill.fp4_linear(x, w), w, dy)
         assert torch.equal(got, want)
+
+
+def test_updates_are_of_the_call_that_asks():
+    """Clients in any order, weights and delays of any call: nothing is answered from an earlier one.  (95 positions: a client's
+    part of the batch begins at odd places.)"""
+    toy = block.ToyAdapters(3, DEV, positions=95)
+    other = [w + 0.05 * randn(*w.shape, seed=s) for s, w in enumerate(toy.weights)]
+
+    def ask(client, weights, delay):
+        toy.numbers.rng[1] = 5
+        return toy.local_update(client, weights, delay)
+
+    before = [w.clone() for w in toy.weights]
+    first = ask(1, toy.weights, 2)                     # not the first client first
+    assert all(torch.equal(a, b) for a, b in zip(before, toy.weights))
+    assert all(bool(torch.isfinite(u).all()) and float(u.abs().max()) > 0 for u in first)
+    assert all(torch.equal(a, b) for a, b in zip(first, ask(1, toy.weights, 2)))
+    for another in (ask(1, other, 2), ask(1, toy.weights, 1), ask(2, toy.weights, 2)):
+        assert not torch.equal(first[1], another[1])
+    assert all(torch.equal(a, b) for a, b in zip(first, ask(1, toy.weights, 2)))
+    with pytest.raises(IndexError):
+        toy.local_update(3, toy.weights, 1)
+
+
+def test_clients_together_and_alone():
+    """Without dropout a client's update in the batch is the one that it gets alone, up to roundings that fall to the other side
+    (as in test_gpu_block: within 2^-6 of the whole)."""
+    toy = block.ToyAdapters(3, DEV)
+    toy.block.p = 0.0
+    weights = [w + 0.05 * randn(*w.shape, seed=s) for s, w in enumerate(toy.weights)]
+    together = toy.local_updates(weights, 1)
+    for c in range(3):
+        for a, b in zip(together[c], toy.local_update(c, weights, 1)):
+            assert a.shape == b.shape and float((a - b).double().norm()) <= 2.0 ** -6 * float(b.double().norm())
+
+
+def test_federated_run_of_all_clients_in_one_batch():
+    toy = block.ToyAdapters(3, DEV)
+    run = DelayedSGD(toy.weights, 3, 0.05, 2, local_updates=toy.local_updates)
+    before = [w.clone() for w in run.weights]
+    for _ in range(3):
+        run.round()
+    run.check()
+    assert len(run.last_updates) == 3 and not torch.equal(run.last_updates[0][1], run.last_updates[1][1])
+    assert all(not torch.equal(a, b) and bool(torch.isfinite(b).all()) for a, b in zip(before, run.weights))
+    with pytest.raises(ValueError):
+        DelayedSGD(toy.weights, 3, 0.05, 2)
+    with pytest.raises(ValueError):
+        DelayedSGD(toy.weights, 3, 0.05, 2, toy.local_update, local_updates=toy.local_updates)
+    short = DelayedSGD(toy.weights, 2, 0.05, 2, local_updates=toy.local_updates)
+    with pytest.raises(ValueError):
+        short.round()
