@@ -50,7 +50,10 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
 
 class DropoutNumbers:
     """The random numbers of a client's steps: a key, a step that lies on the GPU, and how many of the step's numbers
-    its layers have taken so far.  A captured step draws anew in each replay if ``next_step`` is captured with it."""
+    its layers have taken so far.  A captured step draws anew in each replay if ``next_step`` is captured with it.
+
+    A layer that its backward pass computes again (activation checkpointing) has to draw what its forward pass drew:
+    ``take`` its numbers outside of what is computed again and give them to ``dropout`` as ``at``."""
 
     def __init__(self, seed: int, device: torch.device):
         self.rng = torch.tensor([int(seed) & ((1 << 63) - 1), 0], dtype=torch.int64, device=device)
@@ -62,6 +65,10 @@ class DropoutNumbers:
         self.taken = 0
 
     def take(self, elements: int) -> int:
+        """Numbers for so many elements that no other layer of the step has; where they begin."""
+        if torch._C._current_graph_task_id() != -1:
+            # (what is computed again would take others than its forward pass did, and nothing else would tell)
+            raise RuntimeError("numbers are taken in a backward pass: take them before the forward pass and give them to dropout as `at`")
         at, self.taken = self.taken, self.taken + (elements + 7) // 8
         return at
 
@@ -85,13 +92,15 @@ class _Dropout(torch.autograd.Function):
         return dx, dy if added and ctx.needs_input_grad[1] else None, None, None, None, None
 
 
-def dropout(x: torch.Tensor, p: float, numbers: DropoutNumbers, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """residual + x, elements of x dropped with probability p and the others scaled up; neither a mask nor x is kept."""
+def dropout(x: torch.Tensor, p: float, numbers: DropoutNumbers, residual: Optional[torch.Tensor] = None,
+            at: Optional[int] = None) -> torch.Tensor:
+    """residual + x, elements of x dropped with probability p and the others scaled up; neither a mask nor x is kept.
+    ``at``: where x's numbers begin, from ``numbers.take(x.numel())`` before; None: they are taken here."""
     if residual is not None and (residual.shape != x.shape or residual.dtype != x.dtype):
         raise ValueError("the residual must have x's shape and type")
     # an empty tensor stands for x where a gradient's gradient is asked for (in a list: it is no input)
     tie = [_FirstOnly.apply(x.new_empty(0), x)] if torch.is_grad_enabled() and x.requires_grad else []
-    return _Dropout.apply(x, residual, p, numbers.rng, numbers.take(x.numel()), tie)
+    return _Dropout.apply(x, residual, p, numbers.rng, numbers.take(x.numel()) if at is None else at, tie)
 
 
 class _Gated(torch.autograd.Function):
@@ -182,11 +191,12 @@ class AdaptedBlock:
         g = torch.Generator(device="cpu").manual_seed(seed)
         return [(torch.randn(rank, hidden, generator=g) / hidden ** 0.5).to(self.gate.device), torch.zeros(rank, width, device=self.gate.device)]
 
-    def train(self, x: torch.Tensor, down: torch.Tensor, up: torch.Tensor, plan: binding.AdapterPlan, numbers: DropoutNumbers) -> torch.Tensor:
-        """Tokens of many clients, each with its client's adapter."""
+    def train(self, x: torch.Tensor, down: torch.Tensor, up: torch.Tensor, plan: binding.AdapterPlan, numbers: DropoutNumbers,
+              at: Optional[int] = None) -> torch.Tensor:
+        """Tokens of many clients, each with its client's adapter.  ``at``: as for ``dropout``."""
         h = gated(layer_norm(x, *self.norm), self.gate, self.up, self.act)
         y = adapter(h, down, up, None, self.scale, fp4_linear(h, self.projection, self.format), plan)
-        return dropout(y, self.p, numbers, x)
+        return dropout(y, self.p, numbers, x, at)
 
     def serve(self, x: torch.Tensor, down: torch.Tensor, up: torch.Tensor, ids: torch.Tensor) -> torch.Tensor:
         """The next token of each of many requests, or whole prompts: nothing is dropped or kept."""

@@ -4,6 +4,7 @@ import itertools
 
 import pytest
 import torch
+from torch.utils.checkpoint import checkpoint
 
 from paper_1805_08768_b200 import binding, block
 
@@ -62,3 +63,31 @@ def test_adapter_takes_a_base_of_any_leading_dimensions(plain, fixed):
     dy = torch.randn(y.shape, generator=g)
     (got,) = torch.autograd.grad(y, base, dy)
     assert torch.equal(got, dy.view(6, 5))
+
+
+def drop(x, p, rng, at=0, residual=None):
+    """(each place in the step's numbers keeps other elements)"""
+    keep = (torch.arange(x.numel()) // 8 + at).view(x.shape) % 2 == 0
+    y = x * keep
+    return y if residual is None else y + residual
+
+
+@pytest.mark.parametrize("reentrant", [False, True])
+def test_dropout_that_is_computed_again(monkeypatch, reentrant):
+    """Under activation checkpointing the forward pass runs twice: with numbers taken before, the second time draws the same;
+    taking them there is refused, since the gradients would be another mask's."""
+    monkeypatch.setattr(binding, "sbc_dropout", drop)
+    x = torch.randn(3, 8, generator=torch.Generator().manual_seed(1)).requires_grad_(True)
+    numbers = block.DropoutNumbers(1, torch.device("cpu"))
+    numbers.take(8)
+    at = numbers.take(x.numel())
+    assert at == 1 and numbers.taken == 4
+    (want,) = torch.autograd.grad((block.dropout(x, 0.5, numbers, at=at) ** 2).sum(), x)
+    y = checkpoint(lambda t: block.dropout(t, 0.5, numbers, at=at) ** 2, x, use_reentrant=reentrant)
+    y.sum().backward()
+    assert torch.equal(x.grad, want) and numbers.taken == 4
+    y = checkpoint(lambda t: block.dropout(t, 0.5, numbers) ** 2, x, use_reentrant=reentrant)
+    with pytest.raises(RuntimeError, match="taken in a backward pass"):
+        y.sum().backward()
+    # outside of a backward pass numbers can be taken again
+    assert numbers.take(1) == 7

@@ -1,6 +1,7 @@
 """The operators of a client's own layers behind autograd, where a caller asks for less, or for more, than a whole step."""
 import pytest
 import torch
+from torch.utils.checkpoint import checkpoint
 
 pytestmark = pytest.mark.gpu
 
@@ -83,3 +84,27 @@ def test_federated_run_of_all_clients_in_one_batch():
     short = DelayedSGD(toy.weights, 2, 0.05, 2, local_updates=toy.local_updates)
     with pytest.raises(ValueError):
         short.round()
+
+
+@pytest.mark.parametrize("reentrant", [False, True])
+def test_block_that_is_computed_again(reentrant):
+    """A block under activation checkpointing gives the output and the gradients that it gives without, its dropout's numbers
+    taken before; without them it is refused."""
+    b = block.AdaptedBlock(96, 160, DEV, p=0.5, seed=3)
+    ids = (torch.arange(70, device=DEV) % 4).to(torch.int32)
+    plan = sbc.sbc_adapter_plan(ids, 4)
+    dy = randn(70, 96, seed=6, dtype=torch.bfloat16)
+    numbers = block.DropoutNumbers(5, DEV)
+
+    def grads(run):
+        leaves = [t.requires_grad_(True) for t in (randn(70, 96, seed=1, dtype=torch.bfloat16), randn(4, 6, 160, seed=3), randn(4, 6, 96, seed=4))]
+        y = run(*leaves)
+        y.backward(dy)
+        return [y.detach()] + [t.grad for t in leaves]
+
+    at = numbers.take(70 * 96)
+    want = grads(lambda x, d, u: b.train(x, d, u, plan, numbers, at))
+    got = grads(lambda x, d, u: checkpoint(lambda *t: b.train(*t, plan, numbers, at), x, d, u, use_reentrant=reentrant))
+    assert all(torch.equal(a, c) for a, c in zip(got, want))
+    with pytest.raises(RuntimeError, match="taken in a backward pass"):
+        grads(lambda x, d, u: checkpoint(lambda *t: b.train(*t, plan, numbers), x, d, u, use_reentrant=reentrant))
