@@ -136,13 +136,13 @@ def gated(x: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, act: str = "sil
 
 class _Adapter(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, base, down, up, ids, plan, scale, keep):
+    def forward(ctx, x, base, down, up, ids, plan, scale, keep, status):
         flat, d, u = _flat(x.detach()), down.detach().contiguous(), up.detach().contiguous()
         shared = None if base is None else _flat(base.detach())
         ctx.keep, ctx.base = keep, None if base is None else base.shape
         if not keep:   # (at most the base asks for a gradient, which is the output's)
-            return binding.sbc_adapter(flat, d, u, ids, scale, shared, plan).view(*x.shape[:-1], u.shape[2])
-        y, kept = binding.sbc_adapter(flat, d, u, ids, scale, shared, plan, keep=True)
+            return binding.sbc_adapter(flat, d, u, ids, scale, shared, plan, status=status).view(*x.shape[:-1], u.shape[2])
+        y, kept = binding.sbc_adapter(flat, d, u, ids, scale, shared, plan, keep=True, status=status)
         ctx.save_for_backward(x, down, up, flat, d, u, kept.mid, kept.plan.room)
         ctx.about = (scale, kept.plan.tokens, kept.plan.count)
         return y.view(*x.shape[:-1], u.shape[2])
@@ -150,7 +150,7 @@ class _Adapter(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         if not ctx.keep:
-            return None, dy.reshape(ctx.base), None, None, None, None, None, None
+            return None, dy.reshape(ctx.base), None, None, None, None, None, None, None
         x, down, up, flat, d, u, mid, room = ctx.saved_tensors
         scale, tokens, count = ctx.about
         need_x, need_base, need_d, need_u = ctx.needs_input_grad[:4]
@@ -158,16 +158,17 @@ class _Adapter(torch.autograd.Function):
         dx, dd, du = binding.sbc_adapter_grad(_flat(dy.to(flat.dtype)), flat, d, u, kept, scale, None, need_x, need_d or need_u)
         sources = (dy, x, down, up)
         return (_first_only(dx.view(x.shape), *sources) if need_x else None, dy.reshape(ctx.base) if need_base else None,
-                _first_only(dd, *sources) if need_d else None, _first_only(du, *sources) if need_u else None, None, None, None, None)
+                _first_only(dd, *sources) if need_d else None, _first_only(du, *sources) if need_u else None, None, None, None, None, None)
 
 
 def adapter(x: torch.Tensor, down: torch.Tensor, up: torch.Tensor, ids: Optional[torch.Tensor] = None, scale: float = 1.0,
-            base: Optional[torch.Tensor] = None, plan: Optional[binding.AdapterPlan] = None) -> torch.Tensor:
+            base: Optional[torch.Tensor] = None, plan: Optional[binding.AdapterPlan] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """base + scale (x down_i^T) up_i, i the adapter of the token (``ids``: int32, one per row of x, negative: none; or a
     ``plan`` of them, binding.sbc_adapter_plan, for all layers of a batch).  ``down`` [adapters, rank, in] and ``up``
-    [adapters, rank, out] are float32 or of x's type."""
+    [adapters, rank, out] are float32 or of x's type.  An id that is no adapter's counts as none, and STATUS_RANGE is or-ed into
+    ``status`` (int32 on the GPU, zeroed by the caller; with a plan, that of sbc_adapter_plan)."""
     keep = torch.is_grad_enabled() and any(t.requires_grad for t in (x, down, up))
-    return _Adapter.apply(x, base, down, up, ids, plan, scale, keep)
+    return _Adapter.apply(x, base, down, up, ids, plan, scale, keep, status)
 
 
 class AdaptedBlock:
@@ -198,11 +199,11 @@ class AdaptedBlock:
         y = adapter(h, down, up, None, self.scale, fp4_linear(h, self.projection, self.format), plan)
         return dropout(y, self.p, numbers, x, at)
 
-    def serve(self, x: torch.Tensor, down: torch.Tensor, up: torch.Tensor, ids: torch.Tensor) -> torch.Tensor:
-        """The next token of each of many requests, or whole prompts: nothing is dropped or kept."""
+    def serve(self, x: torch.Tensor, down: torch.Tensor, up: torch.Tensor, ids: torch.Tensor, status: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The next token of each of many requests, or whole prompts: nothing is dropped or kept.  ``status``: as for ``adapter``."""
         with torch.no_grad():
             h = gated(layer_norm(x, *self.norm), self.gate, self.up, self.act)
-            return x + adapter(h, down, up, ids, self.scale, fp4_apply(h, self.served))
+            return x + adapter(h, down, up, ids, self.scale, fp4_apply(h, self.served), status=status)
 
 
 class ToyAdapters:

@@ -108,3 +108,26 @@ def test_block_that_is_computed_again(reentrant):
     assert all(torch.equal(a, c) for a, c in zip(got, want))
     with pytest.raises(RuntimeError, match="taken in a backward pass"):
         grads(lambda x, d, u: checkpoint(lambda *t: b.train(*t, plan, numbers), x, d, u, use_reentrant=reentrant))
+
+
+@pytest.mark.parametrize("tokens", [20, 90])
+def test_ids_that_are_no_adapters_are_told(tokens):
+    """With and without gradients, for few tokens and for many: the caller sees it, and the token is one without an adapter."""
+    x, base = randn(tokens, 40, seed=1), randn(tokens, 56, seed=2)
+    down, up = randn(3, 5, 40, seed=3), randn(3, 5, 56, seed=4).requires_grad_(True)
+    ids = (torch.arange(tokens, device=DEV) % 3).to(torch.int32)
+    wrong = ids.clone()
+    wrong[tokens // 2] = 3
+    told = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for grad in (True, False):
+        with torch.set_grad_enabled(grad):
+            right = block.adapter(x, down, up, ids, 1.5, base, status=told)
+            assert int(told) == 0
+            y = block.adapter(x, down, up, wrong, 1.5, base, status=told)
+        assert int(told) == sbc.STATUS_RANGE
+        told.zero_()
+        others = torch.arange(tokens, device=DEV) != tokens // 2
+        assert torch.equal(y[~others], base[~others]) and torch.equal(y[others], right[others])
+    b = block.AdaptedBlock(96, 160, DEV, seed=3)
+    b.serve(randn(tokens, 96, seed=1, dtype=torch.bfloat16), randn(3, 6, 160, seed=3), randn(3, 6, 96, seed=4), wrong, told)
+    assert int(told) == sbc.STATUS_RANGE
