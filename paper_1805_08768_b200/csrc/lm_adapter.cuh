@@ -229,6 +229,44 @@ __device__ __forceinline__ void add_products(float* acc, const uint32_t (*w)[4],
         for (int k = 0; k < 4; ++k) acc[k] += part[k];
 }
 
+// An infinity's first term meets all terms of the other operand, and where one of those is zero the products' sum is a NaN that the
+// operands' product is not.  So what is a NaN is summed up again, by ordinary multiplications of whole operands, which says
+// whether it is one.  (Out of line: nothing of it costs what is finite more than the question.)
+template <typename X, typename Y> __device__ __forceinline__ float sum_again(int n, X x, Y y) {
+    float s = 0.f;
+    for (int k = 0; k < n && s == s; k += 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (k + i < n) s = fmaf(x(k + i), y(k + i), s);
+    }
+    return s;
+}
+// The value whose terms lie `plane` apart.
+__device__ __forceinline__ float joined(const uint16_t* terms, long long plane) {
+    float v = 0.f;
+#pragma unroll
+    for (int n = 2; n >= 0; --n) v += __uint_as_float((uint32_t)terms[n * plane] << 16);
+    return v;
+}
+template <typename T, typename W> __device__ __noinline__ float into_again(const T* x, const W* factor, int wide) {
+    return sum_again(wide, [&](int k) { return to_float(x[k]); }, [&](int k) { return to_float(factor[k]); });
+}
+// (eight neighbours of a row, whose base is in `out`)
+template <typename T, typename W>
+__device__ __noinline__ void out_again(const uint16_t* mid, long long plane, const W* factor, int rank, int wide, float scale, T* out, int have) {
+    for (int e = 0; e < have; ++e) {
+        const float s = sum_again(rank, [&](int j) { return joined(mid + j, plane); }, [&](int j) { return to_float(factor[(long long)j * wide + e]); });
+        out[e] = from_float<T>(fmaf(scale, s, to_float(out[e])));
+    }
+}
+template <typename T, typename W>
+__device__ __noinline__ void over_again(const uint16_t* mid, long long plane, int ranks, const T* x, long long x_stride, const int* order, int n, float scale, W* out, int have) {
+    for (int e = 0; e < have; ++e) {
+        const float s = sum_again(n, [&](int k) { return joined(mid + (long long)order[k] * ranks, plane); }, [&](int k) { return to_float(x[order[k] * x_stride + e]); });
+        out[e] = from_float<W>(s * scale);
+    }
+}
+
 // ---- packs in a thread's ring -----------------------------------------------------------
 //
 // A pack's granules of 16 bytes are 512 bytes apart: a warp's are side by side.
@@ -462,6 +500,8 @@ __global__ void __launch_bounds__(kAThreads, Terms<T>::n + Terms<W>::n <= 3 ? 2 
         const int n = i % 32, e = i / 32 % 4, j = i / 128 % JT, m = i / (128 * JT);   // m: halves and their tiles
         const int t = m * 16 + (e >> 1) * 8 + (n >> 2), r = j0 + 8 * j + (n & 3) * 2 + (e & 1);
         if (t >= at.z || r >= wide_rank) return;
+        if (v != v && r < a.rank)
+            v = into_again(static_cast<const T*>(a.x) + tokens[t] * a.x_stride, static_cast<const W*>(a.factor) + ((long long)at.x * a.rank + r) * a.wide, a.wide);
         uint32_t w[3];
         cut<3>(w, r < a.rank ? v * a.scale : 0.f);
         uint16_t* to = a.mid + (long long)tokens[t] * wide_rank + r;
@@ -630,6 +670,7 @@ __global__ void __launch_bounds__(kAThreads, sizeof(T) == 2 && Terms<W>::n == 1 
                 }
             }
         }
+        unsigned redo = 0;   // packs with a NaN
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -643,13 +684,25 @@ __global__ void __launch_bounds__(kAThreads, sizeof(T) == 2 && Terms<W>::n == 1 
                     if (!a.base) v = {};
                     if (!none) {
                         float f[8];
+                        bool again = false;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) f[e] = fmaf(a.scale, acc[m][e][2 * h + p], to_float(v.e[e]));
-                        pack8(v, f);
+                        for (int e = 0; e < 8; ++e) {
+                            f[e] = fmaf(a.scale, acc[m][e][2 * h + p], to_float(v.e[e]));
+                            again |= f[e] != f[e];
+                        }
+                        if (again)
+                            redo |= 1u << ((m * 2 + h) * 2 + p);   // (the base is left in its place)
+                        else
+                            pack8(v, f);
                     }
                     write8(out + 32 * p, v, a.wide - col - 32 * p - 8 * q, VEC || a.align_out >= 16);
                 }
             }
+        for (; redo; redo &= redo - 1) {
+            const int i = __ffs(redo) - 1, t = tokens[tile % 3][row0 + i / 2 * 8 + g], c = col + i % 2 * 32 + 8 * q;
+            out_again<T, W>(a.mid + (long long)t * ranks, (long long)a.tokens * ranks, static_cast<const W*>(a.factor) + (long long)now * a.rank * a.wide + c, a.rank, a.wide,
+                            a.scale, static_cast<T*>(a.out) + (long long)t * a.out_stride + c, min(8, a.wide - c));
+        }
         __syncthreads();   // this tile's terms and tokens, and the factor, are read
         if (!two && tile + 1 < last && after < a.count) {
             fill_terms(tile + 1);
@@ -860,7 +913,7 @@ __global__ void __launch_bounds__(kAThreads * RH, RH == 1 && Terms<T>::n + Terms
 #pragma unroll
         for (int e = 0; e < 8; ++e)
 #pragma unroll
-            for (int n = 0; n < 4; ++n) sums[((m * 8 + e) * 4 + n) * kThreads + threadIdx.x] = late ? __uint_as_float(0x7fffffffu) : acc[m][e][n];
+            for (int n = 0; n < 4; ++n) sums[((m * 8 + e) * 4 + n) * kThreads + threadIdx.x] = late ? __uint_as_float(0x7fffffffu) : acc[m][e][n];   // (summed up again below)
     if (b.parts > 1)
         cluster_sync();
     else
@@ -873,14 +926,19 @@ __global__ void __launch_bounds__(kAThreads * RH, RH == 1 && Terms<T>::n + Terms
         const long long c = cb + w * 64 + 8 * (n % 8);
         if (j >= ranks || c >= a.wide) continue;
         Pack8<W> v;
+        bool again = false;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const uint32_t from = smem_u32(&sums[at + e * 4 * kThreads]);
             float s = 0.f;
             for (int p = 0; p < b.parts; ++p) s += b.parts > 1 ? ld_cluster(map_rank(from, (uint32_t)p)) : sums[at + e * 4 * kThreads];
+            again |= s != s;
             v.e[e] = from_float<W>(s * a.scale);
         }
         write8(out + (long long)j * a.wide + c, v, (int)min(8ll, a.wide - c), a.align_out >= 16);
+        if (again)
+            over_again(a.mid + j0 + j, (long long)b.tokens * sixteens(b.rank), sixteens(b.rank), static_cast<const T*>(a.x) + c, a.x_stride, b.plan.order + begin, end - begin, a.scale,
+                       out + (long long)j * a.wide + c, (int)min(8ll, a.wide - c));
     }
     if (b.parts > 1) cluster_sync();
 }
