@@ -182,8 +182,12 @@ size_t sbc_adapter_mid_bytes(int64_t tokens, int64_t rank);
 
 /*
  * out[t, :] = base[t, :] + scale * (x[t, :] down_i^T) up_i,  i = ids[t]; sums in
- * 32 bits, operands of any type exact, rounded once.  Tokens without an adapter
- * get base[t, :] as it is.
+ * 32 bits, rounded once.  x and down are taken with all of their bits, and
+ * x down_i^T to 24 bits.  A call with a plan leaves out what is below 2^-21 of a
+ * product's magnitude or, in products that end as 16-bit results, 2^-14; so does
+ * sbc_adapter_grad.
+ * Infinities and NaNs are those of the formula.  Tokens without an adapter get
+ * base[t, :] as it is.
  *
  * x     device, dtype, tokens x inner
  * plan  of the batch, made for `count` adapters, or NULL: then ids are read

@@ -12,11 +12,14 @@
 // (67 and 134 MB of x), out of it 97 and 57 (268 and 134 MB), both sums over tokens 175.  The instructions between the products bound
 // all three (LSU pipe 40 to 58 %, tensor pipe 20 to 33 %).
 //
-// As good as 32-bit arithmetic whatever the types: an operand goes into the products as the bfloat16 terms that it is the sum of (one
-// for bfloat16, two for float16, three for float32, cut off rather than rounded, so that none overflows),
-// and of the terms' products those count that are not below 2^-24 of the first.  mid and dmid are kept as three terms.  Where a result
-// has 32 bits, a product's sum starts from zero and is added by an ordinary addition: the tensor cores cut off what they
-// align to a running sum, which over 4096 elements came to 1.6e-6 of the result instead of 1e-7.
+// Operands go into the products as the bfloat16 terms that they are the sum of (one for bfloat16, two for float16, three for float32,
+// cut off rather than rounded, so that none overflows): n terms leave less than 2^(1 - 8 n) of a value.  mid and dmid are kept as three
+// terms, and where a result has 32 bits all operands have theirs.  Of three by three products the six largest count; the others are below
+// 2^-21 of a product (2^-25 on average), which measures as 32-bit arithmetic does (1e-7 of the result after 4096 elements).  There a
+// step's sum starts from zero and is added by an ordinary addition: the tensor cores cut off what they align to a running sum, which
+// came to 1.6e-6.  Where a result has 16 bits, two terms of mid, dmid and float32 factors are taken, and all of their products: what is
+// left out is below 2^-14 of a product (half a step of the result is 2^-9 or 2^-12 of it), and each error against 64 bits measures
+// the same as that of 32-bit arithmetic, rounded once (1.00 times over all cases).
 //
 // Tokens come in any order.  A plan groups them: the tokens of an adapter one behind the other in the order in which
 // they came (so sums have one order), cut into tiles of 64.
@@ -218,7 +221,7 @@ __device__ __forceinline__ void add_products(float* acc, const uint32_t (*w)[4],
     float part[4] = {};
     float* d = APART ? part : acc;
 #pragma unroll
-    for (int order = X - 1; order >= 0; --order)   // the small products first
+    for (int order = 2; order >= 0; --order)   // the small products first
 #pragma unroll
         for (int n = 0; n < X; ++n) {
             const int o = order - n;
@@ -538,7 +541,7 @@ __global__ void __launch_bounds__(kAThreads, Terms<T>::n + Terms<W>::n <= 3 ? 2 
 // tile are on their way while this one's products are made.  A warp has 64 columns and as many tokens as leaves eight
 // warps busy.  The factor's columns are so placed that a thread ends with eight neighbours of a row, twice.
 template <typename T, typename W, int CB> struct OutShape {
-    // 16-bit results: what lies 2^-16 below a factor does not reach them
+    // 16-bit results: two terms, what is left out is below 2^-15 of a factor
     static constexpr int X = sizeof(T) == 4 ? 3 : 2, Y = sizeof(T) == 4 ? Terms<W>::n : (Terms<W>::n < 2 ? Terms<W>::n : 2);
     static constexpr int kGroups = CB / 64, MT = kGroups / 2, kBase = MT * 4 * (int)kPackBytes<T>, kFactorPitch = CB + 8;
     static __host__ __device__ constexpr int pitch(int rank) { return sixteens(rank) + 8; }

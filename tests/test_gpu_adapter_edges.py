@@ -98,3 +98,26 @@ def test_whole_operands_beside_small_terms():
     down[1, :, 3] = 0.5
     up[1] = 2.0 ** -4
     check(x, base, dy, down, up, ids)
+
+
+@pytest.mark.parametrize("kind", [KINDS[2], KINDS[4]])
+def test_terms_at_their_largest(kind):
+    """Two factors whose lower terms are as large as they can be, and a base that takes their product's larger part away: two terms
+    of each and all of their products leave less than 2 x 2^-15 of it (both seconds' product alone is nearly 2^-14)."""
+    tokens, inner, outer = 70, 24, 48
+    v = 1 + 2.0 ** -7 - 2.0 ** -23
+    x = torch.zeros(tokens, inner, device=DEV, dtype=kind[0])
+    x[:, 3] = 1
+    base = torch.full((tokens, outer), -1.0, device=DEV, dtype=kind[0])
+    down, up = torch.zeros(1, 1, inner, device=DEV), torch.full((1, 1, outer), v, device=DEV)
+    down[0, 0, 3] = v
+    ids = torch.zeros(tokens, dtype=torch.int32, device=DEV)
+    y_of = expected(x, base, base, torch.zeros_like(x), down, up, ids, 1.0)[0]
+    near(sbc.sbc_adapter(x, down, up, ids, 1.0, base), *y_of)
+    # the same on the way back: dy up^T is v, its product with down v^2
+    dy = torch.zeros_like(base)
+    dy[:, 5] = 1
+    dx_base = torch.full_like(x, -1.0)
+    _, kept = sbc.sbc_adapter(x, down, up, ids, 1.0, base, keep=True)
+    dx_of = expected(x, base, dy, dx_base, down, up, ids, 1.0)[1]
+    near(sbc.sbc_adapter_grad(dy, x, down, up, kept, 1.0, dx_base)[0], *dx_of)
