@@ -19,7 +19,9 @@ namespace sbclm {
 
 // ---- activations ------------------------------------------------------------------------
 
-// act(g) and its derivative.  Sigmoids by exp(-g), so that small ones keep their digits.
+// act(g) and its derivative.  Sigmoids by exp(-|g|), so that small ones keep their digits down to the smallest numbers.  The fast
+// exponential and quotient (off by (2 + 1.2 |z|) 2^-23 and 2^-22 of themselves) are far below the results' 2^-9 or 2^-12, and the
+// epilogue is what the tensor cores wait for.
 template <int ACT, bool SLOPE> __device__ __forceinline__ void activate(float g, float& value, float& slope) {
     if (ACT == SBC_ACT_RELU) {
         value = g < 0.f ? 0.f : g;   // (a NaN stays one)
@@ -29,24 +31,27 @@ template <int ACT, bool SLOPE> __device__ __forceinline__ void activate(float g,
     if (ACT == SBC_ACT_GELU) {
         const float p = normcdff(g);
         value = g * p;
-        if (SLOPE) slope = fmaf(g * 0.3989422804f, __expf(-0.5f * g * g), p);
+        if (SLOPE) {
+            const float density = __expf(-0.5f * g * g);
+            slope = density == 0.f ? p : fmaf(g * 0.3989422804f, density, p);   // (an infinite g times nothing)
+        }
         return;
     }
-    // share = 1 / (1 + exp(-z))
+    // share = 1 / (1 + exp(-z)), other = 1 - share
     float z = g, dz = 1.f;
     if (ACT == SBC_ACT_GELU_TANH) {
         z = 1.5957691216f * g * fmaf(0.044715f, g * g, 1.f);
         if (SLOPE) dz = 1.5957691216f * fmaf(3.f * 0.044715f, g * g, 1.f);
     }
-    const float e = __expf(-z), share = __fdividef(1.f, 1.f + e);
-    const float other = z > 0.f ? e * share : 1.f - share;
+    const float e = __expf(-fabsf(z)), large = __fdividef(1.f, 1.f + e), small = e * large;   // (the divisor is 1 .. 2)
+    const float share = z > 0.f ? large : small, other = z > 0.f ? small : large;
     if (ACT == SBC_ACT_SIGMOID) {
         value = share;
         if (SLOPE) slope = share * other;
     } else {
         value = g * share;
         // (far out g dz leaves 32 bits where what it is multiplied by has become zero)
-        if (SLOPE) slope = share == 0.f ? 0.f : ACT == SBC_ACT_GELU_TANH && other == 0.f ? share : share * fmaf(g * dz, other, 1.f);
+        if (SLOPE) slope = share == 0.f ? 0.f : other == 0.f ? share : share * fmaf(g * dz, other, 1.f);
     }
 }
 
