@@ -40,3 +40,18 @@ def test_layer_norm_rows_do_not_see_their_neighbours(dtype):
             spoilt = x.clone()
             spoilt[1::2] = bad
             assert torch.equal(sbc.sbc_layer_norm(spoilt)[0][::2], want[::2])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [8193, 9000, 16384, 20001])
+def test_layer_norm_gradients_of_many_long_rows(cols, dtype):
+    """Rows longer than a group holds, several for every block (two an SM), so that its sums over rows go on from row to row."""
+    rows = 2 * torch.cuda.get_device_properties(DEV).multi_processor_count * 3 + 5
+    x, dy = values(rows, cols, dtype, 1), values(rows, cols, dtype, 2)
+    w, b = torch.randn(cols, device=DEV), torch.randn(cols, device=DEV)
+    y, stats = sbc.sbc_layer_norm(x, w, b)
+    check_forward(y, x, w, b, 1e-5)
+    dx, dw, db = sbc.sbc_layer_norm_grad(dy, x, stats, w)
+    check_backward(dx, dw, db, dy, x, w, 1e-5)
+    _, dw2, db2 = sbc.sbc_layer_norm_grad(dy, x, stats, w, need_input=False)
+    assert torch.equal(dw, dw2) and torch.equal(db, db2)
