@@ -235,14 +235,29 @@ __device__ __forceinline__ void add_products(float* acc, const uint32_t (*w)[4],
 // An infinity's first term meets all terms of the other operand, and where one of those is zero the products' sum is a NaN that the
 // operands' product is not.  So what is a NaN is summed up again, by ordinary multiplications of whole operands, which says
 // whether it is one.  (Out of line: nothing of it costs what is finite more than the question.)
-template <typename X, typename Y> __device__ __forceinline__ float sum_again(int n, X x, Y y) {
-    float s = 0.f;
-    for (int k = 0; k < n && s == s; k += 8) {
+//
+// out[e] = first(e) + scale * sum over k < n of factor(k) row(k)[e], e < have; done once all of them are NaNs.
+template <typename O, typename F, typename R, typename B>
+__device__ __forceinline__ void sum_again(int n, F factor, R row, float scale, O* out, int have, B first) {
+    float s[8] = {};
+    bool open = true;
+    for (int k = 0; k < n && open; k += 4) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (k + i < n) s = fmaf(x(k + i), y(k + i), s);
+        for (int i = 0; i < 4; ++i) {
+            if (k + i >= n) break;
+            const float f = factor(k + i);
+            const auto* r = row(k + i);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e < have) s[e] = fmaf(f, to_float(r[e]), s[e]);
+        }
+        open = false;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) open |= e < have && s[e] == s[e];
     }
-    return s;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < have) out[e] = from_float<O>(fmaf(scale, s[e], first(e)));
 }
 // The value whose terms lie `plane` apart.
 __device__ __forceinline__ float joined(const uint16_t* terms, long long plane) {
@@ -252,22 +267,19 @@ __device__ __forceinline__ float joined(const uint16_t* terms, long long plane) 
     return v;
 }
 template <typename T, typename W> __device__ __noinline__ float into_again(const T* x, const W* factor, int wide) {
-    return sum_again(wide, [&](int k) { return to_float(x[k]); }, [&](int k) { return to_float(factor[k]); });
+    float s;
+    sum_again(wide, [&](int k) { return to_float(x[k]); }, [&](int k) { return factor + k; }, 1.f, &s, 1, [](int) { return 0.f; });
+    return s;
 }
 // (eight neighbours of a row, whose base is in `out`)
 template <typename T, typename W>
 __device__ __noinline__ void out_again(const uint16_t* mid, long long plane, const W* factor, int rank, int wide, float scale, T* out, int have) {
-    for (int e = 0; e < have; ++e) {
-        const float s = sum_again(rank, [&](int j) { return joined(mid + j, plane); }, [&](int j) { return to_float(factor[(long long)j * wide + e]); });
-        out[e] = from_float<T>(fmaf(scale, s, to_float(out[e])));
-    }
+    sum_again(rank, [&](int j) { return joined(mid + j, plane); }, [&](int j) { return factor + (long long)j * wide; }, scale, out, have, [&](int e) { return to_float(out[e]); });
 }
 template <typename T, typename W>
 __device__ __noinline__ void over_again(const uint16_t* mid, long long plane, int ranks, const T* x, long long x_stride, const int* order, int n, float scale, W* out, int have) {
-    for (int e = 0; e < have; ++e) {
-        const float s = sum_again(n, [&](int k) { return joined(mid + (long long)order[k] * ranks, plane); }, [&](int k) { return to_float(x[order[k] * x_stride + e]); });
-        out[e] = from_float<W>(s * scale);
-    }
+    sum_again(n, [&](int k) { return joined(mid + (long long)order[k] * ranks, plane); }, [&](int k) { return x + order[k] * x_stride; }, scale, out, have,
+              [](int) { return 0.f; });
 }
 
 // ---- packs in a thread's ring -----------------------------------------------------------
@@ -690,8 +702,9 @@ __global__ void __launch_bounds__(kAThreads, sizeof(T) == 2 && Terms<W>::n == 1 
                         bool again = false;
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
-                            f[e] = fmaf(a.scale, acc[m][e][2 * h + p], to_float(v.e[e]));
-                            again |= f[e] != f[e];
+                            const float sum = acc[m][e][2 * h + p];
+                            f[e] = fmaf(a.scale, sum, to_float(v.e[e]));
+                            again |= sum != sum;
                         }
                         if (again)
                             redo |= 1u << ((m * 2 + h) * 2 + p);   // (the base is left in its place)
