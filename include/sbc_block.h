@@ -135,7 +135,8 @@ int sbc_gated(const sbc_gated_weights *w, const void *x, int64_t tokens, int64_t
  * each rounded to the weights' type,
  *   dx    = dg gate + du up                       (tokens x inner, the weights' type)
  *   dgate = dg^T x,  dup = du^T x                 (hidden x inner, grad_dtype: SBC_F32 or the weights' type)
- * sums in 32 bits.  With no tokens, dgate and dup are zeros.
+ * sums in 32 bits.  (Float16 dg and du have that type's range: a loss is scaled for
+ * them as for dh.)  With no tokens, dgate and dup are zeros.
  *
  * kept   what sbc_gated left for the same x and w
  * dx, dgate and dup  each may be NULL (not all; dgate and dup both or neither, rows grad_stride apart)

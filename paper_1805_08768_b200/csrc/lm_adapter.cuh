@@ -8,9 +8,10 @@
 // What memory needs is x, base and y once: a rank of 16 is 16 to 32 operations for each byte of them, which warp-wide
 // products (16 x 8 x 16, 516 TFLOP/s) make several times over, without staging operands in the tensor cores' layouts.
 //
-// 8191 tokens of 12 requests and 8 adapters of rank 64, 4096 -> 8192 bfloat16, there and back 444 us: into the rank 38 and 67 us
-// (67 and 134 MB of x), out of it 97 and 57 (268 and 134 MB), both sums over tokens 175.  The instructions between the products bound
-// all three (LSU pipe 40 to 58 %, tensor pipe 20 to 33 %).
+// 8191 tokens of 12 requests and 8 adapters of rank 64, 4096 -> 8192 bfloat16, there and back 424 to 480 us (by the requests'
+// lengths): into the rank 41 and 67 us (67 and 134 MB of x), out of it 96 and 55 (268 and 134 MB), both sums over tokens 178.  The instructions between the products bound
+// the first two (LSU pipe 39 to 56 %, tensor pipe 19 to 33 %); the third's 192 blocks, one an SM, are a round and a third, and keep the tensor
+// pipe 55 % busy while they run.
 //
 // Operands go into the products as the bfloat16 terms that they are the sum of (one for bfloat16, two for float16, three for float32,
 // cut off rather than rounded, so that none overflows): n terms leave less than 2^(1 - 8 n) of a value.  mid and dmid are kept as three

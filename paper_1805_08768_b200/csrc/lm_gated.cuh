@@ -395,7 +395,7 @@ __global__ void __launch_bounds__(kMThreads, 1)
 // k's of two products.  The warps of a block share the units and cut the rows in turn; their sums
 // meet in shared memory in the warps' order.
 //
-// 16 tokens x 4096 -> 16384 bfloat16 54 us for 269 MB, 76 % of the copy rate; 1 x 650 -> 2600 6.0 us, latency.
+// 16 tokens x 4096 -> 16384 bfloat16 55 us for 269 MB, 74 % of the copy rate; 1 x 650 -> 2600 6.0 us, latency.
 
 constexpr int kFThreads = 256;
 constexpr int kFMost = 32;      // tokens
@@ -504,6 +504,10 @@ struct GateGradArgs {
 };
 
 // dg = dh P, du = dh Q.  Bound by memory: 14 bytes a unit (2 + 8 read, 4 written); 8192 x 8192 157 us, 6.0 TB/s.
+//
+// Both are rounded to the inputs' type, which is what the tensor cores take: the one rounding on the way, beside the results' own, so that the
+// gradients are off by 1.41 (the root of two) times what 32-bit factors would leave.  As two 16-bit terms each they would double the
+// backward products (1430 of 2790 us for 8192 x 4096 -> 8192).  float16 has its range, too: above 65504 they are infinities, as dh itself would be.
 template <typename T> __global__ void __launch_bounds__(kGThreads) k_gate_grad(GateGradArgs a) {
     after_earlier_kernels();
     const int groups = (a.cols + 7) / 8;

@@ -12,9 +12,12 @@
 // begin at the same place within 16 bytes (their distance is a multiple of eight rows), so an element's
 // column, weight and sum never change place.
 //
-// 16384 x 4096 bfloat16 (cold, the buffers before in the caches): forward 81 us for 268 MB, backward 90 us for 403 MB and 4 us for the
-// blocks' sums; 8191 x 2601 float16 forward 40 us for 85 MB.  Instructions bound both (about 30 an element), a quarter of them for the
-// sums over a row's threads.
+// 16384 x 4096 bfloat16 (cold, the buffers before in the caches): forward 79 us for 268 MB, backward 89 us for 403 MB and 7 us for the
+// blocks' sums; 8191 x 2601 float16 forward 40 us for 85 MB.  The latency of a row's steps bounds the forward pass: no load of the next
+// row runs under this one's sums and stores, and 15 warps an SM issue 22 to 32 instructions an element at half of the rate that
+// they could (DRAM at 14 to 34 % of its peak).  Backward, with the next row's loads ahead, 30 an element at 0.64 a cycle (DRAM 52 %).  Rows
+// above 8192 elements go through the long kernels, which keep no row: 4096 x 16384 bfloat16 252 us forward, 222 for the input's gradient, 704 with the
+// sums over rows, which are read and written in memory for every row.
 #pragma once
 
 #include <type_traits>
@@ -100,8 +103,7 @@ template <typename T> __device__ __forceinline__ int phase_of(const T* row) { re
 // Whole granules of one row are whole granules of the other's memory too (for all rows of a group, if for its first).
 __device__ __forceinline__ bool same_phase(const void* p, const void* q) { return ((uintptr_t)p - (uintptr_t)q) % 16 == 0; }
 
-// Arithmetic is on two neighbours at a time (one instruction does both): with sixteen elements of a row a thread, instructions
-// are what these kernels are short of before memory is.
+// Arithmetic is on two neighbours at a time: one instruction does both.
 typedef unsigned long long Two;
 __device__ __forceinline__ Two both(float v) { return pair(v, v); }
 template <typename T> __device__ __forceinline__ void as_pairs(Two* to, const Pack8<T>& v) {
@@ -155,7 +157,7 @@ __host__ __device__ constexpr bool whole_granules_within(long long r, long long 
     return !ends || (cols >= 8 && r > 0 && r < rows - 1);
 }
 
-// Few threads hold a row, each up to 64 elements of it, since sums over threads are what most instructions go into.  The weights
+// Few threads hold a row, each up to 64 elements of it: a sum over threads is a wait for all of them.  The weights
 // wait in shared memory as fours, so placed that a row's granules begin at them: all rows of a block begin at the same
 // place within 16 bytes.
 
@@ -223,6 +225,7 @@ template <typename T, int NV> __global__ void __maxnreg__(NV * sizeof(T) <= 8 ? 
 #pragma unroll
             for (int i = 0; i < 4; ++i) total = fma2(f[i], f[i], total);
         }
+        // (the fast root is off by 2^-22 of itself, in 16 bits less than a result's rounding, in 32 about as much as the sum under it)
         const float rstd = rsqrtf(group_sum(make_float2(sum_of(total), 0.f), red[1], warps).x * share + a.eps);
         if (r >= a.rows) continue;
         if (t == 0 && a.stats) a.stats[r] = make_float2(mean, rstd);
